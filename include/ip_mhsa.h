@@ -406,6 +406,50 @@ int ip_relpos_mhsa_i8_host_async(const int8_t *q, const int8_t *k, const int8_t 
 int ip_relpos_mhsa_host_status(const void *arena, int B, int H, int T, int dh,
                                ip_stream_t stream);
 
+/* ---- products with run-time scales -------------------------------------
+ *
+ * Where a tensor's range is not known before the call (a decoder's activations, a
+ * front end with outliers), each row (token) carries a scale found from its own
+ * values, beside the weights' scale per output channel (Sec. 2.2).  The sums stay
+ * exact integers; the scales are 32-bit floats. */
+#define IP_F32 0
+#define IP_F16 1
+#define IP_BF16 2
+
+/* Rows of real values to int8 with a scale each: for row r with amax = max |x|,
+ *   scale[r] = amax / 127 (f32, nearest),  q[r][i] = 127 x[r][i] / amax to the
+ * nearest integer, ties to even (both exactly as stated, whatever the type).
+ * amax = 0 gives scale 0 and q 0; a row that holds a NaN or an infinity gets the
+ * scale NaN and q 0 (a product with it is NaN).
+ * x: device, dtype IP_F32, IP_F16 or IP_BF16, rows of ldx >= d elements; q: device
+ * int8, rows of ldq >= d bytes (those behind column d are left as they were); scale:
+ * device f32 [rows].  d in [1, IP_LINEAR_MAX_K].  rows == 0 returns IP_OK without
+ * touching any pointer.  Asynchronous on `stream`.  The same call quantises weights
+ * by output channel.  Returns IP_OK or IP_ERR_*. */
+int ip_quantize_rows_i8(const void *x, int dtype, long long rows, int d, long long ldx, int8_t *q,
+                        long long ldq, float *scale, ip_stream_t stream);
+
+#define IP_ACT_NONE 0
+#define IP_ACT_SWISH 1
+
+/* y[m][n] = act(sx[m] sw[n] sum_k x[m][k] w[n][k] + bias[n]) for m < rows, n < N: the
+ * sum is exact (int32), the rest is in f32, rounded once to y's type.  act:
+ * IP_ACT_NONE, or IP_ACT_SWISH for z / (1 + exp(-z)).
+ * x: device int8, rows of ldx >= K bytes; w: device int8 [N], rows of ldw >= K bytes
+ * (one per output channel; any values, -128 included); x, w 16-byte aligned, ldx and
+ * ldw multiples of 16 (K itself may be any size; bytes behind column K are not used).
+ * sx: device f32 [rows]; sw: device f32 [N]; bias: device f32 [N] or NULL.
+ * y: device, dtype IP_F32, IP_F16 or IP_BF16, rows of ldy >= N elements (those behind
+ * column N are left as they were).
+ * rows <= IP_LINEAR_MAX_FRAMES, K in [1, IP_LINEAR_MAX_K], N in [1, IP_LINEAR_MAX_N].
+ * workspace as for ip_linear_i8 (256 bytes, its status word reports a timeout by
+ * ip_relpos_mhsa_status).  rows == 0 returns IP_OK without touching any pointer.
+ * Asynchronous on `stream`.  Returns IP_OK or IP_ERR_*. */
+int ip_linear_scaled_i8(const int8_t *x, long long ldx, const float *sx, const int8_t *w,
+                        long long ldw, const float *sw, const float *bias, int act, long long rows,
+                        int K, int N, void *y, long long ldy, int dtype, void *workspace,
+                        size_t workspace_bytes, ip_stream_t stream);
+
 /* Text of an IP_* code. */
 const char *ip_strerror(int code);
 

@@ -35,10 +35,13 @@ EXPORTS = (
     "ip_swish16_params_from_scales", "ip_relpos_mhsa_i8_host_async", "ip_relpos_mhsa_host_status",
     "ip_set_workspace", "ip_probe_int8_mix", "ip_linear_residual_i8",
     "ip_relpos_layer_constants", "ip_linear_constants", "ip_relpos_mhsa_noalloc_status",
+    "ip_quantize_rows_i8", "ip_linear_scaled_i8",
 )
 
 ROWS = 0    # IP_LAYOUT_ROWS:  [B][T][C]
 HEADS = 1   # IP_LAYOUT_HEADS: [G][B][C/G/128][T][128]
+ACT_NONE = 0    # IP_ACT_NONE
+ACT_SWISH = 1   # IP_ACT_SWISH: z / (1 + exp(-z))
 
 
 class LibraryError(RuntimeError):
@@ -169,6 +172,11 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         lib.ip_dwconv_swish_i8.restype = I
         lib.ip_swish16_params_from_scales.argtypes = [D, D, ctypes.POINTER(Swish16Params)]
         lib.ip_swish16_params_from_scales.restype = I
+        lib.ip_quantize_rows_i8.argtypes = [P, I, LL, I, LL, P, LL, P, P]
+        lib.ip_quantize_rows_i8.restype = I
+        lib.ip_linear_scaled_i8.argtypes = [P, LL, P, P, LL, P, P, I, LL, I, I, P, LL, I, P,
+                                            ctypes.c_size_t, P]
+        lib.ip_linear_scaled_i8.restype = I
         lib.ip_probe_int8_mma.argtypes = [I, I, P, P]
         lib.ip_probe_int8_mma.restype = ctypes.c_longlong
         lib.ip_probe_int8_mix.argtypes = [I, I, I, P, P]
@@ -666,6 +674,155 @@ def dwconv_swish_i8(x, w, bias, m, s, sw16: tuple[int, int, int, int], *, out=No
     return out
 
 
+# ------------------------------------------------------- run-time scales
+
+def _dtype_code(dtype, name="dtype"):
+    import torch
+    code = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}.get(dtype)
+    if code is None:
+        raise TypeError(f"{name} must be torch.float32, float16 or bfloat16, got {dtype}")
+    return code
+
+
+def _need(t, name, dtype=None, shape=None, device=None):
+    """Checks a CUDA tensor's type, shape and device; its strides are the caller's."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    return t
+
+
+def _dense(t, name, dtype, shape, device):
+    if not _need(t, name, dtype, shape, device).is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _as_rows(t, name):
+    """(rows, columns, row stride) of the last axis's rows; the leading axes must be
+    walked with one stride (a matrix, a contiguous tensor, column slices of either)."""
+    d = t.shape[-1] if t.dim() else 0
+    if t.dim() < 1 or d < 1:
+        raise ValueError(f"{name} needs a last axis of at least one element")
+    if t.stride(-1) != 1 and d > 1:
+        raise ValueError(f"{name}'s last axis must be contiguous")
+    rows, stride = 1, None
+    for size, st in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size != 1 and rows:
+            if stride is None:
+                stride = st
+            elif st != stride * rows:
+                raise ValueError(f"{name}'s rows must follow one another with one stride")
+        rows *= size
+    if stride is None:
+        stride = -(-d // 16) * 16      # one row (or none): any stride does
+    if stride < d:
+        raise ValueError(f"{name}'s rows must not overlap")
+    return rows, d, stride
+
+
+class _On:
+    """Makes `device` and `stream` (None: the device's current one) current, so that what
+    a call allocates belongs to the stream that uses it, and gives the raw handle."""
+
+    def __init__(self, device, stream):
+        import torch
+        if stream is not None and stream.device != device:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+        self.ctx = torch.cuda.stream(stream) if stream is not None else (
+            torch.cuda.device(device) if device.index != torch._C._cuda_getDevice() else None)
+
+    def __enter__(self):
+        import torch
+        if self.ctx is not None:
+            self.ctx.__enter__()
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+    def __exit__(self, *exc):
+        if self.ctx is not None:
+            self.ctx.__exit__(*exc)
+
+
+def _status_space(workspace, device, size=256):
+    """Pointer and bytes of the caller's workspace, or of a fresh zeroed one."""
+    import torch
+    if workspace is None:
+        workspace = torch.zeros(size, dtype=torch.uint8, device=device)
+    else:
+        _dense(workspace, "workspace", torch.uint8, (workspace.numel(),), device)
+    return workspace, workspace.data_ptr(), workspace.numel()
+
+
+def quantize_rows_i8(x, *, q=None, scale=None, stream=None):
+    """Rows (the last axis) of a float32, float16 or bfloat16 CUDA tensor to int8 with a
+    scale each: scale = amax / 127 (float32), q = 127 x / amax to the nearest integer,
+    ties to even.  A row of zeros gives scale 0; one with a NaN or an infinity the scale
+    NaN and q 0.  Returns (q, scale): int8 of x's shape and float32 of x.shape[:-1].  A
+    new q has rows of a multiple of 16 bytes, as linear_scaled_i8 reads them, so it
+    is a view of them where 16 does not divide the last axis.  Asynchronous on
+    `stream` (default: torch's current stream)."""
+    import torch
+    code = _dtype_code(_need(x, "x").dtype, "x")
+    rows, d, ldx = _as_rows(x, "x")
+    with _On(x.device, stream) as handle:
+        if q is None:
+            ldq = -(-d // 16) * 16
+            q = torch.empty((*x.shape[:-1], ldq), dtype=torch.int8, device=x.device)
+            q = q if ldq == d else q[..., :d]
+        else:
+            ldq = _as_rows(_need(q, "q", torch.int8, x.shape, x.device), "q")[2]
+        if scale is None:
+            scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+        rc = (_lib or load()).ip_quantize_rows_i8(
+            x.data_ptr(), code, rows, d, ldx, q.data_ptr(), ldq,
+            _dense(scale, "scale", torch.float32, x.shape[:-1], x.device), handle)
+    if rc:
+        _check("ip_quantize_rows_i8", rc)
+    return q, scale
+
+
+def linear_scaled_i8(x, sx, w, sw, bias=None, *, act: int = ACT_NONE, dtype=None, out=None,
+                     workspace=None, stream=None):
+    """Int8 matrix product with a scale per token and per channel:
+    out[..., n] = act(sx sw[n] sum_k x[..., k] w[n, k] + bias[n]), the sum exact, the rest
+    in float32.  x: int8 [..., K], sx: float32 [...] (quantize_rows_i8); w: int8 [N, K], sw:
+    float32 [N]; bias: float32 [N] or None; act: ACT_NONE or ACT_SWISH; all CUDA tensors.
+    K and N may be any size; the rows of x and w start on multiples of 16 bytes.
+    Returns out: [..., N] of `dtype` (bfloat16 unless out gives it).  Asynchronous on
+    `stream` (default: torch's current stream)."""
+    import torch
+    rows, K, ldx = _as_rows(_need(x, "x", torch.int8), "x")
+    if _need(w, "w", torch.int8, None, x.device).dim() != 2 or w.shape[1] != K:
+        raise ValueError(f"w must have shape (N, {K}), got {tuple(w.shape)}")
+    N, _, ldw = _as_rows(w, "w")
+    shape = (*x.shape[:-1], N)
+    if out is not None:
+        dtype = out.dtype if dtype is None else dtype
+        ldy = _as_rows(_need(out, "out", dtype, shape, x.device), "out")[2]
+    else:
+        dtype, ldy = dtype or torch.bfloat16, N
+    code = _dtype_code(dtype)
+    psx = _dense(sx, "sx", torch.float32, x.shape[:-1], x.device)
+    psw = _dense(sw, "sw", torch.float32, (N,), x.device)
+    pb = None if bias is None else _dense(bias, "bias", torch.float32, (N,), x.device)
+    with _On(x.device, stream) as handle:
+        if out is None:
+            out = torch.empty(shape, dtype=dtype, device=x.device)
+        workspace, ws, wsb = _status_space(workspace, x.device)
+        rc = (_lib or load()).ip_linear_scaled_i8(
+            x.data_ptr(), ldx, psx, w.data_ptr(), ldw, psw, pb, int(act), rows, K, N, out.data_ptr(),
+            ldy, code, ws, wsb, handle)
+    if rc:
+        _check("ip_linear_scaled_i8", rc)
+    return out
+
+
 def relpos_mhsa_i8_host(q, k, v, p, u, v_bias, consts: LayerConstants, lengths, out, arena,
                         stream=None, wait: bool = True):
     """Whole layer from host buffers (torch CPU tensors, ideally pinned):
@@ -709,4 +866,5 @@ __all__ = ["build", "load", "relpos_mhsa_i8", "relpos_mhsa_i8_host", "status", "
            "layernorm_i8", "layernorm_constants", "NormConstants", "residual_i8",
            "residual_params", "linear_glu_i8", "glu_params", "dwconv_swish_i8", "swish16_params",
            "host_status", "set_workspace", "int8_pipe_rates", "linear_residual_i8",
+           "quantize_rows_i8", "linear_scaled_i8", "ACT_NONE", "ACT_SWISH",
            "IpError", "LibraryError", "EXPORTS"]

@@ -1,0 +1,215 @@
+// Host side of the operators with run-time scales of the C ABI (include/ip_mhsa.h):
+// argument validation, tensor maps and launches.  Device code: ip_scaled_kernels.cuh.
+#include "ip_mhsa.h"
+#include "ip_scaled_kernels.cuh"
+#include "ip_host_util.h"
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <mutex>
+
+namespace {
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
+                                  const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+    static EncodeTiledFn fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000,
+                                             cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeTiledFn>(p);
+    });
+    return fn;
+}
+
+// int8 rows [rows][K] of `ld` bytes each, boxes of BK x box_rows, elements outside read
+// as zero (a K that BK does not divide, the rows behind the last).
+bool make_map(CUtensorMap *m, const void *base, int K, long long rows, long long ld, unsigned box_rows) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(K), static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld)};
+    const cuuint32_t box[2] = {ips::BK, box_rows};
+    const cuuint32_t estride[2] = {1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estride,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+std::mutex g_mu;
+int g_sms[64] = {0};
+
+int sm_count() {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    std::lock_guard<std::mutex> lock(g_mu);
+    if (g_sms[dev] == 0) {
+        int n = 0;
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+        g_sms[dev] = n;
+    }
+    return g_sms[dev];
+}
+
+size_t elem_size(int dtype) { return dtype == IP_F32 ? 4 : 2; }
+bool dtype_ok(int dtype) { return dtype == IP_F32 || dtype == IP_F16 || dtype == IP_BF16; }
+
+int launched(cudaError_t rc) {
+    return rc == cudaSuccess && cudaGetLastError() == cudaSuccess ? IP_OK : IP_ERR_CUDA;
+}
+
+template <typename T>
+int quantize(const ips::QuantParams &prm, int nsm, cudaStream_t st) {
+    // a warp a row while its lanes can hold the row, then four warps, then the CTA
+    const int tpr = prm.d <= 32 * 8 * ips::QUANT_UNITS ? 32 : (prm.d <= 128 * 8 * ips::QUANT_UNITS ? 128 : 256);
+    const int rpc = ips::QUANT_THREADS / tpr;
+    const long long need = (prm.rows + rpc - 1) / rpc, cap = 16ll * nsm;
+    const dim3 grid(static_cast<unsigned>(need < cap ? need : cap)), block(ips::QUANT_THREADS);
+    switch (tpr) {
+        case 32: return launched(iph::launch_pdl(ips::quantize_rows_kernel<T, 32>, grid, block, 0, st, prm));
+        case 128: return launched(iph::launch_pdl(ips::quantize_rows_kernel<T, 128>, grid, block, 0, st, prm));
+        default: return launched(iph::launch_pdl(ips::quantize_rows_kernel<T, 256>, grid, block, 0, st, prm));
+    }
+}
+
+// Up to this many tokens the weights are read by the vector kernel.
+constexpr long long VEC_TOKENS = 8;
+
+template <typename T, int MT, int CPT>
+int launch_vec(const ips::ScaledParams &prm, cudaStream_t st) {
+    const int per = ips::VEC_THREADS / ips::VEC_KT * CPT;
+    const dim3 grid(static_cast<unsigned>((prm.N + per - 1) / per), static_cast<unsigned>((prm.M + MT - 1) / MT));
+    return launched(iph::launch_pdl(ips::scaled_vec_kernel<T, MT, CPT>, grid, dim3(ips::VEC_THREADS), 0, st, prm));
+}
+
+template <typename T, int MT>
+int launch_vec_m(const ips::ScaledParams &prm, int nsm, cudaStream_t st) {
+    // the most channels a CTA for which every SM still gets two CTAs
+    if (prm.N >= 2 * nsm * 16) return launch_vec<T, MT, 4>(prm, st);
+    if (prm.N >= 2 * nsm * 8) return launch_vec<T, MT, 2>(prm, st);
+    return launch_vec<T, MT, 1>(prm, st);
+}
+
+template <typename T, int BN, bool LONG>
+int launch_tc(const CUtensorMap &tx, const CUtensorMap &tw, const ips::ScaledParams &prm, int nsm,
+              cudaStream_t st) {
+    static bool set[64] = {false};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return IP_ERR_CUDA;
+    auto *fn = ips::scaled_tc_kernel<T, BN, LONG>;
+    {
+        std::lock_guard<std::mutex> lock(g_mu);
+        if (!set[dev]) {
+            if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, ips::Tile<BN>::SMEM) !=
+                cudaSuccess)
+                return IP_ERR_CUDA;
+            set[dev] = true;
+        }
+    }
+    const unsigned grid = static_cast<unsigned>(prm.tiles < nsm ? prm.tiles : nsm);
+    return launched(iph::launch_pdl(fn, dim3(grid), dim3(ips::TC_THREADS), ips::Tile<BN>::SMEM, st, tx, tw, prm));
+}
+
+template <typename T, int BN>
+int run_tc(ips::ScaledParams prm, int nsm, cudaStream_t st) {
+    CUtensorMap tx, tw;
+    if (!make_map(&tx, prm.x, prm.K, prm.M, prm.ldx, ips::TILE_M) ||
+        !make_map(&tw, prm.w, prm.K, prm.N, prm.ldw, BN))
+        return IP_ERR_CUDA;
+    prm.tiles_n = (prm.N + BN - 1) / BN;
+    prm.tiles = (prm.M + ips::TILE_M - 1) / ips::TILE_M * prm.tiles_n;
+    // the sums of several segments take BN / 2 registers of an epilogue thread
+    if constexpr (BN <= 128)
+        if (prm.K > ips::SEG * ips::BK) return launch_tc<T, BN, true>(tx, tw, prm, nsm, st);
+    return launch_tc<T, BN, false>(tx, tw, prm, nsm, st);
+}
+
+template <typename T>
+int run_scaled(const ips::ScaledParams &prm, int nsm, cudaStream_t st) {
+    if (prm.M <= VEC_TOKENS) {
+        if (prm.M == 1) return launch_vec_m<T, 1>(prm, nsm, st);
+        if (prm.M == 2) return launch_vec_m<T, 2>(prm, nsm, st);
+        if (prm.M <= 4) return launch_vec_m<T, 4>(prm, nsm, st);
+        return launch_vec_m<T, 8>(prm, nsm, st);
+    }
+    const long long tm = (prm.M + ips::TILE_M - 1) / ips::TILE_M;
+    if (prm.K <= ips::SEG * ips::BK && tm * ((prm.N + 255) / 256) >= nsm)
+        return run_tc<T, 256>(prm, nsm, st);
+    if (tm * ((prm.N + 127) / 128) >= nsm) return run_tc<T, 128>(prm, nsm, st);
+    return run_tc<T, 32>(prm, nsm, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+int ip_quantize_rows_i8(const void *x, int dtype, long long rows, int d, long long ldx, int8_t *q,
+                        long long ldq, float *scale, ip_stream_t stream) {
+    if (!dtype_ok(dtype)) return IP_ERR_PARAM;
+    if (rows < 0 || rows > IP_NORM_MAX_ROWS || d < 1 || d > IP_LINEAR_MAX_K) return IP_ERR_SHAPE;
+    if (ldx < d || ldq < d) return IP_ERR_SHAPE;
+    if (rows == 0) return IP_OK;
+    if (!x || !q || !scale) return IP_ERR_NULL;
+    if (!aligned(x, elem_size(dtype)) || !aligned(scale, 4)) return IP_ERR_ALIGN;
+    const int nsm = sm_count();
+    if (nsm <= 0) return IP_ERR_CUDA;
+    const ips::QuantParams prm{x, rows, ldx, ldq, d, q, scale};
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (dtype == IP_F32) return quantize<float>(prm, nsm, st);
+    if (dtype == IP_F16) return quantize<__half>(prm, nsm, st);
+    return quantize<__nv_bfloat16>(prm, nsm, st);
+}
+
+int ip_linear_scaled_i8(const int8_t *x, long long ldx, const float *sx, const int8_t *w,
+                        long long ldw, const float *sw, const float *bias, int act, long long rows,
+                        int K, int N, void *y, long long ldy, int dtype, void *workspace,
+                        size_t workspace_bytes, ip_stream_t stream) {
+    if (!dtype_ok(dtype) || (act != IP_ACT_NONE && act != IP_ACT_SWISH)) return IP_ERR_PARAM;
+    if (rows < 0 || rows > IP_LINEAR_MAX_FRAMES || K < 1 || K > IP_LINEAR_MAX_K || N < 1 ||
+        N > IP_LINEAR_MAX_N || ldx < K || ldw < K || ldy < N || ldx > (1ll << 40) || ldw > (1ll << 40) ||
+        ldy > (1ll << 31))
+        return IP_ERR_SHAPE;
+    if (rows == 0) return IP_OK;
+    if (!x || !sx || !w || !sw || !y || !workspace) return IP_ERR_NULL;
+    if (!aligned(x, 16) || !aligned(w, 16) || ldx % 16 != 0 || ldw % 16 != 0 || !aligned(sx, 4) ||
+        !aligned(sw, 4) || (bias && !aligned(bias, 4)) || !aligned(y, elem_size(dtype)) ||
+        !aligned(workspace, 256))
+        return IP_ERR_ALIGN;
+    if (workspace_bytes < 256) return IP_ERR_WORKSPACE;
+    const int nsm = sm_count();
+    if (nsm <= 0) return IP_ERR_CUDA;
+    ips::ScaledParams prm;
+    prm.x = x;
+    prm.w = w;
+    prm.sx = sx;
+    prm.sw = sw;
+    prm.bias = bias;
+    prm.y = y;
+    prm.M = rows;
+    prm.ldx = ldx;
+    prm.ldw = ldw;
+    prm.ldy = ldy;
+    prm.K = K;
+    prm.N = N;
+    prm.act = act;
+    prm.tiles_n = 0;
+    prm.tiles = 0;
+    prm.err = static_cast<int *>(workspace);
+    prm.timeout_cycles = 4000000000ll;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (dtype == IP_F32) return run_scaled<float>(prm, nsm, st);
+    if (dtype == IP_F16) return run_scaled<__half>(prm, nsm, st);
+    return run_scaled<__nv_bfloat16>(prm, nsm, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,642 @@
+// Device code of the operators with run-time scales for sm_103a: rows quantised to
+// int8 with one scale each, and the int8 matrix product with a scale per row of X
+// (token) and per row of W (channel).  Floating point holds the scales and, in the
+// tensor-core kernel, integers that it represents exactly.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include "ip_ptx.cuh"
+
+namespace ips {
+
+using namespace ipk;
+
+// ---- element types ------------------------------------------------------
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+template <typename T> __device__ __forceinline__ T from_f32(float x);
+template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) {
+    return __float2bfloat16_rn(x);
+}
+
+// Eight consecutive elements as floats; `vec`: p is 16-byte aligned.
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, bool vec, int n, float (&v)[8]) {
+    if (vec && n >= 8) {
+        constexpr int W = 16 / sizeof(T);
+#pragma unroll
+        for (int i = 0; i < 8 / W; ++i) {
+            const uint4 w = *reinterpret_cast<const uint4 *>(p + i * W);
+            const T *e = reinterpret_cast<const T *>(&w);
+#pragma unroll
+            for (int j = 0; j < W; ++j) v[i * W + j] = to_f32(e[j]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f32(p[i]) : 0.0f;
+    }
+}
+
+// ---- rows to int8 -------------------------------------------------------
+//
+// scale = amax / 127 rounded to f32 and q = the integer nearest to 127 x / amax, ties
+// to even, for the row's largest magnitude amax.  The quotient is formed as x times
+// the rounded reciprocal (error below 127 2^-22 = 2^-15); within 2^-12 of a half
+// integer n + 1/2 the exact sign of 254 |x| - (2n + 1) amax decides: both products
+// as unevaluated sums of two floats, whose leading parts differ by little there (an
+// exact subtraction) and whose errors have eight bits.  A power of two brings amax to
+// [1, 4) first, so that nothing of this overflows or underflows.  amax = 0: scale
+// and q are 0.  A NaN or an infinity in the row: the scale is NaN and q is 0, so
+// that a product with the row is NaN and not a plausible number.
+//
+// What bounds it: DRAM.  A row stays in registers between the two passes up to
+// 8 UNITS elements a thread; a longer one is read again (from L2).
+
+constexpr int QUANT_THREADS = 256;
+constexpr int QUANT_UNITS = 4;      // units of eight elements that a thread keeps
+
+struct QuantParams {
+    const void *x;
+    long long rows, ldx, ldq;
+    int d;
+    int8_t *q;
+    float *scale;
+};
+
+__device__ __forceinline__ int quant_one(float x, float inv, float top) {
+    const float y = x * inv;
+    int r = __float2int_rn(y);
+    const float a = fabsf(y), n = rintf(a - 0.5f);
+    if (fabsf(a - 0.5f - n) < 0x1p-12f) {
+        const float ax = fabsf(x), odd = 2.0f * n + 1.0f;
+        const float p1 = 254.0f * ax, e1 = __fmaf_rn(254.0f, ax, -p1);
+        const float p2 = odd * top, e2 = __fmaf_rn(odd, top, -p2);
+        const float diff = __fadd_rn(__fsub_rn(p1, p2), __fsub_rn(e1, e2));
+        const int ni = static_cast<int>(n);
+        int m = diff > 0.0f ? ni + 1 : (diff < 0.0f ? ni : ni + (ni & 1));
+        m = m < 0 ? 0 : m;
+        r = x < 0.0f ? -m : m;
+    }
+    return max(-127, min(127, r));
+}
+
+// TPR threads a row (32, 128 or 256).
+template <typename T, int TPR>
+__global__ void __launch_bounds__(QUANT_THREADS) quantize_rows_kernel(const QuantParams prm) {
+    constexpr int RPC = QUANT_THREADS / TPR;
+    __shared__ unsigned red[QUANT_THREADS / 32];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+    const int d = prm.d;
+    for (long long r0 = static_cast<long long>(blockIdx.x) * RPC; r0 < prm.rows;
+         r0 += static_cast<long long>(gridDim.x) * RPC) {
+        const long long row = r0 + sub;
+        const bool live = row < prm.rows;
+        const T *x = static_cast<const T *>(prm.x) + (live ? row : 0) * prm.ldx;
+        const bool vec = (reinterpret_cast<uintptr_t>(x) & 15) == 0;
+        float v[QUANT_UNITS][8];
+        unsigned top = 0;   // largest magnitude as bits: a NaN exceeds an infinity
+#pragma unroll
+        for (int i = 0; i < QUANT_UNITS; ++i) {
+            const int c = (i * TPR + t) * 8;
+            if (live && c < d) load8(x + c, vec, d - c, v[i]);
+            else
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < QUANT_UNITS; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[i][j]) & 0x7fffffffu);
+        if (live)
+            for (int c = (QUANT_UNITS * TPR + t) * 8; c < d; c += TPR * 8) {
+                float w[8];
+                load8(x + c, vec, d - c, w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(w[j]) & 0x7fffffffu);
+            }
+        top = __reduce_max_sync(0xffffffffu, top);
+        if (TPR > 32) {
+            __syncthreads();
+            if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = top;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < TPR / 32; ++i) top = max(top, red[sub * (TPR / 32) + i]);
+        }
+        if (!live) continue;   // no thread of the row's group is live, all meet at the next row
+        const bool finite = top < 0x7f800000u;
+        const float amax = __uint_as_float(top);
+        if (t == 0) prm.scale[row] = finite ? __fdiv_rn(amax, 127.0f) : __uint_as_float(0x7fc00000u);
+        // 2^(127 - e) for an amax of exponent field e, kept a normal number
+        const int e = static_cast<int>(top >> 23);
+        const int fe = 254 - e < 1 ? 1 : (254 - e > 253 ? 253 : 254 - e);
+        const float f = __uint_as_float(static_cast<unsigned>(fe) << 23);
+        const float ntop = amax * f;
+        const bool zero = !finite || top == 0;
+        const float inv = zero ? 0.0f : __fdiv_rn(127.0f, ntop);
+        int8_t *q = prm.q + row * prm.ldq;
+        const bool qvec = (reinterpret_cast<uintptr_t>(q) & 7) == 0;
+        auto put = [&](int c, const float (&w)[8]) {
+            int k[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) k[j] = zero ? 0 : quant_one(w[j] * f, inv, ntop);
+            if (qvec && c + 8 <= d) {
+                *reinterpret_cast<uint2 *>(q + c) =
+                    make_uint2(pack_sat4(k[0], k[1], k[2], k[3]), pack_sat4(k[4], k[5], k[6], k[7]));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c + j < d) q[c + j] = static_cast<int8_t>(k[j]);
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < QUANT_UNITS; ++i) {
+            const int c = (i * TPR + t) * 8;
+            if (c < d) put(c, v[i]);
+        }
+        for (int c = (QUANT_UNITS * TPR + t) * 8; c < d; c += TPR * 8) {
+            float w[8];
+            load8(x + c, vec, d - c, w);
+            put(c, w);
+        }
+    }
+}
+
+// ---- the scaled product -------------------------------------------------
+//
+// y[m][n] = act(sx[m] sw[n] S + bias[n]), S = sum_k x[m][k] w[n][k] as an exact
+// integer, act the identity or z / (1 + exp(-z)).
+
+constexpr int ERR_TIMEOUT = 1;      // status word: a barrier wait ran out
+
+struct ScaledParams {
+    const int8_t *x, *w;            // the vector kernel's operands (the tiles come by TMA)
+    const float *sx, *sw, *bias;
+    void *y;
+    long long M, ldx, ldw, ldy;
+    int K, N, act;
+    int tiles_n;
+    long long tiles;
+    int *err;
+    long long timeout_cycles;
+};
+
+template <typename T>
+__device__ __forceinline__ float finish(float s, float scale, float bias, int act) {
+    float z = __fmaf_rn(s, scale, bias);
+    if (act) z = sizeof(T) == 4 ? __fdiv_rn(z, 1.0f + expf(-z)) : __fdividef(z, 1.0f + __expf(-z));
+    return z;
+}
+
+// Few tokens: the weights are read once and the products formed by dp4a.  A CTA takes
+// 4 CPT channels; 64 threads share a channel's K in chunks of 16 bytes, so that a
+// warp reads 512 consecutive bytes of a weight row at a time and each chunk of x is
+// loaded once for CPT channels.  Bound by the weights' bytes.
+constexpr int VEC_THREADS = 256;
+constexpr int VEC_KT = 64;
+
+__device__ __forceinline__ uint4 chunk16(const int8_t *p, int n) {
+    if (n >= 16) return *reinterpret_cast<const uint4 *>(p);
+    uint32_t w[4] = {0, 0, 0, 0};
+    for (int i = 0; i < n; ++i)
+        w[i >> 2] |= static_cast<uint32_t>(static_cast<uint8_t>(p[i])) << (8 * (i & 3));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <typename T, int MT, int CPT>
+__global__ void __launch_bounds__(VEC_THREADS) scaled_vec_kernel(const ScaledParams prm) {
+    constexpr int GROUPS = VEC_THREADS / VEC_KT;
+    __shared__ int part[GROUPS][2][MT * CPT];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int t = threadIdx.x % VEC_KT, g = threadIdx.x / VEC_KT;
+    const long long m0 = static_cast<long long>(blockIdx.y) * MT;
+    const int n0 = (static_cast<int>(blockIdx.x) * GROUPS + g) * CPT;
+    const int mv = static_cast<int>(prm.M - m0 < MT ? prm.M - m0 : MT);
+    int acc[MT][CPT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < CPT; ++j) acc[i][j] = 0;
+#pragma unroll 2
+    for (int k = t * 16; k < prm.K; k += VEC_KT * 16) {
+        uint4 w[CPT];
+#pragma unroll
+        for (int j = 0; j < CPT; ++j)
+            w[j] = n0 + j < prm.N ? chunk16(prm.w + (n0 + j) * prm.ldw + k, prm.K - k)
+                                  : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            if (i >= mv) continue;
+            const uint4 x = chunk16(prm.x + (m0 + i) * prm.ldx + k, prm.K - k);
+#pragma unroll
+            for (int j = 0; j < CPT; ++j) {
+                int a = acc[i][j];
+                a = __dp4a(static_cast<int>(x.x), static_cast<int>(w[j].x), a);
+                a = __dp4a(static_cast<int>(x.y), static_cast<int>(w[j].y), a);
+                a = __dp4a(static_cast<int>(x.z), static_cast<int>(w[j].z), a);
+                acc[i][j] = __dp4a(static_cast<int>(x.w), static_cast<int>(w[j].w), a);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < CPT; ++j) {
+            const int s = __reduce_add_sync(0xffffffffu, acc[i][j]);
+            if ((threadIdx.x & 31) == 0) part[g][t >> 5][i * CPT + j] = s;
+        }
+    __syncthreads();
+    // consecutive threads finish consecutive channels of a token
+    for (int e = threadIdx.x; e < GROUPS * MT * CPT; e += VEC_THREADS) {
+        const int i = e / (GROUPS * CPT), c = e % (GROUPS * CPT);
+        const int n = static_cast<int>(blockIdx.x) * GROUPS * CPT + c;
+        if (i >= mv || n >= prm.N) continue;
+        const int at = i * CPT + c % CPT;
+        const int s = part[c / CPT][0][at] + part[c / CPT][1][at];
+        const float z = finish<T>(static_cast<float>(s), prm.sx[m0 + i] * prm.sw[n],
+                                  prm.bias ? prm.bias[n] : 0.0f, prm.act);
+        static_cast<T *>(prm.y)[(m0 + i) * prm.ldy + n] = from_f32<T>(z);
+    }
+}
+
+// Many tokens: tiles of 128 tokens x BN channels on the fp16 tensor cores.
+//
+// sm_103a has no integer tcgen05 kind, and its integer warp MMA and dp4a together
+// reach 289 TOPS; but fp16 holds every int8 value, the product of two is exact in the
+// fp32 accumulator, and so is every partial sum below 2^24: at most 1024 products of
+// magnitude 2^14.  So the K axis runs in segments of 1024, each summed exactly in
+// TMEM, and the segments are added as int32 in registers.
+//
+// Roles of a persistent CTA (one per SM): warp 16 fetches stages of 64 K bytes of
+// both operands by TMA, warps 8-15 convert them to fp16 in the 128-byte swizzled
+// K-major layout of the MMA, one thread of warp 17 issues tcgen05.mma, warps 0-7
+// drain one of two TMEM accumulators and write the output while the other fills.
+
+constexpr int TILE_M = 128;
+constexpr int BK = 64;              // K elements per stage
+constexpr int SEG = 1024 / BK;      // stages of an exact segment
+constexpr int TC_THREADS = 640;     // five warpgroups (registers are dealt by warpgroup)
+constexpr int EPI_WARPS = 8, CONV_WARPS = 8;
+constexpr int TMA_WARP = 16, MMA_WARP = 17;
+
+template <int BN_>
+struct Tile {
+    static constexpr int BN = BN_;
+    static constexpr int RAW = (TILE_M + BN) * BK;
+    static constexpr int F16 = RAW * 2;
+    static constexpr int RS = BN == 256 ? 3 : 4;      // raw stages
+    static constexpr int FS = BN == 256 ? 3 : 4;      // fp16 stages
+    static constexpr int BARS = 0;                    // 2 RS + 2 FS + 5 barriers
+    static constexpr int TMEM_PTR = 256, DEAD = 260;
+    static constexpr int CONSTS = 512;                // per epilogue warp: sw and bias of its columns
+    static constexpr int F16_AT = (CONSTS + EPI_WARPS * 2 * 4 * (BN / 2) + 1023) & ~1023;
+    static constexpr int RAW_AT = F16_AT + FS * F16;
+    static constexpr int SMEM = RAW_AT + RS * RAW + 1024;
+    static constexpr int COLS = 2 * BN;               // TMEM columns
+    static_assert(8 * (2 * RS + 2 * FS + 5) <= 256, "barriers");
+    static_assert(SMEM <= 232448, "shared memory");
+    static_assert((COLS & (COLS - 1)) == 0 && COLS <= 512, "TMEM columns");
+};
+
+// Four int8 values to fp16 pairs, exactly: with its sign bit flipped a byte is u = b +
+// 128, and 0x6400 | u is the fp16 number 1024 + u.
+__device__ __forceinline__ void cvt4(uint32_t w, uint32_t &lo, uint32_t &hi) {
+    const uint32_t u = w ^ 0x80808080u;
+    uint32_t a, b;
+    asm("prmt.b32 %0, %1, %2, 0x4140;" : "=r"(a) : "r"(u), "r"(0x64646464u));
+    asm("prmt.b32 %0, %1, %2, 0x4342;" : "=r"(b) : "r"(u), "r"(0x64646464u));
+    const uint32_t c = 0xe480e480u;   // -1152
+    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(lo) : "r"(a), "r"(c));
+    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(hi) : "r"(b), "r"(c));
+}
+
+// Bounded wait that also ends when another role of the CTA has given up.
+__device__ __forceinline__ bool wait_or_dead(uint32_t bar, uint32_t parity, volatile int *dead,
+                                             long long limit) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+    while (!mbar_try_wait(bar, parity)) {
+        if (*dead) return false;
+        if (clock64() - t0 > limit) {
+            *dead = 1;
+            return false;
+        }
+    }
+    return true;
+}
+__device__ __forceinline__ bool warp_wait_or_dead(uint32_t bar, uint32_t parity, volatile int *dead,
+                                                  long long limit) {
+    return __all_sync(0xffffffffu, wait_or_dead(bar, parity, dead, limit)) != 0;
+}
+
+// Shared-memory descriptor of a K-major operand with 128-byte swizzle: rows of 128
+// bytes, groups of eight rows 1024 bytes apart.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr) {
+    return static_cast<uint64_t>((addr & 0x3ffff) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) |
+           (2ull << 61);
+}
+
+__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
+                                        uint32_t accumulate) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15},"
+        " [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]),
+          "=r"(r[15])
+        : "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+// 16 outputs of one token from column n on.
+template <typename T>
+__device__ __forceinline__ void store16(T *row, int n, int N, bool vec, const float (&z)[16]) {
+    if (vec && n + 16 <= N) {
+        constexpr int W = 16 / sizeof(T);
+#pragma unroll
+        for (int i = 0; i < 16 / W; ++i) {
+            T v[W];
+#pragma unroll
+            for (int j = 0; j < W; ++j) v[j] = from_f32<T>(z[i * W + j]);
+            *reinterpret_cast<uint4 *>(row + n + i * W) = *reinterpret_cast<const uint4 *>(v);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (n + j < N) row[n + j] = from_f32<T>(z[j]);
+    }
+}
+
+// LONG: K > 1024, several segments per tile.
+template <typename T, int BN, bool LONG>
+__global__ void __launch_bounds__(TC_THREADS, 1)
+    scaled_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w,
+                     const ScaledParams prm) {
+    using C = Tile<BN>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>(
+        (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    const uint32_t base = smem_u32(smem);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    auto raw_full = [&](int s) { return base + C::BARS + 8u * s; };
+    auto raw_empty = [&](int s) { return base + C::BARS + 8u * (C::RS + s); };
+    auto f16_full = [&](int s) { return base + C::BARS + 8u * (2 * C::RS + s); };
+    auto f16_empty = [&](int s) { return base + C::BARS + 8u * (2 * C::RS + C::FS + s); };
+    auto acc_full = [&](int s) { return base + C::BARS + 8u * (2 * C::RS + 2 * C::FS + s); };
+    auto acc_empty = [&](int s) { return base + C::BARS + 8u * (2 * C::RS + 2 * C::FS + 2 + s); };
+    const uint32_t drained = base + C::BARS + 8u * (2 * C::RS + 2 * C::FS + 4);
+    volatile int *dead = reinterpret_cast<volatile int *>(smem + C::DEAD);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::RS; ++s) {
+            mbar_init(raw_full(s), 1);
+            mbar_init(raw_empty(s), CONV_WARPS);
+        }
+        for (int s = 0; s < C::FS; ++s) {
+            mbar_init(f16_full(s), CONV_WARPS);
+            mbar_init(f16_empty(s), 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(acc_full(s), 1);
+            mbar_init(acc_empty(s), EPI_WARPS);
+        }
+        mbar_init(drained, 1);
+        *dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == MMA_WARP) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                         base + C::TMEM_PTR),
+                     "r"(C::COLS)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    // only now: a CTA of the next launch that took this SM's TMEM first would wait for
+    // this grid with it
+    pdl_launch_dependents();
+    const uint32_t tmem = lds32(base + C::TMEM_PTR);
+    pdl_wait();
+
+    const int stages = (prm.K + BK - 1) / BK;
+    const long long limit = prm.timeout_cycles;
+
+    if (warp == TMA_WARP) {
+        if (lane == 0) {
+            int s = 0, ph = 0;
+            long long issued = 0;
+            bool ok = true;
+            for (long long tile = blockIdx.x; ok && tile < prm.tiles; tile += gridDim.x) {
+                const int m0 = static_cast<int>(tile / prm.tiles_n) * TILE_M;
+                const int n0 = static_cast<int>(tile % prm.tiles_n) * BN;
+                for (int it = 0; it < stages; ++it) {
+                    ok = wait_or_dead(raw_empty(s), ph ^ 1, dead, limit);
+                    if (!ok) break;
+                    const uint32_t st = base + C::RAW_AT + s * C::RAW;
+                    mbar_expect_tx(raw_full(s), C::RAW);
+                    tma_load_2d(st, &tm_x, it * BK, m0, raw_full(s));
+                    tma_load_2d(st + TILE_M * BK, &tm_w, it * BK, n0, raw_full(s));
+                    ++issued;
+                    if (++s == C::RS) s = 0, ph ^= 1;
+                }
+            }
+            // after a wait that ran out: the copies in flight land before the CTA ends
+            if (!ok)
+                for (long long i = issued > C::RS ? issued - C::RS : 0; i < issued; ++i)
+                    mbar_wait(raw_full(static_cast<int>(i % C::RS)),
+                              static_cast<uint32_t>((i / C::RS) & 1), limit);
+        }
+    } else if (warp == MMA_WARP) {
+        if (lane == 0) {
+            constexpr uint32_t idesc = (1u << 4) | (static_cast<uint32_t>(BN / 8) << 17) |
+                                       (static_cast<uint32_t>(TILE_M / 16) << 24);
+            int s = 0, ph = 0, a = 0, aph = 0;
+            bool ok = true;
+            for (long long tile = blockIdx.x; ok && tile < prm.tiles; tile += gridDim.x) {
+                for (int it = 0; ok && it < stages;) {
+                    ok = wait_or_dead(acc_empty(a), aph ^ 1, dead, limit);
+                    if (!ok) break;
+                    const int end = it + SEG < stages ? it + SEG : stages;
+                    for (int first = it; it < end; ++it) {
+                        ok = wait_or_dead(f16_full(s), ph, dead, limit);
+                        if (!ok) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint32_t st = base + C::F16_AT + s * C::F16;
+                        const uint64_t da = smem_desc(st), db = smem_desc(st + TILE_M * BK * 2);
+#pragma unroll
+                        for (int k = 0; k < BK / 16; ++k)
+                            mma_f16(tmem + a * BN, da + 2 * k, db + 2 * k, idesc, it > first || k > 0);
+                        mma_commit(f16_empty(s));
+                        if (++s == C::FS) s = 0, ph ^= 1;
+                    }
+                    if (!ok) break;
+                    mma_commit(acc_full(a));
+                    a ^= 1;
+                    aph ^= a == 0;
+                }
+            }
+            if (!ok) {   // the MMAs in flight end before their TMEM is freed
+                mma_commit(drained);
+                mbar_wait(drained, 0, limit);
+            }
+        }
+    } else if (warp >= EPI_WARPS && warp < EPI_WARPS + CONV_WARPS) {
+        constexpr int UNITS = (TILE_M + BN) / 8;   // of eight rows
+        const int cw = warp - EPI_WARPS;
+        const int r8 = lane >> 2, j = lane & 3;
+        // byte offsets of this lane's chunk in eight raw rows and of its two fp16 chunks
+        const uint32_t src = static_cast<uint32_t>(lane * 16);
+        const uint32_t d0 = swz(r8, 2 * j), d1 = swz(r8, 2 * j + 1);
+        int rs = 0, rph = 0, fs = 0, fph = 0;
+        bool ok = true;
+        for (long long tile = blockIdx.x; ok && tile < prm.tiles; tile += gridDim.x) {
+            const long long m0 = tile / prm.tiles_n * TILE_M;
+            const int n0 = static_cast<int>(tile % prm.tiles_n) * BN;
+            // groups of eight rows that hold anything (rows past the end feed outputs that
+            // are not written)
+            const int ma = static_cast<int>(prm.M - m0 < TILE_M ? (prm.M - m0 + 7) / 8 : TILE_M / 8);
+            const int nb = prm.N - n0 < BN ? (prm.N - n0 + 7) / 8 : BN / 8;
+            for (int it = 0; it < stages; ++it) {
+                ok = warp_wait_or_dead(raw_full(rs), rph, dead, limit) &&
+                     warp_wait_or_dead(f16_empty(fs), fph ^ 1, dead, limit);
+                if (!ok) break;
+                const uint32_t raw = base + C::RAW_AT + rs * C::RAW, dst = base + C::F16_AT + fs * C::F16;
+#pragma unroll
+                for (int i = 0; i < (UNITS + CONV_WARPS - 1) / CONV_WARPS; ++i) {
+                    const int u = i * CONV_WARPS + cw;
+                    if (UNITS % CONV_WARPS != 0 && u >= UNITS) continue;
+                    if (u < TILE_M / 8 ? u >= ma : u - TILE_M / 8 >= nb) continue;
+                    const uint4 v = lds128(raw + u * 512 + src);
+                    uint32_t h[8];
+                    cvt4(v.x, h[0], h[1]);
+                    cvt4(v.y, h[2], h[3]);
+                    cvt4(v.z, h[4], h[5]);
+                    cvt4(v.w, h[6], h[7]);
+                    sts128(dst + u * 1024 + d0, h[0], h[1], h[2], h[3]);
+                    sts128(dst + u * 1024 + d1, h[4], h[5], h[6], h[7]);
+                }
+                // the fp16 stage to the MMA, the raw stage to the next TMA copy
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(f16_full(fs));
+                    mbar_arrive(raw_empty(rs));
+                }
+                if (++rs == C::RS) rs = 0, rph ^= 1;
+                if (++fs == C::FS) fs = 0, fph ^= 1;
+            }
+        }
+    } else if (warp < EPI_WARPS) {
+        const int quarter = warp & 3, half = warp >> 2;
+        constexpr int CW = BN / 2;            // columns of a warp
+        constexpr int CH = CW < 16 ? 1 : CW / 16;
+        const int col0 = half * CW;
+        const bool vec = ((reinterpret_cast<uintptr_t>(prm.y) | (static_cast<uintptr_t>(prm.ldy) * sizeof(T))) &
+                          15) == 0;
+        const uint32_t cst = base + C::CONSTS + warp * (8 * CW);
+        int a = 0, aph = 0;
+        bool ok = true;
+        for (long long tile = blockIdx.x; ok && tile < prm.tiles; tile += gridDim.x) {
+            const long long m = tile / prm.tiles_n * TILE_M + quarter * 32 + lane;
+            const int n0 = static_cast<int>(tile % prm.tiles_n) * BN + col0;
+            __syncwarp();
+            for (int c = lane; c < CW; c += 32) {
+                const int n = n0 + c;
+                sts32(cst + 4 * c, __float_as_uint(n < prm.N ? prm.sw[n] : 0.0f));
+                sts32(cst + 4 * (CW + c), __float_as_uint(n < prm.N && prm.bias ? prm.bias[n] : 0.0f));
+            }
+            __syncwarp();
+            const float sx = m < prm.M ? prm.sx[m] : 0.0f;
+            T *row = static_cast<T *>(prm.y) + (m < prm.M ? m : 0) * prm.ldy;
+            auto write = [&](int c, const float (&s)[16]) {
+                float z[16];
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const uint4 w4 = lds128(cst + 4 * (c + i));
+                    const uint4 b4 = lds128(cst + 4 * (CW + c + i));
+                    z[i] = finish<T>(s[i], sx * __uint_as_float(w4.x), __uint_as_float(b4.x), prm.act);
+                    z[i + 1] = finish<T>(s[i + 1], sx * __uint_as_float(w4.y), __uint_as_float(b4.y), prm.act);
+                    z[i + 2] = finish<T>(s[i + 2], sx * __uint_as_float(w4.z), __uint_as_float(b4.z), prm.act);
+                    z[i + 3] = finish<T>(s[i + 3], sx * __uint_as_float(w4.w), __uint_as_float(b4.w), prm.act);
+                }
+                if (m < prm.M) store16<T>(row, n0 + c, prm.N, vec, z);
+            };
+            int sum[LONG ? CH : 1][16];
+            if (LONG)
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sum[c][i] = 0;
+            for (int it = 0; it < stages; it += SEG) {
+                ok = warp_wait_or_dead(acc_full(a), aph, dead, limit);
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t at = tmem + a * BN + col0 + (static_cast<uint32_t>(quarter * 32) << 16);
+#pragma unroll
+                for (int c = 0; c < CH; ++c) {
+                    uint32_t r[16];
+                    tmem_ld16(at + 16 * c, r);
+                    tmem_wait_ld();
+                    if (LONG) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sum[c][i] += __float2int_rn(__uint_as_float(r[i]));
+                    } else {
+                        float s[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[i] = __uint_as_float(r[i]);
+                        write(16 * c, s);
+                    }
+                }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(acc_empty(a));
+                a ^= 1;
+                aph ^= a == 0;
+            }
+            if (LONG && ok) {
+#pragma unroll
+                for (int c = 0; c < CH; ++c) {
+                    float s[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] = static_cast<float>(sum[c][i]);
+                    write(16 * c, s);
+                }
+            }
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    if (warp == MMA_WARP)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::COLS)
+                     : "memory");
+    if (threadIdx.x == 0 && *dead) atomicOr(prm.err, ERR_TIMEOUT);
+}
+
+}  // namespace ips
