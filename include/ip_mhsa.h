@@ -450,6 +450,76 @@ int ip_linear_scaled_i8(const int8_t *x, long long ldx, const float *sx, const i
                         int K, int N, void *y, long long ldy, int dtype, void *workspace,
                         size_t workspace_bytes, ip_stream_t stream);
 
+/* ---- key/value cache in 4 bits ------------------------------------------
+ *
+ * Keys and values of a sequence's tokens (a decoder's own, or the encoder's frames for
+ * a cross attention), 128 channels a head, in 144 bytes a token and head.  Each group
+ * of 32 channels (channel / 32) has a bf16 scale s, the bf16 value nearest to
+ * max |x| / 7 (ties to even), and codes c = x / s to the nearest integer (ties to even)
+ * within -7 .. 7; a channel reads as c s.  A group that holds a NaN or an infinity reads
+ * as NaN.
+ * The cache is n_pages pages of `page` tokens (16, 32 or 64), each [H] blocks of
+ * ip_kv4_page_bytes(page, 128) = 144 page bytes: page x 64 bytes of K codes, page x 4 bf16
+ * K scales, page x 64 bytes of V codes, page x 4 bf16 V scales.  A code is the nibble
+ * c + 8, low nibble first; channel d = 32 g + r of a row sits in byte 16 (r / 8) + 4 g +
+ * (r mod 8) / 2 of a K row and in byte 8 (r / 4) + 2 g + (r mod 4) / 2 of a V row.
+ * page_table: device int32 [B][max_pages]; position i of sequence b lies in page
+ * page_table[b][i / page].  Entries behind a sequence's tokens are not read.  Where a
+ * call needs an entry outside [0, n_pages), or a position outside [0, max_pages page), it
+ * skips these tokens (attention: as if masked) and reports IP_ERR_PARAM by
+ * ip_relpos_mhsa_status on its workspace (256 bytes, 256-aligned, zero-filled once).
+ * max_pages page <= IP_KV4_MAX_LEN.  B, T, H, dh = 128 as elsewhere; calls are
+ * asynchronous on `stream` and return IP_OK or IP_ERR_*. */
+#define IP_KV4_MAX_LEN (1 << 28)
+
+/* Bytes of one page of one head, 0 for a page size or dh that is not offered. */
+size_t ip_kv4_page_bytes(int page, int dh);
+
+/* Writes the rows t < count[b] of k and v to the positions start[b] + t.
+ * k, v: device, dtype IP_F32, IP_F16 or IP_BF16, [B][T][H][128] with the element strides
+ * k_strides, v_strides (HOST arrays {batch, token, head}, each in [0, 2^40]; channels
+ * are consecutive).  start: device int32 [B]; count: device int32 [B] (values above T
+ * count as T) or NULL for T.  Two rows of one call must not meet in one place of the
+ * cache (what it then holds is undefined). */
+int ip_kv4_append(const void *k, const void *v, int dtype, const long long *k_strides,
+                  const long long *v_strides, const int32_t *start, const int32_t *count, int B, int T,
+                  int H, int dh, const int32_t *page_table, int max_pages, void *cache, int n_pages,
+                  int page, void *workspace, size_t workspace_bytes, ip_stream_t stream);
+
+/* Reads the positions start[b] + t, t < count[b], back as real values: k, v: device,
+ * dtype as above, [B][T][H][128] contiguous and 16-byte aligned; rows t >= count[b] and
+ * positions without a page are written as 0. */
+int ip_kv4_read(const void *cache, int n_pages, int page, const int32_t *page_table, int max_pages,
+                const int32_t *start, const int32_t *count, int B, int T, int H, int dh, void *k,
+                void *v, int dtype, void *workspace, size_t workspace_bytes, ip_stream_t stream);
+
+/* Bytes of workspace of ip_kv4_attention: the status word and, where it cuts the keys into
+ * chunks, their partial rows (which need no zero fill).  Depends on the arguments only.
+ * 0 if the shape is invalid. */
+size_t ip_kv4_attention_workspace_bytes(int B, int T, int H, int Hkv, int max_len);
+
+/* Attention of T query tokens a sequence over its cached tokens:
+ *   out[b][t][h] = softmax_j(scale q[b][t][h] . K[b][j][h / (H / Hkv)]) V
+ * q: device, IP_F16 or IP_BF16, [B][T][H][128] with element strides q_strides (HOST, as
+ * k_strides); out: device, same type, contiguous, 16-byte aligned.  H query heads share Hkv
+ * cache heads in groups of H / Hkv.  lengths: device int32 [B], cached tokens (those of
+ * this call's queries included, if they are cached); values below 0 count as 0, values above
+ * max_len or max_pages page as the smaller of these (and are reported as IP_ERR_PARAM).  count: device int32 [B], query
+ * tokens (clamped to [0, T]), or NULL for T.  causal = 1: the queries are the last
+ * count[b] cached tokens, so query t sees the positions up to lengths[b] - count[b] + t;
+ * causal = 0: all of them (cross attention).  A query that sees none, and the rows
+ * t >= count[b], are written as 0.  Scores, softmax and sums are in f32; the
+ * probabilities times the V scales enter the output product as fp16 (relative 2^-11).
+ * max_len: host upper bound of the lengths, in [0, IP_KV4_MAX_LEN]; it sizes the split of
+ * the keys, and the result depends on it in the last bits only.
+ * 1 <= T <= IP_MAX_T; scale in (0, 1e30).  Workspace: at least the size above, 256-byte
+ * aligned; calls that share one must not overlap on the GPU. */
+int ip_kv4_attention(const void *q, int dtype, const long long *q_strides, const int32_t *lengths,
+                     const int32_t *count, int causal, float scale, int B, int T, int H, int Hkv, int dh,
+                     int max_len, const int32_t *page_table, int max_pages, const void *cache,
+                     int n_pages, int page, void *out, void *workspace, size_t workspace_bytes,
+                     ip_stream_t stream);
+
 /* Text of an IP_* code. */
 const char *ip_strerror(int code);
 

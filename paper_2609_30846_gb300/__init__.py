@@ -35,7 +35,8 @@ EXPORTS = (
     "ip_swish16_params_from_scales", "ip_relpos_mhsa_i8_host_async", "ip_relpos_mhsa_host_status",
     "ip_set_workspace", "ip_probe_int8_mix", "ip_linear_residual_i8",
     "ip_relpos_layer_constants", "ip_linear_constants", "ip_relpos_mhsa_noalloc_status",
-    "ip_quantize_rows_i8", "ip_linear_scaled_i8",
+    "ip_quantize_rows_i8", "ip_linear_scaled_i8", "ip_kv4_page_bytes", "ip_kv4_append", "ip_kv4_read",
+    "ip_kv4_attention_workspace_bytes", "ip_kv4_attention",
 )
 
 ROWS = 0    # IP_LAYOUT_ROWS:  [B][T][C]
@@ -177,6 +178,17 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         lib.ip_linear_scaled_i8.argtypes = [P, LL, P, P, LL, P, P, I, LL, I, I, P, LL, I, P,
                                             ctypes.c_size_t, P]
         lib.ip_linear_scaled_i8.restype = I
+        S, F = ctypes.c_size_t, ctypes.c_float
+        lib.ip_kv4_page_bytes.argtypes = [I, I]
+        lib.ip_kv4_page_bytes.restype = S
+        lib.ip_kv4_append.argtypes = [P, P, I, P, P, P, P, I, I, I, I, P, I, P, I, I, P, S, P]
+        lib.ip_kv4_append.restype = I
+        lib.ip_kv4_read.argtypes = [P, I, I, P, I, P, P, I, I, I, I, P, P, I, P, S, P]
+        lib.ip_kv4_read.restype = I
+        lib.ip_kv4_attention_workspace_bytes.argtypes = [I] * 5
+        lib.ip_kv4_attention_workspace_bytes.restype = S
+        lib.ip_kv4_attention.argtypes = [P, I, P, P, P, I, F, I, I, I, I, I, I, P, I, P, I, I, P, P, S, P]
+        lib.ip_kv4_attention.restype = I
         lib.ip_probe_int8_mma.argtypes = [I, I, P, P]
         lib.ip_probe_int8_mma.restype = ctypes.c_longlong
         lib.ip_probe_int8_mix.argtypes = [I, I, I, P, P]
@@ -823,6 +835,140 @@ def linear_scaled_i8(x, sx, w, sw, bias=None, *, act: int = ACT_NONE, dtype=None
     return out
 
 
+def kv4_page_bytes(page: int, dh: int = IP_DH) -> int:
+    """Bytes of one page of one head of a 4-bit cache (144 a token)."""
+    n = load().ip_kv4_page_bytes(page, dh)
+    if n == 0:
+        raise IpError("ip_kv4_page_bytes", -4, "pages of 16, 32 or 64 tokens, heads of 128")
+    return n
+
+
+def kv4_cache(n_pages: int, heads: int, page: int = 64, device="cuda"):
+    """A cache of n_pages pages of `page` tokens: uint8 [n_pages, heads, 144 page]."""
+    import torch
+    return torch.zeros((n_pages, heads, kv4_page_bytes(page)), dtype=torch.uint8, device=device)
+
+
+def _kv4(cache, table, B, heads=None):
+    """(pages, heads, page size, table width) of a cache and its page table."""
+    import torch
+    if _need(cache, "cache", torch.uint8).dim() != 3 or cache.shape[2] % 144 or not cache.is_contiguous():
+        raise ValueError("cache must be a contiguous uint8 tensor [pages, heads, 144 page]")
+    if heads is not None and cache.shape[1] != heads:
+        raise ValueError(f"cache holds {cache.shape[1]} heads, not {heads}")
+    if _need(table, "page_table", torch.int32, None, cache.device).dim() != 2 or table.shape[0] != B:
+        raise ValueError(f"page_table must have shape ({B}, pages), got {tuple(table.shape)}")
+    if not table.is_contiguous():
+        raise ValueError("page_table must be contiguous")
+    return cache.shape[0], cache.shape[1], cache.shape[2] // 144, table.shape[1]
+
+
+def _strides(t, name):
+    if t.stride(3) != 1:
+        raise ValueError(f"{name}'s channels must be contiguous")
+    return (ctypes.c_longlong * 3)(*t.stride()[:3])
+
+
+def kv4_append(k, v, start, page_table, cache, *, count=None, workspace=None, stream=None):
+    """Quantises k, v (float32, float16 or bfloat16 [B, T, H, 128], any strides with
+    contiguous channels) to 4 bits into the cache: rows t < count[b] (int32 [B]; None:
+    T) go to the positions start[b] + t (int32 [B]) of sequence b, whose pages are
+    page_table[b] (int32 [B, pages]).  No two rows may meet in one place.  All CUDA
+    tensors; asynchronous on `stream`.  Pages or positions that do not exist are
+    skipped and reported by status(workspace)."""
+    import torch
+    if _need(k, "k").dim() != 4 or k.shape[3] != IP_DH:
+        raise ValueError(f"k must have shape (B, T, H, 128), got {tuple(k.shape)}")
+    B, T, H, dh = k.shape
+    dev = k.device
+    code = _dtype_code(k.dtype, "k")
+    _need(v, "v", k.dtype, k.shape, dev)
+    n_pages, _, page, width = _kv4(_need(cache, "cache", None, None, dev), page_table, B, H)
+    pst = _dense(start, "start", torch.int32, (B,), dev)
+    pct = None if count is None else _dense(count, "count", torch.int32, (B,), dev)
+    with _On(dev, stream) as handle:
+        workspace, ws, wsb = _status_space(workspace, dev)
+        rc = (_lib or load()).ip_kv4_append(
+            k.data_ptr(), v.data_ptr(), code, _strides(k, "k"), _strides(v, "v"), pst, pct, B, T, H, dh,
+            page_table.data_ptr(), width, cache.data_ptr(), n_pages, page, ws, wsb, handle)
+    if rc:
+        _check("ip_kv4_append", rc)
+    return cache
+
+
+def kv4_read(cache, start, page_table, T: int, *, count=None, dtype=None, out=None, workspace=None,
+             stream=None):
+    """Positions start[b] .. start[b] + T - 1 of every sequence back as real values:
+    (k, v), each [B, T, H, 128] of `dtype` (bfloat16 unless out gives it), zeros in rows
+    t >= count[b].  out: such a pair, contiguous.  Arguments as kv4_append."""
+    import torch
+    B = start.shape[0] if start.dim() == 1 else -1
+    n_pages, H, page, width = _kv4(cache, page_table, B)
+    dev = cache.device
+    pst = _dense(start, "start", torch.int32, (B,), dev)
+    pct = None if count is None else _dense(count, "count", torch.int32, (B,), dev)
+    shape = (B, T, H, IP_DH)
+    dtype = dtype or (torch.bfloat16 if out is None else out[0].dtype)
+    code = _dtype_code(dtype)
+    with _On(dev, stream) as handle:
+        if out is None:
+            out = torch.empty(shape, dtype=dtype, device=dev), torch.empty(shape, dtype=dtype, device=dev)
+        pk, pv = _dense(out[0], "out[0]", dtype, shape, dev), _dense(out[1], "out[1]", dtype, shape, dev)
+        workspace, ws, wsb = _status_space(workspace, dev)
+        rc = (_lib or load()).ip_kv4_read(cache.data_ptr(), n_pages, page, page_table.data_ptr(), width, pst,
+                                          pct, B, T, H, IP_DH, pk, pv, code, ws, wsb, handle)
+    if rc:
+        _check("ip_kv4_read", rc)
+    return out
+
+
+def kv4_attention_workspace_bytes(B: int, T: int, heads: int, cache_heads: int, max_len: int) -> int:
+    """Bytes of workspace of kv4_attention for these sizes."""
+    n = load().ip_kv4_attention_workspace_bytes(B, T, heads, cache_heads, max_len)
+    if n == 0:
+        raise IpError("ip_kv4_attention_workspace_bytes", -2, "invalid shape")
+    return n
+
+
+def kv4_attention(q, lengths, page_table, cache, *, count=None, causal: bool = True, scale=None,
+                  max_len=None, out=None, workspace=None, stream=None):
+    """Attention of q (float16 or bfloat16 [B, T, H, 128], any strides with contiguous
+    channels) over a 4-bit cache of Hkv heads, H a multiple of Hkv: softmax(scale q K^T) V
+    with scale 1/sqrt(128) unless given.  lengths (int32 [B]): cached tokens, with this
+    call's own; count (int32 [B], None: T): query tokens, which causal makes the last
+    ones of the sequence; causal=False lets every query see all cached tokens.  A query that
+    sees none, and rows past count, give 0.  max_len: a host bound of lengths (default: what
+    the table can hold); a close one splits the work better.  Returns [B, T, H, 128] of
+    q's type.  workspace: a zero-filled uint8 tensor of kv4_attention_workspace_bytes(B, T,
+    H, Hkv, max_len).  Asynchronous on `stream`."""
+    import torch
+    if _need(q, "q").dim() != 4 or q.shape[3] != IP_DH:
+        raise ValueError(f"q must have shape (B, T, H, 128), got {tuple(q.shape)}")
+    if q.dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError(f"q must be float16 or bfloat16, got {q.dtype}")
+    B, T, H, dh = q.shape
+    dev = q.device
+    n_pages, Hkv, page, width = _kv4(_need(cache, "cache", None, None, dev), page_table, B)
+    if max_len is None:
+        max_len = width * page
+    pln = _dense(lengths, "lengths", torch.int32, (B,), dev)
+    pct = None if count is None else _dense(count, "count", torch.int32, (B,), dev)
+    lib = _lib or load()
+    with _On(dev, stream) as handle:
+        if out is None:
+            out = torch.empty((B, T, H, dh), dtype=q.dtype, device=dev)
+        po = _dense(out, "out", q.dtype, (B, T, H, dh), dev)
+        size = 0 if workspace is not None else kv4_attention_workspace_bytes(B, T, H, Hkv, max_len)
+        workspace, ws, wsb = _status_space(workspace, dev, size)
+        rc = lib.ip_kv4_attention(
+            q.data_ptr(), 1 if q.dtype == torch.float16 else 2, _strides(q, "q"), pln, pct, 1 if causal else 0,
+            dh ** -0.5 if scale is None else scale, B, T, H, Hkv, dh, max_len, page_table.data_ptr(), width,
+            cache.data_ptr(), n_pages, page, po, ws, wsb, handle)
+    if rc:
+        _check("ip_kv4_attention", rc)
+    return out
+
+
 def relpos_mhsa_i8_host(q, k, v, p, u, v_bias, consts: LayerConstants, lengths, out, arena,
                         stream=None, wait: bool = True):
     """Whole layer from host buffers (torch CPU tensors, ideally pinned):
@@ -867,4 +1013,6 @@ __all__ = ["build", "load", "relpos_mhsa_i8", "relpos_mhsa_i8_host", "status", "
            "residual_params", "linear_glu_i8", "glu_params", "dwconv_swish_i8", "swish16_params",
            "host_status", "set_workspace", "int8_pipe_rates", "linear_residual_i8",
            "quantize_rows_i8", "linear_scaled_i8", "ACT_NONE", "ACT_SWISH",
+           "kv4_page_bytes", "kv4_cache", "kv4_append", "kv4_read", "kv4_attention",
+           "kv4_attention_workspace_bytes",
            "IpError", "LibraryError", "EXPORTS"]

@@ -15,10 +15,10 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libipmhsa.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("ip_mhsa.cu", "ip_linear.cu", "ip_norm.cu",
-                                           "ip_block.cu", "ip_scaled.cu")]
+                                           "ip_block.cu", "ip_scaled.cu", "ip_kv4.cu")]
 DEPS = SOURCES + [os.path.join(CSRC, f) for f in ("ip_mhsa_kernels.cuh", "ip_linear_kernels.cuh",
                                                   "ip_norm_kernels.cuh", "ip_block_kernels.cuh",
-                                                  "ip_scaled_kernels.cuh",
+                                                  "ip_scaled_kernels.cuh", "ip_kv4_kernels.cuh", "ip_real.cuh",
                                                   "ip_ptx.cuh",
                                                   "ip_probe.cuh", "ip_host_util.h")] + [
     os.path.join(INCLUDE, "ip_mhsa.h")]

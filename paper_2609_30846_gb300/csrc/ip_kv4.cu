@@ -1,0 +1,216 @@
+// Host side of the 4-bit key/value cache of the C ABI (include/ip_mhsa.h): argument
+// validation, the split of the attention and the launches.  Device code:
+// ip_kv4_kernels.cuh.
+#include "ip_mhsa.h"
+#include "ip_kv4_kernels.cuh"
+#include "ip_host_util.h"
+
+#include <cuda_runtime.h>
+
+namespace {
+
+bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+size_t elem_size(int dtype) { return dtype == IP_F32 ? 4 : 2; }
+bool dtype_ok(int dtype) { return dtype == IP_F32 || dtype == IP_F16 || dtype == IP_BF16; }
+bool page_ok(int page) { return page == 16 || page == 32 || page == 64; }
+
+int launched(cudaError_t rc) {
+    return rc == cudaSuccess && cudaGetLastError() == cudaSuccess ? IP_OK : IP_ERR_CUDA;
+}
+
+// What the calls on a cache share: IP_OK if its description is sound.
+int check_cache(const int32_t *page_table, int max_pages, const void *cache, int n_pages, int page, int H,
+                int dh, const void *workspace, size_t workspace_bytes, size_t need) {
+    if (dh != IP_DH || !page_ok(page)) return IP_ERR_UNSUPPORTED;
+    if (H < 1 || H > IP_MAX_H || max_pages < 1 || n_pages < 0 ||
+        static_cast<long long>(max_pages) * page > IP_KV4_MAX_LEN)
+        return IP_ERR_SHAPE;
+    if (!page_table || !cache || !workspace) return IP_ERR_NULL;
+    if (!aligned(page_table, 4) || !aligned(cache, 16) || !aligned(workspace, 256)) return IP_ERR_ALIGN;
+    return workspace_bytes < need ? IP_ERR_WORKSPACE : IP_OK;
+}
+
+ipv::Pages pages_of(const int32_t *page_table, int max_pages, const void *cache, int n_pages, int page, int H) {
+    ipv::Pages p;
+    p.cache = static_cast<uint8_t *>(const_cast<void *>(cache));
+    p.table = page_table;
+    p.max_pages = max_pages;
+    p.n_pages = n_pages;
+    p.shift = page == 16 ? 4 : (page == 32 ? 5 : 6);
+    p.heads = H;
+    return p;
+}
+
+// Element strides of batch, token and head: any that keep an offset within 63 bits.
+bool strides_ok(const long long *s) {
+    for (int i = 0; i < 3; ++i)
+        if (s[i] < 0 || s[i] > (1ll << 40)) return false;
+    return true;
+}
+
+// How the attention cuts its keys: chunks of a multiple of 64 tokens, at least 64, so
+// that the grid has about PLAN_CTAS CTAs however few the sequences and heads are.  The
+// plan depends on the call's sizes alone, never on the lengths.
+constexpr long long PLAN_CTAS = 4 * 3 * 152;
+struct Plan {
+    int nt, tiles, chunk, chunks;
+    long long items;
+    size_t bytes;
+};
+bool plan_of(int B, int T, int H, int Hkv, int max_len, Plan *p) {
+    const long long rows = static_cast<long long>(H / Hkv) * T;
+    if (rows > (1ll << 24)) return false;
+    p->nt = rows > 8 ? 2 : 1;
+    p->tiles = static_cast<int>((rows + 8 * p->nt - 1) / (8 * p->nt));
+    p->items = static_cast<long long>(B) * Hkv * p->tiles;
+    if (p->items > 0x7fffffffll) return false;
+    const long long len = max_len < 1 ? 1 : max_len;
+    long long chunk = (len * p->items / PLAN_CTAS + 63) / 64 * 64;
+    if (chunk < 64) chunk = 64;
+    if ((len + chunk - 1) / chunk > 65535) chunk = (len / 65535 + 64) / 64 * 64;
+    if (chunk > len) chunk = (len + 63) / 64 * 64;
+    p->chunk = static_cast<int>(chunk);
+    p->chunks = static_cast<int>((len + chunk - 1) / chunk);
+    p->bytes = 256;
+    if (p->chunks > 1)
+        p->bytes += static_cast<size_t>(p->items) * p->chunks * 8 * p->nt * ipv::PART * sizeof(float);
+    return true;
+}
+
+bool attention_shape_ok(int B, int T, int H, int Hkv, int max_len) {
+    return B >= 0 && B <= IP_MAX_B && T >= 1 && T <= IP_MAX_T && H >= 1 && H <= IP_MAX_H && Hkv >= 1 &&
+           H % Hkv == 0 && max_len >= 0 && max_len <= IP_KV4_MAX_LEN;
+}
+
+template <typename T, int NT>
+int launch_attention(const ipv::AttParams &prm, const Plan &p, cudaStream_t st) {
+    const dim3 grid(static_cast<unsigned>(p.items), static_cast<unsigned>(p.chunks)), block(ipv::ATT_THREADS);
+    int rc = launched(iph::launch_pdl(ipv::kv4_attention_kernel<T, NT>, grid, block, 0, st, prm));
+    if (rc != IP_OK || p.chunks == 1) return rc;
+    const dim3 rows(static_cast<unsigned>(p.items), 8 * NT);
+    return launched(iph::launch_pdl(ipv::kv4_join_kernel<T, NT>, rows, block, 0, st, prm));
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ip_kv4_page_bytes(int page, int dh) {
+    return dh == IP_DH && page_ok(page) ? static_cast<size_t>(ipv::ROW_BYTES) * page : 0;
+}
+
+int ip_kv4_append(const void *k, const void *v, int dtype, const long long *k_strides,
+                  const long long *v_strides, const int32_t *start, const int32_t *count, int B, int T, int H,
+                  int dh, const int32_t *page_table, int max_pages, void *cache, int n_pages, int page,
+                  void *workspace, size_t workspace_bytes, ip_stream_t stream) {
+    if (!dtype_ok(dtype)) return IP_ERR_PARAM;
+    if (B < 0 || B > IP_MAX_B || T < 0 || static_cast<long long>(B) * T > IP_LINEAR_MAX_FRAMES) return IP_ERR_SHAPE;
+    if (B == 0 || T == 0) return IP_OK;
+    const int rc = check_cache(page_table, max_pages, cache, n_pages, page, H, dh, workspace, workspace_bytes, 256);
+    if (rc != IP_OK) return rc;
+    if (!k || !v || !k_strides || !v_strides || !start) return IP_ERR_NULL;
+    if (!aligned(k, elem_size(dtype)) || !aligned(v, elem_size(dtype)) || !aligned(start, 4) ||
+        (count && !aligned(count, 4)))
+        return IP_ERR_ALIGN;
+    if (!strides_ok(k_strides) || !strides_ok(v_strides)) return IP_ERR_SHAPE;
+    const long long warps = static_cast<long long>(B) * T * H;
+    const long long ctas = (warps + ipv::ROW_THREADS / 32 - 1) / (ipv::ROW_THREADS / 32);
+    if (ctas > 0x7fffffffll) return IP_ERR_SHAPE;
+    ipv::RowParams prm{};
+    prm.k = k;
+    prm.v = v;
+    for (int i = 0; i < 3; ++i) prm.ks[i] = k_strides[i], prm.vs[i] = v_strides[i];
+    prm.start = start;
+    prm.count = count;
+    prm.B = B;
+    prm.T = T;
+    prm.H = H;
+    prm.pages = pages_of(page_table, max_pages, cache, n_pages, page, H);
+    prm.err = static_cast<int *>(workspace);
+    const dim3 grid(static_cast<unsigned>(ctas)), block(ipv::ROW_THREADS);
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (dtype == IP_F32) return launched(iph::launch_pdl(ipv::kv4_append_kernel<float>, grid, block, 0, st, prm));
+    if (dtype == IP_F16) return launched(iph::launch_pdl(ipv::kv4_append_kernel<__half>, grid, block, 0, st, prm));
+    return launched(iph::launch_pdl(ipv::kv4_append_kernel<__nv_bfloat16>, grid, block, 0, st, prm));
+}
+
+int ip_kv4_read(const void *cache, int n_pages, int page, const int32_t *page_table, int max_pages,
+                const int32_t *start, const int32_t *count, int B, int T, int H, int dh, void *k, void *v,
+                int dtype, void *workspace, size_t workspace_bytes, ip_stream_t stream) {
+    if (!dtype_ok(dtype)) return IP_ERR_PARAM;
+    if (B < 0 || B > IP_MAX_B || T < 0 || static_cast<long long>(B) * T > IP_LINEAR_MAX_FRAMES) return IP_ERR_SHAPE;
+    if (B == 0 || T == 0) return IP_OK;
+    const int rc = check_cache(page_table, max_pages, cache, n_pages, page, H, dh, workspace, workspace_bytes, 256);
+    if (rc != IP_OK) return rc;
+    if (!k || !v || !start) return IP_ERR_NULL;
+    if (!aligned(k, 16) || !aligned(v, 16) || !aligned(start, 4) || (count && !aligned(count, 4)))
+        return IP_ERR_ALIGN;
+    const long long warps = static_cast<long long>(B) * T * H;
+    const long long ctas = (warps + ipv::ROW_THREADS / 32 - 1) / (ipv::ROW_THREADS / 32);
+    if (ctas > 0x7fffffffll) return IP_ERR_SHAPE;
+    ipv::RowParams prm{};
+    prm.ko = k;
+    prm.vo = v;
+    prm.start = start;
+    prm.count = count;
+    prm.B = B;
+    prm.T = T;
+    prm.H = H;
+    prm.pages = pages_of(page_table, max_pages, cache, n_pages, page, H);
+    prm.err = static_cast<int *>(workspace);
+    const dim3 grid(static_cast<unsigned>(ctas)), block(ipv::ROW_THREADS);
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (dtype == IP_F32) return launched(iph::launch_pdl(ipv::kv4_read_kernel<float>, grid, block, 0, st, prm));
+    if (dtype == IP_F16) return launched(iph::launch_pdl(ipv::kv4_read_kernel<__half>, grid, block, 0, st, prm));
+    return launched(iph::launch_pdl(ipv::kv4_read_kernel<__nv_bfloat16>, grid, block, 0, st, prm));
+}
+
+size_t ip_kv4_attention_workspace_bytes(int B, int T, int H, int Hkv, int max_len) {
+    Plan p;
+    if (!attention_shape_ok(B, T, H, Hkv, max_len) || !plan_of(B, T, H, Hkv, max_len, &p)) return 0;
+    return p.bytes;
+}
+
+int ip_kv4_attention(const void *q, int dtype, const long long *q_strides, const int32_t *lengths,
+                     const int32_t *count, int causal, float scale, int B, int T, int H, int Hkv, int dh,
+                     int max_len, const int32_t *page_table, int max_pages, const void *cache, int n_pages,
+                     int page, void *out, void *workspace, size_t workspace_bytes, ip_stream_t stream) {
+    if (dtype != IP_F16 && dtype != IP_BF16) return IP_ERR_PARAM;
+    if ((causal != 0 && causal != 1) || !(scale > 0.0f && scale < 1e30f)) return IP_ERR_PARAM;
+    Plan p;
+    if (!attention_shape_ok(B, T, H, Hkv, max_len) || !plan_of(B, T, H, Hkv, max_len, &p)) return IP_ERR_SHAPE;
+    if (B == 0) return IP_OK;
+    const int rc = check_cache(page_table, max_pages, cache, n_pages, page, Hkv, dh, workspace, workspace_bytes,
+                               p.bytes);
+    if (rc != IP_OK) return rc;
+    if (!q || !q_strides || !lengths || !out) return IP_ERR_NULL;
+    if (!aligned(q, 2) || !aligned(out, 16) || !aligned(lengths, 4) || (count && !aligned(count, 4)))
+        return IP_ERR_ALIGN;
+    if (!strides_ok(q_strides)) return IP_ERR_SHAPE;
+    ipv::AttParams prm{};
+    prm.q = q;
+    prm.out = out;
+    for (int i = 0; i < 3; ++i) prm.qs[i] = q_strides[i];
+    prm.lengths = lengths;
+    prm.count = count;
+    prm.B = B;
+    prm.T = T;
+    prm.H = Hkv;
+    prm.G = H / Hkv;
+    prm.causal = causal;
+    prm.max_len = max_len < max_pages * page ? max_len : max_pages * page;
+    prm.chunk = p.chunk;
+    prm.chunks = p.chunks;
+    prm.tiles = p.tiles;
+    prm.scale_log2 = scale * 1.44269504088896f;
+    prm.pages = pages_of(page_table, max_pages, cache, n_pages, page, Hkv);
+    prm.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + 256);
+    prm.err = static_cast<int *>(workspace);
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (dtype == IP_F16)
+        return p.nt == 1 ? launch_attention<__half, 1>(prm, p, st) : launch_attention<__half, 2>(prm, p, st);
+    return p.nt == 1 ? launch_attention<__nv_bfloat16, 1>(prm, p, st)
+                     : launch_attention<__nv_bfloat16, 2>(prm, p, st);
+}
+
+}  // extern "C"

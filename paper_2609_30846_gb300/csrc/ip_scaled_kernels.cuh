@@ -9,41 +9,12 @@
 #include <stdint.h>
 
 #include "ip_ptx.cuh"
+#include "ip_real.cuh"
 
 namespace ips {
 
 using namespace ipk;
-
-// ---- element types ------------------------------------------------------
-
-__device__ __forceinline__ float to_f32(float x) { return x; }
-__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
-__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
-
-template <typename T> __device__ __forceinline__ T from_f32(float x);
-template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
-template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
-template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) {
-    return __float2bfloat16_rn(x);
-}
-
-// Eight consecutive elements as floats; `vec`: p is 16-byte aligned.
-template <typename T>
-__device__ __forceinline__ void load8(const T *p, bool vec, int n, float (&v)[8]) {
-    if (vec && n >= 8) {
-        constexpr int W = 16 / sizeof(T);
-#pragma unroll
-        for (int i = 0; i < 8 / W; ++i) {
-            const uint4 w = *reinterpret_cast<const uint4 *>(p + i * W);
-            const T *e = reinterpret_cast<const T *>(&w);
-#pragma unroll
-            for (int j = 0; j < W; ++j) v[i * W + j] = to_f32(e[j]);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f32(p[i]) : 0.0f;
-    }
-}
+using namespace ipr;
 
 // ---- rows to int8 -------------------------------------------------------
 //
