@@ -193,6 +193,7 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         lib.ip_probe_int8_mma.restype = ctypes.c_longlong
         lib.ip_probe_int8_mix.argtypes = [I, I, I, P, P]
         lib.ip_probe_int8_mix.restype = ctypes.c_longlong
+        _Torch.bind()
         _lib = lib
         return lib
 
@@ -687,6 +688,31 @@ def dwconv_swish_i8(x, w, bias, m, s, sw16: tuple[int, int, int, int], *, out=No
 
 
 # ------------------------------------------------------- run-time scales
+#
+# A decoder's single-token calls are shorter on the GPU than in Python (1.8 us for a
+# 1024 x 4096 product), so each call has a short form for its usual arguments (plain
+# tensors, contiguous or matrices, the current device and stream), which makes the same
+# checks in place, and leaves everything else and every error to the general form.
+# (On a Grace core: quantize_rows_i8 9.5 -> 7, linear_scaled_i8 16 -> 9, kv4_attention
+# 15 -> 9 us a call.)
+
+class _Torch:
+    """torch's names that the short forms use, resolved once."""
+    tensor = None
+
+    @classmethod
+    def bind(cls):
+        try:
+            import torch
+        except ImportError:      # the C entry points need no torch
+            return
+        cls.empty, cls.zeros = torch.empty, torch.zeros
+        cls.i8, cls.u8, cls.i32, cls.f32 = torch.int8, torch.uint8, torch.int32, torch.float32
+        cls.f16, cls.bf16 = torch.float16, torch.bfloat16
+        cls.codes = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+        cls.current, cls.raw = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+        cls.tensor = torch.Tensor
+
 
 def _dtype_code(dtype, name="dtype"):
     import torch
@@ -732,7 +758,7 @@ def _as_rows(t, name):
             elif st != stride * rows:
                 raise ValueError(f"{name}'s rows must follow one another with one stride")
         rows *= size
-    if stride is None:
+    if rows < 2:
         stride = -(-d // 16) * 16      # one row (or none): any stride does
     if stride < d:
         raise ValueError(f"{name}'s rows must not overlap")
@@ -779,9 +805,22 @@ def quantize_rows_i8(x, *, q=None, scale=None, stream=None):
     new q has rows of a multiple of 16 bytes, as linear_scaled_i8 reads them, so it
     is a view of them where 16 does not divide the last axis.  Asynchronous on
     `stream` (default: torch's current stream)."""
+    t = _Torch
+    if x.__class__ is t.tensor and q is None and scale is None and stream is None:
+        dev, code, shape = x.get_device(), t.codes.get(x.dtype), x.shape
+        d = shape[-1] if shape else 0
+        if dev >= 0 and dev == t.current() and code is not None and d and not d & 15 and x.is_contiguous():
+            q = t.empty(shape, dtype=t.i8, device=x.device)
+            scale = t.empty(shape[:-1], dtype=t.f32, device=x.device)
+            rc = _lib.ip_quantize_rows_i8(x.data_ptr(), code, x.numel() // d, d, d, q.data_ptr(), d,
+                                          scale.data_ptr(), t.raw(dev))
+            if rc:
+                _check("ip_quantize_rows_i8", rc)
+            return q, scale
     import torch
     code = _dtype_code(_need(x, "x").dtype, "x")
     rows, d, ldx = _as_rows(x, "x")
+    lib = _lib or load()
     with _On(x.device, stream) as handle:
         if q is None:
             ldq = -(-d // 16) * 16
@@ -791,7 +830,7 @@ def quantize_rows_i8(x, *, q=None, scale=None, stream=None):
             ldq = _as_rows(_need(q, "q", torch.int8, x.shape, x.device), "q")[2]
         if scale is None:
             scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-        rc = (_lib or load()).ip_quantize_rows_i8(
+        rc = lib.ip_quantize_rows_i8(
             x.data_ptr(), code, rows, d, ldx, q.data_ptr(), ldq,
             _dense(scale, "scale", torch.float32, x.shape[:-1], x.device), handle)
     if rc:
@@ -808,6 +847,30 @@ def linear_scaled_i8(x, sx, w, sw, bias=None, *, act: int = ACT_NONE, dtype=None
     K and N may be any size; the rows of x and w start on multiples of 16 bytes.
     Returns out: [..., N] of `dtype` (bfloat16 unless out gives it).  Asynchronous on
     `stream` (default: torch's current stream)."""
+    t = _Torch
+    T = t.tensor
+    if (x.__class__ is T and w.__class__ is T and sx.__class__ is T and sw.__class__ is T and
+            workspace.__class__ is T and out is None and stream is None):
+        dev, xs, ws = x.get_device(), x.shape, w.shape
+        code = t.codes.get(dtype)
+        if (dev >= 0 and dev == t.current() and code is not None and len(ws) == 2 and xs and
+                xs[-1] == ws[1] and x.dtype is t.i8 and w.dtype is t.i8 and sx.dtype is t.f32 and
+                sw.dtype is t.f32 and workspace.dtype is t.u8 and w.get_device() == dev and
+                sx.get_device() == dev and sw.get_device() == dev and workspace.get_device() == dev and
+                sx.shape == xs[:-1] and sw.shape == ws[:1] and x.is_contiguous() and w.is_contiguous() and
+                sx.is_contiguous() and sw.is_contiguous() and workspace.is_contiguous() and
+                (bias is None or bias.__class__ is T and bias.dtype is t.f32 and bias.shape == ws[:1] and
+                 bias.get_device() == dev and bias.is_contiguous())):
+            N, K = ws
+            if N and K and not K & 15:
+                out = t.empty(xs[:-1] + ws[:1], dtype=dtype, device=x.device)
+                rc = _lib.ip_linear_scaled_i8(
+                    x.data_ptr(), K, sx.data_ptr(), w.data_ptr(), K, sw.data_ptr(),
+                    None if bias is None else bias.data_ptr(), act, x.numel() // K, K, N, out.data_ptr(), N,
+                    code, workspace.data_ptr(), workspace.numel(), t.raw(dev))
+                if rc:
+                    _check("ip_linear_scaled_i8", rc)
+                return out
     import torch
     rows, K, ldx = _as_rows(_need(x, "x", torch.int8), "x")
     if _need(w, "w", torch.int8, None, x.device).dim() != 2 or w.shape[1] != K:
@@ -823,11 +886,12 @@ def linear_scaled_i8(x, sx, w, sw, bias=None, *, act: int = ACT_NONE, dtype=None
     psx = _dense(sx, "sx", torch.float32, x.shape[:-1], x.device)
     psw = _dense(sw, "sw", torch.float32, (N,), x.device)
     pb = None if bias is None else _dense(bias, "bias", torch.float32, (N,), x.device)
+    lib = _lib or load()
     with _On(x.device, stream) as handle:
         if out is None:
             out = torch.empty(shape, dtype=dtype, device=x.device)
         workspace, ws, wsb = _status_space(workspace, x.device)
-        rc = (_lib or load()).ip_linear_scaled_i8(
+        rc = lib.ip_linear_scaled_i8(
             x.data_ptr(), ldx, psx, w.data_ptr(), ldw, psw, pb, int(act), rows, K, N, out.data_ptr(),
             ldy, code, ws, wsb, handle)
     if rc:
@@ -849,24 +913,70 @@ def kv4_cache(n_pages: int, heads: int, page: int = 64, device="cuda"):
     return torch.zeros((n_pages, heads, kv4_page_bytes(page)), dtype=torch.uint8, device=device)
 
 
-def _kv4(cache, table, B, heads=None):
-    """(pages, heads, page size, table width) of a cache and its page table."""
+def _strides(t, name):
+    st = t.stride()
+    if st[3] != 1:
+        raise ValueError(f"{name}'s channels must be contiguous")
+    return _Stride3(*st[:3])
+
+
+_Stride3 = ctypes.c_longlong * 3
+
+
+def _kv4_plain(dev, *ints):
+    """Whether the int32 tensors of a cache call are plain, contiguous and on device dev."""
+    t = _Torch
+    for i in ints:
+        if i is not None and not (i.__class__ is t.tensor and i.dtype is t.i32 and i.is_contiguous() and
+                                  i.get_device() == dev):
+            return False
+    return True
+
+
+def _kv4_args(x, cache, table, workspace, size, lens, names, stream):
+    """Checks what the calls on a cache share: x [B, T, H, 128] (or B, for a call without
+    one), the cache, its table and the int32 [B] tensors lens; returns B, the cache's
+    (pages, heads, page size, table width), the pointers of lens, a workspace and the
+    raw stream (None: the call goes through _On, on the device of the cache)."""
+    t = _Torch
+    B = x if x.__class__ is int else x.shape[0]
+    if (cache.__class__ is t.tensor and workspace.__class__ is t.tensor and stream is None and
+            cache.dtype is t.u8 and workspace.dtype is t.u8 and cache.is_contiguous() and
+            workspace.is_contiguous()):
+        dev, cs = cache.get_device(), cache.shape
+        if (dev >= 0 and dev == t.current() and workspace.get_device() == dev and len(cs) == 3 and
+                (x is B or x.get_device() == dev) and not cs[2] % 144 and _kv4_plain(dev, table, *lens)):
+            ts = table.shape
+            if len(ts) == 2 and ts[0] == B and all(i is None or i.shape == ts[:1] for i in lens):
+                return (B, (cs[0], cs[1], cs[2] // 144, ts[1]),
+                        [None if i is None else i.data_ptr() for i in lens], workspace, t.raw(dev))
     import torch
-    if _need(cache, "cache", torch.uint8).dim() != 3 or cache.shape[2] % 144 or not cache.is_contiguous():
+    dev = _need(cache, "cache", torch.uint8).device
+    if x is not B:
+        _need(x, names[0], None, None, dev)
+    if cache.dim() != 3 or cache.shape[2] % 144 or not cache.is_contiguous():
         raise ValueError("cache must be a contiguous uint8 tensor [pages, heads, 144 page]")
-    if heads is not None and cache.shape[1] != heads:
-        raise ValueError(f"cache holds {cache.shape[1]} heads, not {heads}")
-    if _need(table, "page_table", torch.int32, None, cache.device).dim() != 2 or table.shape[0] != B:
+    if _need(table, "page_table", torch.int32, None, dev).dim() != 2 or table.shape[0] != B:
         raise ValueError(f"page_table must have shape ({B}, pages), got {tuple(table.shape)}")
     if not table.is_contiguous():
         raise ValueError("page_table must be contiguous")
-    return cache.shape[0], cache.shape[1], cache.shape[2] // 144, table.shape[1]
+    ptrs = [None if i is None else _dense(i, n, torch.int32, (B,), dev) for i, n in zip(lens, names[1:])]
+    if workspace is not None:
+        _dense(workspace, "workspace", torch.uint8, (workspace.numel(),), dev)
+    load()
+    return B, (cache.shape[0], cache.shape[1], cache.shape[2] // 144, table.shape[1]), ptrs, workspace, None
 
 
-def _strides(t, name):
-    if t.stride(3) != 1:
-        raise ValueError(f"{name}'s channels must be contiguous")
-    return (ctypes.c_longlong * 3)(*t.stride()[:3])
+def _kv4_run(fn, call, handle, device, stream, workspace, size):
+    """call(workspace, raw stream) on the right device and stream, with a fresh workspace
+    of `size` bytes where there is none."""
+    if handle is not None:
+        rc = call(workspace, handle)
+    else:
+        with _On(device, stream) as handle:
+            rc = call(_status_space(workspace, device, size)[0] if workspace is None else workspace, handle)
+    if rc:
+        _check(fn, rc)
 
 
 def kv4_append(k, v, start, page_table, cache, *, count=None, workspace=None, stream=None):
@@ -876,23 +986,21 @@ def kv4_append(k, v, start, page_table, cache, *, count=None, workspace=None, st
     page_table[b] (int32 [B, pages]).  No two rows may meet in one place.  All CUDA
     tensors; asynchronous on `stream`.  Pages or positions that do not exist are
     skipped and reported by status(workspace)."""
-    import torch
-    if _need(k, "k").dim() != 4 or k.shape[3] != IP_DH:
+    code = _dtype_code(_need(k, "k").dtype, "k")
+    if k.dim() != 4 or k.shape[3] != IP_DH:
         raise ValueError(f"k must have shape (B, T, H, 128), got {tuple(k.shape)}")
-    B, T, H, dh = k.shape
-    dev = k.device
-    code = _dtype_code(k.dtype, "k")
-    _need(v, "v", k.dtype, k.shape, dev)
-    n_pages, _, page, width = _kv4(_need(cache, "cache", None, None, dev), page_table, B, H)
-    pst = _dense(start, "start", torch.int32, (B,), dev)
-    pct = None if count is None else _dense(count, "count", torch.int32, (B,), dev)
-    with _On(dev, stream) as handle:
-        workspace, ws, wsb = _status_space(workspace, dev)
-        rc = (_lib or load()).ip_kv4_append(
-            k.data_ptr(), v.data_ptr(), code, _strides(k, "k"), _strides(v, "v"), pst, pct, B, T, H, dh,
-            page_table.data_ptr(), width, cache.data_ptr(), n_pages, page, ws, wsb, handle)
-    if rc:
-        _check("ip_kv4_append", rc)
+    _, T, H, dh = k.shape
+    _need(v, "v", k.dtype, k.shape, k.device)
+    if start is None:
+        raise TypeError("start must be a CUDA tensor")
+    B, (n_pages, heads, page, width), (pst, pct), ws, handle = _kv4_args(
+        k, cache, page_table, workspace, 256, (start, count), ("k", "start", "count"), stream)
+    if heads != H:
+        raise ValueError(f"cache holds {heads} heads, not {H}")
+    ks, vs = _strides(k, "k"), _strides(v, "v")
+    _kv4_run("ip_kv4_append", lambda w, st: _lib.ip_kv4_append(
+        k.data_ptr(), v.data_ptr(), code, ks, vs, pst, pct, B, T, H, dh, page_table.data_ptr(), width,
+        cache.data_ptr(), n_pages, page, w.data_ptr(), w.numel(), st), handle, k.device, stream, ws, 256)
     return cache
 
 
@@ -902,23 +1010,21 @@ def kv4_read(cache, start, page_table, T: int, *, count=None, dtype=None, out=No
     (k, v), each [B, T, H, 128] of `dtype` (bfloat16 unless out gives it), zeros in rows
     t >= count[b].  out: such a pair, contiguous.  Arguments as kv4_append."""
     import torch
-    B = start.shape[0] if start.dim() == 1 else -1
-    n_pages, H, page, width = _kv4(cache, page_table, B)
-    dev = cache.device
-    pst = _dense(start, "start", torch.int32, (B,), dev)
-    pct = None if count is None else _dense(count, "count", torch.int32, (B,), dev)
-    shape = (B, T, H, IP_DH)
+    B, (n_pages, H, page, width), (pst, pct), ws, handle = _kv4_args(
+        _need(start, "start").numel(), cache, page_table, workspace, 256, (start, count),
+        ("", "start", "count"), stream)
+    dev, shape = cache.device, (B, T, H, IP_DH)
     dtype = dtype or (torch.bfloat16 if out is None else out[0].dtype)
     code = _dtype_code(dtype)
-    with _On(dev, stream) as handle:
+
+    def call(w, st):
+        nonlocal out
         if out is None:
             out = torch.empty(shape, dtype=dtype, device=dev), torch.empty(shape, dtype=dtype, device=dev)
         pk, pv = _dense(out[0], "out[0]", dtype, shape, dev), _dense(out[1], "out[1]", dtype, shape, dev)
-        workspace, ws, wsb = _status_space(workspace, dev)
-        rc = (_lib or load()).ip_kv4_read(cache.data_ptr(), n_pages, page, page_table.data_ptr(), width, pst,
-                                          pct, B, T, H, IP_DH, pk, pv, code, ws, wsb, handle)
-    if rc:
-        _check("ip_kv4_read", rc)
+        return _lib.ip_kv4_read(cache.data_ptr(), n_pages, page, page_table.data_ptr(), width, pst, pct, B, T,
+                                H, IP_DH, pk, pv, code, w.data_ptr(), w.numel(), st)
+    _kv4_run("ip_kv4_read", call, handle, dev, stream, ws, 256)
     return out
 
 
@@ -941,31 +1047,33 @@ def kv4_attention(q, lengths, page_table, cache, *, count=None, causal: bool = T
     the table can hold); a close one splits the work better.  Returns [B, T, H, 128] of
     q's type.  workspace: a zero-filled uint8 tensor of kv4_attention_workspace_bytes(B, T,
     H, Hkv, max_len).  Asynchronous on `stream`."""
-    import torch
-    if _need(q, "q").dim() != 4 or q.shape[3] != IP_DH:
-        raise ValueError(f"q must have shape (B, T, H, 128), got {tuple(q.shape)}")
-    if q.dtype not in (torch.float16, torch.bfloat16):
+    code = _dtype_code(_need(q, "q").dtype, "q")
+    if code == 0:
         raise TypeError(f"q must be float16 or bfloat16, got {q.dtype}")
-    B, T, H, dh = q.shape
-    dev = q.device
-    n_pages, Hkv, page, width = _kv4(_need(cache, "cache", None, None, dev), page_table, B)
+    if q.dim() != 4 or q.shape[3] != IP_DH:
+        raise ValueError(f"q must have shape (B, T, H, 128), got {tuple(q.shape)}")
+    _, T, H, dh = q.shape
+    if lengths is None:
+        raise TypeError("lengths must be a CUDA tensor")
+    B, (n_pages, Hkv, page, width), (pln, pct), ws, handle = _kv4_args(
+        q, cache, page_table, workspace, 0, (lengths, count), ("q", "lengths", "count"), stream)
     if max_len is None:
         max_len = width * page
-    pln = _dense(lengths, "lengths", torch.int32, (B,), dev)
-    pct = None if count is None else _dense(count, "count", torch.int32, (B,), dev)
-    lib = _lib or load()
-    with _On(dev, stream) as handle:
+    qs = _strides(q, "q")
+    dev = q.device
+    if scale is None:
+        scale = dh ** -0.5
+
+    def call(w, st):
+        nonlocal out
         if out is None:
-            out = torch.empty((B, T, H, dh), dtype=q.dtype, device=dev)
-        po = _dense(out, "out", q.dtype, (B, T, H, dh), dev)
-        size = 0 if workspace is not None else kv4_attention_workspace_bytes(B, T, H, Hkv, max_len)
-        workspace, ws, wsb = _status_space(workspace, dev, size)
-        rc = lib.ip_kv4_attention(
-            q.data_ptr(), 1 if q.dtype == torch.float16 else 2, _strides(q, "q"), pln, pct, 1 if causal else 0,
-            dh ** -0.5 if scale is None else scale, B, T, H, Hkv, dh, max_len, page_table.data_ptr(), width,
-            cache.data_ptr(), n_pages, page, po, ws, wsb, handle)
-    if rc:
-        _check("ip_kv4_attention", rc)
+            out = _Torch.empty(q.shape, dtype=q.dtype, device=dev)
+        po = _dense(out, "out", q.dtype, q.shape, dev)
+        return _lib.ip_kv4_attention(q.data_ptr(), code, qs, pln, pct, 1 if causal else 0, scale, B, T, H, Hkv, dh,
+                                     max_len, page_table.data_ptr(), width, cache.data_ptr(), n_pages, page, po,
+                                     w.data_ptr(), w.numel(), st)
+    size = 0 if ws is not None else kv4_attention_workspace_bytes(B, T, H, Hkv, max_len)
+    _kv4_run("ip_kv4_attention", call, handle, dev, stream, ws, size)
     return out
 
 

@@ -7,6 +7,8 @@
 
 #include <cuda_runtime.h>
 
+#include <mutex>
+
 namespace {
 
 bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
@@ -48,32 +50,33 @@ bool strides_ok(const long long *s) {
     return true;
 }
 
-// How the attention cuts its keys: chunks of a multiple of 64 tokens, at least 64, so
-// that the grid has about PLAN_CTAS CTAs however few the sequences and heads are.  The
-// plan depends on the call's sizes alone, never on the lengths.
-constexpr long long PLAN_CTAS = 4 * 3 * 152;
+// How the attention deals its work: one wave of CTAs (as many as fit on 152 SMs) in equal shares, or a CTA per item where there are too many row tiles to
+// sum up.  The plan depends on the call's sizes alone.
+constexpr long long SMS = 152;
 struct Plan {
-    int nt, tiles, chunk, chunks;
-    long long items;
-    size_t bytes;
+    int nt, tiles;
+    bool split;
+    long long ctas;
+    size_t open_bytes, bytes;
 };
 bool plan_of(int B, int T, int H, int Hkv, int max_len, Plan *p) {
     const long long rows = static_cast<long long>(H / Hkv) * T;
     if (rows > (1ll << 24)) return false;
     p->nt = rows > 8 ? 2 : 1;
     p->tiles = static_cast<int>((rows + 8 * p->nt - 1) / (8 * p->nt));
-    p->items = static_cast<long long>(B) * Hkv * p->tiles;
-    if (p->items > 0x7fffffffll) return false;
-    const long long len = max_len < 1 ? 1 : max_len;
-    long long chunk = (len * p->items / PLAN_CTAS + 63) / 64 * 64;
-    if (chunk < 64) chunk = 64;
-    if ((len + chunk - 1) / chunk > 65535) chunk = (len / 65535 + 64) / 64 * 64;
-    if (chunk > len) chunk = (len + 63) / 64 * 64;
-    p->chunk = static_cast<int>(chunk);
-    p->chunks = static_cast<int>((len + chunk - 1) / chunk);
+    const long long tiles = static_cast<long long>(B) * p->tiles, items = tiles * Hkv;
+    const long long units = max_len < ipv::UNIT ? 1 : (max_len + ipv::UNIT - 1ll) / ipv::UNIT;
+    if (items > 0x7fffffffll || items * (units + ipv::OVER) > 0x7fffffffll) return false;
+    p->split = tiles <= ipv::MAX_SCAN && units > 1;
+    p->ctas = items;
+    p->open_bytes = 0;
     p->bytes = 256;
-    if (p->chunks > 1)
-        p->bytes += static_cast<size_t>(p->items) * p->chunks * 8 * p->nt * ipv::PART * sizeof(float);
+    if (p->split) {
+        const long long wave = SMS * (p->nt == 1 ? ipv::CTAS_8 : ipv::CTAS_16);
+        p->ctas = items * units < wave ? items * units : wave;
+        p->open_bytes = (static_cast<size_t>(p->ctas) * sizeof(int2) + 255) / 256 * 256;
+        p->bytes += p->open_bytes + static_cast<size_t>(p->ctas) * 2 * 8 * p->nt * ipv::PART * sizeof(float);
+    }
     return true;
 }
 
@@ -82,13 +85,35 @@ bool attention_shape_ok(int B, int T, int H, int Hkv, int max_len) {
            H % Hkv == 0 && max_len >= 0 && max_len <= IP_KV4_MAX_LEN;
 }
 
+std::mutex g_mu;
+
+template <typename T, int NT, int PAGE>
+int launch_pages(const ipv::AttParams &prm, const Plan &p, cudaStream_t st) {
+    static bool set[64] = {false};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return IP_ERR_CUDA;
+    auto *fn = ipv::kv4_attention_kernel<T, NT, PAGE>;
+    constexpr int smem = ipv::smem_bytes(8 * NT);
+    {
+        std::lock_guard<std::mutex> lock(g_mu);
+        if (!set[dev]) {
+            if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+                return IP_ERR_CUDA;
+            set[dev] = true;
+        }
+    }
+    return launched(iph::launch_pdl(fn, dim3(static_cast<unsigned>(p.ctas)), dim3(ipv::ATT_THREADS), smem, st, prm));
+}
+
 template <typename T, int NT>
 int launch_attention(const ipv::AttParams &prm, const Plan &p, cudaStream_t st) {
-    const dim3 grid(static_cast<unsigned>(p.items), static_cast<unsigned>(p.chunks)), block(ipv::ATT_THREADS);
-    int rc = launched(iph::launch_pdl(ipv::kv4_attention_kernel<T, NT>, grid, block, 0, st, prm));
-    if (rc != IP_OK || p.chunks == 1) return rc;
-    const dim3 rows(static_cast<unsigned>(p.items), 8 * NT);
-    return launched(iph::launch_pdl(ipv::kv4_join_kernel<T, NT>, rows, block, 0, st, prm));
+    const int rc = prm.pages.shift == 4 ? launch_pages<T, NT, 16>(prm, p, st)
+                                        : (prm.pages.shift == 5 ? launch_pages<T, NT, 32>(prm, p, st)
+                                                                : launch_pages<T, NT, 64>(prm, p, st));
+    if (rc != IP_OK || !p.split) return rc;
+    const int r = prm.G * prm.T < 8 * NT ? prm.G * prm.T : 8 * NT;      // rows that an item can have
+    const dim3 rows(static_cast<unsigned>(p.ctas), static_cast<unsigned>(r));
+    return launched(iph::launch_pdl(ipv::kv4_join_kernel<T, NT>, rows, dim3(ipv::ATT_THREADS), 0, st, prm));
 }
 
 }  // namespace
@@ -199,12 +224,12 @@ int ip_kv4_attention(const void *q, int dtype, const long long *q_strides, const
     prm.G = H / Hkv;
     prm.causal = causal;
     prm.max_len = max_len < max_pages * page ? max_len : max_pages * page;
-    prm.chunk = p.chunk;
-    prm.chunks = p.chunks;
     prm.tiles = p.tiles;
+    prm.split = p.split ? 1 : 0;
     prm.scale_log2 = scale * 1.44269504088896f;
     prm.pages = pages_of(page_table, max_pages, cache, n_pages, page, Hkv);
-    prm.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + 256);
+    prm.open = reinterpret_cast<int2 *>(static_cast<char *>(workspace) + 256);
+    prm.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + 256 + p.open_bytes);
     prm.err = static_cast<int *>(workspace);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     if (dtype == IP_F16)

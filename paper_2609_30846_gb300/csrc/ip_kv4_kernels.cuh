@@ -208,17 +208,26 @@ __global__ void __launch_bounds__(ROW_THREADS) kv4_read_kernel(const RowParams p
 // Softmax: running maximum and sum in f32, per warp over its own tokens (16 at a time).
 //
 // Output: p times the V scale, relative to the running largest exponent of the V scales
-// and times 2^13, rounds to fp16 (half a step 2^-11; terms below 2^-27 of the largest fade
+// and times 2^HEAD, rounds to fp16 (half a step 2^-11; terms below 2^-23 of the largest fade
 // out gradually): the codes enter exactly as u - 8, and the sums are f32.  The
 // rounding is below that of a bf16 output and no worse than that of an fp16 one.
 //
-// The warps of a CTA merge in shared memory, the chunks of an item through the workspace
-// in a second kernel, in order (so the result does not depend on the schedule, and the
-// workspace carries nothing from one call to the next).
+// Split: the keys of all items in a row, cut into units of 128, are dealt in equal shares to
+// one wave of CTAs, whatever the lengths: each CTA sums up the lengths to find where its
+// share begins.  A share may end one item, hold some and begin another; only the first and
+// the last of its parts can be parts of an item, and these two go to the workspace, where
+// a second kernel joins them in order.  (Equal chunks of every item instead, 912 of them for
+// 608 CTAs at a time: 64 sequences of 4096 tokens, 8 heads: 84 us; ragged to 8192: 102 us.)
+// The workspace carries nothing from one call to the next.  The warps of a CTA merge in
+// shared memory.
 
 constexpr int ATT_WARPS = 4;
 constexpr int ATT_THREADS = 32 * ATT_WARPS;
-constexpr int PART = DH + 2;                  // floats of a partial row: output, max, sum
+constexpr int CTAS_8 = 3, CTAS_16 = 2;        // CTAs on an SM with 8 and 16 rows
+constexpr int UNIT = 128;                     // keys of a unit of work: 32 to a warp
+constexpr int OVER = 3;
+constexpr int MAX_SCAN = 2048;                // row tiles of all sequences that a CTA will sum up
+constexpr int PART = DH + 4;                  // floats of a partial row: output, maximum, sum, two unused
 
 struct AttParams {
     const void *q;
@@ -226,26 +235,26 @@ struct AttParams {
     long long qs[3];
     const int32_t *lengths, *count;
     int B, T, H, G;                           // H cache heads, G query heads to each
-    int causal, max_len, chunk, chunks;       // tokens of a chunk, chunks an item has at most
+    int causal, max_len;
     int tiles;                                // row tiles of (b, h)
+    int split;                                // 0: a CTA per item
     float scale_log2;                         // softmax scale times log2 e
     Pages pages;
-    float *part;
+    int2 *open;                               // [CTA]: item that its last part leaves open (-1: none), CTAs
+    float *part;                              // [CTA][2][R][PART]
     int *err;
 };
 
-// A work item: the 8 NT query rows `tile` of cache head h of sequence b.
+// A work item: the R = 8 NT query rows of tile e mod tiles of sequence e / tiles, cache head h.
 struct Item {
     int b, h, row0, rows;
     int n, cnt;               // cached tokens, query tokens
     int kv_end, kv_full;      // keys that some row sees; that all rows see which see any
-    int nchunks;
 
-    __device__ Item(const AttParams &p, unsigned item, int R) {
-        const unsigned bh = item / static_cast<unsigned>(p.tiles);
-        const int tile = static_cast<int>(item - bh * p.tiles);
-        b = static_cast<int>(bh / static_cast<unsigned>(p.H));
-        h = static_cast<int>(bh - static_cast<unsigned>(b) * p.H);
+    __device__ Item(const AttParams &p, int e, int head, int R) {
+        b = static_cast<int>(static_cast<unsigned>(e) / static_cast<unsigned>(p.tiles));
+        h = head;
+        const int tile = e - b * p.tiles;
         n = p.lengths[b];
         n = n < 0 ? 0 : (n > p.max_len ? p.max_len : n);
         cnt = p.count ? p.count[b] : p.T;
@@ -256,9 +265,9 @@ struct Item {
         kv_end = t_last < t_lo ? 0 : (p.causal ? n - cnt + t_last + 1 : n);
         kv_end = kv_end < 0 ? 0 : kv_end;
         kv_full = p.causal ? n - cnt + t_lo + 1 : n;
-        nchunks = (kv_end + p.chunk - 1) / p.chunk;
-        nchunks = nchunks < 1 ? 1 : nchunks;
     }
+    // its work: units of 128 keys, one at least (its rows have to be written)
+    __device__ int units() const { return kv_end <= UNIT ? 1 : (kv_end + UNIT - 1) / UNIT; }
     // keys that a row sees: the first limit(row) positions
     __device__ int limit(const AttParams &p, int row) const {
         const int t = (row0 + row) / p.G;
@@ -281,7 +290,15 @@ __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, u
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+// The same with d = (c0, c1, c0, c1) + A B.
+__device__ __forceinline__ void mma16_from(float (&d)[4], const float (&c)[2], uint32_t a0, uint32_t a1,
+                                           uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9},"
+        " {%10,%11,%10,%11};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {      // of an 8 x 8 matrix of 16-bit values
     uint32_t r;
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
     return r;
@@ -317,41 +334,190 @@ __device__ __forceinline__ float row_value(int limit, float acc, float sum) {
     return limit > 0 && sum != 0.0f ? __fdiv_rn(acc, sum) : 0.0f;
 }
 
-// What a lane reads of 16 tokens.  Row i of the score MMA is token i / 2 + 4 (i & 1) of its
-// half, so that the transposed probabilities of lane (g, t4) belong to tokens t4, t4 + 4,
-// t4 + 8, t4 + 12.
-struct Batch {
-    uint4 k[2];
-    uint2 ks[2], v[4], vs[4];
-};
+// 32 tokens of a warp in shared memory: K codes, V codes, K scales, V scales, copied as they
+// lie in their pages, STAGES deep.
+constexpr int STAGES = 2;
+constexpr int HEAD = 9, SLACK = 4;      // p s / 2^e < 2^(SLACK + 1), so its fp16 value is below 2^14
+constexpr int BATCH = 32, BATCH_BYTES = BATCH * ROW_BYTES;
+constexpr int RING = STAGES * BATCH_BYTES;
+__host__ __device__ constexpr int row_floats(int R) { return R * (DH + 2); }              // [R][DH], then maximum and sum [R][2]
+__host__ __device__ constexpr int smem_bytes(int R) { return ATT_WARPS * (RING + row_floats(R) * 4); }
+constexpr int B_V = BATCH * 64, B_KS = 2 * BATCH * 64, B_VS = B_KS + BATCH * 8;
 
-template <typename T, int NT>
-__global__ void __launch_bounds__(ATT_THREADS, NT == 1 ? 3 : 2) kv4_attention_kernel(const AttParams prm) {
+template <int D = 0, int S = 0>
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0+%2], [%1+%3], 16;" ::"r"(dst), "l"(src), "n"(D), "n"(S)
+                 : "memory");
+}
+template <int O>
+__device__ __forceinline__ uint4 at128(const uint8_t *p) { return *reinterpret_cast<const uint4 *>(p + O); }
+template <int O>
+__device__ __forceinline__ uint2 at64(const uint8_t *p) { return *reinterpret_cast<const uint2 *>(p + O); }
+
+template <typename T, int NT, int PAGE>
+__global__ void __launch_bounds__(ATT_THREADS, NT == 1 ? CTAS_8 : CTAS_16) kv4_attention_kernel(const AttParams prm) {
     constexpr int R = 8 * NT;
-    __shared__ float s_o[ATT_WARPS][R][DH], s_ml[ATT_WARPS][R][2];
+    extern __shared__ __align__(128) uint8_t s_mem[];     // per warp its ring, then its rows
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g8 = lane >> 2, t4 = lane & 3;
     pdl_launch_dependents();
     pdl_wait();
 
-    const int chunk = blockIdx.y;
-    const Item it(prm, blockIdx.x, R);
-    if (chunk >= it.nchunks) return;
-    if (chunk == 0 && threadIdx.x == 0 && prm.lengths[it.b] > prm.max_len) atomicOr(prm.err, ERR_PARAM);
-    const int b = it.b, h = it.h, row0 = it.row0, rows = it.rows, kv_end = it.kv_end;
-    const int begin = chunk * prm.chunk, end = kv_end < begin + prm.chunk ? kv_end : begin + prm.chunk;
-    const int shift = prm.pages.shift, page = 1 << shift;
-    const int32_t *table = prm.pages.table + static_cast<long long>(b) * prm.pages.max_pages;
-    auto limit = [&](int row) { return it.limit(prm, row); };
+    // this CTA's share: `left` units of all, from unit u0 of item (e, head) on
+    __shared__ int s_start[3], s_sum[ATT_WARPS];
+    int e, head, u0 = 0, share = 0, left = 0x7fffffff, over = 0;
+    if (prm.split) {
+        const int tid = threadIdx.x, E = prm.B * prm.tiles, per = (E + ATT_THREADS - 1) / ATT_THREADS;
+        int mine = 0;
+        for (int i = 0; i < per; ++i)
+            if (tid * per + i < E) mine += Item(prm, tid * per + i, 0, R).units() * prm.H;
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        if (lane == 31) s_sum[warp] = upto;
+        __syncthreads();
+        int total = 0;
+#pragma unroll
+        for (int w = 0; w < ATT_WARPS; ++w) {
+            if (w < warp) upto += s_sum[w];
+            total += s_sum[w];
+        }
+        // beginning an item takes about as long as OVER units: it is counted so, unless there
+        // is a CTA for every unit
+        if (total > static_cast<int>(gridDim.x)) {
+            over = OVER;
+            total += over * E * prm.H;
+            const int items = (tid * per < E ? (E - tid * per < per ? E - tid * per : per) : 0) * prm.H;
+            mine += over * items;
+            upto += over * prm.H * (tid * per + per < E ? tid * per + per : E);
+        }
+        share = (total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x);
+        const long long pos = static_cast<long long>(blockIdx.x) * share;
+        if (tid == 0) prm.open[blockIdx.x] = make_int2(-1, 0);
+        if (pos >= total) return;
+        left = total - pos < share ? static_cast<int>(total - pos) : share;
+        if (pos >= upto - mine && pos < upto) {
+            int at = upto - mine;
+            for (int i = 0; i < per; ++i) {
+                const int u = over + Item(prm, tid * per + i, 0, R).units();
+                if (pos < at + u * prm.H) {
+                    s_start[0] = tid * per + i;
+                    s_start[1] = (static_cast<int>(pos) - at) / u;
+                    s_start[2] = (static_cast<int>(pos) - at) % u;
+                    break;
+                }
+                at += u * prm.H;
+            }
+        }
+        __syncthreads();
+        e = s_start[0];
+        head = s_start[1];
+        u0 = s_start[2] - over;       // below 0: inside what the item's beginning is counted as
+    } else {
+        e = static_cast<int>(blockIdx.x / static_cast<unsigned>(prm.H));
+        head = static_cast<int>(blockIdx.x - static_cast<unsigned>(e) * prm.H);
+    }
 
-    // query fragments, group sums and per-row constants
+    // the part of item `it` that the share holds: units u0 .. u1 - 1; false if it ends before
+    // the item's first key
+    Item it(prm, e, head, R);
+    int units = it.units(), u1 = 0;
+    auto take = [&]() {
+        u1 = units - u0 <= left ? units : u0 + left;
+        left -= u1 - u0;
+        u0 = u0 < 0 ? 0 : u0;
+        if (u0 == 0 && u1 > 0 && head == 0 && threadIdx.x == 0 &&
+            (prm.lengths[it.b] > prm.max_len || (it.kv_end > 0 && prm.pages.n_pages == 0)))
+            atomicOr(prm.err, ERR_PARAM);
+        return u1 > 0;
+    };
+    if (!take()) return;
+
+    // the warp's batches: 32 tokens every 128; the copies run STAGES - 1 ahead of the products, the
+    // page ids one more
+    constexpr int STEP = BATCH * ATT_WARPS;
+    uint8_t *const my_ring = s_mem + warp * RING;
+    const uint32_t ring = smem_u32(my_ring);
+    float *const my_rows = reinterpret_cast<float *>(s_mem + ATT_WARPS * RING) + warp * row_floats(R);
+    int ahead = 0, end = 0, slot = 0, pid[2] = {0, 0};
+    uint32_t use = 0;            // offset of the slot in use
+    uint32_t dead = 0;           // two bits per copied batch, the newest lowest: half without a page
+    const int32_t *table = nullptr;
+    auto pages_ahead = [&]() {
+        pid[0] = ahead < end ? table[static_cast<unsigned>(ahead) / PAGE] : 0;
+        pid[1] = PAGE == 16 && ahead + 16 < end ? table[static_cast<unsigned>(ahead) / PAGE + 1] : pid[0];
+    };
+    auto copy = [&]() {
+        dead <<= 2;
+        if (ahead < end) {
+            const bool bad0 = pid[0] < 0 || pid[0] >= prm.pages.n_pages;
+            const bool bad1 = pid[1] < 0 || pid[1] >= prm.pages.n_pages;
+            if (bad0 || bad1) {
+                dead |= (bad0 ? 1u : 0u) | (bad1 ? 2u : 0u);
+                if (lane == 0) atomicOr(prm.err, ERR_PARAM);
+            }
+            const uint32_t dst = ring + slot * BATCH_BYTES + lane * 16;
+            const long long stride = static_cast<long long>(prm.H) * (ROW_BYTES * PAGE);
+            const uint8_t *first = prm.pages.cache + it.h * (ROW_BYTES * PAGE);
+            if (PAGE == 16) {
+                // half a batch each from two pages; scales: a quarter of the lanes for K, K, V, V
+                const uint8_t *p0 = first + (bad0 ? 0 : pid[0]) * stride, *p1 = first + (bad1 ? 0 : pid[1]) * stride;
+                const uint8_t *c0 = p0 + lane * 16, *c1 = p1 + lane * 16;
+                copy16(dst, c0);
+                copy16<512, 512>(dst, c0);
+                copy16<1024>(dst, c1);
+                copy16<1536, 512>(dst, c1);
+                copy16<B_V, v_codes(PAGE)>(dst, c0);
+                copy16<B_V + 512, v_codes(PAGE) + 512>(dst, c0);
+                copy16<B_V + 1024, v_codes(PAGE)>(dst, c1);
+                copy16<B_V + 1536, v_codes(PAGE) + 512>(dst, c1);
+                copy16<B_KS>(dst, (lane & 8 ? p1 : p0) + (lane & 16 ? v_scales(PAGE) : k_scales(PAGE)) + (lane & 7) * 16);
+            } else {
+                const int o0 = ahead & (PAGE - 1);
+                const uint8_t *blk = first + (bad0 ? 0 : pid[0]) * stride + (o0 * 64 + lane * 16);
+                copy16(dst, blk);
+                copy16<512, 512>(dst, blk);
+                copy16<1024, 1024>(dst, blk);
+                copy16<1536, 1536>(dst, blk);
+                copy16<B_V, v_codes(PAGE)>(dst, blk);
+                copy16<B_V + 512, v_codes(PAGE) + 512>(dst, blk);
+                copy16<B_V + 1024, v_codes(PAGE) + 1024>(dst, blk);
+                copy16<B_V + 1536, v_codes(PAGE) + 1536>(dst, blk);
+                // K scales by lanes 0-15, V scales by lanes 16-31
+                copy16<B_KS>(dst, blk + ((lane < 16 ? k_scales(PAGE) : v_scales(PAGE) - 256) - o0 * 56));
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        ahead += STEP;
+        pages_ahead();
+        slot = slot + 1 == STAGES ? 0 : slot + 1;
+    };
+    auto start = [&]() {          // the first copies of a part
+        table = prm.pages.table + static_cast<long long>(it.b) * prm.pages.max_pages;
+        ahead = u0 * UNIT + warp * BATCH;
+        end = it.kv_end < u1 * UNIT ? it.kv_end : u1 * UNIT;
+        end = prm.pages.n_pages > 0 ? end : 0;
+        use = slot * BATCH_BYTES;
+        pages_ahead();
+#pragma unroll
+        for (int i = 0; i < STAGES - 1; ++i) copy();
+    };
+    start();
+
+    for (;;) {
+    const int b = it.b, h = it.h, row0 = it.row0, kv_end = it.kv_end, t_begin = u0 * UNIT + warp * BATCH, t_end = end;
+
+    // query fragments (row g8 of each eight), group sums and per-row constants (rows 2 t4, 2 t4 + 1)
     uint32_t qf[NT][4][4];
     float qsum[NT][4][2], rscale[NT][2];
     int lim[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int row = nt * 8 + g8;
-        const bool live = limit(row) > 0;
+        const bool live = it.limit(prm, row) > 0;
         float x[4][8], top = 0.0f;
         const int t = (row0 + row) / prm.G, g = (row0 + row) - t * prm.G;
         const T *src = static_cast<const T *>(prm.q) +
@@ -359,19 +525,18 @@ __global__ void __launch_bounds__(ATT_THREADS, NT == 1 ? 3 : 2) kv4_attention_ke
         const bool vec = (reinterpret_cast<uintptr_t>(src) & 15) == 0;
 #pragma unroll
         for (int gr = 0; gr < 4; ++gr) {
-            if (live) load8(src + 32 * gr + 8 * t4, vec, 8, x[gr]);
-            else
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[gr][i] = 0.0f;
+            for (int i = 0; i < 8; ++i) x[gr][i] = 0.0f;
+            if (live) load8(src + 32 * gr + 8 * t4, vec, 8, x[gr]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[gr][i]));
         }
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const int e = 268 - static_cast<int>(__float_as_uint(top) >> 23);
-        const int fe = e > 254 ? 254 : e;
+        const int ex = 268 - static_cast<int>(__float_as_uint(top) >> 23);
+        const int fe = ex > 254 ? 254 : ex;
         const float up = __uint_as_float(static_cast<uint32_t>(fe) << 23);
-        const float rs = ldexpf(prm.scale_log2, 24 - (fe - 127));
+        const float rs = fmaxf(ldexpf(prm.scale_log2, 24 - (fe - 127)), 0x1p-126f);   // > 0: -inf times it
         float sums[4];
 #pragma unroll
         for (int gr = 0; gr < 4; ++gr) {
@@ -396,12 +561,20 @@ __global__ void __launch_bounds__(ATT_THREADS, NT == 1 ? 3 : 2) kv4_attention_ke
 #pragma unroll
             for (int gr = 0; gr < 4; ++gr) qsum[nt][gr][i] = __shfl_sync(0xffffffffu, sums[gr], from);
             rscale[nt][i] = __shfl_sync(0xffffffffu, rs, from);
-            lim[nt][i] = limit(nt * 8 + 2 * t4 + i);
+            lim[nt][i] = it.limit(prm, nt * 8 + 2 * t4 + i);
         }
     }
 
-    const int tok = (g8 >> 1) + 4 * (g8 & 1);
-    float o[NT][8][4], m[NT][2], l[NT][2];
+    // Row i of the score MMA is token i / 2 of its eight for even i, 4 + (i / 2 ^ 1) for odd i: the
+    // 16-byte reads of neighbouring rows fall on different banks, and the transposed
+    // probabilities of lane (g8, t4) belong to the tokens t4 and 4 + (t4 ^ 1) of each eight.
+    const int tok = g8 & 1 ? 4 + ((g8 >> 1) ^ 1) : g8 >> 1, odd4 = 4 + (t4 ^ 1);
+    const uint8_t *at_k = my_ring + tok * 64 + t4 * 16, *at_s = my_ring + tok * 8;
+    const uint8_t *at_v = my_ring + t4 * 64 + g8 * 8, *at_vo = my_ring + odd4 * 64 + g8 * 8;
+    // m: the reference of the row's exponentials, mr: in units of log2.  It is raised to the
+    // maximum only when a score exceeds it by more than SLACK there (lift: the score that does):
+    // the probabilities reach 2^SLACK at most, and most batches skip the rescaling.
+    float o[NT][8][4], m[NT][2], mr[NT][2], l[NT][2], lift[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -409,274 +582,301 @@ __global__ void __launch_bounds__(ATT_THREADS, NT == 1 ? 3 : 2) kv4_attention_ke
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[nt][i][j] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) m[nt][i] = -INFINITY, l[nt][i] = 0.0f;
+        for (int i = 0; i < 2; ++i) {
+            m[nt][i] = lift[nt][i] = -INFINITY;
+            mr[nt][i] = l[nt][i] = 0.0f;
+        }
     }
     int ev = 16;          // running largest exponent field of the V scales
+    float norm = __uint_as_float((254u + HEAD - 16u) << 23);      // 2^(HEAD - (ev - 127))
+    uint32_t ev_top = (17u << 7) - 1u;                            // largest scale of that exponent
 
-    // page of a batch, -1 if there is none
-    auto page_of = [&](int t0) {
-        if (t0 >= end) return -1;
-        const int pid = table[t0 >> shift];
-        return pid >= 0 && pid < prm.pages.n_pages ? pid : -1;
-    };
-    auto load = [&](int t0, int pid, Batch &x) {
-        if (pid < 0) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) x.k[i] = make_uint4(0, 0, 0, 0), x.ks[i] = make_uint2(0, 0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x.v[i] = x.vs[i] = make_uint2(0, 0);
-            return;
-        }
-        const uint8_t *blk = prm.pages.cache + ((static_cast<long long>(pid) * prm.H + h) * ROW_BYTES << shift);
-        const int o0 = t0 & (page - 1);
-        const uint8_t *kc = blk + (o0 + tok) * 64 + t4 * 16, *ks = blk + k_scales(page) + (o0 + tok) * 8;
-        const uint8_t *vc = blk + v_codes(page) + (o0 + t4) * 64 + g8 * 8, *vs = blk + v_scales(page) + (o0 + t4) * 8;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            x.k[i] = ldg_stream128(kc + i * 512);
-            x.ks[i] = ldg_stream64(ks + i * 64);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x.v[i] = ldg_stream64(vc + i * 256);
-            x.vs[i] = ldg_stream64(vs + i * 32);
-        }
-    };
+    for (int t0 = t_begin; t0 < t_end; t0 += STEP) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+        __syncwarp();     // all lanes' copies have landed, and all have read the slot before
+        copy();
+        const uint32_t gone = (dead >> (2 * (STAGES - 1))) & 3u;       // this batch was copied so long ago
+        const bool full = t0 + BATCH <= it.kv_full && gone == 0;
 
-    auto compute = [&](int t0, int pid, const Batch &x) {
-        const bool dead = pid < 0;      // no such page: all masked
-        const bool full = t0 + 16 <= it.kv_full && !dead;
-        float s[NT][4];
+        // scores: rows 2 t4 and 2 t4 + 1 for the tokens tok, 8 + tok, 16 + tok, 24 + tok
+        float s[NT][8];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int hf = 0; hf < 2; ++hf) {
+            const uint4 k0 = hf ? at128<1024>(at_k + use) : at128<0>(at_k + use);
+            const uint4 k1 = hf ? at128<1536>(at_k + use) : at128<512>(at_k + use);
+            const uint2 c0 = hf ? at64<B_KS + 128>(at_s + use) : at64<B_KS>(at_s + use);
+            const uint2 c1 = hf ? at64<B_KS + 192>(at_s + use) : at64<B_KS + 64>(at_s + use);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[nt][i] = 0.0f;
+            for (int gr = 0; gr < 4; ++gr) {
+                const uint32_t w0 = gr == 0 ? k0.x : (gr == 1 ? k0.y : (gr == 2 ? k0.z : k0.w)), y0 = w0 >> 8;
+                const uint32_t w1 = gr == 0 ? k1.x : (gr == 1 ? k1.y : (gr == 2 ? k1.z : k1.w)), y1 = w1 >> 8;
+                const uint32_t s0 = gr < 2 ? c0.x : c0.y, s1 = gr < 2 ? c1.x : c1.y;
+                const float f0 = gr & 1 ? bf16_hi(s0) : bf16_lo(s0), f1 = gr & 1 ? bf16_hi(s1) : bf16_lo(s1);
 #pragma unroll
-        for (int gr = 0; gr < 4; ++gr) {
-            const uint32_t w0 = gr == 0 ? x.k[0].x : (gr == 1 ? x.k[0].y : (gr == 2 ? x.k[0].z : x.k[0].w));
-            const uint32_t w1 = gr == 0 ? x.k[1].x : (gr == 1 ? x.k[1].y : (gr == 2 ? x.k[1].z : x.k[1].w));
-            const uint32_t y0 = w0 >> 8, y1 = w1 >> 8;
-            const uint32_t sw0 = gr < 2 ? x.ks[0].x : x.ks[0].y, sw1 = gr < 2 ? x.ks[1].x : x.ks[1].y;
-            const float k0 = gr & 1 ? bf16_hi(sw0) : bf16_lo(sw0), k1 = gr & 1 ? bf16_hi(sw1) : bf16_lo(sw1);
+                for (int nt = 0; nt < NT; ++nt) {
+                    float acc[4], (&r)[8] = s[nt];
+                    mma16_from(acc, qsum[nt][gr], w0 & 0x000f000fu, w1 & 0x000f000fu, y0 & 0x000f000fu,
+                               y1 & 0x000f000fu, qf[nt][gr][0], qf[nt][gr][1]);
+                    mma16(acc, w0 & 0x00f000f0u, w1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u,
+                          qf[nt][gr][2], qf[nt][gr][3]);
+                    r[4 * hf] = gr == 0 ? f0 * acc[0] : fmaf(f0, acc[0], r[4 * hf]);
+                    r[4 * hf + 1] = gr == 0 ? f0 * acc[1] : fmaf(f0, acc[1], r[4 * hf + 1]);
+                    r[4 * hf + 2] = gr == 0 ? f1 * acc[2] : fmaf(f1, acc[2], r[4 * hf + 2]);
+                    r[4 * hf + 3] = gr == 0 ? f1 * acc[3] : fmaf(f1, acc[3], r[4 * hf + 3]);
+                }
+            }
+        }
+        uint2 vs[4] = {at64<B_VS>(at_s + use), at64<B_VS + 64>(at_s + use), at64<B_VS + 128>(at_s + use),
+                       at64<B_VS + 192>(at_s + use)};
+        if (!full) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                float acc[4] = {qsum[nt][gr][0], qsum[nt][gr][1], qsum[nt][gr][0], qsum[nt][gr][1]};
-                mma16(acc, w0 & 0x000f000fu, w1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu,
-                      qf[nt][gr][0], qf[nt][gr][1]);
-                mma16(acc, w0 & 0x00f000f0u, w1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u,
-                      qf[nt][gr][2], qf[nt][gr][3]);
-                s[nt][0] = fmaf(k0, acc[0], s[nt][0]);
-                s[nt][1] = fmaf(k0, acc[1], s[nt][1]);
-                s[nt][2] = fmaf(k1, acc[2], s[nt][2]);
-                s[nt][3] = fmaf(k1, acc[3], s[nt][3]);
+            for (int i = 0; i < 4; ++i) {
+                const int pos = t0 + 8 * i + tok;
+                const bool none = (gone >> (i >> 1)) & 1u;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        if (none || pos >= lim[nt][j]) s[nt][2 * i + j] = -INFINITY;
+                // V scales of tokens that no row sees may hold anything
+                if (none || pos >= kv_end) vs[i] = make_uint2(0, 0);
             }
         }
         bool raise = false;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[nt][i] *= rscale[nt][i & 1];
-            if (!full)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (dead || t0 + tok + 8 * (i >> 1) >= lim[nt][i & 1]) s[nt][i] = -INFINITY;
-            raise |= fmaxf(s[nt][0], s[nt][2]) > m[nt][0] || fmaxf(s[nt][1], s[nt][3]) > m[nt][1];
-        }
-        // V scales; those of tokens that no row sees may hold anything
-        uint2 vs[4];
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            vs[i] = x.vs[i];
-            if (!full && (dead || t0 + t4 + 4 * i >= kv_end)) vs[i] = make_uint2(0, 0);
-            top = __vmaxu2(top, __vmaxu2(vs[i].x, vs[i].y));
-        }
-        int et = static_cast<int>(max(top >> 16, top & 0xffffu) >> 7) & 0xff;
-        if (et == 255) {       // a NaN among them: it must not hide the others' range
-            et = 0;
+            for (int j = 0; j < 2; ++j)
+                raise |= fmaxf(fmaxf(s[nt][j], s[nt][2 + j]), fmaxf(s[nt][4 + j], s[nt][6 + j])) > lift[nt][j];
+        uint32_t top = __vimax3_u16x2(vs[0].x, vs[0].y, vs[1].x);
+        top = __vimax3_u16x2(__vimax3_u16x2(top, vs[1].y, vs[2].x), vs[2].y, vs[3].x);
+        top = __vimax3_u16x2(top, vs[3].y, 0u);
+        raise |= (top >> 16) > ev_top || (top & 0xffffu) > ev_top;
+        if (__any_sync(0xffffffffu, raise)) {
+            int et = ev;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t w = j < 2 ? vs[i].x : vs[i].y;
-                    const int f = static_cast<int>(w >> (j & 1 ? 23 : 7)) & 0xff;
+                for (int j = 0; j < 4; ++j) {     // a NaN (field 255) must not hide the others' range
+                    const int f = static_cast<int>((j < 2 ? vs[i].x : vs[i].y) >> (j & 1 ? 23 : 7)) & 0xff;
                     et = f < 255 && f > et ? f : et;
                 }
-        }
-        raise |= et > ev;
-        if (__any_sync(0xffffffffu, raise)) {
-            const int en = static_cast<int>(__reduce_max_sync(0xffffffffu, static_cast<unsigned>(et > ev ? et : ev)));
+            const int en = static_cast<int>(__reduce_max_sync(0xffffffffu, static_cast<unsigned>(et)));
             const float down = ev - en < -126 ? 0.0f : __uint_as_float(static_cast<uint32_t>(127 + ev - en) << 23);
             ev = en;
+            norm = __uint_as_float(static_cast<uint32_t>(254 + HEAD - ev) << 23);
+            ev_top = (static_cast<uint32_t>(ev + 1) << 7) - 1u;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float t = fmaxf(fmaxf(s[nt][i], s[nt][2 + i]), m[nt][i]);
+                for (int j = 0; j < 2; ++j) {
+                    float t = m[nt][j];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) t = fmaxf(t, s[nt][2 * i + j]);
                     t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
                     t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
                     t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
-                    const float a = t == -INFINITY ? 1.0f : fast_exp2(m[nt][i] - t);
-                    m[nt][i] = t;
-                    l[nt][i] *= a;
+                    const float tr = t == -INFINITY ? 0.0f : t * rscale[nt][j];
+                    const float a = m[nt][j] == -INFINITY ? 0.0f : fast_exp2(mr[nt][j] - tr);
+                    m[nt][j] = t;
+                    mr[nt][j] = tr;
+                    lift[nt][j] = t + __fdividef(static_cast<float>(SLACK), rscale[nt][j]);
+                    l[nt][j] *= a;
                     const float ad = a * down;
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) o[nt][c][i] *= ad, o[nt][c][2 + i] *= ad;
+                    for (int c = 0; c < 8; ++c) o[nt][c][j] *= ad, o[nt][c][2 + j] *= ad;
                 }
         }
-        float p[NT][4];           // probability of query row 8 nt + g8 for tokens t4 + 4 i
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const float m0 = m[nt][0] == -INFINITY ? 0.0f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.0f : m[nt][1];
-            float e[4];
+        for (int hf = 0; hf < 2; ++hf) {
+            float p[NT][4];           // norm times the probabilities
 #pragma unroll
-            for (int i = 0; i < 4; ++i) e[i] = fast_exp2(s[nt][i] - (i & 1 ? m1 : m0));
-            l[nt][0] += e[0] + e[2];
-            l[nt][1] += e[1] + e[3];
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint32_t a = __float_as_uint(e[2 * i]), c = __float_as_uint(e[2 * i + 1]);
-                const uint32_t lo = transpose8(__byte_perm(a, c, 0x5410)), hi = transpose8(__byte_perm(a, c, 0x7632));
-                p[nt][2 * i] = __uint_as_float(__byte_perm(lo, hi, 0x5410));
-                p[nt][2 * i + 1] = __uint_as_float(__byte_perm(lo, hi, 0x7632));
+                for (int i = 0; i < 4; ++i) {
+                    const float e1 = fast_exp2(fmaf(s[nt][4 * hf + i], rscale[nt][i & 1], -mr[nt][i & 1]));
+                    l[nt][i & 1] += e1;
+                    p[nt][i] = e1 * norm;
+                }
+            const uint2 v0 = hf ? at64<B_V + 1024>(at_v + use) : at64<B_V>(at_v + use);
+            const uint2 v1 = hf ? at64<B_V + 1024>(at_vo + use) : at64<B_V>(at_vo + use);
+            const uint2 v2 = hf ? at64<B_V + 1536>(at_v + use) : at64<B_V + 512>(at_v + use);
+            const uint2 v3 = hf ? at64<B_V + 1536>(at_vo + use) : at64<B_V + 512>(at_vo + use);
+#pragma unroll
+            for (int gr = 0; gr < 4; ++gr) {
+                const uint32_t x0 = gr < 2 ? vs[2 * hf].x : vs[2 * hf].y, x1 = gr < 2 ? vs[2 * hf + 1].x : vs[2 * hf + 1].y;
+                const float f0 = gr & 1 ? bf16_hi(x0) : bf16_lo(x0), f1 = gr & 1 ? bf16_hi(x1) : bf16_lo(x1);
+                const uint32_t sel = gr & 1 ? 0x7632 : 0x5410;
+                const uint32_t a = gr < 2 ? __byte_perm(v0.x, v1.x, sel) : __byte_perm(v0.y, v1.y, sel);
+                const uint32_t c = gr < 2 ? __byte_perm(v2.x, v3.x, sel) : __byte_perm(v2.y, v3.y, sel);
+                const uint32_t a8 = a >> 8, c8 = c >> 8;
+                const uint32_t a0 = centred_lo(a), a1 = centred_hi(a), a2 = centred_lo(c), a3 = centred_hi(c);
+                const uint32_t d0 = centred_lo(a8), d1 = centred_hi(a8), d2 = centred_lo(c8), d3 = centred_hi(c8);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    // p s rounded to fp16, then tokens against rows turned into the MMA's order
+                    const uint32_t b0 = transpose8(pack_half2(p[nt][0] * f0, p[nt][1] * f0));
+                    const uint32_t b1 = transpose8(pack_half2(p[nt][2] * f1, p[nt][3] * f1));
+                    mma16(o[nt][2 * gr], a0, a1, a2, a3, b0, b1);
+                    mma16(o[nt][2 * gr + 1], d0, d1, d2, d3, b0, b1);
+                }
             }
         }
-        const float norm = __uint_as_float(static_cast<uint32_t>(267 - ev) << 23);    // 2^(13 - (ev - 127))
-#pragma unroll
-        for (int gr = 0; gr < 4; ++gr) {
-            float f[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t w = gr < 2 ? vs[i].x : vs[i].y;
-                f[i] = (gr & 1 ? bf16_hi(w) : bf16_lo(w)) * norm;
-            }
-            const uint32_t sel = gr & 1 ? 0x7632 : 0x5410;
-            const uint32_t a = gr < 2 ? __byte_perm(x.v[0].x, x.v[1].x, sel) : __byte_perm(x.v[0].y, x.v[1].y, sel);
-            const uint32_t c = gr < 2 ? __byte_perm(x.v[2].x, x.v[3].x, sel) : __byte_perm(x.v[2].y, x.v[3].y, sel);
-            const uint32_t a8 = a >> 8, c8 = c >> 8;
-            const uint32_t a0 = centred_lo(a), a1 = centred_hi(a), a2 = centred_lo(c), a3 = centred_hi(c);
-            const uint32_t d0 = centred_lo(a8), d1 = centred_hi(a8), d2 = centred_lo(c8), d3 = centred_hi(c8);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const uint32_t b0 = pack_half2(p[nt][0] * f[0], p[nt][1] * f[1]);
-                const uint32_t b1 = pack_half2(p[nt][2] * f[2], p[nt][3] * f[3]);
-                mma16(o[nt][2 * gr], a0, a1, a2, a3, b0, b1);
-                mma16(o[nt][2 * gr + 1], d0, d1, d2, d3, b0, b1);
-            }
-        }
-    };
-
-    {
-        int t0 = begin + warp * 16;
-        constexpr int STEP = 16 * ATT_WARPS;
-        // the pages run two batches ahead of the products, the rows one
-        int pid = page_of(t0), pid1 = page_of(t0 + STEP);
-        Batch x;
-        if (t0 < end) load(t0, pid, x);
-        while (t0 < end) {
-            const int pid2 = page_of(t0 + 2 * STEP);
-            Batch y;
-            if (t0 + STEP < end) load(t0 + STEP, pid1, y);
-            if (pid < 0 && lane == 0) atomicOr(prm.err, ERR_PARAM);
-            compute(t0, pid, x);
-            x = y;
-            pid = pid1;
-            pid1 = pid2;
-            t0 += STEP;
-        }
+        use = use + BATCH_BYTES == STAGES * BATCH_BYTES ? 0 : use + BATCH_BYTES;
     }
 
-    // a warp's rows to shared memory: output over 2^(ev - 140), maximum, sum
+    // the share's next part: its first copies run while this part's rows are joined
+    const Item done = it;
+    const int d0 = u0, d1 = u1, d_units = units, d_item = e * prm.H + head;
+    bool more = prm.split && u1 == units && left > 0;
+    if (more) {
+        u0 = -over;
+        if (++head == prm.H) head = 0, ++e;
+        it = Item(prm, e, head, R);
+        units = it.units();
+        more = take();
+        __syncwarp();
+        if (more) start();
+    }
+    __syncthreads();              // the rows before these have been read
+
+    // a warp's rows to shared memory: output over norm, maximum, sum
     {
-        const float unit = ldexpf(1.0f, ev - 140);
+        const float unit = ldexpf(1.0f, ev - 127 - HEAD);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int row = nt * 8 + 2 * t4 + i;
-                float s = l[nt][i];
-                s += __shfl_xor_sync(0xffffffffu, s, 4);
-                s += __shfl_xor_sync(0xffffffffu, s, 8);
-                s += __shfl_xor_sync(0xffffffffu, s, 16);
-                if (g8 == 0) s_ml[warp][row][0] = m[nt][i], s_ml[warp][row][1] = s;
+                float sum = l[nt][i];
+                sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+                if (g8 == 0) {
+                    float *ml = my_rows + R * DH + 2 * (nt * 8 + 2 * t4 + i);
+                    ml[0] = m[nt][i] == -INFINITY ? -INFINITY : mr[nt][i];
+                    ml[1] = sum;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int c = 0; c < 8; ++c)      // m-tile c: channels 32 (c / 2) + 4 g8 + 2 (c & 1), + 1
-                    *reinterpret_cast<float2 *>(&s_o[warp][row][32 * (c >> 1) + 4 * g8 + 2 * (c & 1)]) =
-                        make_float2(o[nt][c][i] * unit, o[nt][c][2 + i] * unit);
-            }
+                    *reinterpret_cast<float2 *>(my_rows + (nt * 8 + 2 * t4 + i) * DH + 32 * (c >> 1) + 4 * g8 +
+                                                2 * (c & 1)) = make_float2(o[nt][c][i] * unit, o[nt][c][2 + i] * unit);
+        }
     }
     __syncthreads();
 
     const int d = threadIdx.x;                    // one channel a thread
-    for (int row = 0; row < rows; ++row) {
+    const bool whole = d0 == 0 && d1 == d_units;
+    const float *all_rows = reinterpret_cast<const float *>(s_mem + ATT_WARPS * RING);
+    for (int row = 0; row < done.rows; ++row) {
+        const float *ml = all_rows + R * DH + 2 * row, *src = all_rows + row * DH + d;
         float mx = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < ATT_WARPS; ++w) mx = fmaxf(mx, s_ml[w][row][0]);
+        for (int w = 0; w < ATT_WARPS; ++w) mx = fmaxf(mx, ml[w * row_floats(R)]);
         const float ref = mx == -INFINITY ? 0.0f : mx;
         float acc = 0.0f, sum = 0.0f;
 #pragma unroll
         for (int w = 0; w < ATT_WARPS; ++w) {
-            const float a = fast_exp2(s_ml[w][row][0] - ref);
-            acc += a * s_o[w][row][d];
-            sum += a * s_ml[w][row][1];
+            const float a = fast_exp2(ml[w * row_floats(R)] - ref);
+            acc += a * src[w * row_floats(R)];
+            sum += a * ml[w * row_floats(R) + 1];
         }
-        if (it.nchunks == 1) {
-            it.out<T>(prm, row)[d] = from_f32<T>(row_value(it.limit(prm, row), acc, sum));
+        if (whole) {
+            done.out<T>(prm, row)[d] = from_f32<T>(row_value(done.limit(prm, row), acc, sum));
         } else {
-            float *dst = prm.part + ((static_cast<long long>(blockIdx.x) * prm.chunks + chunk) * R + row) * PART;
+            float *dst = prm.part + ((static_cast<long long>(blockIdx.x) * 2 + (d0 > 0 ? 0 : 1)) * R + row) * PART;
             dst[d] = acc;
             if (d == 0) dst[DH] = mx, dst[DH + 1] = sum;
         }
     }
+    // the item goes on in the next CTAs: the one where it begins says so
+    if (d1 < d_units && d0 == 0 && threadIdx.x == 0)
+        prm.open[blockIdx.x] = make_int2(d_item, 1 + (d_units - d1 + share - 1) / share);
+    if (!more) return;
+    }
 }
 
-// The chunks of one query row: a CTA per row, warp w the chunks w, w + 4, ..., four channels
-// a lane, then the warps in order.
+// One query row of an item that lies in several CTAs, by the CTA (x) where it begins: part 1
+// of that one, part 0 of the next ones.  Each thread first weighs the parts t, t + 128, ... of a
+// round by their maxima, then warp w adds the parts w, w + 4, ..., four channels a lane.
 template <typename T, int NT>
 __global__ void __launch_bounds__(ATT_THREADS) kv4_join_kernel(const AttParams prm) {
     constexpr int R = 8 * NT;
-    __shared__ float s_o[ATT_WARPS][DH], s_ml[ATT_WARPS][2];
+    __shared__ float s_w[ATT_THREADS], s_red[2][ATT_WARPS], s_o[ATT_WARPS][DH];
     pdl_launch_dependents();
     pdl_wait();
-    const Item it(prm, blockIdx.x, R);
+    const int2 open = prm.open[blockIdx.x];
+    if (open.x < 0) return;
+    const int parts = open.y;
+    const Item it(prm, open.x / prm.H, open.x % prm.H, R);
     const int row = blockIdx.y;
-    if (it.nchunks == 1 || row >= it.rows) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const float *src = prm.part + (static_cast<long long>(blockIdx.x) * prm.chunks * R + row) * PART;
-    const long long step = static_cast<long long>(R) * PART;
+    if (row >= it.rows) return;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    constexpr long long step = 2ll * R * PART;
+    // part c > 0 is part 0 of CTA x + c; part 0 lies R rows further on
+    const float *src = prm.part + (static_cast<long long>(blockIdx.x) * 2 * R + row) * PART;
+    auto at = [&](int c) { return src + c * step + (c == 0 ? R * PART : 0); };
     float mx = -INFINITY, sum = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-    for (int c = warp; c < it.nchunks; c += ATT_WARPS) {
-        const float *p = src + c * step;
-        const float2 lo = *reinterpret_cast<const float2 *>(p + 4 * lane);
-        const float2 hi = *reinterpret_cast<const float2 *>(p + 4 * lane + 2);
-        const float2 ml = *reinterpret_cast<const float2 *>(p + DH);
-        const float t = fmaxf(mx, ml.x), ref = t == -INFINITY ? 0.0f : t;
-        const float a = fast_exp2(mx - ref), e = fast_exp2(ml.x - ref);
+    for (int c0 = 0; c0 < parts; c0 += ATT_THREADS) {
+        const int left = parts - c0 < ATT_THREADS ? parts - c0 : ATT_THREADS;
+        const float2 ml = tid < left ? *reinterpret_cast<const float2 *>(at(c0 + tid) + DH)
+                                     : make_float2(-INFINITY, 0.0f);
+        float t = ml.x;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
+        if (lane == 0) s_red[0][warp] = t;
+        __syncthreads();
+        t = mx;
+#pragma unroll
+        for (int w = 0; w < ATT_WARPS; ++w) t = fmaxf(t, s_red[0][w]);
+        const float ref = t == -INFINITY ? 0.0f : t;
+        const float e = fast_exp2(ml.x - ref), a = fast_exp2(mx - ref);
+        s_w[tid] = e;
+        float l = ml.y * e;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        if (lane == 0) s_red[1][warp] = l;
+        __syncthreads();
         mx = t;
-        sum = sum * a + ml.y * e;
-        acc[0] = acc[0] * a + lo.x * e;
-        acc[1] = acc[1] * a + lo.y * e;
-        acc[2] = acc[2] * a + hi.x * e;
-        acc[3] = acc[3] * a + hi.y * e;
+        sum *= a;
+#pragma unroll
+        for (int w = 0; w < ATT_WARPS; ++w) sum += s_red[1][w];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] *= a;
+        int c = warp;
+        for (; c + 7 * ATT_WARPS < left; c += 8 * ATT_WARPS) {
+            float4 v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const float4 *>(at(c0 + c + i * ATT_WARPS) + 4 * lane);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float w = s_w[c + i * ATT_WARPS];
+                acc[0] = fmaf(w, v[i].x, acc[0]);
+                acc[1] = fmaf(w, v[i].y, acc[1]);
+                acc[2] = fmaf(w, v[i].z, acc[2]);
+                acc[3] = fmaf(w, v[i].w, acc[3]);
+            }
+        }
+#pragma unroll 4
+        for (; c < left; c += ATT_WARPS) {
+            const float4 v = *reinterpret_cast<const float4 *>(at(c0 + c) + 4 * lane);
+            const float w = s_w[c];
+            acc[0] = fmaf(w, v.x, acc[0]);
+            acc[1] = fmaf(w, v.y, acc[1]);
+            acc[2] = fmaf(w, v.z, acc[2]);
+            acc[3] = fmaf(w, v.w, acc[3]);
+        }
+        __syncthreads();      // the weights are read before the next round's
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) s_o[warp][4 * lane + i] = acc[i];
-    if (lane == 0) s_ml[warp][0] = mx, s_ml[warp][1] = sum;
     __syncthreads();
-    const int d = threadIdx.x;
-    float top = -INFINITY;
+    float o = 0.0f;
 #pragma unroll
-    for (int w = 0; w < ATT_WARPS; ++w) top = fmaxf(top, s_ml[w][0]);
-    const float ref = top == -INFINITY ? 0.0f : top;
-    float o = 0.0f, l = 0.0f;
-#pragma unroll
-    for (int w = 0; w < ATT_WARPS; ++w) {
-        const float a = fast_exp2(s_ml[w][0] - ref);
-        o += a * s_o[w][d];
-        l += a * s_ml[w][1];
-    }
-    it.out<T>(prm, row)[d] = from_f32<T>(row_value(it.limit(prm, row), o, l));
+    for (int w = 0; w < ATT_WARPS; ++w) o += s_o[w][tid];
+    it.out<T>(prm, row)[tid] = from_f32<T>(row_value(it.limit(prm, row), o, sum));
 }
 
 }  // namespace ipv

@@ -68,7 +68,7 @@ int launched(cudaError_t rc) {
     return rc == cudaSuccess && cudaGetLastError() == cudaSuccess ? IP_OK : IP_ERR_CUDA;
 }
 
-template <typename T>
+template <typename T, bool VEC>
 int quantize(const ips::QuantParams &prm, int nsm, cudaStream_t st) {
     // a warp a row while its lanes can hold the row, then four warps, then the CTA
     const int tpr = prm.d <= 32 * 8 * ips::QUANT_UNITS ? 32 : (prm.d <= 128 * 8 * ips::QUANT_UNITS ? 128 : 256);
@@ -76,10 +76,17 @@ int quantize(const ips::QuantParams &prm, int nsm, cudaStream_t st) {
     const long long need = (prm.rows + rpc - 1) / rpc, cap = 16ll * nsm;
     const dim3 grid(static_cast<unsigned>(need < cap ? need : cap)), block(ips::QUANT_THREADS);
     switch (tpr) {
-        case 32: return launched(iph::launch_pdl(ips::quantize_rows_kernel<T, 32>, grid, block, 0, st, prm));
-        case 128: return launched(iph::launch_pdl(ips::quantize_rows_kernel<T, 128>, grid, block, 0, st, prm));
-        default: return launched(iph::launch_pdl(ips::quantize_rows_kernel<T, 256>, grid, block, 0, st, prm));
+        case 32: return launched(iph::launch_pdl(ips::quantize_rows_kernel<T, 32, VEC>, grid, block, 0, st, prm));
+        case 128: return launched(iph::launch_pdl(ips::quantize_rows_kernel<T, 128, VEC>, grid, block, 0, st, prm));
+        default: return launched(iph::launch_pdl(ips::quantize_rows_kernel<T, 256, VEC>, grid, block, 0, st, prm));
     }
+}
+
+template <typename T>
+int quantize(const ips::QuantParams &prm, int nsm, cudaStream_t st) {
+    const bool vec = prm.d % 8 == 0 && aligned(prm.x, 16) && aligned(prm.q, 8) &&
+                     (prm.rows == 1 || (prm.ldx * sizeof(T) % 16 == 0 && prm.ldq % 8 == 0));
+    return vec ? quantize<T, true>(prm, nsm, st) : quantize<T, false>(prm, nsm, st);
 }
 
 // Up to this many tokens the weights are read by the vector kernel.

@@ -20,13 +20,14 @@ using namespace ipr;
 //
 // scale = amax / 127 rounded to f32 and q = the integer nearest to 127 x / amax, ties
 // to even, for the row's largest magnitude amax.  The quotient is formed as x times
-// the rounded reciprocal (error below 127 2^-22 = 2^-15); within 2^-12 of a half
-// integer n + 1/2 the exact sign of 254 |x| - (2n + 1) amax decides: both products
-// as unevaluated sums of two floats, whose leading parts differ by little there (an
-// exact subtraction) and whose errors have eight bits.  A power of two brings amax to
-// [1, 4) first, so that nothing of this overflows or underflows.  amax = 0: scale
-// and q are 0.  A NaN or an infinity in the row: the scale is NaN and q is 0, so
-// that a product with the row is NaN and not a plausible number.
+// the rounded reciprocal (error below 127 2^-22 = 2^-15) and rounded by adding 1.5 2^23;
+// where it lies within 2^-14 of a half integer n + 1/2 the exact sign of 254 |x| -
+// (2n + 1) amax decides: both products as unevaluated sums of two floats, whose leading
+// parts differ by little there (an exact subtraction) and whose errors have eight bits.
+// An amax near the ends of the range is first brought to [1, 4) by a power of two, its
+// row with it, so that nothing of this overflows or underflows.  amax = 0: scale and q
+// are 0.  A NaN or an infinity in the row: the scale is NaN and q is 0, so that a product
+// with the row is NaN and not a plausible number.
 //
 // What bounds it: DRAM.  A row stays in registers between the two passes up to
 // 8 UNITS elements a thread; a longer one is read again (from L2).
@@ -42,28 +43,30 @@ struct QuantParams {
     float *scale;
 };
 
-__device__ __forceinline__ int quant_one(float x, float inv, float top) {
-    const float y = x * inv;
-    int r = __float2int_rn(y);
-    const float a = fabsf(y), n = rintf(a - 0.5f);
-    if (fabsf(a - 0.5f - n) < 0x1p-12f) {
-        const float ax = fabsf(x), odd = 2.0f * n + 1.0f;
-        const float p1 = 254.0f * ax, e1 = __fmaf_rn(254.0f, ax, -p1);
-        const float p2 = odd * top, e2 = __fmaf_rn(odd, top, -p2);
-        const float diff = __fadd_rn(__fsub_rn(p1, p2), __fsub_rn(e1, e2));
-        const int ni = static_cast<int>(n);
-        int m = diff > 0.0f ? ni + 1 : (diff < 0.0f ? ni : ni + (ni & 1));
-        m = m < 0 ? 0 : m;
-        r = x < 0.0f ? -m : m;
-    }
-    return max(-127, min(127, r));
+__device__ __forceinline__ float max_abs(float top, float x) {   // NaN if either is
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(top), "f"(fabsf(x)));
+    return r;
 }
 
-// TPR threads a row (32, 128 or 256).
-template <typename T, int TPR>
+// q of one element whose quotient y lies close to a half integer.
+__device__ __noinline__ int quant_near(float x, float y, float top) {
+    const float n = rintf(fabsf(y) - 0.5f), ax = fabsf(x), odd = 2.0f * n + 1.0f;
+    const float p1 = 254.0f * ax, e1 = __fmaf_rn(254.0f, ax, -p1);
+    const float p2 = odd * top, e2 = __fmaf_rn(odd, top, -p2);
+    const float diff = __fadd_rn(__fsub_rn(p1, p2), __fsub_rn(e1, e2));
+    const int ni = static_cast<int>(n);
+    int m = diff > 0.0f ? ni + 1 : (diff < 0.0f ? ni : ni + (ni & 1));
+    m = m < 0 ? 0 : m;
+    return x < 0.0f ? -m : m;
+}
+
+// TPR threads a row (32, 128 or 256).  VEC: x's rows start on 16 bytes, q's on 8 and d is a
+// multiple of eight, so that a row's loads are in flight together.
+template <typename T, int TPR, bool VEC>
 __global__ void __launch_bounds__(QUANT_THREADS) quantize_rows_kernel(const QuantParams prm) {
     constexpr int RPC = QUANT_THREADS / TPR;
-    __shared__ unsigned red[QUANT_THREADS / 32];
+    __shared__ float red[QUANT_THREADS / 32];
     pdl_launch_dependents();
     pdl_wait();
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
@@ -73,56 +76,74 @@ __global__ void __launch_bounds__(QUANT_THREADS) quantize_rows_kernel(const Quan
         const long long row = r0 + sub;
         const bool live = row < prm.rows;
         const T *x = static_cast<const T *>(prm.x) + (live ? row : 0) * prm.ldx;
-        const bool vec = (reinterpret_cast<uintptr_t>(x) & 15) == 0;
         float v[QUANT_UNITS][8];
-        unsigned top = 0;   // largest magnitude as bits: a NaN exceeds an infinity
 #pragma unroll
         for (int i = 0; i < QUANT_UNITS; ++i) {
             const int c = (i * TPR + t) * 8;
-            if (live && c < d) load8(x + c, vec, d - c, v[i]);
-            else
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
+            for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
+            if (live && c < d) load8(x + c, VEC, VEC ? 8 : d - c, v[i]);
         }
+        float top = 0.0f;
 #pragma unroll
         for (int i = 0; i < QUANT_UNITS; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[i][j]) & 0x7fffffffu);
+            for (int j = 0; j < 8; ++j) top = max_abs(top, v[i][j]);
         if (live)
             for (int c = (QUANT_UNITS * TPR + t) * 8; c < d; c += TPR * 8) {
                 float w[8];
-                load8(x + c, vec, d - c, w);
+                load8(x + c, VEC, VEC ? 8 : d - c, w);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(w[j]) & 0x7fffffffu);
+                for (int j = 0; j < 8; ++j) top = max_abs(top, w[j]);
             }
-        top = __reduce_max_sync(0xffffffffu, top);
+        // as bits a NaN (made positive) exceeds an infinity and that every number
+        unsigned bits = __reduce_max_sync(0xffffffffu, __float_as_uint(top) & 0x7fffffffu);
         if (TPR > 32) {
             __syncthreads();
-            if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = top;
+            if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = __uint_as_float(bits);
             __syncthreads();
 #pragma unroll
-            for (int i = 0; i < TPR / 32; ++i) top = max(top, red[sub * (TPR / 32) + i]);
+            for (int i = 0; i < TPR / 32; ++i) bits = max(bits, __float_as_uint(red[sub * (TPR / 32) + i]));
         }
         if (!live) continue;   // no thread of the row's group is live, all meet at the next row
-        const bool finite = top < 0x7f800000u;
-        const float amax = __uint_as_float(top);
+        const bool finite = bits < 0x7f800000u;
+        const float amax = __uint_as_float(bits);
         if (t == 0) prm.scale[row] = finite ? __fdiv_rn(amax, 127.0f) : __uint_as_float(0x7fc00000u);
-        // 2^(127 - e) for an amax of exponent field e, kept a normal number
-        const int e = static_cast<int>(top >> 23);
+        const bool zero = !finite || bits == 0;
+        // 2^(127 - e) for an amax of exponent field e, kept a normal number; 1 in the middle
+        const int e = static_cast<int>(bits >> 23);
+        const bool far = e < 32 || e > 222;
         const int fe = 254 - e < 1 ? 1 : (254 - e > 253 ? 253 : 254 - e);
-        const float f = __uint_as_float(static_cast<unsigned>(fe) << 23);
-        const float ntop = amax * f;
-        const bool zero = !finite || top == 0;
-        const float inv = zero ? 0.0f : __fdiv_rn(127.0f, ntop);
+        const float f = far ? __uint_as_float(static_cast<unsigned>(fe) << 23) : 1.0f;
+        const float ntop = amax * f, inv = zero ? 0.0f : __fdiv_rn(127.0f, ntop);
         int8_t *q = prm.q + row * prm.ldq;
-        const bool qvec = (reinterpret_cast<uintptr_t>(q) & 7) == 0;
-        auto put = [&](int c, const float (&w)[8]) {
-            int k[8];
+        auto put = [&](int c, float (&w)[8]) {
+            if (far)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) k[j] = zero ? 0 : quant_one(w[j] * f, inv, ntop);
-            if (qvec && c + 8 <= d) {
-                *reinterpret_cast<uint2 *>(q + c) =
-                    make_uint2(pack_sat4(k[0], k[1], k[2], k[3]), pack_sat4(k[4], k[5], k[6], k[7]));
+                for (int j = 0; j < 8; ++j) w[j] *= f;
+            uint32_t k[8];
+            float off = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float y = w[j] * inv, r = __fadd_rn(y, 12582912.0f);
+                k[j] = __float_as_uint(r);          // the integer in two's complement below bit 22
+                off = fmaxf(off, fabsf(__fsub_rn(y, __fsub_rn(r, 12582912.0f))));
+            }
+            if (zero) {          // NaN times 0 above: whatever it gave, q is 0
+#pragma unroll
+                for (int j = 0; j < 8; ++j) k[j] = 0;
+            } else if (off > 0.5f - 0x1p-14f) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float y = w[j] * inv, r = __fsub_rn(__fadd_rn(y, 12582912.0f), 12582912.0f);
+                    if (fabsf(__fsub_rn(y, r)) > 0.5f - 0x1p-14f)
+                        k[j] = static_cast<uint32_t>(quant_near(w[j], y, ntop));
+                }
+            }
+            uint32_t lo = __byte_perm(__byte_perm(k[0], k[1], 0x0040), __byte_perm(k[2], k[3], 0x0040), 0x5410);
+            uint32_t hi = __byte_perm(__byte_perm(k[4], k[5], 0x0040), __byte_perm(k[6], k[7], 0x0040), 0x5410);
+            if (VEC) {
+                *reinterpret_cast<uint2 *>(q + c) = make_uint2(lo, hi);
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -136,7 +157,7 @@ __global__ void __launch_bounds__(QUANT_THREADS) quantize_rows_kernel(const Quan
         }
         for (int c = (QUANT_UNITS * TPR + t) * 8; c < d; c += TPR * 8) {
             float w[8];
-            load8(x + c, vec, d - c, w);
+            load8(x + c, VEC, VEC ? 8 : d - c, w);
             put(c, w);
         }
     }
@@ -257,7 +278,7 @@ constexpr int TILE_M = 128;
 constexpr int BK = 64;              // K elements per stage
 constexpr int SEG = 1024 / BK;      // stages of an exact segment
 constexpr int TC_THREADS = 640;     // five warpgroups (registers are dealt by warpgroup)
-constexpr int EPI_WARPS = 8, CONV_WARPS = 8;
+constexpr int EPI_WARPS = 8, CONV_WARPS = 8, CONV_GROUPS = 2;
 constexpr int TMA_WARP = 16, MMA_WARP = 17;
 
 template <int BN_>
@@ -385,10 +406,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::RS; ++s) {
             mbar_init(raw_full(s), 1);
-            mbar_init(raw_empty(s), CONV_WARPS);
+            mbar_init(raw_empty(s), CONV_WARPS / CONV_GROUPS);
         }
         for (int s = 0; s < C::FS; ++s) {
-            mbar_init(f16_full(s), CONV_WARPS);
+            mbar_init(f16_full(s), CONV_WARPS / CONV_GROUPS);
             mbar_init(f16_empty(s), 1);
         }
         for (int s = 0; s < 2; ++s) {
@@ -479,13 +500,16 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             }
         }
     } else if (warp >= EPI_WARPS && warp < EPI_WARPS + CONV_WARPS) {
+        // The warps form CONV_GROUPS groups that take the stages in turn, so that one group's
+        // loads and fence overlap the others' arithmetic.
         constexpr int UNITS = (TILE_M + BN) / 8;   // of eight rows
-        const int cw = warp - EPI_WARPS;
+        constexpr int GW = CONV_WARPS / CONV_GROUPS, PER = (UNITS + GW - 1) / GW;
+        const int cw = (warp - EPI_WARPS) % GW, grp = (warp - EPI_WARPS) / GW;
         const int r8 = lane >> 2, j = lane & 3;
         // byte offsets of this lane's chunk in eight raw rows and of its two fp16 chunks
         const uint32_t src = static_cast<uint32_t>(lane * 16);
         const uint32_t d0 = swz(r8, 2 * j), d1 = swz(r8, 2 * j + 1);
-        int rs = 0, rph = 0, fs = 0, fph = 0;
+        int rs = 0, rph = 0, fs = 0, fph = 0, turn = 0;
         bool ok = true;
         for (long long tile = blockIdx.x; ok && tile < prm.tiles; tile += gridDim.x) {
             const long long m0 = tile / prm.tiles_n * TILE_M;
@@ -495,33 +519,48 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             const int ma = static_cast<int>(prm.M - m0 < TILE_M ? (prm.M - m0 + 7) / 8 : TILE_M / 8);
             const int nb = prm.N - n0 < BN ? (prm.N - n0 + 7) / 8 : BN / 8;
             for (int it = 0; it < stages; ++it) {
-                ok = warp_wait_or_dead(raw_full(rs), rph, dead, limit) &&
-                     warp_wait_or_dead(f16_empty(fs), fph ^ 1, dead, limit);
-                if (!ok) break;
-                const uint32_t raw = base + C::RAW_AT + rs * C::RAW, dst = base + C::F16_AT + fs * C::F16;
+                if (turn == grp) {
+                    ok = warp_wait_or_dead(raw_full(rs), rph, dead, limit) &&
+                         warp_wait_or_dead(f16_empty(fs), fph ^ 1, dead, limit);
+                    if (!ok) break;
+                    const uint32_t raw = base + C::RAW_AT + rs * C::RAW, dst = base + C::F16_AT + fs * C::F16;
+                    auto one = [&](int u, const uint4 &v) {
+                        uint32_t h[8];
+                        cvt4(v.x, h[0], h[1]);
+                        cvt4(v.y, h[2], h[3]);
+                        cvt4(v.z, h[4], h[5]);
+                        cvt4(v.w, h[6], h[7]);
+                        sts128(dst + u * 1024 + d0, h[0], h[1], h[2], h[3]);
+                        sts128(dst + u * 1024 + d1, h[4], h[5], h[6], h[7]);
+                    };
+                    if (ma == TILE_M / 8 && nb == BN / 8 && UNITS % GW == 0) {
+                        constexpr int AHEAD = PER < 4 ? PER : 4;
+                        uint4 v[AHEAD];
 #pragma unroll
-                for (int i = 0; i < (UNITS + CONV_WARPS - 1) / CONV_WARPS; ++i) {
-                    const int u = i * CONV_WARPS + cw;
-                    if (UNITS % CONV_WARPS != 0 && u >= UNITS) continue;
-                    if (u < TILE_M / 8 ? u >= ma : u - TILE_M / 8 >= nb) continue;
-                    const uint4 v = lds128(raw + u * 512 + src);
-                    uint32_t h[8];
-                    cvt4(v.x, h[0], h[1]);
-                    cvt4(v.y, h[2], h[3]);
-                    cvt4(v.z, h[4], h[5]);
-                    cvt4(v.w, h[6], h[7]);
-                    sts128(dst + u * 1024 + d0, h[0], h[1], h[2], h[3]);
-                    sts128(dst + u * 1024 + d1, h[4], h[5], h[6], h[7]);
-                }
-                // the fp16 stage to the MMA, the raw stage to the next TMA copy
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(f16_full(fs));
-                    mbar_arrive(raw_empty(rs));
+                        for (int i = 0; i < AHEAD; ++i) v[i] = lds128(raw + (i * GW + cw) * 512 + src);
+#pragma unroll
+                        for (int i = 0; i < PER; ++i) {
+                            one(i * GW + cw, v[i % AHEAD]);
+                            if (i + AHEAD < PER) v[i % AHEAD] = lds128(raw + ((i + AHEAD) * GW + cw) * 512 + src);
+                        }
+                    } else {
+#pragma unroll 2
+                        for (int u = cw; u < UNITS; u += GW) {
+                            if (u < TILE_M / 8 ? u >= ma : u - TILE_M / 8 >= nb) continue;
+                            one(u, lds128(raw + u * 512 + src));
+                        }
+                    }
+                    // the fp16 stage to the MMA, the raw stage to the next TMA copy
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(f16_full(fs));
+                        mbar_arrive(raw_empty(rs));
+                    }
                 }
                 if (++rs == C::RS) rs = 0, rph ^= 1;
                 if (++fs == C::FS) fs = 0, fph ^= 1;
+                if (++turn == CONV_GROUPS) turn = 0;
             }
         }
     } else if (warp < EPI_WARPS) {

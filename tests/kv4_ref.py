@@ -80,9 +80,9 @@ def attention(q, ks, vs, counts, causal, scale):
     below A, two MMAs and four multiply-adds a group cost at most (4 2^-23 + 6 2^-24) A <
     2^-20 A; weights are then off by 2 * 2^-20 A relative (numerator and sum), by 2^-11 for
     the rounding of p s to fp16, and by 2^-16 + n 2^-28 for exp2, the f32 sums of n terms
-    (n / 64 steps of a warp, 2^-23 each) and the merges.  p s is held relative to 2^e 2^-13 with
+    (n / 64 steps of a warp, 2^-23 each) and the merges.  p s is held relative to 2^e 2^-9 with
     2^e at most the largest V scale: below fp16's normal range its rounding is absolute, half of
-    2^-24 there, which with codes up to 7 is at most 7 smax 2^-38 for each of the n terms (a
+    2^-24 there, which with codes up to 7 is at most 7 smax 2^-34 for each of the n terms (a
     one-hot softmax shows it: the other tokens' shares are all there is of a channel whose
     code is 0)."""
     B, T, H, _ = q.shape
@@ -110,5 +110,5 @@ def attention(q, ks, vs, counts, causal, scale):
             A = (absq @ s[:, kv].T * 15 * scale).max(-1, keepdims=True)
             rel = 2 * 2.0 ** -20 * A + 2.0 ** -11 + 2.0 ** -16 + n * 2.0 ** -28
             top = 7 * quant(vs[b])[1][:, kv].max()
-            bound[b, :c, h] = np.where(lim[:, None] > 0, rel * (p @ np.abs(v[:, kv])) + n * 2.0 ** -38 * top, 0)
+            bound[b, :c, h] = np.where(lim[:, None] > 0, rel * (p @ np.abs(v[:, kv])) + n * 2.0 ** -34 * top, 0)
     return out, bound

@@ -125,13 +125,12 @@ def test_attention_refusals(lib):
 
 
 def test_attention_workspace_covers_its_plan():
-    # at least the status word, more rows and longer caches never need less per chunk, and
-    # shapes out of range have none
+    # the status word, and for one wave of CTAs two partial rows each; shapes out of range have none
     assert ip.kv4_attention_workspace_bytes(1, 1, 1, 1, 1) == 256
     for B, T, H, Hkv, n in ((1, 1, 8, 8, 375), (64, 1, 32, 8, 8192), (1, 1, 1, 1, 1 << 28), (65535, 1, 8, 1, 4096),
                             (4, 33, 8, 8, 1500), (1, 2048, 64, 1, 100000), (0, 1, 8, 8, 10), (3, 1, 8, 8, 0)):
         size = ip.kv4_attention_workspace_bytes(B, T, H, Hkv, n)
-        assert size >= 256 and (size - 256) % 520 == 0
+        assert 256 <= size <= 1 << 23 and size % 256 == 0
     for bad in ((1, 0, 8, 8, 10), (1, 1, 8, 3, 10), (1, 1, 0, 1, 10), (1, 1, 8, 8, -1), (-1, 1, 8, 8, 10)):
         with pytest.raises(ip.IpError):
             ip.kv4_attention_workspace_bytes(*bad)
