@@ -923,34 +923,30 @@ def _strides(t, name):
 _Stride3 = ctypes.c_longlong * 3
 
 
-def _kv4_plain(dev, *ints):
-    """Whether the int32 tensors of a cache call are plain, contiguous and on device dev."""
+def _kv4_plain(dev, B, cache, table, workspace, first, second):
+    """Whether a cache call's arguments are plain contiguous tensors of device dev, the current
+    one, with the types and shapes that they must have (second may be None)."""
     t = _Torch
-    for i in ints:
-        if i is not None and not (i.__class__ is t.tensor and i.dtype is t.i32 and i.is_contiguous() and
-                                  i.get_device() == dev):
-            return False
-    return True
+    T, i32 = t.tensor, t.i32
+    if not (cache.__class__ is T and table.__class__ is T and workspace.__class__ is T and first.__class__ is T and
+            dev >= 0 and dev == t.current() and cache.dtype is t.u8 and workspace.dtype is t.u8 and
+            table.dtype is i32 and first.dtype is i32 and cache.get_device() == dev and
+            table.get_device() == dev and workspace.get_device() == dev and first.get_device() == dev and
+            cache.is_contiguous() and table.is_contiguous() and workspace.is_contiguous() and
+            first.is_contiguous()):
+        return False
+    cs, ts, fs = cache.shape, table.shape, first.shape
+    return (len(cs) == 3 and not cs[2] % 144 and len(ts) == 2 and ts[0] == B and len(fs) == 1 and fs[0] == B and
+            (second is None or second.__class__ is T and second.dtype is i32 and second.get_device() == dev and
+             second.shape == fs and second.is_contiguous()))
 
 
-def _kv4_args(x, cache, table, workspace, size, lens, names, stream):
+def _kv4_args(x, cache, table, workspace, lens, names):
     """Checks what the calls on a cache share: x [B, T, H, 128] (or B, for a call without
     one), the cache, its table and the int32 [B] tensors lens; returns B, the cache's
-    (pages, heads, page size, table width), the pointers of lens, a workspace and the
-    raw stream (None: the call goes through _On, on the device of the cache)."""
-    t = _Torch
-    B = x if x.__class__ is int else x.shape[0]
-    if (cache.__class__ is t.tensor and workspace.__class__ is t.tensor and stream is None and
-            cache.dtype is t.u8 and workspace.dtype is t.u8 and cache.is_contiguous() and
-            workspace.is_contiguous()):
-        dev, cs = cache.get_device(), cache.shape
-        if (dev >= 0 and dev == t.current() and workspace.get_device() == dev and len(cs) == 3 and
-                (x is B or x.get_device() == dev) and not cs[2] % 144 and _kv4_plain(dev, table, *lens)):
-            ts = table.shape
-            if len(ts) == 2 and ts[0] == B and all(i is None or i.shape == ts[:1] for i in lens):
-                return (B, (cs[0], cs[1], cs[2] // 144, ts[1]),
-                        [None if i is None else i.data_ptr() for i in lens], workspace, t.raw(dev))
+    (pages, heads, page size, table width) and the pointers of lens."""
     import torch
+    B = x if x.__class__ is int else x.shape[0]
     dev = _need(cache, "cache", torch.uint8).device
     if x is not B:
         _need(x, names[0], None, None, dev)
@@ -964,19 +960,7 @@ def _kv4_args(x, cache, table, workspace, size, lens, names, stream):
     if workspace is not None:
         _dense(workspace, "workspace", torch.uint8, (workspace.numel(),), dev)
     load()
-    return B, (cache.shape[0], cache.shape[1], cache.shape[2] // 144, table.shape[1]), ptrs, workspace, None
-
-
-def _kv4_run(fn, call, handle, device, stream, workspace, size):
-    """call(workspace, raw stream) on the right device and stream, with a fresh workspace
-    of `size` bytes where there is none."""
-    if handle is not None:
-        rc = call(workspace, handle)
-    else:
-        with _On(device, stream) as handle:
-            rc = call(_status_space(workspace, device, size)[0] if workspace is None else workspace, handle)
-    if rc:
-        _check(fn, rc)
+    return B, (cache.shape[0], cache.shape[1], cache.shape[2] // 144, table.shape[1]), ptrs
 
 
 def kv4_append(k, v, start, page_table, cache, *, count=None, workspace=None, stream=None):
@@ -986,6 +970,21 @@ def kv4_append(k, v, start, page_table, cache, *, count=None, workspace=None, st
     page_table[b] (int32 [B, pages]).  No two rows may meet in one place.  All CUDA
     tensors; asynchronous on `stream`.  Pages or positions that do not exist are
     skipped and reported by status(workspace)."""
+    t = _Torch
+    if stream is None and k.__class__ is t.tensor and v.__class__ is t.tensor:
+        ks, dev, code = k.shape, k.get_device(), t.codes.get(k.dtype)
+        if (len(ks) == 4 and ks[3] == IP_DH and code is not None and v.shape == ks and v.dtype is k.dtype and
+                v.get_device() == dev and _kv4_plain(dev, ks[0], cache, page_table, workspace, start, count)):
+            cs, kst, vst = cache.shape, k.stride(), v.stride()
+            if cs[1] == ks[2] and kst[3] == 1 and vst[3] == 1:
+                rc = _lib.ip_kv4_append(
+                    k.data_ptr(), v.data_ptr(), code, _Stride3(*kst[:3]), _Stride3(*vst[:3]), start.data_ptr(),
+                    None if count is None else count.data_ptr(), ks[0], ks[1], ks[2], IP_DH, page_table.data_ptr(),
+                    page_table.shape[1], cache.data_ptr(), cs[0], cs[2] // 144, workspace.data_ptr(),
+                    workspace.numel(), t.raw(dev))
+                if rc:
+                    _check("ip_kv4_append", rc)
+                return cache
     code = _dtype_code(_need(k, "k").dtype, "k")
     if k.dim() != 4 or k.shape[3] != IP_DH:
         raise ValueError(f"k must have shape (B, T, H, 128), got {tuple(k.shape)}")
@@ -993,14 +992,17 @@ def kv4_append(k, v, start, page_table, cache, *, count=None, workspace=None, st
     _need(v, "v", k.dtype, k.shape, k.device)
     if start is None:
         raise TypeError("start must be a CUDA tensor")
-    B, (n_pages, heads, page, width), (pst, pct), ws, handle = _kv4_args(
-        k, cache, page_table, workspace, 256, (start, count), ("k", "start", "count"), stream)
+    B, (n_pages, heads, page, width), (pst, pct) = _kv4_args(k, cache, page_table, workspace, (start, count),
+                                                             ("k", "start", "count"))
     if heads != H:
         raise ValueError(f"cache holds {heads} heads, not {H}")
-    ks, vs = _strides(k, "k"), _strides(v, "v")
-    _kv4_run("ip_kv4_append", lambda w, st: _lib.ip_kv4_append(
-        k.data_ptr(), v.data_ptr(), code, ks, vs, pst, pct, B, T, H, dh, page_table.data_ptr(), width,
-        cache.data_ptr(), n_pages, page, w.data_ptr(), w.numel(), st), handle, k.device, stream, ws, 256)
+    kst, vst = _strides(k, "k"), _strides(v, "v")
+    with _On(k.device, stream) as handle:
+        workspace, ws, wsb = _status_space(workspace, k.device)
+        rc = _lib.ip_kv4_append(k.data_ptr(), v.data_ptr(), code, kst, vst, pst, pct, B, T, H, dh,
+                                page_table.data_ptr(), width, cache.data_ptr(), n_pages, page, ws, wsb, handle)
+    if rc:
+        _check("ip_kv4_append", rc)
     return cache
 
 
@@ -1009,22 +1011,37 @@ def kv4_read(cache, start, page_table, T: int, *, count=None, dtype=None, out=No
     """Positions start[b] .. start[b] + T - 1 of every sequence back as real values:
     (k, v), each [B, T, H, 128] of `dtype` (bfloat16 unless out gives it), zeros in rows
     t >= count[b].  out: such a pair, contiguous.  Arguments as kv4_append."""
+    t = _Torch
+    if stream is None and out is None and cache.__class__ is t.tensor and page_table.__class__ is t.tensor:
+        code, dev = t.codes.get(dtype), cache.get_device()
+        B = page_table.shape[0] if page_table.dim() == 2 else -1
+        if code is not None and T.__class__ is int and T >= 0 and _kv4_plain(dev, B, cache, page_table, workspace,
+                                                                            start, count):
+            cs, where = cache.shape, cache.device
+            shape = (B, T, cs[1], IP_DH)
+            k, v = t.empty(shape, dtype=dtype, device=where), t.empty(shape, dtype=dtype, device=where)
+            rc = _lib.ip_kv4_read(cache.data_ptr(), cs[0], cs[2] // 144, page_table.data_ptr(),
+                                  page_table.shape[1], start.data_ptr(), None if count is None else count.data_ptr(),
+                                  B, T, cs[1], IP_DH, k.data_ptr(), v.data_ptr(), code, workspace.data_ptr(),
+                                  workspace.numel(), t.raw(dev))
+            if rc:
+                _check("ip_kv4_read", rc)
+            return k, v
     import torch
-    B, (n_pages, H, page, width), (pst, pct), ws, handle = _kv4_args(
-        _need(start, "start").numel(), cache, page_table, workspace, 256, (start, count),
-        ("", "start", "count"), stream)
+    B, (n_pages, H, page, width), (pst, pct) = _kv4_args(
+        _need(start, "start").numel(), cache, page_table, workspace, (start, count), ("", "start", "count"))
     dev, shape = cache.device, (B, T, H, IP_DH)
     dtype = dtype or (torch.bfloat16 if out is None else out[0].dtype)
     code = _dtype_code(dtype)
-
-    def call(w, st):
-        nonlocal out
+    with _On(dev, stream) as handle:
         if out is None:
             out = torch.empty(shape, dtype=dtype, device=dev), torch.empty(shape, dtype=dtype, device=dev)
         pk, pv = _dense(out[0], "out[0]", dtype, shape, dev), _dense(out[1], "out[1]", dtype, shape, dev)
-        return _lib.ip_kv4_read(cache.data_ptr(), n_pages, page, page_table.data_ptr(), width, pst, pct, B, T,
-                                H, IP_DH, pk, pv, code, w.data_ptr(), w.numel(), st)
-    _kv4_run("ip_kv4_read", call, handle, dev, stream, ws, 256)
+        workspace, ws, wsb = _status_space(workspace, dev)
+        rc = _lib.ip_kv4_read(cache.data_ptr(), n_pages, page, page_table.data_ptr(), width, pst, pct, B, T, H,
+                              IP_DH, pk, pv, code, ws, wsb, handle)
+    if rc:
+        _check("ip_kv4_read", rc)
     return out
 
 
@@ -1047,6 +1064,25 @@ def kv4_attention(q, lengths, page_table, cache, *, count=None, causal: bool = T
     the table can hold); a close one splits the work better.  Returns [B, T, H, 128] of
     q's type.  workspace: a zero-filled uint8 tensor of kv4_attention_workspace_bytes(B, T,
     H, Hkv, max_len).  Asynchronous on `stream`."""
+    t = _Torch
+    if stream is None and out is None and q.__class__ is t.tensor:
+        qs, dev, code = q.shape, q.get_device(), t.codes.get(q.dtype)
+        if (len(qs) == 4 and qs[3] == IP_DH and code and
+                _kv4_plain(dev, qs[0], cache, page_table, workspace, lengths, count)):
+            st, cs, width = q.stride(), cache.shape, page_table.shape[1]
+            if st[3] == 1:
+                out = t.empty(qs, dtype=q.dtype, device=q.device)
+                rc = _lib.ip_kv4_attention(
+                    q.data_ptr(), code, _Stride3(*st[:3]), lengths.data_ptr(),
+                    None if count is None else count.data_ptr(), 1 if causal else 0,
+                    IP_DH ** -0.5 if scale is None else scale, qs[0], qs[1], qs[2], cs[1], IP_DH,
+                    width * (cs[2] // 144) if max_len is None else max_len, page_table.data_ptr(), width,
+                    cache.data_ptr(), cs[0], cs[2] // 144, out.data_ptr(), workspace.data_ptr(),
+                    workspace.numel(), t.raw(dev))
+                if rc:
+                    _check("ip_kv4_attention", rc)
+                return out
+    import torch
     code = _dtype_code(_need(q, "q").dtype, "q")
     if code == 0:
         raise TypeError(f"q must be float16 or bfloat16, got {q.dtype}")
@@ -1055,25 +1091,22 @@ def kv4_attention(q, lengths, page_table, cache, *, count=None, causal: bool = T
     _, T, H, dh = q.shape
     if lengths is None:
         raise TypeError("lengths must be a CUDA tensor")
-    B, (n_pages, Hkv, page, width), (pln, pct), ws, handle = _kv4_args(
-        q, cache, page_table, workspace, 0, (lengths, count), ("q", "lengths", "count"), stream)
+    B, (n_pages, Hkv, page, width), (pln, pct) = _kv4_args(q, cache, page_table, workspace, (lengths, count),
+                                                           ("q", "lengths", "count"))
     if max_len is None:
         max_len = width * page
-    qs = _strides(q, "q")
-    dev = q.device
-    if scale is None:
-        scale = dh ** -0.5
-
-    def call(w, st):
-        nonlocal out
+    qst, dev = _strides(q, "q"), q.device
+    size = 0 if workspace is not None else kv4_attention_workspace_bytes(B, T, H, Hkv, max_len)
+    with _On(dev, stream) as handle:
         if out is None:
-            out = _Torch.empty(q.shape, dtype=q.dtype, device=dev)
+            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
         po = _dense(out, "out", q.dtype, q.shape, dev)
-        return _lib.ip_kv4_attention(q.data_ptr(), code, qs, pln, pct, 1 if causal else 0, scale, B, T, H, Hkv, dh,
-                                     max_len, page_table.data_ptr(), width, cache.data_ptr(), n_pages, page, po,
-                                     w.data_ptr(), w.numel(), st)
-    size = 0 if ws is not None else kv4_attention_workspace_bytes(B, T, H, Hkv, max_len)
-    _kv4_run("ip_kv4_attention", call, handle, dev, stream, ws, size)
+        workspace, ws, wsb = _status_space(workspace, dev, size)
+        rc = _lib.ip_kv4_attention(q.data_ptr(), code, qst, pln, pct, 1 if causal else 0,
+                                   dh ** -0.5 if scale is None else scale, B, T, H, Hkv, dh, max_len,
+                                   page_table.data_ptr(), width, cache.data_ptr(), n_pages, page, po, ws, wsb, handle)
+    if rc:
+        _check("ip_kv4_attention", rc)
     return out
 
 
