@@ -30,19 +30,23 @@ EncodeTiledFn encode_fn() {
     return fn;
 }
 
-// int8 rows [rows][K] of `ld` bytes each, boxes of BK x box_rows, elements outside read
+// int8 rows [rows][K] of `ld` bytes each, boxes of RAW_K x box_rows, elements outside read
 // as zero (a K that BK does not divide, the rows behind the last).
 bool make_map(CUtensorMap *m, const void *base, int K, long long rows, long long ld, unsigned box_rows) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(K), static_cast<cuuint64_t>(rows)};
     const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld)};
-    const cuuint32_t box[2] = {ips::BK, box_rows};
+    const cuuint32_t box[2] = {ips::RAW_K, box_rows};
     const cuuint32_t estride[2] = {1, 1};
     return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estride,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+// The output [M][N] in blocks of 32 rows x 64 bytes, swizzled as the kernel's stage16 writes them.
+template <typename T>
+bool make_out_map(CUtensorMap *m, const ips::ScaledParams &prm);
 
 bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
@@ -89,6 +93,22 @@ int quantize(const ips::QuantParams &prm, int nsm, cudaStream_t st) {
     return vec ? quantize<T, true>(prm, nsm, st) : quantize<T, false>(prm, nsm, st);
 }
 
+template <typename T> constexpr CUtensorMapDataType MAP_TYPE = CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+template <> constexpr CUtensorMapDataType MAP_TYPE<__half> = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+template <> constexpr CUtensorMapDataType MAP_TYPE<__nv_bfloat16> = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+
+template <typename T>
+bool make_out_map(CUtensorMap *m, const ips::ScaledParams &prm) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(prm.N), static_cast<cuuint64_t>(prm.M)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(prm.ldy) * sizeof(T)};
+    const cuuint32_t box[2] = {64 / sizeof(T), 32};
+    const cuuint32_t estride[2] = {1, 1};
+    return fn(m, MAP_TYPE<T>, 2, prm.y, dims, strides, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Up to this many tokens the weights are read by the vector kernel.
 constexpr long long VEC_TOKENS = 8;
 
@@ -107,38 +127,59 @@ int launch_vec_m(const ips::ScaledParams &prm, int nsm, cudaStream_t st) {
     return launch_vec<T, MT, 1>(prm, st);
 }
 
-template <typename T, int BN, bool LONG>
-int launch_tc(const CUtensorMap &tx, const CUtensorMap &tw, const ips::ScaledParams &prm, int nsm,
-              cudaStream_t st) {
+template <typename T, int BN, bool LONG, bool PAIR>
+int launch_tc(const CUtensorMap &tx, const CUtensorMap &tw, const CUtensorMap &ty, const ips::ScaledParams &prm,
+              int nsm, cudaStream_t st) {
+    using C = ips::Tile<BN, PAIR>;
     static bool set[64] = {false};
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return IP_ERR_CUDA;
-    auto *fn = ips::scaled_tc_kernel<T, BN, LONG>;
+    auto *fn = ips::scaled_tc_kernel<T, BN, LONG, PAIR>;
     {
         std::lock_guard<std::mutex> lock(g_mu);
         if (!set[dev]) {
-            if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, ips::Tile<BN>::SMEM) !=
-                cudaSuccess)
+            // the kernel deals out TC_REGS registers a thread: never launch a build with fewer
+            cudaFuncAttributes attr;
+            if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess ||
+                cudaFuncGetAttributes(&attr, fn) != cudaSuccess ||
+                (LONG && BN == 256 && attr.numRegs < ips::TC_REGS))
                 return IP_ERR_CUDA;
             set[dev] = true;
         }
     }
-    const unsigned grid = static_cast<unsigned>(prm.tiles < nsm ? prm.tiles : nsm);
-    return launched(iph::launch_pdl(fn, dim3(grid), dim3(ips::TC_THREADS), ips::Tile<BN>::SMEM, st, tx, tw, prm));
+    const long long most = nsm / C::CTAS, workers = prm.tiles < most ? prm.tiles : most;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(workers * C::CTAS));
+    cfg.blockDim = dim3(ips::TC_THREADS);
+    cfg.dynamicSmemBytes = C::SMEM;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = PAIR ? 2 : 1;
+    return launched(cudaLaunchKernelEx(&cfg, fn, tx, tw, ty, prm));
 }
 
-template <typename T, int BN>
+template <typename T, int BN, bool PAIR>
 int run_tc(ips::ScaledParams prm, int nsm, cudaStream_t st) {
-    CUtensorMap tx, tw;
+    using C = ips::Tile<BN, PAIR>;
+    CUtensorMap tx, tw, ty;
     if (!make_map(&tx, prm.x, prm.K, prm.M, prm.ldx, ips::TILE_M) ||
-        !make_map(&tw, prm.w, prm.K, prm.N, prm.ldw, BN))
+        !make_map(&tw, prm.w, prm.K, prm.N, prm.ldw, C::BR))
         return IP_ERR_CUDA;
+    prm.out_map = aligned(prm.y, 16) && prm.ldy * sizeof(T) % 16 == 0 && prm.N * sizeof(T) % 16 == 0;
+    ty = tx;       // not used then
+    if (prm.out_map && !make_out_map<T>(&ty, prm)) return IP_ERR_CUDA;
     prm.tiles_n = (prm.N + BN - 1) / BN;
-    prm.tiles = (prm.M + ips::TILE_M - 1) / ips::TILE_M * prm.tiles_n;
-    // the sums of several segments take BN / 2 registers of an epilogue thread
-    if constexpr (BN <= 128)
-        if (prm.K > ips::SEG * ips::BK) return launch_tc<T, BN, true>(tx, tw, prm, nsm, st);
-    return launch_tc<T, BN, false>(tx, tw, prm, nsm, st);
+    prm.tiles = (prm.M + ips::TILE_M * C::CTAS - 1) / (ips::TILE_M * C::CTAS) * prm.tiles_n;
+    if constexpr (BN <= 128 || PAIR)
+        if (prm.K > ips::SEG * ips::BK) return launch_tc<T, BN, true, PAIR>(tx, tw, ty, prm, nsm, st);
+    return launch_tc<T, BN, false, PAIR>(tx, tw, ty, prm, nsm, st);
 }
 
 template <typename T>
@@ -150,10 +191,9 @@ int run_scaled(const ips::ScaledParams &prm, int nsm, cudaStream_t st) {
         return launch_vec_m<T, 8>(prm, nsm, st);
     }
     const long long tm = (prm.M + ips::TILE_M - 1) / ips::TILE_M;
-    if (prm.K <= ips::SEG * ips::BK && tm * ((prm.N + 255) / 256) >= nsm)
-        return run_tc<T, 256>(prm, nsm, st);
-    if (tm * ((prm.N + 127) / 128) >= nsm) return run_tc<T, 128>(prm, nsm, st);
-    return run_tc<T, 32>(prm, nsm, st);
+    if ((tm + 1) / 2 * ((prm.N + 255) / 256) >= nsm / 2) return run_tc<T, 256, true>(prm, nsm, st);
+    if (tm * ((prm.N + 127) / 128) >= nsm) return run_tc<T, 128, false>(prm, nsm, st);
+    return run_tc<T, 32, false>(prm, nsm, st);
 }
 
 }  // namespace
@@ -209,6 +249,7 @@ int ip_linear_scaled_i8(const int8_t *x, long long ldx, const float *sx, const i
     prm.K = K;
     prm.N = N;
     prm.act = act;
+    prm.out_map = 0;
     prm.tiles_n = 0;
     prm.tiles = 0;
     prm.err = static_cast<int *>(workspace);

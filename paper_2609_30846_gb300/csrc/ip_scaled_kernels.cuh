@@ -176,6 +176,7 @@ struct ScaledParams {
     void *y;
     long long M, ldx, ldw, ldy;
     int K, N, act;
+    int out_map;                    // y has a tensor map
     int tiles_n;
     long long tiles;
     int *err;
@@ -261,37 +262,53 @@ __global__ void __launch_bounds__(VEC_THREADS) scaled_vec_kernel(const ScaledPar
     }
 }
 
-// Many tokens: tiles of 128 tokens x BN channels on the fp16 tensor cores.
+// Many tokens: tiles of 128 tokens x BN channels on the fp16 tensor cores, or of 256 x 256 by
+// two CTAs (PAIR).
 //
 // sm_103a has no integer tcgen05 kind, and its integer warp MMA and dp4a together
 // reach 289 TOPS; but fp16 holds every int8 value, the product of two is exact in the
-// fp32 accumulator, and so is every partial sum below 2^24: at most 1024 products of
+// fp32 accumulator, and so is every partial sum up to 2^24: at most 1024 products of
 // magnitude 2^14.  So the K axis runs in segments of 1024, each summed exactly in
 // TMEM, and the segments are added as int32 in registers.
 //
-// Roles of a persistent CTA (one per SM): warp 16 fetches stages of 64 K bytes of
-// both operands by TMA, warps 8-15 convert them to fp16 in the 128-byte swizzled
-// K-major layout of the MMA, one thread of warp 17 issues tcgen05.mma, warps 0-7
+// Roles of a persistent CTA (one per SM): warp 16 fetches stages of 128 K bytes of
+// both operands by TMA, warps 8-15 convert halves of them to fp16 in the 128-byte
+// swizzled K-major layout of the MMA, one thread of warp 17 issues tcgen05.mma, warps 0-7
 // drain one of two TMEM accumulators and write the output while the other fills.
+//
+// What bounds it: the shared-memory accesses of the conversion (a read and two writes per
+// operand byte; 80 % of that pipe with 128 x 256 tiles a CTA, the tensor pipe at 36 %).
+// So the CTAs of a pair share their channels: each converts its 128 tokens and half of
+// the 256 channels for an MMA of 256 x 256 (cta_group::2), a third less for the same
+// products; and the output leaves by TMA stores.
 
 constexpr int TILE_M = 128;
-constexpr int BK = 64;              // K elements per stage
+constexpr int RAW_K = 128;          // K bytes of a raw stage: TMA moves rows of 64 bytes at half the rate
+constexpr int BK = 64;              // K elements of an fp16 stage (rows of 128 bytes)
 constexpr int SEG = 1024 / BK;      // stages of an exact segment
+constexpr int OUT_BLOCK = 32 * 64;
 constexpr int TC_THREADS = 640;     // five warpgroups (registers are dealt by warpgroup)
-constexpr int EPI_WARPS = 8, CONV_WARPS = 8, CONV_GROUPS = 2;
+constexpr int TC_REGS = 96;         // registers a thread at launch
+constexpr int EPI_WARPS = 8, CONV_WARPS = 8, CONV_GROUPS = 4;
 constexpr int TMA_WARP = 16, MMA_WARP = 17;
 
-template <int BN_>
+template <int BN_, bool PAIR_>
 struct Tile {
     static constexpr int BN = BN_;
-    static constexpr int RAW = (TILE_M + BN) * BK;
-    static constexpr int F16 = RAW * 2;
-    static constexpr int RS = BN == 256 ? 3 : 4;      // raw stages
-    static constexpr int FS = BN == 256 ? 3 : 4;      // fp16 stages
+    static constexpr int CTAS = PAIR_ ? 2 : 1;
+    static constexpr int BR = BN / CTAS;              // channels that a CTA converts
+    static constexpr int RAW = (TILE_M + BR) * RAW_K;
+    static constexpr int F16 = (TILE_M + BR) * BK * 2;
+    static constexpr int RS = BN == 32 ? 4 : 2;       // raw stages
+    static constexpr int FS = 4;                      // fp16 stages
+    // a group of warps must not wait for the phase after next of a slot: their parities are alike
+    static_assert(CONV_GROUPS <= FS && CONV_GROUPS % 2 == 0 && CONV_GROUPS / 2 <= 2 * RS, "groups");
     static constexpr int BARS = 0;                    // 2 RS + 2 FS + 5 barriers
     static constexpr int TMEM_PTR = 256, DEAD = 260;
     static constexpr int CONSTS = 512;                // per epilogue warp: sw and bias of its columns
-    static constexpr int F16_AT = (CONSTS + EPI_WARPS * 2 * 4 * (BN / 2) + 1023) & ~1023;
+    // per epilogue warp: a block of 32 rows x 64 bytes on its way out
+    static constexpr int OUT_AT = (CONSTS + EPI_WARPS * 2 * 4 * (BN / 2) + 1023) & ~1023;
+    static constexpr int F16_AT = OUT_AT + EPI_WARPS * OUT_BLOCK;
     static constexpr int RAW_AT = F16_AT + FS * F16;
     static constexpr int SMEM = RAW_AT + RS * RAW + 1024;
     static constexpr int COLS = 2 * BN;               // TMEM columns
@@ -312,12 +329,26 @@ __device__ __forceinline__ void cvt4(uint32_t w, uint32_t &lo, uint32_t &hi) {
     asm("add.rn.f16x2 %0, %1, %2;" : "=r"(hi) : "r"(b), "r"(c));
 }
 
+// One poll of a barrier that threads of the other CTA of a pair arrive on as well.
+template <bool PAIR>
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+    if (!PAIR) return mbar_try_wait(bar, parity);
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+        " selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
 // Bounded wait that also ends when another role of the CTA has given up.
+template <bool PAIR>
 __device__ __forceinline__ bool wait_or_dead(uint32_t bar, uint32_t parity, volatile int *dead,
                                              long long limit) {
-    if (mbar_try_wait(bar, parity)) return true;
+    if (try_wait<PAIR>(bar, parity)) return true;
     const long long t0 = clock64();
-    while (!mbar_try_wait(bar, parity)) {
+    while (!try_wait<PAIR>(bar, parity)) {
         if (*dead) return false;
         if (clock64() - t0 > limit) {
             *dead = 1;
@@ -326,9 +357,31 @@ __device__ __forceinline__ bool wait_or_dead(uint32_t bar, uint32_t parity, vola
     }
     return true;
 }
+template <bool PAIR>
 __device__ __forceinline__ bool warp_wait_or_dead(uint32_t bar, uint32_t parity, volatile int *dead,
                                                   long long limit) {
-    return __all_sync(0xffffffffu, wait_or_dead(bar, parity, dead, limit)) != 0;
+    return __all_sync(0xffffffffu, wait_or_dead<PAIR>(bar, parity, dead, limit)) != 0;
+}
+// Arrives on the barrier at this shared-memory offset of the pair's first CTA.
+template <bool PAIR>
+__device__ __forceinline__ void arrive_first(uint32_t bar) {
+    if (!PAIR) {
+        mbar_arrive(bar);
+        return;
+    }
+    asm volatile(
+        "{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, 0;\n"
+        " mbarrier.arrive.release.cluster.shared::cluster.b64 _, [r];\n}\n" ::"r"(bar)
+        : "memory");
+}
+// True in one lane of a converged warp, always the same.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // Shared-memory descriptor of a K-major operand with 128-byte swizzle: rows of 128
@@ -338,17 +391,53 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr) {
            (2ull << 61);
 }
 
+template <bool PAIR>
 __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
                                         uint32_t accumulate) {
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
-        " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-        : "memory");
+    if (PAIR)
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+            " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+            : "memory");
+    else
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+            " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+            : "memory");
 }
+// Arrives on the barrier (of both CTAs of a pair) when the MMAs so far have completed.
+template <bool PAIR>
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
-                 : "memory");
+    if (PAIR)
+        asm volatile(
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                bar),
+            "h"(static_cast<uint16_t>(3))
+            : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
+                     : "memory");
+}
+template <bool PAIR>
+__device__ __forceinline__ void tmem_alloc(uint32_t at, int cols) {
+    if (PAIR) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(at), "r"(cols)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(at), "r"(cols)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+}
+template <bool PAIR>
+__device__ __forceinline__ void tmem_free(uint32_t tmem, int cols) {
+    if (PAIR)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
+    else
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
 }
 __device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16]) {
     asm volatile(
@@ -382,18 +471,42 @@ __device__ __forceinline__ void store16(T *row, int n, int N, bool vec, const fl
             if (n + j < N) row[n + j] = from_f32<T>(z[j]);
     }
 }
+// The same into a block of 32 rows x 64 bytes in shared memory, from its 16-byte chunk c0 on, in
+// the layout of the TMA store (64-byte swizzle: no bank conflicts).
+template <typename T>
+__device__ __forceinline__ void stage16(uint32_t block, int row, int c0, const float (&z)[16]) {
+    constexpr int W = 16 / sizeof(T);
+#pragma unroll
+    for (int i = 0; i < 16 / W; ++i) {
+        T v[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) v[j] = from_f32<T>(z[i * W + j]);
+        const uint4 w = *reinterpret_cast<const uint4 *>(v);
+        sts128(block + row * 64 + (((c0 + i) ^ ((row >> 1) & 3)) << 4), w.x, w.y, w.z, w.w);
+    }
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t src, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
+                     reinterpret_cast<uint64_t>(map)),
+                 "r"(c0), "r"(c1), "r"(src)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
 
 // LONG: K > 1024, several segments per tile.
-template <typename T, int BN, bool LONG>
+template <typename T, int BN, bool LONG, bool PAIR>
 __global__ void __launch_bounds__(TC_THREADS, 1)
     scaled_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w,
-                     const ScaledParams prm) {
-    using C = Tile<BN>;
+                     const __grid_constant__ CUtensorMap tm_y, const ScaledParams prm) {
+    using C = Tile<BN, PAIR>;
+    // The sums of a long K take 128 registers of an epilogue thread (BN = 256): its warpgroups
+    // take over what the others can spare, 2 x 168 + 2 x 56 + 32 = 5 x 96.
+    constexpr bool DEAL = LONG && BN == 256;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const uint32_t base = smem_u32(smem);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     auto raw_full = [&](int s) { return base + C::BARS + 8u * s; };
     auto raw_empty = [&](int s) { return base + C::BARS + 8u * (C::RS + s); };
     auto f16_full = [&](int s) { return base + C::BARS + 8u * (2 * C::RS + s); };
@@ -402,34 +515,33 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     auto acc_empty = [&](int s) { return base + C::BARS + 8u * (2 * C::RS + 2 * C::FS + 2 + s); };
     const uint32_t drained = base + C::BARS + 8u * (2 * C::RS + 2 * C::FS + 4);
     volatile int *dead = reinterpret_cast<volatile int *>(smem + C::DEAD);
+    const int rank = PAIR ? static_cast<int>(blockIdx.x & 1u) : 0;      // clusters are (2, 1, 1)
+    const long long worker = blockIdx.x / C::CTAS, workers = gridDim.x / C::CTAS;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::RS; ++s) {
             mbar_init(raw_full(s), 1);
-            mbar_init(raw_empty(s), CONV_WARPS / CONV_GROUPS);
+            mbar_init(raw_empty(s), 2 * CONV_WARPS / CONV_GROUPS);      // both halves read
         }
         for (int s = 0; s < C::FS; ++s) {
-            mbar_init(f16_full(s), CONV_WARPS / CONV_GROUPS);
+            mbar_init(f16_full(s), CONV_WARPS / CONV_GROUPS * C::CTAS);
             mbar_init(f16_empty(s), 1);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(acc_full(s), 1);
-            mbar_init(acc_empty(s), EPI_WARPS);
+            mbar_init(acc_empty(s), EPI_WARPS * C::CTAS);
         }
         mbar_init(drained, 1);
         *dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (warp == MMA_WARP) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
-                         base + C::TMEM_PTR),
-                     "r"(C::COLS)
-                     : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
+    __syncwarp();
+    if (PAIR) cluster_sync();
+    if (warp == MMA_WARP) tmem_alloc<PAIR>(base + C::TMEM_PTR, C::COLS);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
+    if (PAIR) cluster_sync();
+    else __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     // only now: a CTA of the next launch that took this SM's TMEM first would wait for
     // this grid with it
@@ -437,24 +549,25 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     const uint32_t tmem = lds32(base + C::TMEM_PTR);
     pdl_wait();
 
-    const int stages = (prm.K + BK - 1) / BK;
+    const int stages = (prm.K + RAW_K - 1) / RAW_K * 2;      // fp16 stages (K behind the end reads as 0)
     const long long limit = prm.timeout_cycles;
 
-    if (warp == TMA_WARP) {
-        if (lane == 0) {
+    if (warp >= EPI_WARPS + CONV_WARPS) {
+        if (DEAL) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+        if (warp == TMA_WARP && lane == 0) {
             int s = 0, ph = 0;
             long long issued = 0;
             bool ok = true;
-            for (long long tile = blockIdx.x; ok && tile < prm.tiles; tile += gridDim.x) {
-                const int m0 = static_cast<int>(tile / prm.tiles_n) * TILE_M;
-                const int n0 = static_cast<int>(tile % prm.tiles_n) * BN;
-                for (int it = 0; it < stages; ++it) {
-                    ok = wait_or_dead(raw_empty(s), ph ^ 1, dead, limit);
+            for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
+                const int m0 = static_cast<int>(tile / prm.tiles_n) * (TILE_M * C::CTAS) + rank * TILE_M;
+                const int n0 = static_cast<int>(tile % prm.tiles_n) * BN + rank * C::BR;
+                for (int k = 0; k < prm.K; k += RAW_K) {
+                    ok = wait_or_dead<false>(raw_empty(s), ph ^ 1, dead, limit);
                     if (!ok) break;
                     const uint32_t st = base + C::RAW_AT + s * C::RAW;
                     mbar_expect_tx(raw_full(s), C::RAW);
-                    tma_load_2d(st, &tm_x, it * BK, m0, raw_full(s));
-                    tma_load_2d(st + TILE_M * BK, &tm_w, it * BK, n0, raw_full(s));
+                    tma_load_2d(st, &tm_x, k, m0, raw_full(s));
+                    tma_load_2d(st + TILE_M * RAW_K, &tm_w, k, n0, raw_full(s));
                     ++issued;
                     if (++s == C::RS) s = 0, ph ^= 1;
                 }
@@ -464,117 +577,139 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                 for (long long i = issued > C::RS ? issued - C::RS : 0; i < issued; ++i)
                     mbar_wait(raw_full(static_cast<int>(i % C::RS)),
                               static_cast<uint32_t>((i / C::RS) & 1), limit);
-        }
-    } else if (warp == MMA_WARP) {
-        if (lane == 0) {
+        } else if (warp == MMA_WARP && rank == 0) {
+            // the whole warp runs the loop, so that the descriptors stay uniform; one lane issues
             constexpr uint32_t idesc = (1u << 4) | (static_cast<uint32_t>(BN / 8) << 17) |
-                                       (static_cast<uint32_t>(TILE_M / 16) << 24);
+                                       (static_cast<uint32_t>(TILE_M * C::CTAS / 16) << 24);
             int s = 0, ph = 0, a = 0, aph = 0;
             bool ok = true;
-            for (long long tile = blockIdx.x; ok && tile < prm.tiles; tile += gridDim.x) {
+            for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
                 for (int it = 0; ok && it < stages;) {
-                    ok = wait_or_dead(acc_empty(a), aph ^ 1, dead, limit);
+                    ok = warp_wait_or_dead<PAIR>(acc_empty(a), aph ^ 1, dead, limit);
                     if (!ok) break;
                     const int end = it + SEG < stages ? it + SEG : stages;
                     for (int first = it; it < end; ++it) {
-                        ok = wait_or_dead(f16_full(s), ph, dead, limit);
+                        ok = warp_wait_or_dead<PAIR>(f16_full(s), ph, dead, limit);
                         if (!ok) break;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                         const uint32_t st = base + C::F16_AT + s * C::F16;
                         const uint64_t da = smem_desc(st), db = smem_desc(st + TILE_M * BK * 2);
+                        if (elect_one()) {
 #pragma unroll
-                        for (int k = 0; k < BK / 16; ++k)
-                            mma_f16(tmem + a * BN, da + 2 * k, db + 2 * k, idesc, it > first || k > 0);
-                        mma_commit(f16_empty(s));
+                            for (int k = 0; k < BK / 16; ++k)
+                                mma_f16<PAIR>(tmem + a * BN, da + 2 * k, db + 2 * k, idesc, it > first || k > 0);
+                            mma_commit<PAIR>(f16_empty(s));
+                        }
+                        __syncwarp();
                         if (++s == C::FS) s = 0, ph ^= 1;
                     }
                     if (!ok) break;
-                    mma_commit(acc_full(a));
+                    if (elect_one()) mma_commit<PAIR>(acc_full(a));
+                    __syncwarp();
                     a ^= 1;
                     aph ^= a == 0;
                 }
             }
             if (!ok) {   // the MMAs in flight end before their TMEM is freed
-                mma_commit(drained);
+                if (elect_one()) mma_commit<PAIR>(drained);
+                __syncwarp();
                 mbar_wait(drained, 0, limit);
             }
         }
-    } else if (warp >= EPI_WARPS && warp < EPI_WARPS + CONV_WARPS) {
+    } else if (warp >= EPI_WARPS) {
+        if (DEAL) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         // The warps form CONV_GROUPS groups that take the stages in turn, so that one group's
         // loads and fence overlap the others' arithmetic.
-        constexpr int UNITS = (TILE_M + BN) / 8;   // of eight rows
+        constexpr int UNITS = (TILE_M + C::BR) / 8;   // of eight rows
         constexpr int GW = CONV_WARPS / CONV_GROUPS, PER = (UNITS + GW - 1) / GW;
         const int cw = (warp - EPI_WARPS) % GW, grp = (warp - EPI_WARPS) / GW;
-        const int r8 = lane >> 2, j = lane & 3;
-        // byte offsets of this lane's chunk in eight raw rows and of its two fp16 chunks
-        const uint32_t src = static_cast<uint32_t>(lane * 16);
-        const uint32_t d0 = swz(r8, 2 * j), d1 = swz(r8, 2 * j + 1);
+        // A unit is eight rows of half a raw stage.  A lane takes chunk j (16 bytes) of row r8; the
+        // quarter-warps hold rows r and r + 4, whose four chunks of a half fall on different banks
+        // under the swizzle, and write their two fp16 chunks in opposite order for the same reason.
+        const int r8 = (lane >> 3) + (lane & 4), j = lane & 3, odd = (lane >> 2) & 1;
+        const uint32_t src0 = swz(r8, j), src1 = swz(r8, 4 + j);
+        const uint32_t d0 = swz(r8, 2 * j + odd), d1 = swz(r8, 2 * j + (odd ^ 1));
         int rs = 0, rph = 0, fs = 0, fph = 0, turn = 0;
         bool ok = true;
-        for (long long tile = blockIdx.x; ok && tile < prm.tiles; tile += gridDim.x) {
-            const long long m0 = tile / prm.tiles_n * TILE_M;
-            const int n0 = static_cast<int>(tile % prm.tiles_n) * BN;
+        for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
+            const long long m0 = tile / prm.tiles_n * (TILE_M * C::CTAS) + rank * TILE_M;
+            const int n0 = static_cast<int>(tile % prm.tiles_n) * BN + rank * C::BR;
             // groups of eight rows that hold anything (rows past the end feed outputs that
             // are not written)
-            const int ma = static_cast<int>(prm.M - m0 < TILE_M ? (prm.M - m0 + 7) / 8 : TILE_M / 8);
-            const int nb = prm.N - n0 < BN ? (prm.N - n0 + 7) / 8 : BN / 8;
+            const long long mr = prm.M - m0;
+            const int ma = mr <= 0 ? 0 : (mr < TILE_M ? static_cast<int>((mr + 7) / 8) : TILE_M / 8);
+            const int nr = prm.N - n0, nb = nr <= 0 ? 0 : (nr < C::BR ? (nr + 7) / 8 : C::BR / 8);
             for (int it = 0; it < stages; ++it) {
                 if (turn == grp) {
-                    ok = warp_wait_or_dead(raw_full(rs), rph, dead, limit) &&
-                         warp_wait_or_dead(f16_empty(fs), fph ^ 1, dead, limit);
-                    if (!ok) break;
-                    const uint32_t raw = base + C::RAW_AT + rs * C::RAW, dst = base + C::F16_AT + fs * C::F16;
-                    auto one = [&](int u, const uint4 &v) {
-                        uint32_t h[8];
-                        cvt4(v.x, h[0], h[1]);
-                        cvt4(v.y, h[2], h[3]);
-                        cvt4(v.z, h[4], h[5]);
-                        cvt4(v.w, h[6], h[7]);
+                    // the first loads run while the fp16 slot is waited for; a wait that ran out shows
+                    // after both (what was read meanwhile is not used)
+                    ok = wait_or_dead<false>(raw_full(rs), rph, dead, limit);
+                    const uint32_t src = base + C::RAW_AT + rs * C::RAW + (it & 1 ? src1 : src0);
+                    const uint32_t dst = base + C::F16_AT + fs * C::F16;
+                    const bool whole = ma == TILE_M / 8 && nb == C::BR / 8 && UNITS % GW == 0;
+                    constexpr int AHEAD = PER < 4 ? PER : 4;
+                    uint4 v[AHEAD];
+                    if (whole)
+#pragma unroll
+                        for (int i = 0; i < AHEAD; ++i) v[i] = lds128(src + (i * GW + cw) * 1024);
+                    ok = wait_or_dead<PAIR>(f16_empty(fs), fph ^ 1, dead, limit) && ok;
+                    if (!__all_sync(0xffffffffu, ok)) {
+                        ok = false;
+                        break;
+                    }
+                    auto one = [&](int u, uint4 v) {
+                        uint32_t h[8];      // the half of the chunk that is written first in front
+                        cvt4(odd ? v.z : v.x, h[0], h[1]);
+                        cvt4(odd ? v.w : v.y, h[2], h[3]);
+                        cvt4(odd ? v.x : v.z, h[4], h[5]);
+                        cvt4(odd ? v.y : v.w, h[6], h[7]);
                         sts128(dst + u * 1024 + d0, h[0], h[1], h[2], h[3]);
                         sts128(dst + u * 1024 + d1, h[4], h[5], h[6], h[7]);
                     };
-                    if (ma == TILE_M / 8 && nb == BN / 8 && UNITS % GW == 0) {
-                        constexpr int AHEAD = PER < 4 ? PER : 4;
-                        uint4 v[AHEAD];
-#pragma unroll
-                        for (int i = 0; i < AHEAD; ++i) v[i] = lds128(raw + (i * GW + cw) * 512 + src);
+                    if (whole) {
 #pragma unroll
                         for (int i = 0; i < PER; ++i) {
                             one(i * GW + cw, v[i % AHEAD]);
-                            if (i + AHEAD < PER) v[i % AHEAD] = lds128(raw + ((i + AHEAD) * GW + cw) * 512 + src);
+                            if (i + AHEAD < PER) v[i % AHEAD] = lds128(src + ((i + AHEAD) * GW + cw) * 1024);
                         }
                     } else {
 #pragma unroll 2
                         for (int u = cw; u < UNITS; u += GW) {
                             if (u < TILE_M / 8 ? u >= ma : u - TILE_M / 8 >= nb) continue;
-                            one(u, lds128(raw + u * 512 + src));
+                            one(u, lds128(src + u * 1024));
                         }
                     }
                     // the fp16 stage to the MMA, the raw stage to the next TMA copy
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) {
-                        mbar_arrive(f16_full(fs));
+                        arrive_first<PAIR>(f16_full(fs));
                         mbar_arrive(raw_empty(rs));
                     }
                 }
-                if (++rs == C::RS) rs = 0, rph ^= 1;
+                if ((it & 1) && ++rs == C::RS) rs = 0, rph ^= 1;
                 if (++fs == C::FS) fs = 0, fph ^= 1;
                 if (++turn == CONV_GROUPS) turn = 0;
             }
         }
-    } else if (warp < EPI_WARPS) {
+    } else {
+        if (DEAL) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
         const int quarter = warp & 3, half = warp >> 2;
         constexpr int CW = BN / 2;            // columns of a warp
         constexpr int CH = CW < 16 ? 1 : CW / 16;
         const int col0 = half * CW;
         const bool vec = ((reinterpret_cast<uintptr_t>(prm.y) | (static_cast<uintptr_t>(prm.ldy) * sizeof(T))) &
                           15) == 0;
+        // blocks of 64 bytes a row leave by TMA where the output's rows are aligned for it and N ends
+        // on 16 bytes (the last 16 of a row are written whole)
+        constexpr int PER_BLOCK = 4 / static_cast<int>(sizeof(T));      // chunks of 16 columns in one
+        const bool staged = CH % PER_BLOCK == 0 && prm.out_map;
+        const uint32_t block = base + C::OUT_AT + warp * OUT_BLOCK;
         const uint32_t cst = base + C::CONSTS + warp * (8 * CW);
         int a = 0, aph = 0;
         bool ok = true;
-        for (long long tile = blockIdx.x; ok && tile < prm.tiles; tile += gridDim.x) {
-            const long long m = tile / prm.tiles_n * TILE_M + quarter * 32 + lane;
+        for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
+            const long long mq = tile / prm.tiles_n * (TILE_M * C::CTAS) + rank * TILE_M + quarter * 32, m = mq + lane;
             const int n0 = static_cast<int>(tile % prm.tiles_n) * BN + col0;
             __syncwarp();
             for (int c = lane; c < CW; c += 32) {
@@ -585,7 +720,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             __syncwarp();
             const float sx = m < prm.M ? prm.sx[m] : 0.0f;
             T *row = static_cast<T *>(prm.y) + (m < prm.M ? m : 0) * prm.ldy;
-            auto write = [&](int c, const float (&s)[16]) {
+            auto write = [&](int ch, const float (&s)[16]) {
+                const int c = 16 * ch;
                 float z[16];
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
@@ -596,7 +732,22 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                     z[i + 2] = finish<T>(s[i + 2], sx * __uint_as_float(w4.z), __uint_as_float(b4.z), prm.act);
                     z[i + 3] = finish<T>(s[i + 3], sx * __uint_as_float(w4.w), __uint_as_float(b4.w), prm.act);
                 }
-                if (m < prm.M) store16<T>(row, n0 + c, prm.N, vec, z);
+                if (!staged) {
+                    if (m < prm.M) store16<T>(row, n0 + c, prm.N, vec, z);
+                    return;
+                }
+                if (ch % PER_BLOCK == 0) {      // the store before has read the block
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    __syncwarp();
+                }
+                stage16<T>(block, lane, ch % PER_BLOCK * 2, z);
+                if (ch % PER_BLOCK == PER_BLOCK - 1) {
+                    const int cb = c - 16 * (PER_BLOCK - 1);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0 && mq < prm.M && n0 + cb < prm.N)
+                        tma_store_2d(&tm_y, block, n0 + cb, static_cast<int>(mq));
+                }
             };
             int sum[LONG ? CH : 1][16];
             if (LONG)
@@ -605,7 +756,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) sum[c][i] = 0;
             for (int it = 0; it < stages; it += SEG) {
-                ok = warp_wait_or_dead(acc_full(a), aph, dead, limit);
+                ok = warp_wait_or_dead<PAIR>(acc_full(a), aph, dead, limit);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t at = tmem + a * BN + col0 + (static_cast<uint32_t>(quarter * 32) << 16);
@@ -621,12 +772,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                         float s[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) s[i] = __uint_as_float(r[i]);
-                        write(16 * c, s);
+                        write(c, s);
                     }
                 }
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive(acc_empty(a));
+                if (lane == 0) arrive_first<PAIR>(acc_empty(a));
                 a ^= 1;
                 aph ^= a == 0;
             }
@@ -636,16 +787,16 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                     float s[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[i] = static_cast<float>(sum[c][i]);
-                    write(16 * c, s);
+                    write(c, s);
                 }
             }
         }
+        if (staged && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
-    __syncthreads();
-    if (warp == MMA_WARP)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::COLS)
-                     : "memory");
+    if (PAIR) cluster_sync();     // neither CTA ends while the other may still arrive on its barriers
+    else __syncthreads();
+    if (warp == MMA_WARP) tmem_free<PAIR>(tmem, C::COLS);
     if (threadIdx.x == 0 && *dead) atomicOr(prm.err, ERR_TIMEOUT);
 }
 
