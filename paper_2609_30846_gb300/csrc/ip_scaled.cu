@@ -73,11 +73,11 @@ int launched(cudaError_t rc) {
 }
 
 template <typename T, bool VEC>
-int quantize(const ips::QuantParams &prm, int nsm, cudaStream_t st) {
+int quantize(const ips::QuantParams &prm, cudaStream_t st) {
     // a warp a row while its lanes can hold the row, then four warps, then the CTA
     const int tpr = prm.d <= 32 * 8 * ips::QUANT_UNITS ? 32 : (prm.d <= 128 * 8 * ips::QUANT_UNITS ? 128 : 256);
     const int rpc = ips::QUANT_THREADS / tpr;
-    const long long need = (prm.rows + rpc - 1) / rpc, cap = 16ll * nsm;
+    const long long need = (prm.rows + rpc - 1) / rpc, cap = 1ll << 20;
     const dim3 grid(static_cast<unsigned>(need < cap ? need : cap)), block(ips::QUANT_THREADS);
     switch (tpr) {
         case 32: return launched(iph::launch_pdl(ips::quantize_rows_kernel<T, 32, VEC>, grid, block, 0, st, prm));
@@ -87,10 +87,10 @@ int quantize(const ips::QuantParams &prm, int nsm, cudaStream_t st) {
 }
 
 template <typename T>
-int quantize(const ips::QuantParams &prm, int nsm, cudaStream_t st) {
+int quantize(const ips::QuantParams &prm, cudaStream_t st) {
     const bool vec = prm.d % 8 == 0 && aligned(prm.x, 16) && aligned(prm.q, 8) &&
                      (prm.rows == 1 || (prm.ldx * sizeof(T) % 16 == 0 && prm.ldq % 8 == 0));
-    return vec ? quantize<T, true>(prm, nsm, st) : quantize<T, false>(prm, nsm, st);
+    return vec ? quantize<T, true>(prm, st) : quantize<T, false>(prm, st);
 }
 
 template <typename T> constexpr CUtensorMapDataType MAP_TYPE = CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
@@ -112,19 +112,22 @@ bool make_out_map(CUtensorMap *m, const ips::ScaledParams &prm) {
 // Up to this many tokens the weights are read by the vector kernel.
 constexpr long long VEC_TOKENS = 8;
 
-template <typename T, int MT, int CPT>
+template <typename T, int MT, int CPT, int KT>
 int launch_vec(const ips::ScaledParams &prm, cudaStream_t st) {
-    const int per = ips::VEC_THREADS / ips::VEC_KT * CPT;
+    constexpr int per = ips::VEC_THREADS / KT * CPT;
     const dim3 grid(static_cast<unsigned>((prm.N + per - 1) / per), static_cast<unsigned>((prm.M + MT - 1) / MT));
-    return launched(iph::launch_pdl(ips::scaled_vec_kernel<T, MT, CPT>, grid, dim3(ips::VEC_THREADS), 0, st, prm));
+    return launched(iph::launch_pdl(ips::scaled_vec_kernel<T, MT, CPT, KT>, grid, dim3(ips::VEC_THREADS), 0, st, prm));
 }
 
 template <typename T, int MT>
 int launch_vec_m(const ips::ScaledParams &prm, int nsm, cudaStream_t st) {
-    // the most channels a CTA for which every SM still gets two CTAs
-    if (prm.N >= 2 * nsm * 16) return launch_vec<T, MT, 4>(prm, st);
-    if (prm.N >= 2 * nsm * 8) return launch_vec<T, MT, 2>(prm, st);
-    return launch_vec<T, MT, 1>(prm, st);
+    // the most channels a CTA for which every SM still gets one and a half CTAs
+    if (prm.K > 2048) {
+        if (prm.N >= nsm * 6) return launch_vec<T, MT, 4, 256>(prm, st);
+        return launch_vec<T, MT, 1, 256>(prm, st);
+    }
+    if (prm.N >= nsm * 24) return launch_vec<T, MT, 4, 64>(prm, st);
+    return launch_vec<T, MT, 1, 64>(prm, st);
 }
 
 template <typename T, int BN, bool LONG, bool PAIR>
@@ -208,13 +211,11 @@ int ip_quantize_rows_i8(const void *x, int dtype, long long rows, int d, long lo
     if (rows == 0) return IP_OK;
     if (!x || !q || !scale) return IP_ERR_NULL;
     if (!aligned(x, elem_size(dtype)) || !aligned(scale, 4)) return IP_ERR_ALIGN;
-    const int nsm = sm_count();
-    if (nsm <= 0) return IP_ERR_CUDA;
     const ips::QuantParams prm{x, rows, ldx, ldq, d, q, scale};
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    if (dtype == IP_F32) return quantize<float>(prm, nsm, st);
-    if (dtype == IP_F16) return quantize<__half>(prm, nsm, st);
-    return quantize<__nv_bfloat16>(prm, nsm, st);
+    if (dtype == IP_F32) return quantize<float>(prm, st);
+    if (dtype == IP_F16) return quantize<__half>(prm, st);
+    return quantize<__nv_bfloat16>(prm, st);
 }
 
 int ip_linear_scaled_i8(const int8_t *x, long long ldx, const float *sx, const int8_t *w,

@@ -20,10 +20,16 @@ using namespace ipr;
 //
 // scale = amax / 127 rounded to f32 and q = the integer nearest to 127 x / amax, ties
 // to even, for the row's largest magnitude amax.  The quotient is formed as x times
-// the rounded reciprocal (error below 127 2^-22 = 2^-15) and rounded by adding 1.5 2^23;
-// where it lies within 2^-14 of a half integer n + 1/2 the exact sign of 254 |x| -
-// (2n + 1) amax decides: both products as unevaluated sums of two floats, whose leading
-// parts differ by little there (an exact subtraction) and whose errors have eight bits.
+// the reciprocal rounded up (error below 127 2^-23 < 2^-16) and rounded by adding 1.5 2^23.
+// That is right except near half integers n + 1/2, where 254 x = (2n + 1) amax is close:
+//   16-bit x: two integers of eleven bits at most, so what is not equal is 2^-12 off and
+//     safe.  Equality needs 2n + 1 = 127, x = amax / 2 (common: one element a row of 1024
+//     bf16 values; the reciprocal rounded up takes it to the even 64), or an amax whose
+//     significand 127 divides: those rows look at every element.
+//   f32 x: units of eight elements with one near a half integer are looked at.
+//   Looking: within 2^-14 of a half integer the exact sign of 254 |x| - (2n + 1) amax
+//     decides: both products as unevaluated sums of two floats, whose leading parts differ
+//     by little there (an exact subtraction) and whose errors have eight bits.
 // An amax near the ends of the range is first brought to [1, 4) by a power of two, its
 // row with it, so that nothing of this overflows or underflows.  amax = 0: scale and q
 // are 0.  A NaN or an infinity in the row: the scale is NaN and q is 0, so that a product
@@ -43,29 +49,87 @@ struct QuantParams {
     float *scale;
 };
 
-__device__ __forceinline__ float max_abs(float top, float x) {   // NaN if either is
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(top), "f"(fabsf(x)));
-    return r;
+// Eight elements as they lie in memory.
+template <typename T>
+struct Raw8 {
+    static constexpr int WORDS = 2 * sizeof(T);
+    uint32_t w[WORDS];
+
+    template <bool VEC>
+    __device__ __forceinline__ void load(const T *p, int n) {      // the first n, the others 0
+        if (VEC) {
+#pragma unroll
+            for (int i = 0; i < WORDS; i += 4) {
+                const uint4 v = *reinterpret_cast<const uint4 *>(reinterpret_cast<const uint32_t *>(p) + i);
+                w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
+            }
+        } else {
+            zero();
+            for (int i = 0; i < n && i < 8; ++i) {
+                if constexpr (sizeof(T) == 4) w[i] = reinterpret_cast<const uint32_t *>(p)[i];
+                else w[i >> 1] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t *>(p)[i]) << (16 * (i & 1));
+            }
+        }
+    }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) w[i] = 0;
+    }
+    // largest magnitude so far, as the bits of T (two halves for the 16-bit types): magnitudes
+    // order as integers, a NaN above an infinity above every number
+    __device__ __forceinline__ void largest(uint32_t &top) const {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i)
+            top = sizeof(T) == 4 ? max(top, w[i] & 0x7fffffffu) : __vmaxu2(top, w[i] & 0x7fff7fffu);
+    }
+    // `top` of a thread as bits of an f32 of the same order and value
+    static __device__ __forceinline__ uint32_t value(uint32_t top) {
+        if constexpr (sizeof(T) == 4) return top;
+        const uint16_t h = static_cast<uint16_t>(max(top >> 16, top & 0xffffu));
+        return __float_as_uint(to_f32(*reinterpret_cast<const T *>(&h))) & 0x7fffffffu;
+    }
+    __device__ __forceinline__ float at(int i) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        const uint16_t h = static_cast<uint16_t>(i & 1 ? w[i >> 1] >> 16 : w[i >> 1]);
+        return to_f32(*reinterpret_cast<const T *>(&h));
+    }
+};
+
+// The low bytes of eight words.
+__device__ __forceinline__ uint2 low_bytes(const uint32_t (&k)[8]) {
+    return make_uint2(
+        __byte_perm(__byte_perm(k[0], k[1], 0x0040), __byte_perm(k[2], k[3], 0x0040), 0x5410),
+        __byte_perm(__byte_perm(k[4], k[5], 0x0040), __byte_perm(k[6], k[7], 0x0040), 0x5410));
 }
 
-// q of one element whose quotient y lies close to a half integer.
-__device__ __noinline__ int quant_near(float x, float y, float top) {
-    const float n = rintf(fabsf(y) - 0.5f), ax = fabsf(x), odd = 2.0f * n + 1.0f;
-    const float p1 = 254.0f * ax, e1 = __fmaf_rn(254.0f, ax, -p1);
-    const float p2 = odd * top, e2 = __fmaf_rn(odd, top, -p2);
-    const float diff = __fadd_rn(__fsub_rn(p1, p2), __fsub_rn(e1, e2));
-    const int ni = static_cast<int>(n);
-    int m = diff > 0.0f ? ni + 1 : (diff < 0.0f ? ni : ni + (ni & 1));
-    m = m < 0 ? 0 : m;
-    return x < 0.0f ? -m : m;
+// Eight elements, each looked at near half integers (out of line: rare, and the registers // it takes would cost the others their occupancy).
+template <typename T>
+__device__ __noinline__ uint2 quant_look(Raw8<T> raw, float f, float inv, float top) {
+    uint32_t k[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float x = raw.at(j) * f, y = x * inv, r = __fsub_rn(__fmaf_rn(x, inv, 12582912.0f), 12582912.0f);
+        int q = __float2int_rn(r);
+        if (fabsf(__fmaf_rn(x, inv, -r)) > 0.5f - 0x1p-14f) {
+            const float n = rintf(fabsf(y) - 0.5f), ax = fabsf(x), odd = 2.0f * n + 1.0f;
+            const float p1 = 254.0f * ax, e1 = __fmaf_rn(254.0f, ax, -p1);
+            const float p2 = odd * top, e2 = __fmaf_rn(odd, top, -p2);
+            const float diff = __fadd_rn(__fsub_rn(p1, p2), __fsub_rn(e1, e2));
+            const int ni = static_cast<int>(n);
+            q = diff > 0.0f ? ni + 1 : (diff < 0.0f ? ni : ni + (ni & 1));
+            q = q < 0 ? 0 : q;
+            q = x < 0.0f ? -q : q;
+        }
+        k[j] = static_cast<uint32_t>(q);
+    }
+    return low_bytes(k);
 }
 
 // TPR threads a row (32, 128 or 256).  VEC: x's rows start on 16 bytes, q's on 8 and d is a
 // multiple of eight, so that a row's loads are in flight together.
 template <typename T, int TPR, bool VEC>
 __global__ void __launch_bounds__(QUANT_THREADS) quantize_rows_kernel(const QuantParams prm) {
-    constexpr int RPC = QUANT_THREADS / TPR;
+    constexpr int RPC = QUANT_THREADS / TPR, UNITS = QUANT_UNITS;
     __shared__ float red[QUANT_THREADS / 32];
     pdl_launch_dependents();
     pdl_wait();
@@ -76,28 +140,23 @@ __global__ void __launch_bounds__(QUANT_THREADS) quantize_rows_kernel(const Quan
         const long long row = r0 + sub;
         const bool live = row < prm.rows;
         const T *x = static_cast<const T *>(prm.x) + (live ? row : 0) * prm.ldx;
-        float v[QUANT_UNITS][8];
+        Raw8<T> v[UNITS];
 #pragma unroll
-        for (int i = 0; i < QUANT_UNITS; ++i) {
+        for (int i = 0; i < UNITS; ++i) {
             const int c = (i * TPR + t) * 8;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
-            if (live && c < d) load8(x + c, VEC, VEC ? 8 : d - c, v[i]);
+            if (live && c < d) v[i].template load<VEC>(x + c, d - c);
+            else v[i].zero();
         }
-        float top = 0.0f;
+        uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < QUANT_UNITS; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) top = max_abs(top, v[i][j]);
+        for (int i = 0; i < UNITS; ++i) v[i].largest(top);
         if (live)
-            for (int c = (QUANT_UNITS * TPR + t) * 8; c < d; c += TPR * 8) {
-                float w[8];
-                load8(x + c, VEC, VEC ? 8 : d - c, w);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) top = max_abs(top, w[j]);
+            for (int c = (UNITS * TPR + t) * 8; c < d; c += TPR * 8) {
+                Raw8<T> w;
+                w.template load<VEC>(x + c, d - c);
+                w.largest(top);
             }
-        // as bits a NaN (made positive) exceeds an infinity and that every number
-        unsigned bits = __reduce_max_sync(0xffffffffu, __float_as_uint(top) & 0x7fffffffu);
+        unsigned bits = __reduce_max_sync(0xffffffffu, Raw8<T>::value(top));
         if (TPR > 32) {
             __syncthreads();
             if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = __uint_as_float(bits);
@@ -115,49 +174,44 @@ __global__ void __launch_bounds__(QUANT_THREADS) quantize_rows_kernel(const Quan
         const bool far = e < 32 || e > 222;
         const int fe = 254 - e < 1 ? 1 : (254 - e > 253 ? 253 : 254 - e);
         const float f = far ? __uint_as_float(static_cast<unsigned>(fe) << 23) : 1.0f;
-        const float ntop = amax * f, inv = zero ? 0.0f : __fdiv_rn(127.0f, ntop);
+        const float ntop = amax * f, inv = zero ? 0.0f : __fdiv_ru(127.0f, ntop);
+        // rows near the ends of the range go the same way
+        const bool look = !zero && (far || (sizeof(T) == 2 && ((bits & 0x7fffffu) | 0x800000u) % 127u == 0));
         int8_t *q = prm.q + row * prm.ldq;
-        auto put = [&](int c, float (&w)[8]) {
-            if (far)
+        auto put = [&](int c, const Raw8<T> &raw) {
+            uint2 b = make_uint2(0u, 0u);
+            if (look) {
+                b = quant_look(raw, f, inv, ntop);
+            } else if (!zero) {
+                uint32_t k[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] *= f;
-            uint32_t k[8];
-            float off = 0.0f;
+                for (int j = 0; j < 8; ++j)      // the integer in two's complement below bit 22
+                    k[j] = __float_as_uint(__fmaf_rn(raw.at(j), inv, 12582912.0f));
+                b = low_bytes(k);
+                if (sizeof(T) == 4) {
+                    float off = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float y = w[j] * inv, r = __fadd_rn(y, 12582912.0f);
-                k[j] = __float_as_uint(r);          // the integer in two's complement below bit 22
-                off = fmaxf(off, fabsf(__fsub_rn(y, __fsub_rn(r, 12582912.0f))));
-            }
-            if (zero) {          // NaN times 0 above: whatever it gave, q is 0
-#pragma unroll
-                for (int j = 0; j < 8; ++j) k[j] = 0;
-            } else if (off > 0.5f - 0x1p-14f) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float y = w[j] * inv, r = __fsub_rn(__fadd_rn(y, 12582912.0f), 12582912.0f);
-                    if (fabsf(__fsub_rn(y, r)) > 0.5f - 0x1p-14f)
-                        k[j] = static_cast<uint32_t>(quant_near(w[j], y, ntop));
+                    for (int j = 0; j < 8; ++j)
+                        off = fmaxf(off, fabsf(__fmaf_rn(raw.at(j), inv, -__fsub_rn(__uint_as_float(k[j]), 12582912.0f))));
+                    if (off > 0.5f - 0x1p-14f) b = quant_look(raw, f, inv, ntop);
                 }
             }
-            uint32_t lo = __byte_perm(__byte_perm(k[0], k[1], 0x0040), __byte_perm(k[2], k[3], 0x0040), 0x5410);
-            uint32_t hi = __byte_perm(__byte_perm(k[4], k[5], 0x0040), __byte_perm(k[6], k[7], 0x0040), 0x5410);
             if (VEC) {
-                *reinterpret_cast<uint2 *>(q + c) = make_uint2(lo, hi);
+                *reinterpret_cast<uint2 *>(q + c) = b;
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (c + j < d) q[c + j] = static_cast<int8_t>(k[j]);
+                    if (c + j < d) q[c + j] = static_cast<int8_t>((j < 4 ? b.x : b.y) >> (8 * (j & 3)));
             }
         };
 #pragma unroll
-        for (int i = 0; i < QUANT_UNITS; ++i) {
+        for (int i = 0; i < UNITS; ++i) {
             const int c = (i * TPR + t) * 8;
             if (c < d) put(c, v[i]);
         }
-        for (int c = (QUANT_UNITS * TPR + t) * 8; c < d; c += TPR * 8) {
-            float w[8];
-            load8(x + c, VEC, VEC ? 8 : d - c, w);
+        for (int c = (UNITS * TPR + t) * 8; c < d; c += TPR * 8) {
+            Raw8<T> w;
+            w.template load<VEC>(x + c, d - c);
             put(c, w);
         }
     }
@@ -190,12 +244,12 @@ __device__ __forceinline__ float finish(float s, float scale, float bias, int ac
     return z;
 }
 
-// Few tokens: the weights are read once and the products formed by dp4a.  A CTA takes
-// 4 CPT channels; 64 threads share a channel's K in chunks of 16 bytes, so that a
-// warp reads 512 consecutive bytes of a weight row at a time and each chunk of x is
-// loaded once for CPT channels.  Bound by the weights' bytes.
+// Few tokens: the weights are read once and the products formed by dp4a.  KT threads share
+// a channel's K in chunks of 16 bytes (64 where K is short, all 256 of the CTA where it is
+// long, so that a thread has one or two rounds of loads), a thread takes CPT channels, so
+// that each chunk of x is loaded once for them, and 256 / KT x CPT channels are a CTA's.
+// Bound by latency and the weights' bytes.
 constexpr int VEC_THREADS = 256;
-constexpr int VEC_KT = 64;
 
 __device__ __forceinline__ uint4 chunk16(const int8_t *p, int n) {
     if (n >= 16) return *reinterpret_cast<const uint4 *>(p);
@@ -205,13 +259,13 @@ __device__ __forceinline__ uint4 chunk16(const int8_t *p, int n) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-template <typename T, int MT, int CPT>
+template <typename T, int MT, int CPT, int KT>
 __global__ void __launch_bounds__(VEC_THREADS) scaled_vec_kernel(const ScaledParams prm) {
-    constexpr int GROUPS = VEC_THREADS / VEC_KT;
-    __shared__ int part[GROUPS][2][MT * CPT];
+    constexpr int GROUPS = VEC_THREADS / KT, WARPS = KT / 32;
+    __shared__ int part[GROUPS][WARPS][MT * CPT];
     pdl_launch_dependents();
     pdl_wait();
-    const int t = threadIdx.x % VEC_KT, g = threadIdx.x / VEC_KT;
+    const int t = threadIdx.x % KT, g = threadIdx.x / KT;
     const long long m0 = static_cast<long long>(blockIdx.y) * MT;
     const int n0 = (static_cast<int>(blockIdx.x) * GROUPS + g) * CPT;
     const int mv = static_cast<int>(prm.M - m0 < MT ? prm.M - m0 : MT);
@@ -221,7 +275,7 @@ __global__ void __launch_bounds__(VEC_THREADS) scaled_vec_kernel(const ScaledPar
 #pragma unroll
         for (int j = 0; j < CPT; ++j) acc[i][j] = 0;
 #pragma unroll 2
-    for (int k = t * 16; k < prm.K; k += VEC_KT * 16) {
+    for (int k = t * 16; k < prm.K; k += KT * 16) {
         uint4 w[CPT];
 #pragma unroll
         for (int j = 0; j < CPT; ++j)
@@ -255,7 +309,9 @@ __global__ void __launch_bounds__(VEC_THREADS) scaled_vec_kernel(const ScaledPar
         const int n = static_cast<int>(blockIdx.x) * GROUPS * CPT + c;
         if (i >= mv || n >= prm.N) continue;
         const int at = i * CPT + c % CPT;
-        const int s = part[c / CPT][0][at] + part[c / CPT][1][at];
+        int s = 0;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) s += part[c / CPT][w][at];
         const float z = finish<T>(static_cast<float>(s), prm.sx[m0 + i] * prm.sw[n],
                                   prm.bias ? prm.bias[n] : 0.0f, prm.act);
         static_cast<T *>(prm.y)[(m0 + i) * prm.ldy + n] = from_f32<T>(z);

@@ -69,6 +69,22 @@ def test_quantize_ties_and_neighbours(ip, dtype):
     same_quant(ip, torch.stack(rows).cuda())
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_quantize_every_pair_of_significands(ip, dtype):
+    # a row for every significand of amax, with every significand below it in nine binades:
+    # all quotients that the 16-bit types can have in the rounding's reach, ties among them
+    dt, bits = DT[dtype], 10 if dtype == "f16" else 7
+    sig = torch.arange(1 << bits, 2 << bits, device="cuda", dtype=torch.float64) * 2.0 ** -bits
+    vals = torch.cat([sig * 2.0 ** -j for j in range(9)])
+    for top in sig.split(128):
+        x = torch.where(vals[None] <= top[:, None], vals[None], torch.zeros((), device="cuda", dtype=torch.float64))
+        x = torch.cat([top[:, None], x, -x], 1).to(dt)
+        q, s = ip.quantize_rows_i8(x)
+        want = (127.0 * x.double() / top[:, None]).round()     # exact enough: 53 bits, ties representable
+        assert torch.equal(q.double(), want)
+        assert torch.equal(s.double(), (top / 127.0).float().double())
+
+
 @pytest.mark.parametrize("scale", [1e-45, 1e-42, 1e-38, 3e-37, 1e-20, 1e20, 1e36, 3e38])
 def test_quantize_extreme_ranges(ip, scale):
     g = torch.Generator(device="cuda").manual_seed(3)
