@@ -109,35 +109,36 @@ bool make_out_map(CUtensorMap *m, const ips::ScaledParams &prm) {
               CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Up to this many tokens the weights are read by the vector kernel.
-constexpr long long VEC_TOKENS = 8;
-
 template <typename T, int MT, int CPT, int KT>
-int launch_vec(const ips::ScaledParams &prm, cudaStream_t st) {
+int launch_vec(const ips::ScaledParams &prm, int nsm, cudaStream_t st) {
     constexpr int per = ips::VEC_THREADS / KT * CPT;
-    const dim3 grid(static_cast<unsigned>((prm.N + per - 1) / per), static_cast<unsigned>((prm.M + MT - 1) / MT));
-    return launched(iph::launch_pdl(ips::scaled_vec_kernel<T, MT, CPT, KT>, grid, dim3(ips::VEC_THREADS), 0, st, prm));
+    const long long blocks = (prm.N + per - 1) / per, most = 4ll * nsm;
+    const dim3 grid(static_cast<unsigned>(blocks < most ? blocks : most),
+                    static_cast<unsigned>((prm.M + MT - 1) / MT)), block(ips::VEC_THREADS);
+    if (prm.K <= KT * 16)
+        return launched(iph::launch_pdl(ips::scaled_vec_kernel<T, MT, CPT, KT, true>, grid, block, 0, st, prm));
+    return launched(iph::launch_pdl(ips::scaled_vec_kernel<T, MT, CPT, KT, false>, grid, block, 0, st, prm));
 }
 
 template <typename T, int MT>
 int launch_vec_m(const ips::ScaledParams &prm, int nsm, cudaStream_t st) {
     // the most channels a CTA for which every SM still gets one and a half CTAs
     if (prm.K > 2048) {
-        if (prm.N >= nsm * 6) return launch_vec<T, MT, 4, 256>(prm, st);
-        return launch_vec<T, MT, 1, 256>(prm, st);
+        if (prm.N >= nsm * 6) return launch_vec<T, MT, 4, 256>(prm, nsm, st);
+        return launch_vec<T, MT, 1, 256>(prm, nsm, st);
     }
-    if (prm.N >= nsm * 24) return launch_vec<T, MT, 4, 64>(prm, st);
-    return launch_vec<T, MT, 1, 64>(prm, st);
+    if (prm.N >= nsm * 24) return launch_vec<T, MT, 4, 64>(prm, nsm, st);
+    return launch_vec<T, MT, 1, 64>(prm, nsm, st);
 }
 
-template <typename T, int BN, bool LONG, bool PAIR>
+template <typename T, int BN, bool LONG, bool PAIR, bool KSPLIT = false>
 int launch_tc(const CUtensorMap &tx, const CUtensorMap &tw, const CUtensorMap &ty, const ips::ScaledParams &prm,
               int nsm, cudaStream_t st) {
     using C = ips::Tile<BN, PAIR>;
     static bool set[64] = {false};
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return IP_ERR_CUDA;
-    auto *fn = ips::scaled_tc_kernel<T, BN, LONG, PAIR>;
+    auto *fn = ips::scaled_tc_kernel<T, BN, LONG, PAIR, KSPLIT>;
     {
         std::lock_guard<std::mutex> lock(g_mu);
         if (!set[dev]) {
@@ -150,9 +151,11 @@ int launch_tc(const CUtensorMap &tx, const CUtensorMap &tw, const CUtensorMap &t
             set[dev] = true;
         }
     }
-    const long long most = nsm / C::CTAS, workers = prm.tiles < most ? prm.tiles : most;
+    // parts of a tile do not loop over tiles
+    const int ctas = KSPLIT ? prm.splits : C::CTAS;
+    const long long most = KSPLIT ? prm.tiles : nsm / ctas, workers = prm.tiles < most ? prm.tiles : most;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(workers * C::CTAS));
+    cfg.gridDim = dim3(static_cast<unsigned>(workers * ctas));
     cfg.blockDim = dim3(ips::TC_THREADS);
     cfg.dynamicSmemBytes = C::SMEM;
     cfg.stream = st;
@@ -160,11 +163,11 @@ int launch_tc(const CUtensorMap &tx, const CUtensorMap &tw, const CUtensorMap &t
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.x = static_cast<unsigned>(ctas);
     attr[1].val.clusterDim.y = 1;
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = PAIR ? 2 : 1;
+    cfg.numAttrs = ctas > 1 ? 2 : 1;
     return launched(cudaLaunchKernelEx(&cfg, fn, tx, tw, ty, prm));
 }
 
@@ -180,23 +183,66 @@ int run_tc(ips::ScaledParams prm, int nsm, cudaStream_t st) {
     if (prm.out_map && !make_out_map<T>(&ty, prm)) return IP_ERR_CUDA;
     prm.tiles_n = (prm.N + BN - 1) / BN;
     prm.tiles = (prm.M + ips::TILE_M * C::CTAS - 1) / (ips::TILE_M * C::CTAS) * prm.tiles_n;
+    if constexpr (BN == 32) {
+        const int raws = (prm.K + ips::RAW_K - 1) / ips::RAW_K;
+        if (prm.splits > 1)
+            return (raws + prm.splits - 1) / prm.splits * ips::RAW_K > 1024
+                       ? launch_tc<T, BN, true, PAIR, true>(tx, tw, ty, prm, nsm, st)
+                       : launch_tc<T, BN, false, PAIR, true>(tx, tw, ty, prm, nsm, st);
+    }
     if constexpr (BN <= 128 || PAIR)
         if (prm.K > ips::SEG * ips::BK) return launch_tc<T, BN, true, PAIR>(tx, tw, ty, prm, nsm, st);
     return launch_tc<T, BN, false, PAIR>(tx, tw, ty, prm, nsm, st);
 }
 
-template <typename T>
-int run_scaled(const ips::ScaledParams &prm, int nsm, cudaStream_t st) {
-    if (prm.M <= VEC_TOKENS) {
-        if (prm.M == 1) return launch_vec_m<T, 1>(prm, nsm, st);
-        if (prm.M == 2) return launch_vec_m<T, 2>(prm, nsm, st);
-        if (prm.M <= 4) return launch_vec_m<T, 4>(prm, nsm, st);
-        return launch_vec_m<T, 8>(prm, nsm, st);
-    }
+// The form that a launch is expected to take the least time in, ns.  Fitted on GB300 to sweeps of
+// M = 12 .. 4096 tokens over N = 512 .. 16384 at K = 1024 and 4096, every form timed at each point:
+// the vector kernel reads the weights once per eight tokens; the tensor-core forms take so
+// long per fp16 stage (64 of K) of a round of tiles over the SMs.  (us, vector / 32 / 128 / pairs:
+// 32 x 1024 -> 1024 4.4 / 7.7 / 10.6 / 15, 64 x 4096 -> 1024 11.4 / 10.4 / 33 / 45,
+// 16 x 4096 -> 16384 33 / 72 / 40 / 50, 1024 x 1024 -> 4096 - / 35 / 17.3 / 15.2.)
+enum Form { FORM_VEC, FORM_32, FORM_128, FORM_PAIR };
+struct Choice {
+    Form form;
+    int splits;
+};
+
+long long rounds(long long tiles, int workers) { return (tiles + workers - 1) / workers; }
+
+Choice choose(const ips::ScaledParams &prm, int nsm) {
+    const long long raws = (prm.K + ips::RAW_K - 1) / ips::RAW_K, stages = 2 * raws;
     const long long tm = (prm.M + ips::TILE_M - 1) / ips::TILE_M;
-    if ((tm + 1) / 2 * ((prm.N + 255) / 256) >= nsm / 2) return run_tc<T, 256, true>(prm, nsm, st);
-    if (tm * ((prm.N + 127) / 128) >= nsm) return run_tc<T, 128, false>(prm, nsm, st);
-    return run_tc<T, 32, false>(prm, nsm, st);
+    const long long t32 = tm * ((prm.N + 31) / 32), t128 = tm * ((prm.N + 127) / 128);
+    const long long pairs = (tm + 1) / 2 * ((prm.N + 255) / 256);
+    // few tiles: up to four parts of at least 512 bytes of K that fit the SMs at once (eight: slower,
+    // 12 x 4096 -> 512 13.5 us for 10)
+    int splits = 1;
+    while (splits < 4 && 2 * splits * t32 <= nsm && raws >= 8 * splits) splits *= 2;
+    Choice best = {FORM_32, splits};
+    long long least = splits > 1 ? 5800 + 270 * (stages / splits) : 3400 + 270 * stages * rounds(t32, nsm);
+    const long long ns128 = 4600 + 375 * stages * rounds(t128, nsm);
+    if (ns128 < least) best = {FORM_128, 1}, least = ns128;
+    const long long ns_pair = 6000 + 520 * stages * rounds(pairs, nsm / 2);
+    if (ns_pair < least) best = {FORM_PAIR, 1}, least = ns_pair;
+    const long long blocks = (prm.M + 7) / 8, kv = prm.K > 1024 ? prm.K : 1024;     // a channel's reduction
+    if (blocks <= 65535 && 2200 + 29 * (prm.N * kv * blocks) / 100000 < least) best = {FORM_VEC, 1};
+    return best;
+}
+
+template <typename T>
+int run_scaled(ips::ScaledParams prm, int nsm, cudaStream_t st) {
+    const Choice c = choose(prm, nsm);
+    prm.splits = c.splits;
+    switch (c.form) {
+        case FORM_VEC:
+            if (prm.M == 1) return launch_vec_m<T, 1>(prm, nsm, st);
+            if (prm.M == 2) return launch_vec_m<T, 2>(prm, nsm, st);
+            if (prm.M <= 4) return launch_vec_m<T, 4>(prm, nsm, st);
+            return launch_vec_m<T, 8>(prm, nsm, st);
+        case FORM_32: return run_tc<T, 32, false>(prm, nsm, st);
+        case FORM_128: return run_tc<T, 128, false>(prm, nsm, st);
+        default: return run_tc<T, 256, true>(prm, nsm, st);
+    }
 }
 
 }  // namespace
@@ -251,6 +297,7 @@ int ip_linear_scaled_i8(const int8_t *x, long long ldx, const float *sx, const i
     prm.N = N;
     prm.act = act;
     prm.out_map = 0;
+    prm.splits = 1;
     prm.tiles_n = 0;
     prm.tiles = 0;
     prm.err = static_cast<int *>(workspace);

@@ -231,6 +231,7 @@ struct ScaledParams {
     long long M, ldx, ldw, ldy;
     int K, N, act;
     int out_map;                    // y has a tensor map
+    int splits;                     // CTAs that share a tile's K
     int tiles_n;
     long long tiles;
     int *err;
@@ -259,62 +260,69 @@ __device__ __forceinline__ uint4 chunk16(const int8_t *p, int n) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-template <typename T, int MT, int CPT, int KT>
+// ONE: K fits one round of chunks, whose x a thread keeps for all its channels.
+template <typename T, int MT, int CPT, int KT, bool ONE>
 __global__ void __launch_bounds__(VEC_THREADS) scaled_vec_kernel(const ScaledParams prm) {
-    constexpr int GROUPS = VEC_THREADS / KT, WARPS = KT / 32;
-    __shared__ int part[GROUPS][WARPS][MT * CPT];
+    constexpr int GROUPS = VEC_THREADS / KT, WARPS = KT / 32, BLOCK = GROUPS * CPT;
+    __shared__ int part[2][GROUPS][WARPS][MT * CPT];
     pdl_launch_dependents();
     pdl_wait();
     const int t = threadIdx.x % KT, g = threadIdx.x / KT;
     const long long m0 = static_cast<long long>(blockIdx.y) * MT;
-    const int n0 = (static_cast<int>(blockIdx.x) * GROUPS + g) * CPT;
     const int mv = static_cast<int>(prm.M - m0 < MT ? prm.M - m0 : MT);
-    int acc[MT][CPT];
+    auto load_x = [&](uint4 (&x)[MT], int k) {
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+        for (int i = 0; i < MT; ++i)
+            x[i] = i < mv && k < prm.K ? chunk16(prm.x + (m0 + i) * prm.ldx + k, prm.K - k) : make_uint4(0, 0, 0, 0);
+    };
+    uint4 x[MT];
+    if (ONE) load_x(x, t * 16);
+    int turn = 0;
+    for (int c0 = static_cast<int>(blockIdx.x) * BLOCK; c0 < prm.N; c0 += static_cast<int>(gridDim.x) * BLOCK) {
+        const int n0 = c0 + g * CPT;
+        int acc[MT][CPT];
 #pragma unroll
-        for (int j = 0; j < CPT; ++j) acc[i][j] = 0;
-#pragma unroll 2
-    for (int k = t * 16; k < prm.K; k += KT * 16) {
-        uint4 w[CPT];
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < CPT; ++j)
-            w[j] = n0 + j < prm.N ? chunk16(prm.w + (n0 + j) * prm.ldw + k, prm.K - k)
-                                  : make_uint4(0, 0, 0, 0);
+            for (int j = 0; j < CPT; ++j) acc[i][j] = 0;
+        for (int k = t * 16; k < (ONE ? t * 16 + 1 : prm.K); k += KT * 16) {
+            uint4 w[CPT];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            if (i >= mv) continue;
-            const uint4 x = chunk16(prm.x + (m0 + i) * prm.ldx + k, prm.K - k);
+            for (int j = 0; j < CPT; ++j)
+                w[j] = n0 + j < prm.N && k < prm.K ? chunk16(prm.w + (n0 + j) * prm.ldw + k, prm.K - k)
+                                                   : make_uint4(0, 0, 0, 0);
+            if (!ONE) load_x(x, k);
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < CPT; ++j) {
+                    int a = acc[i][j];
+                    a = __dp4a(static_cast<int>(x[i].x), static_cast<int>(w[j].x), a);
+                    a = __dp4a(static_cast<int>(x[i].y), static_cast<int>(w[j].y), a);
+                    a = __dp4a(static_cast<int>(x[i].z), static_cast<int>(w[j].z), a);
+                    acc[i][j] = __dp4a(static_cast<int>(x[i].w), static_cast<int>(w[j].w), a);
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < CPT; ++j) {
-                int a = acc[i][j];
-                a = __dp4a(static_cast<int>(x.x), static_cast<int>(w[j].x), a);
-                a = __dp4a(static_cast<int>(x.y), static_cast<int>(w[j].y), a);
-                a = __dp4a(static_cast<int>(x.z), static_cast<int>(w[j].z), a);
-                acc[i][j] = __dp4a(static_cast<int>(x.w), static_cast<int>(w[j].w), a);
+                const int s = __reduce_add_sync(0xffffffffu, acc[i][j]);
+                if ((threadIdx.x & 31) == 0) part[turn][g][t >> 5][i * CPT + j] = s;
             }
+        __syncthreads();       // the other half of `part` is read until the next one
+        // consecutive threads finish consecutive channels of a token
+        for (int e = threadIdx.x; e < MT * BLOCK; e += VEC_THREADS) {
+            const int i = e / BLOCK, c = e % BLOCK, n = c0 + c;
+            if (i >= mv || n >= prm.N) continue;
+            int s = 0;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) s += part[turn][c / CPT][w][i * CPT + c % CPT];
+            const float z = finish<T>(static_cast<float>(s), prm.sx[m0 + i] * prm.sw[n],
+                                      prm.bias ? prm.bias[n] : 0.0f, prm.act);
+            static_cast<T *>(prm.y)[(m0 + i) * prm.ldy + n] = from_f32<T>(z);
         }
-    }
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < CPT; ++j) {
-            const int s = __reduce_add_sync(0xffffffffu, acc[i][j]);
-            if ((threadIdx.x & 31) == 0) part[g][t >> 5][i * CPT + j] = s;
-        }
-    __syncthreads();
-    // consecutive threads finish consecutive channels of a token
-    for (int e = threadIdx.x; e < GROUPS * MT * CPT; e += VEC_THREADS) {
-        const int i = e / (GROUPS * CPT), c = e % (GROUPS * CPT);
-        const int n = static_cast<int>(blockIdx.x) * GROUPS * CPT + c;
-        if (i >= mv || n >= prm.N) continue;
-        const int at = i * CPT + c % CPT;
-        int s = 0;
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) s += part[c / CPT][w][at];
-        const float z = finish<T>(static_cast<float>(s), prm.sx[m0 + i] * prm.sw[n],
-                                  prm.bias ? prm.bias[n] : 0.0f, prm.act);
-        static_cast<T *>(prm.y)[(m0 + i) * prm.ldy + n] = from_f32<T>(z);
+        turn ^= 1;
     }
 }
 
@@ -429,6 +437,15 @@ __device__ __forceinline__ void arrive_first(uint32_t bar) {
         "{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, 0;\n"
         " mbarrier.arrive.release.cluster.shared::cluster.b64 _, [r];\n}\n" ::"r"(bar)
         : "memory");
+}
+// Word at this shared-memory offset of the cluster's CTA `rank`.
+__device__ __forceinline__ int ld_cluster(uint32_t addr, int rank) {
+    int v;
+    asm volatile("{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %1, %2;\n ld.shared::cluster.s32 %0, [r];\n}\n"
+                 : "=r"(v)
+                 : "r"(addr), "r"(rank)
+                 : "memory");
+    return v;
 }
 // True in one lane of a converged warp, always the same.
 __device__ __forceinline__ bool elect_one() {
@@ -549,8 +566,10 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t sr
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
 
-// LONG: K > 1024, several segments per tile.
-template <typename T, int BN, bool LONG, bool PAIR>
+// LONG: a CTA's K is longer than 1024, several segments per tile.  KSPLIT: the CTAs of a cluster
+// share one tile's K and add their sums through each other's shared memory, a part of the
+// rows each (few tiles: 64 x 4096 -> 1024 in 32 tiles 20 us, by clusters of four 8).
+template <typename T, int BN, bool LONG, bool PAIR, bool KSPLIT>
 __global__ void __launch_bounds__(TC_THREADS, 1)
     scaled_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w,
                      const __grid_constant__ CUtensorMap tm_y, const ScaledParams prm) {
@@ -572,7 +591,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     const uint32_t drained = base + C::BARS + 8u * (2 * C::RS + 2 * C::FS + 4);
     volatile int *dead = reinterpret_cast<volatile int *>(smem + C::DEAD);
     const int rank = PAIR ? static_cast<int>(blockIdx.x & 1u) : 0;      // clusters are (2, 1, 1)
-    const long long worker = blockIdx.x / C::CTAS, workers = gridDim.x / C::CTAS;
+    static_assert(!KSPLIT || (BN == 32 && !PAIR && 4 * TILE_M * BN == EPI_WARPS * OUT_BLOCK), "sums fit");
+    const int splits = KSPLIT ? prm.splits : 1;                         // else clusters are (splits, 1, 1)
+    const int part = KSPLIT ? static_cast<int>(blockIdx.x) % splits : 0;
+    const long long worker = blockIdx.x / (KSPLIT ? splits : C::CTAS), workers = gridDim.x / (KSPLIT ? splits : C::CTAS);
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::RS; ++s) {
@@ -605,7 +627,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     const uint32_t tmem = lds32(base + C::TMEM_PTR);
     pdl_wait();
 
-    const int stages = (prm.K + RAW_K - 1) / RAW_K * 2;      // fp16 stages (K behind the end reads as 0)
+    // raw stages of this CTA (K behind the end reads as 0), two fp16 stages each
+    const int raws = (prm.K + RAW_K - 1) / RAW_K;
+    const int raw0 = KSPLIT ? raws * part / splits : 0, raw1 = KSPLIT ? raws * (part + 1) / splits : raws;
+    const int stages = 2 * (raw1 - raw0);
     const long long limit = prm.timeout_cycles;
 
     if (warp >= EPI_WARPS + CONV_WARPS) {
@@ -617,7 +642,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
                 const int m0 = static_cast<int>(tile / prm.tiles_n) * (TILE_M * C::CTAS) + rank * TILE_M;
                 const int n0 = static_cast<int>(tile % prm.tiles_n) * BN + rank * C::BR;
-                for (int k = 0; k < prm.K; k += RAW_K) {
+                for (int r = raw0; r < raw1; ++r) {
+                    const int k = r * RAW_K;
                     ok = wait_or_dead<false>(raw_empty(s), ph ^ 1, dead, limit);
                     if (!ok) break;
                     const uint32_t st = base + C::RAW_AT + s * C::RAW;
@@ -805,8 +831,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                         tma_store_2d(&tm_y, block, n0 + cb, static_cast<int>(mq));
                 }
             };
-            int sum[LONG ? CH : 1][16];
-            if (LONG)
+            int sum[LONG || KSPLIT ? CH : 1][16];
+            if (LONG || KSPLIT)
 #pragma unroll
                 for (int c = 0; c < CH; ++c)
 #pragma unroll
@@ -821,7 +847,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                     uint32_t r[16];
                     tmem_ld16(at + 16 * c, r);
                     tmem_wait_ld();
-                    if (LONG) {
+                    if (LONG || KSPLIT) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) sum[c][i] += __float2int_rn(__uint_as_float(r[i]));
                     } else {
@@ -837,7 +863,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                 a ^= 1;
                 aph ^= a == 0;
             }
-            if (LONG && ok) {
+            if (KSPLIT && ok) {
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    sts128(base + C::OUT_AT + 4u * ((quarter * 32 + lane) * BN + col0 + i), sum[0][i], sum[0][i + 1],
+                           sum[0][i + 2], sum[0][i + 3]);
+            } else if (LONG && ok) {
 #pragma unroll
                 for (int c = 0; c < CH; ++c) {
                     float s[16];
@@ -850,6 +881,22 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         if (staged && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
+    if (KSPLIT) {
+        cluster_sync();           // every part's sums are in place
+        const int row0 = TILE_M * part / splits, rows = TILE_M * (part + 1) / splits - row0;
+        const long long m0 = worker / prm.tiles_n * TILE_M;
+        const int n0 = static_cast<int>(worker % prm.tiles_n) * BN;
+        for (int e = threadIdx.x; e < rows * BN; e += TC_THREADS) {
+            const int r = row0 + e / BN, c = e % BN, n = n0 + c;
+            if (m0 + r >= prm.M || n >= prm.N) continue;
+            int sum = 0;
+            for (int i = 0; i < splits; ++i) sum += ld_cluster(base + C::OUT_AT + 4u * (r * BN + c), i);
+            static_cast<T *>(prm.y)[(m0 + r) * prm.ldy + n] =
+                from_f32<T>(finish<T>(static_cast<float>(sum), prm.sx[m0 + r] * prm.sw[n],
+                                      prm.bias ? prm.bias[n] : 0.0f, prm.act));
+        }
+        cluster_sync();           // no part ends while another reads its sums
+    }
     if (PAIR) cluster_sync();     // neither CTA ends while the other may still arrive on its barriers
     else __syncthreads();
     if (warp == MMA_WARP) tmem_free<PAIR>(tmem, C::COLS);

@@ -164,7 +164,8 @@ def check_product(ip, M, K, N, dt, swish=False, bias=True, seed=0, lo=-127, hi=1
                                    (5, 17, 640), (8, 4096, 1024), (7, 2049, 5000), (1, 1024, 20000),
                                    (9, 64, 32), (9, 1, 1), (33, 100, 77), (127, 1024, 256), (128, 63, 128),
                                    (129, 65, 129), (200, 1025, 300), (333, 1000, 777), (257, 4096, 96),
-                                   (1000, 128, 5000), (2500, 520, 2100), (3000, 2100, 1030)])
+                                   (1000, 128, 5000), (2500, 520, 2100), (3000, 2100, 1030),
+                                   (17, 4096, 1024), (100, 8192, 70), (129, 3000, 33), (12, 32768, 40)])
 def test_product(ip, dtype, M, K, N):
     check_product(ip, M, K, N, DT[dtype])
 
