@@ -1030,6 +1030,8 @@ def kv4_read(cache, start, page_table, T: int, *, count=None, dtype=None, out=No
     import torch
     B, (n_pages, H, page, width), (pst, pct) = _kv4_args(
         _need(start, "start").numel(), cache, page_table, workspace, (start, count), ("", "start", "count"))
+    if T < 0:
+        raise ValueError(f"T must not be negative, got {T}")
     dev, shape = cache.device, (B, T, H, IP_DH)
     dtype = dtype or (torch.bfloat16 if out is None else out[0].dtype)
     code = _dtype_code(dtype)

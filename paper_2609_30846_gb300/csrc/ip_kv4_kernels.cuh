@@ -193,10 +193,17 @@ __global__ void __launch_bounds__(ROW_THREADS) kv4_read_kernel(const RowParams p
 // ---- attention over the pages -------------------------------------------
 //
 // o[r] = sum_j p_rj v_j / sum_j p_rj, p_rj = exp(scale q_r k_j - max), for the G T query
-// rows r = t G + g that share a cache head, 8 NT rows to a CTA and the keys cut into
-// chunks.  Bound by the cache's bytes: every code is read once per row tile, straight from
-// global memory into the fragments of the fp16 warp MMA (m16n8k16) with tokens or
-// channels as its 16 rows and the query rows as its 8 columns.
+// rows r = t G + g that share a cache head, 8 NT rows to a CTA.  Every code is read once per row
+// tile, by asynchronous copies into a ring of each warp, and goes from there into the
+// fragments of the fp16 warp MMA (m16n8k16) with tokens or channels as its 16 rows and the
+// query rows as its 8 columns: with 8 rows the MMA's half-empty other form would cost
+// as much as the codes' conversion.
+//
+// What bounds it (64 sequences of 4096 tokens, 8 heads, one row each): 73 us for 302 MB, 4.15
+// TB/s; the copies alone take 53 us, copies and scores 55 us.  An instruction that turns
+// codes into fragments works on two codes a lane, which makes some 340 instructions for 16
+// tokens (171 on the integer pipe, which would take 85 cycles at full rate) where the bytes
+// take 101 cycles an SM; with three CTAs an SM the warps cannot hide all their latencies.
 //
 // Scores: a nibble u = c + 8 masked out of its word is the subnormal fp16 number u 2^-24
 // (or u 2^-20), exact in the MMA, so a fragment costs one instruction; the accumulators
@@ -205,7 +212,7 @@ __global__ void __launch_bounds__(ROW_THREADS) kv4_read_kernel(const RowParams p
 // of its row (largest magnitude in [2^14, 2^15)): exact but for elements more than 2^24
 // smaller than the largest, which lose parts below 2^-39 of it.
 //
-// Softmax: running maximum and sum in f32, per warp over its own tokens (16 at a time).
+// Softmax: running reference and sum in f32, per warp over its own tokens (32 at a time).
 //
 // Output: p times the V scale, relative to the running largest exponent of the V scales
 // and times 2^HEAD, rounds to fp16 (half a step 2^-11; terms below 2^-23 of the largest fade
@@ -225,7 +232,7 @@ constexpr int ATT_WARPS = 4;
 constexpr int ATT_THREADS = 32 * ATT_WARPS;
 constexpr int CTAS_8 = 3, CTAS_16 = 2;        // CTAs on an SM with 8 and 16 rows
 constexpr int UNIT = 128;                     // keys of a unit of work: 32 to a warp
-constexpr int OVER = 3;
+constexpr int OVER = 3;                       // units that beginning an item is counted as (ragged to 8192: 1 91 us, 2 85, 3 78)
 constexpr int MAX_SCAN = 2048;                // row tiles of all sequences that a CTA will sum up
 constexpr int PART = DH + 4;                  // floats of a partial row: output, maximum, sum, two unused
 
@@ -340,7 +347,8 @@ constexpr int STAGES = 2;
 constexpr int HEAD = 9, SLACK = 4;      // p s / 2^e < 2^(SLACK + 1), so its fp16 value is below 2^14
 constexpr int BATCH = 32, BATCH_BYTES = BATCH * ROW_BYTES;
 constexpr int RING = STAGES * BATCH_BYTES;
-__host__ __device__ constexpr int row_floats(int R) { return R * (DH + 2); }              // [R][DH], then maximum and sum [R][2]
+// a warp's rows: [R][DH], then maximum and sum [R][2]
+__host__ __device__ constexpr int row_floats(int R) { return R * (DH + 2); }
 __host__ __device__ constexpr int smem_bytes(int R) { return ATT_WARPS * (RING + row_floats(R) * 4); }
 constexpr int B_V = BATCH * 64, B_KS = 2 * BATCH * 64, B_VS = B_KS + BATCH * 8;
 
@@ -508,293 +516,293 @@ __global__ void __launch_bounds__(ATT_THREADS, NT == 1 ? CTAS_8 : CTAS_16) kv4_a
     start();
 
     for (;;) {
-    const int b = it.b, h = it.h, row0 = it.row0, kv_end = it.kv_end, t_begin = u0 * UNIT + warp * BATCH, t_end = end;
+        const int b = it.b, h = it.h, row0 = it.row0, kv_end = it.kv_end, t_begin = u0 * UNIT + warp * BATCH, t_end = end;
 
-    // query fragments (row g8 of each eight), group sums and per-row constants (rows 2 t4, 2 t4 + 1)
-    uint32_t qf[NT][4][4];
-    float qsum[NT][4][2], rscale[NT][2];
-    int lim[NT][2];
+        // query fragments (row g8 of each eight), group sums and per-row constants (rows 2 t4, 2 t4 + 1)
+        uint32_t qf[NT][4][4];
+        float qsum[NT][4][2], rscale[NT][2];
+        int lim[NT][2];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int row = nt * 8 + g8;
-        const bool live = it.limit(prm, row) > 0;
-        float x[4][8], top = 0.0f;
-        const int t = (row0 + row) / prm.G, g = (row0 + row) - t * prm.G;
-        const T *src = static_cast<const T *>(prm.q) +
-                       (live ? b * prm.qs[0] + t * prm.qs[1] + (static_cast<long long>(h) * prm.G + g) * prm.qs[2] : 0);
-        const bool vec = (reinterpret_cast<uintptr_t>(src) & 15) == 0;
-#pragma unroll
-        for (int gr = 0; gr < 4; ++gr) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[gr][i] = 0.0f;
-            if (live) load8(src + 32 * gr + 8 * t4, vec, 8, x[gr]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[gr][i]));
-        }
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const int ex = 268 - static_cast<int>(__float_as_uint(top) >> 23);
-        const int fe = ex > 254 ? 254 : ex;
-        const float up = __uint_as_float(static_cast<uint32_t>(fe) << 23);
-        const float rs = fmaxf(ldexpf(prm.scale_log2, 24 - (fe - 127)), 0x1p-126f);   // > 0: -inf times it
-        float sums[4];
-#pragma unroll
-        for (int gr = 0; gr < 4; ++gr) {
-            float s = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[gr][i] *= up;
-                s += x[gr][i];
-            }
-            s += __shfl_xor_sync(0xffffffffu, s, 1);
-            s += __shfl_xor_sync(0xffffffffu, s, 2);
-            sums[gr] = s * -0x1p-21f;      // -8 2^-24
-            // nibbles 0, 4 and 2, 6 (u 2^-24), then 1, 5 and 3, 7 (u 2^-20: q by 2^-4)
-            qf[nt][gr][0] = pack_half2(x[gr][0], x[gr][4]);
-            qf[nt][gr][1] = pack_half2(x[gr][2], x[gr][6]);
-            qf[nt][gr][2] = pack_half2(x[gr][1] * 0.0625f, x[gr][5] * 0.0625f);
-            qf[nt][gr][3] = pack_half2(x[gr][3] * 0.0625f, x[gr][7] * 0.0625f);
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int from = (2 * t4 + i) * 4;       // a lane of that row
-#pragma unroll
-            for (int gr = 0; gr < 4; ++gr) qsum[nt][gr][i] = __shfl_sync(0xffffffffu, sums[gr], from);
-            rscale[nt][i] = __shfl_sync(0xffffffffu, rs, from);
-            lim[nt][i] = it.limit(prm, nt * 8 + 2 * t4 + i);
-        }
-    }
-
-    // Row i of the score MMA is token i / 2 of its eight for even i, 4 + (i / 2 ^ 1) for odd i: the
-    // 16-byte reads of neighbouring rows fall on different banks, and the transposed
-    // probabilities of lane (g8, t4) belong to the tokens t4 and 4 + (t4 ^ 1) of each eight.
-    const int tok = g8 & 1 ? 4 + ((g8 >> 1) ^ 1) : g8 >> 1, odd4 = 4 + (t4 ^ 1);
-    const uint8_t *at_k = my_ring + tok * 64 + t4 * 16, *at_s = my_ring + tok * 8;
-    const uint8_t *at_v = my_ring + t4 * 64 + g8 * 8, *at_vo = my_ring + odd4 * 64 + g8 * 8;
-    // m: the reference of the row's exponentials, mr: in units of log2.  It is raised to the
-    // maximum only when a score exceeds it by more than SLACK there (lift: the score that does):
-    // the probabilities reach 2^SLACK at most, and most batches skip the rescaling.
-    float o[NT][8][4], m[NT][2], mr[NT][2], l[NT][2], lift[NT][2];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[nt][i][j] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            m[nt][i] = lift[nt][i] = -INFINITY;
-            mr[nt][i] = l[nt][i] = 0.0f;
-        }
-    }
-    int ev = 16;          // running largest exponent field of the V scales
-    float norm = __uint_as_float((254u + HEAD - 16u) << 23);      // 2^(HEAD - (ev - 127))
-    uint32_t ev_top = (17u << 7) - 1u;                            // largest scale of that exponent
-
-    for (int t0 = t_begin; t0 < t_end; t0 += STEP) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
-        __syncwarp();     // all lanes' copies have landed, and all have read the slot before
-        copy();
-        const uint32_t gone = (dead >> (2 * (STAGES - 1))) & 3u;       // this batch was copied so long ago
-        const bool full = t0 + BATCH <= it.kv_full && gone == 0;
-
-        // scores: rows 2 t4 and 2 t4 + 1 for the tokens tok, 8 + tok, 16 + tok, 24 + tok
-        float s[NT][8];
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-            const uint4 k0 = hf ? at128<1024>(at_k + use) : at128<0>(at_k + use);
-            const uint4 k1 = hf ? at128<1536>(at_k + use) : at128<512>(at_k + use);
-            const uint2 c0 = hf ? at64<B_KS + 128>(at_s + use) : at64<B_KS>(at_s + use);
-            const uint2 c1 = hf ? at64<B_KS + 192>(at_s + use) : at64<B_KS + 64>(at_s + use);
+        for (int nt = 0; nt < NT; ++nt) {
+            const int row = nt * 8 + g8;
+            const bool live = it.limit(prm, row) > 0;
+            float x[4][8], top = 0.0f;
+            const int t = (row0 + row) / prm.G, g = (row0 + row) - t * prm.G;
+            const T *src = static_cast<const T *>(prm.q) +
+                           (live ? b * prm.qs[0] + t * prm.qs[1] + (static_cast<long long>(h) * prm.G + g) * prm.qs[2] : 0);
+            const bool vec = (reinterpret_cast<uintptr_t>(src) & 15) == 0;
 #pragma unroll
             for (int gr = 0; gr < 4; ++gr) {
-                const uint32_t w0 = gr == 0 ? k0.x : (gr == 1 ? k0.y : (gr == 2 ? k0.z : k0.w)), y0 = w0 >> 8;
-                const uint32_t w1 = gr == 0 ? k1.x : (gr == 1 ? k1.y : (gr == 2 ? k1.z : k1.w)), y1 = w1 >> 8;
-                const uint32_t s0 = gr < 2 ? c0.x : c0.y, s1 = gr < 2 ? c1.x : c1.y;
-                const float f0 = gr & 1 ? bf16_hi(s0) : bf16_lo(s0), f1 = gr & 1 ? bf16_hi(s1) : bf16_lo(s1);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    float acc[4], (&r)[8] = s[nt];
-                    mma16_from(acc, qsum[nt][gr], w0 & 0x000f000fu, w1 & 0x000f000fu, y0 & 0x000f000fu,
-                               y1 & 0x000f000fu, qf[nt][gr][0], qf[nt][gr][1]);
-                    mma16(acc, w0 & 0x00f000f0u, w1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u,
-                          qf[nt][gr][2], qf[nt][gr][3]);
-                    r[4 * hf] = gr == 0 ? f0 * acc[0] : fmaf(f0, acc[0], r[4 * hf]);
-                    r[4 * hf + 1] = gr == 0 ? f0 * acc[1] : fmaf(f0, acc[1], r[4 * hf + 1]);
-                    r[4 * hf + 2] = gr == 0 ? f1 * acc[2] : fmaf(f1, acc[2], r[4 * hf + 2]);
-                    r[4 * hf + 3] = gr == 0 ? f1 * acc[3] : fmaf(f1, acc[3], r[4 * hf + 3]);
-                }
+                for (int i = 0; i < 8; ++i) x[gr][i] = 0.0f;
+                if (live) load8(src + 32 * gr + 8 * t4, vec, 8, x[gr]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[gr][i]));
             }
-        }
-        uint2 vs[4] = {at64<B_VS>(at_s + use), at64<B_VS + 64>(at_s + use), at64<B_VS + 128>(at_s + use),
-                       at64<B_VS + 192>(at_s + use)};
-        if (!full) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int pos = t0 + 8 * i + tok;
-                const bool none = (gone >> (i >> 1)) & 1u;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        if (none || pos >= lim[nt][j]) s[nt][2 * i + j] = -INFINITY;
-                // V scales of tokens that no row sees may hold anything
-                if (none || pos >= kv_end) vs[i] = make_uint2(0, 0);
-            }
-        }
-        bool raise = false;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                raise |= fmaxf(fmaxf(s[nt][j], s[nt][2 + j]), fmaxf(s[nt][4 + j], s[nt][6 + j])) > lift[nt][j];
-        uint32_t top = __vimax3_u16x2(vs[0].x, vs[0].y, vs[1].x);
-        top = __vimax3_u16x2(__vimax3_u16x2(top, vs[1].y, vs[2].x), vs[2].y, vs[3].x);
-        top = __vimax3_u16x2(top, vs[3].y, 0u);
-        raise |= (top >> 16) > ev_top || (top & 0xffffu) > ev_top;
-        if (__any_sync(0xffffffffu, raise)) {
-            int et = ev;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {     // a NaN (field 255) must not hide the others' range
-                    const int f = static_cast<int>((j < 2 ? vs[i].x : vs[i].y) >> (j & 1 ? 23 : 7)) & 0xff;
-                    et = f < 255 && f > et ? f : et;
-                }
-            const int en = static_cast<int>(__reduce_max_sync(0xffffffffu, static_cast<unsigned>(et)));
-            const float down = ev - en < -126 ? 0.0f : __uint_as_float(static_cast<uint32_t>(127 + ev - en) << 23);
-            ev = en;
-            norm = __uint_as_float(static_cast<uint32_t>(254 + HEAD - ev) << 23);
-            ev_top = (static_cast<uint32_t>(ev + 1) << 7) - 1u;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    float t = m[nt][j];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) t = fmaxf(t, s[nt][2 * i + j]);
-                    t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
-                    t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
-                    t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
-                    const float tr = t == -INFINITY ? 0.0f : t * rscale[nt][j];
-                    const float a = m[nt][j] == -INFINITY ? 0.0f : fast_exp2(mr[nt][j] - tr);
-                    m[nt][j] = t;
-                    mr[nt][j] = tr;
-                    lift[nt][j] = t + __fdividef(static_cast<float>(SLACK), rscale[nt][j]);
-                    l[nt][j] *= a;
-                    const float ad = a * down;
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) o[nt][c][j] *= ad, o[nt][c][2 + j] *= ad;
-                }
-        }
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-            float p[NT][4];           // norm times the probabilities
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float e1 = fast_exp2(fmaf(s[nt][4 * hf + i], rscale[nt][i & 1], -mr[nt][i & 1]));
-                    l[nt][i & 1] += e1;
-                    p[nt][i] = e1 * norm;
-                }
-            const uint2 v0 = hf ? at64<B_V + 1024>(at_v + use) : at64<B_V>(at_v + use);
-            const uint2 v1 = hf ? at64<B_V + 1024>(at_vo + use) : at64<B_V>(at_vo + use);
-            const uint2 v2 = hf ? at64<B_V + 1536>(at_v + use) : at64<B_V + 512>(at_v + use);
-            const uint2 v3 = hf ? at64<B_V + 1536>(at_vo + use) : at64<B_V + 512>(at_vo + use);
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const int ex = 268 - static_cast<int>(__float_as_uint(top) >> 23);
+            const int fe = ex > 254 ? 254 : ex;
+            const float up = __uint_as_float(static_cast<uint32_t>(fe) << 23);
+            const float rs = fmaxf(ldexpf(prm.scale_log2, 24 - (fe - 127)), 0x1p-126f);   // > 0: -inf times it
+            float sums[4];
 #pragma unroll
             for (int gr = 0; gr < 4; ++gr) {
-                const uint32_t x0 = gr < 2 ? vs[2 * hf].x : vs[2 * hf].y, x1 = gr < 2 ? vs[2 * hf + 1].x : vs[2 * hf + 1].y;
-                const float f0 = gr & 1 ? bf16_hi(x0) : bf16_lo(x0), f1 = gr & 1 ? bf16_hi(x1) : bf16_lo(x1);
-                const uint32_t sel = gr & 1 ? 0x7632 : 0x5410;
-                const uint32_t a = gr < 2 ? __byte_perm(v0.x, v1.x, sel) : __byte_perm(v0.y, v1.y, sel);
-                const uint32_t c = gr < 2 ? __byte_perm(v2.x, v3.x, sel) : __byte_perm(v2.y, v3.y, sel);
-                const uint32_t a8 = a >> 8, c8 = c >> 8;
-                const uint32_t a0 = centred_lo(a), a1 = centred_hi(a), a2 = centred_lo(c), a3 = centred_hi(c);
-                const uint32_t d0 = centred_lo(a8), d1 = centred_hi(a8), d2 = centred_lo(c8), d3 = centred_hi(c8);
+                float s = 0.0f;
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    // p s rounded to fp16, then tokens against rows turned into the MMA's order
-                    const uint32_t b0 = transpose8(pack_half2(p[nt][0] * f0, p[nt][1] * f0));
-                    const uint32_t b1 = transpose8(pack_half2(p[nt][2] * f1, p[nt][3] * f1));
-                    mma16(o[nt][2 * gr], a0, a1, a2, a3, b0, b1);
-                    mma16(o[nt][2 * gr + 1], d0, d1, d2, d3, b0, b1);
+                for (int i = 0; i < 8; ++i) {
+                    x[gr][i] *= up;
+                    s += x[gr][i];
                 }
+                s += __shfl_xor_sync(0xffffffffu, s, 1);
+                s += __shfl_xor_sync(0xffffffffu, s, 2);
+                sums[gr] = s * -0x1p-21f;      // -8 2^-24
+                // nibbles 0, 4 and 2, 6 (u 2^-24), then 1, 5 and 3, 7 (u 2^-20: q by 2^-4)
+                qf[nt][gr][0] = pack_half2(x[gr][0], x[gr][4]);
+                qf[nt][gr][1] = pack_half2(x[gr][2], x[gr][6]);
+                qf[nt][gr][2] = pack_half2(x[gr][1] * 0.0625f, x[gr][5] * 0.0625f);
+                qf[nt][gr][3] = pack_half2(x[gr][3] * 0.0625f, x[gr][7] * 0.0625f);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int from = (2 * t4 + i) * 4;       // a lane of that row
+#pragma unroll
+                for (int gr = 0; gr < 4; ++gr) qsum[nt][gr][i] = __shfl_sync(0xffffffffu, sums[gr], from);
+                rscale[nt][i] = __shfl_sync(0xffffffffu, rs, from);
+                lim[nt][i] = it.limit(prm, nt * 8 + 2 * t4 + i);
             }
         }
-        use = use + BATCH_BYTES == STAGES * BATCH_BYTES ? 0 : use + BATCH_BYTES;
-    }
 
-    // the share's next part: its first copies run while this part's rows are joined
-    const Item done = it;
-    const int d0 = u0, d1 = u1, d_units = units, d_item = e * prm.H + head;
-    bool more = prm.split && u1 == units && left > 0;
-    if (more) {
-        u0 = -over;
-        if (++head == prm.H) head = 0, ++e;
-        it = Item(prm, e, head, R);
-        units = it.units();
-        more = take();
-        __syncwarp();
-        if (more) start();
-    }
-    __syncthreads();              // the rows before these have been read
-
-    // a warp's rows to shared memory: output over norm, maximum, sum
-    {
-        const float unit = ldexpf(1.0f, ev - 127 - HEAD);
+        // Row i of the score MMA is token i / 2 of its eight for even i, 4 + (i / 2 ^ 1) for odd i: the
+        // 16-byte reads of neighbouring rows fall on different banks, and the transposed
+        // probabilities of lane (g8, t4) belong to the tokens t4 and 4 + (t4 ^ 1) of each eight.
+        const int tok = g8 & 1 ? 4 + ((g8 >> 1) ^ 1) : g8 >> 1, odd4 = 4 + (t4 ^ 1);
+        const uint8_t *at_k = my_ring + tok * 64 + t4 * 16, *at_s = my_ring + tok * 8;
+        const uint8_t *at_v = my_ring + t4 * 64 + g8 * 8, *at_vo = my_ring + odd4 * 64 + g8 * 8;
+        // m: the reference of the row's exponentials, mr: in units of log2.  It is raised to the
+        // maximum only when a score exceeds it by more than SLACK there (lift: the score that does):
+        // the probabilities reach 2^SLACK at most, and most batches skip the rescaling.
+        float o[NT][8][4], m[NT][2], mr[NT][2], l[NT][2], lift[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[nt][i][j] = 0.0f;
+#pragma unroll
             for (int i = 0; i < 2; ++i) {
-                float sum = l[nt][i];
-                sum += __shfl_xor_sync(0xffffffffu, sum, 4);
-                sum += __shfl_xor_sync(0xffffffffu, sum, 8);
-                sum += __shfl_xor_sync(0xffffffffu, sum, 16);
-                if (g8 == 0) {
-                    float *ml = my_rows + R * DH + 2 * (nt * 8 + 2 * t4 + i);
-                    ml[0] = m[nt][i] == -INFINITY ? -INFINITY : mr[nt][i];
-                    ml[1] = sum;
+                m[nt][i] = lift[nt][i] = -INFINITY;
+                mr[nt][i] = l[nt][i] = 0.0f;
+            }
+        }
+        int ev = 16;          // running largest exponent field of the V scales
+        float norm = __uint_as_float((254u + HEAD - 16u) << 23);      // 2^(HEAD - (ev - 127))
+        uint32_t ev_top = (17u << 7) - 1u;                            // largest scale of that exponent
+
+        for (int t0 = t_begin; t0 < t_end; t0 += STEP) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+            __syncwarp();     // all lanes' copies have landed, and all have read the slot before
+            copy();
+            const uint32_t gone = (dead >> (2 * (STAGES - 1))) & 3u;       // this batch was copied so long ago
+            const bool full = t0 + BATCH <= it.kv_full && gone == 0;
+
+            // scores: rows 2 t4 and 2 t4 + 1 for the tokens tok, 8 + tok, 16 + tok, 24 + tok
+            float s[NT][8];
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+                const uint4 k0 = hf ? at128<1024>(at_k + use) : at128<0>(at_k + use);
+                const uint4 k1 = hf ? at128<1536>(at_k + use) : at128<512>(at_k + use);
+                const uint2 c0 = hf ? at64<B_KS + 128>(at_s + use) : at64<B_KS>(at_s + use);
+                const uint2 c1 = hf ? at64<B_KS + 192>(at_s + use) : at64<B_KS + 64>(at_s + use);
+#pragma unroll
+                for (int gr = 0; gr < 4; ++gr) {
+                    const uint32_t w0 = gr == 0 ? k0.x : (gr == 1 ? k0.y : (gr == 2 ? k0.z : k0.w)), y0 = w0 >> 8;
+                    const uint32_t w1 = gr == 0 ? k1.x : (gr == 1 ? k1.y : (gr == 2 ? k1.z : k1.w)), y1 = w1 >> 8;
+                    const uint32_t s0 = gr < 2 ? c0.x : c0.y, s1 = gr < 2 ? c1.x : c1.y;
+                    const float f0 = gr & 1 ? bf16_hi(s0) : bf16_lo(s0), f1 = gr & 1 ? bf16_hi(s1) : bf16_lo(s1);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        float acc[4], (&r)[8] = s[nt];
+                        mma16_from(acc, qsum[nt][gr], w0 & 0x000f000fu, w1 & 0x000f000fu, y0 & 0x000f000fu,
+                                   y1 & 0x000f000fu, qf[nt][gr][0], qf[nt][gr][1]);
+                        mma16(acc, w0 & 0x00f000f0u, w1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u,
+                              qf[nt][gr][2], qf[nt][gr][3]);
+                        r[4 * hf] = gr == 0 ? f0 * acc[0] : fmaf(f0, acc[0], r[4 * hf]);
+                        r[4 * hf + 1] = gr == 0 ? f0 * acc[1] : fmaf(f0, acc[1], r[4 * hf + 1]);
+                        r[4 * hf + 2] = gr == 0 ? f1 * acc[2] : fmaf(f1, acc[2], r[4 * hf + 2]);
+                        r[4 * hf + 3] = gr == 0 ? f1 * acc[3] : fmaf(f1, acc[3], r[4 * hf + 3]);
+                    }
                 }
             }
+            uint2 vs[4] = {at64<B_VS>(at_s + use), at64<B_VS + 64>(at_s + use), at64<B_VS + 128>(at_s + use),
+                           at64<B_VS + 192>(at_s + use)};
+            if (!full) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < 4; ++i) {
+                    const int pos = t0 + 8 * i + tok;
+                    const bool none = (gone >> (i >> 1)) & 1u;
 #pragma unroll
-                for (int c = 0; c < 8; ++c)      // m-tile c: channels 32 (c / 2) + 4 g8 + 2 (c & 1), + 1
-                    *reinterpret_cast<float2 *>(my_rows + (nt * 8 + 2 * t4 + i) * DH + 32 * (c >> 1) + 4 * g8 +
-                                                2 * (c & 1)) = make_float2(o[nt][c][i] * unit, o[nt][c][2 + i] * unit);
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            if (none || pos >= lim[nt][j]) s[nt][2 * i + j] = -INFINITY;
+                    // V scales of tokens that no row sees may hold anything
+                    if (none || pos >= kv_end) vs[i] = make_uint2(0, 0);
+                }
+            }
+            bool raise = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    raise |= fmaxf(fmaxf(s[nt][j], s[nt][2 + j]), fmaxf(s[nt][4 + j], s[nt][6 + j])) > lift[nt][j];
+            uint32_t top = __vimax3_u16x2(vs[0].x, vs[0].y, vs[1].x);
+            top = __vimax3_u16x2(__vimax3_u16x2(top, vs[1].y, vs[2].x), vs[2].y, vs[3].x);
+            top = __vimax3_u16x2(top, vs[3].y, 0u);
+            raise |= (top >> 16) > ev_top || (top & 0xffffu) > ev_top;
+            if (__any_sync(0xffffffffu, raise)) {
+                int et = ev;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {     // a NaN (field 255) must not hide the others' range
+                        const int f = static_cast<int>((j < 2 ? vs[i].x : vs[i].y) >> (j & 1 ? 23 : 7)) & 0xff;
+                        et = f < 255 && f > et ? f : et;
+                    }
+                const int en = static_cast<int>(__reduce_max_sync(0xffffffffu, static_cast<unsigned>(et)));
+                const float down = ev - en < -126 ? 0.0f : __uint_as_float(static_cast<uint32_t>(127 + ev - en) << 23);
+                ev = en;
+                norm = __uint_as_float(static_cast<uint32_t>(254 + HEAD - ev) << 23);
+                ev_top = (static_cast<uint32_t>(ev + 1) << 7) - 1u;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        float t = m[nt][j];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) t = fmaxf(t, s[nt][2 * i + j]);
+                        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
+                        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
+                        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
+                        const float tr = t == -INFINITY ? 0.0f : t * rscale[nt][j];
+                        const float a = m[nt][j] == -INFINITY ? 0.0f : fast_exp2(mr[nt][j] - tr);
+                        m[nt][j] = t;
+                        mr[nt][j] = tr;
+                        lift[nt][j] = t + __fdividef(static_cast<float>(SLACK), rscale[nt][j]);
+                        l[nt][j] *= a;
+                        const float ad = a * down;
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) o[nt][c][j] *= ad, o[nt][c][2 + j] *= ad;
+                    }
+            }
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+                float p[NT][4];           // norm times the probabilities
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float e1 = fast_exp2(fmaf(s[nt][4 * hf + i], rscale[nt][i & 1], -mr[nt][i & 1]));
+                        l[nt][i & 1] += e1;
+                        p[nt][i] = e1 * norm;
+                    }
+                const uint2 v0 = hf ? at64<B_V + 1024>(at_v + use) : at64<B_V>(at_v + use);
+                const uint2 v1 = hf ? at64<B_V + 1024>(at_vo + use) : at64<B_V>(at_vo + use);
+                const uint2 v2 = hf ? at64<B_V + 1536>(at_v + use) : at64<B_V + 512>(at_v + use);
+                const uint2 v3 = hf ? at64<B_V + 1536>(at_vo + use) : at64<B_V + 512>(at_vo + use);
+#pragma unroll
+                for (int gr = 0; gr < 4; ++gr) {
+                    const uint32_t x0 = gr < 2 ? vs[2 * hf].x : vs[2 * hf].y, x1 = gr < 2 ? vs[2 * hf + 1].x : vs[2 * hf + 1].y;
+                    const float f0 = gr & 1 ? bf16_hi(x0) : bf16_lo(x0), f1 = gr & 1 ? bf16_hi(x1) : bf16_lo(x1);
+                    const uint32_t sel = gr & 1 ? 0x7632 : 0x5410;
+                    const uint32_t a = gr < 2 ? __byte_perm(v0.x, v1.x, sel) : __byte_perm(v0.y, v1.y, sel);
+                    const uint32_t c = gr < 2 ? __byte_perm(v2.x, v3.x, sel) : __byte_perm(v2.y, v3.y, sel);
+                    const uint32_t a8 = a >> 8, c8 = c >> 8;
+                    const uint32_t a0 = centred_lo(a), a1 = centred_hi(a), a2 = centred_lo(c), a3 = centred_hi(c);
+                    const uint32_t d0 = centred_lo(a8), d1 = centred_hi(a8), d2 = centred_lo(c8), d3 = centred_hi(c8);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        // p s rounded to fp16, then tokens against rows turned into the MMA's order
+                        const uint32_t b0 = transpose8(pack_half2(p[nt][0] * f0, p[nt][1] * f0));
+                        const uint32_t b1 = transpose8(pack_half2(p[nt][2] * f1, p[nt][3] * f1));
+                        mma16(o[nt][2 * gr], a0, a1, a2, a3, b0, b1);
+                        mma16(o[nt][2 * gr + 1], d0, d1, d2, d3, b0, b1);
+                    }
+                }
+            }
+            use = use + BATCH_BYTES == STAGES * BATCH_BYTES ? 0 : use + BATCH_BYTES;
         }
-    }
-    __syncthreads();
 
-    const int d = threadIdx.x;                    // one channel a thread
-    const bool whole = d0 == 0 && d1 == d_units;
-    const float *all_rows = reinterpret_cast<const float *>(s_mem + ATT_WARPS * RING);
-    for (int row = 0; row < done.rows; ++row) {
-        const float *ml = all_rows + R * DH + 2 * row, *src = all_rows + row * DH + d;
-        float mx = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < ATT_WARPS; ++w) mx = fmaxf(mx, ml[w * row_floats(R)]);
-        const float ref = mx == -INFINITY ? 0.0f : mx;
-        float acc = 0.0f, sum = 0.0f;
-#pragma unroll
-        for (int w = 0; w < ATT_WARPS; ++w) {
-            const float a = fast_exp2(ml[w * row_floats(R)] - ref);
-            acc += a * src[w * row_floats(R)];
-            sum += a * ml[w * row_floats(R) + 1];
+        // the share's next part: its first copies run while this part's rows are joined
+        const Item done = it;
+        const int d0 = u0, d1 = u1, d_units = units, d_item = e * prm.H + head;
+        bool more = prm.split && u1 == units && left > 0;
+        if (more) {
+            u0 = -over;
+            if (++head == prm.H) head = 0, ++e;
+            it = Item(prm, e, head, R);
+            units = it.units();
+            more = take();
+            __syncwarp();
+            if (more) start();
         }
-        if (whole) {
-            done.out<T>(prm, row)[d] = from_f32<T>(row_value(done.limit(prm, row), acc, sum));
-        } else {
-            float *dst = prm.part + ((static_cast<long long>(blockIdx.x) * 2 + (d0 > 0 ? 0 : 1)) * R + row) * PART;
-            dst[d] = acc;
-            if (d == 0) dst[DH] = mx, dst[DH + 1] = sum;
+        __syncthreads();              // the rows before these have been read
+
+        // a warp's rows to shared memory: output over norm, maximum, sum
+        {
+            const float unit = ldexpf(1.0f, ev - 127 - HEAD);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float sum = l[nt][i];
+                    sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+                    sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+                    sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+                    if (g8 == 0) {
+                        float *ml = my_rows + R * DH + 2 * (nt * 8 + 2 * t4 + i);
+                        ml[0] = m[nt][i] == -INFINITY ? -INFINITY : mr[nt][i];
+                        ml[1] = sum;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)      // m-tile c: channels 32 (c / 2) + 4 g8 + 2 (c & 1), + 1
+                        *reinterpret_cast<float2 *>(my_rows + (nt * 8 + 2 * t4 + i) * DH + 32 * (c >> 1) + 4 * g8 +
+                                                    2 * (c & 1)) = make_float2(o[nt][c][i] * unit, o[nt][c][2 + i] * unit);
+            }
         }
-    }
-    // the item goes on in the next CTAs: the one where it begins says so
-    if (d1 < d_units && d0 == 0 && threadIdx.x == 0)
-        prm.open[blockIdx.x] = make_int2(d_item, 1 + (d_units - d1 + share - 1) / share);
-    if (!more) return;
+        __syncthreads();
+
+        const int d = threadIdx.x;                    // one channel a thread
+        const bool whole = d0 == 0 && d1 == d_units;
+        const float *all_rows = reinterpret_cast<const float *>(s_mem + ATT_WARPS * RING);
+        for (int row = 0; row < done.rows; ++row) {
+            const float *ml = all_rows + R * DH + 2 * row, *src = all_rows + row * DH + d;
+            float mx = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < ATT_WARPS; ++w) mx = fmaxf(mx, ml[w * row_floats(R)]);
+            const float ref = mx == -INFINITY ? 0.0f : mx;
+            float acc = 0.0f, sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < ATT_WARPS; ++w) {
+                const float a = fast_exp2(ml[w * row_floats(R)] - ref);
+                acc += a * src[w * row_floats(R)];
+                sum += a * ml[w * row_floats(R) + 1];
+            }
+            if (whole) {
+                done.out<T>(prm, row)[d] = from_f32<T>(row_value(done.limit(prm, row), acc, sum));
+            } else {
+                float *dst = prm.part + ((static_cast<long long>(blockIdx.x) * 2 + (d0 > 0 ? 0 : 1)) * R + row) * PART;
+                dst[d] = acc;
+                if (d == 0) dst[DH] = mx, dst[DH + 1] = sum;
+            }
+        }
+        // the item goes on in the next CTAs: the one where it begins says so
+        if (d1 < d_units && d0 == 0 && threadIdx.x == 0)
+            prm.open[blockIdx.x] = make_int2(d_item, 1 + (d_units - d1 + share - 1) / share);
+        if (!more) return;
     }
 }
 

@@ -238,11 +238,13 @@ struct ScaledParams {
     long long timeout_cycles;
 };
 
+// z / (1 + exp(-z)) is formed with t = exp(-|z|) <= 1, so that nothing overflows.
 template <typename T>
 __device__ __forceinline__ float finish(float s, float scale, float bias, int act) {
-    float z = __fmaf_rn(s, scale, bias);
-    if (act) z = sizeof(T) == 4 ? __fdiv_rn(z, 1.0f + expf(-z)) : __fdividef(z, 1.0f + __expf(-z));
-    return z;
+    const float z = __fmaf_rn(s, scale, bias);
+    if (!act) return z;
+    const float t = sizeof(T) == 4 ? expf(-fabsf(z)) : __expf(-fabsf(z)), num = z < 0.0f ? z * t : z;
+    return sizeof(T) == 4 ? __fdiv_rn(num, 1.0f + t) : __fdividef(num, 1.0f + t);
 }
 
 // Few tokens: the weights are read once and the products formed by dp4a.  KT threads share

@@ -346,3 +346,134 @@ def test_decode_steps_end_to_end(ip):
         want = (oq.double() @ wo.double().t()) * s.double()[..., None] * so.double()
         assert (y.double() - want).abs().max() <= want.abs().max() * 2.0 ** -22
     assert ip.status(ws) == 0
+
+
+# ------------------------------------------------------------ larger shapes, on the GPU's own values
+
+def big_check(ip, B, T, H, Hkv, lens, counts, page, dtype, causal, seed, scale=None, max_len=None, heads_off=0):
+    """Attention against float64 torch on the values that kv4_read gives (pinned above), with
+    kv4_ref.attention's bound."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    need = [-(-n // page) for n in lens]
+    total = sum(need) + 2
+    ids = torch.randperm(total, generator=g, device="cuda").int()
+    table = torch.full((B, max(1, max(need))), -7, dtype=torch.int32, device="cuda")
+    at = 0
+    for b, n in enumerate(need):
+        table[b, :n] = ids[at:at + n]
+        at += n
+    cache = ip.kv4_cache(total, Hkv, page)
+    cache.fill_(255)
+    L = max(1, max(lens))
+    zero = torch.zeros(B, dtype=torch.int32, device="cuda")
+    ws = space(ip.kv4_attention_workspace_bytes(B, T, H, Hkv, max(L, max_len or 0)))
+    for b in range(B):      # one sequence at a time bounds the memory
+        if lens[b]:
+            k, v = (torch.randn(1, lens[b], Hkv, 128, generator=g, device="cuda") for _ in range(2))
+            ip.kv4_append(k, v, zero[:1], table[b:b + 1], cache, workspace=ws)
+    q = (1.5 * torch.randn(B, T, H, 128, generator=g, device="cuda")).to(DT[dtype])
+    cnt = None if counts is None else ints(counts)
+    out = ip.kv4_attention(q, ints(lens), table, cache, count=cnt, causal=causal, scale=scale,
+                           max_len=max_len, workspace=ws if max_len else None)
+    assert ip.status(ws) == 0
+    sc = 128 ** -0.5 if scale is None else scale
+    eps = torch.finfo(q.dtype).eps
+    for b in range(B):
+        c = T if counts is None else min(counts[b], T)
+        assert not out[b, c:].any()
+        n = lens[b]
+        if n == 0 or c == 0:
+            assert not out[b].any()
+            continue
+        k, v = ip.kv4_read(cache, zero[:1], table[b:b + 1], n, dtype=torch.float32)
+        k, v = (x[0].double().repeat_interleave(H // Hkv, 1).transpose(0, 1) for x in (k, v))      # [H, n, 128]
+        qq = q[b, :c].double().transpose(0, 1)
+        x = qq @ k.transpose(1, 2) * sc
+        if causal:
+            x = x.masked_fill(torch.arange(n, device="cuda") > n - c + torch.arange(c, device="cuda")[:, None], -np.inf)
+        p = torch.nan_to_num(torch.softmax(x, -1))
+        want = p @ v
+        # 15 s sum |q| <= 15 max(s) sum |q|, s <= max|k| / 7 (1 + 2^-8) in a group
+        A = 15 / 7 * 1.01 * k.abs().amax((1, 2), keepdim=True) * qq.abs().sum(-1, keepdim=True) * sc
+        rel = 2 * 2.0 ** -20 * A + 2.0 ** -11 + 2.0 ** -16 + n * 2.0 ** -28
+        top = v.abs().amax((1, 2), keepdim=True) * 1.01
+        tol = rel * (p @ v.abs()) + n * 2.0 ** -34 * top
+        # a result below the type's normal range rounds by half of smallest_normal eps (2^-25 for f16)
+        tol = tol * (1 + eps) + want.abs() * eps / 2 + torch.finfo(q.dtype).smallest_normal * eps
+        err = (out[b, :c].double().transpose(0, 1) - want).abs()
+        assert (err <= tol).all(), (b, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("case", [
+    dict(B=2, T=1, H=8, Hkv=2, lens=[70001, 333], page=32, causal=True),            # one long, one short
+    dict(B=40, T=1, H=8, Hkv=4, lens=[(37 * i * i) % 900 for i in range(40)], page=16, causal=True),
+    dict(B=1, T=700, H=4, Hkv=2, lens=[1100], page=64, causal=True),                # a long chunk
+    dict(B=2, T=300, H=3, Hkv=3, lens=[300, 37], page=16, causal=False),
+    dict(B=2100, T=1, H=2, Hkv=1, lens=[(i * 7) % 200 for i in range(2100)], page=16, causal=True),   # a CTA an item
+    dict(B=3, T=2, H=96, Hkv=2, lens=[500, 20, 1], page=16, causal=True),           # 48 heads to a cache head
+], ids=["long", "ragged", "chunk", "cross", "items", "groups"])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_attention_at_size(ip, case, dtype):
+    big_check(ip, counts=None, dtype=dtype, seed=len(case["lens"]), **case)
+
+
+def test_attention_seeded_sweep(ip):
+    rng = np.random.default_rng(5)
+    for i in range(40):
+        B, Hkv, G = int(rng.integers(1, 12)), int(rng.choice([1, 2, 3, 8])), int(rng.choice([1, 2, 4, 7]))
+        T = int(rng.choice([1, 1, 2, 5, 17, 40]))
+        top = int(np.exp(rng.uniform(0, np.log(5000))))
+        lens = [int(x) for x in rng.integers(0, top + 1, B)]
+        counts = None if rng.random() < 0.5 else [int(x) for x in rng.integers(0, T + 2, B)]
+        big_check(ip, B, T, G * Hkv, Hkv, lens, counts, int(rng.choice([16, 32, 64])), ["f16", "bf16"][i % 2],
+                  bool(rng.random() < 0.6), seed=i, scale=None if rng.random() < 0.5 else float(rng.uniform(0.01, 0.3)),
+                  max_len=None if rng.random() < 0.5 else top + int(rng.integers(1, 4000)))
+
+
+def test_a_cache_past_31_bits(ip):
+    H, page = 8, 64
+    n_pages = (5 << 30) // (H * 144 * page)
+    cache = torch.empty(n_pages, H, 144 * page, dtype=torch.uint8, device="cuda")
+    small = ip.kv4_cache(4, H, page)
+    far, near = ints([[n_pages - 1, n_pages // 2 + 3, n_pages - 7]]), ints([[2, 0, 3]])
+    k, v = (torch.randn(1, 170, H, 128, device="cuda") for _ in range(2))
+    q = torch.randn(1, 1, H, 128, device="cuda").half()
+    res = []
+    for c, t in ((cache, far), (small, near)):
+        ip.kv4_append(k, v, ints([0]), t, c)
+        res.append((ip.kv4_attention(q, ints([170]), t, c), *ip.kv4_read(c, ints([0]), t, 170)))
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
+
+
+def test_refusals(ip):
+    q = torch.zeros(2, 1, 4, 128, device="cuda").half()
+    k = torch.zeros(2, 3, 2, 128, device="cuda").half()
+    cache, table, i2 = ip.kv4_cache(4, 2, 16), ints([[0], [1]]), ints([0, 1])
+    ok = dict(q=q, lengths=i2, page_table=table, cache=cache)
+    ip.kv4_attention(**ok)
+    for err, over in ((TypeError, dict(q=q.float())), (TypeError, dict(lengths=i2.long())), (TypeError, dict(lengths=None)),
+                      (ValueError, dict(lengths=ints([1]))), (ValueError, dict(count=ints([1]))),
+                      (ValueError, dict(page_table=ints([[0]]))), (TypeError, dict(page_table=table.cpu())),
+                      (ValueError, dict(cache=cache[:, :, :-1])), (TypeError, dict(cache=cache.to(torch.int8))),
+                      (ValueError, dict(q=q[..., ::2])), (ValueError, dict(q=q.transpose(2, 3))),
+                      (ip.IpError, dict(q=torch.zeros(2, 1, 3, 128, device="cuda").half())),
+                      (ip.IpError, dict(scale=-1.0)), (ip.IpError, dict(max_len=-1)),
+                      (ip.IpError, dict(q=torch.zeros(2, 0, 4, 128, device="cuda").half())),
+                      (ip.IpError, dict(q=torch.zeros(2, 2049, 4, 128, device="cuda").half())),
+                      (ip.IpError, dict(cache=torch.zeros(4, 2, 144 * 8, dtype=torch.uint8, device="cuda"))),
+                      (ip.IpError, dict(workspace=torch.zeros(300, dtype=torch.uint8, device="cuda"), max_len=4096))):
+        with pytest.raises(err):
+            ip.kv4_attention(**dict(ok, **over))
+    ok = dict(k=k, v=k, start=i2, page_table=table, cache=cache)
+    ip.kv4_append(**ok)
+    for err, over in ((ValueError, dict(v=k[:, :2])), (TypeError, dict(v=k.float())), (TypeError, dict(start=None)),
+                      (ValueError, dict(k=k[:, :, :1], v=k[:, :, :1])), (TypeError, dict(k=k.int(), v=k.int())),
+                      (ValueError, dict(k=k[..., :64], v=k[..., :64])),
+                      (ValueError, dict(k=k.transpose(2, 3).contiguous().transpose(2, 3)))):
+        with pytest.raises(err):
+            ip.kv4_append(**dict(ok, **over))
+    with pytest.raises(TypeError):
+        ip.kv4_read(cache, i2, table, 2, dtype=torch.float64)
+    with pytest.raises(ValueError):
+        ip.kv4_read(cache, i2, table, -1)

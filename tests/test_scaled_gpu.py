@@ -176,13 +176,11 @@ def test_product_swish(ip, dtype, M, K, N):
     check_product(ip, M, K, N, DT[dtype], swish=True, bias=M != 6)
 
 
-@pytest.mark.parametrize("M,N", [(3, 40), (40, 64), (140, 300), (2600, 2048)])
+@pytest.mark.parametrize("M,N", [(3, 40), (40, 64), (140, 300), (64, 16384), (2600, 2048)])
 @pytest.mark.parametrize("K", [1024, 1040, 2048, 5000])
 def test_sums_are_exact_at_the_extremes(ip, M, N, K):
     # every product has the largest magnitude: the partial sums reach 2^24 in each
     # segment, and the two halves of K cancel up to a few units
-    if M == 2600 and K > 2048:
-        pytest.skip("covered by the smaller shapes")
     ld = -(-K // 16) * 16
     x = torch.full((M, ld), -128, dtype=torch.int8, device="cuda")[:, :K]
     w = torch.full((N, ld), -128, dtype=torch.int8, device="cuda")[:, :K]
@@ -236,3 +234,80 @@ def test_empty(ip):
     assert q.shape == (0, 64) and s.shape == (0,)
     w = torch.zeros(8, 64, dtype=torch.int8, device="cuda")
     assert ip.linear_scaled_i8(q, s, w, torch.ones(8, device="cuda")).shape == (0, 8)
+
+
+@pytest.mark.parametrize("M", [5, 90, 3000])
+def test_rows_without_a_scale_and_far_activations(ip, M):
+    # rows of zeros, rows that were not finite, and a swish far out on both sides, in each form
+    x = torch.randn(M, 640, device="cuda").to(torch.bfloat16)
+    x[1] = 0
+    x[3, 5] = float("inf")
+    w, sw = ip.quantize_rows_i8(torch.randn(1500, 640, device="cuda") * 9)
+    b = torch.linspace(-120, 120, 1500, device="cuda")
+    q, s = ip.quantize_rows_i8(x)
+    for dt in DT.values():
+        y = ip.linear_scaled_i8(q, s, w, sw, b, act=ip.ACT_SWISH, dtype=dt)
+        assert torch.isnan(y[3]).all()
+        keep = [i for i in range(M) if i != 3]
+        err = (y[keep].double() - product_ref(q[keep], s[keep], w, sw, b, True)).abs()
+        # below exp(-87) the exponential itself is a subnormal number: 2^-149 off, times |z|
+        assert (err <= product_bound(q[keep], s[keep], w, sw, b, True, dt) + 2.0 ** -140).all()
+        z = b.double()
+        want = z * torch.sigmoid(z)
+        tol = want.abs() * (2.0 ** -17 + z.abs() * 2.0 ** -21 + torch.finfo(dt).eps / 2) + 2.0 ** -140 + \
+            torch.finfo(dt).smallest_normal * torch.finfo(dt).eps
+        assert ((y[1].double() - want).abs() <= tol).all()
+
+
+def test_offsets_past_31_bits(ip):
+    M, N, K = 36000, 65536, 48
+    x = torch.randint(-127, 128, (M, K), dtype=torch.int8, device="cuda")
+    w = torch.randint(-127, 128, (N, K), dtype=torch.int8, device="cuda")
+    one = lambda n: torch.ones(n, device="cuda")
+    y = ip.linear_scaled_i8(x, one(M), w, one(N), dtype=torch.float16)
+    assert y.numel() > 2 ** 31
+    for r in (slice(0, 3), slice(32760, 32776), slice(M - 3, M)):
+        assert torch.equal(y[r].double(), (x[r].double() @ w.double().t()).half().double())
+    base = torch.zeros(40, 1 << 26, dtype=torch.int8, device="cuda")     # rows 64 MB apart
+    base[:, :K] = x[:40]
+    assert torch.equal(ip.linear_scaled_i8(base[:, :K], one(40), w[:300], one(300), dtype=torch.float32),
+                       ip.linear_scaled_i8(x[:40], one(40), w[:300], one(300), dtype=torch.float32))
+    xf = torch.randn(40, 1 << 26, device="cuda", dtype=torch.float16)
+    q, s = ip.quantize_rows_i8(xf[:, -K:])
+    q2, s2 = ip.quantize_rows_i8(xf[:, -K:].contiguous())
+    assert torch.equal(q, q2) and torch.equal(s, s2)
+
+
+def test_seeded_sweep(ip):
+    rng = np.random.default_rng(77)
+    for i in range(60):
+        M, K, N = (int(round(np.exp(rng.uniform(0, np.log(t))))) for t in (5000, 9000, 6000))
+        if M * K * N > 4e10:
+            K = max(1, int(4e10 / M / N))
+        check_product(ip, M, K, N, list(DT.values())[i % 3], swish=bool(rng.random() < 0.5),
+                      bias=bool(rng.random() < 0.5), seed=i, lo=-128)
+
+
+def test_refusals(ip):
+    x = torch.zeros(4, 64, dtype=torch.int8, device="cuda")
+    w, s4, s8 = torch.zeros(8, 64, dtype=torch.int8, device="cuda"), torch.ones(4, device="cuda"), torch.ones(8, device="cuda")
+    ok = dict(x=x, sx=s4, w=w, sw=s8)
+    ip.linear_scaled_i8(**ok)
+    odd = torch.zeros(4, 65, dtype=torch.int8, device="cuda")
+    for err, over in ((ValueError, dict(sx=s8)), (ValueError, dict(sw=s4)), (TypeError, dict(sx=s4.half())),
+                      (TypeError, dict(x=x.float())), (TypeError, dict(w=w.cpu())), (ValueError, dict(w=w[:, :48])),
+                      (ValueError, dict(bias=s4)), (TypeError, dict(dtype=torch.float64)),
+                      (ip.IpError, dict(x=odd[:, :64])), (ip.IpError, dict(x=odd[:, 1:], w=w)),
+                      (ip.IpError, dict(act=7)), (ValueError, dict(x=x.t())),
+                      (ValueError, dict(x=x[:1].expand(4, 64))),
+                      (ValueError, dict(out=torch.zeros(4, 9, device="cuda"))),
+                      (ValueError, dict(workspace=torch.zeros(512, dtype=torch.uint8, device="cuda")[::2])),
+                      (ip.IpError, dict(workspace=torch.zeros(128, dtype=torch.uint8, device="cuda")))):
+        with pytest.raises(err):
+            ip.linear_scaled_i8(**dict(ok, **over))
+    for err, t in ((TypeError, x), (TypeError, torch.zeros(3, 4)), (ValueError, torch.zeros(4, 6, device="cuda").t()),
+                   (ValueError, torch.zeros(2, 3, 4, device="cuda").transpose(0, 1)),
+                   (ValueError, torch.zeros(3, 0, device="cuda")),
+                   (ip.IpError, torch.zeros(1, 40000, device="cuda"))):
+        with pytest.raises(err):
+            ip.quantize_rows_i8(t)
