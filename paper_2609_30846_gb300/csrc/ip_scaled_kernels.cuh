@@ -707,12 +707,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         constexpr int UNITS = (TILE_M + C::BR) / 8;   // of eight rows
         constexpr int GW = CONV_WARPS / CONV_GROUPS, PER = (UNITS + GW - 1) / GW;
         const int cw = (warp - EPI_WARPS) % GW, grp = (warp - EPI_WARPS) / GW;
-        // A unit is eight rows of half a raw stage.  A lane takes chunk j (16 bytes) of row r8; the
-        // quarter-warps hold rows r and r + 4, whose four chunks of a half fall on different banks
-        // under the swizzle, and write their two fp16 chunks in opposite order for the same reason.
-        const int r8 = (lane >> 3) + (lane & 4), j = lane & 3, odd = (lane >> 2) & 1;
+        // A unit is eight rows of half a raw stage.  A lane takes chunk j (16 bytes) of row r8; a
+        // quarter-warp holds the rows r and r ^ 5: under the swizzle their four chunks of a half fall
+        // on different banks (bit 2), and so do the even (odd) ones of their fp16 chunks (bit 0).
+        const int r8 = (lane >> 3) ^ (lane & 4 ? 5 : 0), j = lane & 3;
         const uint32_t src0 = swz(r8, j), src1 = swz(r8, 4 + j);
-        const uint32_t d0 = swz(r8, 2 * j + odd), d1 = swz(r8, 2 * j + (odd ^ 1));
+        const uint32_t d0 = swz(r8, 2 * j), d1 = swz(r8, 2 * j + 1);
         int rs = 0, rph = 0, fs = 0, fph = 0, turn = 0;
         bool ok = true;
         for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
@@ -741,12 +741,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                         ok = false;
                         break;
                     }
-                    auto one = [&](int u, uint4 v) {
-                        uint32_t h[8];      // the half of the chunk that is written first in front
-                        cvt4(odd ? v.z : v.x, h[0], h[1]);
-                        cvt4(odd ? v.w : v.y, h[2], h[3]);
-                        cvt4(odd ? v.x : v.z, h[4], h[5]);
-                        cvt4(odd ? v.y : v.w, h[6], h[7]);
+                    auto one = [&](int u, const uint4 &v) {
+                        uint32_t h[8];
+                        cvt4(v.x, h[0], h[1]);
+                        cvt4(v.y, h[2], h[3]);
+                        cvt4(v.z, h[4], h[5]);
+                        cvt4(v.w, h[6], h[7]);
                         sts128(dst + u * 1024 + d0, h[0], h[1], h[2], h[3]);
                         sts128(dst + u * 1024 + d1, h[4], h[5], h[6], h[7]);
                     };
