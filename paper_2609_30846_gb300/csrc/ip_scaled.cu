@@ -44,10 +44,6 @@ bool make_map(CUtensorMap *m, const void *base, int K, long long rows, long long
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The output [M][N] in blocks of 32 rows x 64 bytes, swizzled as the kernel's stage16 writes them.
-template <typename T>
-bool make_out_map(CUtensorMap *m, const ips::ScaledParams &prm);
-
 bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 std::mutex g_mu;
@@ -93,22 +89,6 @@ int quantize(const ips::QuantParams &prm, cudaStream_t st) {
     return vec ? quantize<T, true>(prm, st) : quantize<T, false>(prm, st);
 }
 
-template <typename T> constexpr CUtensorMapDataType MAP_TYPE = CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
-template <> constexpr CUtensorMapDataType MAP_TYPE<__half> = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-template <> constexpr CUtensorMapDataType MAP_TYPE<__nv_bfloat16> = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-
-template <typename T>
-bool make_out_map(CUtensorMap *m, const ips::ScaledParams &prm) {
-    EncodeTiledFn fn = encode_fn();
-    if (!fn) return false;
-    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(prm.N), static_cast<cuuint64_t>(prm.M)};
-    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(prm.ldy) * sizeof(T)};
-    const cuuint32_t box[2] = {64 / sizeof(T), 32};
-    const cuuint32_t estride[2] = {1, 1};
-    return fn(m, MAP_TYPE<T>, 2, prm.y, dims, strides, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <typename T, int MT, int CPT, int KT>
 int launch_vec(const ips::ScaledParams &prm, int nsm, cudaStream_t st) {
     constexpr int per = ips::VEC_THREADS / KT * CPT;
@@ -132,8 +112,8 @@ int launch_vec_m(const ips::ScaledParams &prm, int nsm, cudaStream_t st) {
 }
 
 template <typename T, int BN, bool LONG, bool PAIR, bool KSPLIT = false>
-int launch_tc(const CUtensorMap &tx, const CUtensorMap &tw, const CUtensorMap &ty, const ips::ScaledParams &prm,
-              int nsm, cudaStream_t st) {
+int launch_tc(const CUtensorMap &tx, const CUtensorMap &tw, const ips::ScaledParams &prm, int nsm,
+              cudaStream_t st) {
     using C = ips::Tile<BN, PAIR>;
     static bool set[64] = {false};
     int dev = 0;
@@ -168,31 +148,28 @@ int launch_tc(const CUtensorMap &tx, const CUtensorMap &tw, const CUtensorMap &t
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = ctas > 1 ? 2 : 1;
-    return launched(cudaLaunchKernelEx(&cfg, fn, tx, tw, ty, prm));
+    return launched(cudaLaunchKernelEx(&cfg, fn, tx, tw, prm));
 }
 
 template <typename T, int BN, bool PAIR>
 int run_tc(ips::ScaledParams prm, int nsm, cudaStream_t st) {
     using C = ips::Tile<BN, PAIR>;
-    CUtensorMap tx, tw, ty;
+    CUtensorMap tx, tw;
     if (!make_map(&tx, prm.x, prm.K, prm.M, prm.ldx, ips::TILE_M) ||
         !make_map(&tw, prm.w, prm.K, prm.N, prm.ldw, C::BR))
         return IP_ERR_CUDA;
-    prm.out_map = aligned(prm.y, 16) && prm.ldy * sizeof(T) % 16 == 0 && prm.N * sizeof(T) % 16 == 0;
-    ty = tx;       // not used then
-    if (prm.out_map && !make_out_map<T>(&ty, prm)) return IP_ERR_CUDA;
     prm.tiles_n = (prm.N + BN - 1) / BN;
     prm.tiles = (prm.M + ips::TILE_M * C::CTAS - 1) / (ips::TILE_M * C::CTAS) * prm.tiles_n;
     if constexpr (BN == 32) {
         const int raws = (prm.K + ips::RAW_K - 1) / ips::RAW_K;
         if (prm.splits > 1)
             return (raws + prm.splits - 1) / prm.splits * ips::RAW_K > 1024
-                       ? launch_tc<T, BN, true, PAIR, true>(tx, tw, ty, prm, nsm, st)
-                       : launch_tc<T, BN, false, PAIR, true>(tx, tw, ty, prm, nsm, st);
+                       ? launch_tc<T, BN, true, PAIR, true>(tx, tw, prm, nsm, st)
+                       : launch_tc<T, BN, false, PAIR, true>(tx, tw, prm, nsm, st);
     }
     if constexpr (BN <= 128 || PAIR)
-        if (prm.K > ips::SEG * ips::BK) return launch_tc<T, BN, true, PAIR>(tx, tw, ty, prm, nsm, st);
-    return launch_tc<T, BN, false, PAIR>(tx, tw, ty, prm, nsm, st);
+        if (prm.K > ips::SEG * ips::BK) return launch_tc<T, BN, true, PAIR>(tx, tw, prm, nsm, st);
+    return launch_tc<T, BN, false, PAIR>(tx, tw, prm, nsm, st);
 }
 
 // The form that a launch is expected to take the least time in, ns.  Fitted on GB300 to sweeps of
@@ -296,7 +273,6 @@ int ip_linear_scaled_i8(const int8_t *x, long long ldx, const float *sx, const i
     prm.K = K;
     prm.N = N;
     prm.act = act;
-    prm.out_map = 0;
     prm.splits = 1;
     prm.tiles_n = 0;
     prm.tiles = 0;

@@ -230,7 +230,6 @@ struct ScaledParams {
     void *y;
     long long M, ldx, ldw, ldy;
     int K, N, act;
-    int out_map;                    // y has a tensor map
     int splits;                     // CTAs that share a tile's K
     int tiles_n;
     long long tiles;
@@ -238,13 +237,24 @@ struct ScaledParams {
     long long timeout_cycles;
 };
 
-// z / (1 + exp(-z)) is formed with t = exp(-|z|) <= 1, so that nothing overflows.
+// z / (1 + exp(-z)) is formed with t = exp(-|z|) <= 1, so that nothing overflows: z / (1 + t) or
+// z t / (1 + t).  For 16-bit outputs t and the reciprocal of 1 + t, in [1, 2], come from the
+// approximate units (2^-22 and less; the argument's rounding adds |z| 2^-24).
+template <typename T>
+__device__ __forceinline__ float swish(float z) {
+    if (sizeof(T) == 4) {
+        const float t = expf(-fabsf(z));
+        return __fdiv_rn(z < 0.0f ? z * t : z, 1.0f + t);
+    }
+    float t, r;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(t) : "f"(fabsf(z) * -1.44269504f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + t));
+    return (z < 0.0f ? z * t : z) * r;
+}
 template <typename T>
 __device__ __forceinline__ float finish(float s, float scale, float bias, int act) {
     const float z = __fmaf_rn(s, scale, bias);
-    if (!act) return z;
-    const float t = sizeof(T) == 4 ? expf(-fabsf(z)) : __expf(-fabsf(z)), num = z < 0.0f ? z * t : z;
-    return sizeof(T) == 4 ? __fdiv_rn(num, 1.0f + t) : __fdividef(num, 1.0f + t);
+    return act ? swish<T>(z) : z;
 }
 
 // Few tokens: the weights are read once and the products formed by dp4a.  KT threads share
@@ -346,13 +356,12 @@ __global__ void __launch_bounds__(VEC_THREADS) scaled_vec_kernel(const ScaledPar
 // operand byte; 80 % of that pipe with 128 x 256 tiles a CTA, the tensor pipe at 36 %).
 // So the CTAs of a pair share their channels: each converts its 128 tokens and half of
 // the 256 channels for an MMA of 256 x 256 (cta_group::2), a third less for the same
-// products; and the output leaves by TMA stores.
+// products.
 
 constexpr int TILE_M = 128;
 constexpr int RAW_K = 128;          // K bytes of a raw stage: TMA moves rows of 64 bytes at half the rate
 constexpr int BK = 64;              // K elements of an fp16 stage (rows of 128 bytes)
 constexpr int SEG = 1024 / BK;      // stages of an exact segment
-constexpr int OUT_BLOCK = 32 * 64;
 constexpr int TC_THREADS = 640;     // five warpgroups (registers are dealt by warpgroup)
 constexpr int TC_REGS = 96;         // registers a thread at launch
 constexpr int EPI_WARPS = 8, CONV_WARPS = 8, CONV_GROUPS = 4;
@@ -372,9 +381,9 @@ struct Tile {
     static constexpr int BARS = 0;                    // 2 RS + 2 FS + 5 barriers
     static constexpr int TMEM_PTR = 256, DEAD = 260;
     static constexpr int CONSTS = 512;                // per epilogue warp: sw and bias of its columns
-    // per epilogue warp: a block of 32 rows x 64 bytes on its way out
-    static constexpr int OUT_AT = (CONSTS + EPI_WARPS * 2 * 4 * (BN / 2) + 1023) & ~1023;
-    static constexpr int F16_AT = OUT_AT + EPI_WARPS * OUT_BLOCK;
+    // the sums of a tile, where the CTAs of a cluster share its K
+    static constexpr int SUMS_AT = (CONSTS + EPI_WARPS * 2 * 4 * (BN / 2) + 1023) & ~1023;
+    static constexpr int F16_AT = SUMS_AT + (BN == 32 ? 4 * TILE_M * BN : 0);
     static constexpr int RAW_AT = F16_AT + FS * F16;
     static constexpr int SMEM = RAW_AT + RS * RAW + 1024;
     static constexpr int COLS = 2 * BN;               // TMEM columns
@@ -528,44 +537,28 @@ __device__ __forceinline__ void tmem_wait_ld() {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
-// 16 outputs of one token from column n on.
+// 16 outputs of one token from column n on.  `vec`: the row starts on 32 bytes.  Whole sectors
+// straight from the registers: by way of shared memory and TMA stores the epilogue waited
+// for its buffers (12000 x 1024 -> 4096 with swish 115 us, all else left out 104 us).
 template <typename T>
 __device__ __forceinline__ void store16(T *row, int n, int N, bool vec, const float (&z)[16]) {
     if (vec && n + 16 <= N) {
-        constexpr int W = 16 / sizeof(T);
+        constexpr int W = 32 / sizeof(T);
 #pragma unroll
         for (int i = 0; i < 16 / W; ++i) {
-            T v[W];
+            struct alignas(32) Vec { T e[W]; } v;
 #pragma unroll
-            for (int j = 0; j < W; ++j) v[j] = from_f32<T>(z[i * W + j]);
-            *reinterpret_cast<uint4 *>(row + n + i * W) = *reinterpret_cast<const uint4 *>(v);
+            for (int j = 0; j < W; ++j) v.e[j] = from_f32<T>(z[i * W + j]);
+            const uint32_t *w = reinterpret_cast<const uint32_t *>(&v);
+            asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(row + n + i * W), "r"(w[0]), "r"(w[1]),
+                         "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                         : "memory");
         }
     } else {
 #pragma unroll
         for (int j = 0; j < 16; ++j)
             if (n + j < N) row[n + j] = from_f32<T>(z[j]);
     }
-}
-// The same into a block of 32 rows x 64 bytes in shared memory, from its 16-byte chunk c0 on, in
-// the layout of the TMA store (64-byte swizzle: no bank conflicts).
-template <typename T>
-__device__ __forceinline__ void stage16(uint32_t block, int row, int c0, const float (&z)[16]) {
-    constexpr int W = 16 / sizeof(T);
-#pragma unroll
-    for (int i = 0; i < 16 / W; ++i) {
-        T v[W];
-#pragma unroll
-        for (int j = 0; j < W; ++j) v[j] = from_f32<T>(z[i * W + j]);
-        const uint4 w = *reinterpret_cast<const uint4 *>(v);
-        sts128(block + row * 64 + (((c0 + i) ^ ((row >> 1) & 3)) << 4), w.x, w.y, w.z, w.w);
-    }
-}
-__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t src, int c0, int c1) {
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
-                     reinterpret_cast<uint64_t>(map)),
-                 "r"(c0), "r"(c1), "r"(src)
-                 : "memory");
-    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
 
 // LONG: a CTA's K is longer than 1024, several segments per tile.  KSPLIT: the CTAs of a cluster
@@ -574,7 +567,7 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t sr
 template <typename T, int BN, bool LONG, bool PAIR, bool KSPLIT>
 __global__ void __launch_bounds__(TC_THREADS, 1)
     scaled_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w,
-                     const __grid_constant__ CUtensorMap tm_y, const ScaledParams prm) {
+                     const ScaledParams prm) {
     using C = Tile<BN, PAIR>;
     // The sums of a long K take 128 registers of an epilogue thread (BN = 256): its warpgroups
     // take over what the others can spare, 2 x 168 + 2 x 56 + 32 = 5 x 96.
@@ -593,7 +586,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     const uint32_t drained = base + C::BARS + 8u * (2 * C::RS + 2 * C::FS + 4);
     volatile int *dead = reinterpret_cast<volatile int *>(smem + C::DEAD);
     const int rank = PAIR ? static_cast<int>(blockIdx.x & 1u) : 0;      // clusters are (2, 1, 1)
-    static_assert(!KSPLIT || (BN == 32 && !PAIR && 4 * TILE_M * BN == EPI_WARPS * OUT_BLOCK), "sums fit");
+    static_assert(!KSPLIT || (BN == 32 && !PAIR), "room for the sums");
     const int splits = KSPLIT ? prm.splits : 1;                         // else clusters are (splits, 1, 1)
     const int part = KSPLIT ? static_cast<int>(blockIdx.x) % splits : 0;
     const long long worker = blockIdx.x / (KSPLIT ? splits : C::CTAS), workers = gridDim.x / (KSPLIT ? splits : C::CTAS);
@@ -783,12 +776,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         constexpr int CH = CW < 16 ? 1 : CW / 16;
         const int col0 = half * CW;
         const bool vec = ((reinterpret_cast<uintptr_t>(prm.y) | (static_cast<uintptr_t>(prm.ldy) * sizeof(T))) &
-                          15) == 0;
-        // blocks of 64 bytes a row leave by TMA where the output's rows are aligned for it and N ends
-        // on 16 bytes (the last 16 of a row are written whole)
-        constexpr int PER_BLOCK = 4 / static_cast<int>(sizeof(T));      // chunks of 16 columns in one
-        const bool staged = CH % PER_BLOCK == 0 && prm.out_map;
-        const uint32_t block = base + C::OUT_AT + warp * OUT_BLOCK;
+                          31) == 0;
         const uint32_t cst = base + C::CONSTS + warp * (8 * CW);
         int a = 0, aph = 0;
         bool ok = true;
@@ -811,27 +799,15 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                 for (int i = 0; i < 16; i += 4) {
                     const uint4 w4 = lds128(cst + 4 * (c + i));
                     const uint4 b4 = lds128(cst + 4 * (CW + c + i));
-                    z[i] = finish<T>(s[i], sx * __uint_as_float(w4.x), __uint_as_float(b4.x), prm.act);
-                    z[i + 1] = finish<T>(s[i + 1], sx * __uint_as_float(w4.y), __uint_as_float(b4.y), prm.act);
-                    z[i + 2] = finish<T>(s[i + 2], sx * __uint_as_float(w4.z), __uint_as_float(b4.z), prm.act);
-                    z[i + 3] = finish<T>(s[i + 3], sx * __uint_as_float(w4.w), __uint_as_float(b4.w), prm.act);
+                    z[i] = __fmaf_rn(s[i], sx * __uint_as_float(w4.x), __uint_as_float(b4.x));
+                    z[i + 1] = __fmaf_rn(s[i + 1], sx * __uint_as_float(w4.y), __uint_as_float(b4.y));
+                    z[i + 2] = __fmaf_rn(s[i + 2], sx * __uint_as_float(w4.z), __uint_as_float(b4.z));
+                    z[i + 3] = __fmaf_rn(s[i + 3], sx * __uint_as_float(w4.w), __uint_as_float(b4.w));
                 }
-                if (!staged) {
-                    if (m < prm.M) store16<T>(row, n0 + c, prm.N, vec, z);
-                    return;
-                }
-                if (ch % PER_BLOCK == 0) {      // the store before has read the block
-                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                    __syncwarp();
-                }
-                stage16<T>(block, lane, ch % PER_BLOCK * 2, z);
-                if (ch % PER_BLOCK == PER_BLOCK - 1) {
-                    const int cb = c - 16 * (PER_BLOCK - 1);
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0 && mq < prm.M && n0 + cb < prm.N)
-                        tma_store_2d(&tm_y, block, n0 + cb, static_cast<int>(mq));
-                }
+                if (prm.act)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[i] = swish<T>(z[i]);
+                if (m < prm.M) store16<T>(row, n0 + c, prm.N, vec, z);
             };
             int sum[LONG || KSPLIT ? CH : 1][16];
             if (LONG || KSPLIT)
@@ -844,18 +820,20 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t at = tmem + a * BN + col0 + (static_cast<uint32_t>(quarter * 32) << 16);
+                uint32_t r[2][16];      // the next columns are fetched while these are worked on
+                tmem_ld16(at, r[0]);
 #pragma unroll
                 for (int c = 0; c < CH; ++c) {
-                    uint32_t r[16];
-                    tmem_ld16(at + 16 * c, r);
                     tmem_wait_ld();
+                    if (c + 1 < CH) tmem_ld16(at + 16 * (c + 1), r[(c + 1) & 1]);
+                    const uint32_t (&v)[16] = r[c & 1];
                     if (LONG || KSPLIT) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) sum[c][i] += __float2int_rn(__uint_as_float(r[i]));
+                        for (int i = 0; i < 16; ++i) sum[c][i] += __float2int_rn(__uint_as_float(v[i]));
                     } else {
                         float s[16];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = __uint_as_float(r[i]);
+                        for (int i = 0; i < 16; ++i) s[i] = __uint_as_float(v[i]);
                         write(c, s);
                     }
                 }
@@ -868,7 +846,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             if (KSPLIT && ok) {
 #pragma unroll
                 for (int i = 0; i < 16; i += 4)
-                    sts128(base + C::OUT_AT + 4u * ((quarter * 32 + lane) * BN + col0 + i), sum[0][i], sum[0][i + 1],
+                    sts128(base + C::SUMS_AT + 4u * ((quarter * 32 + lane) * BN + col0 + i), sum[0][i], sum[0][i + 1],
                            sum[0][i + 2], sum[0][i + 3]);
             } else if (LONG && ok) {
 #pragma unroll
@@ -880,7 +858,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                 }
             }
         }
-        if (staged && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
     if (KSPLIT) {
@@ -892,7 +869,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             const int r = row0 + e / BN, c = e % BN, n = n0 + c;
             if (m0 + r >= prm.M || n >= prm.N) continue;
             int sum = 0;
-            for (int i = 0; i < splits; ++i) sum += ld_cluster(base + C::OUT_AT + 4u * (r * BN + c), i);
+            for (int i = 0; i < splits; ++i) sum += ld_cluster(base + C::SUMS_AT + 4u * (r * BN + c), i);
             static_cast<T *>(prm.y)[(m0 + r) * prm.ldy + n] =
                 from_f32<T>(finish<T>(static_cast<float>(sum), prm.sx[m0 + r] * prm.sw[n],
                                       prm.bias ? prm.bias[n] : 0.0f, prm.act));
