@@ -30,17 +30,17 @@ EncodeTiledFn encode_fn() {
     return fn;
 }
 
-// int8 rows [rows][K] of `ld` bytes each, boxes of RAW_K x box_rows, elements outside read
+// int8 rows [rows][K] of `ld` bytes each, boxes of BK x box_rows, elements outside read
 // as zero (a K that BK does not divide, the rows behind the last).
 bool make_map(CUtensorMap *m, const void *base, int K, long long rows, long long ld, unsigned box_rows) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(K), static_cast<cuuint64_t>(rows)};
     const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld)};
-    const cuuint32_t box[2] = {ips::RAW_K, box_rows};
+    const cuuint32_t box[2] = {ips::BK, box_rows};
     const cuuint32_t estride[2] = {1, 1};
     return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estride,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -161,9 +161,9 @@ int run_tc(ips::ScaledParams prm, int nsm, cudaStream_t st) {
     prm.tiles_n = (prm.N + BN - 1) / BN;
     prm.tiles = (prm.M + ips::TILE_M * C::CTAS - 1) / (ips::TILE_M * C::CTAS) * prm.tiles_n;
     if constexpr (BN == 32) {
-        const int raws = (prm.K + ips::RAW_K - 1) / ips::RAW_K;
+        const int stages = (prm.K + ips::BK - 1) / ips::BK;
         if (prm.splits > 1)
-            return (raws + prm.splits - 1) / prm.splits * ips::RAW_K > 1024
+            return (stages + prm.splits - 1) / prm.splits > ips::SEG
                        ? launch_tc<T, BN, true, PAIR, true>(tx, tw, prm, nsm, st)
                        : launch_tc<T, BN, false, PAIR, true>(tx, tw, prm, nsm, st);
     }
@@ -176,8 +176,8 @@ int run_tc(ips::ScaledParams prm, int nsm, cudaStream_t st) {
 // M = 12 .. 4096 tokens over N = 512 .. 16384 at K = 1024 and 4096, every form timed at each point:
 // the vector kernel reads the weights once per eight tokens; the tensor-core forms take so
 // long per fp16 stage (64 of K) of a round of tiles over the SMs.  (us, vector / 32 / 128 / pairs:
-// 32 x 1024 -> 1024 4.4 / 7.7 / 10.6 / 15, 64 x 4096 -> 1024 11.4 / 10.4 / 33 / 45,
-// 16 x 4096 -> 16384 33 / 72 / 40 / 50, 1024 x 1024 -> 4096 - / 35 / 17.3 / 15.2.)
+// 32 x 1024 -> 512 3.4 / 6.8 / 8.8 / 12.7, 128 x 4096 -> 512 - / 10.0 / 22.9 / 38,
+// 32 x 4096 -> 16384 60 / 66 / 29 / 43, 2048 x 1024 -> 16384 - / 237 / 89 / 71.)
 enum Form { FORM_VEC, FORM_32, FORM_128, FORM_PAIR };
 struct Choice {
     Form form;
@@ -187,19 +187,19 @@ struct Choice {
 long long rounds(long long tiles, int workers) { return (tiles + workers - 1) / workers; }
 
 Choice choose(const ips::ScaledParams &prm, int nsm) {
-    const long long raws = (prm.K + ips::RAW_K - 1) / ips::RAW_K, stages = 2 * raws;
+    const long long stages = (prm.K + ips::BK - 1) / ips::BK;
     const long long tm = (prm.M + ips::TILE_M - 1) / ips::TILE_M;
     const long long t32 = tm * ((prm.N + 31) / 32), t128 = tm * ((prm.N + 127) / 128);
     const long long pairs = (tm + 1) / 2 * ((prm.N + 255) / 256);
     // few tiles: up to four parts of at least 512 bytes of K that fit the SMs at once (eight: slower,
     // 12 x 4096 -> 512 13.5 us for 10)
     int splits = 1;
-    while (splits < 4 && 2 * splits * t32 <= nsm && raws >= 8 * splits) splits *= 2;
+    while (splits < 4 && 2 * splits * t32 <= nsm && stages >= 16 * splits) splits *= 2;
     Choice best = {FORM_32, splits};
-    long long least = splits > 1 ? 5800 + 270 * (stages / splits) : 3400 + 270 * stages * rounds(t32, nsm);
-    const long long ns128 = 4600 + 375 * stages * rounds(t128, nsm);
+    long long least = splits > 1 ? 5800 + 265 * (stages / splits) : 3400 + 265 * stages * rounds(t32, nsm);
+    const long long ns128 = 3800 + 305 * stages * rounds(t128, nsm);
     if (ns128 < least) best = {FORM_128, 1}, least = ns128;
-    const long long ns_pair = 6000 + 520 * stages * rounds(pairs, nsm / 2);
+    const long long ns_pair = 5700 + 475 * stages * rounds(pairs, nsm / 2);
     if (ns_pair < least) best = {FORM_PAIR, 1}, least = ns_pair;
     const long long blocks = (prm.M + 7) / 8, kv = prm.K > 1024 ? prm.K : 1024;     // a channel's reduction
     if (blocks <= 65535 && 2200 + 29 * (prm.N * kv * blocks) / 100000 < least) best = {FORM_VEC, 1};

@@ -347,9 +347,9 @@ __global__ void __launch_bounds__(VEC_THREADS) scaled_vec_kernel(const ScaledPar
 // magnitude 2^14.  So the K axis runs in segments of 1024, each summed exactly in
 // TMEM, and the segments are added as int32 in registers.
 //
-// Roles of a persistent CTA (one per SM): warp 16 fetches stages of 128 K bytes of
-// both operands by TMA, warps 8-15 convert halves of them to fp16 in the 128-byte
-// swizzled K-major layout of the MMA, one thread of warp 17 issues tcgen05.mma, warps 0-7
+// Roles of a persistent CTA (one per SM): warp 16 fetches raw stages of 64 K bytes of
+// both operands by TMA, warps 8-15 convert them to fp16 in the 128-byte swizzled
+// K-major layout of the MMA, one thread of warp 17 issues tcgen05.mma, warps 0-7
 // drain one of two TMEM accumulators and write the output while the other fills.
 //
 // What bounds it: the shared-memory accesses of the conversion (a read and two writes per
@@ -359,8 +359,7 @@ __global__ void __launch_bounds__(VEC_THREADS) scaled_vec_kernel(const ScaledPar
 // products.
 
 constexpr int TILE_M = 128;
-constexpr int RAW_K = 128;          // K bytes of a raw stage: TMA moves rows of 64 bytes at half the rate
-constexpr int BK = 64;              // K elements of an fp16 stage (rows of 128 bytes)
+constexpr int BK = 64;              // K elements of a stage (rows of 64 bytes raw, of 128 in fp16)
 constexpr int SEG = 1024 / BK;      // stages of an exact segment
 constexpr int TC_THREADS = 640;     // five warpgroups (registers are dealt by warpgroup)
 constexpr int TC_REGS = 96;         // registers a thread at launch
@@ -372,12 +371,13 @@ struct Tile {
     static constexpr int BN = BN_;
     static constexpr int CTAS = PAIR_ ? 2 : 1;
     static constexpr int BR = BN / CTAS;              // channels that a CTA converts
-    static constexpr int RAW = (TILE_M + BR) * RAW_K;
+    static constexpr int RAW = (TILE_M + BR) * BK;
     static constexpr int F16 = (TILE_M + BR) * BK * 2;
-    static constexpr int RS = BN == 32 ? 4 : 2;       // raw stages
+    static constexpr int RS = BN == 32 ? 8 : 5;       // raw stages (as many bytes in two stages of 128: 20 % slower)
     static constexpr int FS = 4;                      // fp16 stages
-    // a group of warps must not wait for the phase after next of a slot: their parities are alike
-    static_assert(CONV_GROUPS <= FS && CONV_GROUPS % 2 == 0 && CONV_GROUPS / 2 <= 2 * RS, "groups");
+    // a group of warps, which sees every CONV_GROUPS-th use of the slots, must not wait for the
+    // phase after next of one: their parities are alike
+    static_assert(CONV_GROUPS <= FS && CONV_GROUPS <= RS, "groups");
     static constexpr int BARS = 0;                    // 2 RS + 2 FS + 5 barriers
     static constexpr int TMEM_PTR = 256, DEAD = 260;
     static constexpr int CONSTS = 512;                // per epilogue warp: sw and bias of its columns
@@ -594,7 +594,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::RS; ++s) {
             mbar_init(raw_full(s), 1);
-            mbar_init(raw_empty(s), 2 * CONV_WARPS / CONV_GROUPS);      // both halves read
+            mbar_init(raw_empty(s), CONV_WARPS / CONV_GROUPS);
         }
         for (int s = 0; s < C::FS; ++s) {
             mbar_init(f16_full(s), CONV_WARPS / CONV_GROUPS * C::CTAS);
@@ -622,10 +622,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     const uint32_t tmem = lds32(base + C::TMEM_PTR);
     pdl_wait();
 
-    // raw stages of this CTA (K behind the end reads as 0), two fp16 stages each
-    const int raws = (prm.K + RAW_K - 1) / RAW_K;
-    const int raw0 = KSPLIT ? raws * part / splits : 0, raw1 = KSPLIT ? raws * (part + 1) / splits : raws;
-    const int stages = 2 * (raw1 - raw0);
+    // stages of this CTA: st0 .. st1 - 1 of all (K behind the end reads as 0)
+    const int all = (prm.K + BK - 1) / BK;
+    const int st0 = KSPLIT ? all * part / splits : 0, st1 = KSPLIT ? all * (part + 1) / splits : all;
+    const int stages = st1 - st0;
     const long long limit = prm.timeout_cycles;
 
     if (warp >= EPI_WARPS + CONV_WARPS) {
@@ -637,14 +637,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
                 const int m0 = static_cast<int>(tile / prm.tiles_n) * (TILE_M * C::CTAS) + rank * TILE_M;
                 const int n0 = static_cast<int>(tile % prm.tiles_n) * BN + rank * C::BR;
-                for (int r = raw0; r < raw1; ++r) {
-                    const int k = r * RAW_K;
+                for (int k = st0 * BK; k < st1 * BK; k += BK) {
                     ok = wait_or_dead<false>(raw_empty(s), ph ^ 1, dead, limit);
                     if (!ok) break;
                     const uint32_t st = base + C::RAW_AT + s * C::RAW;
                     mbar_expect_tx(raw_full(s), C::RAW);
                     tma_load_2d(st, &tm_x, k, m0, raw_full(s));
-                    tma_load_2d(st + TILE_M * RAW_K, &tm_w, k, n0, raw_full(s));
+                    tma_load_2d(st + TILE_M * BK, &tm_w, k, n0, raw_full(s));
                     ++issued;
                     if (++s == C::RS) s = 0, ph ^= 1;
                 }
@@ -700,11 +699,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         constexpr int UNITS = (TILE_M + C::BR) / 8;   // of eight rows
         constexpr int GW = CONV_WARPS / CONV_GROUPS, PER = (UNITS + GW - 1) / GW;
         const int cw = (warp - EPI_WARPS) % GW, grp = (warp - EPI_WARPS) / GW;
-        // A unit is eight rows of half a raw stage.  A lane takes chunk j (16 bytes) of row r8; a
-        // quarter-warp holds the rows r and r ^ 5: under the swizzle their four chunks of a half fall
-        // on different banks (bit 2), and so do the even (odd) ones of their fp16 chunks (bit 0).
-        const int r8 = (lane >> 3) ^ (lane & 4 ? 5 : 0), j = lane & 3;
-        const uint32_t src0 = swz(r8, j), src1 = swz(r8, 4 + j);
+        // A unit is eight rows.  A lane takes 16 bytes of row r8: a quarter-warp reads 128 consecutive
+        // bytes, two rows, whose fp16 chunks of one parity fall on different banks under the swizzle.
+        const int r8 = lane >> 2, j = lane & 3;
         const uint32_t d0 = swz(r8, 2 * j), d1 = swz(r8, 2 * j + 1);
         int rs = 0, rph = 0, fs = 0, fph = 0, turn = 0;
         bool ok = true;
@@ -721,14 +718,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                     // the first loads run while the fp16 slot is waited for; a wait that ran out shows
                     // after both (what was read meanwhile is not used)
                     ok = wait_or_dead<false>(raw_full(rs), rph, dead, limit);
-                    const uint32_t src = base + C::RAW_AT + rs * C::RAW + (it & 1 ? src1 : src0);
+                    const uint32_t src = base + C::RAW_AT + rs * C::RAW + lane * 16;
                     const uint32_t dst = base + C::F16_AT + fs * C::F16;
                     const bool whole = ma == TILE_M / 8 && nb == C::BR / 8 && UNITS % GW == 0;
                     constexpr int AHEAD = PER < 4 ? PER : 4;
                     uint4 v[AHEAD];
                     if (whole)
 #pragma unroll
-                        for (int i = 0; i < AHEAD; ++i) v[i] = lds128(src + (i * GW + cw) * 1024);
+                        for (int i = 0; i < AHEAD; ++i) v[i] = lds128(src + (i * GW + cw) * 512);
                     ok = wait_or_dead<PAIR>(f16_empty(fs), fph ^ 1, dead, limit) && ok;
                     if (!__all_sync(0xffffffffu, ok)) {
                         ok = false;
@@ -747,13 +744,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 #pragma unroll
                         for (int i = 0; i < PER; ++i) {
                             one(i * GW + cw, v[i % AHEAD]);
-                            if (i + AHEAD < PER) v[i % AHEAD] = lds128(src + ((i + AHEAD) * GW + cw) * 1024);
+                            if (i + AHEAD < PER) v[i % AHEAD] = lds128(src + ((i + AHEAD) * GW + cw) * 512);
                         }
                     } else {
 #pragma unroll 2
                         for (int u = cw; u < UNITS; u += GW) {
                             if (u < TILE_M / 8 ? u >= ma : u - TILE_M / 8 >= nb) continue;
-                            one(u, lds128(src + u * 1024));
+                            one(u, lds128(src + u * 512));
                         }
                     }
                     // the fp16 stage to the MMA, the raw stage to the next TMA copy
@@ -764,7 +761,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                         mbar_arrive(raw_empty(rs));
                     }
                 }
-                if ((it & 1) && ++rs == C::RS) rs = 0, rph ^= 1;
+                if (++rs == C::RS) rs = 0, rph ^= 1;
                 if (++fs == C::FS) fs = 0, fph ^= 1;
                 if (++turn == CONV_GROUPS) turn = 0;
             }
