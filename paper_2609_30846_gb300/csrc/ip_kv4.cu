@@ -50,8 +50,13 @@ bool strides_ok(const long long *s) {
     return true;
 }
 
-// How the attention deals its work: one wave of CTAs (as many as fit on 152 SMs) in equal shares, or a CTA per item where there are too many row tiles to
-// sum up.  The plan depends on the call's sizes alone.
+// How the attention deals its work: one wave of CTAs (as many as fit on 152 SMs) in equal
+// shares, or a CTA per item where an item is short, so that the second launch and the search
+// for the share would cost more than they give (us, CTA per item / shares; 1 sequence, 8 heads:
+// 384 tokens 6.4 / 8.3, 768 8.8 / 8.5, 2048 17 / 9.1; 64 sequences: 384 16 / 20, 768 27 / 29,
+// 2048 52 / 49), or where there are too many row tiles to sum up.  The plan depends on the
+// call's sizes alone.
+constexpr int WHOLE_UNITS = 5;
 constexpr long long SMS = 152;
 struct Plan {
     int nt, tiles;
@@ -67,7 +72,7 @@ bool plan_of(int B, int T, int H, int Hkv, int max_len, Plan *p) {
     const long long tiles = static_cast<long long>(B) * p->tiles, items = tiles * Hkv;
     const long long units = max_len < ipv::UNIT ? 1 : (max_len + ipv::UNIT - 1ll) / ipv::UNIT;
     if (items > 0x7fffffffll || items * (units + ipv::OVER) > 0x7fffffffll) return false;
-    p->split = tiles <= ipv::MAX_SCAN && units > 1;
+    p->split = tiles <= ipv::MAX_SCAN && units > WHOLE_UNITS;
     p->ctas = items;
     p->open_bytes = 0;
     p->bytes = 256;
