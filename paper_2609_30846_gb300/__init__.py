@@ -806,13 +806,18 @@ def quantize_rows_i8(x, *, q=None, scale=None, stream=None):
     is a view of them where 16 does not divide the last axis.  Asynchronous on
     `stream` (default: torch's current stream)."""
     t = _Torch
-    if x.__class__ is t.tensor and q is None and scale is None and stream is None:
+    if x.__class__ is t.tensor and q is None and scale is None and stream is None and x.is_contiguous():
         dev, code, shape = x.get_device(), t.codes.get(x.dtype), x.shape
         d = shape[-1] if shape else 0
-        if dev >= 0 and dev == t.current() and code is not None and d and not d & 15 and x.is_contiguous():
-            q = t.empty(shape, dtype=t.i8, device=x.device)
-            scale = t.empty(shape[:-1], dtype=t.f32, device=x.device)
-            rc = _lib.ip_quantize_rows_i8(x.data_ptr(), code, x.numel() // d, d, d, q.data_ptr(), d,
+        if d and code is not None and dev >= 0 and dev == t.current():
+            ld, where, lead = (d + 15) & -16, x.device, shape[:-1]
+            if ld == d:
+                q = whole = t.empty(shape, dtype=t.i8, device=where)
+            else:
+                whole = t.empty((*lead, ld), dtype=t.i8, device=where)
+                q = whole.narrow(-1, 0, d)
+            scale = t.empty(lead, dtype=t.f32, device=where)
+            rc = _lib.ip_quantize_rows_i8(x.data_ptr(), code, x.numel() // d, d, d, whole.data_ptr(), ld,
                                           scale.data_ptr(), t.raw(dev))
             if rc:
                 _check("ip_quantize_rows_i8", rc)
@@ -851,21 +856,25 @@ def linear_scaled_i8(x, sx, w, sw, bias=None, *, act: int = ACT_NONE, dtype=None
     T = t.tensor
     if (x.__class__ is T and w.__class__ is T and sx.__class__ is T and sw.__class__ is T and
             workspace.__class__ is T and out is None and stream is None):
-        dev, xs, ws = x.get_device(), x.shape, w.shape
-        code = t.codes.get(dtype)
-        if (dev >= 0 and dev == t.current() and code is not None and len(ws) == 2 and xs and
-                xs[-1] == ws[1] and x.dtype is t.i8 and w.dtype is t.i8 and sx.dtype is t.f32 and
-                sw.dtype is t.f32 and workspace.dtype is t.u8 and w.get_device() == dev and
-                sx.get_device() == dev and sw.get_device() == dev and workspace.get_device() == dev and
-                sx.shape == xs[:-1] and sw.shape == ws[:1] and x.is_contiguous() and w.is_contiguous() and
-                sx.is_contiguous() and sw.is_contiguous() and workspace.is_contiguous() and
-                (bias is None or bias.__class__ is T and bias.dtype is t.f32 and bias.shape == ws[:1] and
-                 bias.get_device() == dev and bias.is_contiguous())):
+        i8, f32 = t.i8, t.f32
+        dev, code, xs, ws = x.get_device(), t.codes.get(dtype), x.shape, w.shape
+        if (code is not None and dev >= 0 and dev == t.current() and len(ws) == 2 and xs and
+                x.dtype is i8 and w.dtype is i8 and sx.dtype is f32 and sw.dtype is f32 and workspace.dtype is t.u8 and
+                w.get_device() == dev and sx.get_device() == dev and sw.get_device() == dev and
+                workspace.get_device() == dev and sx.is_contiguous() and sw.is_contiguous() and
+                workspace.is_contiguous()):
             N, K = ws
-            if N and K and not K & 15:
-                out = t.empty(xs[:-1] + ws[:1], dtype=dtype, device=x.device)
+            lead = xs[:-1]
+            # row strides of x and w: 0 for what the general form has to look at
+            ldx = K if x.is_contiguous() else x.stride(0) if len(xs) == 2 and x.stride(1) == 1 else 0
+            ldw = K if w.is_contiguous() else w.stride(0) if w.stride(1) == 1 else 0
+            if (K and N and xs[-1] == K and ldx >= K and ldw >= K and not (ldx | ldw) & 15 and sx.shape == lead and
+                    sw.shape == (N,) and
+                    (bias is None or bias.__class__ is T and bias.dtype is f32 and bias.shape == (N,) and
+                     bias.get_device() == dev and bias.is_contiguous())):
+                out = t.empty((*lead, N), dtype=dtype, device=x.device)
                 rc = _lib.ip_linear_scaled_i8(
-                    x.data_ptr(), K, sx.data_ptr(), w.data_ptr(), K, sw.data_ptr(),
+                    x.data_ptr(), ldx, sx.data_ptr(), w.data_ptr(), ldw, sw.data_ptr(),
                     None if bias is None else bias.data_ptr(), act, x.numel() // K, K, N, out.data_ptr(), N,
                     code, workspace.data_ptr(), workspace.numel(), t.raw(dev))
                 if rc:
