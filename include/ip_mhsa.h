@@ -440,7 +440,7 @@ int ip_quantize_rows_i8(const void *x, int dtype, long long rows, int d, long lo
  * ldw multiples of 16 (K itself may be any size; bytes behind column K are not used).
  * sx: device f32 [rows]; sw: device f32 [N]; bias: device f32 [N] or NULL.
  * y: device, dtype IP_F32, IP_F16 or IP_BF16, rows of ldy >= N elements (those behind
- * column N are left as they were).
+ * column N are left as they were), apart from the inputs.
  * rows <= IP_LINEAR_MAX_FRAMES, K in [1, IP_LINEAR_MAX_K], N in [1, IP_LINEAR_MAX_N].
  * workspace as for ip_linear_i8 (256 bytes, its status word reports a timeout by
  * ip_relpos_mhsa_status).  rows == 0 returns IP_OK without touching any pointer.
@@ -494,7 +494,7 @@ int ip_kv4_read(const void *cache, int n_pages, int page, const int32_t *page_ta
                 void *v, int dtype, void *workspace, size_t workspace_bytes, ip_stream_t stream);
 
 /* Bytes of workspace of ip_kv4_attention: the status word and, where it cuts the keys into
- * chunks, their partial rows (which need no zero fill).  Depends on the arguments only.
+ * shares, their partial rows (which need no zero fill).  Depends on the arguments only.
  * 0 if the shape is invalid. */
 size_t ip_kv4_attention_workspace_bytes(int B, int T, int H, int Hkv, int max_len);
 
@@ -504,14 +504,17 @@ size_t ip_kv4_attention_workspace_bytes(int B, int T, int H, int Hkv, int max_le
  * k_strides); out: device, same type, contiguous, 16-byte aligned.  H query heads share Hkv
  * cache heads in groups of H / Hkv.  lengths: device int32 [B], cached tokens (those of
  * this call's queries included, if they are cached); values below 0 count as 0, values above
- * max_len or max_pages page as the smaller of these (and are reported as IP_ERR_PARAM).  count: device int32 [B], query
- * tokens (clamped to [0, T]), or NULL for T.  causal = 1: the queries are the last
+ * max_len or max_pages page as the smaller of these (and are reported as IP_ERR_PARAM).
+ * count: device int32 [B], query tokens (clamped to [0, T]), or NULL for T.  causal = 1: the queries are the last
  * count[b] cached tokens, so query t sees the positions up to lengths[b] - count[b] + t;
  * causal = 0: all of them (cross attention).  A query that sees none, and the rows
- * t >= count[b], are written as 0.  Scores, softmax and sums are in f32; the
- * probabilities times the V scales enter the output product as fp16 (relative 2^-11).
+ * t >= count[b], are written as 0; a token that a query does not see has no effect on its
+ * row, whatever it holds.  Scores, softmax and sums are in f32; the probabilities (1 for the
+ * largest) times the V scales enter the output product as fp16: relative 2^-11, or
+ * absolute 2^-34 of the largest V scale that the query sees, where that is more.
  * max_len: host upper bound of the lengths, in [0, IP_KV4_MAX_LEN]; it sizes the split of
- * the keys, and the result depends on it in the last bits only.
+ * the keys, and the result depends on it, and on the lengths of the call's other sequences,
+ * in the last bits only (equal calls give equal bits).
  * 1 <= T <= IP_MAX_T; scale in (0, 1e30).  Workspace: at least the size above, 256-byte
  * aligned; calls that share one must not overlap on the GPU. */
 int ip_kv4_attention(const void *q, int dtype, const long long *q_strides, const int32_t *lengths,

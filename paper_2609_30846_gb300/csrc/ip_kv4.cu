@@ -71,7 +71,8 @@ bool plan_of(int B, int T, int H, int Hkv, int max_len, Plan *p) {
     p->tiles = static_cast<int>((rows + 8 * p->nt - 1) / (8 * p->nt));
     const long long tiles = static_cast<long long>(B) * p->tiles, items = tiles * Hkv;
     const long long units = max_len < ipv::UNIT ? 1 : (max_len + ipv::UNIT - 1ll) / ipv::UNIT;
-    if (items > 0x7fffffffll || items * (units + ipv::OVER) > 0x7fffffffll) return false;
+    // sums of units stay within 31 bits, rounded up to whole shares too
+    if (items > 0x7fffffffll || items * (units + ipv::OVER) > 0x7ffff000ll) return false;
     p->split = tiles <= ipv::MAX_SCAN && units > WHOLE_UNITS;
     p->ctas = items;
     p->open_bytes = 0;

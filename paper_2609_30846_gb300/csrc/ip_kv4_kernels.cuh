@@ -214,9 +214,9 @@ __global__ void __launch_bounds__(ROW_THREADS) kv4_read_kernel(const RowParams p
 //
 // Softmax: running reference and sum in f32, per warp over its own tokens (32 at a time).
 //
-// Output: p times the V scale, relative to the running largest exponent of the V scales
-// and times 2^HEAD, rounds to fp16 (half a step 2^-11; terms below 2^-23 of the largest fade
-// out gradually): the codes enter exactly as u - 8, and the sums are f32.  The
+// Output: p times the V scale, relative to the running largest exponent of the V scales that
+// the row sees and times 2^HEAD, rounds to fp16 (half a step 2^-11; terms below 2^-23 of the
+// largest fade out gradually): the codes enter exactly as u - 8, and the sums are f32.  The
 // rounding is below that of a bf16 output and no worse than that of an fp16 one.
 //
 // Split: the keys of all items in a row, cut into units of 128, are dealt in equal shares to
@@ -595,9 +595,12 @@ __global__ void __launch_bounds__(ATT_THREADS, NT == 1 ? CTAS_8 : CTAS_16) kv4_a
                 mr[nt][i] = l[nt][i] = 0.0f;
             }
         }
-        int ev = 16;          // running largest exponent field of the V scales
-        float norm = __uint_as_float((254u + HEAD - 16u) << 23);      // 2^(HEAD - (ev - 127))
-        uint32_t ev_top = (17u << 7) - 1u;                            // largest scale of that exponent
+        // 2^(HEAD - (ev - 127)) for ev, the running largest exponent field of the V scales that the
+        // row sees (all rows alike until a batch that some see in part)
+        float norm[NT][2];
+        uint32_t ev_top = (17u << 7) - 1u;            // largest scale of the lane's smallest ev
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) norm[nt][0] = norm[nt][1] = __uint_as_float((254u + HEAD - 16u) << 23);
 
         for (int t0 = t_begin; t0 < t_end; t0 += STEP) {
             asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
@@ -649,6 +652,39 @@ __global__ void __launch_bounds__(ATT_THREADS, NT == 1 ? CTAS_8 : CTAS_16) kv4_a
                     // V scales of tokens that no row sees may hold anything
                     if (none || pos >= kv_end) vs[i] = make_uint2(0, 0);
                 }
+                // a scale that is no number times a probability of 0 would reach the rows that do not see
+                // it: it goes straight to the sums of those that do
+                uint32_t hit[NT][2] = {};      // a bit per group
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int gr = 0; gr < 4; ++gr) {
+                        uint32_t &w = gr < 2 ? vs[i].x : vs[i].y;
+                        if (((w >> (gr & 1 ? 23 : 7)) & 0xffu) != 255u) continue;
+                        w &= gr & 1 ? 0xffffu : 0xffff0000u;
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j)
+                                if (s[nt][2 * i + j] != -INFINITY) hit[nt][j] |= 1u << gr;
+                    }
+                uint32_t any = 0;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) any |= hit[nt][0] | hit[nt][1];
+                if (__any_sync(0xffffffffu, any != 0)) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            uint32_t x = hit[nt][j];
+                            x |= __shfl_xor_sync(0xffffffffu, x, 4);
+                            x |= __shfl_xor_sync(0xffffffffu, x, 8);
+                            x |= __shfl_xor_sync(0xffffffffu, x, 16);
+#pragma unroll
+                            for (int c = 0; c < 8; ++c)
+                                if ((x >> (c >> 1)) & 1u) o[nt][c][j] = o[nt][c][2 + j] = __uint_as_float(0x7fc00000u);
+                        }
+                }
             }
             bool raise = false;
 #pragma unroll
@@ -661,19 +697,17 @@ __global__ void __launch_bounds__(ATT_THREADS, NT == 1 ? CTAS_8 : CTAS_16) kv4_a
             top = __vimax3_u16x2(top, vs[3].y, 0u);
             raise |= (top >> 16) > ev_top || (top & 0xffffu) > ev_top;
             if (__any_sync(0xffffffffu, raise)) {
-                int et = ev;
+                int field[4];       // of the largest scale of each token
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < 4; ++i) {
+                    field[i] = 0;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {     // a NaN (field 255) must not hide the others' range
                         const int f = static_cast<int>((j < 2 ? vs[i].x : vs[i].y) >> (j & 1 ? 23 : 7)) & 0xff;
-                        et = f < 255 && f > et ? f : et;
+                        field[i] = f < 255 && f > field[i] ? f : field[i];
                     }
-                const int en = static_cast<int>(__reduce_max_sync(0xffffffffu, static_cast<unsigned>(et)));
-                const float down = ev - en < -126 ? 0.0f : __uint_as_float(static_cast<uint32_t>(127 + ev - en) << 23);
-                ev = en;
-                norm = __uint_as_float(static_cast<uint32_t>(254 + HEAD - ev) << 23);
-                ev_top = (static_cast<uint32_t>(ev + 1) << 7) - 1u;
+                }
+                ev_top = 0xffffu;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -690,7 +724,16 @@ __global__ void __launch_bounds__(ATT_THREADS, NT == 1 ? CTAS_8 : CTAS_16) kv4_a
                         mr[nt][j] = tr;
                         lift[nt][j] = t + __fdividef(static_cast<float>(SLACK), rscale[nt][j]);
                         l[nt][j] *= a;
-                        const float ad = a * down;
+                        const int ev = 254 + HEAD - static_cast<int>(__float_as_uint(norm[nt][j]) >> 23);
+                        int en = ev;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) en = s[nt][2 * i + j] != -INFINITY ? max(en, field[i]) : en;
+                        en = max(en, __shfl_xor_sync(0xffffffffu, en, 4));
+                        en = max(en, __shfl_xor_sync(0xffffffffu, en, 8));
+                        en = max(en, __shfl_xor_sync(0xffffffffu, en, 16));
+                        norm[nt][j] = __uint_as_float(static_cast<uint32_t>(254 + HEAD - en) << 23);
+                        ev_top = min(ev_top, (static_cast<uint32_t>(en + 1) << 7) - 1u);
+                        const float ad = ev - en < -126 ? 0.0f : a * __uint_as_float(static_cast<uint32_t>(127 + ev - en) << 23);
 #pragma unroll
                         for (int c = 0; c < 8; ++c) o[nt][c][j] *= ad, o[nt][c][2 + j] *= ad;
                     }
@@ -704,7 +747,7 @@ __global__ void __launch_bounds__(ATT_THREADS, NT == 1 ? CTAS_8 : CTAS_16) kv4_a
                     for (int i = 0; i < 4; ++i) {
                         const float e1 = fast_exp2(fmaf(s[nt][4 * hf + i], rscale[nt][i & 1], -mr[nt][i & 1]));
                         l[nt][i & 1] += e1;
-                        p[nt][i] = e1 * norm;
+                        p[nt][i] = e1 * norm[nt][i & 1];
                     }
                 const uint2 v0 = hf ? at64<B_V + 1024>(at_v + use) : at64<B_V>(at_v + use);
                 const uint2 v1 = hf ? at64<B_V + 1024>(at_vo + use) : at64<B_V>(at_vo + use);
@@ -750,7 +793,6 @@ __global__ void __launch_bounds__(ATT_THREADS, NT == 1 ? CTAS_8 : CTAS_16) kv4_a
 
         // a warp's rows to shared memory: output over norm, maximum, sum
         {
-            const float unit = ldexpf(1.0f, ev - 127 - HEAD);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -766,11 +808,14 @@ __global__ void __launch_bounds__(ATT_THREADS, NT == 1 ? CTAS_8 : CTAS_16) kv4_a
                     }
                 }
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < 2; ++i) {
+                    // 1 / norm
+                    const float unit = ldexpf(1.0f, 127 - static_cast<int>(__float_as_uint(norm[nt][i]) >> 23));
 #pragma unroll
                     for (int c = 0; c < 8; ++c)      // m-tile c: channels 32 (c / 2) + 4 g8 + 2 (c & 1), + 1
                         *reinterpret_cast<float2 *>(my_rows + (nt * 8 + 2 * t4 + i) * DH + 32 * (c >> 1) + 4 * g8 +
                                                     2 * (c & 1)) = make_float2(o[nt][c][i] * unit, o[nt][c][2 + i] * unit);
+                }
             }
         }
         __syncthreads();

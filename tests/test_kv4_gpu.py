@@ -266,6 +266,32 @@ def test_the_other_groups_keep_their_values_beside_a_nan(ip):
     assert torch.equal(a[..., keep], b[..., keep]) and torch.isnan(b[..., 64:96]).all()
 
 
+@pytest.mark.parametrize("what", ["nan", "inf", "huge"])
+@pytest.mark.parametrize("T,H,page", [(4, 2, 16), (7, 1, 32), (40, 2, 64)])
+def test_what_a_query_does_not_see_does_not_reach_it(ip, what, T, H, page):
+    # causal queries before the tokens that hold a NaN, infinities or values 2^60 times the others':
+    # the definition's output, as if the later tokens were not there
+    n, bad = 90 + T, T // 2          # the queries at 90 + bad and later see them
+    q, ks, vs, _, _ = make(1, T, H, 1, [n], page, "bf16", seed=T)
+    val = {"nan": float("nan"), "inf": float("-inf"), "huge": 2.0 ** 60}[what]
+    for x in (ks, vs) if what != "huge" else (vs,):
+        x[0][90 + bad:, 0, 70::9] = val
+    cache = ip.kv4_cache(-(-n // page), 1, page)
+    table = ints([list(range(-(-n // page)))[::-1]])
+    k, v = (torch.from_numpy(x[0][None]).float().cuda() for x in (ks, vs))
+    ip.kv4_append(k, v, ints([0]), table, cache)
+    got = ip.kv4_attention(q, ints([n]), table, cache, max_len=n)
+    m = 90 + bad
+    cut = [[f64(x)[0, :m]] for x in (k, v)]
+    check(ip, got[:, :bad], q[:, :bad], *cut, [bad], True)
+    if what != "huge":
+        assert torch.isnan(got[:, bad:]).all()
+        only_v = ip.kv4_cache(-(-n // page), 1, page)
+        ip.kv4_append(torch.nan_to_num(k, 1.0, 1.0, -1.0), v, ints([0]), table, only_v)
+        got = torch.isnan(ip.kv4_attention(q, ints([n]), table, only_v, max_len=n))
+        assert got[:, bad:, :, 64:].all() and not got[:, bad:, :, :64].any() and not got[:, :bad].any()
+
+
 def test_missing_pages_and_long_lengths_are_reported(ip):
     q, ks, vs, cache, table = make(2, 1, 2, 2, [100, 40], 16, "f16", seed=9)
     bad = table.clone()
