@@ -433,7 +433,7 @@ int ip_quantize_rows_i8(const void *x, int dtype, long long rows, int d, long lo
 #define IP_ACT_SWISH 1
 
 /* y[m][n] = act(sx[m] sw[n] sum_k x[m][k] w[n][k] + bias[n]) for m < rows, n < N: the
- * sum is exact (int32), the rest is in f32, rounded once to y's type.  act:
+ * sum is exact (int32), the rest is in f32 (sx[m] sw[n] first), rounded once to y's type.  act:
  * IP_ACT_NONE, or IP_ACT_SWISH for z / (1 + exp(-z)).
  * x: device int8, rows of ldx >= K bytes; w: device int8 [N], rows of ldw >= K bytes
  * (one per output channel; any values, -128 included); x, w 16-byte aligned, ldx and

@@ -693,8 +693,8 @@ def dwconv_swish_i8(x, w, bias, m, s, sw16: tuple[int, int, int, int], *, out=No
 # 1024 x 4096 product), so each call has a short form for its usual arguments (plain
 # tensors, contiguous or matrices, the current device and stream), which makes the same
 # checks in place, and leaves everything else and every error to the general form.
-# (On a Grace core: quantize_rows_i8 9.5 -> 7, linear_scaled_i8 16 -> 9, kv4_attention
-# 15 -> 9 us a call.)
+# (On a Grace core: quantize_rows_i8 10.5 -> 9, linear_scaled_i8 16 -> 11, kv4_attention
+# 21 -> 13, kv4_append 11 -> 8 us a call.)
 
 class _Torch:
     """torch's names that the short forms use, resolved once."""

@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(ROW_THREADS) kv4_read_kernel(const RowParams p
 // query rows as its 8 columns: with 8 rows the MMA's half-empty other form would cost
 // as much as the codes' conversion.
 //
-// What bounds it (64 sequences of 4096 tokens, 8 heads, one row each): 73 us for 302 MB, 4.15
+// What bounds it (64 sequences of 4096 tokens, 8 heads, one row each): 74 us for 302 MB, 4.1
 // TB/s; the copies alone take 53 us, copies and scores 55 us.  An instruction that turns
 // codes into fragments works on two codes a lane, which makes some 340 instructions for 16
 // tokens (171 on the integer pipe, which would take 85 cycles at full rate) where the bytes
@@ -535,7 +535,7 @@ __global__ void __launch_bounds__(ATT_THREADS, NT == 1 ? CTAS_8 : CTAS_16) kv4_a
             for (int gr = 0; gr < 4; ++gr) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[gr][i] = 0.0f;
-                if (live) load8(src + 32 * gr + 8 * t4, vec, 8, x[gr]);
+                if (live) load8(src + 32 * gr + 8 * t4, vec, x[gr]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[gr][i]));
             }

@@ -19,11 +19,10 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(flo
     return __float2bfloat16_rn(x);
 }
 
-// The first n (at most eight) consecutive elements as floats, the others as 0; `vec`: p is
-// 16-byte aligned.
+// Eight consecutive elements; `vec`: p is 16-byte aligned.
 template <typename T>
-__device__ __forceinline__ void load8(const T *p, bool vec, int n, float (&v)[8]) {
-    if (vec && n >= 8) {
+__device__ __forceinline__ void load8(const T *p, bool vec, float (&v)[8]) {
+    if (vec) {
         constexpr int W = 16 / sizeof(T);
 #pragma unroll
         for (int i = 0; i < 8 / W; ++i) {
@@ -34,7 +33,7 @@ __device__ __forceinline__ void load8(const T *p, bool vec, int n, float (&v)[8]
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f32(p[i]) : 0.0f;
+        for (int i = 0; i < 8; ++i) v[i] = to_f32(p[i]);
     }
 }
 
@@ -59,20 +58,6 @@ __device__ __forceinline__ void store4(T *p, const float (&v)[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) w.e[i] = from_f32<T>(v[i]);
     *reinterpret_cast<Vec *>(p) = w;
-}
-
-// Read-only data that is used once.
-__device__ __forceinline__ uint4 ldg_stream128(const void *p) {
-    uint4 v;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                 : "l"(p));
-    return v;
-}
-__device__ __forceinline__ uint2 ldg_stream64(const void *p) {
-    uint2 v;
-    asm volatile("ld.global.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
-    return v;
 }
 
 }  // namespace ipr
