@@ -8,6 +8,8 @@
 #include <cuda_fp16.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "ip_ptx.cuh"
 #include "ip_real.cuh"
 
@@ -25,11 +27,13 @@ using namespace ipr;
 //   16-bit x: two integers of eleven bits at most, so what is not equal is 2^-12 off and
 //     safe.  Equality needs 2n + 1 = 127, x = amax / 2 (common: one element a row of 1024
 //     bf16 values; the reciprocal rounded up takes it to the even 64), or an amax whose
-//     significand 127 divides: those rows look at every element.
-//   f32 x: units of eight elements with one near a half integer are looked at.
-//   Looking: within 2^-14 of a half integer the exact sign of 254 |x| - (2n + 1) amax
-//     decides: both products as unevaluated sums of two floats, whose leading parts differ
-//     by little there (an exact subtraction) and whose errors have eight bits.
+//     significand 127 divides.  In bf16 that is 254 alone, where 127 / amax is a power of
+//     two and all quotients are exact; fp16 rows with such an amax (8 of 1024) look at
+//     every element: by the quotient of 127 x, which is exact at a half integer.
+//   f32 x: units of eight elements with one near a half integer are looked at: within
+//     2^-14 of one the exact sign of 254 |x| - (2n + 1) amax decides, both products as
+//     unevaluated sums of two floats, whose leading parts differ by little there (an exact
+//     subtraction) and whose errors have eight bits.
 // An amax near the ends of the range is first brought to [1, 4) by a power of two, its
 // row with it, so that nothing of this overflows or underflows.  amax = 0: scale and q
 // are 0.  A NaN or an infinity in the row: the scale is NaN and q is 0, so that a product
@@ -110,7 +114,12 @@ __device__ __noinline__ uint2 quant_look(Raw8<T> raw, float f, float inv, float 
     uint32_t k[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const float x = raw.at(j) * f, y = x * inv, r = __fsub_rn(__fmaf_rn(x, inv, 12582912.0f), 12582912.0f);
+        const float x = raw.at(j) * f;
+        if constexpr (sizeof(T) == 2) {
+            k[j] = static_cast<uint32_t>(__float2int_rn(__fdiv_rn(127.0f * x, top)));
+            continue;
+        }
+        const float y = x * inv, r = __fsub_rn(__fmaf_rn(x, inv, 12582912.0f), 12582912.0f);
         int q = __float2int_rn(r);
         if (fabsf(__fmaf_rn(x, inv, -r)) > 0.5f - 0x1p-14f) {
             const float n = rintf(fabsf(y) - 0.5f), ax = fabsf(x), odd = 2.0f * n + 1.0f;
@@ -132,6 +141,7 @@ __device__ __noinline__ uint2 quant_look(Raw8<T> raw, float f, float inv, float 
 template <typename T, int TPR, bool VEC>
 __global__ void __launch_bounds__(QUANT_THREADS) quantize_rows_kernel(const QuantParams prm) {
     constexpr int RPC = QUANT_THREADS / TPR, UNITS = QUANT_UNITS;
+    constexpr bool BF16 = std::is_same<T, __nv_bfloat16>::value;
     __shared__ float red[QUANT_THREADS / 32];
     pdl_launch_dependents();
     pdl_wait();
@@ -178,7 +188,7 @@ __global__ void __launch_bounds__(QUANT_THREADS) quantize_rows_kernel(const Quan
         const float f = far ? __uint_as_float(static_cast<unsigned>(fe) << 23) : 1.0f;
         const float ntop = amax * f, inv = zero ? 0.0f : __fdiv_ru(127.0f, ntop);
         // rows near the ends of the range go the same way
-        const bool look = !zero && (far || (sizeof(T) == 2 && ((bits & 0x7fffffu) | 0x800000u) % 127u == 0));
+        const bool look = !zero && (far || (sizeof(T) == 2 && !BF16 && ((bits & 0x7fffffu) | 0x800000u) % 127u == 0));
         int8_t *q = prm.q + row * prm.ldq;
         auto put = [&](int c, const Raw8<T> &raw) {
             uint2 b = make_uint2(0u, 0u);
