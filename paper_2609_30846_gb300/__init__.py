@@ -82,7 +82,7 @@ def build(force: bool = False) -> str:
 
 def load(build_if_missing: bool = True) -> ctypes.CDLL:
     """Load libipmhsa.so and declare the C signatures."""
-    global _lib
+    global _lib, _short
     with _lock:
         if _lib is not None:
             return _lib
@@ -193,7 +193,10 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         lib.ip_probe_int8_mma.restype = ctypes.c_longlong
         lib.ip_probe_int8_mix.argtypes = [I, I, I, P, P]
         lib.ip_probe_int8_mix.restype = ctypes.c_longlong
-        _Torch.bind()
+        try:
+            _short = _bind_short(lib)
+        except Exception as exc:  # noqa: BLE001 - reported with context
+            raise LibraryError(f"cannot load the short forms: {exc}") from exc
         _lib = lib
         return lib
 
@@ -689,29 +692,38 @@ def dwconv_swish_i8(x, w, bias, m, s, sw16: tuple[int, int, int, int], *, out=No
 
 # ------------------------------------------------------- run-time scales
 #
-# A decoder's single-token calls are shorter on the GPU than in Python (1.8 us for a
-# 1024 x 4096 product), so each call has a short form for its usual arguments (plain
-# tensors, contiguous or matrices, the current device and stream), which makes the same
-# checks in place, and leaves everything else and every error to the general form.
-# (On a Grace core: quantize_rows_i8 10.5 -> 9, linear_scaled_i8 16 -> 11, kv4_attention
-# 21 -> 13, kv4_append 11 -> 8 us a call.)
+# A decoder's single-token calls are shorter on the GPU than in Python (2 us for a 1024 x 4096
+# product), so a call with its usual arguments first goes to its short form in ip_torch.cpp,
+# which makes the same checks natively; everything else and every error is left to the forms here.
+# (On a Grace core, us a call over ctypes / natively: quantize_rows_i8 15 / 4.4, linear_scaled_i8
+# 19 / 3.7, kv4_append 15 / 2.1, kv4_attention 21 / 3.5, kv4_read 21 / 4.7.)
 
-class _Torch:
-    """torch's names that the short forms use, resolved once."""
-    tensor = None
+class _Unbound:
+    """Stands for the short forms until the library is loaded."""
 
-    @classmethod
-    def bind(cls):
-        try:
-            import torch
-        except ImportError:      # the C entry points need no torch
-            return
-        cls.empty, cls.zeros = torch.empty, torch.zeros
-        cls.i8, cls.u8, cls.i32, cls.f32 = torch.int8, torch.uint8, torch.int32, torch.float32
-        cls.f16, cls.bf16 = torch.float16, torch.bfloat16
-        cls.codes = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
-        cls.current, cls.raw = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
-        cls.tensor = torch.Tensor
+    @staticmethod
+    def quantize_rows(*args):
+        return None
+
+    linear_scaled = kv4_append = kv4_read = kv4_attention = quantize_rows
+
+
+_short = _Unbound
+
+
+def _bind_short(lib):
+    """The short forms, bound to the library; none without torch (the C entry points need none)."""
+    path = _build.torch_extension()
+    if path is None:
+        return _Unbound
+    import importlib.util
+    import torch  # noqa: F401 - its libraries have to be there
+    spec = importlib.util.spec_from_file_location("ip_torch", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    mod.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        lib.ip_quantize_rows_i8, lib.ip_linear_scaled_i8, lib.ip_kv4_append, lib.ip_kv4_read, lib.ip_kv4_attention)))
+    return mod
 
 
 def _dtype_code(dtype, name="dtype"):
@@ -805,23 +817,10 @@ def quantize_rows_i8(x, *, q=None, scale=None, stream=None):
     new q has rows of a multiple of 16 bytes, as linear_scaled_i8 reads them, so it
     is a view of them where 16 does not divide the last axis.  Asynchronous on
     `stream` (default: torch's current stream)."""
-    t = _Torch
-    if x.__class__ is t.tensor and q is None and scale is None and stream is None and x.is_contiguous():
-        dev, code, shape = x.get_device(), t.codes.get(x.dtype), x.shape
-        d = shape[-1] if shape else 0
-        if d and code is not None and dev >= 0 and dev == t.current():
-            ld, where, lead = (d + 15) & -16, x.device, shape[:-1]
-            if ld == d:
-                q = whole = t.empty(shape, dtype=t.i8, device=where)
-            else:
-                whole = t.empty((*lead, ld), dtype=t.i8, device=where)
-                q = whole.narrow(-1, 0, d)
-            scale = t.empty(lead, dtype=t.f32, device=where)
-            rc = _lib.ip_quantize_rows_i8(x.data_ptr(), code, x.numel() // d, d, d, whole.data_ptr(), ld,
-                                          scale.data_ptr(), t.raw(dev))
-            if rc:
-                _check("ip_quantize_rows_i8", rc)
-            return q, scale
+    if stream is None:
+        r = _short.quantize_rows(x, q, scale)
+        if r is not None:
+            return r if r.__class__ is tuple else _check("ip_quantize_rows_i8", r)
     import torch
     code = _dtype_code(_need(x, "x").dtype, "x")
     rows, d, ldx = _as_rows(x, "x")
@@ -852,34 +851,10 @@ def linear_scaled_i8(x, sx, w, sw, bias=None, *, act: int = ACT_NONE, dtype=None
     K and N may be any size; the rows of x and w start on multiples of 16 bytes.
     Returns out: [..., N] of `dtype` (bfloat16 unless out gives it).  Asynchronous on
     `stream` (default: torch's current stream)."""
-    t = _Torch
-    T = t.tensor
-    if (x.__class__ is T and w.__class__ is T and sx.__class__ is T and sw.__class__ is T and
-            workspace.__class__ is T and out is None and stream is None):
-        i8, f32 = t.i8, t.f32
-        dev, code, xs, ws = x.get_device(), t.codes.get(dtype), x.shape, w.shape
-        if (code is not None and dev >= 0 and dev == t.current() and len(ws) == 2 and xs and
-                x.dtype is i8 and w.dtype is i8 and sx.dtype is f32 and sw.dtype is f32 and workspace.dtype is t.u8 and
-                w.get_device() == dev and sx.get_device() == dev and sw.get_device() == dev and
-                workspace.get_device() == dev and sx.is_contiguous() and sw.is_contiguous() and
-                workspace.is_contiguous()):
-            N, K = ws
-            lead = xs[:-1]
-            # row strides of x and w: 0 for what the general form has to look at
-            ldx = K if x.is_contiguous() else x.stride(0) if len(xs) == 2 and x.stride(1) == 1 else 0
-            ldw = K if w.is_contiguous() else w.stride(0) if w.stride(1) == 1 else 0
-            if (K and N and xs[-1] == K and ldx >= K and ldw >= K and not (ldx | ldw) & 15 and sx.shape == lead and
-                    sw.shape == (N,) and
-                    (bias is None or bias.__class__ is T and bias.dtype is f32 and bias.shape == (N,) and
-                     bias.get_device() == dev and bias.is_contiguous())):
-                out = t.empty((*lead, N), dtype=dtype, device=x.device)
-                rc = _lib.ip_linear_scaled_i8(
-                    x.data_ptr(), ldx, sx.data_ptr(), w.data_ptr(), ldw, sw.data_ptr(),
-                    None if bias is None else bias.data_ptr(), act, x.numel() // K, K, N, out.data_ptr(), N,
-                    code, workspace.data_ptr(), workspace.numel(), t.raw(dev))
-                if rc:
-                    _check("ip_linear_scaled_i8", rc)
-                return out
+    if stream is None:
+        r = _short.linear_scaled(x, sx, w, sw, bias, act, dtype, out, workspace)
+        if r is not None:
+            return r if r.__class__ is not int else _check("ip_linear_scaled_i8", r)
     import torch
     rows, K, ldx = _as_rows(_need(x, "x", torch.int8), "x")
     if _need(w, "w", torch.int8, None, x.device).dim() != 2 or w.shape[1] != K:
@@ -932,24 +907,6 @@ def _strides(t, name):
 _Stride3 = ctypes.c_longlong * 3
 
 
-def _kv4_plain(dev, B, cache, table, workspace, first, second):
-    """Whether a cache call's arguments are plain contiguous tensors of device dev, the current
-    one, with the types and shapes that they must have (second may be None)."""
-    t = _Torch
-    T, i32 = t.tensor, t.i32
-    if not (cache.__class__ is T and table.__class__ is T and workspace.__class__ is T and first.__class__ is T and
-            dev >= 0 and dev == t.current() and cache.dtype is t.u8 and workspace.dtype is t.u8 and
-            table.dtype is i32 and first.dtype is i32 and cache.get_device() == dev and
-            table.get_device() == dev and workspace.get_device() == dev and first.get_device() == dev and
-            cache.is_contiguous() and table.is_contiguous() and workspace.is_contiguous() and
-            first.is_contiguous()):
-        return False
-    cs, ts, fs = cache.shape, table.shape, first.shape
-    return (len(cs) == 3 and not cs[2] % 144 and len(ts) == 2 and ts[0] == B and len(fs) == 1 and fs[0] == B and
-            (second is None or second.__class__ is T and second.dtype is i32 and second.get_device() == dev and
-             second.shape == fs and second.is_contiguous()))
-
-
 def _kv4_args(x, cache, table, workspace, lens, names):
     """Checks what the calls on a cache share: x [B, T, H, 128] (or B, for a call without
     one), the cache, its table and the int32 [B] tensors lens; returns B, the cache's
@@ -979,21 +936,10 @@ def kv4_append(k, v, start, page_table, cache, *, count=None, workspace=None, st
     page_table[b] (int32 [B, pages]).  No two rows may meet in one place.  All CUDA
     tensors; asynchronous on `stream`.  Pages or positions that do not exist are
     skipped and reported by status(workspace)."""
-    t = _Torch
-    if stream is None and k.__class__ is t.tensor and v.__class__ is t.tensor:
-        ks, dev, code = k.shape, k.get_device(), t.codes.get(k.dtype)
-        if (len(ks) == 4 and ks[3] == IP_DH and code is not None and v.shape == ks and v.dtype is k.dtype and
-                v.get_device() == dev and _kv4_plain(dev, ks[0], cache, page_table, workspace, start, count)):
-            cs, kst, vst = cache.shape, k.stride(), v.stride()
-            if cs[1] == ks[2] and kst[3] == 1 and vst[3] == 1:
-                rc = _lib.ip_kv4_append(
-                    k.data_ptr(), v.data_ptr(), code, _Stride3(*kst[:3]), _Stride3(*vst[:3]), start.data_ptr(),
-                    None if count is None else count.data_ptr(), ks[0], ks[1], ks[2], IP_DH, page_table.data_ptr(),
-                    page_table.shape[1], cache.data_ptr(), cs[0], cs[2] // 144, workspace.data_ptr(),
-                    workspace.numel(), t.raw(dev))
-                if rc:
-                    _check("ip_kv4_append", rc)
-                return cache
+    if stream is None:
+        rc = _short.kv4_append(k, v, start, page_table, cache, count, workspace)
+        if rc is not None:
+            return _check("ip_kv4_append", rc) if rc else cache
     code = _dtype_code(_need(k, "k").dtype, "k")
     if k.dim() != 4 or k.shape[3] != IP_DH:
         raise ValueError(f"k must have shape (B, T, H, 128), got {tuple(k.shape)}")
@@ -1020,22 +966,10 @@ def kv4_read(cache, start, page_table, T: int, *, count=None, dtype=None, out=No
     """Positions start[b] .. start[b] + T - 1 of every sequence back as real values:
     (k, v), each [B, T, H, 128] of `dtype` (bfloat16 unless out gives it), zeros in rows
     t >= count[b].  out: such a pair, contiguous.  Arguments as kv4_append."""
-    t = _Torch
-    if stream is None and out is None and cache.__class__ is t.tensor and page_table.__class__ is t.tensor:
-        code, dev = t.codes.get(dtype), cache.get_device()
-        B = page_table.shape[0] if page_table.dim() == 2 else -1
-        if code is not None and T.__class__ is int and T >= 0 and _kv4_plain(dev, B, cache, page_table, workspace,
-                                                                            start, count):
-            cs, where = cache.shape, cache.device
-            shape = (B, T, cs[1], IP_DH)
-            k, v = t.empty(shape, dtype=dtype, device=where), t.empty(shape, dtype=dtype, device=where)
-            rc = _lib.ip_kv4_read(cache.data_ptr(), cs[0], cs[2] // 144, page_table.data_ptr(),
-                                  page_table.shape[1], start.data_ptr(), None if count is None else count.data_ptr(),
-                                  B, T, cs[1], IP_DH, k.data_ptr(), v.data_ptr(), code, workspace.data_ptr(),
-                                  workspace.numel(), t.raw(dev))
-            if rc:
-                _check("ip_kv4_read", rc)
-            return k, v
+    if out is None and stream is None:
+        r = _short.kv4_read(cache, start, page_table, T, count, dtype, workspace)
+        if r is not None:
+            return r if r.__class__ is tuple else _check("ip_kv4_read", r)
     import torch
     B, (n_pages, H, page, width), (pst, pct) = _kv4_args(
         _need(start, "start").numel(), cache, page_table, workspace, (start, count), ("", "start", "count"))
@@ -1075,24 +1009,10 @@ def kv4_attention(q, lengths, page_table, cache, *, count=None, causal: bool = T
     the table can hold); a close one splits the work better.  Returns [B, T, H, 128] of
     q's type.  workspace: a zero-filled uint8 tensor of kv4_attention_workspace_bytes(B, T,
     H, Hkv, max_len).  Asynchronous on `stream`."""
-    t = _Torch
-    if stream is None and out is None and q.__class__ is t.tensor:
-        qs, dev, code = q.shape, q.get_device(), t.codes.get(q.dtype)
-        if (len(qs) == 4 and qs[3] == IP_DH and code and
-                _kv4_plain(dev, qs[0], cache, page_table, workspace, lengths, count)):
-            st, cs, width = q.stride(), cache.shape, page_table.shape[1]
-            if st[3] == 1:
-                out = t.empty(qs, dtype=q.dtype, device=q.device)
-                rc = _lib.ip_kv4_attention(
-                    q.data_ptr(), code, _Stride3(*st[:3]), lengths.data_ptr(),
-                    None if count is None else count.data_ptr(), 1 if causal else 0,
-                    IP_DH ** -0.5 if scale is None else scale, qs[0], qs[1], qs[2], cs[1], IP_DH,
-                    width * (cs[2] // 144) if max_len is None else max_len, page_table.data_ptr(), width,
-                    cache.data_ptr(), cs[0], cs[2] // 144, out.data_ptr(), workspace.data_ptr(),
-                    workspace.numel(), t.raw(dev))
-                if rc:
-                    _check("ip_kv4_attention", rc)
-                return out
+    if stream is None:
+        r = _short.kv4_attention(q, lengths, page_table, cache, count, causal, scale, max_len, out, workspace)
+        if r is not None:
+            return r if r.__class__ is not int else _check("ip_kv4_attention", r)
     import torch
     code = _dtype_code(_need(q, "q").dtype, "q")
     if code == 0:

@@ -1,13 +1,17 @@
 """Builds the GPU library ``libipmhsa.so`` in-tree with nvcc for sm_103a.
 
 The library is the whole product path: the C ABI of include/ip_mhsa.h and
-the CUDA kernels behind it.  Nothing here needs a GPU; nvcc cross-compiles.
+the CUDA kernels behind it.  Beside it, where torch is installed, the host compiler
+builds ``ip_torch.so``, the native short forms of some Python calls.  Nothing here needs a
+GPU; nvcc cross-compiles.
 """
 from __future__ import annotations
 
+import importlib.util
 import os
 import shutil
 import subprocess
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -22,6 +26,8 @@ DEPS = SOURCES + [os.path.join(CSRC, f) for f in ("ip_mhsa_kernels.cuh", "ip_lin
                                                   "ip_ptx.cuh",
                                                   "ip_probe.cuh", "ip_host_util.h")] + [
     os.path.join(INCLUDE, "ip_mhsa.h")]
+TORCH_LIB = os.path.join(PKG, "ip_torch.so")
+TORCH_SOURCE = os.path.join(CSRC, "ip_torch.cpp")
 ARCH = "-gencode=arch=compute_103a,code=sm_103a"
 
 
@@ -43,24 +49,53 @@ def link_command(objs: list[str], out: str) -> list[str]:
     return [nvcc(), ARCH, "-shared", "-o", out] + objs
 
 
-def up_to_date() -> bool:
-    if not os.path.exists(LIB):
+def _torch_dir():
+    """Folder of a torch built with CUDA, None without one."""
+    spec = importlib.util.find_spec("torch")
+    path = os.path.dirname(spec.origin) if spec is not None and spec.origin else None
+    return path if path and os.path.exists(os.path.join(path, "lib", "libc10_cuda.so")) else None
+
+
+def torch_command(out: str) -> list[str]:
+    torch = _torch_dir()
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc())))
+    dirs = [INCLUDE, os.path.join(torch, "include"), os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
+    libs = os.path.join(torch, "lib")
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-o", out, TORCH_SOURCE] + [
+        "-I" + d for d in dirs] + ["-L" + libs, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+
+
+def torch_extension():
+    """Path of ip_torch.so, None without a torch for it."""
+    return TORCH_LIB if _torch_dir() is not None else None
+
+
+def _fresh(lib: str, deps: list[str]) -> bool:
+    if not os.path.exists(lib):
         return False
-    t = os.path.getmtime(LIB)
-    return all(os.path.getmtime(d) <= t for d in DEPS)
+    t = os.path.getmtime(lib)
+    return all(os.path.getmtime(d) <= t for d in deps)
+
+
+def up_to_date() -> bool:
+    return _fresh(LIB, DEPS) and (_torch_dir() is None or
+                                  _fresh(TORCH_LIB, [TORCH_SOURCE, os.path.join(INCLUDE, "ip_mhsa.h")]))
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile (if stale) and return the path of libipmhsa.so."""
+    """Compile (if stale) both libraries and return the path of libipmhsa.so."""
     if not force and up_to_date():
         return LIB
     tag = f".tmp{os.getpid()}"
     objs = [os.path.join(CSRC, os.path.basename(s) + tag + ".o") for s in SOURCES]
+    tmp_torch = TORCH_LIB + tag
+    cmds = [compile_command(src, obj) for src, obj in zip(SOURCES, objs)]
+    if _torch_dir() is not None:
+        cmds.append(torch_command(tmp_torch))
     try:
         # the translation units compile in parallel, then one link
         procs = []
-        for src, obj in zip(SOURCES, objs):
-            cmd = compile_command(src, obj)
+        for cmd in cmds:
             if verbose:
                 print(" ".join(cmd), flush=True)
             procs.append((cmd, subprocess.Popen(cmd, cwd=CSRC)))
@@ -70,8 +105,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
         tmp = LIB + tag
         subprocess.run(link_command(objs, tmp), check=True, cwd=CSRC)
         os.replace(tmp, LIB)
+        if os.path.exists(tmp_torch):
+            os.replace(tmp_torch, TORCH_LIB)
     finally:
-        for obj in objs:
+        for obj in objs + [tmp_torch]:
             if os.path.exists(obj):
                 os.unlink(obj)
     return LIB
