@@ -40,16 +40,6 @@ struct Pages {
     int max_pages, n_pages, shift, heads;    // page size 1 << shift
 };
 
-// Block of the page of position pos, nullptr (and the status word) if the table has none.
-__device__ __forceinline__ uint8_t *page_block(const Pages &p, int b, int pos, int h, int *err) {
-    const int pid = p.table[static_cast<long long>(b) * p.max_pages + (pos >> p.shift)];
-    if (pid < 0 || pid >= p.n_pages) {
-        atomicOr(err, ERR_PARAM);
-        return nullptr;
-    }
-    return p.cache + ((static_cast<long long>(pid) * p.heads + h) * ROW_BYTES << p.shift);
-}
-
 // ---- rows into pages and back -------------------------------------------
 
 struct RowParams {
@@ -62,131 +52,197 @@ struct RowParams {
     int *err;
 };
 
-constexpr int ROW_THREADS = 256;             // a warp per token and head
+// A row (token and head) is a warp's: half of it for K, half for V, eight channels to a lane, so
+// that a group of 32 is four lanes'.  Bound by the instructions of the conversion and the latency
+// of the page table, so a warp takes two rows where there are many: 6000 tokens of 8 heads,
+// 16 bits, 31 MB: append 13.5 us, read back 11 us (one row a warp: 15.1 and 12.2).
+constexpr int ROW_THREADS = 256;
 
-// The bf16 value nearest to amax / 7, ties to even.  The f32 quotient decides unless it
-// falls on the middle of two bf16 values: seven times that middle (twelve bits) is exact.
+// The bf16 value nearest to amax / 7, ties to even (its bits).  The approximate quotient gives the
+// value below, or a neighbour of it where it lies next to one; the middle of the next interval
+// decides: seven times that (twelve bits) is exact.
 __device__ __forceinline__ uint32_t scale4(float amax) {
-    const float q = __fdiv_rn(amax, 7.0f);
-    const uint32_t bits = __float_as_uint(q), lo = bits >> 16, rem = bits & 0xffffu;
-    if (rem != 0x8000u) return lo + (rem > 0x8000u ? 1u : 0u);
-    const float t = 7.0f * q;
-    return lo + (amax > t ? 1u : (amax < t ? 0u : (lo & 1u)));
+    const uint32_t lo = __float_as_uint(amax * (1.0f / 7.0f)) >> 16;
+    const float t = 7.0f * __uint_as_float(lo << 16 | 0x8000u);
+    return lo + (amax > t || (amax == t && (lo & 1u)) ? 1u : 0u);
 }
 
-// Nibble of x for the scale s > 0: the integer nearest to x / s, ties to even, within
-// -7 .. 7, plus 8.  Near a half integer |x| is compared with (n + 1/2) s, twelve bits and exact.
-__device__ __forceinline__ uint32_t code4(float x, float s, float inv) {
-    const float ax = fabsf(x), y = ax * inv;
-    int n = __float2int_rn(fminf(y, 8.0f));
-    const float f = rintf(y - 0.5f);
-    if (fabsf(y - 0.5f - f) < 0x1p-12f) {
-        const float t = (f + 0.5f) * s;
-        const int ni = static_cast<int>(f);
-        n = ax > t ? ni + 1 : (ax < t ? ni : ni + (ni & 1));
-    }
-    n = min(n, 7);
-    return static_cast<uint32_t>(8 + (x < 0.0f ? -n : n));
-}
-
-// One row of a warp: lane l holds channels 4 l .. 4 l + 3 of group l / 8; returns its four
-// nibbles and the group's scale (bf16 bits).
-__device__ __forceinline__ uint32_t quant4(const float (&x)[4], uint32_t &scale) {
+// Eight channels of a group, which the lanes l ^ 1, l ^ 2 and l ^ 3 hold the rest of: their
+// nibbles, the integer n nearest to x / s, ties to even, within -7 .. 7, plus 8, and the group's
+// scale s (bf16 bits).
+//   16-bit x: the quotient by an approximate reciprocal, once corrected by its residue (the
+//     Newton step of Markstein's division): exact at a half integer, where the residue of the
+//     first quotient is exact too, and within 2^-20 elsewhere, where a half integer is 2^-13
+//     away at least.
+//   f32 x: n by the reciprocal, right but next to a half integer.  x - n s is exact (n s has
+//     twelve bits, and the difference is about half of s at most), so comparing it with s / 2
+//     shows what is left to do.
+template <typename T>
+__device__ __forceinline__ uint32_t quant8(const Raw8<T> &raw, uint32_t &scale) {
+    constexpr bool WIDE = sizeof(T) == 4;
+    constexpr float ROUND = 12582912.0f;      // 1.5 2^23, bits 0x4b400000
     uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    raw.largest(top);
+    top = Raw8<T>::value(top);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
     if (top >= 0x7f800000u) {      // a NaN or an infinity: the group reads back as NaN
         scale = 0x7fc0u;
-        return 0x8888u;
+        return 0x88888888u;
     }
     scale = scale4(__uint_as_float(top));
-    if (scale == 0) return 0x8888u;
-    // a tiny scale and its row brought up by 2^100, exactly
-    const float up = scale < (27u << 7) ? 0x1p100f : 1.0f;
-    const float s = __uint_as_float(scale << 16) * up, inv = __fdiv_rn(1.0f, s);
-    uint32_t w = 0;
+    if (scale == 0) return 0x88888888u;
+    // a scale near the ends of the range and its row brought inside by 2^+-100; exactly but for
+    // elements that are 0 either way
+    const bool tiny = scale < (27u << 7), far = tiny || scale > (250u << 7);
+    float x[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w |= code4(x[i] * up, s, inv) << (4 * i);
-    return w;
+    for (int i = 0; i < 8; ++i) x[i] = raw.at(i);
+    if (far)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= tiny ? 0x1p100f : 0x1p-100f;
+    const float s = __uint_as_float(scale << 16) * (far ? (tiny ? 0x1p100f : 0x1p-100f) : 1.0f), half = 0.5f * s;
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+    uint32_t k[8];      // the bits of ROUND + n
+    float e[8], most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (WIDE) {
+            const float r = __fmaf_rn(x[i], inv, ROUND);
+            k[i] = __float_as_uint(r);
+            e[i] = __fmaf_rn(__fsub_rn(ROUND, r), s, x[i]);
+            most = fmaxf(most, fabsf(e[i]));
+        } else {
+            const float y = x[i] * inv;
+            k[i] = __float_as_uint(__fadd_rn(__fmaf_rn(__fmaf_rn(-y, s, x[i]), inv, y), ROUND));
+        }
+    }
+    if (WIDE && most >= half) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (fabsf(e[i]) > half || (fabsf(e[i]) == half && (k[i] & 1u))) k[i] += e[i] > 0.0f ? 1u : ~0u;
+    }
+    if (scale < 0x80u)      // subnormal: it may be far below amax / 7
+#pragma unroll
+        for (int i = 0; i < 8; ++i) k[i] = min(max(k[i], 0x4b400000u - 7u), 0x4b400000u + 7u);
+    uint32_t w = 0;      // sum of (n + 8) 16^i, modulo 2^32
+#pragma unroll
+    for (int i = 7; i >= 0; --i) w = 16u * w + k[i];
+    return w + (0x88888888u - 0x11111111u * 0x4b400000u);
 }
 
-// The row of one warp of the launch; false if the warp has none.
-__device__ __forceinline__ bool row_of(const RowParams &p, int &b, int &t, int &h) {
-    const long long r = static_cast<long long>(blockIdx.x) * (ROW_THREADS / 32) + (threadIdx.x >> 5);
-    if (r >= static_cast<long long>(p.B) * p.T * p.H) return false;
-    const unsigned bt = static_cast<unsigned>(r / p.H);
-    h = static_cast<int>(r - static_cast<long long>(bt) * p.H);
-    b = static_cast<int>(bt / static_cast<unsigned>(p.T));
-    t = static_cast<int>(bt - static_cast<unsigned>(b) * p.T);
-    return true;
-}
+// A warp's rows r, r + 1, ... of sequence b (grid: rows of a sequence, sequences).
+struct Rows {
+    int b, t, h, left;        // the next row, the rows from it to the sequence's last
+    int n;                    // tokens that are no padding
+    long long start;
 
-// Page block of the warp's position, nullptr if the token is padding or has no place.
-__device__ __forceinline__ uint8_t *row_block(const RowParams &p, int b, int t, int h, int &off) {
-    const int n = p.count ? p.count[b] : p.T;
-    if (t >= n) return nullptr;
-    const long long pos = static_cast<long long>(p.start[b]) + t;
-    if (pos < 0 || pos >= static_cast<long long>(p.pages.max_pages) << p.pages.shift) {
+    template <int R>
+    static __device__ __forceinline__ Rows of(const RowParams &p) {
+        Rows w;
+        const unsigned r = (blockIdx.x * (ROW_THREADS / 32) + (threadIdx.x >> 5)) * R;
+        w.b = static_cast<int>(blockIdx.y);
+        w.t = static_cast<int>(r / static_cast<unsigned>(p.H));
+        w.h = static_cast<int>(r - static_cast<unsigned>(w.t) * p.H);
+        w.left = static_cast<int>(static_cast<unsigned>(p.T) * p.H - r);
+        w.n = p.count ? p.count[w.b] : p.T;
+        w.start = p.start[w.b];
+        return w;
+    }
+    __device__ __forceinline__ void next(const RowParams &p) {
+        --left;
+        if (++h == p.H) h = 0, ++t;
+    }
+    // Page block of the row's position, nullptr if the token is padding or (status word) has no place.
+    __device__ __forceinline__ uint8_t *block(const RowParams &p, int &off) const {
+        if (t >= n) return nullptr;
+        const long long pos = start + t;
+        const int page = static_cast<int>(pos >> p.pages.shift);
+        if (pos >= 0 && pos < static_cast<long long>(p.pages.max_pages) << p.pages.shift) {
+            const int pid = p.pages.table[static_cast<long long>(b) * p.pages.max_pages + page];
+            off = static_cast<int>(pos) & ((1 << p.pages.shift) - 1);
+            if (pid >= 0 && pid < p.pages.n_pages)
+                return p.pages.cache + ((static_cast<long long>(pid) * p.pages.heads + h) * ROW_BYTES << p.pages.shift);
+        }
         atomicOr(p.err, ERR_PARAM);
         return nullptr;
     }
-    off = static_cast<int>(pos) & ((1 << p.pages.shift) - 1);
-    return page_block(p.pages, b, static_cast<int>(pos), h, p.err);
-}
+};
 
-template <typename T>
+template <typename T, int R>
 __global__ void __launch_bounds__(ROW_THREADS) kv4_append_kernel(const RowParams prm) {
     pdl_launch_dependents();
     pdl_wait();
-    int b, t, h, off;
-    if (!row_of(prm, b, t, h)) return;
-    const int lane = threadIdx.x & 31;
-    uint8_t *blk = row_block(prm, b, t, h, off);
-    if (!blk) return;
-    const int page = 1 << prm.pages.shift, g = lane >> 3, r = (lane & 7) * 4;
+    const int kv = (threadIdx.x >> 4) & 1, l = threadIdx.x & 15, g = l >> 2, j = l & 3;
+    const int page = 1 << prm.pages.shift;
+    const long long s0 = kv ? prm.vs[0] : prm.ks[0], s1 = kv ? prm.vs[1] : prm.ks[1], s2 = kv ? prm.vs[2] : prm.ks[2];
+    Rows row = Rows::of<R>(prm);
+    const T *base = static_cast<const T *>(kv ? prm.v : prm.k) + row.b * s0 + 8 * l;
+    Raw8<T> x[R];
+    uint8_t *blk[R];
+    int off[R];
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-        const long long *st = kv ? prm.vs : prm.ks;
-        const T *src = static_cast<const T *>(kv ? prm.v : prm.k) + b * st[0] + t * st[1] + h * st[2];
-        float x[4];
-        load4(src + 4 * lane, x);
+    for (int i = 0; i < R; ++i) {
+        blk[i] = nullptr;
+        if (row.left <= 0) continue;
+        const T *src = base + row.t * s1 + row.h * s2;
+        if ((reinterpret_cast<uintptr_t>(src) & 15) == 0) x[i].template load<true>(src, 8);      // beside the reads of the table
+        else x[i].template load<false>(src, 8);
+        blk[i] = row.block(prm, off[i]);
+        row.next(prm);
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        if (!blk[i]) continue;
         uint32_t scale;
-        const uint32_t w = quant4(x, scale);
-        uint8_t *codes = blk + (kv ? v_codes(page) : 0) + off * 64;
-        const int byte = kv ? 8 * (r >> 2) + 2 * g : 16 * (r >> 3) + 4 * g + ((r & 7) >> 1);
-        *reinterpret_cast<uint16_t *>(codes + byte) = static_cast<uint16_t>(w);
-        if ((lane & 7) == 0)
-            reinterpret_cast<uint16_t *>(blk + (kv ? v_scales(page) : k_scales(page)))[off * 4 + g] =
+        const uint32_t w = quant8(x[i], scale);
+        uint8_t *codes = blk[i] + (kv ? v_codes(page) : 0) + off[i] * 64 + 16 * j;
+        if (kv) {
+            *reinterpret_cast<uint16_t *>(codes + 2 * g) = static_cast<uint16_t>(w);
+            *reinterpret_cast<uint16_t *>(codes + 8 + 2 * g) = static_cast<uint16_t>(w >> 16);
+        } else {
+            *reinterpret_cast<uint32_t *>(codes + 4 * g) = w;
+        }
+        if (j == 0)
+            reinterpret_cast<uint16_t *>(blk[i] + (kv ? v_scales(page) : k_scales(page)))[off[i] * 4 + g] =
                 static_cast<uint16_t>(scale);
     }
 }
 
-template <typename T>
+template <typename T, int R>
 __global__ void __launch_bounds__(ROW_THREADS) kv4_read_kernel(const RowParams prm) {
     pdl_launch_dependents();
     pdl_wait();
-    int b, t, h, off = 0;
-    if (!row_of(prm, b, t, h)) return;
-    const int lane = threadIdx.x & 31;
-    const uint8_t *blk = row_block(prm, b, t, h, off);
-    const int page = 1 << prm.pages.shift, g = lane >> 3, r = (lane & 7) * 4;
-    const long long at = ((static_cast<long long>(b) * prm.T + t) * prm.H + h) * DH + 4 * lane;
+    const int kv = (threadIdx.x >> 4) & 1, l = threadIdx.x & 15, g = l >> 2, j = l & 3;
+    const int page = 1 << prm.pages.shift;
+    const Rows first = Rows::of<R>(prm);
+    Rows row = first;
+    uint32_t w[R], s[R];
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-        float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (blk) {
-            const uint8_t *codes = blk + (kv ? v_codes(page) : 0) + off * 64;
-            const int byte = kv ? 8 * (r >> 2) + 2 * g : 16 * (r >> 3) + 4 * g + ((r & 7) >> 1);
-            const uint32_t w = *reinterpret_cast<const uint16_t *>(codes + byte);
-            const uint32_t s = reinterpret_cast<const uint16_t *>(
-                blk + (kv ? v_scales(page) : k_scales(page)))[off * 4 + g];
+    for (int i = 0; i < R; ++i) {
+        int off = 0;
+        w[i] = s[i] = 0;
+        const uint8_t *blk = row.left > 0 ? row.block(prm, off) : nullptr;
+        row.next(prm);
+        if (!blk) continue;
+        const uint8_t *codes = blk + (kv ? v_codes(page) : 0) + off * 64 + 16 * j;
+        w[i] = kv ? *reinterpret_cast<const uint16_t *>(codes + 2 * g) |
+                        static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(codes + 8 + 2 * g)) << 16
+                  : *reinterpret_cast<const uint32_t *>(codes + 4 * g);
+        s[i] = reinterpret_cast<const uint16_t *>(blk + (kv ? v_scales(page) : k_scales(page)))[off * 4 + g];
+    }
+    T *out = static_cast<T *>(kv ? prm.vo : prm.ko) +
+             ((static_cast<long long>(first.b) * prm.T + first.t) * prm.H + first.h) * DH + 8 * l;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                x[i] = static_cast<float>(static_cast<int>((w >> (4 * i)) & 15u) - 8) * __uint_as_float(s << 16);
-        }
-        store4(static_cast<T *>(kv ? prm.vo : prm.ko) + at, x);
+    for (int i = 0; i < R; ++i) {
+        if (i >= first.left) break;
+        float x[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c)      // 2^23 + u is the f32 number of these bits; a scale of 0 gives 0
+            x[c] = __fsub_rn(__uint_as_float(0x4b000000u | ((w[i] >> (4 * c)) & 15u)), 8388616.0f) *
+                   __uint_as_float(s[i] << 16);
+        store8(out + i * DH, x);      // rows follow one another
     }
 }
 

@@ -54,52 +54,6 @@ struct QuantParams {
     float *scale;
 };
 
-// Eight elements as they lie in memory.
-template <typename T>
-struct Raw8 {
-    static constexpr int WORDS = 2 * sizeof(T);
-    uint32_t w[WORDS];
-
-    template <bool VEC>
-    __device__ __forceinline__ void load(const T *p, int n) {      // the first n, the others 0
-        if (VEC) {
-#pragma unroll
-            for (int i = 0; i < WORDS; i += 4) {
-                const uint4 v = *reinterpret_cast<const uint4 *>(reinterpret_cast<const uint32_t *>(p) + i);
-                w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
-            }
-        } else {
-            zero();
-            for (int i = 0; i < n && i < 8; ++i) {
-                if constexpr (sizeof(T) == 4) w[i] = reinterpret_cast<const uint32_t *>(p)[i];
-                else w[i >> 1] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t *>(p)[i]) << (16 * (i & 1));
-            }
-        }
-    }
-    __device__ __forceinline__ void zero() {
-#pragma unroll
-        for (int i = 0; i < WORDS; ++i) w[i] = 0;
-    }
-    // largest magnitude so far, as the bits of T (two halves for the 16-bit types): magnitudes
-    // order as integers, a NaN above an infinity above every number
-    __device__ __forceinline__ void largest(uint32_t &top) const {
-#pragma unroll
-        for (int i = 0; i < WORDS; ++i)
-            top = sizeof(T) == 4 ? max(top, w[i] & 0x7fffffffu) : __vmaxu2(top, w[i] & 0x7fff7fffu);
-    }
-    // `top` of a thread as bits of an f32 of the same order and value
-    static __device__ __forceinline__ uint32_t value(uint32_t top) {
-        if constexpr (sizeof(T) == 4) return top;
-        const uint16_t h = static_cast<uint16_t>(max(top >> 16, top & 0xffffu));
-        return __float_as_uint(to_f32(*reinterpret_cast<const T *>(&h))) & 0x7fffffffu;
-    }
-    __device__ __forceinline__ float at(int i) const {
-        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
-        const uint16_t h = static_cast<uint16_t>(i & 1 ? w[i >> 1] >> 16 : w[i >> 1]);
-        return to_f32(*reinterpret_cast<const T *>(&h));
-    }
-};
-
 // The low bytes of eight words.
 __device__ __forceinline__ uint2 low_bytes(const uint32_t (&k)[8]) {
     return make_uint2(

@@ -503,3 +503,22 @@ def test_refusals(ip):
         ip.kv4_read(cache, i2, table, 2, dtype=torch.float64)
     with pytest.raises(ValueError):
         ip.kv4_read(cache, i2, table, -1)
+
+
+def test_append_where_the_scale_is_subnormal(ip):
+    # the nearest scale may be a third below amax / 7: codes end at 7
+    unit = 2.0 ** -133                      # of a bf16 subnormal
+    rng = np.random.default_rng(12)
+    x = np.zeros((1, 64, 1, 128), np.float32)
+    for t in range(64):
+        x[0, t, 0] = (rng.uniform(-1, 1, 128) * unit * rng.uniform(1, 60)).astype(np.float32)
+        x[0, t, 0, 32 * (t % 4)] = np.float32(unit * (3.6 + 0.17 * t))
+    k = torch.from_numpy(x).cuda()
+    cache, table = ip.kv4_cache(1, 1, 64), ints([[0]])
+    ip.kv4_append(k, -k, ints([0]), table, cache)
+    got = cache.cpu().numpy()[0, 0]
+    base = 0
+    for part, size in zip((*ref.rows_bytes(f64(k)[0, :, 0], ref.K_BYTE), *ref.rows_bytes(f64(-k)[0, :, 0], ref.V_BYTE)),
+                          (64, 8, 64, 8)):
+        np.testing.assert_array_equal(got[base:base + 64 * size].reshape(64, size), part)
+        base += size * 64
