@@ -677,13 +677,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         int rs = 0, rph = 0, fs = 0, fph = 0, turn = 0;
         bool ok = true;
         for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
-            const long long m0 = tile / prm.tiles_n * (TILE_M * C::CTAS) + rank * TILE_M;
-            const int n0 = static_cast<int>(tile % prm.tiles_n) * BN + rank * C::BR;
-            // groups of eight rows that hold anything (rows past the end feed outputs that
-            // are not written)
-            const long long mr = prm.M - m0;
-            const int ma = mr <= 0 ? 0 : (mr < TILE_M ? static_cast<int>((mr + 7) / 8) : TILE_M / 8);
-            const int nr = prm.N - n0, nb = nr <= 0 ? 0 : (nr < C::BR ? (nr + 7) / 8 : C::BR / 8);
             for (int it = 0; it < stages; ++it) {
                 if (turn == grp) {
                     // the first loads run while the fp16 slot is waited for; a wait that ran out shows
@@ -691,12 +684,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                     ok = wait_or_dead<false>(raw_full(rs), rph, dead, limit);
                     const uint32_t src = base + C::RAW_AT + rs * C::RAW + lane * 16;
                     const uint32_t dst = base + C::F16_AT + fs * C::F16;
-                    const bool whole = ma == TILE_M / 8 && nb == C::BR / 8 && UNITS % GW == 0;
+                    static_assert(UNITS % GW == 0, "units");
                     constexpr int AHEAD = PER < 4 ? PER : 4;
                     uint4 v[AHEAD];
-                    if (whole)
 #pragma unroll
-                        for (int i = 0; i < AHEAD; ++i) v[i] = lds128(src + (i * GW + cw) * 512);
+                    for (int i = 0; i < AHEAD; ++i) v[i] = lds128(src + (i * GW + cw) * 512);
                     ok = wait_or_dead<PAIR>(f16_empty(fs), fph ^ 1, dead, limit) && ok;
                     if (!__all_sync(0xffffffffu, ok)) {
                         ok = false;
@@ -711,18 +703,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                         sts128(dst + u * 1024 + d0, h[0], h[1], h[2], h[3]);
                         sts128(dst + u * 1024 + d1, h[4], h[5], h[6], h[7]);
                     };
-                    if (whole) {
 #pragma unroll
-                        for (int i = 0; i < PER; ++i) {
-                            one(i * GW + cw, v[i % AHEAD]);
-                            if (i + AHEAD < PER) v[i % AHEAD] = lds128(src + ((i + AHEAD) * GW + cw) * 512);
-                        }
-                    } else {
-#pragma unroll 2
-                        for (int u = cw; u < UNITS; u += GW) {
-                            if (u < TILE_M / 8 ? u >= ma : u - TILE_M / 8 >= nb) continue;
-                            one(u, lds128(src + u * 512));
-                        }
+                    for (int i = 0; i < PER; ++i) {
+                        one(i * GW + cw, v[i % AHEAD]);
+                        if (i + AHEAD < PER) v[i % AHEAD] = lds128(src + ((i + AHEAD) * GW + cw) * 512);
                     }
                     // the fp16 stage to the MMA, the raw stage to the next TMA copy
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
