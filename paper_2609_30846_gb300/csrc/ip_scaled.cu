@@ -175,7 +175,7 @@ int run_tc(ips::ScaledParams prm, int nsm, cudaStream_t st) {
 // The form that a launch is expected to take the least time in, ns.  Fitted on GB300 to sweeps of
 // M = 12 .. 4096 tokens over N = 512 .. 16384 at K = 1024 and 4096, every form timed at each point:
 // the vector kernel reads the weights once per eight tokens; the tensor-core forms take so
-// long per fp16 stage (64 of K) of a round of tiles over the SMs.  (us, vector / 32 / 128 / pairs:
+// long per fp16 stage (64 of K) of a round of tiles over the SMs.  (us as fitted, vector / 32 / 128 / pairs:
 // 32 x 1024 -> 512 3.4 / 6.8 / 8.8 / 12.7, 128 x 4096 -> 512 - / 10.0 / 22.9 / 38,
 // 32 x 4096 -> 16384 60 / 66 / 29 / 43, 2048 x 1024 -> 16384 - / 237 / 89 / 71.)
 enum Form { FORM_VEC, FORM_32, FORM_128, FORM_PAIR };

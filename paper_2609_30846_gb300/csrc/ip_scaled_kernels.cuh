@@ -41,7 +41,7 @@ using namespace ipr;
 //
 // What bounds it: DRAM.  A row stays in registers between the two passes up to
 // 8 UNITS elements a thread; a longer one is read again (from L2).  12000 x 4096 bf16
-// 28.6 us, 5.1 TB/s; a single row of 1024 1.4 us, a launch's latency.
+// 26.5 us, 5.6 TB/s; a single row of 1024 1.6 us, a launch's latency.
 
 constexpr int QUANT_THREADS = 256;
 constexpr int QUANT_UNITS = 4;      // units of eight elements that a thread keeps
@@ -324,9 +324,11 @@ __global__ void __launch_bounds__(VEC_THREADS) scaled_vec_kernel(const ScaledPar
 // where K is short.  So the CTAs of a pair share their channels: each converts its 128
 // tokens and half of the 256 channels for an MMA of 256 x 256 (cta_group::2), a third
 // less for the same products (a CTA alone on 128 x 256: 80 % of that pipe, the tensor pipe
-// at 36 %).  12000 x 1024 -> 4096 98 us (without the epilogue's arithmetic and stores 77,
-// without the conversion either 62), 12000 x 4096 -> 1024 107 us (188 pair tiles for 76
-// pairs: the third round is half empty), 4096 x 8192 -> 8192 429 us, 1282 TFLOP/s.
+// at 36 %).  12000 x 1024 -> 4096 96 us (without the epilogue's arithmetic and stores some
+// 20 less, without the conversion as well some 35), 12000 x 4096 -> 1024 98 us (188 pair
+// tiles for 76 pairs: the third round is half empty; its tiles cut in halves of 128
+// channels gave 5 us there and cost up to 2 elsewhere), 4096 x 8192 -> 8192 423 us,
+// 1300 TFLOP/s.
 
 constexpr int TILE_M = 128;
 constexpr int BK = 64;              // K elements of a stage (rows of 64 bytes raw, of 128 in fp16)
@@ -509,8 +511,8 @@ __device__ __forceinline__ void tmem_wait_ld() {
 
 // 16 outputs of one token from column n on.  `vec`: the row starts on 32 bytes.  Whole sectors
 // straight from the registers: the blocks that TMA stores need take the room of a raw
-// stage (12000 x 1024 -> 4096 95 us for 98, but 12000 x 4096 -> 1024 118 us for 107), and a
-// tensor store writes behind column N up to the next 16 bytes.
+// stage (12000 x 1024 -> 4096 3 us less, but 12000 x 4096 -> 1024 11 us more), and a tensor
+// store writes behind column N up to the next 16 bytes.
 template <typename T>
 __device__ __forceinline__ void store16(T *row, int n, int N, bool vec, const float (&z)[16]) {
     if (vec && n + 16 <= N) {
@@ -670,7 +672,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         constexpr int UNITS = (TILE_M + C::BR) / 8;   // of eight rows
         constexpr int GW = CONV_WARPS / CONV_GROUPS, PER = (UNITS + GW - 1) / GW;
         const int cw = (warp - EPI_WARPS) % GW, grp = (warp - EPI_WARPS) / GW;
-        // A unit is eight rows.  A lane takes 16 bytes of row r8: a quarter-warp reads 128 consecutive
+        // A unit is eight rows (past the end of X or W zeros, converted like the others: a second loop
+        // that leaves them out costs registers, 12000 x 4096 -> 1024 107 us for 98).  A lane takes 16 bytes of row r8: a quarter-warp reads 128 consecutive
         // bytes, two rows, whose fp16 chunks of one parity fall on different banks under the swizzle.
         const int r8 = lane >> 2, j = lane & 3;
         const uint32_t d0 = swz(r8, 2 * j), d1 = swz(r8, 2 * j + 1);
