@@ -78,13 +78,14 @@ bool output(PyObject *o, at::IntArrayRef shape, const at::Tensor &like, at::Scal
 }
 
 // Calls without the interpreter's lock: a launch may wait for room in its stream's queue.
+struct Unlocked {
+    PyThreadState *state = PyEval_SaveThread();
+    ~Unlocked() { PyEval_RestoreThread(state); }      // before an exception becomes Python's too
+};
 template <typename F>
 int unlocked(F &&f) {
-    int rc;
-    Py_BEGIN_ALLOW_THREADS;
-    rc = f();
-    Py_END_ALLOW_THREADS;
-    return rc;
+    const Unlocked u;
+    return f();
 }
 
 PyObject *pair(const at::Tensor &a, const at::Tensor &b) {
