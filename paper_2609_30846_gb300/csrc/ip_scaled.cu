@@ -100,15 +100,14 @@ int launch_vec(const ips::ScaledParams &prm, int nsm, cudaStream_t st) {
     return launched(iph::launch_pdl(ips::scaled_vec_kernel<T, MT, CPT, KT, false>, grid, block, 0, st, prm));
 }
 
+// Four channels a thread where every SM still gets one and a half CTAs, else one.
+bool vec_four(int K, int N, int nsm) { return N >= nsm * (K > 2048 ? 6 : 24); }
+
 template <typename T, int MT>
 int launch_vec_m(const ips::ScaledParams &prm, int nsm, cudaStream_t st) {
-    // the most channels a CTA for which every SM still gets one and a half CTAs
-    if (prm.K > 2048) {
-        if (prm.N >= nsm * 6) return launch_vec<T, MT, 4, 256>(prm, nsm, st);
-        return launch_vec<T, MT, 1, 256>(prm, nsm, st);
-    }
-    if (prm.N >= nsm * 24) return launch_vec<T, MT, 4, 64>(prm, nsm, st);
-    return launch_vec<T, MT, 1, 64>(prm, nsm, st);
+    const bool four = vec_four(prm.K, prm.N, nsm);
+    if (prm.K > 2048) return four ? launch_vec<T, MT, 4, 256>(prm, nsm, st) : launch_vec<T, MT, 1, 256>(prm, nsm, st);
+    return four ? launch_vec<T, MT, 4, 64>(prm, nsm, st) : launch_vec<T, MT, 1, 64>(prm, nsm, st);
 }
 
 template <typename T, int BN, bool LONG, bool PAIR, bool KSPLIT = false>
@@ -173,11 +172,11 @@ int run_tc(ips::ScaledParams prm, int nsm, cudaStream_t st) {
 }
 
 // The form that a launch is expected to take the least time in, ns.  Fitted on GB300 to sweeps of
-// M = 12 .. 4096 tokens over N = 512 .. 16384 at K = 1024 and 4096, every form timed at each point:
+// M = 16 .. 4096 tokens over N = 512 .. 16384 at K = 1024 and 4096, every form timed at each point:
 // the vector kernel reads the weights once per eight tokens; the tensor-core forms take so
-// long per fp16 stage (64 of K) of a round of tiles over the SMs.  (us as fitted, vector / 32 / 128 / pairs:
-// 32 x 1024 -> 512 3.4 / 6.8 / 8.8 / 12.7, 128 x 4096 -> 512 - / 10.0 / 22.9 / 38,
-// 32 x 4096 -> 16384 60 / 66 / 29 / 43, 2048 x 1024 -> 16384 - / 237 / 89 / 71.)
+// long per fp16 stage (64 of K) of a round of tiles over the SMs.  (us, vector / 32 / 128 / pairs:
+// 32 x 1024 -> 512 3.0 / 7.0 / 7.8 / 12.0, 128 x 1024 -> 1024 12.5 / 7.1 / 8.3 / 12.9, 32 x 4096 -> 4096
+// 18.5 / 19.6 / 23.1 / 34.6, 32 x 4096 -> 16384 - / 70.6 / 23.8 / 35.9, 2048 x 1024 -> 16384 - / - / 86 / 69.)
 enum Form { FORM_VEC, FORM_32, FORM_128, FORM_PAIR };
 struct Choice {
     Form form;
@@ -186,29 +185,35 @@ struct Choice {
 
 long long rounds(long long tiles, int workers) { return (tiles + workers - 1) / workers; }
 
-Choice choose(const ips::ScaledParams &prm, int nsm) {
+Choice choose(const ips::ScaledParams &prm, size_t es, int nsm) {
     const long long stages = (prm.K + ips::BK - 1) / ips::BK;
     const long long tm = (prm.M + ips::TILE_M - 1) / ips::TILE_M;
     const long long t32 = tm * ((prm.N + 31) / 32), t128 = tm * ((prm.N + 127) / 128);
     const long long pairs = (tm + 1) / 2 * ((prm.N + 255) / 256);
-    // few tiles: up to four parts of at least 512 bytes of K that fit the SMs at once (eight: slower,
-    // 12 x 4096 -> 512 13.5 us for 10)
-    int splits = 1;
-    while (splits < 4 && 2 * splits * t32 <= nsm && stages >= 16 * splits) splits *= 2;
-    Choice best = {FORM_32, splits};
-    long long least = splits > 1 ? 5800 + 265 * (stages / splits) : 3400 + 265 * stages * rounds(t32, nsm);
-    const long long ns128 = 3800 + 305 * stages * rounds(t128, nsm);
+    // Output rows that are not aligned to 8 bytes are written one element at a time, a row a lane: so
+    // long for each of a warp's columns, half the tile's (800 x 1024 -> 777, bf16: 128 24 us, 32 17).
+    const long long odd = (reinterpret_cast<uintptr_t>(prm.y) | (static_cast<size_t>(prm.ldy) * es)) & 7 ? 240 : 0;
+    Choice best = {FORM_32, 1};
+    long long least = 3400 + (265 * stages + 16 * odd) * rounds(t32, nsm);
+    // few tiles: up to four parts of K that fit the SMs at once (512 x 1024 -> 512: one part 7.1 us, two
+    // 8.4; 128 x 4096 -> 512: one 19.8, four 9.5; eight are slower, 12 x 4096 -> 512 13.5 us for 10)
+    for (int splits = 2; splits <= 4 && splits * t32 <= nsm && splits <= stages; splits *= 2) {
+        const long long ns = 5800 + 265 * ((stages + splits - 1) / splits);
+        if (ns < least) best = {FORM_32, splits}, least = ns;
+    }
+    const long long ns128 = 3800 + (305 * stages + 64 * odd) * rounds(t128, nsm);
     if (ns128 < least) best = {FORM_128, 1}, least = ns128;
-    const long long ns_pair = 5700 + 475 * stages * rounds(pairs, nsm / 2);
+    const long long ns_pair = 5700 + (475 * stages + 128 * odd) * rounds(pairs, nsm / 2);
     if (ns_pair < least) best = {FORM_PAIR, 1}, least = ns_pair;
     const long long blocks = (prm.M + 7) / 8, kv = prm.K > 1024 ? prm.K : 1024;     // a channel's reduction
-    if (blocks <= 65535 && 2200 + 29 * (prm.N * kv * blocks) / 100000 < least) best = {FORM_VEC, 1};
+    const long long rate = vec_four(prm.K, prm.N, nsm) ? (prm.K > 4096 ? 57 : (prm.K > 2048 ? 26 : 31)) : 63;
+    if (blocks <= 65535 && 1900 + rate * (prm.N * kv * blocks) / 100000 < least) best = {FORM_VEC, 1};
     return best;
 }
 
 template <typename T>
 int run_scaled(ips::ScaledParams prm, int nsm, cudaStream_t st) {
-    const Choice c = choose(prm, nsm);
+    const Choice c = choose(prm, sizeof(T), nsm);
     prm.splits = c.splits;
     switch (c.form) {
         case FORM_VEC:
