@@ -110,14 +110,18 @@ int launch_vec_m(const ips::ScaledParams &prm, int nsm, cudaStream_t st) {
     return four ? launch_vec<T, MT, 4, 64>(prm, nsm, st) : launch_vec<T, MT, 1, 64>(prm, nsm, st);
 }
 
-template <typename T, int BN, bool LONG, bool PAIR, bool KSPLIT = false>
+bool odd_rows(const ips::ScaledParams &prm, size_t es) {
+    return ((reinterpret_cast<uintptr_t>(prm.y) | (static_cast<size_t>(prm.ldy) * es)) & 7) != 0;
+}
+
+template <typename T, int BN, bool LONG, bool PAIR, bool KSPLIT = false, bool ODD = false>
 int launch_tc(const CUtensorMap &tx, const CUtensorMap &tw, const ips::ScaledParams &prm, int nsm,
               cudaStream_t st) {
     using C = ips::Tile<BN, PAIR>;
     static bool set[64] = {false};
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return IP_ERR_CUDA;
-    auto *fn = ips::scaled_tc_kernel<T, BN, LONG, PAIR, KSPLIT>;
+    auto *fn = ips::scaled_tc_kernel<T, BN, LONG, PAIR, KSPLIT, ODD>;
     {
         std::lock_guard<std::mutex> lock(g_mu);
         if (!set[dev]) {
@@ -150,6 +154,12 @@ int launch_tc(const CUtensorMap &tx, const CUtensorMap &tw, const ips::ScaledPar
     return launched(cudaLaunchKernelEx(&cfg, fn, tx, tw, prm));
 }
 
+template <typename T, int BN, bool LONG, bool PAIR>
+int launch_rows(const CUtensorMap &tx, const CUtensorMap &tw, const ips::ScaledParams &prm, int nsm, cudaStream_t st) {
+    return odd_rows(prm, sizeof(T)) || prm.N % 16 != 0 ? launch_tc<T, BN, LONG, PAIR, false, true>(tx, tw, prm, nsm, st)
+                                                       : launch_tc<T, BN, LONG, PAIR>(tx, tw, prm, nsm, st);
+}
+
 template <typename T, int BN, bool PAIR>
 int run_tc(ips::ScaledParams prm, int nsm, cudaStream_t st) {
     using C = ips::Tile<BN, PAIR>;
@@ -166,9 +176,8 @@ int run_tc(ips::ScaledParams prm, int nsm, cudaStream_t st) {
                        ? launch_tc<T, BN, true, PAIR, true>(tx, tw, prm, nsm, st)
                        : launch_tc<T, BN, false, PAIR, true>(tx, tw, prm, nsm, st);
     }
-    if constexpr (BN <= 128 || PAIR)
-        if (prm.K > ips::SEG * ips::BK) return launch_tc<T, BN, true, PAIR>(tx, tw, prm, nsm, st);
-    return launch_tc<T, BN, false, PAIR>(tx, tw, prm, nsm, st);
+    if (prm.K > ips::SEG * ips::BK) return launch_rows<T, BN, true, PAIR>(tx, tw, prm, nsm, st);
+    return launch_rows<T, BN, false, PAIR>(tx, tw, prm, nsm, st);
 }
 
 // The form that a launch is expected to take the least time in, ns.  Fitted on GB300 to sweeps of
@@ -190,9 +199,9 @@ Choice choose(const ips::ScaledParams &prm, size_t es, int nsm) {
     const long long tm = (prm.M + ips::TILE_M - 1) / ips::TILE_M;
     const long long t32 = tm * ((prm.N + 31) / 32), t128 = tm * ((prm.N + 127) / 128);
     const long long pairs = (tm + 1) / 2 * ((prm.N + 255) / 256);
-    // Output rows that are not aligned to 8 bytes are written one element at a time, a row a lane: so
-    // long for each of a warp's columns, half the tile's (800 x 1024 -> 777, bf16: 128 24 us, 32 17).
-    const long long odd = (reinterpret_cast<uintptr_t>(prm.y) | (static_cast<size_t>(prm.ldy) * es)) & 7 ? 240 : 0;
+    // output rows that are not aligned to 8 bytes are turned in shared memory first: so long for each
+    // of a warp's columns, half the tile's
+    const long long odd = odd_rows(prm, es) ? 45 : 0;
     Choice best = {FORM_32, 1};
     long long least = 3400 + (265 * stages + 16 * odd) * rounds(t32, nsm);
     // few tiles: up to four parts of K that fit the SMs at once (512 x 1024 -> 512: one part 7.1 us, two

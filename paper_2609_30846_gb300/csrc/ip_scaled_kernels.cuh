@@ -338,6 +338,8 @@ constexpr int TC_REGS = 96;         // registers a thread at launch
 constexpr int EPI_WARPS = 8, CONV_WARPS = 8, CONV_GROUPS = 4;
 constexpr int TMA_WARP = 16, MMA_WARP = 17;
 
+constexpr int TURN_LD = 17, TURN_BYTES = 16 * TURN_LD * 4;
+
 template <int BN_, bool PAIR_>
 struct Tile {
     static constexpr int BN = BN_;
@@ -354,7 +356,8 @@ struct Tile {
     static constexpr int TMEM_PTR = 256, DEAD = 260;
     static constexpr int CONSTS = 512;                // per epilogue warp: sw and bias of its columns
     // the sums of a tile, where the CTAs of a cluster share its K
-    static constexpr int SUMS_AT = (CONSTS + EPI_WARPS * 2 * 4 * (BN / 2) + 1023) & ~1023;
+    static constexpr int TURN = CONSTS + EPI_WARPS * 2 * 4 * (BN / 2);      // per epilogue warp: store_odd's block
+    static constexpr int SUMS_AT = (TURN + EPI_WARPS * TURN_BYTES + 1023) & ~1023;
     static constexpr int F16_AT = SUMS_AT + (BN == 32 ? 4 * TILE_M * BN : 0);
     static constexpr int RAW_AT = F16_AT + FS * F16;
     static constexpr int SMEM = RAW_AT + RS * RAW + 1024;
@@ -509,41 +512,57 @@ __device__ __forceinline__ void tmem_wait_ld() {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
-// 16 outputs of one token from column n on, in stores of what all rows are aligned to (`align`, up
-// to 32 bytes; 800 x 1024 -> 700 in bf16, rows of 1400 bytes: 10.7 us, element by element 24).  Whole sectors straight from
-// the registers: the blocks that TMA stores need take the room of a raw stage (12000 x 1024
+// 16 outputs of one token from column n on, in stores of 32 bytes (WIDE) or 8, as all rows are
+// aligned.  Whole sectors straight from the registers: the blocks that TMA stores need take the room of a raw stage (12000 x 1024
 // -> 4096 3 us less, but 12000 x 4096 -> 1024 11 us more), and a tensor store writes behind
 // column N up to the next 16 bytes.
 template <typename T>
-__device__ __forceinline__ void store16(T *row, int n, int N, int align, const float (&z)[16]) {
+__device__ __forceinline__ void store16(T *row, int n, bool wide, const float (&z)[16]) {
     constexpr int WORDS = 4 * sizeof(T);
-    if (align >= 8 && n + 16 <= N) {
-        union { T e[16]; uint32_t w[WORDS]; } v;
+    union { T e[16]; uint32_t w[WORDS]; } v;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v.e[j] = from_f32<T>(z[j]);
-        const uint32_t (&w)[WORDS] = v.w;
-        uint32_t *p = reinterpret_cast<uint32_t *>(row + n);
-        if (align == 32) {
+    for (int j = 0; j < 16; ++j) v.e[j] = from_f32<T>(z[j]);
+    const uint32_t (&w)[WORDS] = v.w;
+    uint32_t *p = reinterpret_cast<uint32_t *>(row + n);
+    if (wide) {
 #pragma unroll
-            for (int i = 0; i < WORDS; i += 8)
-                asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p + i), "r"(w[i]), "r"(w[i + 1]),
-                             "r"(w[i + 2]), "r"(w[i + 3]), "r"(w[i + 4]), "r"(w[i + 5]), "r"(w[i + 6]), "r"(w[i + 7])
-                             : "memory");
-        } else {
-#pragma unroll
-            for (int i = 0; i < WORDS; i += 2) *reinterpret_cast<uint2 *>(p + i) = make_uint2(w[i], w[i + 1]);
-        }
+        for (int i = 0; i < WORDS; i += 8)
+            asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p + i), "r"(w[i]), "r"(w[i + 1]),
+                         "r"(w[i + 2]), "r"(w[i + 3]), "r"(w[i + 4]), "r"(w[i + 5]), "r"(w[i + 6]), "r"(w[i + 7])
+                         : "memory");
     } else {
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-            if (n + j < N) row[n + j] = from_f32<T>(z[j]);
+        for (int i = 0; i < WORDS; i += 2) *reinterpret_cast<uint2 *>(p + i) = make_uint2(w[i], w[i + 1]);
+    }
+}
+// 16 columns of the tokens of a warp's lanes for rows of any alignment, `rows` and `cols` of them (y: the
+// first token's first): turned in shared memory, 16 tokens at a time, so that half a warp writes
+// consecutive columns (12000 x 1024 -> 4097 in bf16: 164 us, a lane a row 476).
+template <typename T>
+__device__ __forceinline__ void store_odd(T *y, long long ldy, int rows, int cols, uint32_t turn, const float (&z)[16]) {
+    const int lane = threadIdx.x & 31, half = lane >> 4, col = lane & 15;
+    y += half * ldy + col;
+#pragma unroll 1
+    for (int h = 0; h < 2; ++h) {
+        __syncwarp();
+        if (half == h)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sts32(turn + 4 * (col * TURN_LD + j), __float_as_uint(z[j]));
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+            const float x = __uint_as_float(lds32(turn + 4 * ((i + half) * TURN_LD + col)));
+            if (16 * h + i + half < rows && col < cols) y[(16 * h + i) * ldy] = from_f32<T>(x);
+        }
     }
 }
 
 // LONG: a CTA's K is longer than 1024, several segments per tile.  KSPLIT: the CTAs of a cluster
 // share one tile's K and add their sums through each other's shared memory, a part of the
 // rows each (few tiles: 64 x 4096 -> 1024 in 32 tiles 20 us, by clusters of four 10).
-template <typename T, int BN, bool LONG, bool PAIR, bool KSPLIT>
+// ODD: output rows that are not aligned to 8 bytes, or an N that 16 does not divide (for the others the
+// registers of store_odd would cost 12000 x 4096 -> 1024 104 us for 98).
+template <typename T, int BN, bool LONG, bool PAIR, bool KSPLIT, bool ODD>
 __global__ void __launch_bounds__(TC_THREADS, 1)
     scaled_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w,
                      const ScaledParams prm) {
@@ -737,7 +756,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         constexpr int CH = CW < 16 ? 1 : CW / 16;
         const int col0 = half * CW;
         const unsigned low = static_cast<unsigned>(reinterpret_cast<uintptr_t>(prm.y) | (prm.ldy * sizeof(T))) & 31u;
-        const int align = low == 0 ? 32 : (low & 7u ? 1 : 8);
+        const bool wide = low == 0, even = (low & 7u) == 0;
         const uint32_t cst = base + C::CONSTS + warp * (8 * CW);
         int a = 0, aph = 0;
         bool ok = true;
@@ -768,7 +787,15 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                 if (prm.act)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) z[i] = swish<T>(z[i]);
-                if (m < prm.M) store16<T>(row, n0 + c, prm.N, align, z);
+                if (ODD && (!even || n0 + c + 16 > prm.N)) {
+                    const long long first = m - lane, left = prm.M - first;
+                    if (n0 + c < prm.N)
+                        store_odd<T>(static_cast<T *>(prm.y) + first * prm.ldy + n0 + c, prm.ldy,
+                                     left < 32 ? static_cast<int>(left) : 32, prm.N - n0 - c,
+                                     base + C::TURN + warp * TURN_BYTES, z);
+                } else if (m < prm.M && n0 + c < prm.N) {
+                    store16<T>(row, n0 + c, wide, z);
+                }
             };
             int sum[LONG || KSPLIT ? CH : 1][16];
             if (LONG || KSPLIT)

@@ -259,6 +259,32 @@ def test_rows_without_a_scale_and_far_activations(ip, M):
         assert ((y[1].double() - want).abs() <= tol).all()
 
 
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("M,K,N", [(40, 1024, 1500), (100, 4096, 100), (1000, 1024, 1037), (900, 2100, 1033),
+                                   (2000, 1024, 4097), (1001, 2100, 4090)])
+@pytest.mark.parametrize("shift,ld", [(0, 0), (1, 3), (4, 8), (2, 2)])
+def test_output_rows_of_any_alignment(ip, dtype, M, K, N, shift, ld):
+    # the same bits whatever the rows' alignment, and nothing beside them
+    g = torch.Generator(device="cuda").manual_seed(M)
+    q, s = ip.quantize_rows_i8(torch.randn(M, K, generator=g, device="cuda"))
+    w, sw = ip.quantize_rows_i8(torch.randn(N, K, generator=g, device="cuda"))
+    b = torch.randn(N, generator=g, device="cuda")
+    wide = torch.empty(M, (N + 31) // 32 * 32, dtype=DT[dtype], device="cuda")
+    base = torch.full((M, N + shift + ld), 7.0, dtype=DT[dtype], device="cuda")
+    for act in (ip.ACT_NONE, ip.ACT_SWISH):
+        want = ip.linear_scaled_i8(q, s, w, sw, b, act=act, out=wide[:, :N])
+        ip.linear_scaled_i8(q, s, w, sw, b, act=act, out=base[:, shift:shift + N])
+        assert torch.equal(base[:, shift:shift + N], want)
+        assert (base[:, :shift] == 7).all() and (base[:, shift + N:] == 7).all()
+    z = (q[:9].double() @ w.double().t()) * s[:9, None].double() * sw.double() + b.double()
+    mag = (q[:9].double() @ w.double().t()).abs() * s[:9, None].double() * sw.double() + b.double().abs()
+    got = ip.linear_scaled_i8(q, s, w, sw, b, out=base[:, shift:shift + N])[:9].double()
+    fin = torch.finfo(DT[dtype])
+    # sx sw, the sum to f32 and the multiply-add round once each (2^-24), then the output
+    tol = mag * 4 * 2.0 ** -24 + z.abs() * fin.eps / 2 * 1.01 + fin.smallest_normal * fin.eps
+    assert ((got - z).abs() <= tol).all()
+
+
 def test_offsets_past_31_bits(ip):
     M, N, K = 36000, 65536, 48
     x = torch.randint(-127, 128, (M, K), dtype=torch.int8, device="cuda")
