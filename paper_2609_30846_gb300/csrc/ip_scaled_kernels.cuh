@@ -349,9 +349,11 @@ struct Tile {
     static constexpr int F16 = (TILE_M + BR) * BK * 2;
     static constexpr int RS = BN == 32 ? 8 : 5;       // raw stages (as many bytes in two stages of 128: 20 % slower)
     static constexpr int FS = 4;                      // fp16 stages
-    // a group of warps, which sees every CONV_GROUPS-th use of the slots, must not wait for the
-    // phase after next of one: their parities are alike
-    static_assert(CONV_GROUPS <= FS && CONV_GROUPS <= RS, "groups");
+    // A parity is also that of the phase two before, and a group of warps sees every CONV_GROUPS-th
+    // stage only.  The slot of its next fp16 stage was its own before, so that wait is unambiguous; it
+    // says that the MMA is done with all stages up to FS back, so the raw slot's stage before, RS
+    // back, has landed too: the raw barrier may be asked after the fp16 one, not before it.
+    static_assert(FS % CONV_GROUPS == 0 && RS >= FS, "phases");
     static constexpr int BARS = 0;                    // 2 RS + 2 FS + 5 barriers
     static constexpr int TMEM_PTR = 256, DEAD = 260;
     static constexpr int CONSTS = 512;                // per epilogue warp: sw and bias of its columns
@@ -707,9 +709,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
             for (int it = 0; it < stages; ++it) {
                 if (turn == grp) {
-                    // the first loads run while the fp16 slot is waited for; a wait that ran out shows
-                    // after both (what was read meanwhile is not used)
-                    ok = wait_or_dead<false>(raw_full(rs), rph, dead, limit);
+                    // in this order (Tile's phases); a wait that ran out shows after both
+                    ok = wait_or_dead<PAIR>(f16_empty(fs), fph ^ 1, dead, limit);
+                    ok = wait_or_dead<false>(raw_full(rs), rph, dead, limit) && ok;
+                    if (!__all_sync(0xffffffffu, ok)) {
+                        ok = false;
+                        break;
+                    }
                     const uint32_t src = base + C::RAW_AT + rs * C::RAW + lane * 16;
                     const uint32_t dst = base + C::F16_AT + fs * C::F16;
                     static_assert(UNITS % GW == 0, "units");
@@ -717,11 +723,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                     uint4 v[AHEAD];
 #pragma unroll
                     for (int i = 0; i < AHEAD; ++i) v[i] = lds128(src + (i * GW + cw) * 512);
-                    ok = wait_or_dead<PAIR>(f16_empty(fs), fph ^ 1, dead, limit) && ok;
-                    if (!__all_sync(0xffffffffu, ok)) {
-                        ok = false;
-                        break;
-                    }
                     auto one = [&](int u, const uint4 &v) {
                         uint32_t h[8];
                         cvt4(v.x, h[0], h[1]);
