@@ -600,7 +600,10 @@ __global__ void __launch_bounds__(ATT_THREADS, NT == 1 ? CTAS_8 : CTAS_16) kv4_a
             const int ex = 268 - static_cast<int>(__float_as_uint(top) >> 23);
             const int fe = ex > 254 ? 254 : ex;
             const float up = __uint_as_float(static_cast<uint32_t>(fe) << 23);
-            const float rs = fmaxf(ldexpf(prm.scale_log2, 24 - (fe - 127)), 0x1p-126f);   // > 0: -inf times it
+            // > 0, since it multiplies -inf, and finite, since it multiplies 0: at the upper end (a
+            // query of 2^121 at 1 / sqrt(128)) scores that differ still do by 2^7 and more, as long as
+            // their keys are above 2^-96
+            const float rs = fminf(fmaxf(ldexpf(prm.scale_log2, 24 - (fe - 127)), 0x1p-126f), 0x1p127f);
             float sums[4];
 #pragma unroll
             for (int gr = 0; gr < 4; ++gr) {
@@ -638,6 +641,10 @@ __global__ void __launch_bounds__(ATT_THREADS, NT == 1 ? CTAS_8 : CTAS_16) kv4_a
         // m: the reference of the row's exponentials, mr: in units of log2.  It is raised to the
         // maximum only when a score exceeds it by more than SLACK there (lift: the score that does):
         // the probabilities reach 2^SLACK at most, and most batches skip the rescaling.
+        // far: a row's reference is 2^20 or more, where the rounding of mr begins to show in the
+        // exponents (2^25: a step of 1).  Then the scores are taken less m before they are scaled,
+        // and every score above m raises it.
+        bool far = false;
         float o[NT][8][4], m[NT][2], mr[NT][2], l[NT][2], lift[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -793,6 +800,24 @@ __global__ void __launch_bounds__(ATT_THREADS, NT == 1 ? CTAS_8 : CTAS_16) kv4_a
 #pragma unroll
                         for (int c = 0; c < 8; ++c) o[nt][c][j] *= ad, o[nt][c][2 + j] *= ad;
                     }
+                bool high = false;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) high |= fmaxf(fabsf(mr[nt][0]), fabsf(mr[nt][1])) >= 0x1p20f;
+                far = __any_sync(0xffffffffu, high);
+                if (far)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) lift[nt][0] = m[nt][0], lift[nt][1] = m[nt][1];
+            }
+            float less[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) less[nt][0] = mr[nt][0], less[nt][1] = mr[nt][1];
+            if (far) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s[nt][i] -= m[nt][i & 1] == -INFINITY ? 0.0f : m[nt][i & 1];
+                    less[nt][0] = less[nt][1] = 0.0f;
+                }
             }
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
@@ -801,7 +826,7 @@ __global__ void __launch_bounds__(ATT_THREADS, NT == 1 ? CTAS_8 : CTAS_16) kv4_a
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float e1 = fast_exp2(fmaf(s[nt][4 * hf + i], rscale[nt][i & 1], -mr[nt][i & 1]));
+                        const float e1 = fast_exp2(fmaf(s[nt][4 * hf + i], rscale[nt][i & 1], -less[nt][i & 1]));
                         l[nt][i & 1] += e1;
                         p[nt][i] = e1 * norm[nt][i & 1];
                     }
