@@ -142,6 +142,7 @@ PyObject *quantize_rows(PyObject *, PyObject *const *a, Py_ssize_t n) {
 
 // Row stride of a matrix or a contiguous tensor, 0 for what the general form has to look at.
 int64_t row_stride(const at::Tensor &t) {
+    if (t.stride(-1) != 1 && t.size(-1) != 1) return 0;      // one row too: its elements are read as consecutive
     if (t.numel() == t.size(-1)) return (t.size(-1) + 15) / 16 * 16;      // one row: any stride does
     if (t.is_contiguous()) return t.size(-1);
     return t.dim() == 2 && t.stride(1) == 1 ? t.stride(0) : 0;
