@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(ROW_THREADS) kv4_read_kernel(const RowParams p
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         int off = 0;
-        w[i] = s[i] = 0;
+        w[i] = 0x88888888u, s[i] = 0;      // without a place in the cache: codes of 0, so 0 and not -0
         const uint8_t *blk = row.left > 0 ? row.block(prm, off) : nullptr;
         row.next(prm);
         if (!blk) continue;
