@@ -9,6 +9,7 @@ streams only.
 from __future__ import annotations
 
 import ctypes
+import operator
 import threading
 from dataclasses import dataclass
 
@@ -69,6 +70,15 @@ class Swish16Params(ctypes.Structure):
 
 class SoftmaxParams(ctypes.Structure):
     _fields_ = [("q_ln2", ctypes.c_int32), ("q_b", ctypes.c_int32), ("q_c", ctypes.c_int32)]
+
+
+class _Int:
+    """An int argument of an entry point.  What 32 bits do not hold becomes the end of their range,
+    which the entry points refuse, where c_int would wrap it to a value they may take."""
+
+    @classmethod
+    def from_param(cls, v):
+        return ctypes.c_int(max(-1 << 31, min(operator.index(v), (1 << 31) - 1)))
 
 
 _lock = threading.Lock()
@@ -173,21 +183,22 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         lib.ip_dwconv_swish_i8.restype = I
         lib.ip_swish16_params_from_scales.argtypes = [D, D, ctypes.POINTER(Swish16Params)]
         lib.ip_swish16_params_from_scales.restype = I
-        lib.ip_quantize_rows_i8.argtypes = [P, I, LL, I, LL, P, LL, P, P]
+        N = _Int
+        lib.ip_quantize_rows_i8.argtypes = [P, N, LL, N, LL, P, LL, P, P]
         lib.ip_quantize_rows_i8.restype = I
-        lib.ip_linear_scaled_i8.argtypes = [P, LL, P, P, LL, P, P, I, LL, I, I, P, LL, I, P,
+        lib.ip_linear_scaled_i8.argtypes = [P, LL, P, P, LL, P, P, N, LL, N, N, P, LL, N, P,
                                             ctypes.c_size_t, P]
         lib.ip_linear_scaled_i8.restype = I
         S, F = ctypes.c_size_t, ctypes.c_float
-        lib.ip_kv4_page_bytes.argtypes = [I, I]
+        lib.ip_kv4_page_bytes.argtypes = [N, N]
         lib.ip_kv4_page_bytes.restype = S
-        lib.ip_kv4_append.argtypes = [P, P, I, P, P, P, P, I, I, I, I, P, I, P, I, I, P, S, P]
+        lib.ip_kv4_append.argtypes = [P, P, N, P, P, P, P, N, N, N, N, P, N, P, N, N, P, S, P]
         lib.ip_kv4_append.restype = I
-        lib.ip_kv4_read.argtypes = [P, I, I, P, I, P, P, I, I, I, I, P, P, I, P, S, P]
+        lib.ip_kv4_read.argtypes = [P, N, N, P, N, P, P, N, N, N, N, P, P, N, P, S, P]
         lib.ip_kv4_read.restype = I
-        lib.ip_kv4_attention_workspace_bytes.argtypes = [I] * 5
+        lib.ip_kv4_attention_workspace_bytes.argtypes = [N] * 5
         lib.ip_kv4_attention_workspace_bytes.restype = S
-        lib.ip_kv4_attention.argtypes = [P, I, P, P, P, I, F, I, I, I, I, I, I, P, I, P, I, I, P, P, S, P]
+        lib.ip_kv4_attention.argtypes = [P, N, P, P, P, N, F, N, N, N, N, N, N, P, N, P, N, N, P, P, S, P]
         lib.ip_kv4_attention.restype = I
         lib.ip_probe_int8_mma.argtypes = [I, I, P, P]
         lib.ip_probe_int8_mma.restype = ctypes.c_longlong
