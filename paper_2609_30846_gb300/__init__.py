@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import operator
 import threading
+import warnings
 from dataclasses import dataclass
 
 from . import build as _build
@@ -183,23 +184,18 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         lib.ip_dwconv_swish_i8.restype = I
         lib.ip_swish16_params_from_scales.argtypes = [D, D, ctypes.POINTER(Swish16Params)]
         lib.ip_swish16_params_from_scales.restype = I
-        N = _Int
-        lib.ip_quantize_rows_i8.argtypes = [P, N, LL, N, LL, P, LL, P, P]
-        lib.ip_quantize_rows_i8.restype = I
-        lib.ip_linear_scaled_i8.argtypes = [P, LL, P, P, LL, P, P, N, LL, N, N, P, LL, N, P,
-                                            ctypes.c_size_t, P]
-        lib.ip_linear_scaled_i8.restype = I
-        S, F = ctypes.c_size_t, ctypes.c_float
-        lib.ip_kv4_page_bytes.argtypes = [N, N]
-        lib.ip_kv4_page_bytes.restype = S
-        lib.ip_kv4_append.argtypes = [P, P, N, P, P, P, P, N, N, N, N, P, N, P, N, N, P, S, P]
-        lib.ip_kv4_append.restype = I
-        lib.ip_kv4_read.argtypes = [P, N, N, P, N, P, P, N, N, N, N, P, P, N, P, S, P]
-        lib.ip_kv4_read.restype = I
-        lib.ip_kv4_attention_workspace_bytes.argtypes = [N] * 5
-        lib.ip_kv4_attention_workspace_bytes.restype = S
-        lib.ip_kv4_attention.argtypes = [P, N, P, P, P, N, F, N, N, N, N, N, N, P, N, P, N, N, P, P, S, P]
-        lib.ip_kv4_attention.restype = I
+        N, S, F = _Int, ctypes.c_size_t, ctypes.c_float
+        for name, args, result in (
+                ("ip_quantize_rows_i8", [P, N, LL, N, LL, P, LL, P, P], I),
+                ("ip_linear_scaled_i8", [P, LL, P, P, LL, P, P, N, LL, N, N, P, LL, N, P, S, P], I),
+                ("ip_kv4_page_bytes", [N, N], S),
+                ("ip_kv4_append", [P, P, N, P, P, P, P, N, N, N, N, P, N, P, N, N, P, S, P], I),
+                ("ip_kv4_read", [P, N, N, P, N, P, P, N, N, N, N, P, P, N, P, S, P], I),
+                ("ip_kv4_attention_workspace_bytes", [N] * 5, S),
+                ("ip_kv4_attention", [P, N, P, P, P, N, F, N, N, N, N, N, N, P, N, P, N, N, P, P, S, P], I)):
+            fn = getattr(lib, name, None)      # a library built before these calls does the others
+            if fn is not None:
+                fn.argtypes, fn.restype = args, result
         lib.ip_probe_int8_mma.argtypes = [I, I, P, P]
         lib.ip_probe_int8_mma.restype = ctypes.c_longlong
         lib.ip_probe_int8_mix.argtypes = [I, I, I, P, P]
@@ -207,7 +203,8 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         try:
             _short = _bind_short(lib)
         except Exception as exc:  # noqa: BLE001 - reported with context
-            raise LibraryError(f"cannot load the short forms: {exc}") from exc
+            warnings.warn(f"cannot load the native short forms: {exc}; the calls take their general forms",
+                          RuntimeWarning, stacklevel=2)
         _lib = lib
         return lib
 
