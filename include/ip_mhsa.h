@@ -527,15 +527,16 @@ int ip_kv4_attention(const void *q, int dtype, const long long *q_strides, const
 const char *ip_strerror(int code);
 
 /* Test hook: bound, in SM clock cycles, of every barrier wait inside the
- * kernels launched afterwards by this process (0 = give up at the first
- * wait that is not already satisfied; negative = the default of about two
- * seconds).  A wait that runs out records IP_ERR_TIMEOUT for
- * ip_relpos_mhsa_status; the kernel lets its own copies in flight land and
- * returns. */
+ * attention kernels (ip_relpos_mhsa_*) and the tensor-core kernels of
+ * ip_linear_scaled_i8 launched afterwards by this process (0 = give up at the
+ * first wait that is not already satisfied; negative = the default of about two
+ * seconds, which the other kernels keep).  A wait that runs out records
+ * IP_ERR_TIMEOUT for ip_relpos_mhsa_status; the kernel lets its own copies in
+ * flight land and returns. */
 int ip_debug_set_timeout_cycles(long long cycles);
 
-/* Test hook: when on, the kernels launched afterwards by this process first
- * make every consumer warp wait on a barrier that nothing arrives on, so
+/* Test hook: when on, these kernels first make every consumer warp (the
+ * product's: every output warp) wait on a barrier that nothing arrives on, so
  * that the bounded wait runs out and the error path (IP_ERR_TIMEOUT, copies
  * in flight drained, early return) is exercised without faulting or hanging
  * the GPU.  Off by default. */

@@ -25,6 +25,11 @@ inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, s
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<Args &&>(args)...);
 }
 
+// The test hooks of the kernels' bounded waits, as ip_debug_set_timeout_cycles and
+// ip_debug_set_stall_injection left them (kept in ip_mhsa.cu).
+__attribute__((visibility("hidden"))) long long wait_limit();
+__attribute__((visibility("hidden"))) int stall_injection();
+
 // The constant of udiv_magic (device side) for d: floor(2^64 / d) + 1, or 0
 // for d = 1, so that floor(n / d) = the high word of n times it.
 inline unsigned long long div_magic(unsigned long long d) {

@@ -226,6 +226,13 @@ ItemPlan plan_items(long long N, int slots, int sms) {
 
 }  // namespace
 
+namespace iph {
+
+long long wait_limit() { return g_timeout_cycles; }
+int stall_injection() { return g_stall_injection; }
+
+}  // namespace iph
+
 extern "C" {
 
 size_t ip_relpos_mhsa_workspace_bytes(int B, int H, int T, int dh) {

@@ -291,7 +291,8 @@ int ip_linear_scaled_i8(const int8_t *x, long long ldx, const float *sx, const i
     prm.tiles_n = 0;
     prm.tiles = 0;
     prm.err = static_cast<int *>(workspace);
-    prm.timeout_cycles = 4000000000ll;
+    prm.timeout_cycles = iph::wait_limit();
+    prm.stall = iph::stall_injection();
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     if (dtype == IP_F32) return run_scaled<float>(prm, nsm, st);
     if (dtype == IP_F16) return run_scaled<__half>(prm, nsm, st);

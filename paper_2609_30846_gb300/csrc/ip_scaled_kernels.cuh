@@ -189,6 +189,9 @@ __global__ void __launch_bounds__(QUANT_THREADS) quantize_rows_kernel(const Quan
 // integer, act the identity or z / (1 + exp(-z)).
 
 constexpr int ERR_TIMEOUT = 1;      // status word: a barrier wait ran out
+// Bound of the waits for a CTA's own copies and MMAs in flight once it has given up, whatever the
+// limit of the others: it must not end before them.
+constexpr long long LAND_CYCLES = 4000000000ll;
 
 struct ScaledParams {
     const int8_t *x, *w;            // the vector kernel's operands (the tiles come by TMA)
@@ -201,6 +204,7 @@ struct ScaledParams {
     long long tiles;
     int *err;
     long long timeout_cycles;
+    int stall;                      // test hook: the output warps first wait on a barrier that nothing arrives on
 };
 
 // z / (1 + exp(-z)) is formed with t = exp(-|z|) <= 1, so that nothing overflows: z / (1 + t) or
@@ -354,7 +358,7 @@ struct Tile {
     // says that the MMA is done with all stages up to FS back, so the raw slot's stage before, RS
     // back, has landed too: the raw barrier may be asked after the fp16 one, not before it.
     static_assert(FS % CONV_GROUPS == 0 && RS >= FS, "phases");
-    static constexpr int BARS = 0;                    // 2 RS + 2 FS + 5 barriers
+    static constexpr int BARS = 0;                    // 2 RS + 2 FS + 6 barriers
     static constexpr int TMEM_PTR = 256, DEAD = 260;
     static constexpr int CONSTS = 512;                // per epilogue warp: sw and bias of its columns
     // the sums of a tile, where the CTAs of a cluster share its K
@@ -364,7 +368,7 @@ struct Tile {
     static constexpr int RAW_AT = F16_AT + FS * F16;
     static constexpr int SMEM = RAW_AT + RS * RAW + 1024;
     static constexpr int COLS = 2 * BN;               // TMEM columns
-    static_assert(8 * (2 * RS + 2 * FS + 5) <= 256, "barriers");
+    static_assert(8 * (2 * RS + 2 * FS + 6) <= 256, "barriers");
     static_assert(SMEM <= 232448, "shared memory");
     static_assert((COLS & (COLS - 1)) == 0 && COLS <= 512, "TMEM columns");
 };
@@ -583,7 +587,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     auto f16_empty = [&](int s) { return base + C::BARS + 8u * (2 * C::RS + C::FS + s); };
     auto acc_full = [&](int s) { return base + C::BARS + 8u * (2 * C::RS + 2 * C::FS + s); };
     auto acc_empty = [&](int s) { return base + C::BARS + 8u * (2 * C::RS + 2 * C::FS + 2 + s); };
-    const uint32_t drained = base + C::BARS + 8u * (2 * C::RS + 2 * C::FS + 4);
+    const uint32_t drained = base + C::BARS + 8u * (2 * C::RS + 2 * C::FS + 4), never = drained + 8u;
     volatile int *dead = reinterpret_cast<volatile int *>(smem + C::DEAD);
     const int rank = PAIR ? static_cast<int>(blockIdx.x & 1u) : 0;      // clusters are (2, 1, 1)
     static_assert(!KSPLIT || (BN == 32 && !PAIR), "room for the sums");
@@ -605,6 +609,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             mbar_init(acc_empty(s), EPI_WARPS * C::CTAS);
         }
         mbar_init(drained, 1);
+        mbar_init(never, 1);
         *dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -652,7 +657,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             if (!ok)
                 for (long long i = issued > C::RS ? issued - C::RS : 0; i < issued; ++i)
                     mbar_wait(raw_full(static_cast<int>(i % C::RS)),
-                              static_cast<uint32_t>((i / C::RS) & 1), limit);
+                              static_cast<uint32_t>((i / C::RS) & 1), LAND_CYCLES);
         } else if (warp == MMA_WARP && rank == 0) {
             // the whole warp runs the loop, so that the descriptors stay uniform; one lane issues
             constexpr uint32_t idesc = (1u << 4) | (static_cast<uint32_t>(BN / 8) << 17) |
@@ -689,7 +694,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             if (!ok) {   // the MMAs in flight end before their TMEM is freed
                 if (elect_one()) mma_commit<PAIR>(drained);
                 __syncwarp();
-                mbar_wait(drained, 0, limit);
+                mbar_wait(drained, 0, LAND_CYCLES);
             }
         }
     } else if (warp >= EPI_WARPS) {
@@ -761,6 +766,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         const uint32_t cst = base + C::CONSTS + warp * (8 * CW);
         int a = 0, aph = 0;
         bool ok = true;
+        if (prm.stall) ok = warp_wait_or_dead<false>(never, 0, dead, limit);
         for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
             const long long mq = tile / prm.tiles_n * (TILE_M * C::CTAS) + rank * TILE_M + quarter * 32, m = mq + lane;
             const int n0 = static_cast<int>(tile % prm.tiles_n) * BN + col0;
