@@ -515,7 +515,7 @@ size_t ip_kv4_attention_workspace_bytes(int B, int T, int H, int Hkv, int max_le
  * max_len: host upper bound of the lengths, in [0, IP_KV4_MAX_LEN]; it sizes the split of
  * the keys, and the result depends on it, and on the lengths of the call's other sequences,
  * in the last bits only (equal calls give equal bits).
- * 1 <= T <= IP_MAX_T; scale in (0, 1e30).  Workspace: at least the size above, 256-byte
+ * 1 <= T <= IP_MAX_T, B Hkv ceil(T H / Hkv / 8) within 31 bits; scale in (0, 1e30).  Workspace: at least the size above, 256-byte
  * aligned; calls that share one must not overlap on the GPU. */
 int ip_kv4_attention(const void *q, int dtype, const long long *q_strides, const int32_t *lengths,
                      const int32_t *count, int causal, float scale, int B, int T, int H, int Hkv, int dh,

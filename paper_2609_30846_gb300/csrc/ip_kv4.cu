@@ -73,8 +73,9 @@ int launch_read(const ipv::RowParams &prm, long long rows, cudaStream_t st) {
 // shares, or a CTA per item where an item is short, so that the second launch and the search
 // for the share would cost more than they give (us, CTA per item / shares; 1 sequence, 8 heads:
 // 384 tokens 6.4 / 8.3, 768 8.8 / 8.5, 2048 17 / 9.1; 64 sequences: 384 16 / 20, 768 27 / 29,
-// 2048 52 / 49), or where there are too many row tiles to sum up.  The plan depends on the
-// call's sizes alone.
+// 2048 52 / 49), or where there are too many row tiles or units to sum up.  The plan depends on
+// the call's sizes alone.  SMS is the whole GPU's, whatever part of it a process has: on fewer SMs the
+// CTAs take turns, none waits for another.
 constexpr int WHOLE_UNITS = 5;
 constexpr long long SMS = 152;
 struct Plan {
@@ -85,14 +86,13 @@ struct Plan {
 };
 bool plan_of(int B, int T, int H, int Hkv, int max_len, Plan *p) {
     const long long rows = static_cast<long long>(H / Hkv) * T;
-    if (rows > (1ll << 24)) return false;
     p->nt = rows > 8 ? 2 : 1;
     p->tiles = static_cast<int>((rows + 8 * p->nt - 1) / (8 * p->nt));
     const long long tiles = static_cast<long long>(B) * p->tiles, items = tiles * Hkv;
     const long long units = max_len < ipv::UNIT ? 1 : (max_len + ipv::UNIT - 1ll) / ipv::UNIT;
+    if (items > 0x7fffffffll) return false;      // a grid's width
     // sums of units stay within 31 bits, rounded up to whole shares too
-    if (items > 0x7fffffffll || items * (units + ipv::OVER) > 0x7ffff000ll) return false;
-    p->split = tiles <= ipv::MAX_SCAN && units > WHOLE_UNITS;
+    p->split = tiles <= ipv::MAX_SCAN && units > WHOLE_UNITS && items * (units + ipv::OVER) <= 0x7ffff000ll;
     p->ctas = items;
     p->open_bytes = 0;
     p->bytes = 256;
