@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import operator
+import sys
 import threading
 import warnings
 from dataclasses import dataclass
@@ -200,11 +201,8 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         lib.ip_probe_int8_mma.restype = ctypes.c_longlong
         lib.ip_probe_int8_mix.argtypes = [I, I, I, P, P]
         lib.ip_probe_int8_mix.restype = ctypes.c_longlong
-        try:
-            _short = _bind_short(lib)
-        except Exception as exc:  # noqa: BLE001 - reported with context
-            warnings.warn(f"cannot load the native short forms: {exc}; the calls take their general forms",
-                          RuntimeWarning, stacklevel=2)
+        # a process that has not imported torch has no use for them yet
+        _short = _bound_short(lib) if "torch" in sys.modules else _Pending(lib)
         _lib = lib
         return lib
 
@@ -732,6 +730,31 @@ def _bind_short(lib):
     mod.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
         lib.ip_quantize_rows_i8, lib.ip_linear_scaled_i8, lib.ip_kv4_append, lib.ip_kv4_read, lib.ip_kv4_attention)))
     return mod
+
+
+def _bound_short(lib):
+    try:
+        return _bind_short(lib)
+    except Exception as exc:  # noqa: BLE001 - reported with context
+        warnings.warn(f"cannot load the native short forms: {exc}; the calls take their general forms",
+                      RuntimeWarning, stacklevel=3)
+        return _Unbound
+
+
+class _Pending:
+    """Stands for the short forms from the library's loading to the first call that may take them:
+    they need torch, which the calls without tensors do not."""
+
+    def __init__(self, lib):
+        self._lib, self._forms = lib, None
+
+    def __getattr__(self, name):
+        global _short
+        if self._forms is None:
+            self._forms = _bound_short(self._lib)
+            if _short is self:
+                _short = self._forms
+        return getattr(self._forms, name)
 
 
 def _dtype_code(dtype, name="dtype"):
