@@ -511,7 +511,8 @@ size_t ip_kv4_attention_workspace_bytes(int B, int T, int H, int Hkv, int max_le
  * t >= count[b], are written as 0; a token that a query does not see has no effect on its
  * row, whatever it holds.  Scores, softmax and sums are in f32; the probabilities (1 for the
  * largest) times the V scales enter the output product as fp16: relative 2^-11, or
- * absolute 2^-34 of the largest V scale that the query sees, where that is more.
+ * absolute 2^-34 of the largest V scale that the query sees, where that is more.  This adds
+ * to the rounding of the output: up to a third for IP_F16, nothing to speak of for IP_BF16.
  * max_len: host upper bound of the lengths, in [0, IP_KV4_MAX_LEN]; it sizes the split of
  * the keys, and the result depends on it, and on the lengths of the call's other sequences,
  * in the last bits only (equal calls give equal bits).

@@ -1036,7 +1036,8 @@ def kv4_attention(q, lengths, page_table, cache, *, count=None, causal: bool = T
     with scale 1/sqrt(128) unless given.  lengths (int32 [B]): cached tokens, with this
     call's own; count (int32 [B], None: T): query tokens, which causal makes the last
     ones of the sequence; causal=False lets every query see all cached tokens.  A query that
-    sees none, and rows past count, give 0.  max_len: a host bound of lengths (default: what
+    sees none, and rows past count, give 0.  In float32, but for the weights of the output
+    product, which are rounded to float16.  max_len: a host bound of lengths (default: what
     the table can hold); a close one splits the work better.  Returns [B, T, H, 128] of
     q's type.  workspace: a zero-filled uint8 tensor of kv4_attention_workspace_bytes(B, T,
     H, Hkv, max_len).  Asynchronous on `stream`."""

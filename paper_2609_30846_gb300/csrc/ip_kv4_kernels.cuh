@@ -255,7 +255,7 @@ __global__ void __launch_bounds__(ROW_THREADS) kv4_read_kernel(const RowParams p
 // query rows as its 8 columns: with 8 rows the MMA's half-empty other form would cost
 // as much as the codes' conversion.
 //
-// What bounds it (64 sequences of 4096 tokens, 8 heads, one row each): 74 us for 302 MB, 4.1
+// What bounds it (64 sequences of 4096 tokens, 8 heads, one row each): 75 us for 302 MB, 4.0
 // TB/s; the copies alone take 53 us, copies and scores 55 us.  An instruction that turns
 // codes into fragments works on two codes a lane, which makes some 340 instructions for 16
 // tokens (171 on the integer pipe, which would take 85 cycles at full rate) where the bytes
@@ -272,8 +272,11 @@ __global__ void __launch_bounds__(ROW_THREADS) kv4_read_kernel(const RowParams p
 //
 // Output: p times the V scale, relative to the running largest exponent of the V scales that
 // the row sees and times 2^HEAD, rounds to fp16 (half a step 2^-11; terms below 2^-23 of the
-// largest fade out gradually): the codes enter exactly as u - 8, and the sums are f32.  The
-// rounding is below that of a bf16 output and no worse than that of an fp16 one.
+// largest fade out gradually): the codes enter exactly as u - 8, and the sums are f32.  A choice
+// for the MMA's rate, since a second piece of p s would double the output product.  It is not
+// free: the error of fp16 outputs against 64 bits is 1.15 to 1.3 times that of f32 arithmetic
+// rounded once (33 queries over 1500 tokens 2.4e-4 for 2.1e-4, one over 375 2.6e-4 for 2.0e-4);
+// that of bf16 outputs is their own rounding (1.7e-3 either way).
 //
 // Split: the keys of all items in a row, cut into units of 128, are dealt in equal shares to
 // one wave of CTAs, whatever the lengths: each CTA sums up the lengths to find where its
@@ -638,7 +641,8 @@ __global__ void __launch_bounds__(ATT_THREADS, NT == 1 ? CTAS_8 : CTAS_16) kv4_a
         const int tok = g8 & 1 ? 4 + ((g8 >> 1) ^ 1) : g8 >> 1, odd4 = 4 + (t4 ^ 1);
         const uint8_t *at_k = my_ring + tok * 64 + t4 * 16, *at_s = my_ring + tok * 8;
         const uint8_t *at_v = my_ring + t4 * 64 + g8 * 8, *at_vo = my_ring + odd4 * 64 + g8 * 8;
-        // m: the reference of the row's exponentials, mr: in units of log2.  It is raised to the
+        // m: the reference of the row's exponentials (-inf: no key yet, and then none in the later
+        // batches either, a row sees the first keys), mr: in units of log2.  It is raised to the
         // maximum only when a score exceeds it by more than SLACK there (lift: the score that does):
         // the probabilities reach 2^SLACK at most, and most batches skip the rescaling.
         // far: a row's reference is 2^20 or more, where the rounding of mr begins to show in the

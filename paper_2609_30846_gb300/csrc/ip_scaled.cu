@@ -181,7 +181,8 @@ int run_tc(ips::ScaledParams prm, int nsm, cudaStream_t st) {
 }
 
 // The form that a launch is expected to take the least time in, ns.  Fitted on GB300 to sweeps of
-// M = 16 .. 4096 tokens over N = 512 .. 16384 at K = 1024 and 4096, every form timed at each point:
+// M = 16 .. 4096 tokens over N = 512 .. 16384 at K = 1024 and 4096, every form timed at each point
+// (beyond these K and N it is extrapolated, but for the vector kernel's rate, taken at K = 9000 too):
 // the vector kernel reads the weights once per eight tokens; the tensor-core forms take so
 // long per fp16 stage (64 of K) of a round of tiles over the SMs.  (us, vector / 32 / 128 / pairs:
 // 32 x 1024 -> 512 3.0 / 7.0 / 7.8 / 12.0, 128 x 1024 -> 1024 12.5 / 7.1 / 8.3 / 12.9, 32 x 4096 -> 4096

@@ -24,8 +24,9 @@ using namespace ipr;
 // to even, for the row's largest magnitude amax.  The quotient is formed as x times
 // the reciprocal rounded up (error below 127 2^-23 < 2^-16) and rounded by adding 1.5 2^23.
 // That is right except near half integers n + 1/2, where 254 x = (2n + 1) amax is close:
-//   16-bit x: two integers of eleven bits at most, so what is not equal is 2^-12 off and
-//     safe.  Equality needs 2n + 1 = 127, x = amax / 2 (common: one element a row of 1024
+//   16-bit x: with significands X of x and A of amax, integers below 2^11 (bf16: 2^8), a quotient
+//     y = 127 x / amax that is no half integer is at least y / (254 X) from one, y 2^-19 (bf16
+//     y 2^-16), and the error is below y 2^-23: safe.  Equality needs 2n + 1 = 127, x = amax / 2 (common: one element a row of 1024
 //     bf16 values; the reciprocal rounded up takes it to the even 64), or an amax whose
 //     significand 127 divides.  In bf16 that is 254 alone, where 127 / amax is a power of
 //     two and all quotients are exact; fp16 rows with such an amax (8 of 1024) look at
@@ -328,11 +329,11 @@ __global__ void __launch_bounds__(VEC_THREADS) scaled_vec_kernel(const ScaledPar
 // where K is short.  So the CTAs of a pair share their channels: each converts its 128
 // tokens and half of the 256 channels for an MMA of 256 x 256 (cta_group::2), a third
 // less for the same products (a CTA alone on 128 x 256: 80 % of that pipe, the tensor pipe
-// at 36 %).  12000 x 1024 -> 4096 96 us (without the epilogue's arithmetic and stores some
-// 20 less, without the conversion as well some 35), 12000 x 4096 -> 1024 98 us (188 pair
+// at 36 %).  12000 x 1024 -> 4096 97 us (without the epilogue's arithmetic and stores some
+// 20 less, without the conversion as well some 35), 12000 x 4096 -> 1024 100 us (188 pair
 // tiles for 76 pairs: the third round is half empty; its tiles cut in halves of 128
-// channels gave 5 us there and cost up to 2 elsewhere), 4096 x 8192 -> 8192 423 us,
-// 1300 TFLOP/s.
+// channels gave 5 us there and cost up to 2 elsewhere), 4096 x 8192 -> 8192 431 us,
+// 1275 TFLOP/s.
 
 constexpr int TILE_M = 128;
 constexpr int BK = 64;              // K elements of a stage (rows of 64 bytes raw, of 128 in fp16)
