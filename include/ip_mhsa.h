@@ -450,6 +450,63 @@ int ip_linear_scaled_i8(const int8_t *x, long long ldx, const float *sx, const i
                         int K, int N, void *y, long long ldy, int dtype, void *workspace,
                         size_t workspace_bytes, ip_stream_t stream);
 
+/* ---- rows in 4-bit floating point, and the norm that writes quantised rows ----
+ *
+ * A 4-bit row of d elements: e2m1 codes (sign bit, then the magnitudes 0 .5 1 1.5 2 3 4 6), two
+ * in a byte, the first in the low nibble (behind an odd d the last high nibble is 0); each block
+ * of 16 consecutive elements has an e4m3 scale s and the row an f32 scale r: an element is code s r.
+ * From real values with amax = max |x| over the row:
+ *   r = 2^e, the least power of two with amax <= 2688 r and e >= -126 (2688 = 6 x 448),
+ *   s = max |x| over the block / (6 r), rounded to e4m3,  code = x / (s r), rounded to e2m1
+ *   (0 where s is 0), both to nearest, ties to even, exactly as stated, whatever the type; a code
+ *   keeps the element's sign, zeros too.
+ * amax = 0 gives r = 0, s = 0 and codes 0; a row that holds a NaN or an infinity gets r = NaN, the
+ * rest 0 (a product with it is NaN).
+ * Memory: rows of ldq >= ceil(d / 2) bytes, q 16-byte aligned and ldq a multiple of 16; blocks:
+ * ip_fp4_block_bytes(rows, d) bytes, 16-byte aligned, 512 for 128 rows x 64 elements in row-major
+ * order [ceil(rows / 128)][ceil(d / 64)]; in them the scale of row m and block b (element / 16) is byte
+ * 16 (m mod 32) + 4 ((m mod 128) / 32) + (b mod 4).  Blocks behind column d have the scale 0;
+ * scales of rows behind the last are neither written nor used.  scale: f32 [rows].
+ * Any r is fine in what the calls read, and any s but NaN. */
+
+/* Bytes of the block scales, 0 for an invalid shape (and for no rows). */
+size_t ip_fp4_block_bytes(long long rows, int d);
+
+/* Rows of real values to 4-bit rows.  x: device, dtype IP_F32, IP_F16 or IP_BF16, rows of ldx >= d
+ * elements; q, blocks, scale as above (bytes of q behind column d are left as they were).  d in
+ * [1, IP_LINEAR_MAX_K].  rows == 0 returns IP_OK without touching any pointer.  Asynchronous on
+ * `stream`.  The same call quantises weights by output channel.  Returns IP_OK or IP_ERR_*. */
+int ip_quantize_fp4(const void *x, int dtype, long long rows, int d, long long ldx, uint8_t *q,
+                    long long ldq, uint8_t *blocks, float *scale, ip_stream_t stream);
+
+/* Root-mean-square norm with the residual's addition, its rows quantised:
+ *   h = x + residual, rounded to the type (residual NULL: h = x), written to `sum`;
+ *   z = h weight, rounded to f32;  rstd = 1 / sqrt(mean(h^2) + eps) in f32;
+ *   the row z rstd as int8 (ip_quantize_rows_i8) or as a 4-bit row.
+ * rstd scales the whole row, so it enters the row's scale alone: the codes (and block scales) are
+ * those of z, exactly, and the int8 scale is max |z| rstd / 127, a 4-bit row's r rstd, in f32.
+ * x, residual, sum: device, dtype, rows of ldx, ldres, ldsum >= d elements; weight: device, dtype
+ * [d]; eps in [0, 1e30).  sum may be x or residual itself (with its stride); otherwise the
+ * outputs are apart from the inputs.  sum is not used without a residual.  A row of z that holds
+ * a NaN or an infinity gets the scale NaN and codes 0.  d in [1, IP_LINEAR_MAX_K].  rows == 0
+ * returns IP_OK without touching any pointer.  Asynchronous on `stream`.  Returns IP_OK or IP_ERR_*. */
+int ip_rmsnorm_i8(const void *x, long long ldx, const void *residual, long long ldres,
+                  const void *weight, float eps, int dtype, long long rows, int d, void *sum,
+                  long long ldsum, int8_t *q, long long ldq, float *scale, ip_stream_t stream);
+int ip_rmsnorm_fp4(const void *x, long long ldx, const void *residual, long long ldres,
+                   const void *weight, float eps, int dtype, long long rows, int d, void *sum,
+                   long long ldsum, uint8_t *q, long long ldq, uint8_t *blocks, float *scale,
+                   ip_stream_t stream);
+
+/* The values of int8 rows (code x scale) and of 4-bit rows (code x s, x r), in f32, rounded once
+ * to y's type: device, dtype, rows of ldy >= d elements (those behind column d are left as they
+ * were).  rows == 0 returns IP_OK without touching any pointer.  Asynchronous on `stream`. */
+int ip_dequantize_i8(const int8_t *q, long long ldq, const float *scale, long long rows, int d,
+                     void *y, long long ldy, int dtype, ip_stream_t stream);
+int ip_dequantize_fp4(const uint8_t *q, long long ldq, const uint8_t *blocks, const float *scale,
+                      long long rows, int d, void *y, long long ldy, int dtype,
+                      ip_stream_t stream);
+
 /* ---- key/value cache in 4 bits ------------------------------------------
  *
  * Keys and values of a sequence's tokens (a decoder's own, or the encoder's frames for

@@ -40,6 +40,8 @@ EXPORTS = (
     "ip_relpos_layer_constants", "ip_linear_constants", "ip_relpos_mhsa_noalloc_status",
     "ip_quantize_rows_i8", "ip_linear_scaled_i8", "ip_kv4_page_bytes", "ip_kv4_append", "ip_kv4_read",
     "ip_kv4_attention_workspace_bytes", "ip_kv4_attention",
+    "ip_fp4_block_bytes", "ip_quantize_fp4", "ip_rmsnorm_i8", "ip_rmsnorm_fp4", "ip_dequantize_i8",
+    "ip_dequantize_fp4",
 )
 
 ROWS = 0    # IP_LAYOUT_ROWS:  [B][T][C]
@@ -193,7 +195,13 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
                 ("ip_kv4_append", [P, P, N, P, P, P, P, N, N, N, N, P, N, P, N, N, P, S, P], I),
                 ("ip_kv4_read", [P, N, N, P, N, P, P, N, N, N, N, P, P, N, P, S, P], I),
                 ("ip_kv4_attention_workspace_bytes", [N] * 5, S),
-                ("ip_kv4_attention", [P, N, P, P, P, N, F, N, N, N, N, N, N, P, N, P, N, N, P, P, S, P], I)):
+                ("ip_kv4_attention", [P, N, P, P, P, N, F, N, N, N, N, N, N, P, N, P, N, N, P, P, S, P], I),
+                ("ip_fp4_block_bytes", [LL, N], S),
+                ("ip_quantize_fp4", [P, N, LL, N, LL, P, LL, P, P, P], I),
+                ("ip_rmsnorm_i8", [P, LL, P, LL, P, F, N, LL, N, P, LL, P, LL, P, P], I),
+                ("ip_rmsnorm_fp4", [P, LL, P, LL, P, F, N, LL, N, P, LL, P, LL, P, P, P], I),
+                ("ip_dequantize_i8", [P, LL, P, LL, N, P, LL, N, P], I),
+                ("ip_dequantize_fp4", [P, LL, P, P, LL, N, P, LL, N, P], I)):
             fn = getattr(lib, name, None)      # a library built before these calls does the others
             if fn is not None:
                 fn.argtypes, fn.restype = args, result
@@ -914,6 +922,178 @@ def linear_scaled_i8(x, sx, w, sw, bias=None, *, act: int = ACT_NONE, dtype=None
     return out
 
 
+# ------------------------------------------------------- 4-bit rows, norm
+
+def fp4_block_shape(rows: int, d: int) -> tuple[int, int, int]:
+    """Shape of the block scales of `rows` 4-bit rows of d elements: uint8 [ceil(rows / 128),
+    ceil(d / 64), 512], the scale of row m and block b (16 elements) at [m // 128, b // 4,
+    16 (m % 32) + 4 (m % 128 // 32) + b % 4]."""
+    return -(-rows // 128), -(-d // 64), 512
+
+
+def _fp4_out(q, blocks, scale, lead, rows, d, dev):
+    """New or checked (q, its row stride, blocks, scale) of 4-bit rows."""
+    import torch
+    n = -(-d // 2)
+    if q is None:
+        ldq = -(-n // 16) * 16
+        q = torch.empty((*lead, ldq), dtype=torch.uint8, device=dev)
+        q = q if ldq == n else q[..., :n]
+    else:
+        ldq = _as_rows(_need(q, "q", torch.uint8, (*lead, n), dev), "q")[2]
+    if blocks is None:
+        blocks = torch.empty(fp4_block_shape(rows, d), dtype=torch.uint8, device=dev)
+    _dense(blocks, "blocks", torch.uint8, fp4_block_shape(rows, d), dev)
+    if scale is None:
+        scale = torch.empty(lead, dtype=torch.float32, device=dev)
+    _dense(scale, "scale", torch.float32, lead, dev)
+    return q, ldq, blocks, scale
+
+
+def quantize_fp4(x, *, q=None, blocks=None, scale=None, stream=None):
+    """Rows (the last axis, d elements) of a float32, float16 or bfloat16 CUDA tensor to 4-bit
+    floating point: e2m1 codes, an e4m3 scale s for each 16 of them, a float32 scale r a row, an
+    element being code s r.  r is the least power of two with amax <= 2688 r, s and the codes
+    are rounded to nearest, ties to even, exactly.  A row of zeros gives scale 0; one with a
+    NaN or an infinity the scale NaN and codes 0.  Returns (q, blocks, scale): uint8
+    [..., ceil(d / 2)] (the first code in the low nibble; a new q has rows of a multiple of 16
+    bytes, as linear_fp4 reads them, so it may be a view of them), uint8
+    fp4_block_shape(rows, d) and float32 of x.shape[:-1].  Asynchronous on `stream`
+    (default: torch's current stream)."""
+    code = _dtype_code(_need(x, "x").dtype, "x")
+    rows, d, ldx = _as_rows(x, "x")
+    lib = _lib or load()
+    with _On(x.device, stream) as handle:
+        q, ldq, blocks, scale = _fp4_out(q, blocks, scale, x.shape[:-1], rows, d, x.device)
+        rc = lib.ip_quantize_fp4(x.data_ptr(), code, rows, d, ldx, q.data_ptr(), ldq, blocks.data_ptr(),
+                                 scale.data_ptr(), handle)
+    if rc:
+        _check("ip_quantize_fp4", rc)
+    return q, blocks, scale
+
+
+def _norm_in(x, weight, residual, out):
+    """What the two norms check of their inputs: the type's code, rows, d, the row strides of x,
+    residual and the sum's tensor (None: to be made)."""
+    code = _dtype_code(_need(x, "x").dtype, "x")
+    rows, d, ldx = _as_rows(x, "x")
+    _dense(weight, "weight", x.dtype, (d,), x.device)
+    ldr = lds = 0
+    if residual is not None:
+        ldr = _as_rows(_need(residual, "residual", x.dtype, x.shape, x.device), "residual")[2]
+        lds = d if out is None else _as_rows(_need(out, "out", x.dtype, x.shape, x.device), "out")[2]
+    elif out is not None:
+        raise ValueError("out is the sum with a residual, and there is none")
+    return code, rows, d, ldx, ldr, lds
+
+
+def rmsnorm_i8(x, weight, residual=None, *, eps: float = 1e-5, out=None, q=None, scale=None, stream=None):
+    """Root-mean-square norm over the last axis (d elements) with the residual's addition,
+    its rows in int8: h = x + residual (rounded to x's type), then h weight / sqrt(mean(h^2) + eps)
+    as quantize_rows_i8 rounds rows (the row's factor leaves the codes as they are: they are
+    exactly those of h weight).  x, residual: float32, float16 or bfloat16 [..., d] CUDA
+    tensors; weight: x's type [d].  Returns (q, scale, h): int8 of x's shape (a new q has rows of
+    a multiple of 16 bytes), float32 of x.shape[:-1], and h of x's type, None without a residual.  out:
+    where h goes, which may be x or residual itself.  Asynchronous on `stream`."""
+    import torch
+    code, rows, d, ldx, ldr, lds = _norm_in(x, weight, residual, out)
+    dev, lib = x.device, _lib or load()
+    with _On(dev, stream) as handle:
+        if q is None:
+            ldq = -(-d // 16) * 16
+            q = torch.empty((*x.shape[:-1], ldq), dtype=torch.int8, device=dev)
+            q = q if ldq == d else q[..., :d]
+        else:
+            ldq = _as_rows(_need(q, "q", torch.int8, x.shape, dev), "q")[2]
+        if scale is None:
+            scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev)
+        _dense(scale, "scale", torch.float32, x.shape[:-1], dev)
+        if residual is not None and out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        rc = lib.ip_rmsnorm_i8(x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr,
+                               weight.data_ptr(), eps, code, rows, d, None if out is None else out.data_ptr(), lds,
+                               q.data_ptr(), ldq, scale.data_ptr(), handle)
+    if rc:
+        _check("ip_rmsnorm_i8", rc)
+    return q, scale, out
+
+
+def rmsnorm_fp4(x, weight, residual=None, *, eps: float = 1e-5, out=None, q=None, blocks=None, scale=None,
+                stream=None):
+    """rmsnorm_i8 with 4-bit rows (quantize_fp4): returns (q, blocks, scale, h)."""
+    import torch
+    code, rows, d, ldx, ldr, lds = _norm_in(x, weight, residual, out)
+    dev, lib = x.device, _lib or load()
+    with _On(dev, stream) as handle:
+        q, ldq, blocks, scale = _fp4_out(q, blocks, scale, x.shape[:-1], rows, d, dev)
+        if residual is not None and out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        rc = lib.ip_rmsnorm_fp4(x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr,
+                                weight.data_ptr(), eps, code, rows, d, None if out is None else out.data_ptr(), lds,
+                                q.data_ptr(), ldq, blocks.data_ptr(), scale.data_ptr(), handle)
+    if rc:
+        _check("ip_rmsnorm_fp4", rc)
+    return q, blocks, scale, out
+
+
+def _values_out(out, dtype, shape, dev):
+    """(out or None, its type, its row stride) of a call that writes values of rows."""
+    import torch
+    if out is None:
+        return dtype or torch.bfloat16, shape[-1]
+    dtype = out.dtype if dtype is None else dtype
+    return dtype, _as_rows(_need(out, "out", dtype, shape, dev), "out")[2]
+
+
+def dequantize_i8(q, scale, *, dtype=None, out=None, stream=None):
+    """The values of int8 rows (quantize_rows_i8, rmsnorm_i8): q scale, rounded once to `dtype`
+    (bfloat16 unless out gives it).  q: int8 [..., d], scale: float32 [...], CUDA tensors.
+    Asynchronous on `stream`."""
+    import torch
+    rows, d, ldq = _as_rows(_need(q, "q", torch.int8), "q")
+    ps = _dense(scale, "scale", torch.float32, q.shape[:-1], q.device)
+    dtype, ldy = _values_out(out, dtype, q.shape, q.device)
+    code, lib = _dtype_code(dtype), _lib or load()
+    with _On(q.device, stream) as handle:
+        if out is None:
+            out = torch.empty(q.shape, dtype=dtype, device=q.device)
+        rc = lib.ip_dequantize_i8(q.data_ptr(), ldq, ps, rows, d, out.data_ptr(), ldy, code, handle)
+    if rc:
+        _check("ip_dequantize_i8", rc)
+    return out
+
+
+def _fp4_in(q, blocks, scale, names, d=None):
+    """Checked (rows, d, row stride) of 4-bit rows; d: elements a row (default: two a byte)."""
+    import torch
+    rows, n, ldq = _as_rows(_need(q, names[0], torch.uint8), names[0])
+    d = 2 * n if d is None else d
+    if -(-d // 2) != n:
+        raise ValueError(f"{names[0]}'s rows of {n} bytes do not hold {d} elements")
+    _dense(blocks, names[1], torch.uint8, fp4_block_shape(rows, d), q.device)
+    _dense(scale, names[2], torch.float32, q.shape[:-1], q.device)
+    return rows, d, ldq
+
+
+def dequantize_fp4(q, blocks, scale, d=None, *, dtype=None, out=None, stream=None):
+    """The values of 4-bit rows (quantize_fp4, rmsnorm_fp4), code s r in float32, rounded once to
+    `dtype` (bfloat16 unless out gives it): [..., d], d twice q's bytes unless given.
+    Asynchronous on `stream`."""
+    import torch
+    rows, d, ldq = _fp4_in(q, blocks, scale, ("q", "blocks", "scale"), d)
+    shape = (*q.shape[:-1], d)
+    dtype, ldy = _values_out(out, dtype, shape, q.device)
+    code, lib = _dtype_code(dtype), _lib or load()
+    with _On(q.device, stream) as handle:
+        if out is None:
+            out = torch.empty(shape, dtype=dtype, device=q.device)
+        rc = lib.ip_dequantize_fp4(q.data_ptr(), ldq, blocks.data_ptr(), scale.data_ptr(), rows, d, out.data_ptr(),
+                                   ldy, code, handle)
+    if rc:
+        _check("ip_dequantize_fp4", rc)
+    return out
+
+
 def kv4_page_bytes(page: int, dh: int = IP_DH) -> int:
     """Bytes of one page of one head of a 4-bit cache (144 a token)."""
     n = load().ip_kv4_page_bytes(page, dh)
@@ -1119,4 +1299,5 @@ __all__ = ["build", "load", "relpos_mhsa_i8", "relpos_mhsa_i8_host", "status", "
            "quantize_rows_i8", "linear_scaled_i8", "ACT_NONE", "ACT_SWISH",
            "kv4_page_bytes", "kv4_cache", "kv4_append", "kv4_read", "kv4_attention",
            "kv4_attention_workspace_bytes",
+           "fp4_block_shape", "quantize_fp4", "dequantize_fp4", "dequantize_i8", "rmsnorm_i8", "rmsnorm_fp4",
            "IpError", "LibraryError", "EXPORTS"]
