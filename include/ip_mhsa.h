@@ -507,6 +507,33 @@ int ip_dequantize_fp4(const uint8_t *q, long long ldq, const uint8_t *blocks, co
                       long long rows, int d, void *y, long long ldy, int dtype,
                       ip_stream_t stream);
 
+/* ---- log probabilities ---------------------------------------------------
+ *
+ * Of the distribution softmax(scale x) over each row x of logits, in f32:
+ *   logprob[r] = log p[tokens[r]] (0 for a token below 0, which stands for padding; NaN for one
+ *     past V - 1),
+ *   entropy[r] = -sum p log p (a logit of -inf has p = 0 and no part in it),
+ *   top_token[r][k], top_logprob[r][k]: the `top` tokens of the largest logits, the largest first, of
+ *     equal logits (-0 equals 0) the one of the lowest index first, and their log p.
+ * A row without a distribution (a NaN or +inf among its logits, or nothing but -inf) gives
+ * NaN and top_token -1 (logprob 0 all the same for a token below 0).
+ * logits: device, dtype IP_F32, IP_F16 or IP_BF16, rows of ld >= V elements, any alignment;
+ * tokens: device int32 [rows], or int64 for tokens_i64 = 1, or NULL (logprob is not used then);
+ * scale (1 / temperature) in (0, 1e30); top in [0, min(V, IP_LOGPROBS_MAX_TOP)] (0: top_* are
+ * not used); logprob, entropy: device f32 [rows], top_logprob: f32, top_token: int32 [rows][top].
+ * rows <= IP_LINEAR_MAX_FRAMES, V in [1, IP_LOGPROBS_MAX_V].  Equal calls give equal bits.
+ * workspace: 256-byte aligned, of at least the bytes below (its first 256 as for
+ * ip_linear_i8, the others need no zero fill); calls that share one must not overlap on
+ * the GPU.  rows == 0 returns IP_OK without touching any pointer.  Asynchronous on `stream`.
+ * Returns IP_OK or IP_ERR_*. */
+#define IP_LOGPROBS_MAX_V (1 << 20)
+#define IP_LOGPROBS_MAX_TOP 32
+size_t ip_token_logprobs_workspace_bytes(long long rows, int V, int top);   /* 0: invalid shape */
+int ip_token_logprobs(const void *logits, int dtype, long long rows, int V, long long ld,
+                      const void *tokens, int tokens_i64, float scale, int top, float *logprob,
+                      float *entropy, float *top_logprob, int32_t *top_token, void *workspace,
+                      size_t workspace_bytes, ip_stream_t stream);
+
 /* ---- key/value cache in 4 bits ------------------------------------------
  *
  * Keys and values of a sequence's tokens (a decoder's own, or the encoder's frames for

@@ -41,7 +41,7 @@ EXPORTS = (
     "ip_quantize_rows_i8", "ip_linear_scaled_i8", "ip_kv4_page_bytes", "ip_kv4_append", "ip_kv4_read",
     "ip_kv4_attention_workspace_bytes", "ip_kv4_attention",
     "ip_fp4_block_bytes", "ip_quantize_fp4", "ip_rmsnorm_i8", "ip_rmsnorm_fp4", "ip_dequantize_i8",
-    "ip_dequantize_fp4",
+    "ip_dequantize_fp4", "ip_token_logprobs_workspace_bytes", "ip_token_logprobs",
 )
 
 ROWS = 0    # IP_LAYOUT_ROWS:  [B][T][C]
@@ -201,7 +201,9 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
                 ("ip_rmsnorm_i8", [P, LL, P, LL, P, F, N, LL, N, P, LL, P, LL, P, P], I),
                 ("ip_rmsnorm_fp4", [P, LL, P, LL, P, F, N, LL, N, P, LL, P, LL, P, P, P], I),
                 ("ip_dequantize_i8", [P, LL, P, LL, N, P, LL, N, P], I),
-                ("ip_dequantize_fp4", [P, LL, P, P, LL, N, P, LL, N, P], I)):
+                ("ip_dequantize_fp4", [P, LL, P, P, LL, N, P, LL, N, P], I),
+                ("ip_token_logprobs_workspace_bytes", [LL, N, N], S),
+                ("ip_token_logprobs", [P, N, LL, N, LL, P, N, F, N, P, P, P, P, P, S, P], I)):
             fn = getattr(lib, name, None)      # a library built before these calls does the others
             if fn is not None:
                 fn.argtypes, fn.restype = args, result
@@ -1253,6 +1255,54 @@ def kv4_attention(q, lengths, page_table, cache, *, count=None, causal: bool = T
     return out
 
 
+# ------------------------------------------------------- log probabilities
+
+def token_logprobs_workspace_bytes(rows: int, V: int, top: int = 0) -> int:
+    """Bytes of workspace of token_logprobs for these sizes."""
+    n = load().ip_token_logprobs_workspace_bytes(rows, V, top)
+    if n == 0:
+        raise IpError("ip_token_logprobs_workspace_bytes", -2, "invalid shape")
+    return n
+
+
+def token_logprobs(logits, tokens=None, *, top: int = 0, scale: float = 1.0, out=None, workspace=None, stream=None):
+    """Log probabilities of given tokens, entropy and the best tokens of each row of logits
+    (float32, float16 or bfloat16 [..., V] CUDA tensor), of the distribution softmax(scale logits), in
+    float32.  tokens: int32 or int64 [...], or None; one below 0 (padding) gives 0, one past
+    V - 1 NaN.  top: how many of the best tokens to give, up to 32, the largest logit first, the
+    lowest index first of equal ones.  scale: 1 / temperature.  Returns (logprob, entropy,
+    top_logprob, top_token): float32 [...] (None without tokens), float32 [...], float32 and int32
+    [..., top] (None for top = 0).  A row with a NaN or +inf, or of nothing but -inf, gives NaN and
+    tokens -1.  out: such a tuple, contiguous.  workspace: a uint8 tensor of
+    token_logprobs_workspace_bytes(rows, V, top).  Asynchronous on `stream` (default: torch's
+    current stream)."""
+    import torch
+    code = _dtype_code(_need(logits, "logits").dtype, "logits")
+    rows, V, ld = _as_rows(logits, "logits")
+    dev, lead, wide = logits.device, logits.shape[:-1], 0
+    if tokens is not None:
+        wide = 1 if _need(tokens, "tokens").dtype == torch.int64 else 0
+        _dense(tokens, "tokens", torch.int64 if wide else torch.int32, lead, dev)
+    size = 0 if workspace is not None else token_logprobs_workspace_bytes(rows, V, top)
+    f32, best = torch.float32, (*lead, top)
+    with _On(dev, stream) as handle:
+        if out is None:
+            new = lambda shape, dtype, on: torch.empty(shape, dtype=dtype, device=dev) if on else None
+            out = (new(lead, f32, tokens is not None), new(lead, f32, True), new(best, f32, top > 0),
+                   new(best, torch.int32, top > 0))
+        lp, ent, tlp, ttok = out
+        ptrs = [_dense(t, f"out[{i}]", dtype, shape, dev) if on else None for i, (t, dtype, shape, on) in enumerate((
+            (lp, f32, lead, tokens is not None), (ent, f32, lead, True), (tlp, f32, best, top > 0),
+            (ttok, torch.int32, best, top > 0)))]
+        workspace, ws, wsb = _status_space(workspace, dev, size)
+        rc = (_lib or load()).ip_token_logprobs(
+            logits.data_ptr(), code, rows, V, ld, None if tokens is None else tokens.data_ptr(), wide, scale, top,
+            *ptrs, ws, wsb, handle)
+    if rc:
+        _check("ip_token_logprobs", rc)
+    return out
+
+
 def relpos_mhsa_i8_host(q, k, v, p, u, v_bias, consts: LayerConstants, lengths, out, arena,
                         stream=None, wait: bool = True):
     """Whole layer from host buffers (torch CPU tensors, ideally pinned):
@@ -1300,4 +1350,5 @@ __all__ = ["build", "load", "relpos_mhsa_i8", "relpos_mhsa_i8_host", "status", "
            "kv4_page_bytes", "kv4_cache", "kv4_append", "kv4_read", "kv4_attention",
            "kv4_attention_workspace_bytes",
            "fp4_block_shape", "quantize_fp4", "dequantize_fp4", "dequantize_i8", "rmsnorm_i8", "rmsnorm_fp4",
+           "token_logprobs", "token_logprobs_workspace_bytes",
            "IpError", "LibraryError", "EXPORTS"]

@@ -1,0 +1,316 @@
+// Device code of the log probabilities of given tokens for sm_103a, with the entropy and the best
+// tokens of each row of logits.
+#pragma once
+
+#include <math.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "ip_ptx.cuh"
+#include "ip_real.cuh"
+
+namespace ipl {
+
+using namespace ipk;
+using namespace ipr;
+
+// With a_i = scale x_i, m their maximum, s = sum exp(a_i - m), u = sum (a_i - m) exp(a_i - m):
+//   log p_t = (a_t - m) - log s,   entropy = log s - u / s,
+// both terms of the entropy >= 0, so that nothing cancels.  An a of -inf has no weight.
+//
+// A row (or one of its parts) is held in registers: one pass over memory, the maximum before the
+// exponentials, so one of them an element.  A short row is a warp's, a longer one a CTA's, and
+// what a CTA's registers do not hold is cut into parts, each a CTA's, that a second kernel joins in
+// a fixed order.
+//
+// The `top` best: a token's key is its logit's bits in the order of the numbers (-0 as 0), then its
+// index from behind, so that keys are different and among equal logits the lowest index is the
+// larger key.  A lower bound of the key wanted last: of a warp's 32 lane maxima the one of rank `top`
+// (at least `top` elements reach it), the largest of these over the warps.  The elements that
+// reach it (few more than `top` where logits are not sorted) go to shared memory, and each one's rank is
+// the number of larger keys there.  Where more reach it than there is room for, the best are found one
+// after the other.
+
+constexpr int MAX_TOP = 32;
+constexpr int WARP_CANDS = 256, CTA_CANDS = 512;
+
+typedef unsigned long long Key;
+
+struct LogprobParams {
+    const void *x;
+    long long rows, ld;
+    int V, top;
+    int parts, per;                       // parts a row, elements a part
+    float scale;                          // of the logits
+    const void *tokens;
+    int tokens64;
+    float *logprob, *entropy, *top_logprob;
+    int *top_token;
+    float *sums;                          // [rows][parts][4] of the parts: m, s, u, not a distribution
+    Key *keys;                            // [rows][parts][top]
+};
+
+__device__ __forceinline__ uint32_t order_of(float x) {
+    const uint32_t b = __float_as_uint(x + 0.0f);
+    return b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t k) {
+    return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+}
+__device__ __forceinline__ Key key_of(uint32_t order, int i) {
+    return static_cast<Key>(order) << 32 | static_cast<uint32_t>(~i);
+}
+__device__ __forceinline__ int index_of(Key k) { return static_cast<int>(~static_cast<uint32_t>(k)); }
+
+// The group of threads that holds a row: a warp or a CTA of 256.
+template <int TPR>
+struct Group {
+    static constexpr int WARPS = TPR / 32;
+    static __device__ __forceinline__ void sync() {
+        if (WARPS == 1) __syncwarp();
+        else __syncthreads();
+    }
+    static __device__ __forceinline__ float sum(float v, float *red) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        if (WARPS > 1) {
+            __syncthreads();
+            if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+            __syncthreads();
+            v = red[0];
+#pragma unroll
+            for (int i = 1; i < WARPS; ++i) v += red[i];
+        }
+        return v;
+    }
+    static __device__ __forceinline__ uint32_t max_u32(uint32_t v, uint32_t *red) {
+        v = __reduce_max_sync(0xffffffffu, v);
+        if (WARPS > 1) {
+            __syncthreads();
+            if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+            __syncthreads();
+            v = red[0];
+#pragma unroll
+            for (int i = 1; i < WARPS; ++i) v = max(v, red[i]);
+        }
+        return v;
+    }
+};
+
+__device__ __forceinline__ Key warp_max_key(Key v) {
+    const uint32_t hi = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(v >> 32));
+    const uint32_t lo = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(v >> 32) == hi ? static_cast<uint32_t>(v) : 0u);
+    return static_cast<Key>(hi) << 32 | lo;
+}
+
+// The `top` largest of a group's keys, in order, to put(rank, key).  each(f): f(key) for all of a
+// thread's keys (0: none); lane_top: the largest of their upper halves.
+template <int TPR, int CANDS, typename Each, typename Put>
+__device__ __forceinline__ void best(int top, uint32_t lane_top, Each each, Put put, Key *cand, uint32_t *red) {
+    using G = Group<TPR>;
+    const int lane = threadIdx.x & 31, t = threadIdx.x % TPR;
+    int rank = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        const uint32_t o = __shfl_sync(0xffffffffu, lane_top, i);
+        rank += o > lane_top || (o == lane_top && i < lane);
+    }
+    const uint32_t bound = G::max_u32(rank == top - 1 ? lane_top : 0u, red);
+    uint32_t *count = reinterpret_cast<uint32_t *>(cand);      // the keys from cand[1] on
+    G::sync();
+    if (t == 0) *count = 0;
+    G::sync();
+    if (lane_top >= bound)
+        each([&](Key k) {
+            if (k != 0 && static_cast<uint32_t>(k >> 32) >= bound) {
+                const uint32_t p = atomicAdd(count, 1u);
+                if (p < CANDS) cand[1 + p] = k;
+            }
+        });
+    G::sync();
+    const uint32_t found = *count;
+    if (found <= CANDS) {
+        for (uint32_t p = t; p < found; p += TPR) {
+            const Key k = cand[1 + p];
+            int r = 0;
+            for (uint32_t j = 0; j < found; ++j) r += cand[1 + j] > k;
+            if (r < top) put(r, k);
+        }
+        for (int r = static_cast<int>(found) + t; r < top; r += TPR) put(r, Key(0));
+    } else {
+        Key last = ~Key(0);
+        for (int r = 0; r < top; ++r) {
+            Key k = 0;
+            each([&](Key o) { k = o < last && o > k ? o : k; });
+            k = warp_max_key(k);
+            if (G::WARPS > 1) {
+                __syncthreads();
+                if (lane == 0) cand[threadIdx.x >> 5] = k;
+                __syncthreads();
+                for (int i = 0; i < G::WARPS; ++i) k = cand[i] > k ? cand[i] : k;
+            }
+            if (t == 0) put(r, k);
+            last = k;
+        }
+    }
+}
+
+// Writes a row's results: write(...) by one thread, put(rank, key) by any.  s and u in units of log2.
+template <typename T>
+struct RowOut {
+    const LogprobParams &prm;
+    long long row;
+    float m, ls;
+    bool none;          // no distribution: a NaN or +inf among the logits, or nothing but -inf
+
+    __device__ __forceinline__ RowOut(const LogprobParams &p, long long r, float m_, float s)
+        : prm(p), row(r), m(m_), ls(logf(s)), none(!(m_ > -INFINITY && m_ < INFINITY) || s != s) {}
+    __device__ __forceinline__ float nan() const { return __uint_as_float(0x7fc00000u); }
+    __device__ __forceinline__ float logp(float x) const { return none ? nan() : __fmaf_rn(x - m, prm.scale, -ls); }
+    __device__ __forceinline__ void write(float s, float u) const {
+        prm.entropy[row] = none ? nan() : ls - 0.693147181f * (u / s);
+        if (!prm.tokens) return;
+        const long long tok = prm.tokens64 ? static_cast<const long long *>(prm.tokens)[row]
+                                           : static_cast<long long>(static_cast<const int *>(prm.tokens)[row]);
+        float lp = tok < 0 ? 0.0f : nan();
+        if (tok >= 0 && tok < prm.V) lp = logp(to_f32(static_cast<const T *>(prm.x)[row * prm.ld + tok]));
+        prm.logprob[row] = lp;
+    }
+    __device__ __forceinline__ void put(int r, Key k) const {
+        prm.top_logprob[row * prm.top + r] = logp(value_of(static_cast<uint32_t>(k >> 32)));
+        prm.top_token[row * prm.top + r] = none ? -1 : index_of(k);
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ constexpr uint32_t neg_inf() {
+    return sizeof(T) == 4 ? 0xff800000u : (std::is_same<T, __half>::value ? 0xfc00fc00u : 0xff80ff80u);
+}
+
+// TPR threads (32: four rows a CTA, or 256) hold a row, or a part of one (PART, TPR = 256), in U units
+// of eight elements a thread, the first of them `shift` elements before the row, on 16 bytes.
+template <typename T, int TPR, int U, bool PART>
+__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR) logprob_kernel(const LogprobParams prm) {
+    using G = Group<TPR>;
+    constexpr int RPC = TPR == 32 ? 4 : 1, CANDS = TPR == 32 ? WARP_CANDS : CTA_CANDS;
+    __shared__ Key cands[RPC][CANDS + 1];
+    __shared__ uint32_t red[8];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+    const long long row = static_cast<long long>(blockIdx.x) * RPC + sub;
+    if (row >= prm.rows) return;      // whole warps (TPR = 32), else none
+    const int first = PART ? static_cast<int>(blockIdx.y) * prm.per : 0;
+    const int n = PART ? min(prm.per, prm.V - first) : prm.V;
+    const T *x = static_cast<const T *>(prm.x) + row * prm.ld + first;
+    const int shift = static_cast<int>((reinterpret_cast<uintptr_t>(x) & 15) / sizeof(T));
+    Raw8<T> v[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const int c = (i * TPR + t) * 8 - shift;
+#pragma unroll
+        for (int j = 0; j < Raw8<T>::WORDS; ++j) v[i].w[j] = neg_inf<T>();
+        if (c >= 0 && c + 8 <= n) {
+            v[i].template load<true>(x + c, 8);
+        } else if (c + 8 > 0 && c < n) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (c + j >= 0 && c + j < n) {
+                    if constexpr (sizeof(T) == 4) {
+                        v[i].w[j] = reinterpret_cast<const uint32_t *>(x)[c + j];
+                    } else {
+                        const uint32_t b = reinterpret_cast<const uint16_t *>(x)[c + j];
+                        v[i].w[j >> 1] = j & 1 ? (v[i].w[j >> 1] & 0xffffu) | (b << 16) : (v[i].w[j >> 1] & 0xffff0000u) | b;
+                    }
+                }
+        }
+    }
+    float most = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) most = fmaxf(most, v[i].at(j));
+    const float m = value_of(G::max_u32(order_of(most), red));
+    // nothing but -inf (and NaN): weights of 0, or NaN
+    const float from = m == -INFINITY ? 0.0f : m, c = prm.scale * 1.44269504f;
+    float s = 0.0f, u = 0.0f;
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float p = (v[i].at(j) - from) * c;
+            float e;
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(p));
+            s += e;
+            u = __fmaf_rn(e, fmaxf(p, -1e30f), u);
+        }
+    s = G::sum(s, reinterpret_cast<float *>(red));
+    u = G::sum(u, reinterpret_cast<float *>(red));
+    auto each = [&](auto f) {
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int k = (i * TPR + t) * 8 - shift + j;
+                f(static_cast<uint32_t>(k) < static_cast<uint32_t>(n) ? key_of(order_of(v[i].at(j)), first + k) : Key(0));
+            }
+    };
+    // a thread without elements has nothing to offer (one whose elements are all -inf does)
+    const uint32_t lane_top = t * 8 - shift < n ? order_of(most) : 0u;
+    if (PART) {
+        const long long at = row * prm.parts + blockIdx.y;
+        if (t == 0) *reinterpret_cast<float4 *>(prm.sums + 4 * at) = make_float4(m, s, u, 0.0f);
+        if (prm.top > 0)
+            best<TPR, CANDS>(prm.top, lane_top, each, [&](int r, Key k) { prm.keys[at * prm.top + r] = k; }, cands[sub], red);
+    } else {
+        const RowOut<T> out(prm, row, m, s);
+        if (t == 0) out.write(s, u);
+        if (prm.top > 0) best<TPR, CANDS>(prm.top, lane_top, each, [&](int r, Key k) { out.put(r, k); }, cands[sub], red);
+    }
+}
+
+// Joins a row's parts, a CTA a row.
+template <typename T>
+__global__ void __launch_bounds__(256) logprob_join_kernel(const LogprobParams prm) {
+    using G = Group<256>;
+    __shared__ Key cands[CTA_CANDS + 1];
+    __shared__ uint32_t red[8];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int t = threadIdx.x;
+    const long long row = blockIdx.x;
+    const float4 *parts = reinterpret_cast<const float4 *>(prm.sums) + row * prm.parts;
+    float most = -INFINITY;
+    for (int i = t; i < prm.parts; i += 256) most = fmaxf(most, parts[i].x);
+    const float m = value_of(G::max_u32(order_of(most), red)), c = prm.scale * 1.44269504f;
+    float s = 0.0f, u = 0.0f;
+    for (int i = t; i < prm.parts; i += 256) {
+        const float4 p = parts[i];
+        if (p.x == -INFINITY) {
+            s += p.y;      // 0, or NaN
+            continue;
+        }
+        const float d = (p.x - m) * c;
+        float e;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(d));
+        s = __fmaf_rn(p.y, e, s);
+        u = __fmaf_rn(__fmaf_rn(p.y, fmaxf(d, -1e30f), p.z), e, u);
+    }
+    s = G::sum(s, reinterpret_cast<float *>(red));
+    u = G::sum(u, reinterpret_cast<float *>(red));
+    const RowOut<T> out(prm, row, m, s);
+    if (t == 0) out.write(s, u);
+    if (prm.top > 0) {
+        const Key *keys = prm.keys + row * prm.parts * prm.top;
+        const int n = prm.parts * prm.top;
+        uint32_t lane_top = 0;
+        for (int i = t; i < n; i += 256) lane_top = max(lane_top, static_cast<uint32_t>(keys[i] >> 32));
+        auto each = [&](auto f) {
+            for (int i = t; i < n; i += 256) f(keys[i]);
+        };
+        best<256, CTA_CANDS>(prm.top, lane_top, each, [&](int r, Key k) { out.put(r, k); }, cands, red);
+    }
+}
+
+}  // namespace ipl
