@@ -507,6 +507,23 @@ int ip_dequantize_fp4(const uint8_t *q, long long ldq, const uint8_t *blocks, co
                       long long rows, int d, void *y, long long ldy, int dtype,
                       ip_stream_t stream);
 
+/* Product of 4-bit rows:
+ *   y[m][n] = act(sx[m] sw[n] S + bias[n]),  S = sum over blocks b of s_x[m][b] s_w[n][b] sum of
+ * the block's 16 products of codes, for m < rows, n < N: products and scales are exact, S is
+ * summed in f32 (on the tensor cores), the rest is f32 (sx[m] sw[n] first), rounded once to y's
+ * type.  act: IP_ACT_NONE or IP_ACT_SWISH.
+ * x, x_blocks, sx: 4-bit rows [rows][K] as above, w, w_blocks, sw: [N][K], one per output channel; any
+ * codes behind the first K of a row's last byte count as elements (0 as the calls above write them).
+ * bias: device f32 [N] or NULL.  y: device, dtype IP_F32, IP_F16 or IP_BF16, rows of ldy >= N
+ * elements (those behind column N are left as they were), apart from the inputs.
+ * rows <= IP_LINEAR_MAX_FRAMES, K in [1, IP_LINEAR_MAX_K], N in [1, IP_LINEAR_MAX_N].  workspace as
+ * for ip_linear_scaled_i8.  rows == 0 returns IP_OK without touching any pointer.
+ * Asynchronous on `stream`.  Returns IP_OK or IP_ERR_*. */
+int ip_linear_fp4(const uint8_t *x, long long ldx, const uint8_t *x_blocks, const float *sx,
+                  const uint8_t *w, long long ldw, const uint8_t *w_blocks, const float *sw,
+                  const float *bias, int act, long long rows, int K, int N, void *y, long long ldy,
+                  int dtype, void *workspace, size_t workspace_bytes, ip_stream_t stream);
+
 /* ---- log probabilities ---------------------------------------------------
  *
  * Of the distribution softmax(scale x) over each row x of logits, in f32:
@@ -613,7 +630,7 @@ const char *ip_strerror(int code);
 
 /* Test hook: bound, in SM clock cycles, of every barrier wait inside the
  * attention kernels (ip_relpos_mhsa_*) and the tensor-core kernels of
- * ip_linear_scaled_i8 launched afterwards by this process (0 = give up at the
+ * ip_linear_scaled_i8 and ip_linear_fp4 launched afterwards by this process (0 = give up at the
  * first wait that is not already satisfied; negative = the default of about two
  * seconds, which the other kernels keep).  A wait that runs out records
  * IP_ERR_TIMEOUT for ip_relpos_mhsa_status; the kernel lets its own copies in

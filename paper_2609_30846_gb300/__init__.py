@@ -42,6 +42,7 @@ EXPORTS = (
     "ip_kv4_attention_workspace_bytes", "ip_kv4_attention",
     "ip_fp4_block_bytes", "ip_quantize_fp4", "ip_rmsnorm_i8", "ip_rmsnorm_fp4", "ip_dequantize_i8",
     "ip_dequantize_fp4", "ip_token_logprobs_workspace_bytes", "ip_token_logprobs",
+    "ip_linear_fp4",
 )
 
 ROWS = 0    # IP_LAYOUT_ROWS:  [B][T][C]
@@ -202,6 +203,7 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
                 ("ip_rmsnorm_fp4", [P, LL, P, LL, P, F, N, LL, N, P, LL, P, LL, P, P, P], I),
                 ("ip_dequantize_i8", [P, LL, P, LL, N, P, LL, N, P], I),
                 ("ip_dequantize_fp4", [P, LL, P, P, LL, N, P, LL, N, P], I),
+                ("ip_linear_fp4", [P, LL, P, P, P, LL, P, P, P, N, LL, N, N, P, LL, N, P, S, P], I),
                 ("ip_token_logprobs_workspace_bytes", [LL, N, N], S),
                 ("ip_token_logprobs", [P, N, LL, N, LL, P, N, F, N, P, P, P, P, P, S, P], I)):
             fn = getattr(lib, name, None)      # a library built before these calls does the others
@@ -1096,6 +1098,37 @@ def dequantize_fp4(q, blocks, scale, d=None, *, dtype=None, out=None, stream=Non
     return out
 
 
+def linear_fp4(x, x_blocks, sx, w, w_blocks, sw, bias=None, *, act: int = ACT_NONE, dtype=None, out=None,
+               workspace=None, stream=None):
+    """Product of 4-bit rows (quantize_fp4, rmsnorm_fp4) on the block-scaled tensor cores:
+    out[..., n] = act(sum of the products of the values of x's and w's rows + bias[n]), codes and
+    scales exact, sums in float32.  x: uint8 [..., ceil(K / 2)] with its block scales and sx: float32
+    [...]; w: uint8 [N, ceil(K / 2)], w_blocks, sw: float32 [N] (quantize_fp4 of the weights); bias: float32 [N]
+    or None; act: ACT_NONE or ACT_SWISH; all CUDA tensors.  K and N may be any size; the rows of x
+    and w start on multiples of 16 bytes.  Returns out: [..., N] of `dtype` (bfloat16 unless out
+    gives it).  Asynchronous on `stream` (default: torch's current stream)."""
+    import torch
+    rows, K, ldx = _fp4_in(x, x_blocks, sx, ("x", "x_blocks", "sx"))
+    if _need(w, "w", torch.uint8, None, x.device).dim() != 2 or w.shape[1] != x.shape[-1]:
+        raise ValueError(f"w must have shape (N, {x.shape[-1]}), got {tuple(w.shape)}")
+    N, _, ldw = _fp4_in(w, w_blocks, sw, ("w", "w_blocks", "sw"))
+    shape = (*x.shape[:-1], N)
+    dtype, ldy = _values_out(out, dtype, shape, x.device)
+    code = _dtype_code(dtype)
+    pb = None if bias is None else _dense(bias, "bias", torch.float32, (N,), x.device)
+    lib = _lib or load()
+    with _On(x.device, stream) as handle:
+        if out is None:
+            out = torch.empty(shape, dtype=dtype, device=x.device)
+        workspace, ws, wsb = _status_space(workspace, x.device)
+        rc = lib.ip_linear_fp4(x.data_ptr(), ldx, x_blocks.data_ptr(), sx.data_ptr(), w.data_ptr(), ldw,
+                               w_blocks.data_ptr(), sw.data_ptr(), pb, int(act), rows, K, N, out.data_ptr(), ldy, code,
+                               ws, wsb, handle)
+    if rc:
+        _check("ip_linear_fp4", rc)
+    return out
+
+
 def kv4_page_bytes(page: int, dh: int = IP_DH) -> int:
     """Bytes of one page of one head of a 4-bit cache (144 a token)."""
     n = load().ip_kv4_page_bytes(page, dh)
@@ -1349,6 +1382,6 @@ __all__ = ["build", "load", "relpos_mhsa_i8", "relpos_mhsa_i8_host", "status", "
            "quantize_rows_i8", "linear_scaled_i8", "ACT_NONE", "ACT_SWISH",
            "kv4_page_bytes", "kv4_cache", "kv4_append", "kv4_read", "kv4_attention",
            "kv4_attention_workspace_bytes",
-           "fp4_block_shape", "quantize_fp4", "dequantize_fp4", "dequantize_i8", "rmsnorm_i8", "rmsnorm_fp4",
+           "fp4_block_shape", "quantize_fp4", "linear_fp4", "dequantize_fp4", "dequantize_i8", "rmsnorm_i8", "rmsnorm_fp4",
            "token_logprobs", "token_logprobs_workspace_bytes",
            "IpError", "LibraryError", "EXPORTS"]

@@ -1,0 +1,174 @@
+// Host side of the product of 4-bit rows of the C ABI (include/ip_mhsa.h): argument validation,
+// tensor maps and launches.  Device code: ip_fp4_kernels.cuh.
+#include "ip_mhsa.h"
+#include "ip_fp4_kernels.cuh"
+#include "ip_host_util.h"
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <mutex>
+
+namespace {
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
+                                  const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+    static EncodeTiledFn fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000,
+                                             cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeTiledFn>(p);
+    });
+    return fn;
+}
+
+// Rows of `bytes` bytes of codes, `ld` apart, boxes of 128 x box_rows in the 128-byte swizzled
+// layout; what lies outside reads as zero (a K that 256 does not divide, the rows behind the last).
+bool make_map(CUtensorMap *m, const void *base, int bytes, long long rows, long long ld, unsigned box_rows) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(bytes), static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld)};
+    const cuuint32_t box[2] = {ip4::BKB, box_rows};
+    const cuuint32_t estride[2] = {1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estride,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+std::mutex g_mu;
+int g_sms[64] = {0};
+
+int sm_count() {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    std::lock_guard<std::mutex> lock(g_mu);
+    if (g_sms[dev] == 0) {
+        int n = 0;
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+        g_sms[dev] = n;
+    }
+    return g_sms[dev];
+}
+
+int launched(cudaError_t rc) {
+    return rc == cudaSuccess && cudaGetLastError() == cudaSuccess ? IP_OK : IP_ERR_CUDA;
+}
+
+struct Operands {
+    const uint8_t *x, *w;
+    long long ldx, ldw;
+    int bytes;            // of a row's codes
+};
+
+template <typename T, int BN, bool PAIR, bool ODD>
+int launch(const CUtensorMap &tx, const CUtensorMap &tw, const ip4::Params &prm, int nsm, cudaStream_t st) {
+    using C = ip4::Tile<BN, PAIR>;
+    static bool set[64] = {false};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return IP_ERR_CUDA;
+    auto *fn = ip4::fp4_kernel<T, BN, PAIR, ODD>;
+    {
+        std::lock_guard<std::mutex> lock(g_mu);
+        if (!set[dev]) {
+            if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return IP_ERR_CUDA;
+            set[dev] = true;
+        }
+    }
+    const long long most = nsm / C::CTAS, workers = prm.tiles < most ? prm.tiles : most;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(workers * C::CTAS));
+    cfg.blockDim = dim3(ip4::THREADS);
+    cfg.dynamicSmemBytes = C::SMEM;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = C::CTAS;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = PAIR ? 2 : 1;
+    return launched(cudaLaunchKernelEx(&cfg, fn, tx, tw, prm));
+}
+
+template <typename T, int BN, bool PAIR>
+int run(const Operands &o, ip4::Params prm, int nsm, cudaStream_t st) {
+    using C = ip4::Tile<BN, PAIR>;
+    CUtensorMap tx, tw;
+    if (!make_map(&tx, o.x, o.bytes, prm.M, o.ldx, ip4::TILE_M) || !make_map(&tw, o.w, o.bytes, prm.N, o.ldw, C::BR))
+        return IP_ERR_CUDA;
+    prm.tiles_n = (prm.N + BN - 1) / BN;
+    prm.tiles = (prm.M + ip4::TILE_M * C::CTAS - 1) / (ip4::TILE_M * C::CTAS) * prm.tiles_n;
+    const bool odd = ((reinterpret_cast<uintptr_t>(prm.y) | (static_cast<size_t>(prm.ldy) * sizeof(T))) & 7) != 0 || prm.N % 16 != 0;
+    return odd ? launch<T, BN, PAIR, true>(tx, tw, prm, nsm, st) : launch<T, BN, PAIR, false>(tx, tw, prm, nsm, st);
+}
+
+template <typename T>
+int run(const Operands &o, const ip4::Params &prm, int nsm, cudaStream_t st) {
+    const long long tm = (prm.M + ip4::TILE_M - 1) / ip4::TILE_M;
+    if (tm * ((prm.N + 63) / 64) <= nsm) return run<T, 64, false>(o, prm, nsm, st);
+    if (tm * ((prm.N + 127) / 128) <= 2 * nsm) return run<T, 128, false>(o, prm, nsm, st);
+    return run<T, 256, true>(o, prm, nsm, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+int ip_linear_fp4(const uint8_t *x, long long ldx, const uint8_t *x_blocks, const float *sx, const uint8_t *w,
+                  long long ldw, const uint8_t *w_blocks, const float *sw, const float *bias, int act, long long rows,
+                  int K, int N, void *y, long long ldy, int dtype, void *workspace, size_t workspace_bytes,
+                  ip_stream_t stream) {
+    if ((dtype != IP_F32 && dtype != IP_F16 && dtype != IP_BF16) || (act != IP_ACT_NONE && act != IP_ACT_SWISH))
+        return IP_ERR_PARAM;
+    if (rows < 0 || rows > IP_LINEAR_MAX_FRAMES || K < 1 || K > IP_LINEAR_MAX_K || N < 1 || N > IP_LINEAR_MAX_N) return IP_ERR_SHAPE;
+    const int bytes = (K + 1) / 2;
+    if (ldx < bytes || ldw < bytes || ldy < N || ldx > (1ll << 39) || ldw > (1ll << 39) || ldy > (1ll << 31)) return IP_ERR_SHAPE;
+    if (rows == 0) return IP_OK;
+    if (!x || !x_blocks || !sx || !w || !w_blocks || !sw || !y || !workspace) return IP_ERR_NULL;
+    if (!aligned(x, 16) || !aligned(w, 16) || ldx % 16 != 0 || ldw % 16 != 0 || !aligned(x_blocks, 16) ||
+        !aligned(w_blocks, 16) || !aligned(sx, 4) || !aligned(sw, 4) || (bias && !aligned(bias, 4)) ||
+        !aligned(y, dtype == IP_F32 ? 4 : 2) || !aligned(workspace, 256))
+        return IP_ERR_ALIGN;
+    if (workspace_bytes < 256) return IP_ERR_WORKSPACE;
+    const int nsm = sm_count();
+    if (nsm <= 0) return IP_ERR_CUDA;
+    ip4::Params prm;
+    prm.sx = sx;
+    prm.sw = sw;
+    prm.bias = bias;
+    prm.xb = x_blocks;
+    prm.wb = w_blocks;
+    prm.y = y;
+    prm.M = rows;
+    prm.ldy = ldy;
+    prm.N = N;
+    prm.act = act;
+    prm.steps = (K + 63) / 64;
+    prm.xtiles = static_cast<int>((rows + 127) / 128);
+    prm.wtiles = (N + 127) / 128;
+    prm.tiles_n = 0;
+    prm.tiles = 0;
+    prm.err = static_cast<int *>(workspace);
+    prm.timeout_cycles = iph::wait_limit();
+    prm.stall = iph::stall_injection();
+    const Operands o{x, w, ldx, ldw, bytes};
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (dtype == IP_F32) return run<float>(o, prm, nsm, st);
+    if (dtype == IP_F16) return run<__half>(o, prm, nsm, st);
+    return run<__nv_bfloat16>(o, prm, nsm, st);
+}
+
+}  // extern "C"
