@@ -724,6 +724,7 @@ class _Unbound:
         return None
 
     linear_scaled = kv4_append = kv4_read = kv4_attention = quantize_rows
+    quantize_fp4 = linear_fp4 = rmsnorm_i8 = rmsnorm_fp4 = dequantize_i8 = dequantize_fp4 = token_logprobs = quantize_rows
 
 
 _short = _Unbound
@@ -740,7 +741,9 @@ def _bind_short(lib):
     mod = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(mod)
     mod.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
-        lib.ip_quantize_rows_i8, lib.ip_linear_scaled_i8, lib.ip_kv4_append, lib.ip_kv4_read, lib.ip_kv4_attention)))
+        lib.ip_quantize_rows_i8, lib.ip_linear_scaled_i8, lib.ip_kv4_append, lib.ip_kv4_read, lib.ip_kv4_attention,
+        lib.ip_quantize_fp4, lib.ip_linear_fp4, lib.ip_rmsnorm_i8, lib.ip_rmsnorm_fp4, lib.ip_dequantize_i8,
+        lib.ip_dequantize_fp4, lib.ip_token_logprobs)))
     return mod
 
 
@@ -964,6 +967,10 @@ def quantize_fp4(x, *, q=None, blocks=None, scale=None, stream=None):
     bytes, as linear_fp4 reads them, so it may be a view of them), uint8
     fp4_block_shape(rows, d) and float32 of x.shape[:-1].  Asynchronous on `stream`
     (default: torch's current stream)."""
+    if stream is None:
+        r = _short.quantize_fp4(x, q, blocks, scale)
+        if r is not None:
+            return r if r.__class__ is not int else _check("ip_quantize_fp4", r)
     code = _dtype_code(_need(x, "x").dtype, "x")
     rows, d, ldx = _as_rows(x, "x")
     lib = _lib or load()
@@ -999,6 +1006,10 @@ def rmsnorm_i8(x, weight, residual=None, *, eps: float = 1e-5, out=None, q=None,
     tensors; weight: x's type [d].  Returns (q, scale, h): int8 of x's shape (a new q has rows of
     a multiple of 16 bytes), float32 of x.shape[:-1], and h of x's type, None without a residual.  out:
     where h goes, which may be x or residual itself.  Asynchronous on `stream`."""
+    if stream is None:
+        r = _short.rmsnorm_i8(x, weight, residual, eps, out, q, scale)
+        if r is not None:
+            return r if r.__class__ is not int else _check("ip_rmsnorm_i8", r)
     import torch
     code, rows, d, ldx, ldr, lds = _norm_in(x, weight, residual, out)
     dev, lib = x.device, _lib or load()
@@ -1025,6 +1036,10 @@ def rmsnorm_i8(x, weight, residual=None, *, eps: float = 1e-5, out=None, q=None,
 def rmsnorm_fp4(x, weight, residual=None, *, eps: float = 1e-5, out=None, q=None, blocks=None, scale=None,
                 stream=None):
     """rmsnorm_i8 with 4-bit rows (quantize_fp4): returns (q, blocks, scale, h)."""
+    if stream is None:
+        r = _short.rmsnorm_fp4(x, weight, residual, eps, out, q, blocks, scale)
+        if r is not None:
+            return r if r.__class__ is not int else _check("ip_rmsnorm_fp4", r)
     import torch
     code, rows, d, ldx, ldr, lds = _norm_in(x, weight, residual, out)
     dev, lib = x.device, _lib or load()
@@ -1053,6 +1068,10 @@ def dequantize_i8(q, scale, *, dtype=None, out=None, stream=None):
     """The values of int8 rows (quantize_rows_i8, rmsnorm_i8): q scale, rounded once to `dtype`
     (bfloat16 unless out gives it).  q: int8 [..., d], scale: float32 [...], CUDA tensors.
     Asynchronous on `stream`."""
+    if stream is None:
+        r = _short.dequantize_i8(q, scale, dtype, out)
+        if r is not None:
+            return r if r.__class__ is not int else _check("ip_dequantize_i8", r)
     import torch
     rows, d, ldq = _as_rows(_need(q, "q", torch.int8), "q")
     ps = _dense(scale, "scale", torch.float32, q.shape[:-1], q.device)
@@ -1083,6 +1102,10 @@ def dequantize_fp4(q, blocks, scale, d=None, *, dtype=None, out=None, stream=Non
     """The values of 4-bit rows (quantize_fp4, rmsnorm_fp4), code s r in float32, rounded once to
     `dtype` (bfloat16 unless out gives it): [..., d], d twice q's bytes unless given.
     Asynchronous on `stream`."""
+    if stream is None:
+        r = _short.dequantize_fp4(q, blocks, scale, d, dtype, out)
+        if r is not None:
+            return r if r.__class__ is not int else _check("ip_dequantize_fp4", r)
     import torch
     rows, d, ldq = _fp4_in(q, blocks, scale, ("q", "blocks", "scale"), d)
     shape = (*q.shape[:-1], d)
@@ -1107,6 +1130,10 @@ def linear_fp4(x, x_blocks, sx, w, w_blocks, sw, bias=None, *, act: int = ACT_NO
     or None; act: ACT_NONE or ACT_SWISH; all CUDA tensors.  K and N may be any size; the rows of x
     and w start on multiples of 16 bytes.  Returns out: [..., N] of `dtype` (bfloat16 unless out
     gives it).  Asynchronous on `stream` (default: torch's current stream)."""
+    if stream is None:
+        r = _short.linear_fp4(x, x_blocks, sx, w, w_blocks, sw, bias, act, dtype, out, workspace)
+        if r is not None:
+            return r if r.__class__ is not int else _check("ip_linear_fp4", r)
     import torch
     rows, K, ldx = _fp4_in(x, x_blocks, sx, ("x", "x_blocks", "sx"))
     if _need(w, "w", torch.uint8, None, x.device).dim() != 2 or w.shape[1] != x.shape[-1]:
@@ -1309,6 +1336,10 @@ def token_logprobs(logits, tokens=None, *, top: int = 0, scale: float = 1.0, out
     tokens -1.  out: such a tuple, contiguous.  workspace: a uint8 tensor of
     token_logprobs_workspace_bytes(rows, V, top).  Asynchronous on `stream` (default: torch's
     current stream)."""
+    if stream is None and out is None:
+        r = _short.token_logprobs(logits, tokens, top, scale, workspace)
+        if r is not None:
+            return r if r.__class__ is tuple else _check("ip_token_logprobs", r)
     import torch
     code = _dtype_code(_need(logits, "logits").dtype, "logits")
     rows, V, ld = _as_rows(logits, "logits")

@@ -1,4 +1,4 @@
-// Short forms of the Python calls with run-time scales and on the 4-bit cache, for their usual
+// Short forms of the Python calls with run-time scales, on 4-bit rows and on the 4-bit cache, for their usual
 // arguments: plain contiguous tensors (or matrices) of the current device, its current stream.
 // Each makes the checks of the general form in place, allocates the outputs and calls the C
 // entry point; it returns the outputs, the entry point's error code, or None for arguments that
@@ -16,6 +16,8 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <climits>
+#include <initializer_list>
+#include <type_traits>
 
 #include "ip_mhsa.h"
 
@@ -28,6 +30,13 @@ struct Entries {
     decltype(&ip_kv4_append) append;
     decltype(&ip_kv4_read) read;
     decltype(&ip_kv4_attention) attention;
+    decltype(&ip_quantize_fp4) quantize_fp4;
+    decltype(&ip_linear_fp4) linear_fp4;
+    decltype(&ip_rmsnorm_i8) norm_i8;
+    decltype(&ip_rmsnorm_fp4) norm_fp4;
+    decltype(&ip_dequantize_i8) values_i8;
+    decltype(&ip_dequantize_fp4) values_fp4;
+    decltype(&ip_token_logprobs) logprobs;
 } g_entry;
 
 constexpr int64_t ROW_BYTES = 144;
@@ -300,17 +309,292 @@ PyObject *kv4_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// Addresses of the five entry points, in the order of Entries.
-PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
+// Tensors as a tuple, None for those that are not there.
+PyObject *tuple(std::initializer_list<const at::Tensor *> list) {
+    PyObject *r = PyTuple_New(static_cast<Py_ssize_t>(list.size()));
+    if (!r) return nullptr;
+    Py_ssize_t i = 0;
+    for (const at::Tensor *t : list) {
+        PyObject *o = Py_None;
+        if (t) o = THPVariable_Wrap(*t);
+        else Py_INCREF(o);
+        if (!o) {
+            Py_DECREF(r);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(r, i++, o);
+    }
+    return r;
+}
+
+// New rows of n elements of one byte each, `lead` of them, on multiples of 16 bytes; ld: their stride.
+at::Tensor byte_rows(at::IntArrayRef lead, int64_t n, const at::Tensor &like, at::ScalarType type, int64_t &ld) {
+    c10::SmallVector<int64_t, 6> shape(lead.begin(), lead.end());
+    shape.push_back(n);
+    ld = (n + 15) / 16 * 16;
+    if (ld == n) return empty(shape, like, type);
+    c10::SmallVector<int64_t, 6> strides(shape.size(), 1);
+    int64_t step = ld;
+    for (size_t i = shape.size() - 1; i-- > 0; step *= shape[i] > 1 ? shape[i] : 1) strides[i] = step;
+    return at::empty_strided(shape, strides, like.options().dtype(type).requires_grad(false));
+}
+
+// Contiguous rows of real values on the current device.
+struct Rows {
+    const at::Tensor *x;
+    int dev, code;
+    int64_t d, rows;
+
+    bool take(PyObject *o) {
+        x = tensor(o);
+        if (!x || x->dim() < 1 || !x->is_contiguous()) return false;
+        dev = x->get_device();
+        code = code_of(x->scalar_type());
+        d = x->size(-1);
+        if (code < 0 || d < 1 || !fits(d) || dev != c10::cuda::current_device()) return false;
+        rows = x->numel() / d;
+        return true;
+    }
+    at::IntArrayRef lead() const { return x->sizes().slice(0, x->dim() - 1); }
+    at::Tensor blocks() const {
+        const int64_t shape[3] = {(rows + 127) / 128, (d + 63) / 64, 512};
+        return empty(shape, *x, at::kByte);
+    }
+};
+
+// (x, q, blocks, scale), the last three None
+PyObject *quantize_fp4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!arity(n, 4)) return nullptr;
+    Rows r;
+    if (a[1] != Py_None || a[2] != Py_None || a[3] != Py_None || !r.take(a[0])) Py_RETURN_NONE;
+    int64_t ld;
+    const at::Tensor q = byte_rows(r.lead(), (r.d + 1) / 2, *r.x, at::kByte, ld), blocks = r.blocks(),
+                     scale = empty(r.lead(), *r.x, at::kFloat);
+    const int rc = unlocked([&] {
+        return g_entry.quantize_fp4(r.x->const_data_ptr(), r.code, r.rows, static_cast<int>(r.d), r.d,
+                                    static_cast<uint8_t *>(q.data_ptr()), ld, static_cast<uint8_t *>(blocks.data_ptr()),
+                                    static_cast<float *>(scale.data_ptr()), stream_of(r.dev));
+    });
+    return rc == IP_OK ? tuple({&q, &blocks, &scale}) : PyLong_FromLong(rc);
+    END_HANDLE_TH_ERRORS
+}
+
+// (x, weight, residual, eps, out, q, blocks, scale), the last three None (i8: without blocks)
+PyObject *norm(PyObject *const *a, Py_ssize_t n, bool fp4) {
+    HANDLE_TH_ERRORS
+    if (!arity(n, fp4 ? 8 : 7)) return nullptr;
+    Rows r;
+    for (Py_ssize_t i = 5; i < n; ++i)
+        if (a[i] != Py_None) Py_RETURN_NONE;
+    if (!PyFloat_CheckExact(a[3]) || !r.take(a[0])) Py_RETURN_NONE;
+    const at::ScalarType type = r.x->scalar_type();
+    const at::Tensor *w = tensor(a[1]), *res = nullptr;
+    if (!vector(w, type, r.d, r.dev)) Py_RETURN_NONE;
+    at::Tensor sum;
+    if (a[2] != Py_None) {
+        res = tensor(a[2]);
+        if (!contiguous(res, type, r.dev) || res->sizes() != r.x->sizes() || !output(a[4], r.x->sizes(), *r.x, type, sum))
+            Py_RETURN_NONE;
+    } else if (a[4] != Py_None) {
+        Py_RETURN_NONE;
+    }
+    int64_t ld;
+    const at::Tensor q = byte_rows(r.lead(), fp4 ? (r.d + 1) / 2 : r.d, *r.x, fp4 ? at::kByte : at::kChar, ld);
+    const at::Tensor scale = empty(r.lead(), *r.x, at::kFloat);
+    at::Tensor blocks;
+    if (fp4) blocks = r.blocks();
+    const float eps = static_cast<float>(PyFloat_AS_DOUBLE(a[3]));
+    const void *pr = res ? res->const_data_ptr() : nullptr;
+    void *ps = res ? sum.data_ptr() : nullptr;
+    const int d = static_cast<int>(r.d);
+    const int rc = unlocked([&] {
+        return fp4 ? g_entry.norm_fp4(r.x->const_data_ptr(), d, pr, d, w->const_data_ptr(), eps, r.code, r.rows, d, ps, d,
+                                      static_cast<uint8_t *>(q.data_ptr()), ld, static_cast<uint8_t *>(blocks.data_ptr()),
+                                      static_cast<float *>(scale.data_ptr()), stream_of(r.dev))
+                   : g_entry.norm_i8(r.x->const_data_ptr(), d, pr, d, w->const_data_ptr(), eps, r.code, r.rows, d, ps, d,
+                                     static_cast<int8_t *>(q.data_ptr()), ld, static_cast<float *>(scale.data_ptr()),
+                                     stream_of(r.dev));
+    });
+    if (rc != IP_OK) return PyLong_FromLong(rc);
+    const at::Tensor *total = res ? &sum : nullptr;
+    return fp4 ? tuple({&q, &blocks, &scale, total}) : tuple({&q, &scale, total});
+    END_HANDLE_TH_ERRORS
+}
+PyObject *rmsnorm_i8(PyObject *, PyObject *const *a, Py_ssize_t n) { return norm(a, n, false); }
+PyObject *rmsnorm_fp4(PyObject *, PyObject *const *a, Py_ssize_t n) { return norm(a, n, true); }
+
+// The type that a call writes: `dtype`, else out's, else bfloat16; false for what the general form has to look at.
+bool type_of(PyObject *dtype, PyObject *out, at::ScalarType &type) {
+    type = at::kBFloat16;
+    if (THPDtype_Check(dtype)) type = reinterpret_cast<THPDtype *>(dtype)->scalar_type;
+    else if (dtype != Py_None) return false;
+    else if (THPVariable_CheckExact(out)) type = THPVariable_Unpack(out).scalar_type();
+    return code_of(type) >= 0;
+}
+
+// Rows of bytes with a scale each, and for 4-bit rows (d elements, -1: two a byte) their blocks.
+struct ByteRows {
+    const at::Tensor *q, *scale, *blocks;
+    int64_t rows, d, ld;
+
+    bool take(PyObject *oq, PyObject *oscale, PyObject *oblocks, int64_t want, int dev) {
+        q = tensor(oq), scale = tensor(oscale), blocks = oblocks ? tensor(oblocks) : nullptr;
+        if (!q || q->dim() < 1 || q->scalar_type() != (oblocks ? at::kByte : at::kChar) || q->get_device() != dev ||
+            !contiguous(scale, at::kFloat, dev))
+            return false;
+        const int64_t n = q->size(-1);
+        if (n < 1 || n > INT_MAX / 2 || scale->sizes() != lead()) return false;
+        d = oblocks ? (want < 0 ? 2 * n : want) : n;
+        rows = q->numel() / n;
+        ld = row_stride(*q);
+        if (ld < n) return false;
+        if (!oblocks) return true;
+        return (d + 1) / 2 == n && contiguous(blocks, at::kByte, dev) && blocks->dim() == 3 &&
+               blocks->size(0) == (rows + 127) / 128 && blocks->size(1) == (d + 63) / 64 && blocks->size(2) == 512;
+    }
+    at::IntArrayRef lead() const { return q->sizes().slice(0, q->dim() - 1); }
+    const uint8_t *codes() const { return static_cast<const uint8_t *>(q->const_data_ptr()); }
+    const uint8_t *scales() const { return static_cast<const uint8_t *>(blocks->const_data_ptr()); }
+    const float *factors() const { return static_cast<const float *>(scale->const_data_ptr()); }
+};
+
+PyObject *values(PyObject *oq, PyObject *oscale, PyObject *oblocks, int64_t d, PyObject *dtype, PyObject *o) {
+    const int dev = c10::cuda::current_device();
+    ByteRows r;
+    at::ScalarType type;
+    if (!type_of(dtype, o, type) || !r.take(oq, oscale, oblocks, d, dev)) Py_RETURN_NONE;
+    c10::SmallVector<int64_t, 6> shape(r.lead().begin(), r.lead().end());
+    shape.push_back(r.d);
+    at::Tensor out;
+    if (!output(o, shape, *r.q, type, out)) Py_RETURN_NONE;
+    const int rc = unlocked([&] {
+        return oblocks ? g_entry.values_fp4(r.codes(), r.ld, r.scales(), r.factors(), r.rows, static_cast<int>(r.d),
+                                            out.data_ptr(), r.d, code_of(type), stream_of(dev))
+                       : g_entry.values_i8(reinterpret_cast<const int8_t *>(r.codes()), r.ld, r.factors(), r.rows,
+                                           static_cast<int>(r.d), out.data_ptr(), r.d, code_of(type), stream_of(dev));
+    });
+    return rc == IP_OK ? THPVariable_Wrap(out) : PyLong_FromLong(rc);
+}
+// (q, scale, dtype, out)
+PyObject *dequantize_i8(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!arity(n, 4)) return nullptr;
+    return values(a[0], a[1], nullptr, -1, a[2], a[3]);
+    END_HANDLE_TH_ERRORS
+}
+// (q, blocks, scale, d, dtype, out)
+PyObject *dequantize_fp4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!arity(n, 6)) return nullptr;
+    int64_t d = -1;
+    if (a[3] != Py_None) {
+        int over = 0;
+        if (!PyLong_CheckExact(a[3])) Py_RETURN_NONE;
+        d = PyLong_AsLongAndOverflow(a[3], &over);
+        if (over || d < 1 || !fits(d)) Py_RETURN_NONE;
+    }
+    return values(a[0], a[2], a[1], d, a[4], a[5]);
+    END_HANDLE_TH_ERRORS
+}
+
+// (x, x_blocks, sx, w, w_blocks, sw, bias, act, dtype, out, workspace)
+PyObject *linear_fp4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!arity(n, 11)) return nullptr;
+    const at::Tensor *ws = tensor(a[10]);
+    at::ScalarType type;
+    if (!ws || !PyLong_CheckExact(a[7]) || !type_of(a[8], a[9], type)) Py_RETURN_NONE;
+    const int dev = ws->get_device();
+    ByteRows x, w;
+    if (dev != c10::cuda::current_device() || !contiguous(ws, at::kByte, dev) || !x.take(a[0], a[2], a[1], -1, dev) ||
+        !w.take(a[3], a[5], a[4], -1, dev) || w.q->dim() != 2 || w.d != x.d || (x.ld | w.ld) % 16 != 0 || w.rows < 1 ||
+        !fits(w.rows))
+        Py_RETURN_NONE;
+    int over = 0;
+    const long act = PyLong_AsLongAndOverflow(a[7], &over);
+    const void *bias;
+    if (over || act < 0 || act > INT_MAX || !maybe_vector(a[6], at::kFloat, w.rows, dev, bias)) Py_RETURN_NONE;
+    c10::SmallVector<int64_t, 6> shape(x.lead().begin(), x.lead().end());
+    shape.push_back(w.rows);
+    at::Tensor out;
+    if (!output(a[9], shape, *x.q, type, out)) Py_RETURN_NONE;
+    const int rc = unlocked([&] {
+        return g_entry.linear_fp4(x.codes(), x.ld, x.scales(), x.factors(), w.codes(), w.ld, w.scales(), w.factors(),
+                                  static_cast<const float *>(bias), static_cast<int>(act), x.rows, static_cast<int>(x.d),
+                                  static_cast<int>(w.rows), out.data_ptr(), w.rows, code_of(type), ws->data_ptr(),
+                                  static_cast<size_t>(ws->numel()), stream_of(dev));
+    });
+    return rc == IP_OK ? THPVariable_Wrap(out) : PyLong_FromLong(rc);
+    END_HANDLE_TH_ERRORS
+}
+
+// (logits, tokens, top, scale, workspace)
+PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
     if (!arity(n, 5)) return nullptr;
-    void *p[5];
-    for (int i = 0; i < 5; ++i) {
+    const at::Tensor *x = tensor(a[0]), *tok = nullptr, *ws = tensor(a[4]);
+    if (!x || !ws || x->dim() < 1 || !PyLong_CheckExact(a[2]) || !PyFloat_CheckExact(a[3])) Py_RETURN_NONE;
+    const int dev = x->get_device(), code = code_of(x->scalar_type());
+    const int64_t V = x->size(-1), ld = V < 1 ? 0 : row_stride(*x);
+    int over = 0;
+    const long top = PyLong_AsLongAndOverflow(a[2], &over);
+    if (code < 0 || dev != c10::cuda::current_device() || V < 1 || !fits(V) || ld < V || over || top < 0 ||
+        top > IP_LOGPROBS_MAX_TOP || !contiguous(ws, at::kByte, dev))
+        Py_RETURN_NONE;
+    const at::IntArrayRef lead = x->sizes().slice(0, x->dim() - 1);
+    bool wide = false;
+    if (a[1] != Py_None) {
+        tok = tensor(a[1]);
+        if (!tok || !tok->is_contiguous() || tok->get_device() != dev || tok->sizes() != lead) Py_RETURN_NONE;
+        wide = tok->scalar_type() == at::kLong;
+        if (!wide && tok->scalar_type() != at::kInt) Py_RETURN_NONE;
+    }
+    at::Tensor lp, ent = empty(lead, *x, at::kFloat), tlp, ttok;
+    if (tok) lp = empty(lead, *x, at::kFloat);
+    if (top > 0) {
+        c10::SmallVector<int64_t, 6> shape(lead.begin(), lead.end());
+        shape.push_back(top);
+        tlp = empty(shape, *x, at::kFloat);
+        ttok = empty(shape, *x, at::kInt);
+    }
+    const float scale = static_cast<float>(PyFloat_AS_DOUBLE(a[3]));
+    auto data = [](const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
+    const int rc = unlocked([&] {
+        return g_entry.logprobs(x->const_data_ptr(), code, x->numel() / V, static_cast<int>(V), ld,
+                                tok ? tok->const_data_ptr() : nullptr, wide ? 1 : 0, scale, static_cast<int>(top),
+                                static_cast<float *>(data(lp)), static_cast<float *>(data(ent)),
+                                static_cast<float *>(data(tlp)), static_cast<int32_t *>(data(ttok)), ws->data_ptr(),
+                                static_cast<size_t>(ws->numel()), stream_of(dev));
+    });
+    if (rc != IP_OK) return PyLong_FromLong(rc);
+    return tuple({tok ? &lp : nullptr, &ent, top > 0 ? &tlp : nullptr, top > 0 ? &ttok : nullptr});
+    END_HANDLE_TH_ERRORS
+}
+
+// Addresses of the entry points, in the order of Entries.
+PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    constexpr int N = 12;
+    if (!arity(n, N)) return nullptr;
+    void *p[N];
+    for (int i = 0; i < N; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i]);
         if (PyErr_Occurred()) return nullptr;
     }
-    g_entry = {reinterpret_cast<decltype(g_entry.quantize)>(p[0]), reinterpret_cast<decltype(g_entry.linear)>(p[1]),
-               reinterpret_cast<decltype(g_entry.append)>(p[2]), reinterpret_cast<decltype(g_entry.read)>(p[3]),
-               reinterpret_cast<decltype(g_entry.attention)>(p[4])};
+    int i = 0;
+    auto take = [&](auto &f) { f = reinterpret_cast<std::remove_reference_t<decltype(f)>>(p[i++]); };
+    take(g_entry.quantize);
+    take(g_entry.linear);
+    take(g_entry.append);
+    take(g_entry.read);
+    take(g_entry.attention);
+    take(g_entry.quantize_fp4);
+    take(g_entry.linear_fp4);
+    take(g_entry.norm_i8);
+    take(g_entry.norm_fp4);
+    take(g_entry.values_i8);
+    take(g_entry.values_fp4);
+    take(g_entry.logprobs);
     Py_RETURN_NONE;
 }
 
@@ -321,6 +605,10 @@ PyMethodDef method(const char *name, F f) {
 PyMethodDef g_methods[] = {method("bind", bind), method("quantize_rows", quantize_rows),
                            method("linear_scaled", linear_scaled), method("kv4_append", kv4_append),
                            method("kv4_read", kv4_read), method("kv4_attention", kv4_attention),
+                           method("quantize_fp4", quantize_fp4), method("linear_fp4", linear_fp4),
+                           method("rmsnorm_i8", rmsnorm_i8), method("rmsnorm_fp4", rmsnorm_fp4),
+                           method("dequantize_i8", dequantize_i8), method("dequantize_fp4", dequantize_fp4),
+                           method("token_logprobs", token_logprobs),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "ip_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
