@@ -44,6 +44,32 @@ bool make_map(CUtensorMap *m, const void *base, int bytes, long long rows, long 
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Block scales of `rows` rows as [rows / 128][steps of 64 elements][512 bytes], boxes of four steps of
+// `tiles` times 128 rows; what lies outside reads as zero.
+bool make_scale_map(CUtensorMap *m, const void *base, int steps, long long rows, unsigned tiles) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {128, static_cast<cuuint64_t>(steps), static_cast<cuuint64_t>((rows + 127) / 128)};
+    const cuuint64_t strides[2] = {512, static_cast<cuuint64_t>(steps) * 512};
+    const cuuint32_t box[3] = {128, 4, tiles};
+    const cuuint32_t estride[3] = {1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void *>(base), dims, strides, box, estride,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The output's rows, boxes of 128 bytes x 32 rows in the 128-byte swizzled layout.
+bool make_out_map(CUtensorMap *m, void *y, CUtensorMapDataType type, int es, int N, long long rows, long long ld) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(N), static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * es};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / es), 32};
+    const cuuint32_t estride[2] = {1, 1};
+    return fn(m, type, 2, y, dims, strides, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 std::mutex g_mu;
@@ -66,13 +92,13 @@ int launched(cudaError_t rc) {
 }
 
 struct Operands {
-    const uint8_t *x, *w;
+    const uint8_t *x, *w, *xb, *wb;
     long long ldx, ldw;
     int bytes;            // of a row's codes
 };
 
 template <typename T, int BN, bool PAIR, bool ODD>
-int launch(const CUtensorMap &tx, const CUtensorMap &tw, const ip4::Params &prm, int nsm, cudaStream_t st) {
+int launch(const CUtensorMap (&maps)[5], const ip4::Params &prm, int nsm, cudaStream_t st) {
     using C = ip4::Tile<BN, PAIR>;
     static bool set[64] = {false};
     int dev = 0;
@@ -100,19 +126,26 @@ int launch(const CUtensorMap &tx, const CUtensorMap &tw, const ip4::Params &prm,
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = PAIR ? 2 : 1;
-    return launched(cudaLaunchKernelEx(&cfg, fn, tx, tw, prm));
+    return launched(cudaLaunchKernelEx(&cfg, fn, maps[0], maps[1], maps[2], maps[3], maps[4], prm));
 }
 
 template <typename T, int BN, bool PAIR>
 int run(const Operands &o, ip4::Params prm, int nsm, cudaStream_t st) {
     using C = ip4::Tile<BN, PAIR>;
-    CUtensorMap tx, tw;
-    if (!make_map(&tx, o.x, o.bytes, prm.M, o.ldx, ip4::TILE_M) || !make_map(&tw, o.w, o.bytes, prm.N, o.ldw, C::BR))
+    CUtensorMap maps[5];
+    if (!make_map(&maps[0], o.x, o.bytes, prm.M, o.ldx, ip4::TILE_M) || !make_map(&maps[1], o.w, o.bytes, prm.N, o.ldw, C::BR) ||
+        !make_scale_map(&maps[2], o.xb, prm.steps, prm.M, 1) || !make_scale_map(&maps[3], o.wb, prm.steps, prm.N, C::WT))
         return IP_ERR_CUDA;
     prm.tiles_n = (prm.N + BN - 1) / BN;
     prm.tiles = (prm.M + ip4::TILE_M * C::CTAS - 1) / (ip4::TILE_M * C::CTAS) * prm.tiles_n;
-    const bool odd = ((reinterpret_cast<uintptr_t>(prm.y) | (static_cast<size_t>(prm.ldy) * sizeof(T))) & 7) != 0 || prm.N % 16 != 0;
-    return odd ? launch<T, BN, PAIR, true>(tx, tw, prm, nsm, st) : launch<T, BN, PAIR, false>(tx, tw, prm, nsm, st);
+    constexpr int es = static_cast<int>(sizeof(T));
+    // what the forms' usual ways out ask of the rows: blocks by TMA, or 16 columns by stores of 8 bytes and more
+    const bool odd = BN < 128 ? !aligned(prm.y, 8) || prm.ldy * es % 8 != 0 || prm.N % 16 != 0
+                              : !aligned(prm.y, 16) || prm.ldy * es % 16 != 0 || prm.N * es % 16 != 0;
+    constexpr CUtensorMapDataType type = es == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16;
+    if (odd || BN < 128) maps[4] = maps[0];      // not used
+    else if (!make_out_map(&maps[4], prm.y, type, es, prm.N, prm.M, prm.ldy)) return IP_ERR_CUDA;
+    return odd ? launch<T, BN, PAIR, true>(maps, prm, nsm, st) : launch<T, BN, PAIR, false>(maps, prm, nsm, st);
 }
 
 template <typename T>
@@ -149,22 +182,18 @@ int ip_linear_fp4(const uint8_t *x, long long ldx, const uint8_t *x_blocks, cons
     prm.sx = sx;
     prm.sw = sw;
     prm.bias = bias;
-    prm.xb = x_blocks;
-    prm.wb = w_blocks;
     prm.y = y;
     prm.M = rows;
     prm.ldy = ldy;
     prm.N = N;
     prm.act = act;
     prm.steps = (K + 63) / 64;
-    prm.xtiles = static_cast<int>((rows + 127) / 128);
-    prm.wtiles = (N + 127) / 128;
     prm.tiles_n = 0;
     prm.tiles = 0;
     prm.err = static_cast<int *>(workspace);
     prm.timeout_cycles = iph::wait_limit();
     prm.stall = iph::stall_injection();
-    const Operands o{x, w, ldx, ldw, bytes};
+    const Operands o{x, w, x_blocks, w_blocks, ldx, ldw, bytes};
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     if (dtype == IP_F32) return run<float>(o, prm, nsm, st);
     if (dtype == IP_F16) return run<__half>(o, prm, nsm, st);

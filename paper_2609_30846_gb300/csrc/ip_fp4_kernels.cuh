@@ -11,7 +11,7 @@ namespace ip4 {
 using namespace ipk;
 using namespace ipr;
 using ips::elect_one, ips::cluster_sync, ips::mma_commit, ips::tmem_alloc, ips::tmem_free, ips::tmem_ld16,
-    ips::tmem_wait_ld, ips::wait_or_dead, ips::warp_wait_or_dead, ips::arrive_first, ips::smem_desc;
+    ips::tmem_wait_ld, ips::smem_desc;
 
 // y[m][n] = act(sx[m] sw[n] S + bias[n]), S = sum over blocks of s_x s_w sum of 16 code products, by
 // tcgen05.mma kind::mxf4nvf4 with a scale for each 16 elements: products and scales are exact there, sums
@@ -23,8 +23,8 @@ using ips::elect_one, ips::cluster_sync, ips::mma_commit, ips::tmem_alloc, ips::
 // (tcgen05.cp) and issues the MMAs of 64 elements each, warps 0-7 take the sums to registers, release
 // the accumulator and write the output while the next tile is summed.
 // PAIR: two CTAs share a tile of 256 rows x BN channels (cta_group::2), each fetching its 128 rows and half of
-// the channels; the scales of all channels go to both.  The second CTA's warp 9 tells the first one's
-// of stages that have landed.
+// the channels; the scales of all channels go to both.  Both CTAs' copies report to the first one's
+// barriers, whose warp 9 issues for both.
 
 constexpr int TILE_M = 128;
 constexpr int BKB = 128;                 // bytes of a row in a stage
@@ -34,12 +34,10 @@ constexpr int EPI_WARPS = 8, TMA_WARP = 8, MMA_WARP = 9;
 
 struct Params {
     const float *sx, *sw, *bias;
-    const uint8_t *xb, *wb;              // e4m3 scales
     void *y;
     long long M, ldy;
     int N, act;
     int steps;                           // of 64 elements
-    int xtiles, wtiles;                  // of 128 rows in xb and wb
     int tiles_n;
     long long tiles;
     int *err;
@@ -55,21 +53,66 @@ struct Tile {
     static constexpr int WT = BN <= 128 ? 1 : BN / 128;      // tiles of scales of w
     static constexpr int A = TILE_M * BKB, B = BR * BKB, SA = 2048, SB = 2048 * WT;
     static constexpr int STAGE = A + B + SA + SB;
-    static constexpr int ST = BN == 64 ? 6 : 5;
+    static constexpr int ST = BN == 64 ? 6 : 4;
     static constexpr int ACCS = BN == 256 ? 1 : 2;    // accumulators
     static constexpr int SF = ACCS * BN;              // first column of the scales
     static constexpr int SF_COLS = 16 + 16 * WT;      // of a stage
     static constexpr int COLS = 512;
     static constexpr int TMEM_PTR = 256, DEAD = 260;
+    static constexpr int OTHER = 264;                 // of the other CTA of a pair: given up, stages fetched
     static constexpr int CONSTS = 512;                // per output warp: sw and bias of its columns
     static constexpr int TURN = CONSTS + EPI_WARPS * 2 * 4 * (BN / 2);
-    static constexpr int STAGES_AT = (TURN + EPI_WARPS * ips::TURN_BYTES + 1023) & ~1023;
+    // per output warp: two blocks of 32 rows x 128 bytes on their way out (store_odd's block in their place)
+    static constexpr int OUT_AT = (TURN + 1023) & ~1023;
+    static constexpr int OUT = BN == 64 ? ((ips::TURN_BYTES + 127) & ~127) : 8192;
+    static constexpr int STAGES_AT = (OUT_AT + EPI_WARPS * OUT + 1023) & ~1023;
     static constexpr int SMEM = STAGES_AT + ST * STAGE + 1024;
-    static_assert(8 * (3 * ST + 6) <= 256, "barriers");
+    static_assert(8 * (2 * ST + 6) <= 256, "barriers");
     static_assert(SMEM <= 232448, "shared memory");
     static_assert(SF + ST * SF_COLS <= COLS, "TMEM columns");
-    static_assert(STAGE % 1024 == 0 && B % 1024 == 0, "alignment");
+    static_assert(STAGE % 1024 == 0 && B % 1024 == 0 && OUT >= ips::TURN_BYTES, "alignment");
 };
+
+// The barriers guard what the asynchronous units read and write (tiles, scales, accumulators), never
+// generic accesses, so neither waits nor arrivals order any: a pair's arrivals on the first CTA's
+// barriers with the release of the cluster take 0.7 us each (12000 x 16384 -> 1024: 164 us, relaxed 87).
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n"
+        " selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+// Bounded wait that also ends when another role of the CTA has given up.
+__device__ __forceinline__ bool wait_or_dead(uint32_t bar, uint32_t parity, volatile int *dead, long long limit) {
+    if (try_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+    while (!try_wait(bar, parity)) {
+        if (*dead) return false;
+        if (clock64() - t0 > limit) {
+            *dead = 1;
+            return false;
+        }
+    }
+    return true;
+}
+__device__ __forceinline__ bool warp_wait_or_dead(uint32_t bar, uint32_t parity, volatile int *dead, long long limit) {
+    return __all_sync(0xffffffffu, wait_or_dead(bar, parity, dead, limit)) != 0;
+}
+
+template <bool PAIR>
+__device__ __forceinline__ void arrive_first(uint32_t bar) {
+    if (PAIR)
+        asm volatile(
+            "{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, 0;\n"
+            " mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [r];\n}\n" ::"r"(bar)
+            : "memory");
+    else
+        mbar_arrive(bar);
+}
 
 // Scales of 128 rows x 64 elements to four TMEM columns, in all four quarters of the lanes.
 template <bool PAIR>
@@ -95,16 +138,70 @@ __device__ __forceinline__ void mma_fp4(uint32_t d, uint64_t a, uint64_t b, uint
             "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
             : "memory");
 }
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, int bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-                 "l"(src), "r"(bytes), "r"(bar)
-                 : "memory");
+// This shared-memory offset in the pair's first CTA, as an address of the cluster.
+__device__ __forceinline__ uint32_t of_first(uint32_t addr) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+    return r;
+}
+__device__ __forceinline__ uint32_t of_other(uint32_t addr, int rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank ^ 1));
+    return r;
+}
+// Tile loads that report to a barrier of the pair's first CTA (`bar`: of_first).
+template <bool PAIR>
+__device__ __forceinline__ void load_2d(uint32_t dst, const CUtensorMap *map, int c0, int c1, uint32_t bar) {
+    if (PAIR)
+        asm volatile(
+            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+            " [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+            "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(bar)
+            : "memory");
+    else
+        tma_load_2d(dst, map, c0, c1, bar);
+}
+template <bool PAIR>
+__device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, uint32_t bar) {
+    if (PAIR)
+        asm volatile(
+            "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+            " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+            "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+            : "memory");
+    else
+        tma_load_3d(dst, map, c0, c1, c2, bar);
+}
+template <bool PAIR>
+__device__ __forceinline__ void expect_first(uint32_t bar, uint32_t bytes) {      // bar: of_first
+    if (PAIR)
+        asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
+                     : "memory");
+    else
+        mbar_expect_tx(bar, bytes);
 }
 
-// ODD: output rows that are not aligned to 8 bytes, or an N that 16 does not divide.
+// Block of 32 rows x 128 bytes to the output, from shared memory in the 128-byte swizzled layout.
+__device__ __forceinline__ void store_block(const CUtensorMap *map, uint32_t src, int n, int m) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
+                     reinterpret_cast<uint64_t>(map)),
+                 "r"(n), "r"(m), "r"(src)
+                 : "memory");
+}
+// At most N of this thread's blocks are still being read (N = 0: none is still on its way).
+template <int N>
+__device__ __forceinline__ void blocks_left() {
+    if (N > 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+    else asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+}
+
+// Output leaves by TMA in blocks of 128 bytes a row (BN = 64: in whole sectors from the registers).
+// ODD: rows or an N for which that cannot be (16 bytes; BN = 64: 8 bytes, 16 columns).
 template <typename T, int BN, bool PAIR, bool ODD>
 __global__ void __launch_bounds__(THREADS, 1)
-    fp4_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const Params prm) {
+    fp4_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w,
+               const __grid_constant__ CUtensorMap tm_xb, const __grid_constant__ CUtensorMap tm_wb,
+               const __grid_constant__ CUtensorMap tm_y, const Params prm) {
     using C = Tile<BN, PAIR>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>(
@@ -112,19 +209,17 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t base = smem_u32(smem);
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     auto full = [&](int s) { return base + 8u * s; };
-    auto peer = [&](int s) { return base + 8u * (C::ST + s); };      // the second CTA's stages, told to the first
-    auto empty = [&](int s) { return base + 8u * (2 * C::ST + s); };
-    auto acc_full = [&](int s) { return base + 8u * (3 * C::ST + s); };
-    auto acc_empty = [&](int s) { return base + 8u * (3 * C::ST + 2 + s); };
-    const uint32_t drained = base + 8u * (3 * C::ST + 4), never = drained + 8u;
+    auto empty = [&](int s) { return base + 8u * (C::ST + s); };
+    auto acc_full = [&](int s) { return base + 8u * (2 * C::ST + s); };
+    auto acc_empty = [&](int s) { return base + 8u * (2 * C::ST + 2 + s); };
+    const uint32_t drained = base + 8u * (2 * C::ST + 4), never = drained + 8u;
     volatile int *dead = reinterpret_cast<volatile int *>(smem + C::DEAD);
     const int rank = PAIR ? static_cast<int>(blockIdx.x & 1u) : 0;      // clusters are (2, 1, 1)
     const long long worker = blockIdx.x / C::CTAS, workers = gridDim.x / C::CTAS;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::ST; ++s) {
-            mbar_init(full(s), 1);
-            mbar_init(peer(s), 1);
+            mbar_init(full(s), C::CTAS);
             mbar_init(empty(s), 1);
         }
         for (int s = 0; s < 2; ++s) {
@@ -153,92 +248,90 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int stages = (prm.steps + 3) / 4;
     const long long limit = prm.timeout_cycles;
 
+    int issued = 0;       // stages that this CTA has fetched (the fetching thread)
     if (warp == TMA_WARP) {
         if (lane == 0) {
             int s = 0, ph = 0;
-            long long issued = 0;
             bool ok = true;
             for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
                 const int mt = static_cast<int>(tile / prm.tiles_n) * C::CTAS + rank;
                 const int n0 = static_cast<int>(tile % prm.tiles_n) * BN;
-                // scales of tiles behind the last (rows and channels that are not written): the last's
-                const uint8_t *xb = prm.xb + static_cast<long long>(mt < prm.xtiles ? mt : prm.xtiles - 1) * prm.steps * 512;
                 for (int it = 0; it < stages; ++it) {
-                    ok = wait_or_dead<false>(empty(s), ph ^ 1, dead, limit);
+                    ok = wait_or_dead(empty(s), ph ^ 1, dead, limit);
                     if (!ok) break;
-                    const uint32_t st = base + C::STAGES_AT + s * C::STAGE;
-                    const int left = prm.steps - 4 * it, sc = (left < 4 ? left : 4) * 512;
-                    mbar_expect_tx(full(s), C::A + C::B + (1 + C::WT) * sc);
-                    tma_load_2d(st, &tm_x, it * BKB, mt * TILE_M, full(s));
-                    tma_load_2d(st + C::A, &tm_w, it * BKB, n0 + rank * C::BR, full(s));
-                    bulk_load(st + C::A + C::B, xb + it * 2048, sc, full(s));
-#pragma unroll
-                    for (int j = 0; j < C::WT; ++j) {
-                        const int wt = n0 / 128 + j;
-                        bulk_load(st + C::A + C::B + C::SA + 2048 * j,
-                                  prm.wb + static_cast<long long>(wt < prm.wtiles ? wt : prm.wtiles - 1) * prm.steps * 512 + it * 2048,
-                                  sc, full(s));
-                    }
+                    const uint32_t st = base + C::STAGES_AT + s * C::STAGE, bar = PAIR ? of_first(full(s)) : full(s);
+                    expect_first<PAIR>(bar, C::STAGE);
+                    load_2d<PAIR>(st, &tm_x, it * BKB, mt * TILE_M, bar);
+                    load_2d<PAIR>(st + C::A, &tm_w, it * BKB, n0 + rank * C::BR, bar);
+                    load_3d<PAIR>(st + C::A + C::B, &tm_xb, 0, 4 * it, mt, bar);
+                    load_3d<PAIR>(st + C::A + C::B + C::SA, &tm_wb, 0, 4 * it, n0 / 128, bar);
                     ++issued;
                     if (++s == C::ST) s = 0, ph ^= 1;
                 }
             }
-            // after a wait that ran out: the copies in flight land before the CTA ends
-            if (!ok)
-                for (long long i = issued > C::ST ? issued - C::ST : 0; i < issued; ++i)
-                    mbar_wait(full(static_cast<int>(i % C::ST)), static_cast<uint32_t>((i / C::ST) & 1), ips::LAND_CYCLES);
         }
     } else if (warp == MMA_WARP) {
-        // the whole warp runs the loop, so that the descriptors stay uniform; one lane issues
-        // e2m1 x e2m1, e4m3 scales
-        constexpr uint32_t idesc = (1u << 7) | (1u << 10) | (static_cast<uint32_t>(BN / 8) << 17) |
-                                   (static_cast<uint32_t>(TILE_M * C::CTAS / 16) << 24);
-        int s = 0, ph = 0, a = 0, aph = 0;
-        bool ok = true;
-        for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
-            if (rank == 0) ok = warp_wait_or_dead<PAIR>(acc_empty(a), aph ^ 1, dead, limit);
-            if (!ok) break;
-            const int n0 = static_cast<int>(tile % prm.tiles_n) * BN;
-            for (int it = 0; it < stages; ++it) {
-                ok = warp_wait_or_dead<false>(full(s), ph, dead, limit);
+        if (rank == 0 && worker < prm.tiles) {
+            // the whole warp runs the loop, so that the descriptors stay uniform; one lane issues.
+            // e2m1 x e2m1, e4m3 scales
+            constexpr uint32_t idesc = (1u << 7) | (1u << 10) | (static_cast<uint32_t>(BN / 8) << 17) |
+                                       (static_cast<uint32_t>(TILE_M * C::CTAS / 16) << 24);
+            auto steps_of = [&](int it) { return prm.steps - 4 * it < 4 ? prm.steps - 4 * it : 4; };
+            // waits for a stage and copies its scales to TMEM
+            auto take = [&](int s, int ph, int it) {
+                if (!warp_wait_or_dead(full(s), ph, dead, limit)) return false;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t sa = tmem + C::SF + s * C::SF_COLS, st = base + C::STAGES_AT + s * C::STAGE + C::A + C::B;
+                const int nk = steps_of(it);
+                if (elect_one())
+                    for (int k = 0; k < nk; ++k) {
+                        copy_scales<PAIR>(sa + 4 * k, st + 512 * k);
+#pragma unroll
+                        for (int j = 0; j < C::WT; ++j)
+                            copy_scales<PAIR>(sa + 16 + 4 * (k * C::WT + j), st + C::SA + 2048 * j + 512 * k);
+                    }
+                __syncwarp();
+                return true;
+            };
+            int s = 0, ph = 0, a = 0, aph = 0;
+            bool ok = take(0, 0, 0);
+            for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
+                ok = warp_wait_or_dead(acc_empty(a), aph ^ 1, dead, limit);
                 if (!ok) break;
-                if (PAIR && rank == 1) {
-                    if (lane == 0) arrive_first<PAIR>(peer(s));
-                } else {
-                    if (PAIR) ok = warp_wait_or_dead<PAIR>(peer(s), ph, dead, limit);
-                    if (!ok) break;
+                const int n0 = static_cast<int>(tile % prm.tiles_n) * BN;
+                for (int it = 0; it < stages; ++it) {
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t st = base + C::STAGES_AT + s * C::STAGE;
                     const uint64_t da = smem_desc(st), db = smem_desc(st + C::A);
-                    const uint32_t sa = tmem + C::SF + s * C::SF_COLS, sb = sa + 16;
-                    const int nk = prm.steps - 4 * it < 4 ? prm.steps - 4 * it : 4;
+                    const uint32_t sa = tmem + C::SF + s * C::SF_COLS, sb = sa + 16 + (n0 % 128) / 32;
+                    const int nk = steps_of(it), nh = nk / 2;
+                    auto mma = [&](int k) {
+                        mma_fp4<PAIR>(tmem + a * BN, da + 2 * k, db + 2 * k, idesc, sa + 4 * k, sb + 4 * C::WT * k, it > 0 || k > 0);
+                    };
+                    if (elect_one())
+                        for (int k = 0; k < nh; ++k) mma(k);
+                    __syncwarp();
+                    // the next stage's scales go between this one's MMAs, whose time hides the copies'
+                    const int ns = s + 1 == C::ST ? 0 : s + 1, nph = ph ^ (ns == 0);
+                    if (it + 1 < stages || tile + workers < prm.tiles) ok = take(ns, nph, it + 1 < stages ? it + 1 : 0);
                     if (elect_one()) {
-                        for (int k = 0; k < nk; ++k) {
-                            copy_scales<PAIR>(sa + 4 * k, st + C::A + C::B + 512 * k);
-#pragma unroll
-                            for (int j = 0; j < C::WT; ++j)
-                                copy_scales<PAIR>(sb + 4 * (k * C::WT + j), st + C::A + C::B + C::SA + 2048 * j + 512 * k);
-                        }
-                        for (int k = 0; k < nk; ++k)
-                            mma_fp4<PAIR>(tmem + a * BN, da + 2 * k, db + 2 * k, idesc, sa + 4 * k,
-                                          sb + 4 * C::WT * k + (n0 % 128) / 32, it > 0 || k > 0);
+                        for (int k = nh; k < nk; ++k) mma(k);
                         mma_commit<PAIR>(empty(s));
                     }
                     __syncwarp();
+                    if (!ok) break;
+                    s = ns, ph = nph;
                 }
-                if (++s == C::ST) s = 0, ph ^= 1;
-            }
-            if (!ok) break;
-            if (rank == 0) {
+                if (!ok) break;
                 if (elect_one()) mma_commit<PAIR>(acc_full(a));
                 __syncwarp();
+                if (++a == C::ACCS) a = 0, aph ^= 1;
             }
-            if (++a == C::ACCS) a = 0, aph ^= 1;
-        }
-        if (!ok && rank == 0) {   // the MMAs in flight end before their TMEM is freed
-            if (elect_one()) mma_commit<PAIR>(drained);
-            __syncwarp();
-            mbar_wait(drained, 0, ips::LAND_CYCLES);
+            if (!ok) {   // the MMAs in flight end before their TMEM is freed
+                if (elect_one()) mma_commit<PAIR>(drained);
+                __syncwarp();
+                mbar_wait(drained, 0, ips::LAND_CYCLES);
+            }
         }
     } else {
         const int quarter = warp & 3, half = warp >> 2;
@@ -246,12 +339,13 @@ __global__ void __launch_bounds__(THREADS, 1)
         const int col0 = half * CW;
         const unsigned low = static_cast<unsigned>(reinterpret_cast<uintptr_t>(prm.y) | (prm.ldy * sizeof(T))) & 31u;
         const bool wide = low == 0, even = (low & 7u) == 0;
-        const uint32_t cst = base + C::CONSTS + warp * (8 * CW);
+        constexpr bool BLOCKS = BN >= 128 && !ODD;
+        const uint32_t cst = base + C::CONSTS + warp * (8 * CW), out = base + C::OUT_AT + warp * C::OUT;
         int a = 0, aph = 0;
         bool ok = true;
-        if (prm.stall) ok = warp_wait_or_dead<false>(never, 0, dead, limit);
+        if (prm.stall) ok = warp_wait_or_dead(never, 0, dead, limit);
         for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
-            const long long m = (tile / prm.tiles_n * C::CTAS + rank) * TILE_M + quarter * 32 + lane;
+            const long long first = (tile / prm.tiles_n * C::CTAS + rank) * TILE_M + quarter * 32, m = first + lane;
             const int n0 = static_cast<int>(tile % prm.tiles_n) * BN + col0;
             __syncwarp();
             for (int c = lane; c < CW; c += 32) {
@@ -262,7 +356,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             __syncwarp();
             const float sx = m < prm.M ? prm.sx[m] : 0.0f;
             T *row = static_cast<T *>(prm.y) + (m < prm.M ? m : 0) * prm.ldy;
-            ok = warp_wait_or_dead<PAIR>(acc_full(a), aph, dead, limit);
+            ok = warp_wait_or_dead(acc_full(a), aph, dead, limit);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             uint32_t r[CW / 16][16];
@@ -290,21 +384,64 @@ __global__ void __launch_bounds__(THREADS, 1)
                 if (prm.act)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) z[i] = ips::swish<T>(z[i]);
-                if (ODD && (!even || n0 + c + 16 > prm.N)) {
-                    const long long first = m - lane, left = prm.M - first;
+                if (BLOCKS) {
+                    constexpr int PER = 128 / sizeof(T) / 16;      // chunks of 16 columns a block
+                    const int part = ch % PER;
+                    const uint32_t block = out + (ch / PER & 1) * 4096;
+                    if (part == 0) {
+                        if (lane == 0) blocks_left<1>();
+                        __syncwarp();
+                    }
+                    union { T e[16]; uint32_t w[4 * sizeof(T)]; } v;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) v.e[j] = from_f32<T>(z[j]);
+#pragma unroll
+                    for (int j = 0; j < static_cast<int>(sizeof(T)); ++j)
+                        sts128(block + swz(lane, part * sizeof(T) + j), v.w[4 * j], v.w[4 * j + 1], v.w[4 * j + 2], v.w[4 * j + 3]);
+                    if (part == PER - 1) {
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        const int n = n0 + c + 16 - 16 * PER;
+                        if (lane == 0) {
+                            if (first < prm.M && n < prm.N) store_block(&tm_y, block, n, static_cast<int>(first));
+                            // a block that is left out counts too, or its neighbour's buffer would seem free
+                            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                        }
+                    }
+                } else if (ODD && (!even || n0 + c + 16 > prm.N)) {
+                    const long long left = prm.M - first;
                     if (n0 + c < prm.N)
                         ips::store_odd<T>(static_cast<T *>(prm.y) + first * prm.ldy + n0 + c, prm.ldy,
-                                          left < 32 ? static_cast<int>(left) : 32, prm.N - n0 - c,
-                                          base + C::TURN + warp * ips::TURN_BYTES, z);
+                                          left < 32 ? static_cast<int>(left) : 32, prm.N - n0 - c, out, z);
                 } else if (m < prm.M && n0 + c < prm.N) {
                     ips::store16<T>(row, n0 + c, wide, z);
                 }
             }
         }
+        if (BLOCKS && lane == 0) blocks_left<0>();
     }
     __syncwarp();
-    if (PAIR) cluster_sync();     // neither CTA ends while the other may still arrive on its barriers
-    else __syncthreads();
+    // After a wait that ran out the copies in flight land before a CTA ends.  A pair's report to the first
+    // CTA's barriers, each CTA for itself: a stage that one of them alone has fetched lacks an arrival.
+    volatile int *other = reinterpret_cast<volatile int *>(smem + C::OTHER);
+    if (PAIR) {
+        __syncthreads();
+        if (warp == TMA_WARP && lane == 0) {
+            const uint32_t at = of_other(base + C::OTHER, rank);
+            asm volatile("st.shared::cluster.v2.s32 [%0], {%1, %2};" ::"r"(at), "r"(*dead), "r"(issued) : "memory");
+        }
+        cluster_sync();
+    }
+    if (warp == TMA_WARP && lane == 0 && rank == 0 && (*dead || (PAIR && other[0]))) {
+        const int theirs = PAIR ? other[1] : issued, last = issued > theirs ? issued : theirs;
+        for (int i = last > C::ST ? last - C::ST : 0; i < last; ++i) {
+            if (PAIR && (i >= issued || i >= theirs)) mbar_arrive(full(i % C::ST));
+            mbar_wait(full(i % C::ST), static_cast<uint32_t>((i / C::ST) & 1), ips::LAND_CYCLES);
+        }
+    }
+    __syncwarp();
+    if (PAIR && (*dead || other[0])) cluster_sync();      // the same in both CTAs
+    if (!PAIR) __syncthreads();
     if (warp == MMA_WARP) tmem_free<PAIR>(tmem, C::COLS);
     if (threadIdx.x == 0 && *dead) atomicOr(prm.err, ips::ERR_TIMEOUT);
 }
