@@ -58,15 +58,15 @@ bool make_scale_map(CUtensorMap *m, const void *base, int steps, long long rows,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The output's rows, boxes of 128 bytes x 32 rows in the 128-byte swizzled layout.
+// The output's rows, boxes of 64 bytes x 32 rows in the 64-byte swizzled layout.
 bool make_out_map(CUtensorMap *m, void *y, CUtensorMapDataType type, int es, int N, long long rows, long long ld) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(N), static_cast<cuuint64_t>(rows)};
     const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * es};
-    const cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / es), 32};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(64 / es), 32};
     const cuuint32_t estride[2] = {1, 1};
-    return fn(m, type, 2, y, dims, strides, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+    return fn(m, type, 2, y, dims, strides, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
               CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -107,7 +107,11 @@ int launch(const CUtensorMap (&maps)[5], const ip4::Params &prm, int nsm, cudaSt
     {
         std::lock_guard<std::mutex> lock(g_mu);
         if (!set[dev]) {
-            if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return IP_ERR_CUDA;
+            // the kernel deals out REGS registers a thread: never launch a build with fewer
+            cudaFuncAttributes attr;
+            if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess ||
+                cudaFuncGetAttributes(&attr, fn) != cudaSuccess || (BN == 256 && attr.numRegs < ip4::REGS))
+                return IP_ERR_CUDA;
             set[dev] = true;
         }
     }

@@ -17,20 +17,21 @@ using ips::elect_one, ips::cluster_sync, ips::mma_commit, ips::tmem_alloc, ips::
 // tcgen05.mma kind::mxf4nvf4 with a scale for each 16 elements: products and scales are exact there, sums
 // in f32.
 //
-// Roles of a persistent CTA (one an SM): warp 8 fetches stages of 256 elements of K by TMA (128 rows of
+// Roles of a persistent CTA (one an SM): warp 12 fetches stages of 256 elements of K by TMA (128 rows of
 // x and BN channels of w, 128 bytes each in the 128-byte swizzled layout, and their scales as they
-// lie in memory, 512 bytes for 128 rows x 64 elements), one thread of warp 9 copies the scales to TMEM
-// (tcgen05.cp) and issues the MMAs of 64 elements each, warps 0-7 take the sums to registers, release
+// lie in memory, 512 bytes for 128 rows x 64 elements), warps 8-11 copy the scales to TMEM, one
+// thread of warp 13 issues the MMAs of 64 elements each, warps 0-7 take the sums to registers, release
 // the accumulator and write the output while the next tile is summed.
 // PAIR: two CTAs share a tile of 256 rows x BN channels (cta_group::2), each fetching its 128 rows and half of
 // the channels; the scales of all channels go to both.  Both CTAs' copies report to the first one's
-// barriers, whose warp 9 issues for both.
+// barriers, whose warp 13 issues for both.
 
 constexpr int TILE_M = 128;
 constexpr int BKB = 128;                 // bytes of a row in a stage
 constexpr int BK = 256;                  // elements
-constexpr int THREADS = 320;
-constexpr int EPI_WARPS = 8, TMA_WARP = 8, MMA_WARP = 9;
+constexpr int THREADS = 512;             // four warpgroups (registers are dealt by warpgroup)
+constexpr int REGS = 128;                // registers a thread at launch
+constexpr int EPI_WARPS = 8, SCALE_WARP = 8, TMA_WARP = 12, MMA_WARP = 13;
 
 struct Params {
     const float *sx, *sw, *bias;
@@ -53,21 +54,19 @@ struct Tile {
     static constexpr int WT = BN <= 128 ? 1 : BN / 128;      // tiles of scales of w
     static constexpr int A = TILE_M * BKB, B = BR * BKB, SA = 2048, SB = 2048 * WT;
     static constexpr int STAGE = A + B + SA + SB;
-    static constexpr int ST = BN == 64 ? 6 : 4;
+    static constexpr int ST = BN == 64 ? 6 : 5;
     static constexpr int ACCS = BN == 256 ? 1 : 2;    // accumulators
     static constexpr int SF = ACCS * BN;              // first column of the scales
     static constexpr int SF_COLS = 16 + 16 * WT;      // of a stage
     static constexpr int COLS = 512;
     static constexpr int TMEM_PTR = 256, DEAD = 260;
     static constexpr int OTHER = 264;                 // of the other CTA of a pair: given up, stages fetched
-    static constexpr int CONSTS = 512;                // per output warp: sw and bias of its columns
-    static constexpr int TURN = CONSTS + EPI_WARPS * 2 * 4 * (BN / 2);
-    // per output warp: two blocks of 32 rows x 128 bytes on their way out (store_odd's block in their place)
-    static constexpr int OUT_AT = (TURN + 1023) & ~1023;
-    static constexpr int OUT = BN == 64 ? ((ips::TURN_BYTES + 127) & ~127) : 8192;
-    static constexpr int STAGES_AT = (OUT_AT + EPI_WARPS * OUT + 1023) & ~1023;
+    static constexpr int CONSTS = 512;                // sw and bias of a tile's columns
+    // per output warp: two blocks of 32 rows x 64 bytes on their way out, or store_odd's block
+    static constexpr int OUT_AT = (CONSTS + 8 * BN + 1023) & ~1023, OUT = 4096;
+    static constexpr int STAGES_AT = OUT_AT + EPI_WARPS * OUT;
     static constexpr int SMEM = STAGES_AT + ST * STAGE + 1024;
-    static_assert(8 * (2 * ST + 6) <= 256, "barriers");
+    static_assert(8 * (4 * ST + 6) <= 256, "barriers");
     static_assert(SMEM <= 232448, "shared memory");
     static_assert(SF + ST * SF_COLS <= COLS, "TMEM columns");
     static_assert(STAGE % 1024 == 0 && B % 1024 == 0 && OUT >= ips::TURN_BYTES, "alignment");
@@ -114,13 +113,12 @@ __device__ __forceinline__ void arrive_first(uint32_t bar) {
         mbar_arrive(bar);
 }
 
-// Scales of 128 rows x 64 elements to four TMEM columns, in all four quarters of the lanes.
-template <bool PAIR>
-__device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t smem) {
-    // rows of 16 bytes without swizzle, groups of eight rows 128 bytes apart
-    const uint64_t desc = static_cast<uint64_t>((smem & 0x3ffff) >> 4) | (8ull << 16) | (8ull << 32) | (1ull << 46);
-    if (PAIR) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
-    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint4 (&v)[4]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),
+        "r"(v[0].x), "r"(v[0].y), "r"(v[0].z), "r"(v[0].w), "r"(v[1].x), "r"(v[1].y), "r"(v[1].z), "r"(v[1].w),
+        "r"(v[2].x), "r"(v[2].y), "r"(v[2].z), "r"(v[2].w), "r"(v[3].x), "r"(v[3].y), "r"(v[3].z), "r"(v[3].w)
+        : "memory");
 }
 template <bool PAIR>
 __device__ __forceinline__ void mma_fp4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
@@ -162,17 +160,6 @@ __device__ __forceinline__ void load_2d(uint32_t dst, const CUtensorMap *map, in
         tma_load_2d(dst, map, c0, c1, bar);
 }
 template <bool PAIR>
-__device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, uint32_t bar) {
-    if (PAIR)
-        asm volatile(
-            "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
-            " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-            "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
-            : "memory");
-    else
-        tma_load_3d(dst, map, c0, c1, c2, bar);
-}
-template <bool PAIR>
 __device__ __forceinline__ void expect_first(uint32_t bar, uint32_t bytes) {      // bar: of_first
     if (PAIR)
         asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
@@ -181,7 +168,17 @@ __device__ __forceinline__ void expect_first(uint32_t bar, uint32_t bytes) {    
         mbar_expect_tx(bar, bytes);
 }
 
-// Block of 32 rows x 128 bytes to the output, from shared memory in the 128-byte swizzled layout.
+// Whether all 128 threads that meet at this barrier say so.
+__device__ __forceinline__ bool all_of_half(bool ok, int bar) {
+    uint32_t r;
+    asm volatile(
+        "{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n bar.red.and.pred q, %2, 128, p;\n selp.u32 %0, 1, 0, q;\n}\n"
+        : "=r"(r)
+        : "r"(static_cast<uint32_t>(ok)), "r"(bar)
+        : "memory");
+    return r != 0;
+}
+// Block of 32 rows x 64 bytes to the output, from shared memory in the 64-byte swizzled layout.
 __device__ __forceinline__ void store_block(const CUtensorMap *map, uint32_t src, int n, int m) {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
                      reinterpret_cast<uint64_t>(map)),
@@ -195,7 +192,7 @@ __device__ __forceinline__ void blocks_left() {
     else asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
 }
 
-// Output leaves by TMA in blocks of 128 bytes a row (BN = 64: in whole sectors from the registers).
+// Output leaves by TMA in blocks of 64 bytes a row (BN = 64: in whole sectors from the registers).
 // ODD: rows or an N for which that cannot be (16 bytes; BN = 64: 8 bytes, 16 columns).
 template <typename T, int BN, bool PAIR, bool ODD>
 __global__ void __launch_bounds__(THREADS, 1)
@@ -203,6 +200,9 @@ __global__ void __launch_bounds__(THREADS, 1)
                const __grid_constant__ CUtensorMap tm_xb, const __grid_constant__ CUtensorMap tm_wb,
                const __grid_constant__ CUtensorMap tm_y, const Params prm) {
     using C = Tile<BN, PAIR>;
+    // 256 columns are 128 registers of an output thread: its warpgroups take over what the others can
+    // spare, 2 x 200 + 2 x 56 = 4 x 128
+    constexpr bool DEAL = BN == 256;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -210,9 +210,11 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     auto full = [&](int s) { return base + 8u * s; };
     auto empty = [&](int s) { return base + 8u * (C::ST + s); };
-    auto acc_full = [&](int s) { return base + 8u * (2 * C::ST + s); };
-    auto acc_empty = [&](int s) { return base + 8u * (2 * C::ST + 2 + s); };
-    const uint32_t drained = base + 8u * (2 * C::ST + 4), never = drained + 8u;
+    auto scales = [&](int s) { return base + 8u * (2 * C::ST + s); };      // have landed, in each CTA
+    auto ready = [&](int s) { return base + 8u * (3 * C::ST + s); };       // are in TMEM
+    auto acc_full = [&](int s) { return base + 8u * (4 * C::ST + s); };
+    auto acc_empty = [&](int s) { return base + 8u * (4 * C::ST + 2 + s); };
+    const uint32_t drained = base + 8u * (4 * C::ST + 4), never = drained + 8u;
     volatile int *dead = reinterpret_cast<volatile int *>(smem + C::DEAD);
     const int rank = PAIR ? static_cast<int>(blockIdx.x & 1u) : 0;      // clusters are (2, 1, 1)
     const long long worker = blockIdx.x / C::CTAS, workers = gridDim.x / C::CTAS;
@@ -221,6 +223,8 @@ __global__ void __launch_bounds__(THREADS, 1)
         for (int s = 0; s < C::ST; ++s) {
             mbar_init(full(s), C::CTAS);
             mbar_init(empty(s), 1);
+            mbar_init(scales(s), 1);
+            mbar_init(ready(s), 4 * C::CTAS);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(acc_full(s), 1);
@@ -248,6 +252,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int stages = (prm.steps + 3) / 4;
     const long long limit = prm.timeout_cycles;
 
+    if (DEAL && warp >= SCALE_WARP) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     int issued = 0;       // stages that this CTA has fetched (the fetching thread)
     if (warp == TMA_WARP) {
         if (lane == 0) {
@@ -260,15 +265,20 @@ __global__ void __launch_bounds__(THREADS, 1)
                     ok = wait_or_dead(empty(s), ph ^ 1, dead, limit);
                     if (!ok) break;
                     const uint32_t st = base + C::STAGES_AT + s * C::STAGE, bar = PAIR ? of_first(full(s)) : full(s);
-                    expect_first<PAIR>(bar, C::STAGE);
+                    mbar_expect_tx(scales(s), C::SA + C::SB);
+                    tma_load_3d(st + C::A + C::B, &tm_xb, 0, 4 * it, mt, scales(s));
+                    tma_load_3d(st + C::A + C::B + C::SA, &tm_wb, 0, 4 * it, n0 / 128, scales(s));
+                    expect_first<PAIR>(bar, C::A + C::B);
                     load_2d<PAIR>(st, &tm_x, it * BKB, mt * TILE_M, bar);
                     load_2d<PAIR>(st + C::A, &tm_w, it * BKB, n0 + rank * C::BR, bar);
-                    load_3d<PAIR>(st + C::A + C::B, &tm_xb, 0, 4 * it, mt, bar);
-                    load_3d<PAIR>(st + C::A + C::B + C::SA, &tm_wb, 0, 4 * it, n0 / 128, bar);
                     ++issued;
                     if (++s == C::ST) s = 0, ph ^= 1;
                 }
             }
+            // after a wait that ran out the copies in flight land before the CTA ends (the others: below)
+            if (!ok)
+                for (int i = issued > C::ST ? issued - C::ST : 0; i < issued; ++i)
+                    mbar_wait(scales(i % C::ST), static_cast<uint32_t>((i / C::ST) & 1), ips::LAND_CYCLES);
         }
     } else if (warp == MMA_WARP) {
         if (rank == 0 && worker < prm.tiles) {
@@ -276,51 +286,27 @@ __global__ void __launch_bounds__(THREADS, 1)
             // e2m1 x e2m1, e4m3 scales
             constexpr uint32_t idesc = (1u << 7) | (1u << 10) | (static_cast<uint32_t>(BN / 8) << 17) |
                                        (static_cast<uint32_t>(TILE_M * C::CTAS / 16) << 24);
-            auto steps_of = [&](int it) { return prm.steps - 4 * it < 4 ? prm.steps - 4 * it : 4; };
-            // waits for a stage and copies its scales to TMEM
-            auto take = [&](int s, int ph, int it) {
-                if (!warp_wait_or_dead(full(s), ph, dead, limit)) return false;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t sa = tmem + C::SF + s * C::SF_COLS, st = base + C::STAGES_AT + s * C::STAGE + C::A + C::B;
-                const int nk = steps_of(it);
-                if (elect_one())
-                    for (int k = 0; k < nk; ++k) {
-                        copy_scales<PAIR>(sa + 4 * k, st + 512 * k);
-#pragma unroll
-                        for (int j = 0; j < C::WT; ++j)
-                            copy_scales<PAIR>(sa + 16 + 4 * (k * C::WT + j), st + C::SA + 2048 * j + 512 * k);
-                    }
-                __syncwarp();
-                return true;
-            };
             int s = 0, ph = 0, a = 0, aph = 0;
-            bool ok = take(0, 0, 0);
+            bool ok = true;
             for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
                 ok = warp_wait_or_dead(acc_empty(a), aph ^ 1, dead, limit);
                 if (!ok) break;
                 const int n0 = static_cast<int>(tile % prm.tiles_n) * BN;
                 for (int it = 0; it < stages; ++it) {
+                    ok = warp_wait_or_dead(ready(s), ph, dead, limit) && warp_wait_or_dead(full(s), ph, dead, limit);
+                    if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t st = base + C::STAGES_AT + s * C::STAGE;
                     const uint64_t da = smem_desc(st), db = smem_desc(st + C::A);
                     const uint32_t sa = tmem + C::SF + s * C::SF_COLS, sb = sa + 16 + (n0 % 128) / 32;
-                    const int nk = steps_of(it), nh = nk / 2;
-                    auto mma = [&](int k) {
-                        mma_fp4<PAIR>(tmem + a * BN, da + 2 * k, db + 2 * k, idesc, sa + 4 * k, sb + 4 * C::WT * k, it > 0 || k > 0);
-                    };
-                    if (elect_one())
-                        for (int k = 0; k < nh; ++k) mma(k);
-                    __syncwarp();
-                    // the next stage's scales go between this one's MMAs, whose time hides the copies'
-                    const int ns = s + 1 == C::ST ? 0 : s + 1, nph = ph ^ (ns == 0);
-                    if (it + 1 < stages || tile + workers < prm.tiles) ok = take(ns, nph, it + 1 < stages ? it + 1 : 0);
+                    const int nk = prm.steps - 4 * it < 4 ? prm.steps - 4 * it : 4;
                     if (elect_one()) {
-                        for (int k = nh; k < nk; ++k) mma(k);
+                        for (int k = 0; k < nk; ++k)
+                            mma_fp4<PAIR>(tmem + a * BN, da + 2 * k, db + 2 * k, idesc, sa + 4 * k, sb + 4 * C::WT * k, it > 0 || k > 0);
                         mma_commit<PAIR>(empty(s));
                     }
                     __syncwarp();
-                    if (!ok) break;
-                    s = ns, ph = nph;
+                    if (++s == C::ST) s = 0, ph ^= 1;
                 }
                 if (!ok) break;
                 if (elect_one()) mma_commit<PAIR>(acc_full(a));
@@ -333,31 +319,69 @@ __global__ void __launch_bounds__(THREADS, 1)
                 mbar_wait(drained, 0, ips::LAND_CYCLES);
             }
         }
+    } else if (warp >= TMA_WARP) {
+        // two warps without a role
+    } else if (warp >= SCALE_WARP) {
+        // Scales to TMEM: lane l of every quarter holds those of the rows l, l + 32, l + 64, l + 96, four columns
+        // for each 64 elements.  A stage's slot there is free when its shared memory is: its scales
+        // are fetched after the MMAs that read the ones before.
+        const uint32_t at = tmem + C::SF + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+        int s = 0, ph = 0;
+        bool ok = true;
+        for (long long tile = worker; ok && tile < prm.tiles; tile += workers)
+            for (int it = 0; it < stages; ++it) {
+                ok = warp_wait_or_dead(scales(s), ph, dead, limit);
+                if (!ok) break;
+                const uint32_t src = base + C::STAGES_AT + s * C::STAGE + C::A + C::B + 16 * lane;
+                uint4 v[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] = lds128(src + 512 * k);
+                tmem_st16(at + s * C::SF_COLS, v);
+#pragma unroll
+                for (int h = 0; h < C::WT; ++h) {
+                    // of x then w: columns 4 (WT k + j) for step k and tile j
+                    uint4 u[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int c = 4 * h + i, k = c / C::WT, j = c % C::WT;
+                        u[i] = lds128(src + C::SA + 2048 * j + 512 * k);
+                    }
+                    tmem_st16(at + s * C::SF_COLS + 16 + 16 * h, u);
+                }
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) arrive_first<PAIR>(ready(s));
+                if (++s == C::ST) s = 0, ph ^= 1;
+            }
     } else {
+        if (DEAL) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         const int quarter = warp & 3, half = warp >> 2;
         constexpr int CW = BN / 2;            // columns of a warp
         const int col0 = half * CW;
         const unsigned low = static_cast<unsigned>(reinterpret_cast<uintptr_t>(prm.y) | (prm.ldy * sizeof(T))) & 31u;
         const bool wide = low == 0, even = (low & 7u) == 0;
         constexpr bool BLOCKS = BN >= 128 && !ODD;
-        const uint32_t cst = base + C::CONSTS + warp * (8 * CW), out = base + C::OUT_AT + warp * C::OUT;
+        const uint32_t cst = base + C::CONSTS + half * (8 * CW), out = base + C::OUT_AT + warp * C::OUT;
         int a = 0, aph = 0;
         bool ok = true;
         if (prm.stall) ok = warp_wait_or_dead(never, 0, dead, limit);
         for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
             const long long first = (tile / prm.tiles_n * C::CTAS + rank) * TILE_M + quarter * 32, m = first + lane;
             const int n0 = static_cast<int>(tile % prm.tiles_n) * BN + col0;
-            __syncwarp();
-            for (int c = lane; c < CW; c += 32) {
-                const int n = n0 + c;
-                sts32(cst + 4 * c, __float_as_uint(n < prm.N ? prm.sw[n] : 0.0f));
-                sts32(cst + 4 * (CW + c), __float_as_uint(n < prm.N && prm.bias ? prm.bias[n] : 0.0f));
-            }
-            __syncwarp();
+            // each thread has the constants of one of the columns
+            const int cc = quarter * 32 + lane, cn = n0 + cc;
+            const bool in = cc < CW && cn < prm.N;
+            const float csw = in ? prm.sw[cn] : 0.0f, cb = in && prm.bias ? prm.bias[cn] : 0.0f;
             const float sx = m < prm.M ? prm.sx[m] : 0.0f;
             T *row = static_cast<T *>(prm.y) + (m < prm.M ? m : 0) * prm.ldy;
-            ok = warp_wait_or_dead(acc_full(a), aph, dead, limit);
+            // the four warps of these columns go on together, or none does
+            ok = all_of_half(warp_wait_or_dead(acc_full(a), aph, dead, limit), 1 + half);
             if (!ok) break;
+            if (cc < CW) {
+                sts32(cst + 4 * cc, __float_as_uint(csw));
+                sts32(cst + 4 * (CW + cc), __float_as_uint(cb));
+            }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             uint32_t r[CW / 16][16];
 #pragma unroll
@@ -368,6 +392,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             __syncwarp();
             if (lane == 0) arrive_first<PAIR>(acc_empty(a));
             if (++a == C::ACCS) a = 0, aph ^= 1;
+            asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");      // the constants are there
 #pragma unroll
             for (int ch = 0; ch < CW / 16; ++ch) {
                 const int c = 16 * ch;
@@ -385,9 +410,9 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) z[i] = ips::swish<T>(z[i]);
                 if (BLOCKS) {
-                    constexpr int PER = 128 / sizeof(T) / 16;      // chunks of 16 columns a block
+                    constexpr int PER = 64 / sizeof(T) / 16;      // chunks of 16 columns a block
                     const int part = ch % PER;
-                    const uint32_t block = out + (ch / PER & 1) * 4096;
+                    const uint32_t block = out + (ch / PER & 1) * 2048;
                     if (part == 0) {
                         if (lane == 0) blocks_left<1>();
                         __syncwarp();
@@ -397,7 +422,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                     for (int j = 0; j < 16; ++j) v.e[j] = from_f32<T>(z[j]);
 #pragma unroll
                     for (int j = 0; j < static_cast<int>(sizeof(T)); ++j)
-                        sts128(block + swz(lane, part * sizeof(T) + j), v.w[4 * j], v.w[4 * j + 1], v.w[4 * j + 2], v.w[4 * j + 3]);
+                        sts128(block + 64 * lane + (((part * static_cast<int>(sizeof(T)) + j) ^ (lane >> 1 & 3)) << 4), v.w[4 * j], v.w[4 * j + 1], v.w[4 * j + 2], v.w[4 * j + 3]);
                     if (part == PER - 1) {
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
