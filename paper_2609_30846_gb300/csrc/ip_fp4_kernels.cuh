@@ -17,21 +17,21 @@ using ips::elect_one, ips::cluster_sync, ips::mma_commit, ips::tmem_alloc, ips::
 // tcgen05.mma kind::mxf4nvf4 with a scale for each 16 elements: products and scales are exact there, sums
 // in f32.
 //
-// Roles of a persistent CTA (one an SM): warp 12 fetches stages of 256 elements of K by TMA (128 rows of
+// Roles of a persistent CTA (one an SM): warps 20, 22 and 23 fetch stages of 256 elements of K by TMA (128 rows of
 // x and BN channels of w, 128 bytes each in the 128-byte swizzled layout, and their scales as they
-// lie in memory, 512 bytes for 128 rows x 64 elements), warps 8-11 copy the scales to TMEM, one
-// thread of warp 13 issues the MMAs of 64 elements each, warps 0-7 take the sums to registers, release
+// lie in memory, 512 bytes for 128 rows x 64 elements), warps 16-19 copy the scales to TMEM, one
+// thread of warp 21 issues the MMAs of 64 elements each, warps 0-15 take the sums to registers, release
 // the accumulator and write the output while the next tile is summed.
 // PAIR: two CTAs share a tile of 256 rows x BN channels (cta_group::2), each fetching its 128 rows and half of
 // the channels; the scales of all channels go to both.  Both CTAs' copies report to the first one's
-// barriers, whose warp 13 issues for both.
+// barriers, whose warp 21 issues for both.
 
 constexpr int TILE_M = 128;
 constexpr int BKB = 128;                 // bytes of a row in a stage
 constexpr int BK = 256;                  // elements
-constexpr int THREADS = 512;             // four warpgroups (registers are dealt by warpgroup)
-constexpr int REGS = 128;                // registers a thread at launch
-constexpr int EPI_WARPS = 8, SCALE_WARP = 8, TMA_WARP = 12, MMA_WARP = 13;
+constexpr int THREADS = 768;             // six warpgroups (registers are dealt by warpgroup)
+constexpr int REGS = 80;                 // registers a thread at launch
+constexpr int EPI_WARPS = 16, SCALE_WARP = 16, X_WARP = 20, MMA_WARP = 21, W_WARP = 22, SCALES_WARP = 23;
 
 struct Params {
     const float *sx, *sw, *bias;
@@ -54,16 +54,17 @@ struct Tile {
     static constexpr int WT = BN <= 128 ? 1 : BN / 128;      // tiles of scales of w
     static constexpr int A = TILE_M * BKB, B = BR * BKB, SA = 2048, SB = 2048 * WT;
     static constexpr int STAGE = A + B + SA + SB;
-    static constexpr int ST = BN == 64 ? 6 : 5;
+    static constexpr int ST = BN == 64 || (BN == 128 && PAIR_) ? 6 : 5;
     static constexpr int ACCS = BN == 256 ? 1 : 2;    // accumulators
     static constexpr int SF = ACCS * BN;              // first column of the scales
     static constexpr int SF_COLS = 16 + 16 * WT;      // of a stage
     static constexpr int COLS = 512;
     static constexpr int TMEM_PTR = 256, DEAD = 260;
-    static constexpr int OTHER = 264;                 // of the other CTA of a pair: given up, stages fetched
+    static constexpr int FETCHED = 272;               // stages, of x and of w
+    static constexpr int OTHER = 288;                 // of the other CTA of a pair: given up, -, stages fetched
     static constexpr int CONSTS = 512;                // sw and bias of a tile's columns
-    // per output warp: two blocks of 32 rows x 64 bytes on their way out, or store_odd's block
-    static constexpr int OUT_AT = (CONSTS + 8 * BN + 1023) & ~1023, OUT = 4096;
+    // per output warp: a block of 32 rows x 64 bytes on its way out, or store_odd's block
+    static constexpr int OUT_AT = (CONSTS + 8 * BN + 1023) & ~1023, OUT = 2048;
     static constexpr int STAGES_AT = OUT_AT + EPI_WARPS * OUT;
     static constexpr int SMEM = STAGES_AT + ST * STAGE + 1024;
     static_assert(8 * (4 * ST + 6) <= 256, "barriers");
@@ -169,7 +170,7 @@ __device__ __forceinline__ void expect_first(uint32_t bar, uint32_t bytes) {    
 }
 
 // Whether all 128 threads that meet at this barrier say so.
-__device__ __forceinline__ bool all_of_half(bool ok, int bar) {
+__device__ __forceinline__ bool all_of_group(bool ok, int bar) {
     uint32_t r;
     asm volatile(
         "{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n bar.red.and.pred q, %2, 128, p;\n selp.u32 %0, 1, 0, q;\n}\n"
@@ -178,6 +179,32 @@ __device__ __forceinline__ bool all_of_half(bool ok, int bar) {
         : "memory");
     return r != 0;
 }
+// Four of z / (1 + exp(-z)) as ips::swish forms it; for 16-bit outputs by one reciprocal, that of the product of the
+// four denominators, in [1, 16] (the special unit is what bounds them: five for eight).
+template <typename T>
+__device__ __forceinline__ void swish4(float &z0, float &z1, float &z2, float &z3) {
+    if (sizeof(T) == 4) {
+        z0 = ips::swish<T>(z0), z1 = ips::swish<T>(z1), z2 = ips::swish<T>(z2), z3 = ips::swish<T>(z3);
+        return;
+    }
+    float z[4] = {z0, z1, z2, z3}, n[4], d[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float t;
+        asm("ex2.approx.f32 %0, %1;" : "=f"(t) : "f"(fabsf(z[i]) * -1.44269504f));
+        t = fminf(t, 1.0f);      // a NaN among the four stays its own
+        d[i] = 1.0f + t;
+        n[i] = z[i] * (z[i] < 0.0f ? t : 1.0f);
+    }
+    const float d01 = d[0] * d[1], d23 = d[2] * d[3];
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d01 * d23));
+    const float r01 = r * d23, r23 = r * d01;
+    z0 = n[0] * (r01 * d[1]);
+    z1 = n[1] * (r01 * d[0]);
+    z2 = n[2] * (r23 * d[3]);
+    z3 = n[3] * (r23 * d[2]);
+}
 // Block of 32 rows x 64 bytes to the output, from shared memory in the 64-byte swizzled layout.
 __device__ __forceinline__ void store_block(const CUtensorMap *map, uint32_t src, int n, int m) {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
@@ -185,13 +212,6 @@ __device__ __forceinline__ void store_block(const CUtensorMap *map, uint32_t src
                  "r"(n), "r"(m), "r"(src)
                  : "memory");
 }
-// At most N of this thread's blocks are still being read (N = 0: none is still on its way).
-template <int N>
-__device__ __forceinline__ void blocks_left() {
-    if (N > 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
-    else asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-}
-
 // Output leaves by TMA in blocks of 64 bytes a row (BN = 64: in whole sectors from the registers).
 // ODD: rows or an N for which that cannot be (16 bytes; BN = 64: 8 bytes, 16 columns).
 template <typename T, int BN, bool PAIR, bool ODD>
@@ -200,8 +220,8 @@ __global__ void __launch_bounds__(THREADS, 1)
                const __grid_constant__ CUtensorMap tm_xb, const __grid_constant__ CUtensorMap tm_wb,
                const __grid_constant__ CUtensorMap tm_y, const Params prm) {
     using C = Tile<BN, PAIR>;
-    // 256 columns are 128 registers of an output thread: its warpgroups take over what the others can
-    // spare, 2 x 200 + 2 x 56 = 4 x 128
+    // 256 columns are 64 registers of an output thread: its warpgroups take over what the others can
+    // spare, 4 x 96 + 2 x 48 = 6 x 80
     constexpr bool DEAL = BN == 256;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>(
@@ -221,7 +241,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::ST; ++s) {
-            mbar_init(full(s), C::CTAS);
+            mbar_init(full(s), 2 * C::CTAS);
             mbar_init(empty(s), 1);
             mbar_init(scales(s), 1);
             mbar_init(ready(s), 4 * C::CTAS);
@@ -252,11 +272,13 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int stages = (prm.steps + 3) / 4;
     const long long limit = prm.timeout_cycles;
 
-    if (DEAL && warp >= SCALE_WARP) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    int issued = 0;       // stages that this CTA has fetched (the fetching thread)
-    if (warp == TMA_WARP) {
+    if (DEAL && warp >= SCALE_WARP) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    volatile int *fetched = reinterpret_cast<volatile int *>(smem + C::FETCHED);
+    if (warp == X_WARP || warp == W_WARP || warp == SCALES_WARP) {
+        // a thread each for the rows, the channels and the scales: one for all four copies of a stage
+        // takes 0.34 us a stage, whatever their size
         if (lane == 0) {
-            int s = 0, ph = 0;
+            int s = 0, ph = 0, issued = 0;
             bool ok = true;
             for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
                 const int mt = static_cast<int>(tile / prm.tiles_n) * C::CTAS + rank;
@@ -264,19 +286,29 @@ __global__ void __launch_bounds__(THREADS, 1)
                 for (int it = 0; it < stages; ++it) {
                     ok = wait_or_dead(empty(s), ph ^ 1, dead, limit);
                     if (!ok) break;
-                    const uint32_t st = base + C::STAGES_AT + s * C::STAGE, bar = PAIR ? of_first(full(s)) : full(s);
-                    mbar_expect_tx(scales(s), C::SA + C::SB);
-                    tma_load_3d(st + C::A + C::B, &tm_xb, 0, 4 * it, mt, scales(s));
-                    tma_load_3d(st + C::A + C::B + C::SA, &tm_wb, 0, 4 * it, n0 / 128, scales(s));
-                    expect_first<PAIR>(bar, C::A + C::B);
-                    load_2d<PAIR>(st, &tm_x, it * BKB, mt * TILE_M, bar);
-                    load_2d<PAIR>(st + C::A, &tm_w, it * BKB, n0 + rank * C::BR, bar);
+                    const uint32_t st = base + C::STAGES_AT + s * C::STAGE;
+                    if (warp == SCALES_WARP) {
+                        mbar_expect_tx(scales(s), C::SA + C::SB);
+                        tma_load_3d(st + C::A + C::B, &tm_xb, 0, 4 * it, mt, scales(s));
+                        tma_load_3d(st + C::A + C::B + C::SA, &tm_wb, 0, 4 * it, n0 / 128, scales(s));
+                    } else {
+                        const uint32_t bar = PAIR ? of_first(full(s)) : full(s);
+                        if (warp == X_WARP) {
+                            expect_first<PAIR>(bar, C::A);
+                            load_2d<PAIR>(st, &tm_x, it * BKB, mt * TILE_M, bar);
+                        } else {
+                            expect_first<PAIR>(bar, C::B);
+                            load_2d<PAIR>(st + C::A, &tm_w, it * BKB, n0 + rank * C::BR, bar);
+                        }
+                    }
                     ++issued;
                     if (++s == C::ST) s = 0, ph ^= 1;
                 }
             }
-            // after a wait that ran out the copies in flight land before the CTA ends (the others: below)
-            if (!ok)
+            // after a wait that ran out the copies in flight land before the CTA ends: the scales here, the others below
+            if (warp != SCALES_WARP)
+                fetched[warp == W_WARP] = issued;
+            else if (!ok)
                 for (int i = issued > C::ST ? issued - C::ST : 0; i < issued; ++i)
                     mbar_wait(scales(i % C::ST), static_cast<uint32_t>((i / C::ST) & 1), ips::LAND_CYCLES);
         }
@@ -319,8 +351,6 @@ __global__ void __launch_bounds__(THREADS, 1)
                 mbar_wait(drained, 0, ips::LAND_CYCLES);
             }
         }
-    } else if (warp >= TMA_WARP) {
-        // two warps without a role
     } else if (warp >= SCALE_WARP) {
         // Scales to TMEM: lane l of every quarter holds those of the rows l, l + 32, l + 64, l + 96, four columns
         // for each 64 elements.  A stage's slot there is free when its shared memory is: its scales
@@ -355,14 +385,15 @@ __global__ void __launch_bounds__(THREADS, 1)
                 if (++s == C::ST) s = 0, ph ^= 1;
             }
     } else {
-        if (DEAL) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
-        const int quarter = warp & 3, half = warp >> 2;
-        constexpr int CW = BN / 2;            // columns of a warp
-        const int col0 = half * CW;
+        if (DEAL) asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
+        const int quarter = warp & 3, group = warp >> 2;
+        constexpr int CW = BN / 4;            // columns of a warp
+        const int col0 = group * CW;
+        constexpr bool BLOCKS = BN >= 128 && !ODD;
+        constexpr int BC = BLOCKS ? 64 / static_cast<int>(sizeof(T)) : 16;      // columns at a time
         const unsigned low = static_cast<unsigned>(reinterpret_cast<uintptr_t>(prm.y) | (prm.ldy * sizeof(T))) & 31u;
         const bool wide = low == 0, even = (low & 7u) == 0;
-        constexpr bool BLOCKS = BN >= 128 && !ODD;
-        const uint32_t cst = base + C::CONSTS + half * (8 * CW), out = base + C::OUT_AT + warp * C::OUT;
+        const uint32_t cst = base + C::CONSTS + group * (8 * CW), out = base + C::OUT_AT + warp * C::OUT;
         int a = 0, aph = 0;
         bool ok = true;
         if (prm.stall) ok = warp_wait_or_dead(never, 0, dead, limit);
@@ -374,9 +405,8 @@ __global__ void __launch_bounds__(THREADS, 1)
             const bool in = cc < CW && cn < prm.N;
             const float csw = in ? prm.sw[cn] : 0.0f, cb = in && prm.bias ? prm.bias[cn] : 0.0f;
             const float sx = m < prm.M ? prm.sx[m] : 0.0f;
-            T *row = static_cast<T *>(prm.y) + (m < prm.M ? m : 0) * prm.ldy;
             // the four warps of these columns go on together, or none does
-            ok = all_of_half(warp_wait_or_dead(acc_full(a), aph, dead, limit), 1 + half);
+            ok = all_of_group(warp_wait_or_dead(acc_full(a), aph, dead, limit), 1 + group);
             if (!ok) break;
             if (cc < CW) {
                 sts32(cst + 4 * cc, __float_as_uint(csw));
@@ -392,79 +422,76 @@ __global__ void __launch_bounds__(THREADS, 1)
             __syncwarp();
             if (lane == 0) arrive_first<PAIR>(acc_empty(a));
             if (++a == C::ACCS) a = 0, aph ^= 1;
-            asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");      // the constants are there
+            asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");      // the constants are there
 #pragma unroll
-            for (int ch = 0; ch < CW / 16; ++ch) {
-                const int c = 16 * ch;
-                float z[16];
+            for (int c = 0; c < CW; c += BC) {
+                float z[BC];
 #pragma unroll
-                for (int i = 0; i < 16; i += 4) {
+                for (int i = 0; i < BC; i += 4) {
                     const uint4 w4 = lds128(cst + 4 * (c + i));
                     const uint4 b4 = lds128(cst + 4 * (CW + c + i));
-                    z[i] = __fmaf_rn(__uint_as_float(r[ch][i]), sx * __uint_as_float(w4.x), __uint_as_float(b4.x));
-                    z[i + 1] = __fmaf_rn(__uint_as_float(r[ch][i + 1]), sx * __uint_as_float(w4.y), __uint_as_float(b4.y));
-                    z[i + 2] = __fmaf_rn(__uint_as_float(r[ch][i + 2]), sx * __uint_as_float(w4.z), __uint_as_float(b4.z));
-                    z[i + 3] = __fmaf_rn(__uint_as_float(r[ch][i + 3]), sx * __uint_as_float(w4.w), __uint_as_float(b4.w));
+                    const uint32_t (&v)[16] = r[(c + i) / 16];
+                    const int k = (c + i) % 16;
+                    z[i] = __fmaf_rn(__uint_as_float(v[k]), sx * __uint_as_float(w4.x), __uint_as_float(b4.x));
+                    z[i + 1] = __fmaf_rn(__uint_as_float(v[k + 1]), sx * __uint_as_float(w4.y), __uint_as_float(b4.y));
+                    z[i + 2] = __fmaf_rn(__uint_as_float(v[k + 2]), sx * __uint_as_float(w4.z), __uint_as_float(b4.z));
+                    z[i + 3] = __fmaf_rn(__uint_as_float(v[k + 3]), sx * __uint_as_float(w4.w), __uint_as_float(b4.w));
                 }
-                if (prm.act)
+                if (prm.act) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) z[i] = ips::swish<T>(z[i]);
+                    for (int i = 0; i < BC; i += 4) swish4<T>(z[i], z[i + 1], z[i + 2], z[i + 3]);
+                }
                 if (BLOCKS) {
-                    constexpr int PER = 64 / sizeof(T) / 16;      // chunks of 16 columns a block
-                    const int part = ch % PER;
-                    const uint32_t block = out + (ch / PER & 1) * 2048;
-                    if (part == 0) {
-                        if (lane == 0) blocks_left<1>();
-                        __syncwarp();
-                    }
-                    union { T e[16]; uint32_t w[4 * sizeof(T)]; } v;
+                    union { T e[BC]; uint32_t w[16]; } v;
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) v.e[j] = from_f32<T>(z[j]);
+                    for (int j = 0; j < BC; ++j) v.e[j] = from_f32<T>(z[j]);
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");      // the last block has been read
+                    __syncwarp();
 #pragma unroll
-                    for (int j = 0; j < static_cast<int>(sizeof(T)); ++j)
-                        sts128(block + 64 * lane + (((part * static_cast<int>(sizeof(T)) + j) ^ (lane >> 1 & 3)) << 4), v.w[4 * j], v.w[4 * j + 1], v.w[4 * j + 2], v.w[4 * j + 3]);
-                    if (part == PER - 1) {
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                        __syncwarp();
-                        const int n = n0 + c + 16 - 16 * PER;
-                        if (lane == 0) {
-                            if (first < prm.M && n < prm.N) store_block(&tm_y, block, n, static_cast<int>(first));
-                            // a block that is left out counts too, or its neighbour's buffer would seem free
-                            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                        }
+                    for (int j = 0; j < 4; ++j)
+                        sts128(out + 64 * lane + ((j ^ (lane >> 1 & 3)) << 4), v.w[4 * j], v.w[4 * j + 1], v.w[4 * j + 2], v.w[4 * j + 3]);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (first < prm.M && n0 + c < prm.N) store_block(&tm_y, out, n0 + c, static_cast<int>(first));
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     }
-                } else if (ODD && (!even || n0 + c + 16 > prm.N)) {
-                    const long long left = prm.M - first;
-                    if (n0 + c < prm.N)
-                        ips::store_odd<T>(static_cast<T *>(prm.y) + first * prm.ldy + n0 + c, prm.ldy,
-                                          left < 32 ? static_cast<int>(left) : 32, prm.N - n0 - c, out, z);
-                } else if (m < prm.M && n0 + c < prm.N) {
-                    ips::store16<T>(row, n0 + c, wide, z);
+                } else {
+                    float (&y)[16] = reinterpret_cast<float (&)[16]>(z);
+                    if (ODD && (!even || n0 + c + 16 > prm.N)) {
+                        const long long left = prm.M - first;
+                        if (n0 + c < prm.N)
+                            ips::store_odd<T>(static_cast<T *>(prm.y) + first * prm.ldy + n0 + c, prm.ldy,
+                                              left < 32 ? static_cast<int>(left) : 32, prm.N - n0 - c, out, y);
+                    } else if (m < prm.M && n0 + c < prm.N) {
+                        ips::store16<T>(static_cast<T *>(prm.y) + m * prm.ldy, n0 + c, wide, y);
+                    }
                 }
             }
         }
-        if (BLOCKS && lane == 0) blocks_left<0>();
+        if (BLOCKS && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");      // no block is still on its way
     }
-    __syncwarp();
-    // After a wait that ran out the copies in flight land before a CTA ends.  A pair's report to the first
-    // CTA's barriers, each CTA for itself: a stage that one of them alone has fetched lacks an arrival.
+    // A pair's copies report to the first CTA's barriers, so there is one place to wait for those in flight:
+    // a stage that not all of its fetching threads came to lacks their arrivals.
     volatile int *other = reinterpret_cast<volatile int *>(smem + C::OTHER);
+    __syncthreads();
     if (PAIR) {
-        __syncthreads();
-        if (warp == TMA_WARP && lane == 0) {
+        if (threadIdx.x == 0) {
             const uint32_t at = of_other(base + C::OTHER, rank);
-            asm volatile("st.shared::cluster.v2.s32 [%0], {%1, %2};" ::"r"(at), "r"(*dead), "r"(issued) : "memory");
+            asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(at), "r"(*dead) : "memory");
+            asm volatile("st.shared::cluster.v2.s32 [%0], {%1, %2};" ::"r"(at + 8), "r"(fetched[0]), "r"(fetched[1]) : "memory");
         }
         cluster_sync();
     }
-    if (warp == TMA_WARP && lane == 0 && rank == 0 && (*dead || (PAIR && other[0]))) {
-        const int theirs = PAIR ? other[1] : issued, last = issued > theirs ? issued : theirs;
+    if (threadIdx.x == 0 && rank == 0 && (*dead || (PAIR && other[0]))) {
+        const int n[4] = {fetched[0], fetched[1], PAIR ? other[2] : fetched[0], PAIR ? other[3] : fetched[1]};
+        const int last = max(max(n[0], n[1]), max(n[2], n[3]));
         for (int i = last > C::ST ? last - C::ST : 0; i < last; ++i) {
-            if (PAIR && (i >= issued || i >= theirs)) mbar_arrive(full(i % C::ST));
+            for (int k = 0; k < 2 * C::CTAS; ++k)
+                if (i >= n[k]) mbar_arrive(full(i % C::ST));
             mbar_wait(full(i % C::ST), static_cast<uint32_t>((i / C::ST) & 1), ips::LAND_CYCLES);
         }
     }
-    __syncwarp();
     if (PAIR && (*dead || other[0])) cluster_sync();      // the same in both CTAs
     if (!PAIR) __syncthreads();
     if (warp == MMA_WARP) tmem_free<PAIR>(tmem, C::COLS);

@@ -106,6 +106,19 @@ def test_rows_that_are_not_finite(ip):
 
 
 @pytest.mark.parametrize("dtype", list(DT))
+def test_a_channel_or_a_bias_that_is_not_finite(ip, dtype):
+    for M, K, N in ((3, 64, 100), (300, 256, 512), (2000, 128, 2050)):
+        x, w = rows(M, K, 1), rows(N, K, 2)
+        bias = torch.randn(N, device="cuda")
+        want = ip.linear_fp4(*x, *w, bias, act=ip.ACT_SWISH, dtype=DT[dtype])
+        w[2][5], bias[N - 2], bias[17], bias[18] = float("nan"), float("nan"), float("inf"), -float("inf")
+        y = ip.linear_fp4(*x, *w, bias, act=ip.ACT_SWISH, dtype=DT[dtype])
+        own = torch.tensor([5, 17, 18, N - 2], device="cuda")
+        assert torch.isnan(y[:, [5, 18, N - 2]]).all() and (y[:, 17] == float("inf")).all()
+        assert torch.equal(y.index_fill(1, own, 0), want.index_fill(1, own, 0))
+
+
+@pytest.mark.parametrize("dtype", list(DT))
 def test_output_rows_of_any_alignment(ip, dtype):
     for M, K, N in ((70, 100, 95), (300, 200, 2000), (3000, 128, 3001)):
         x, w = rows(M, K, 5), rows(N, K, 6)
