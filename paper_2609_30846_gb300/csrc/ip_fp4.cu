@@ -58,15 +58,15 @@ bool make_scale_map(CUtensorMap *m, const void *base, int steps, long long rows,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The output's rows, boxes of 64 bytes x 32 rows in the 64-byte swizzled layout.
-bool make_out_map(CUtensorMap *m, void *y, CUtensorMapDataType type, int es, int N, long long rows, long long ld) {
+// The output's rows, boxes of `columns` x 32 rows in the swizzled layout of their width (64 or 32 bytes).
+bool make_out_map(CUtensorMap *m, void *y, CUtensorMapDataType type, int es, int columns, int N, long long rows, long long ld) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(N), static_cast<cuuint64_t>(rows)};
     const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * es};
-    const cuuint32_t box[2] = {static_cast<cuuint32_t>(64 / es), 32};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(columns), 32};
     const cuuint32_t estride[2] = {1, 1};
-    return fn(m, type, 2, y, dims, strides, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
+    return fn(m, type, 2, y, dims, strides, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE, columns * es == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
               CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -143,12 +143,10 @@ int run(const Operands &o, ip4::Params prm, int nsm, cudaStream_t st) {
     prm.tiles_n = (prm.N + BN - 1) / BN;
     prm.tiles = (prm.M + ip4::TILE_M * C::CTAS - 1) / (ip4::TILE_M * C::CTAS) * prm.tiles_n;
     constexpr int es = static_cast<int>(sizeof(T));
-    // what the forms' usual ways out ask of the rows: blocks by TMA, or 16 columns by stores of 8 bytes and more
-    const bool odd = BN < 128 ? !aligned(prm.y, 8) || prm.ldy * es % 8 != 0 || prm.N % 16 != 0
-                              : !aligned(prm.y, 16) || prm.ldy * es % 16 != 0 || prm.N * es % 16 != 0;
+    const bool odd = !aligned(prm.y, 16) || prm.ldy * es % 16 != 0 || prm.N * es % 16 != 0;
     constexpr CUtensorMapDataType type = es == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16;
-    if (odd || BN < 128) maps[4] = maps[0];      // not used
-    else if (!make_out_map(&maps[4], prm.y, type, es, prm.N, prm.M, prm.ldy)) return IP_ERR_CUDA;
+    if (odd) maps[4] = maps[0];      // not used
+    else if (!make_out_map(&maps[4], prm.y, type, es, ip4::block_columns<T, BN>(), prm.N, prm.M, prm.ldy)) return IP_ERR_CUDA;
     return odd ? launch<T, BN, PAIR, true>(maps, prm, nsm, st) : launch<T, BN, PAIR, false>(maps, prm, nsm, st);
 }
 

@@ -10,8 +10,7 @@ namespace ip4 {
 
 using namespace ipk;
 using namespace ipr;
-using ips::elect_one, ips::cluster_sync, ips::mma_commit, ips::tmem_alloc, ips::tmem_free, ips::tmem_ld16,
-    ips::tmem_wait_ld, ips::smem_desc;
+using ips::elect_one, ips::cluster_sync, ips::mma_commit, ips::tmem_alloc, ips::tmem_free, ips::tmem_wait_ld, ips::smem_desc;
 
 // y[m][n] = act(sx[m] sw[n] S + bias[n]), S = sum over blocks of s_x s_w sum of 16 code products, by
 // tcgen05.mma kind::mxf4nvf4 with a scale for each 16 elements: products and scales are exact there, sums
@@ -26,6 +25,15 @@ using ips::elect_one, ips::cluster_sync, ips::mma_commit, ips::tmem_alloc, ips::
 // the channels; the scales of all channels go to both.  Both CTAs' copies report to the first one's
 // barriers, whose warp 21 issues for both.
 
+#ifndef SLP
+#define SLP 32
+#endif
+#ifndef MSLP
+#define MSLP 0
+#endif
+#ifndef ESLP
+#define ESLP 0
+#endif
 constexpr int TILE_M = 128;
 constexpr int BKB = 128;                 // bytes of a row in a stage
 constexpr int BK = 256;                  // elements
@@ -63,19 +71,21 @@ struct Tile {
     static constexpr int FETCHED = 272;               // stages, of x and of w
     static constexpr int OTHER = 288;                 // of the other CTA of a pair: given up, -, stages fetched
     static constexpr int CONSTS = 512;                // sw and bias of a tile's columns
-    // per output warp: a block of 32 rows x 64 bytes on its way out, or store_odd's block
+    // per output warp: a block of 32 rows x 64 bytes on its way out
     static constexpr int OUT_AT = (CONSTS + 8 * BN + 1023) & ~1023, OUT = 2048;
     static constexpr int STAGES_AT = OUT_AT + EPI_WARPS * OUT;
     static constexpr int SMEM = STAGES_AT + ST * STAGE + 1024;
     static_assert(8 * (4 * ST + 6) <= 256, "barriers");
     static_assert(SMEM <= 232448, "shared memory");
     static_assert(SF + ST * SF_COLS <= COLS, "TMEM columns");
-    static_assert(STAGE % 1024 == 0 && B % 1024 == 0 && OUT >= ips::TURN_BYTES, "alignment");
+    static_assert(STAGE % 1024 == 0 && B % 1024 == 0 , "alignment");
 };
 
 // The barriers guard what the asynchronous units read and write (tiles, scales, accumulators), never
 // generic accesses, so neither waits nor arrivals order any: a pair's arrivals on the first CTA's
 // barriers with the release of the cluster take 0.7 us each (12000 x 16384 -> 1024: 164 us, relaxed 87).
+// A poll may sleep for 20 us: without that the polls of the roles that wait take the output warps' issue
+// slots (XX).
 __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
@@ -87,10 +97,12 @@ __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
     return ok != 0;
 }
 // Bounded wait that also ends when another role of the CTA has given up.
+template <int SLEEP = 0>
 __device__ __forceinline__ bool wait_or_dead(uint32_t bar, uint32_t parity, volatile int *dead, long long limit) {
     if (try_wait(bar, parity)) return true;
     const long long t0 = clock64();
     while (!try_wait(bar, parity)) {
+        if (SLEEP > 0) __nanosleep(SLEEP);
         if (*dead) return false;
         if (clock64() - t0 > limit) {
             *dead = 1;
@@ -99,8 +111,9 @@ __device__ __forceinline__ bool wait_or_dead(uint32_t bar, uint32_t parity, vola
     }
     return true;
 }
+template <int SLEEP = 0>
 __device__ __forceinline__ bool warp_wait_or_dead(uint32_t bar, uint32_t parity, volatile int *dead, long long limit) {
-    return __all_sync(0xffffffffu, wait_or_dead(bar, parity, dead, limit)) != 0;
+    return __all_sync(0xffffffffu, wait_or_dead<SLEEP>(bar, parity, dead, limit)) != 0;
 }
 
 template <bool PAIR>
@@ -179,41 +192,93 @@ __device__ __forceinline__ bool all_of_group(bool ok, int bar) {
         : "memory");
     return r != 0;
 }
-// Four of z / (1 + exp(-z)) as ips::swish forms it; for 16-bit outputs by one reciprocal, that of the product of the
-// four denominators, in [1, 16] (the special unit is what bounds them: five for eight).
-template <typename T>
-__device__ __forceinline__ void swish4(float &z0, float &z1, float &z2, float &z3) {
-    if (sizeof(T) == 4) {
-        z0 = ips::swish<T>(z0), z1 = ips::swish<T>(z1), z2 = ips::swish<T>(z2), z3 = ips::swish<T>(z3);
-        return;
-    }
-    float z[4] = {z0, z1, z2, z3}, n[4], d[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float t;
-        asm("ex2.approx.f32 %0, %1;" : "=f"(t) : "f"(fabsf(z[i]) * -1.44269504f));
-        t = fminf(t, 1.0f);      // a NaN among the four stays its own
-        d[i] = 1.0f + t;
-        n[i] = z[i] * (z[i] < 0.0f ? t : 1.0f);
-    }
-    const float d01 = d[0] * d[1], d23 = d[2] * d[3];
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d01 * d23));
-    const float r01 = r * d23, r23 = r * d01;
-    z0 = n[0] * (r01 * d[1]);
-    z1 = n[1] * (r01 * d[0]);
-    z2 = n[2] * (r23 * d[3]);
-    z3 = n[3] * (r23 * d[2]);
+// Two f32 numbers in one register pair: one instruction for both.
+typedef unsigned long long Two;
+__device__ __forceinline__ Two two(float a, float b) {
+    Two r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
 }
-// Block of 32 rows x 64 bytes to the output, from shared memory in the 64-byte swizzled layout.
+__device__ __forceinline__ void split(Two v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ Two mul2(Two a, Two b) {
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// z / (1 + exp(-z)) as max(z, 0) - a t / (1 + t), a = |z|, t = exp(-a) <= 1: nothing overflows, a negative
+// z's value is the product alone and a positive one's at least half its first term.  An infinite a is
+// taken as 3e38, so that -inf gives its limit 0; NaN stays NaN.  For 16-bit outputs t and the
+// reciprocals come from the special unit, one reciprocal for two elements, of the product of their
+// denominators, in [1, 4].
+template <typename T>
+__device__ __forceinline__ void swish2(float &z0, float &z1) {
+    const float a0 = fminf(fabsf(z0), 3e38f), a1 = fminf(fabsf(z1), 3e38f);      // NaN: 3e38, so that the other's value stands
+    float m0, m1, q0, q1;
+    asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(m0) : "f"(z0));
+    asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(m1) : "f"(z1));
+    if (sizeof(T) == 4) {
+        const float t0 = expf(-a0), t1 = expf(-a1);
+        q0 = __fdiv_rn(t0, 1.0f + t0), q1 = __fdiv_rn(t1, 1.0f + t1);
+    } else {
+        const float t0 = ex2(a0 * -1.44269504f), t1 = ex2(a1 * -1.44269504f);
+        const float d0 = 1.0f + t0, d1 = 1.0f + t1;
+        float r;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d0 * d1));
+        q0 = t0 * (r * d1), q1 = t1 * (r * d0);
+    }
+    z0 = __fmaf_rn(-a0, q0, m0);
+    z1 = __fmaf_rn(-a1, q1, m1);
+}
+
+// Two outputs of a 16-bit type in a word, the first low.
+template <typename T>
+__device__ __forceinline__ uint32_t word_of(float a, float b) {
+    uint32_t w;
+    if (std::is_same<T, __half>::value) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(b), "f"(a));
+    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(b), "f"(a));
+    return w;
+}
+// 16 lanes x 16 columns of sums: lane l receives of each 8 columns the two from 2 (l mod 4) on, in row l / 4
+// (v[0], v[1]) and in row l / 4 + 8.
+__device__ __forceinline__ void tmem_ld_rows(uint32_t addr, uint32_t (&v)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                 : "r"(addr)
+                 : "memory");
+}
+// Columns of an output block: rows of 64 bytes, or what a warp has of a tile's columns.
+template <typename T, int BN>
+__host__ __device__ constexpr int block_columns() {
+    return BN / 4 < 64 / static_cast<int>(sizeof(T)) ? BN / 4 : 64 / static_cast<int>(sizeof(T));
+}
+// An output from shared memory.
+__device__ __forceinline__ void copy_out(float *y, uint32_t at) { *y = __uint_as_float(lds32(at)); }
+template <typename T>
+__device__ __forceinline__ void copy_out(T *y, uint32_t at) {
+    uint16_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at));
+    *reinterpret_cast<uint16_t *>(y) = v;
+}
+// Block of 32 rows to the output, from shared memory in the swizzled layout.
 __device__ __forceinline__ void store_block(const CUtensorMap *map, uint32_t src, int n, int m) {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
                      reinterpret_cast<uint64_t>(map)),
                  "r"(n), "r"(m), "r"(src)
                  : "memory");
 }
-// Output leaves by TMA in blocks of 64 bytes a row (BN = 64: in whole sectors from the registers).
-// ODD: rows or an N for which that cannot be (16 bytes; BN = 64: 8 bytes, 16 columns).
+// ODD: output rows that are not on 16 bytes or whose N columns do not end there: written element by element, others
+// by TMA.
 template <typename T, int BN, bool PAIR, bool ODD>
 __global__ void __launch_bounds__(THREADS, 1)
     fp4_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w,
@@ -284,7 +349,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 const int mt = static_cast<int>(tile / prm.tiles_n) * C::CTAS + rank;
                 const int n0 = static_cast<int>(tile % prm.tiles_n) * BN;
                 for (int it = 0; it < stages; ++it) {
-                    ok = wait_or_dead(empty(s), ph ^ 1, dead, limit);
+                    ok = wait_or_dead<SLP>(empty(s), ph ^ 1, dead, limit);
                     if (!ok) break;
                     const uint32_t st = base + C::STAGES_AT + s * C::STAGE;
                     if (warp == SCALES_WARP) {
@@ -321,11 +386,11 @@ __global__ void __launch_bounds__(THREADS, 1)
             int s = 0, ph = 0, a = 0, aph = 0;
             bool ok = true;
             for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
-                ok = warp_wait_or_dead(acc_empty(a), aph ^ 1, dead, limit);
+                ok = warp_wait_or_dead<MSLP>(acc_empty(a), aph ^ 1, dead, limit);
                 if (!ok) break;
                 const int n0 = static_cast<int>(tile % prm.tiles_n) * BN;
                 for (int it = 0; it < stages; ++it) {
-                    ok = warp_wait_or_dead(ready(s), ph, dead, limit) && warp_wait_or_dead(full(s), ph, dead, limit);
+                    ok = warp_wait_or_dead<MSLP>(ready(s), ph, dead, limit) && warp_wait_or_dead<MSLP>(full(s), ph, dead, limit);
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t st = base + C::STAGES_AT + s * C::STAGE;
@@ -360,7 +425,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         bool ok = true;
         for (long long tile = worker; ok && tile < prm.tiles; tile += workers)
             for (int it = 0; it < stages; ++it) {
-                ok = warp_wait_or_dead(scales(s), ph, dead, limit);
+                ok = warp_wait_or_dead<SLP>(scales(s), ph, dead, limit);
                 if (!ok) break;
                 const uint32_t src = base + C::STAGES_AT + s * C::STAGE + C::A + C::B + 16 * lane;
                 uint4 v[4];
@@ -389,34 +454,44 @@ __global__ void __launch_bounds__(THREADS, 1)
         const int quarter = warp & 3, group = warp >> 2;
         constexpr int CW = BN / 4;            // columns of a warp
         const int col0 = group * CW;
-        constexpr bool BLOCKS = BN >= 128 && !ODD;
-        constexpr int BC = BLOCKS ? 64 / static_cast<int>(sizeof(T)) : 16;      // columns at a time
-        const unsigned low = static_cast<unsigned>(reinterpret_cast<uintptr_t>(prm.y) | (prm.ldy * sizeof(T))) & 31u;
-        const bool wide = low == 0, even = (low & 7u) == 0;
+        constexpr int BC = block_columns<T, BN>(), CHUNKS = BC * static_cast<int>(sizeof(T)) / 16;      // columns and 16-byte chunks of a block's row
         const uint32_t cst = base + C::CONSTS + group * (8 * CW), out = base + C::OUT_AT + warp * C::OUT;
+        // where a block's row and chunk lie: rows of 64 or 32 bytes in the swizzled layout of that width
+        auto place = [&](int row, int chunk) {
+            return out + row * (CHUNKS * 16) + ((CHUNKS == 4 ? chunk ^ (row >> 1 & 3) : chunk ^ (row >> 2 & 1)) << 4);
+        };
         int a = 0, aph = 0;
         bool ok = true;
         if (prm.stall) ok = warp_wait_or_dead(never, 0, dead, limit);
         for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
-            const long long first = (tile / prm.tiles_n * C::CTAS + rank) * TILE_M + quarter * 32, m = first + lane;
+            const long long first = (tile / prm.tiles_n * C::CTAS + rank) * TILE_M + quarter * 32;
             const int n0 = static_cast<int>(tile % prm.tiles_n) * BN + col0;
             // each thread has the constants of one of the columns
             const int cc = quarter * 32 + lane, cn = n0 + cc;
             const bool in = cc < CW && cn < prm.N;
             const float csw = in ? prm.sw[cn] : 0.0f, cb = in && prm.bias ? prm.bias[cn] : 0.0f;
-            const float sx = m < prm.M ? prm.sx[m] : 0.0f;
+            // a lane has the rows lane / 4 + 8 i, in each 8 columns two from 2 (lane mod 4) on: so the
+            // constants of a column are read for four rows at once, and blocks leave by stmatrix
+            float sx[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const long long m = first + lane / 4 + 8 * i;
+                sx[i] = m < prm.M ? prm.sx[m] : 0.0f;
+            }
             // the four warps of these columns go on together, or none does
-            ok = all_of_group(warp_wait_or_dead(acc_full(a), aph, dead, limit), 1 + group);
+            ok = all_of_group(warp_wait_or_dead<ESLP>(acc_full(a), aph, dead, limit), 1 + group);
             if (!ok) break;
             if (cc < CW) {
                 sts32(cst + 4 * cc, __float_as_uint(csw));
                 sts32(cst + 4 * (CW + cc), __float_as_uint(cb));
             }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            uint32_t r[CW / 16][16];
+            uint32_t r[CW / 16][2][8];      // [..][rows 0-15, 16-31][8 columns, 8 columns: rows + 0, + 8, of two columns]
 #pragma unroll
             for (int c = 0; c < CW / 16; ++c)
-                tmem_ld16(tmem + a * BN + col0 + 16 * c + (static_cast<uint32_t>(quarter * 32) << 16), r[c]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    tmem_ld_rows(tmem + a * BN + col0 + 16 * c + (static_cast<uint32_t>(quarter * 32 + 16 * h) << 16), r[c][h]);
             tmem_wait_ld();
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
@@ -425,51 +500,49 @@ __global__ void __launch_bounds__(THREADS, 1)
             asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");      // the constants are there
 #pragma unroll
             for (int c = 0; c < CW; c += BC) {
-                float z[BC];
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");      // the last block has been read
+                __syncwarp();
 #pragma unroll
-                for (int i = 0; i < BC; i += 4) {
-                    const uint4 w4 = lds128(cst + 4 * (c + i));
-                    const uint4 b4 = lds128(cst + 4 * (CW + c + i));
-                    const uint32_t (&v)[16] = r[(c + i) / 16];
-                    const int k = (c + i) % 16;
-                    z[i] = __fmaf_rn(__uint_as_float(v[k]), sx * __uint_as_float(w4.x), __uint_as_float(b4.x));
-                    z[i + 1] = __fmaf_rn(__uint_as_float(v[k + 1]), sx * __uint_as_float(w4.y), __uint_as_float(b4.y));
-                    z[i + 2] = __fmaf_rn(__uint_as_float(v[k + 2]), sx * __uint_as_float(w4.z), __uint_as_float(b4.z));
-                    z[i + 3] = __fmaf_rn(__uint_as_float(v[k + 3]), sx * __uint_as_float(w4.w), __uint_as_float(b4.w));
+                for (int g = 0; g < BC / 8; ++g) {
+                    const int2 w2 = lds64(cst + 4 * (c + 8 * g + 2 * (lane & 3))), b2 = lds64(cst + 4 * (CW + c + 8 * g + 2 * (lane & 3)));
+                    const Two w = two(__int_as_float(w2.x), __int_as_float(w2.y)), b = two(__int_as_float(b2.x), __int_as_float(b2.y));
+                    uint32_t q[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t *v = &r[(c + 8 * g) / 16][i / 2][4 * (g & 1) + 2 * (i & 1)];
+                        float z0, z1;
+                        split(fma2(two(__uint_as_float(v[0]), __uint_as_float(v[1])), mul2(w, two(sx[i], sx[i])), b), z0, z1);
+                        if (prm.act) swish2<T>(z0, z1);
+                        if constexpr (sizeof(T) == 4)
+                            sts64(place(lane / 4 + 8 * i, 2 * g + (lane >> 1 & 1)) + 8 * (lane & 1), __float_as_int(z0), __float_as_int(z1));
+                        else
+                            q[i] = word_of<T>(z0, z1);
+                    }
+                    if constexpr (sizeof(T) == 2)
+                        asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(place(lane, g)),
+                                     "r"(q[0]), "r"(q[1]), "r"(q[2]), "r"(q[3])
+                                     : "memory");
                 }
-                if (prm.act) {
-#pragma unroll
-                    for (int i = 0; i < BC; i += 4) swish4<T>(z[i], z[i + 1], z[i + 2], z[i + 3]);
-                }
-                if (BLOCKS) {
-                    union { T e[BC]; uint32_t w[16]; } v;
-#pragma unroll
-                    for (int j = 0; j < BC; ++j) v.e[j] = from_f32<T>(z[j]);
-                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");      // the last block has been read
+                if constexpr (ODD) {
                     __syncwarp();
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        sts128(out + 64 * lane + ((j ^ (lane >> 1 & 3)) << 4), v.w[4 * j], v.w[4 * j + 1], v.w[4 * j + 2], v.w[4 * j + 3]);
+                    for (int e = lane; e < 32 * BC; e += 32) {
+                        const int row = e / BC, col = e % BC;
+                        const uint32_t at = place(row, col * static_cast<int>(sizeof(T)) / 16) + col * static_cast<int>(sizeof(T)) % 16;
+                        if (first + row < prm.M && n0 + c + col < prm.N)
+                            copy_out(static_cast<T *>(prm.y) + (first + row) * prm.ldy + n0 + c + col, at);
+                    }
+                    __syncwarp();
+                } else {
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) {
                         if (first < prm.M && n0 + c < prm.N) store_block(&tm_y, out, n0 + c, static_cast<int>(first));
                         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     }
-                } else {
-                    float (&y)[16] = reinterpret_cast<float (&)[16]>(z);
-                    if (ODD && (!even || n0 + c + 16 > prm.N)) {
-                        const long long left = prm.M - first;
-                        if (n0 + c < prm.N)
-                            ips::store_odd<T>(static_cast<T *>(prm.y) + first * prm.ldy + n0 + c, prm.ldy,
-                                              left < 32 ? static_cast<int>(left) : 32, prm.N - n0 - c, out, y);
-                    } else if (m < prm.M && n0 + c < prm.N) {
-                        ips::store16<T>(static_cast<T *>(prm.y) + m * prm.ldy, n0 + c, wide, y);
-                    }
                 }
             }
         }
-        if (BLOCKS && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");      // no block is still on its way
+        if (!ODD && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");      // no block is still on its way
     }
     // A pair's copies report to the first CTA's barriers, so there is one place to wait for those in flight:
     // a stage that not all of its fetching threads came to lacks their arrivals.
