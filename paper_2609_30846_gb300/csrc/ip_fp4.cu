@@ -150,12 +150,23 @@ int run(const Operands &o, ip4::Params prm, int nsm, cudaStream_t st) {
     return odd ? launch<T, BN, PAIR, true>(maps, prm, nsm, st) : launch<T, BN, PAIR, false>(maps, prm, nsm, st);
 }
 
+long long rounds(long long tiles, int workers) { return (tiles + workers - 1) / workers; }
+
+// The form that a launch is expected to take the least time in, ns: a start, and for each round of tiles over
+// the SMs the stages (all forms are held up by shared memory, which serves the MMAs, the copies in and the
+// scales) with what does not overlap of the hand-over to the output warps, or their time where K is short.
 template <typename T>
 int run(const Operands &o, const ip4::Params &prm, int nsm, cudaStream_t st) {
-    const long long tm = (prm.M + ip4::TILE_M - 1) / ip4::TILE_M;
-    if (tm * ((prm.N + 63) / 64) <= nsm) return run<T, 64, false>(o, prm, nsm, st);
-    if (tm * ((prm.N + 127) / 128) <= 2 * nsm) return run<T, 128, false>(o, prm, nsm, st);
-    return run<T, 256, true>(o, prm, nsm, st);
+    const long long stages = (prm.steps + 3) / 4, tm = (prm.M + ip4::TILE_M - 1) / ip4::TILE_M;
+    auto time = [&](long long start, long long tiles, int workers, long long stage, long long over, long long out) {
+        const long long tile = stage * stages + over;
+        return start + rounds(tiles, workers) * (tile > out ? tile : out);
+    };
+    const long long t64 = time(3300, tm * ((prm.N + 63) / 64), nsm, 340, 300, 930);
+    const long long t128 = time(3700, tm * ((prm.N + 127) / 128), nsm, 340, 360, 1200);
+    const long long pair = time(5100, (tm + 1) / 2 * ((prm.N + 255) / 256), nsm / 2, 385, 1200, 2050);
+    if (pair < t64 && pair < t128) return run<T, 256, true>(o, prm, nsm, st);
+    return t128 < t64 ? run<T, 128, false>(o, prm, nsm, st) : run<T, 64, false>(o, prm, nsm, st);
 }
 
 }  // namespace

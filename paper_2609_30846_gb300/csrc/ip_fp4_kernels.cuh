@@ -16,21 +16,21 @@ using ips::elect_one, ips::cluster_sync, ips::mma_commit, ips::tmem_alloc, ips::
 // tcgen05.mma kind::mxf4nvf4 with a scale for each 16 elements: products and scales are exact there, sums
 // in f32.
 //
-// Roles of a persistent CTA (one an SM): warps 12 and 14 fetch stages of 256 elements of K by TMA (128 rows of
-// x and BN channels of w, 128 bytes each in the 128-byte swizzled layout), warp 15 their scales as they
-// lie in memory, 512 bytes for 128 rows x 64 elements, which warps 8-11 copy to TMEM, one thread of
-// warp 13 issues the MMAs of 64 elements each, warps 0-7 take the sums to registers, release the
-// accumulator and write the output while the next tile is summed.
+// Roles of a persistent CTA (one an SM): warps 20, 22 and 23 fetch stages of 256 elements of K by TMA (128 rows of
+// x and BN channels of w, 128 bytes each in the 128-byte swizzled layout, and their scales as they
+// lie in memory, 512 bytes for 128 rows x 64 elements), warps 16-19 copy the scales to TMEM, one
+// thread of warp 21 issues the MMAs of 64 elements each, warps 0-15 take the sums to registers, release
+// the accumulator and write the output while the next tile is summed.
 // PAIR: two CTAs share a tile of 256 rows x BN channels (cta_group::2), each fetching its 128 rows and half of
 // the channels; the scales of all channels go to both.  Both CTAs' copies report to the first one's
-// barriers, whose warp 13 issues for both.
+// barriers, whose warp 21 issues for both.
 
 constexpr int TILE_M = 128;
 constexpr int BKB = 128;                 // bytes of a row in a stage
 constexpr int BK = 256;                  // elements
-constexpr int THREADS = 512;             // four warpgroups (registers are dealt by warpgroup)
-constexpr int REGS = 128;                // registers a thread at launch
-constexpr int EPI_WARPS = 8, SCALE_WARP = 8, X_WARP = 12, MMA_WARP = 13, W_WARP = 14, SCALES_WARP = 15;
+constexpr int THREADS = 768;             // six warpgroups (registers are dealt by warpgroup)
+constexpr int REGS = 80;                 // registers a thread at launch
+constexpr int EPI_WARPS = 16, SCALE_WARP = 16, X_WARP = 20, MMA_WARP = 21, W_WARP = 22, SCALES_WARP = 23;
 
 struct Params {
     const float *sx, *sw, *bias;
@@ -51,25 +51,25 @@ struct Tile {
     static constexpr int CTAS = PAIR_ ? 2 : 1;
     static constexpr int BR = BN / CTAS;              // channels that a CTA fetches
     static constexpr int WT = BN <= 128 ? 1 : BN / 128;      // tiles of scales of w
-    static constexpr int A = TILE_M * BKB, B = BR * BKB, STAGE = A + B;
-    static constexpr int ST = STAGE == 24576 ? 7 : 5;      // stages
-    static constexpr int SA = 2048, SB = 2048 * WT, SS = 3;      // bytes of a stage's scales, their buffers
+    static constexpr int A = TILE_M * BKB, B = BR * BKB, SA = 2048, SB = 2048 * WT;
+    static constexpr int STAGE = A + B + SA + SB;
+    static constexpr int ST = BN == 64 || (BN == 128 && PAIR_) ? 6 : 5;
     static constexpr int ACCS = BN == 256 ? 1 : 2;    // accumulators
     static constexpr int SF = ACCS * BN;              // first column of the scales
     static constexpr int SF_COLS = 16 + 16 * WT;      // of a stage
     static constexpr int COLS = 512;
-    static constexpr int TMEM_PTR = 272, DEAD = 276;
-    static constexpr int FETCHED = 280;               // stages, of x and of w
+    static constexpr int TMEM_PTR = 256, DEAD = 260;
+    static constexpr int FETCHED = 272;               // stages, of x and of w
     static constexpr int OTHER = 288;                 // of the other CTA of a pair: given up, -, stages fetched
     static constexpr int CONSTS = 512;                // sw and bias of a tile's columns
-    // per output warp: two blocks of 32 rows x 64 bytes on their way out
-    static constexpr int OUT_AT = (CONSTS + 8 * BN + 1023) & ~1023, OUT = 4096;
-    static constexpr int STAGES_AT = OUT_AT + EPI_WARPS * OUT, SCALES_AT = STAGES_AT + ST * STAGE;
-    static constexpr int SMEM = SCALES_AT + SS * (SA + SB) + 1024;
-    static_assert(8 * (3 * ST + 2 * SS + 6) <= 272, "barriers");
+    // per output warp: a block of 32 rows x 64 bytes on its way out
+    static constexpr int OUT_AT = (CONSTS + 8 * BN + 1023) & ~1023, OUT = 2048;
+    static constexpr int STAGES_AT = OUT_AT + EPI_WARPS * OUT;
+    static constexpr int SMEM = STAGES_AT + ST * STAGE + 1024;
+    static_assert(8 * (4 * ST + 6) <= 256, "barriers");
     static_assert(SMEM <= 232448, "shared memory");
     static_assert(SF + ST * SF_COLS <= COLS, "TMEM columns");
-    static_assert(STAGE % 1024 == 0 && B % 1024 == 0, "alignment");
+    static_assert(STAGE % 1024 == 0 && B % 1024 == 0 , "alignment");
 };
 
 // The barriers guard what the asynchronous units read and write (tiles, scales, accumulators), never
@@ -113,11 +113,11 @@ __device__ __forceinline__ void arrive_first(uint32_t bar) {
         mbar_arrive(bar);
 }
 
-__device__ __forceinline__ void tmem_st16(uint32_t addr, uint4 a, uint4 b, uint4 c, uint4 d) {
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint4 (&v)[4]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),
-        "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w), "r"(c.x), "r"(c.y), "r"(c.z),
-        "r"(c.w), "r"(d.x), "r"(d.y), "r"(d.z), "r"(d.w)
+        "r"(v[0].x), "r"(v[0].y), "r"(v[0].z), "r"(v[0].w), "r"(v[1].x), "r"(v[1].y), "r"(v[1].z), "r"(v[1].w),
+        "r"(v[2].x), "r"(v[2].y), "r"(v[2].z), "r"(v[2].w), "r"(v[3].x), "r"(v[3].y), "r"(v[3].z), "r"(v[3].w)
         : "memory");
 }
 template <bool PAIR>
@@ -246,7 +246,7 @@ __device__ __forceinline__ void tmem_ld_rows(uint32_t addr, uint32_t (&v)[8]) {
 // Columns of an output block: rows of 64 bytes, or what a warp has of a tile's columns.
 template <typename T, int BN>
 __host__ __device__ constexpr int block_columns() {
-    return BN / 2 < 64 / static_cast<int>(sizeof(T)) ? BN / 2 : 64 / static_cast<int>(sizeof(T));
+    return BN / 4 < 64 / static_cast<int>(sizeof(T)) ? BN / 4 : 64 / static_cast<int>(sizeof(T));
 }
 // An output from shared memory.
 __device__ __forceinline__ void copy_out(float *y, uint32_t at) { *y = __uint_as_float(lds32(at)); }
@@ -271,8 +271,8 @@ __global__ void __launch_bounds__(THREADS, 1)
                const __grid_constant__ CUtensorMap tm_xb, const __grid_constant__ CUtensorMap tm_wb,
                const __grid_constant__ CUtensorMap tm_y, const Params prm) {
     using C = Tile<BN, PAIR>;
-    // 256 columns are 128 registers of an output thread: its warpgroups take over what the others can
-    // spare, 2 x 192 + 80 + 48 = 4 x 128
+    // 256 columns are 64 registers of an output thread: its warpgroups take over what the others can
+    // spare, 4 x 96 + 2 x 48 = 6 x 80
     constexpr bool DEAL = BN == 256;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>(
@@ -281,12 +281,11 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     auto full = [&](int s) { return base + 8u * s; };
     auto empty = [&](int s) { return base + 8u * (C::ST + s); };
-    auto ready = [&](int s) { return base + 8u * (2 * C::ST + s); };       // the scales are in TMEM
-    auto acc_full = [&](int s) { return base + 8u * (3 * C::ST + s); };
-    auto acc_empty = [&](int s) { return base + 8u * (3 * C::ST + 2 + s); };
-    const uint32_t drained = base + 8u * (3 * C::ST + 4), never = drained + 8u;
-    auto scales = [&](int s) { return base + 8u * (3 * C::ST + 6 + s); };      // have landed, in each CTA
-    auto scales_empty = [&](int s) { return base + 8u * (3 * C::ST + 6 + C::SS + s); };
+    auto scales = [&](int s) { return base + 8u * (2 * C::ST + s); };      // have landed, in each CTA
+    auto ready = [&](int s) { return base + 8u * (3 * C::ST + s); };       // are in TMEM
+    auto acc_full = [&](int s) { return base + 8u * (4 * C::ST + s); };
+    auto acc_empty = [&](int s) { return base + 8u * (4 * C::ST + 2 + s); };
+    const uint32_t drained = base + 8u * (4 * C::ST + 4), never = drained + 8u;
     volatile int *dead = reinterpret_cast<volatile int *>(smem + C::DEAD);
     const int rank = PAIR ? static_cast<int>(blockIdx.x & 1u) : 0;      // clusters are (2, 1, 1)
     const long long worker = blockIdx.x / C::CTAS, workers = gridDim.x / C::CTAS;
@@ -295,15 +294,12 @@ __global__ void __launch_bounds__(THREADS, 1)
         for (int s = 0; s < C::ST; ++s) {
             mbar_init(full(s), 2 * C::CTAS);
             mbar_init(empty(s), 1);
+            mbar_init(scales(s), 1);
             mbar_init(ready(s), 4 * C::CTAS);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(acc_full(s), 1);
             mbar_init(acc_empty(s), EPI_WARPS / 4 * C::CTAS);
-        }
-        for (int s = 0; s < C::SS; ++s) {
-            mbar_init(scales(s), 1);
-            mbar_init(scales_empty(s), 4);
         }
         mbar_init(drained, 1);
         mbar_init(never, 1);
@@ -327,10 +323,11 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int stages = (prm.steps + 3) / 4;
     const long long limit = prm.timeout_cycles;
 
-    if (DEAL && warp >= X_WARP) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    if (DEAL && warp >= SCALE_WARP) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     volatile int *fetched = reinterpret_cast<volatile int *>(smem + C::FETCHED);
-    if (warp == X_WARP || warp == W_WARP) {
-        // a thread each for the rows and the channels
+    if (warp == X_WARP || warp == W_WARP || warp == SCALES_WARP) {
+        // a thread each for the rows, the channels and the scales: one for all four copies of a stage
+        // takes 0.34 us a stage, whatever their size
         if (lane == 0) {
             int s = 0, ph = 0, issued = 0;
             bool ok = true;
@@ -340,43 +337,31 @@ __global__ void __launch_bounds__(THREADS, 1)
                 for (int it = 0; it < stages; ++it) {
                     ok = wait_or_dead(empty(s), ph ^ 1, dead, limit);
                     if (!ok) break;
-                    const uint32_t st = base + C::STAGES_AT + s * C::STAGE, bar = PAIR ? of_first(full(s)) : full(s);
-                    if (warp == X_WARP) {
-                        expect_first<PAIR>(bar, C::A);
-                        load_2d<PAIR>(st, &tm_x, it * BKB, mt * TILE_M, bar);
+                    const uint32_t st = base + C::STAGES_AT + s * C::STAGE;
+                    if (warp == SCALES_WARP) {
+                        mbar_expect_tx(scales(s), C::SA + C::SB);
+                        tma_load_3d(st + C::A + C::B, &tm_xb, 0, 4 * it, mt, scales(s));
+                        tma_load_3d(st + C::A + C::B + C::SA, &tm_wb, 0, 4 * it, n0 / 128, scales(s));
                     } else {
-                        expect_first<PAIR>(bar, C::B);
-                        load_2d<PAIR>(st + C::A, &tm_w, it * BKB, n0 + rank * C::BR, bar);
+                        const uint32_t bar = PAIR ? of_first(full(s)) : full(s);
+                        if (warp == X_WARP) {
+                            expect_first<PAIR>(bar, C::A);
+                            load_2d<PAIR>(st, &tm_x, it * BKB, mt * TILE_M, bar);
+                        } else {
+                            expect_first<PAIR>(bar, C::B);
+                            load_2d<PAIR>(st + C::A, &tm_w, it * BKB, n0 + rank * C::BR, bar);
+                        }
                     }
                     ++issued;
                     if (++s == C::ST) s = 0, ph ^= 1;
                 }
             }
-            fetched[warp == W_WARP] = issued;
-        }
-    } else if (warp == SCALES_WARP) {
-        // the scales ahead of them in buffers of their own: they are in TMEM before the rest has landed
-        if (lane == 0) {
-            int s = 0, ph = 0, issued = 0;
-            bool ok = true;
-            for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
-                const int mt = static_cast<int>(tile / prm.tiles_n) * C::CTAS + rank;
-                const int wt = static_cast<int>(tile % prm.tiles_n) * BN / 128;
-                for (int it = 0; it < stages; ++it) {
-                    ok = wait_or_dead(scales_empty(s), ph ^ 1, dead, limit);
-                    if (!ok) break;
-                    const uint32_t st = base + C::SCALES_AT + s * (C::SA + C::SB);
-                    mbar_expect_tx(scales(s), C::SA + C::SB);
-                    tma_load_3d(st, &tm_xb, 0, 4 * it, mt, scales(s));
-                    tma_load_3d(st + C::SA, &tm_wb, 0, 4 * it, wt, scales(s));
-                    ++issued;
-                    if (++s == C::SS) s = 0, ph ^= 1;
-                }
-            }
-            // after a wait that ran out the copies in flight land before the CTA ends (the others': below)
-            if (!ok)
-                for (int i = issued > C::SS ? issued - C::SS : 0; i < issued; ++i)
-                    mbar_wait(scales(i % C::SS), static_cast<uint32_t>((i / C::SS) & 1), ips::LAND_CYCLES);
+            // after a wait that ran out the copies in flight land before the CTA ends: the scales here, the others below
+            if (warp != SCALES_WARP)
+                fetched[warp == W_WARP] = issued;
+            else if (!ok)
+                for (int i = issued > C::ST ? issued - C::ST : 0; i < issued; ++i)
+                    mbar_wait(scales(i % C::ST), static_cast<uint32_t>((i / C::ST) & 1), ips::LAND_CYCLES);
         }
     } else if (warp == MMA_WARP) {
         if (rank == 0 && worker < prm.tiles) {
@@ -418,32 +403,32 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
         }
     } else if (warp >= SCALE_WARP) {
-        if (DEAL) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
         // Scales to TMEM: lane l of every quarter holds those of the rows l, l + 32, l + 64, l + 96, four columns
-        // for each 64 elements, as they lie in memory.
+        // for each 64 elements.  A stage's slot there is free when its shared memory is: its scales
+        // are fetched after the MMAs that read the ones before.
         const uint32_t at = tmem + C::SF + (static_cast<uint32_t>((warp & 3) * 32) << 16);
-        constexpr int WORDS = 4 + 4 * C::WT;
-        int s = 0, ph = 0, b = 0, bph = 0;
+        int s = 0, ph = 0;
         bool ok = true;
         for (long long tile = worker; ok && tile < prm.tiles; tile += workers)
             for (int it = 0; it < stages; ++it) {
-                ok = warp_wait_or_dead(scales(b), bph, dead, limit);
+                ok = warp_wait_or_dead(scales(s), ph, dead, limit);
                 if (!ok) break;
-                const uint32_t src = base + C::SCALES_AT + b * (C::SA + C::SB) + 16 * lane;
-                uint4 v[WORDS];
+                const uint32_t src = base + C::STAGES_AT + s * C::STAGE + C::A + C::B + 16 * lane;
+                uint4 v[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) v[k] = lds128(src + 512 * k);
+                tmem_st16(at + s * C::SF_COLS, v);
 #pragma unroll
-                for (int c = 0; c < 4 * C::WT; ++c)      // columns 4 (WT k + j) for step k and tile j
-                    v[4 + c] = lds128(src + C::SA + 2048 * (c % C::WT) + 512 * (c / C::WT));
-                release_stage(scales_empty(b), lane);
-                if (++b == C::SS) b = 0, bph ^= 1;
-                ok = warp_wait_or_dead(empty(s), ph ^ 1, dead, limit);
-                if (!ok) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                for (int h = 0; h < C::WT; ++h) {
+                    // of x then w: columns 4 (WT k + j) for step k and tile j
+                    uint4 u[4];
 #pragma unroll
-                for (int h = 0; h <= C::WT; ++h)
-                    tmem_st16(at + s * C::SF_COLS + 16 * h, v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]);
+                    for (int i = 0; i < 4; ++i) {
+                        const int c = 4 * h + i, k = c / C::WT, j = c % C::WT;
+                        u[i] = lds128(src + C::SA + 2048 * j + 512 * k);
+                    }
+                    tmem_st16(at + s * C::SF_COLS + 16 + 16 * h, u);
+                }
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
@@ -451,12 +436,16 @@ __global__ void __launch_bounds__(THREADS, 1)
                 if (++s == C::ST) s = 0, ph ^= 1;
             }
     } else {
-        if (DEAL) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        if (DEAL) asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
         const int quarter = warp & 3, group = warp >> 2;
-        constexpr int CW = BN / 2;            // columns of a warp
+        constexpr int CW = BN / 4;            // columns of a warp
         const int col0 = group * CW;
         constexpr int BC = block_columns<T, BN>(), CHUNKS = BC * static_cast<int>(sizeof(T)) / 16;      // columns and 16-byte chunks of a block's row
-        const uint32_t cst = base + C::CONSTS + group * (8 * CW), outs = base + C::OUT_AT + warp * C::OUT;
+        const uint32_t cst = base + C::CONSTS + group * (8 * CW), out = base + C::OUT_AT + warp * C::OUT;
+        // where a block's row and chunk lie: rows of 64 or 32 bytes in the swizzled layout of that width
+        auto place = [&](int row, int chunk) {
+            return out + row * (CHUNKS * 16) + ((CHUNKS == 4 ? chunk ^ (row >> 1 & 3) : chunk ^ (row >> 2 & 1)) << 4);
+        };
         int a = 0, aph = 0;
         bool ok = true;
         if (prm.stall) ok = warp_wait_or_dead(never, 0, dead, limit);
@@ -496,12 +485,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             if (++a == C::ACCS) a = 0, aph ^= 1;
 #pragma unroll
             for (int c = 0; c < CW; c += BC) {
-                const uint32_t out = outs + (c / BC & 1) * 2048;
-                // where a block's row and chunk lie: rows of 64 or 32 bytes in the swizzled layout of that width
-                auto place = [&](int row, int chunk) {
-                    return out + row * (CHUNKS * 16) + ((CHUNKS == 4 ? chunk ^ (row >> 1 & 3) : chunk ^ (row >> 2 & 1)) << 4);
-                };
-                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");      // the last block but one has been read
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");      // the last block has been read
                 __syncwarp();
 #pragma unroll
                 for (int g = 0; g < BC / 8; ++g) {
@@ -537,7 +521,6 @@ __global__ void __launch_bounds__(THREADS, 1)
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) {
-                        // a block that is left out counts too, or its neighbour's buffer would seem free
                         if (first < prm.M && n0 + c < prm.N) store_block(&tm_y, out, n0 + c, static_cast<int>(first));
                         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     }
