@@ -20,14 +20,21 @@ int launched(cudaError_t rc) {
 
 unsigned grid_of(long long need) { return static_cast<unsigned>(need < (1 << 20) ? need : (1 << 20)); }
 
+template <typename T, int TPR, int UNITS, bool VEC, int OUT, bool NORM>
+int launch_rows(const ipw::RowsParams &prm, cudaStream_t st) {
+    constexpr int THREADS = TPR < 128 ? 128 : TPR, RPC = THREADS / TPR;
+    return launched(iph::launch_pdl(ipw::rows_kernel<T, TPR, UNITS, VEC, OUT, NORM>, dim3(grid_of((prm.rows + RPC - 1) / RPC)),
+                                    dim3(THREADS), 0, st, prm));
+}
+
 template <typename T, bool VEC, int OUT, bool NORM>
 int run_rows(const ipw::RowsParams &prm, cudaStream_t st) {
     // a warp a row while its lanes can hold the row, then four warps, then eight
-    if (prm.d <= 32 * 8 * ipw::UNITS)
-        return launched(iph::launch_pdl(ipw::rows_kernel<T, 32, VEC, OUT, NORM>, dim3(grid_of((prm.rows + 3) / 4)), dim3(128), 0, st, prm));
-    if (prm.d <= 128 * 8 * ipw::UNITS)
-        return launched(iph::launch_pdl(ipw::rows_kernel<T, 128, VEC, OUT, NORM>, dim3(grid_of(prm.rows)), dim3(128), 0, st, prm));
-    return launched(iph::launch_pdl(ipw::rows_kernel<T, 256, VEC, OUT, NORM>, dim3(grid_of(prm.rows)), dim3(256), 0, st, prm));
+    if (prm.d <= 512) return launch_rows<T, 32, 1, VEC, OUT, NORM>(prm, st);
+    if (prm.d <= 1024) return launch_rows<T, 32, 2, VEC, OUT, NORM>(prm, st);
+    if (prm.d <= 2048) return launch_rows<T, 128, 1, VEC, OUT, NORM>(prm, st);
+    if (prm.d <= 4096) return launch_rows<T, 128, 2, VEC, OUT, NORM>(prm, st);
+    return launch_rows<T, 256, 2, VEC, OUT, NORM>(prm, st);
 }
 
 template <typename T, int OUT, bool NORM>
@@ -35,7 +42,7 @@ int run_rows(const ipw::RowsParams &prm, cudaStream_t st) {
     auto rows16 = [&](const void *p, long long ld) { return aligned(p, 16) && (prm.rows == 1 || ld * static_cast<long long>(sizeof(T)) % 16 == 0); };
     const bool vec = prm.d % 8 == 0 && rows16(prm.x, prm.ldx) && (!NORM || aligned(prm.weight, 16)) &&
                      (!prm.res || (rows16(prm.res, prm.ldres) && rows16(prm.sum, prm.ldsum))) &&
-                     (OUT == ipw::OUT_FP4 || (aligned(prm.q, 8) && (prm.rows == 1 || prm.ldq % 8 == 0)));
+                     (OUT == ipw::OUT_FP4 || (aligned(prm.q, 16) && (prm.rows == 1 || prm.ldq % 16 == 0)));
     return vec ? run_rows<T, true, OUT, NORM>(prm, st) : run_rows<T, false, OUT, NORM>(prm, st);
 }
 
@@ -82,7 +89,7 @@ int run_values(int dtype, ipw::ValuesParams prm, ip_stream_t stream) {
     const long long es = static_cast<long long>(elem_size(dtype));
     const int qa = IN == ipw::OUT_I8 ? 16 : 8;
     const bool one = prm.rows == 1;
-    const bool vec = prm.d % 16 == 0 && aligned(prm.q, qa) && (one || prm.ldq % qa == 0) && aligned(prm.y, 16) && (one || prm.ldy * es % 16 == 0);
+    const bool vec = prm.d % 16 == 0 && aligned(prm.q, qa) && (one || prm.ldq % qa == 0) && aligned(prm.y, 32) && (one || prm.ldy * es % 32 == 0);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     if (dtype == IP_F32) return run_values<float, IN>(prm, vec, st);
     if (dtype == IP_F16) return run_values<__half, IN>(prm, vec, st);

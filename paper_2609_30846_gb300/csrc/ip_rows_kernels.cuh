@@ -21,7 +21,7 @@ using namespace ipr;
 // nearest.  That is right although it rounds twice: the midpoints m of both formats have at most
 // five significant bits, so x and m s are neighbours in f32 at best, |x - m s| >= 2^-24 m s, and the
 // f32 quotient of an x that is not m s falls on the side of m that x / s is on.
-// The quotient: q = x i, i the reciprocal of s rounded to nearest, then q - i (q s - x), the
+// A quotient: y = x i, i the reciprocal of s rounded to nearest, then y - i (y s - x), the
 // remainder exact in one fma (Markstein's correction).
 // The e4m3 scales lie in blocks of 512 bytes for 128 rows x 64 elements (4 scales a row), byte
 // 16 (row mod 32) + 4 ((row mod 128) / 32) + (block mod 4): 32 lanes of four words, as the tensor
@@ -73,14 +73,12 @@ __device__ __forceinline__ long long scale_at(long long row, int kc, int kcs) {
 // codes as they are, so they are z's, exactly as the definitions of the rows say, and only the
 // row's scale carries it.
 //
-// What bounds it: DRAM; a row stays in registers between the passes up to 8 UNITS elements a
-// thread (a longer one is read again, from L2).
+// What bounds it: DRAM, and close behind it the instructions (XX).  A row stays in registers
+// between the passes up to 16 UNITS elements a thread (a longer one is read again, from L2).
 //
 // The squares are summed in f32.  Sums that leave the middle of its range (bf16 and f32 rows
 // beyond 2^55 or below 2^-35) are formed again from elements scaled by 2^-80 or 2^96, and the
 // row's magnitude is divided by that root first, so that 1 / root need not be an f32.
-
-constexpr int UNITS = 4;      // units of eight elements that a thread keeps
 
 struct RowsParams {
     const void *x, *res, *weight;
@@ -95,62 +93,83 @@ struct RowsParams {
 
 enum { OUT_I8 = 0, OUT_FP4 = 1 };
 
+// Sum and maximum over a row's warps; red: two buffers that successive calls take in turn.
 template <int WARPS>
-__device__ __forceinline__ float row_sum(float v, float *red) {
+__device__ __forceinline__ void reduce(float &sum, uint32_t &top, float2 (*red)[WARPS], int &turn) {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    top = __reduce_max_sync(0xffffffffu, top);
     if (WARPS > 1) {
+        if ((threadIdx.x & 31) == 0) red[turn][threadIdx.x >> 5] = make_float2(sum, __uint_as_float(top));
         __syncthreads();
-        if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-        __syncthreads();
-        v = red[0];
+        sum = 0.0f;
 #pragma unroll
-        for (int i = 1; i < WARPS; ++i) v += red[i];
+        for (int i = 0; i < WARPS; ++i) {
+            const float2 v = red[turn][i];
+            sum += v.x;
+            top = max(top, __float_as_uint(v.y));
+        }
+        turn ^= 1;
     }
-    return v;
-}
-template <int WARPS>
-__device__ __forceinline__ uint32_t row_max(uint32_t v, float *red) {
-    v = __reduce_max_sync(0xffffffffu, v);
-    if (WARPS > 1) {
-        __syncthreads();
-        if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = __uint_as_float(v);
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < WARPS; ++i) v = max(v, __float_as_uint(red[i]));
-    }
-    return v;
 }
 
-// x + r rounded to T, as bits.
+// Sixteen elements as they lie in memory, the first n of them, the others 0.
 template <typename T>
-__device__ __forceinline__ void add8(Raw8<T> &x, const Raw8<T> &r) {
+struct Raw16 {
+    Raw8<T> h[2];
+
+    template <bool VEC>
+    __device__ __forceinline__ void load(const T *p, int n) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const T h = from_f32<T>(x.at(j) + r.at(j));
-        if constexpr (sizeof(T) == 4) {
-            x.w[j] = __float_as_uint(h);
-        } else {
-            const uint32_t b = *reinterpret_cast<const uint16_t *>(&h);
-            x.w[j >> 1] = j & 1 ? (x.w[j >> 1] & 0xffffu) | (b << 16) : (x.w[j >> 1] & 0xffff0000u) | b;
+        for (int k = 0; k < 2; ++k) {
+            if (8 * k < n) h[k].template load<VEC>(p + 8 * k, n - 8 * k);
+            else h[k].zero();
         }
     }
-}
-template <bool VEC, typename T>
-__device__ __forceinline__ void store_raw(T *p, const Raw8<T> &v, int n) {
-    if (VEC) {
+    template <bool VEC>
+    __device__ __forceinline__ void store(T *p, int n) const {
 #pragma unroll
-        for (int i = 0; i < Raw8<T>::WORDS; i += 4)
-            *reinterpret_cast<uint4 *>(reinterpret_cast<uint32_t *>(p) + i) = make_uint4(v.w[i], v.w[i + 1], v.w[i + 2], v.w[i + 3]);
-    } else {
+        for (int k = 0; k < 2; ++k) {
+            if (VEC) {
+                if (8 * k < n)
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < n) p[j] = from_f32<T>(v.at(j));
+                    for (int i = 0; i < Raw8<T>::WORDS; i += 4)
+                        *reinterpret_cast<uint4 *>(reinterpret_cast<uint32_t *>(p + 8 * k) + i) =
+                            make_uint4(h[k].w[i], h[k].w[i + 1], h[k].w[i + 2], h[k].w[i + 3]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (8 * k + j < n) p[8 * k + j] = from_f32<T>(h[k].at(j));
+            }
+        }
     }
+    __device__ __forceinline__ float at(int j) const { return h[j >> 3].at(j & 7); }
+    // + r, rounded to T once (the sum of two 16-bit numbers by an instruction that rounds the exact one)
+    __device__ __forceinline__ void add(const Raw16 &r) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < Raw8<T>::WORDS; ++i) {
+                if constexpr (sizeof(T) == 4) {
+                    h[k].w[i] = __float_as_uint(__fadd_rn(__uint_as_float(h[k].w[i]), __uint_as_float(r.h[k].w[i])));
+                } else if constexpr (std::is_same<T, __half>::value) {
+                    asm("add.rn.f16x2 %0, %0, %1;" : "+r"(h[k].w[i]) : "r"(r.h[k].w[i]));
+                } else {
+                    asm("add.rn.bf16x2 %0, %0, %1;" : "+r"(h[k].w[i]) : "r"(r.h[k].w[i]));
+                }
+            }
+    }
+};
+
+// The larger magnitude, NaN above all; the sign is of no use.
+__device__ __forceinline__ float larger(float a, float b) {
+    float r;
+    asm("max.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
 }
 
-// Eight elements to int8 (ip_scaled_kernels.cuh has the argument; f, inv, top of the row).
-__device__ __forceinline__ uint2 to_i8(const float (&z)[8], float f, float inv, float top, bool far) {
+// Sixteen elements to int8 (ip_scaled_kernels.cuh has the argument; f, inv, top of the row).
+__device__ __forceinline__ uint2 to_i8(const float *z, float f, float inv, float top, bool far) {
     uint32_t k[8];
     float off = far ? 1.0f : 0.0f;
 #pragma unroll
@@ -167,107 +186,158 @@ __device__ __forceinline__ uint2 to_i8(const float (&z)[8], float f, float inv, 
     return ips::low_bytes(k);
 }
 
-// TPR threads a row: 32 (four rows a CTA), 128 or 256 (the CTA).  VEC: rows of x, residual, sum and
-// the weight start on 16 bytes (q's on 8) and d is a multiple of eight.  NORM: with weight and
-// norm, else the rows of x as they are (4-bit rows only).
-template <typename T, int TPR, bool VEC, int OUT, bool NORM>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) rows_kernel(const RowsParams prm) {
-    constexpr int RPC = TPR < 128 ? 128 / TPR : 1, WARPS = TPR / 32;
-    __shared__ float red[WARPS];
+// What a row's blocks are coded with: their largest magnitude comes to [0, 2688] times `down`; a block scale s
+// stands for s `up` in units of the elements.
+struct Fp4Row {
+    float down, up;
+};
+// Block scale byte and codes of sixteen elements whose largest magnitude is `big`.
+__device__ __forceinline__ uint32_t to_fp4(const float (&z)[16], float big, Fp4Row row, uint2 &code) {
+    // big down / 6, the quotient rounded to nearest (Markstein, as below)
+    const float b = big * row.down, sixth = 0.16666667f, y6 = b * sixth;
+    const uint32_t sb = e4m3_of(__fmaf_rn(-__fmaf_rn(y6, 6.0f, -b), sixth, y6));
+    code = make_uint2(0u, 0u);
+    if (sb == 0) return 0;
+    const float s = e4m3_value(sb);
+    // the reciprocal of the four-bit s to nearest: one Newton step
+    float i;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(i) : "f"(s));
+    i = __fmaf_rn(i, __fmaf_rn(-s, i, 1.0f), i) * row.down;
+    const float su = s * row.up;
+    float q[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        const float y = z[j] * i;
+        q[j] = __fmaf_rn(-__fmaf_rn(y, su, -z[j]), i, y);      // so that -0 stays -0
+    }
+    code = make_uint2(e2m1_of8(*reinterpret_cast<const float (*)[8]>(q)), e2m1_of8(*reinterpret_cast<const float (*)[8]>(q + 8)));
+    return sb;
+}
+
+template <typename T, int TPR, int UNITS, bool NORM>
+constexpr int rows_ctas() { return TPR == 256 ? 2 : (sizeof(T) == 4 && UNITS == 2 ? 4 : 6); }
+
+// TPR threads a row: 32 (four rows a CTA), 128 or 256 (the CTA), UNITS of sixteen elements each in
+// registers.  VEC: rows of x, residual, sum, the weight and q start on 16 bytes and d is a multiple
+// of eight.  NORM: with weight and norm, else the rows of x as they are (4-bit rows only).
+template <typename T, int TPR, int UNITS, bool VEC, int OUT, bool NORM>
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, rows_ctas<T, TPR, UNITS, NORM>()) rows_kernel(const RowsParams prm) {
+    constexpr int RPC = TPR < 128 ? 128 / TPR : 1, WARPS = TPR / 32, KEPT = UNITS * TPR * 16;
+    __shared__ float2 red[2][WARPS];
     pdl_launch_dependents();
     pdl_wait();
     const int t = threadIdx.x % TPR, lane = threadIdx.x & 31;
     const int d = prm.d, kcs = (d + 63) / 64;
     const bool with_res = NORM && prm.res != nullptr;
     const T *g = static_cast<const T *>(prm.weight);
+    int turn = 0;
     for (long long row = static_cast<long long>(blockIdx.x) * RPC + threadIdx.x / TPR; row < prm.rows;
          row += static_cast<long long>(gridDim.x) * RPC) {
         const T *x = static_cast<const T *>(prm.x) + row * prm.ldx;
         const T *res = with_res ? static_cast<const T *>(prm.res) + row * prm.ldres : nullptr;
         T *sum = with_res ? static_cast<T *>(prm.sum) + row * prm.ldsum : nullptr;
-        Raw8<T> h[UNITS], w[UNITS];
+        const T *again = with_res ? sum : x;
+        float ss = 0.0f, top = 0.0f;
+        uint32_t bits = 0;
+        // h's elements: their squares and, in z, what is quantised
+        auto take = [&](const Raw16<T> &h, const Raw16<T> &w, float (&z)[16]) {
 #pragma unroll
-        for (int i = 0; i < UNITS; ++i) {
-            const int c = (i * TPR + t) * 8;
-            h[i].zero();
-            if (NORM) w[i].zero();
-            if (c < d) {
-                h[i].template load<VEC>(x + c, d - c);
-                if (NORM) w[i].template load<VEC>(g + c, d - c);
-            }
-        }
-        if (with_res) {
-            Raw8<T> r[UNITS];
-#pragma unroll
-            for (int i = 0; i < UNITS; ++i) {
-                const int c = (i * TPR + t) * 8;
-                r[i].zero();
-                if (c < d) r[i].template load<VEC>(res + c, d - c);
-            }
-#pragma unroll
-            for (int i = 0; i < UNITS; ++i) {
-                const int c = (i * TPR + t) * 8;
-                add8(h[i], r[i]);
-                if (c < d) store_raw<VEC>(sum + c, h[i], d - c);
-            }
-        }
-        // elements behind those that a thread keeps: read and added here, read again below
-        constexpr int KEPT = UNITS * TPR * 8;
-        float ss = 0.0f;
-        uint32_t top = 0;
-        auto take = [&](const Raw8<T> &v, const Raw8<T> &u, float f) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float a = v.at(j);
-                const float b = NORM ? a * f : 0.0f;
-                ss = __fmaf_rn(b, b, ss);
-                top = max(top, __float_as_uint(NORM ? __fmul_rn(a, u.at(j)) : a) & 0x7fffffffu);
+            for (int j = 0; j < 16; ++j) {
+                const float a = h.at(j);
+                ss = __fmaf_rn(a, a, ss);
+                z[j] = __fmul_rn(a, w.at(j));
+                top = larger(top, z[j]);
             }
         };
+        Raw16<T> raw[NORM ? 1 : UNITS];
+        float z[NORM ? UNITS : 1][16];
+        if constexpr (NORM) {
+            Raw16<T> h[UNITS], w[UNITS];
 #pragma unroll
-        for (int i = 0; i < UNITS; ++i) take(h[i], w[i], 1.0f);
-        for (int c = KEPT + t * 8; c < d; c += TPR * 8) {
-            Raw8<T> v, u;
-            v.template load<VEC>(x + c, d - c);
-            if (with_res) {
-                u.template load<VEC>(res + c, d - c);
-                add8(v, u);
-                store_raw<VEC>(sum + c, v, d - c);
+            for (int i = 0; i < UNITS; ++i) {
+                const int c = (i * TPR + t) * 16;
+                h[i].template load<VEC>(x + c, d - c);
+                w[i].template load<VEC>(g + c, d - c);
             }
-            if (NORM) u.template load<VEC>(g + c, d - c);
-            take(v, u, 1.0f);
+            if (with_res) {
+                Raw16<T> r[UNITS];
+#pragma unroll
+                for (int i = 0; i < UNITS; ++i) {
+                    const int c = (i * TPR + t) * 16;
+                    r[i].template load<VEC>(res + c, d - c);
+                }
+#pragma unroll
+                for (int i = 0; i < UNITS; ++i) {
+                    const int c = (i * TPR + t) * 16;
+                    h[i].add(r[i]);
+                    h[i].template store<VEC>(sum + c, d - c);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < UNITS; ++i) take(h[i], w[i], z[i]);
+            // elements behind those that a thread keeps: added here, read again below
+            for (int c = KEPT + t * 16; c < d; c += TPR * 16) {
+                Raw16<T> v, u;
+                float unused[16];
+                v.template load<VEC>(x + c, d - c);
+                if (with_res) {
+                    u.template load<VEC>(res + c, d - c);
+                    v.add(u);
+                    v.template store<VEC>(sum + c, d - c);
+                }
+                u.template load<VEC>(g + c, d - c);
+                take(v, u, unused);
+            }
+            bits = __float_as_uint(top) & 0x7fffffffu;
+        } else {
+#pragma unroll
+            for (int i = 0; i < UNITS; ++i) {
+                const int c = (i * TPR + t) * 16;
+                raw[i].template load<VEC>(x + c, d - c);
+            }
+#pragma unroll
+            for (int i = 0; i < UNITS; ++i) raw[i].h[0].largest(bits), raw[i].h[1].largest(bits);
+            for (int c = KEPT + t * 16; c < d; c += TPR * 16) {
+                Raw16<T> v;
+                v.template load<VEC>(x + c, d - c);
+                v.h[0].largest(bits), v.h[1].largest(bits);
+            }
+            bits = Raw8<T>::value(bits);
         }
-        const T *again = with_res ? sum : x;
-        const uint32_t bits = row_max<WARPS>(top, red);
+        reduce<WARPS>(ss, bits, red, turn);
         const bool finite = bits < 0x7f800000u;
         const float amax = __uint_as_float(bits);
         float root = 1.0f, up = 1.0f;      // the row is divided by root / up
-        if (NORM) {
-            ss = row_sum<WARPS>(ss, red);
+        if constexpr (NORM) {
             float eps = prm.eps;
             const bool large = !(ss < 0x1p110f), small = ss < 0x1p-70f && prm.eps < 0x1p-80f;
-            if (sizeof(T) == 4 || !std::is_same<T, __half>::value)
-                if (large || small) {
-                    up = large ? 0x1p-80f : 0x1p96f;
-                    eps = eps * up * up;
-                    ss = 0.0f;
-                    uint32_t unused = top;
+            if (!std::is_same<T, __half>::value && (large || small)) {
+                up = large ? 0x1p-80f : 0x1p96f;
+                eps = eps * up * up;
+                ss = 0.0f;
+                uint32_t unused = 0;
+                for (int c = t * 16; c < d; c += TPR * 16) {
+                    Raw16<T> v;
+                    v.template load<VEC>(again + c, d - c);
 #pragma unroll
-                    for (int i = 0; i < UNITS; ++i) take(h[i], w[i], up);
-                    for (int c = KEPT + t * 8; c < d; c += TPR * 8) {
-                        Raw8<T> v;
-                        v.template load<VEC>(again + c, d - c);
-                        take(v, v, up);
-                    }
-                    top = unused;
-                    ss = row_sum<WARPS>(ss, red);
+                    for (int j = 0; j < 16; ++j) ss = __fmaf_rn(v.at(j) * up, v.at(j) * up, ss);
                 }
+                reduce<WARPS>(ss, unused, red, turn);
+            }
             root = __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, static_cast<float>(d)), eps));
         }
         const bool zero = !finite || bits == 0;
         const int e = static_cast<int>(bits >> 23);
         uint8_t *q = prm.q + row * prm.ldq;
-        if (OUT == OUT_I8) {
+        // the elements from c on: those that are kept, or read again
+        auto again16 = [&](int c, float (&v)[16]) {
+            Raw16<T> h, w;
+            h.template load<VEC>(again + c, d - c);
+            if (NORM) w.template load<VEC>(g + c, d - c);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[j] = NORM ? __fmul_rn(h.at(j), w.at(j)) : h.at(j);
+        };
+        if constexpr (OUT == OUT_I8) {
             if (t == 0)
                 prm.scale[row] = finite ? (bits == 0 ? 0.0f : __fdiv_rn(__fmul_rn(__fdiv_rn(amax, root), up), 127.0f)) : __uint_as_float(0x7fc00000u);
             // rows near the ends of the range are brought to the middle by a power of two
@@ -275,29 +345,27 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) rows_kernel(const RowsP
             const int fe = 254 - e < 1 ? 1 : (254 - e > 253 ? 253 : 254 - e);
             const float f = far ? __uint_as_float(static_cast<unsigned>(fe) << 23) : 1.0f;
             const float ntop = amax * f, inv = zero ? 0.0f : __fdiv_ru(127.0f, ntop);
-            auto put = [&](int c, const Raw8<T> &v, const Raw8<T> &u) {
-                float z[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) z[j] = __fmul_rn(v.at(j), u.at(j));
-                const uint2 b = zero ? make_uint2(0u, 0u) : to_i8(z, f, inv, ntop, far);
+            auto put = [&](int c, const float (&v)[16]) {
+                uint2 b[2] = {make_uint2(0u, 0u), make_uint2(0u, 0u)};
+                if (!zero) b[0] = to_i8(v, f, inv, ntop, far), b[1] = to_i8(v + 8, f, inv, ntop, far);
                 if (VEC) {
-                    *reinterpret_cast<uint2 *>(q + c) = b;
+                    if (c + 16 <= d) *reinterpret_cast<uint4 *>(q + c) = make_uint4(b[0].x, b[0].y, b[1].x, b[1].y);
+                    else *reinterpret_cast<uint2 *>(q + c) = b[0];
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (c + j < d) q[c + j] = static_cast<uint8_t>((j < 4 ? b.x : b.y) >> (8 * (j & 3)));
+                    for (int j = 0; j < 16; ++j)
+                        if (c + j < d) q[c + j] = static_cast<uint8_t>(((j & 7) < 4 ? b[j >> 3].x : b[j >> 3].y) >> (8 * (j & 3)));
                 }
             };
 #pragma unroll
             for (int i = 0; i < UNITS; ++i) {
-                const int c = (i * TPR + t) * 8;
-                if (c < d) put(c, h[i], w[i]);
+                const int c = (i * TPR + t) * 16;
+                if (c < d) put(c, z[i]);
             }
-            for (int c = KEPT + t * 8; c < d; c += TPR * 8) {
-                Raw8<T> v, u;
-                v.template load<VEC>(again + c, d - c);
-                u.template load<VEC>(g + c, d - c);
-                put(c, v, u);
+            for (int c = KEPT + t * 16; c < d; c += TPR * 16) {
+                float v[16];
+                again16(c, v);
+                put(c, v);
             }
         } else {
             // amax = m 2^(e - 127), 1 <= m < 2, is at most 2688 r = 1.3125 2^11 r
@@ -306,52 +374,52 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) rows_kernel(const RowsP
             const float f = __uint_as_float(static_cast<unsigned>(127 - ex) << 23);
             const float r = __uint_as_float(static_cast<unsigned>(127 + ex) << 23);
             if (t == 0) prm.scale[row] = finite ? (bits == 0 ? 0.0f : NORM ? __fmul_rn(__fdiv_rn(r, root), up) : r) : __uint_as_float(0x7fc00000u);
-            // all lanes of a warp come here together: four blocks of eight lanes make one word
-            auto put = [&](int c, const Raw8<T> &v, const Raw8<T> &u) {
-                float z[8], big = 0.0f;
+            // a row near the ends of the range is scaled by f itself, others' elements stay as they are
+            const bool far = ex < -100 || ex > 100;
+            const Fp4Row fr{far ? 1.0f : f, far ? 1.0f : r};
+            // all lanes of a warp come here together: the scales of four make one word
+            auto put = [&](int c, float (&v)[16]) {
+                uint32_t sb = 0;
+                uint2 code = make_uint2(0u, 0u);
+                if (!zero) {
+                    if (far)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    z[j] = (NORM ? __fmul_rn(v.at(j), u.at(j)) : v.at(j)) * f;
-                    big = fmaxf(big, fabsf(z[j]));
+                        for (int j = 0; j < 16; ++j) v[j] *= f;
+                    float big = v[0];
+#pragma unroll
+                    for (int j = 1; j < 16; ++j) big = fmaxf(fabsf(big), fabsf(v[j]));
+                    sb = to_fp4(v, fabsf(big), fr, code);
                 }
-                big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
-                const uint32_t sb = zero ? 0u : e4m3_of(__fdiv_rn(big, 6.0f));
-                uint32_t word = lane & 1 ? 0u : sb << (4 * (lane & 6));
+                uint32_t word = sb << (8 * (lane & 3));
+                word |= __shfl_xor_sync(0xffffffffu, word, 1);
                 word |= __shfl_xor_sync(0xffffffffu, word, 2);
-                word |= __shfl_xor_sync(0xffffffffu, word, 4);
-                if ((lane & 7) == 0 && c < d)
-                    *reinterpret_cast<uint32_t *>(prm.blocks + scale_at(row, c >> 6, kcs)) = word;
-                if (c >= d) return;
-                uint32_t code = 0;
-                if (sb != 0) {
-                    const float s = e4m3_value(sb), i = __frcp_rn(s);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float y = z[j] * i;
-                        z[j] = __fmaf_rn(-__fmaf_rn(y, s, -z[j]), i, y);      // so that -0 stays -0
-                    }
-                    code = e2m1_of8(z);
-                }
-                if (c + 8 <= d) {
-                    *reinterpret_cast<uint32_t *>(q + (c >> 1)) = code;
+                if ((lane & 3) == 0 && c < d) *reinterpret_cast<uint32_t *>(prm.blocks + scale_at(row, c >> 6, kcs)) = word;
+                if (c + 16 <= d) {
+                    *reinterpret_cast<uint2 *>(q + (c >> 1)) = code;
                 } else {
-                    for (int j = 0; c + 2 * j < d; ++j) q[(c >> 1) + j] = static_cast<uint8_t>(code >> (8 * j));
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (c + 2 * j < d) q[(c >> 1) + j] = static_cast<uint8_t>((j < 4 ? code.x : code.y) >> (8 * (j & 3)));
                 }
             };
 #pragma unroll
             for (int i = 0; i < UNITS; ++i) {
-                const int c = (i * TPR + t) * 8;
-                if (c - lane * 8 < d) put(c, h[i], w[i]);
-            }
-            for (int c = KEPT + t * 8; c - lane * 8 < d; c += TPR * 8) {
-                Raw8<T> v, u;
-                v.zero();
-                if (NORM) u.zero();
-                if (c < d) {
-                    v.template load<VEC>(again + c, d - c);
-                    if (NORM) u.template load<VEC>(g + c, d - c);
+                const int c = (i * TPR + t) * 16;
+                if (c - lane * 16 < d) {
+                    if constexpr (NORM) {
+                        put(c, z[i]);
+                    } else {
+                        float v[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) v[j] = raw[i].at(j);
+                        put(c, v);
+                    }
                 }
-                put(c, v, u);
+            }
+            for (int c = KEPT + t * 16; c - lane * 16 < d; c += TPR * 16) {
+                float v[16];
+                again16(c, v);
+                put(c, v);
             }
         }
     }
@@ -370,7 +438,8 @@ struct ValuesParams {
 };
 
 // code x scale (a 4-bit row's: code x block scale, exact, x row scale), rounded once.  A thread
-// takes 16 elements.  VEC: rows of q and y start on 16 bytes and d is a multiple of 16.
+// takes 16 elements and writes them in whole sectors.  VEC: rows of y start on 32 bytes, q's on 16 (4-bit
+// rows: 8) and d is a multiple of 16.
 template <typename T, bool VEC, int IN>
 __global__ void __launch_bounds__(256) values_kernel(const ValuesParams prm) {
     pdl_launch_dependents();
@@ -412,11 +481,7 @@ __global__ void __launch_bounds__(256) values_kernel(const ValuesParams prm) {
         }
         T *y = static_cast<T *>(prm.y) + row * prm.ldy + c;
         if (VEC) {
-            float a[8], b[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) a[j] = v[j], b[j] = v[8 + j];
-            store8<T>(y, a);
-            store8<T>(y + 8, b);
+            ips::store16<T>(y, 0, true, v);
         } else {
 #pragma unroll
             for (int j = 0; j < 16; ++j)
