@@ -78,8 +78,9 @@ int check_fp4(long long rows, int d, const void *q, long long ldq, const void *b
 template <typename T, int IN>
 int run_values(const ipw::ValuesParams &prm, bool vec, cudaStream_t st) {
     const dim3 grid(grid_of((prm.rows * prm.units + 255) / 256)), block(256);
-    return vec ? launched(iph::launch_pdl(ipw::values_kernel<T, true, IN>, grid, block, 0, st, prm))
-               : launched(iph::launch_pdl(ipw::values_kernel<T, false, IN>, grid, block, 0, st, prm));
+    auto *fn = !vec ? ipw::values_kernel<T, false, false, IN>
+                    : (prm.d % 16 == 0 ? ipw::values_kernel<T, true, true, IN> : ipw::values_kernel<T, true, false, IN>);
+    return launched(iph::launch_pdl(fn, grid, block, 0, st, prm));
 }
 
 template <int IN>
@@ -89,7 +90,8 @@ int run_values(int dtype, ipw::ValuesParams prm, ip_stream_t stream) {
     const long long es = static_cast<long long>(elem_size(dtype));
     const int qa = IN == ipw::OUT_I8 ? 16 : 8;
     const bool one = prm.rows == 1;
-    const bool vec = prm.d % 16 == 0 && aligned(prm.q, qa) && (one || prm.ldq % qa == 0) && aligned(prm.y, 32) && (one || prm.ldy * es % 32 == 0);
+    const bool vec = aligned(prm.q, qa) && (one || prm.ldq % qa == 0) && aligned(prm.y, 8) && (one || prm.ldy * es % 8 == 0);
+    prm.wide = aligned(prm.y, 32) && (one || prm.ldy * es % 32 == 0);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     if (dtype == IP_F32) return run_values<float, IN>(prm, vec, st);
     if (dtype == IP_F16) return run_values<__half, IN>(prm, vec, st);
@@ -147,7 +149,7 @@ int ip_dequantize_i8(const int8_t *q, long long ldq, const float *scale, long lo
     if (rows == 0) return IP_OK;
     if (!q || !scale || !y) return IP_ERR_NULL;
     if (!aligned(scale, 4) || !aligned(y, elem_size(dtype))) return IP_ERR_ALIGN;
-    return run_values<ipw::OUT_I8>(dtype, ipw::ValuesParams{reinterpret_cast<const uint8_t *>(q), nullptr, scale, rows, ldq, ldy, d, y, 0, 0}, stream);
+    return run_values<ipw::OUT_I8>(dtype, ipw::ValuesParams{reinterpret_cast<const uint8_t *>(q), nullptr, scale, rows, ldq, ldy, d, y, 0, 0, 0}, stream);
 }
 
 int ip_dequantize_fp4(const uint8_t *q, long long ldq, const uint8_t *blocks, const float *scale, long long rows, int d,
@@ -158,7 +160,7 @@ int ip_dequantize_fp4(const uint8_t *q, long long ldq, const uint8_t *blocks, co
     if (rc != IP_OK || rows == 0) return rc;
     if (!y) return IP_ERR_NULL;
     if (!aligned(y, elem_size(dtype))) return IP_ERR_ALIGN;
-    return run_values<ipw::OUT_FP4>(dtype, ipw::ValuesParams{q, blocks, scale, rows, ldq, ldy, d, y, 0, 0}, stream);
+    return run_values<ipw::OUT_FP4>(dtype, ipw::ValuesParams{q, blocks, scale, rows, ldq, ldy, d, y, 0, 0, 0}, stream);
 }
 
 }  // extern "C"

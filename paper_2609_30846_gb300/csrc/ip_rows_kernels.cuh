@@ -47,6 +47,16 @@ __device__ __forceinline__ uint32_t e2m1_of8(const float (&q)[8]) {      // eigh
         : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]), "f"(q[4]), "f"(q[5]), "f"(q[6]), "f"(q[7]));
     return w;
 }
+__device__ __forceinline__ uint32_t e2m1_of8(const uint32_t *h) {      // of eight f16 numbers
+    uint32_t w;
+    asm("{\n .reg .b8 a, b, c, d;\n"
+        " cvt.rn.satfinite.e2m1x2.f16x2 a, %1;\n cvt.rn.satfinite.e2m1x2.f16x2 b, %2;\n"
+        " cvt.rn.satfinite.e2m1x2.f16x2 c, %3;\n cvt.rn.satfinite.e2m1x2.f16x2 d, %4;\n"
+        " mov.b32 %0, {a, b, c, d};\n}\n"
+        : "=r"(w)
+        : "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]));
+    return w;
+}
 __device__ __forceinline__ void e2m1_values8(uint32_t w, float (&v)[8]) {
     uint32_t h[4];
     asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n"
@@ -186,12 +196,22 @@ __device__ __forceinline__ uint2 to_i8(const float *z, float f, float inv, float
     return ips::low_bytes(k);
 }
 
+__device__ __forceinline__ float largest16(const float (&z)[16]) {
+    float big = fabsf(z[0]);
+#pragma unroll
+    for (int j = 1; j < 16; ++j) big = fmaxf(big, fabsf(z[j]));
+    return big;
+}
+
 // What a row's blocks are coded with: their largest magnitude comes to [0, 2688] times `down`; a block scale s
 // stands for s `up` in units of the elements.
 struct Fp4Row {
     float down, up;
 };
-// Block scale byte and codes of sixteen elements whose largest magnitude is `big`.
+// Block scale byte and codes of sixteen elements whose largest magnitude is `big`.  SHORT: elements of 11 bits at most.  The
+// quotient of one that is not m s is 2^-11 m from m at least (m s has seven bits), so that f16, whose
+// half step at m is less, keeps it on its side, and takes an f32 quotient 2^-22 m from m to m: no remainder is needed.
+template <bool SHORT>
 __device__ __forceinline__ uint32_t to_fp4(const float (&z)[16], float big, Fp4Row row, uint2 &code) {
     // big down / 6, the quotient rounded to nearest (Markstein, as below)
     const float b = big * row.down, sixth = 0.16666667f, y6 = b * sixth;
@@ -202,6 +222,14 @@ __device__ __forceinline__ uint32_t to_fp4(const float (&z)[16], float big, Fp4R
     // the reciprocal of the four-bit s to nearest: one Newton step
     float i;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(i) : "f"(s));
+    if (SHORT) {
+        i *= row.down;
+        uint32_t h[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h[j]) : "f"(z[2 * j + 1] * i), "f"(z[2 * j] * i));
+        code = make_uint2(e2m1_of8(h), e2m1_of8(h + 4));
+        return sb;
+    }
     i = __fmaf_rn(i, __fmaf_rn(-s, i, 1.0f), i) * row.down;
     const float su = s * row.up;
     float q[16];
@@ -215,7 +243,9 @@ __device__ __forceinline__ uint32_t to_fp4(const float (&z)[16], float big, Fp4R
 }
 
 template <typename T, int TPR, int UNITS, bool NORM>
-constexpr int rows_ctas() { return TPR == 256 ? 2 : (sizeof(T) == 4 && UNITS == 2 ? 4 : 6); }
+constexpr int rows_ctas() {
+    return TPR == 256 ? (UNITS == 1 ? (NORM ? 3 : 5) : 2) : (sizeof(T) == 4 && UNITS == 2 ? 4 : (NORM || UNITS == 2 ? 6 : 8));
+}
 
 // TPR threads a row: 32 (four rows a CTA), 128 or 256 (the CTA), UNITS of sixteen elements each in
 // registers.  VEC: rows of x, residual, sum, the weight and q start on 16 bytes and d is a multiple
@@ -250,6 +280,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, rows_ctas<T, TPR, UNITS
             }
         };
         Raw16<T> raw[NORM ? 1 : UNITS];
+        uint32_t most[NORM ? 1 : UNITS];      // of a unit's elements, as Raw8::largest has it
         float z[NORM ? UNITS : 1][16];
         if constexpr (NORM) {
             Raw16<T> h[UNITS], w[UNITS];
@@ -296,7 +327,11 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, rows_ctas<T, TPR, UNITS
                 raw[i].template load<VEC>(x + c, d - c);
             }
 #pragma unroll
-            for (int i = 0; i < UNITS; ++i) raw[i].h[0].largest(bits), raw[i].h[1].largest(bits);
+            for (int i = 0; i < UNITS; ++i) {
+                most[i] = 0;
+                raw[i].h[0].largest(most[i]), raw[i].h[1].largest(most[i]);
+                bits = sizeof(T) == 4 ? max(bits, most[i]) : __vmaxu2(bits, most[i]);
+            }
             for (int c = KEPT + t * 16; c < d; c += TPR * 16) {
                 Raw16<T> v;
                 v.template load<VEC>(x + c, d - c);
@@ -378,17 +413,16 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, rows_ctas<T, TPR, UNITS
             const bool far = ex < -100 || ex > 100;
             const Fp4Row fr{far ? 1.0f : f, far ? 1.0f : r};
             // all lanes of a warp come here together: the scales of four make one word
-            auto put = [&](int c, float (&v)[16]) {
+            auto put = [&](int c, float (&v)[16], float big) {
                 uint32_t sb = 0;
                 uint2 code = make_uint2(0u, 0u);
                 if (!zero) {
-                    if (far)
+                    if (far) {
+                        big *= f;
 #pragma unroll
                         for (int j = 0; j < 16; ++j) v[j] *= f;
-                    float big = v[0];
-#pragma unroll
-                    for (int j = 1; j < 16; ++j) big = fmaxf(fabsf(big), fabsf(v[j]));
-                    sb = to_fp4(v, fabsf(big), fr, code);
+                    }
+                    sb = to_fp4<!NORM && sizeof(T) == 2>(v, big, fr, code);
                 }
                 uint32_t word = sb << (8 * (lane & 3));
                 word |= __shfl_xor_sync(0xffffffffu, word, 1);
@@ -407,19 +441,19 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, rows_ctas<T, TPR, UNITS
                 const int c = (i * TPR + t) * 16;
                 if (c - lane * 16 < d) {
                     if constexpr (NORM) {
-                        put(c, z[i]);
+                        put(c, z[i], largest16(z[i]));
                     } else {
                         float v[16];
 #pragma unroll
                         for (int j = 0; j < 16; ++j) v[j] = raw[i].at(j);
-                        put(c, v);
+                        put(c, v, __uint_as_float(Raw8<T>::value(most[i])));
                     }
                 }
             }
             for (int c = KEPT + t * 16; c - lane * 16 < d; c += TPR * 16) {
                 float v[16];
                 again16(c, v);
-                put(c, v);
+                put(c, v, largest16(v));
             }
         }
     }
@@ -435,12 +469,13 @@ struct ValuesParams {
     void *y;
     unsigned long long magic;      // of the units a row
     int units;
+    int wide;                      // rows of y start on 32 bytes
 };
 
 // code x scale (a 4-bit row's: code x block scale, exact, x row scale), rounded once.  A thread
-// takes 16 elements and writes them in whole sectors.  VEC: rows of y start on 32 bytes, q's on 16 (4-bit
-// rows: 8) and d is a multiple of 16.
-template <typename T, bool VEC, int IN>
+// takes 16 elements and writes them in whole sectors.  VEC: rows of y start on 8 bytes, q's on 16 (4-bit
+// rows: 8); EVEN: d is a multiple of 16.
+template <typename T, bool VEC, bool EVEN, int IN>
 __global__ void __launch_bounds__(256) values_kernel(const ValuesParams prm) {
     pdl_launch_dependents();
     pdl_wait();
@@ -449,11 +484,12 @@ __global__ void __launch_bounds__(256) values_kernel(const ValuesParams prm) {
         const long long row = i < (1ll << 32) ? static_cast<long long>(udiv_magic(static_cast<uint32_t>(i), prm.magic)) : i / prm.units;
         const int c = static_cast<int>(i - row * prm.units) * 16, d = prm.d;
         const float scale = prm.scale[row];
+        const bool whole = VEC && (EVEN || c + 16 <= d);
         float v[16];
         if (IN == OUT_I8) {
             const uint8_t *q = prm.q + row * prm.ldq + c;
             uint32_t w[4] = {0, 0, 0, 0};
-            if (VEC) {
+            if (whole) {
                 const uint4 u = *reinterpret_cast<const uint4 *>(q);
                 w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
             } else {
@@ -464,7 +500,7 @@ __global__ void __launch_bounds__(256) values_kernel(const ValuesParams prm) {
         } else {
             const uint8_t *q = prm.q + row * prm.ldq + (c >> 1);
             uint32_t w[2] = {0, 0};
-            if (VEC) {
+            if (whole) {
                 const uint2 u = *reinterpret_cast<const uint2 *>(q);
                 w[0] = u.x, w[1] = u.y;
             } else {
@@ -480,8 +516,8 @@ __global__ void __launch_bounds__(256) values_kernel(const ValuesParams prm) {
             }
         }
         T *y = static_cast<T *>(prm.y) + row * prm.ldy + c;
-        if (VEC) {
-            ips::store16<T>(y, 0, true, v);
+        if (whole) {
+            ips::store16<T>(y, 0, prm.wide, v);
         } else {
 #pragma unroll
             for (int j = 0; j < 16; ++j)
