@@ -17,20 +17,20 @@ int launched(cudaError_t rc) {
 // Elements that U units a thread hold wherever the row starts (up to seven before it).
 constexpr int hold(int threads, int units) { return threads * units * 8 - 8; }
 
-// Parts of a row and their elements: one while a CTA holds the row, else small parts while they
-// come to two CTAs an SM, and parts that fill the registers beyond that.
+// Parts of a row and their elements: one while a CTA holds the row; else a cluster's, as many as come to
+// four CTAs an SM, few rows by sixteen CTAs of few elements (1 x 65536 XX us by 16 CTAs, by 8 XX) and many by those
+// whose registers the parts fill; parts that a second kernel joins for what sixteen CTAs do not hold.
 struct Plan {
-    int parts, per;
+    int parts, per, cluster;
 };
 Plan plan(long long rows, int V) {
-    if (V <= hold(256, 4)) return {1, V};
-    Plan p = {1, V};
-    for (int units = 1; units <= 4; units *= 2) {
-        p.per = hold(256, units);
-        p.parts = (V + p.per - 1) / p.per;
-        if (rows * p.parts <= 304) break;
-    }
-    return p;
+    if (V <= hold(256, 4)) return {1, V, 0};
+    auto per_of = [&](int parts) { return ((V + parts - 1) / parts + 7) / 8 * 8; };
+    int parts = 2;
+    while (parts < ipl::MAX_CLUSTER && per_of(parts) > hold(256, 4)) parts *= 2;
+    if (per_of(parts) > hold(256, 4)) return {(V + hold(256, 4) - 1) / hold(256, 4), hold(256, 4), 0};
+    while (parts < ipl::MAX_CLUSTER && rows * parts * 2 <= 608) parts *= 2;
+    return {parts, per_of(parts), 1};
 }
 
 bool shape_ok(long long rows, int V, int top) {
@@ -40,30 +40,50 @@ bool shape_ok(long long rows, int V, int top) {
 
 size_t keys_at(long long rows, const Plan &p) { return 256 + static_cast<size_t>(rows) * p.parts * 16; }
 size_t space(long long rows, const Plan &p, int top) {
-    return p.parts == 1 ? 256 : keys_at(rows, p) + static_cast<size_t>(rows) * p.parts * top * 8;
+    return p.parts == 1 || p.cluster ? 256 : keys_at(rows, p) + static_cast<size_t>(rows) * p.parts * top * 8;
 }
 
-template <typename T, int TPR, int U, bool PART>
+template <typename T, int TPR, int U, int S, int HOLDS>
 int launch(const ipl::LogprobParams &prm, cudaStream_t st) {
+    auto *fn = ipl::logprob_kernel<T, TPR, U, S, HOLDS>;
     const long long ctas = TPR == 32 ? (prm.rows + 3) / 4 : prm.rows;
-    return launched(iph::launch_pdl(ipl::logprob_kernel<T, TPR, U, PART>,
-                                    dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(PART ? prm.parts : 1)),
-                                    dim3(TPR == 32 ? 128 : TPR), 0, st, prm));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(HOLDS == ipl::WHOLE ? 1 : prm.parts));
+    cfg.blockDim = dim3(TPR == 32 ? 128 : TPR);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 1;
+    attr[1].val.clusterDim.y = static_cast<unsigned>(prm.parts);
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = HOLDS == ipl::CLUSTER ? 2 : 1;
+    if (HOLDS == ipl::CLUSTER && prm.parts > 8 &&
+        cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
+        return IP_ERR_CUDA;
+    return launched(cudaLaunchKernelEx(&cfg, fn, prm));
 }
 
 template <typename T>
-int run(const ipl::LogprobParams &prm, cudaStream_t st) {
+int run(const ipl::LogprobParams &prm, bool cluster, cudaStream_t st) {
+    if (cluster)
+        return prm.per <= hold(256, 1) ? launch<T, 256, 1, 0, ipl::CLUSTER>(prm, st)
+               : prm.per <= hold(256, 2) ? launch<T, 256, 2, 0, ipl::CLUSTER>(prm, st)
+               : prm.per <= hold(256, 3) ? launch<T, 256, 3, 0, ipl::CLUSTER>(prm, st) : launch<T, 256, 4, 0, ipl::CLUSTER>(prm, st);
     if (prm.parts > 1) {
-        const int rc = prm.per <= hold(256, 1) ? launch<T, 256, 1, true>(prm, st)
-                       : prm.per <= hold(256, 2) ? launch<T, 256, 2, true>(prm, st) : launch<T, 256, 4, true>(prm, st);
+        const int rc = launch<T, 256, 4, 0, ipl::PARTS>(prm, st);
         if (rc != IP_OK) return rc;
         return launched(iph::launch_pdl(ipl::logprob_join_kernel<T>, dim3(static_cast<unsigned>(prm.rows)), dim3(256), 0, st, prm));
     }
-    if (prm.V <= hold(32, 2)) return launch<T, 32, 2, false>(prm, st);
-    if (prm.V <= hold(32, 5)) return launch<T, 32, 5, false>(prm, st);
-    if (prm.V <= hold(32, 8)) return launch<T, 32, 8, false>(prm, st);
-    if (prm.V <= hold(256, 2)) return launch<T, 256, 2, false>(prm, st);
-    return launch<T, 256, 4, false>(prm, st);
+    // a warp's lanes hold a row of up to 1048 in four units and one element more
+    if (prm.V <= hold(32, 1)) return launch<T, 32, 1, 0, ipl::WHOLE>(prm, st);
+    if (prm.V <= hold(32, 2)) return launch<T, 32, 2, 0, ipl::WHOLE>(prm, st);
+    if (prm.V <= hold(32, 4) + 32) return launch<T, 32, 4, 1, ipl::WHOLE>(prm, st);
+    if (prm.V <= hold(32, 8)) return launch<T, 32, 8, 0, ipl::WHOLE>(prm, st);
+    if (prm.V <= hold(256, 2)) return launch<T, 256, 2, 0, ipl::WHOLE>(prm, st);
+    return launch<T, 256, 4, 0, ipl::WHOLE>(prm, st);
 }
 
 }  // namespace
@@ -94,9 +114,9 @@ int ip_token_logprobs(const void *logits, int dtype, long long rows, int V, long
                                  top_logprob, top_token, reinterpret_cast<float *>(ws + 256),
                                  reinterpret_cast<ipl::Key *>(ws + keys_at(rows, p))};
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    if (dtype == IP_F32) return run<float>(prm, st);
-    if (dtype == IP_F16) return run<__half>(prm, st);
-    return run<__nv_bfloat16>(prm, st);
+    if (dtype == IP_F32) return run<float>(prm, p.cluster, st);
+    if (dtype == IP_F16) return run<__half>(prm, p.cluster, st);
+    return run<__nv_bfloat16>(prm, p.cluster, st);
 }
 
 }  // extern "C"

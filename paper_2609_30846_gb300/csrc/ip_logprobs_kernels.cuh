@@ -20,9 +20,9 @@ using namespace ipr;
 // both terms of the entropy >= 0, so that nothing cancels.  An a of -inf has no weight.
 //
 // A row (or one of its parts) is held in registers: one pass over memory, the maximum before the
-// exponentials, so one of them an element.  A short row is a warp's, a longer one a CTA's, and
-// what a CTA's registers do not hold is cut into parts, each a CTA's, that a second kernel joins in
-// a fixed order.
+// exponentials, so one of them an element.  A short row is a warp's, a longer one a CTA's, a longer one
+// still a cluster's, whose first CTA joins the parts' sums and best tokens in its shared memory; what
+// sixteen CTAs do not hold is cut into parts for a second kernel, in a fixed order too.
 //
 // The `top` best: a token's key is its logit's bits in the order of the numbers (-0 as 0), then its
 // index from behind, so that keys are different and among equal logits the lowest index is the
@@ -31,8 +31,11 @@ using namespace ipr;
 // reach it (few more than `top` where logits are not sorted) go to shared memory, and each one's rank is
 // the number of larger keys there.  Where more reach it than there is room for, the best are found one
 // after the other.
+//
+// What bounds it: for many short rows the instructions, about seven an element, for few long ones the latency of
+// the load, the reductions and the join.
 
-constexpr int MAX_TOP = 32;
+constexpr int MAX_TOP = 32, MAX_CLUSTER = 16;
 constexpr int WARP_CANDS = 256, CTA_CANDS = 512;
 
 typedef unsigned long long Key;
@@ -41,13 +44,13 @@ struct LogprobParams {
     const void *x;
     long long rows, ld;
     int V, top;
-    int parts, per;                       // parts a row, elements a part
+    int parts, per;                       // parts a row, elements a part (a multiple of eight)
     float scale;                          // of the logits
     const void *tokens;
     int tokens64;
     float *logprob, *entropy, *top_logprob;
     int *top_token;
-    float *sums;                          // [rows][parts][4] of the parts: m, s, u, not a distribution
+    float *sums;                          // [rows][parts] of PARTS, as Sums
     Key *keys;                            // [rows][parts][top]
 };
 
@@ -156,7 +159,12 @@ __device__ __forceinline__ void best(int top, uint32_t lane_top, Each each, Put 
     }
 }
 
-// Writes a row's results: write(...) by one thread, put(rank, key) by any.  s and u in units of log2.
+// Sums of a row or a part, u in units of log2.
+struct alignas(16) Sums {      // travels between CTAs as one vector
+    float m, s, u, unused;
+};
+
+// Writes a row's results: write(...) by one thread, put(rank, key) by any.
 template <typename T>
 struct RowOut {
     const LogprobParams &prm;
@@ -164,12 +172,13 @@ struct RowOut {
     float m, ls;
     bool none;          // no distribution: a NaN or +inf among the logits, or nothing but -inf
 
-    __device__ __forceinline__ RowOut(const LogprobParams &p, long long r, float m_, float s)
-        : prm(p), row(r), m(m_), ls(logf(s)), none(!(m_ > -INFINITY && m_ < INFINITY) || s != s) {}
+    __device__ __forceinline__ RowOut(const LogprobParams &p, long long r, const Sums &v)
+        : prm(p), row(r), m(v.m), ls(logf(v.s)),
+          none(!(v.m > -INFINITY && v.m < INFINITY) || v.s != v.s) {}
     __device__ __forceinline__ float nan() const { return __uint_as_float(0x7fc00000u); }
     __device__ __forceinline__ float logp(float x) const { return none ? nan() : __fmaf_rn(x - m, prm.scale, -ls); }
-    __device__ __forceinline__ void write(float s, float u) const {
-        prm.entropy[row] = none ? nan() : ls - 0.693147181f * (u / s);
+    __device__ __forceinline__ void write(const Sums &v) const {
+        prm.entropy[row] = none ? nan() : ls - 0.693147181f * (v.u / v.s);
         if (!prm.tokens) return;
         const long long tok = prm.tokens64 ? static_cast<const long long *>(prm.tokens)[row]
                                            : static_cast<long long>(static_cast<const int *>(prm.tokens)[row]);
@@ -188,65 +197,130 @@ __device__ __forceinline__ constexpr uint32_t neg_inf() {
     return sizeof(T) == 4 ? 0xff800000u : (std::is_same<T, __half>::value ? 0xfc00fc00u : 0xff80ff80u);
 }
 
-// TPR threads (32: four rows a CTA, or 256) hold a row, or a part of one (PART, TPR = 256), in U units
-// of eight elements a thread, the first of them `shift` elements before the row, on 16 bytes.
-template <typename T, int TPR, int U, bool PART>
-__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR) logprob_kernel(const LogprobParams prm) {
+// Two f32 numbers in a register pair: one instruction for both.
+typedef unsigned long long Two;
+__device__ __forceinline__ Two two(float a, float b) {
+    Two r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void split(Two v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+
+// Adds the exponentials of two elements, 2^p for p = (x - from) c, and p 2^p; p = -inf: 0.  The difference
+// first, so that an error of p is relative to p and the largest element's is 0.
+__device__ __forceinline__ void add_exp(float x0, float x1, Two minus_from, Two c, Two &s, Two &u) {
+    Two p = two(x0, x1);
+    asm("add.rn.f32x2 %0, %0, %1;" : "+l"(p) : "l"(minus_from));
+    asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(p) : "l"(c));
+    float p0, p1, e0, e1;
+    split(p, p0, p1);
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(p0));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(p1));
+    const Two e = two(e0, e1), q = two(fmaxf(p0, -1e30f), fmaxf(p1, -1e30f));
+    asm("add.rn.f32x2 %0, %0, %1;" : "+l"(s) : "l"(e));
+    asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(u) : "l"(e), "l"(q));
+}
+
+// Joins parts' sums, the thread's being first, first + step, ...
+template <int TPR, typename At>
+__device__ __forceinline__ Sums join(int parts, int first, int step, float c, At at, uint32_t *red) {
     using G = Group<TPR>;
+    float most = -INFINITY;
+    for (int i = first; i < parts; i += step) most = fmaxf(most, at(i).m);
+    Sums v{value_of(G::max_u32(order_of(most), red)), 0.0f, 0.0f, 0.0f};
+    for (int i = first; i < parts; i += step) {
+        const Sums p = at(i);
+        if (p.m == -INFINITY) {
+            v.s += p.s;      // 0, or NaN
+            continue;
+        }
+        const float d = (p.m - v.m) * c;
+        float e;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(d));
+        v.s = __fmaf_rn(p.s, e, v.s);
+        v.u = __fmaf_rn(__fmaf_rn(p.s, fmaxf(d, -1e30f), p.u), e, v.u);
+    }
+    v.s = G::sum(v.s, reinterpret_cast<float *>(red));
+    v.u = G::sum(v.u, reinterpret_cast<float *>(red));
+    return v;
+}
+
+enum { WHOLE = 0, CLUSTER = 1, PARTS = 2 };      // what a group holds: a row, a part joined in the cluster, a part joined later
+
+// TPR threads (32: four rows a CTA, or 256) hold a row or a part of one in U units of eight
+// elements a thread, the first of them `shift` elements before the row, on 16 bytes, and S more elements a thread behind
+// them (a row of 1025 would take a fifth unit for its last elements).
+template <typename T, int TPR, int U, int S, int HOLDS>
+__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? (U > 4 ? 4 : (U == 4 ? 6 : 8)) : (U > 2 ? 4 : 5)) logprob_kernel(const LogprobParams prm) {
+    using G = Group<TPR>;
+    constexpr bool PART = HOLDS != WHOLE;
     constexpr int RPC = TPR == 32 ? 4 : 1, CANDS = TPR == 32 ? WARP_CANDS : CTA_CANDS;
     __shared__ Key cands[RPC][CANDS + 1];
     __shared__ uint32_t red[8];
+    __shared__ Sums part_sums[HOLDS == CLUSTER ? MAX_CLUSTER : 1];
+    __shared__ Key part_keys[HOLDS == CLUSTER ? MAX_CLUSTER * MAX_TOP : 1];
     pdl_launch_dependents();
     pdl_wait();
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
     const long long row = static_cast<long long>(blockIdx.x) * RPC + sub;
     if (row >= prm.rows) return;      // whole warps (TPR = 32), else none
     const int first = PART ? static_cast<int>(blockIdx.y) * prm.per : 0;
-    const int n = PART ? min(prm.per, prm.V - first) : prm.V;
+    const int n = PART ? max(0, min(prm.per, prm.V - first)) : prm.V;
     const T *x = static_cast<const T *>(prm.x) + row * prm.ld + first;
     const int shift = static_cast<int>((reinterpret_cast<uintptr_t>(x) & 15) / sizeof(T));
     Raw8<T> v[U];
+    float tail[S + 1];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         const int c = (i * TPR + t) * 8 - shift;
-#pragma unroll
-        for (int j = 0; j < Raw8<T>::WORDS; ++j) v[i].w[j] = neg_inf<T>();
         if (c >= 0 && c + 8 <= n) {
             v[i].template load<true>(x + c, 8);
-        } else if (c + 8 > 0 && c < n) {
+        } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (c + j >= 0 && c + j < n) {
-                    if constexpr (sizeof(T) == 4) {
-                        v[i].w[j] = reinterpret_cast<const uint32_t *>(x)[c + j];
-                    } else {
-                        const uint32_t b = reinterpret_cast<const uint16_t *>(x)[c + j];
-                        v[i].w[j >> 1] = j & 1 ? (v[i].w[j >> 1] & 0xffffu) | (b << 16) : (v[i].w[j >> 1] & 0xffff0000u) | b;
+            for (int j = 0; j < Raw8<T>::WORDS; ++j) v[i].w[j] = neg_inf<T>();
+            if (c + 8 > 0 && c < n)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c + j >= 0 && c + j < n) {
+                        if constexpr (sizeof(T) == 4) {
+                            v[i].w[j] = reinterpret_cast<const uint32_t *>(x)[c + j];
+                        } else {
+                            const uint32_t b = reinterpret_cast<const uint16_t *>(x)[c + j];
+                            v[i].w[j >> 1] = j & 1 ? (v[i].w[j >> 1] & 0xffffu) | (b << 16) : (v[i].w[j >> 1] & 0xffff0000u) | b;
+                        }
                     }
-                }
         }
+    }
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+        const int k = (U * 8 + i) * TPR + t - shift;
+        tail[i] = k < n ? to_f32(x[k]) : -INFINITY;
     }
     float most = -INFINITY;
 #pragma unroll
     for (int i = 0; i < U; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) most = fmaxf(most, v[i].at(j));
-    const float m = value_of(G::max_u32(order_of(most), red));
+#pragma unroll
+    for (int i = 0; i < S; ++i) most = fmaxf(most, tail[i]);
+    Sums sums{value_of(G::max_u32(order_of(most), red)), 0.0f, 0.0f, 0.0f};
     // nothing but -inf (and NaN): weights of 0, or NaN
-    const float from = m == -INFINITY ? 0.0f : m, c = prm.scale * 1.44269504f;
-    float s = 0.0f, u = 0.0f;
+    const float from = sums.m == -INFINITY ? 0.0f : sums.m, c = prm.scale * 1.44269504f;
+    const Two from2 = two(-from, -from), c2 = two(c, c);
+    Two s2 = two(0.0f, 0.0f), u2 = s2;
 #pragma unroll
     for (int i = 0; i < U; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float p = (v[i].at(j) - from) * c;
-            float e;
-            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(p));
-            s += e;
-            u = __fmaf_rn(e, fmaxf(p, -1e30f), u);
-        }
-    s = G::sum(s, reinterpret_cast<float *>(red));
-    u = G::sum(u, reinterpret_cast<float *>(red));
+        for (int j = 0; j < 8; j += 2) add_exp(v[i].at(j), v[i].at(j + 1), from2, c2, s2, u2);
+#pragma unroll
+    for (int i = 0; i < S; ++i) add_exp(tail[i], -INFINITY, from2, c2, s2, u2);
+    float s0, s1, u0, u1;
+    split(s2, s0, s1);
+    split(u2, u0, u1);
+    sums.s = s0 + s1;
+    sums.u = u0 + u1;
+    sums.s = G::sum(sums.s, reinterpret_cast<float *>(red));
+    sums.u = G::sum(sums.u, reinterpret_cast<float *>(red));
     auto each = [&](auto f) {
 #pragma unroll
         for (int i = 0; i < U; ++i)
@@ -255,25 +329,59 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR) logprob_kernel(const Lo
                 const int k = (i * TPR + t) * 8 - shift + j;
                 f(static_cast<uint32_t>(k) < static_cast<uint32_t>(n) ? key_of(order_of(v[i].at(j)), first + k) : Key(0));
             }
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+            const int k = (U * 8 + i) * TPR + t - shift;
+            f(k < n ? key_of(order_of(tail[i]), first + k) : Key(0));
+        }
     };
     // a thread without elements has nothing to offer (one whose elements are all -inf does)
     const uint32_t lane_top = t * 8 - shift < n ? order_of(most) : 0u;
-    if (PART) {
+    if constexpr (HOLDS == WHOLE) {
+        const RowOut<T> out(prm, row, sums);
+        if (t == 0) out.write(sums);
+        if (prm.top > 0) best<TPR, CANDS>(prm.top, lane_top, each, [&](int r, Key k) { out.put(r, k); }, cands[sub], red);
+    } else if constexpr (HOLDS == PARTS) {
         const long long at = row * prm.parts + blockIdx.y;
-        if (t == 0) *reinterpret_cast<float4 *>(prm.sums + 4 * at) = make_float4(m, s, u, 0.0f);
+        if (t == 0) *reinterpret_cast<float4 *>(prm.sums + 4 * at) = make_float4(sums.m, sums.s, sums.u, 0.0f);
         if (prm.top > 0)
             best<TPR, CANDS>(prm.top, lane_top, each, [&](int r, Key k) { prm.keys[at * prm.top + r] = k; }, cands[sub], red);
     } else {
-        const RowOut<T> out(prm, row, m, s);
-        if (t == 0) out.write(s, u);
-        if (prm.top > 0) best<TPR, CANDS>(prm.top, lane_top, each, [&](int r, Key k) { out.put(r, k); }, cands[sub], red);
+        // to the cluster's first CTA, which is not done before all have been there
+        uint32_t to_sums, to_keys;
+        asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(to_sums) : "r"(smem_u32(part_sums + blockIdx.y)));
+        asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(to_keys) : "r"(smem_u32(part_keys + blockIdx.y * prm.top)));
+        // no CTA writes to another one that has not started
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+        if (t == 0)
+            asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to_sums), "f"(sums.m), "f"(sums.s),
+                         "f"(sums.u), "f"(0.0f)
+                         : "memory");
+        if (prm.top > 0)
+            best<TPR, CANDS>(prm.top, lane_top, each, [&](int r, Key k) {
+                asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to_keys + 8 * r), "l"(k) : "memory");
+            }, cands[sub], red);
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (blockIdx.y != 0) return;
+        const Sums all = join<TPR>(prm.parts, t, TPR, c, [&](int i) { return part_sums[i]; }, red);
+        const RowOut<T> out(prm, row, all);
+        if (t == 0) out.write(all);
+        if (prm.top > 0) {
+            const int keys = prm.parts * prm.top;
+            uint32_t my_top = 0;
+            for (int i = t; i < keys; i += TPR) my_top = max(my_top, static_cast<uint32_t>(part_keys[i] >> 32));
+            best<TPR, CANDS>(prm.top, my_top, [&](auto f) {
+                for (int i = t; i < keys; i += TPR) f(part_keys[i]);
+            }, [&](int r, Key k) { out.put(r, k); }, cands[sub], red);
+        }
     }
 }
 
 // Joins a row's parts, a CTA a row.
 template <typename T>
 __global__ void __launch_bounds__(256) logprob_join_kernel(const LogprobParams prm) {
-    using G = Group<256>;
     __shared__ Key cands[CTA_CANDS + 1];
     __shared__ uint32_t red[8];
     pdl_launch_dependents();
@@ -281,26 +389,12 @@ __global__ void __launch_bounds__(256) logprob_join_kernel(const LogprobParams p
     const int t = threadIdx.x;
     const long long row = blockIdx.x;
     const float4 *parts = reinterpret_cast<const float4 *>(prm.sums) + row * prm.parts;
-    float most = -INFINITY;
-    for (int i = t; i < prm.parts; i += 256) most = fmaxf(most, parts[i].x);
-    const float m = value_of(G::max_u32(order_of(most), red)), c = prm.scale * 1.44269504f;
-    float s = 0.0f, u = 0.0f;
-    for (int i = t; i < prm.parts; i += 256) {
+    const Sums all = join<256>(prm.parts, t, 256, prm.scale * 1.44269504f, [&](int i) {
         const float4 p = parts[i];
-        if (p.x == -INFINITY) {
-            s += p.y;      // 0, or NaN
-            continue;
-        }
-        const float d = (p.x - m) * c;
-        float e;
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(d));
-        s = __fmaf_rn(p.y, e, s);
-        u = __fmaf_rn(__fmaf_rn(p.y, fmaxf(d, -1e30f), p.z), e, u);
-    }
-    s = G::sum(s, reinterpret_cast<float *>(red));
-    u = G::sum(u, reinterpret_cast<float *>(red));
-    const RowOut<T> out(prm, row, m, s);
-    if (t == 0) out.write(s, u);
+        return Sums{p.x, p.y, p.z, p.w};
+    }, red);
+    const RowOut<T> out(prm, row, all);
+    if (t == 0) out.write(all);
     if (prm.top > 0) {
         const Key *keys = prm.keys + row * prm.parts * prm.top;
         const int n = prm.parts * prm.top;

@@ -208,7 +208,7 @@ def test_refusals(ip):
                       (ip.IpError, lambda: f(x, top=-1)), (ip.IpError, lambda: f(x[:, :5].contiguous(), top=6)),
                       (ip.IpError, lambda: f(x, scale=0.0)), (ip.IpError, lambda: f(x, scale=math.nan)),
                       (ip.IpError, lambda: f(x, workspace=ws[:128])), (TypeError, lambda: f(x, workspace=x)),
-                      (ip.IpError, lambda: f(torch.zeros(2, 40000, device="cuda"), workspace=ws)),
+                      (ip.IpError, lambda: f(torch.zeros(2, 200000, device="cuda"), workspace=ws)),
                       (ValueError, lambda: f(x, out=(None, x[0], None, None)))):
         with pytest.raises(err):
             call()
