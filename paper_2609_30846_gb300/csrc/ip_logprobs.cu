@@ -14,8 +14,8 @@ int launched(cudaError_t rc) {
     return rc == cudaSuccess && cudaGetLastError() == cudaSuccess ? IP_OK : IP_ERR_CUDA;
 }
 
-// Elements that U units a thread hold wherever the row starts (up to seven before it).
-constexpr int hold(int threads, int units) { return threads * units * 8 - 8; }
+// Elements that U units a thread hold: all, where rows start on 16 bytes, or eight less (up to seven before a row).
+constexpr int hold(int threads, int units, bool on16 = false) { return threads * units * 8 - (on16 ? 0 : 8); }
 
 // Parts of a row and their elements: one while a CTA holds the row; else a cluster's, as many as come to
 // four CTAs an SM, few rows by sixteen CTAs of few elements (1 x 65536 XX us by 16 CTAs, by 8 XX) and many by those
@@ -23,12 +23,13 @@ constexpr int hold(int threads, int units) { return threads * units * 8 - 8; }
 struct Plan {
     int parts, per, cluster;
 };
-Plan plan(long long rows, int V) {
-    if (V <= hold(256, 4)) return {1, V, 0};
+Plan plan(long long rows, int V, bool on16 = false) {
+    const int most = hold(256, 4, on16);
+    if (V <= most) return {1, V, 0};
     auto per_of = [&](int parts) { return ((V + parts - 1) / parts + 7) / 8 * 8; };
     int parts = 2;
-    while (parts < ipl::MAX_CLUSTER && per_of(parts) > hold(256, 4)) parts *= 2;
-    if (per_of(parts) > hold(256, 4)) return {(V + hold(256, 4) - 1) / hold(256, 4), hold(256, 4), 0};
+    while (parts < ipl::MAX_CLUSTER && per_of(parts) > most) parts *= 2;
+    if (per_of(parts) > most) return {(V + hold(256, 4) - 1) / hold(256, 4), hold(256, 4), 0};
     while (parts < ipl::MAX_CLUSTER && rows * parts * 2 <= 608) parts *= 2;
     return {parts, per_of(parts), 1};
 }
@@ -67,11 +68,11 @@ int launch(const ipl::LogprobParams &prm, cudaStream_t st) {
 }
 
 template <typename T>
-int run(const ipl::LogprobParams &prm, bool cluster, cudaStream_t st) {
+int run(const ipl::LogprobParams &prm, bool cluster, bool on16, cudaStream_t st) {
     if (cluster)
-        return prm.per <= hold(256, 1) ? launch<T, 256, 1, 0, ipl::CLUSTER>(prm, st)
-               : prm.per <= hold(256, 2) ? launch<T, 256, 2, 0, ipl::CLUSTER>(prm, st)
-               : prm.per <= hold(256, 3) ? launch<T, 256, 3, 0, ipl::CLUSTER>(prm, st) : launch<T, 256, 4, 0, ipl::CLUSTER>(prm, st);
+        return prm.per <= hold(256, 1, on16) ? launch<T, 256, 1, 0, ipl::CLUSTER>(prm, st)
+               : prm.per <= hold(256, 2, on16) ? launch<T, 256, 2, 0, ipl::CLUSTER>(prm, st)
+               : prm.per <= hold(256, 3, on16) ? launch<T, 256, 3, 0, ipl::CLUSTER>(prm, st) : launch<T, 256, 4, 0, ipl::CLUSTER>(prm, st);
     if (prm.parts > 1) {
         const int rc = launch<T, 256, 4, 0, ipl::PARTS>(prm, st);
         if (rc != IP_OK) return rc;
@@ -82,7 +83,7 @@ int run(const ipl::LogprobParams &prm, bool cluster, cudaStream_t st) {
     if (prm.V <= hold(32, 2)) return launch<T, 32, 2, 0, ipl::WHOLE>(prm, st);
     if (prm.V <= hold(32, 4) + 32) return launch<T, 32, 4, 1, ipl::WHOLE>(prm, st);
     if (prm.V <= hold(32, 8)) return launch<T, 32, 8, 0, ipl::WHOLE>(prm, st);
-    if (prm.V <= hold(256, 2)) return launch<T, 256, 2, 0, ipl::WHOLE>(prm, st);
+    if (prm.V <= hold(256, 2, on16)) return launch<T, 256, 2, 0, ipl::WHOLE>(prm, st);
     return launch<T, 256, 4, 0, ipl::WHOLE>(prm, st);
 }
 
@@ -107,16 +108,18 @@ int ip_token_logprobs(const void *logits, int dtype, long long rows, int V, long
         (tokens && (!aligned(tokens, tokens_i64 ? 8 : 4) || !aligned(logprob, 4))) ||
         (top > 0 && (!aligned(top_logprob, 4) || !aligned(top_token, 4))))
         return IP_ERR_ALIGN;
-    const Plan p = plan(rows, V);
+    // rows that start on 16 bytes may do with a cluster where others do not, never the other way round
+    const bool on16 = aligned(logits, 16) && (rows == 1 || ld * (dtype == IP_F32 ? 4 : 2) % 16 == 0);
+    const Plan p = plan(rows, V, on16);
     if (workspace_bytes < space(rows, p, top)) return IP_ERR_WORKSPACE;
     char *ws = static_cast<char *>(workspace);
     const ipl::LogprobParams prm{logits, rows, ld, V, top, p.parts, p.per, scale, tokens, tokens_i64, logprob, entropy,
                                  top_logprob, top_token, reinterpret_cast<float *>(ws + 256),
                                  reinterpret_cast<ipl::Key *>(ws + keys_at(rows, p))};
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    if (dtype == IP_F32) return run<float>(prm, p.cluster, st);
-    if (dtype == IP_F16) return run<__half>(prm, p.cluster, st);
-    return run<__nv_bfloat16>(prm, p.cluster, st);
+    if (dtype == IP_F32) return run<float>(prm, p.cluster, on16, st);
+    if (dtype == IP_F16) return run<__half>(prm, p.cluster, on16, st);
+    return run<__nv_bfloat16>(prm, p.cluster, on16, st);
 }
 
 }  // extern "C"

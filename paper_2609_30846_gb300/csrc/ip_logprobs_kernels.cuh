@@ -26,8 +26,7 @@ using namespace ipr;
 //
 // The `top` best: a token's key is its logit's bits in the order of the numbers (-0 as 0), then its
 // index from behind, so that keys are different and among equal logits the lowest index is the
-// larger key.  A lower bound of the key wanted last: of a warp's 32 lane maxima the one of rank `top`
-// (at least `top` elements reach it), the largest of these over the warps.  The elements that
+// larger key.  A lower bound of the key wanted last comes from the lanes' maxima (best).  The elements that
 // reach it (few more than `top` where logits are not sorted) go to shared memory, and each one's rank is
 // the number of larger keys there.  Where more reach it than there is room for, the best are found one
 // after the other.
@@ -64,6 +63,7 @@ __device__ __forceinline__ float value_of(uint32_t k) {
 __device__ __forceinline__ Key key_of(uint32_t order, int i) {
     return static_cast<Key>(order) << 32 | static_cast<uint32_t>(~i);
 }
+__device__ __forceinline__ Key key_from(float least) { return static_cast<Key>(order_of(least)) << 32; }
 __device__ __forceinline__ int index_of(Key k) { return static_cast<int>(~static_cast<uint32_t>(k)); }
 
 // The group of threads that holds a row: a warp or a CTA of 256.
@@ -107,29 +107,37 @@ __device__ __forceinline__ Key warp_max_key(Key v) {
     return static_cast<Key>(hi) << 32 | lo;
 }
 
-// The `top` largest of a group's keys, in order, to put(rank, key).  each(f): f(key) for all of a
-// thread's keys (0: none); lane_top: the largest of their upper halves.
+// The `top` largest of a group's keys, in order, to put(rank, key).  each(least, f): f(key) for those of a
+// thread's keys whose logit is not below `least`; lane_top: the largest of their upper halves (0: none).
 template <int TPR, int CANDS, typename Each, typename Put>
 __device__ __forceinline__ void best(int top, uint32_t lane_top, Each each, Put put, Key *cand, uint32_t *red) {
     using G = Group<TPR>;
     const int lane = threadIdx.x & 31, t = threadIdx.x % TPR;
-    int rank = 0;
+    uint32_t bound;
+    if (top == 1) {
+        bound = G::max_u32(lane_top, red);
+    } else {
+        int rank = 0;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        const uint32_t o = __shfl_sync(0xffffffffu, lane_top, i);
-        rank += o > lane_top || (o == lane_top && i < lane);
+        for (int i = 0; i < 32; ++i) {
+            const uint32_t o = __shfl_sync(0xffffffffu, lane_top, i);
+            rank += o > lane_top || (o == lane_top && i < lane);
+        }
+        // `top` elements reach a warp's lane maximum of rank `top`, or every warp's of rank top / warps
+        bound = G::max_u32(rank == top - 1 ? lane_top : 0u, red);
+        if (G::WARPS > 1) {
+            const uint32_t own = __reduce_max_sync(0xffffffffu, rank == (top - 1) / G::WARPS ? lane_top : 0u);
+            bound = max(bound, ~G::max_u32(~own, red));
+        }
     }
-    const uint32_t bound = G::max_u32(rank == top - 1 ? lane_top : 0u, red);
     uint32_t *count = reinterpret_cast<uint32_t *>(cand);      // the keys from cand[1] on
     G::sync();
     if (t == 0) *count = 0;
     G::sync();
-    if (lane_top >= bound)
-        each([&](Key k) {
-            if (k != 0 && static_cast<uint32_t>(k >> 32) >= bound) {
-                const uint32_t p = atomicAdd(count, 1u);
-                if (p < CANDS) cand[1 + p] = k;
-            }
+    if (lane_top != 0 && lane_top >= bound)
+        each(value_of(max(bound, order_of(-INFINITY))), [&](Key k) {
+            const uint32_t p = atomicAdd(count, 1u);
+            if (p < CANDS) cand[1 + p] = k;
         });
     G::sync();
     const uint32_t found = *count;
@@ -145,7 +153,7 @@ __device__ __forceinline__ void best(int top, uint32_t lane_top, Each each, Put 
         Key last = ~Key(0);
         for (int r = 0; r < top; ++r) {
             Key k = 0;
-            each([&](Key o) { k = o < last && o > k ? o : k; });
+            each(-INFINITY, [&](Key o) { k = o < last && o > k ? o : k; });
             k = warp_max_key(k);
             if (G::WARPS > 1) {
                 __syncthreads();
@@ -321,19 +329,16 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? (U > 4 ? 4 
     sums.u = u0 + u1;
     sums.s = G::sum(sums.s, reinterpret_cast<float *>(red));
     sums.u = G::sum(sums.u, reinterpret_cast<float *>(red));
-    auto each = [&](auto f) {
+    auto each = [&](float least, auto f) {
+        auto one = [&](float a, int k) {
+            if (a >= least && static_cast<uint32_t>(k) < static_cast<uint32_t>(n)) f(key_of(order_of(a), first + k));
+        };
 #pragma unroll
         for (int i = 0; i < U; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int k = (i * TPR + t) * 8 - shift + j;
-                f(static_cast<uint32_t>(k) < static_cast<uint32_t>(n) ? key_of(order_of(v[i].at(j)), first + k) : Key(0));
-            }
+            for (int j = 0; j < 8; ++j) one(v[i].at(j), (i * TPR + t) * 8 - shift + j);
 #pragma unroll
-        for (int i = 0; i < S; ++i) {
-            const int k = (U * 8 + i) * TPR + t - shift;
-            f(k < n ? key_of(order_of(tail[i]), first + k) : Key(0));
-        }
+        for (int i = 0; i < S; ++i) one(tail[i], (U * 8 + i) * TPR + t - shift);
     };
     // a thread without elements has nothing to offer (one whose elements are all -inf does)
     const uint32_t lane_top = t * 8 - shift < n ? order_of(most) : 0u;
@@ -372,8 +377,9 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? (U > 4 ? 4 
             const int keys = prm.parts * prm.top;
             uint32_t my_top = 0;
             for (int i = t; i < keys; i += TPR) my_top = max(my_top, static_cast<uint32_t>(part_keys[i] >> 32));
-            best<TPR, CANDS>(prm.top, my_top, [&](auto f) {
-                for (int i = t; i < keys; i += TPR) f(part_keys[i]);
+            best<TPR, CANDS>(prm.top, my_top, [&](float least, auto f) {
+                for (int i = t; i < keys; i += TPR)
+                    if (part_keys[i] >= key_from(least)) f(part_keys[i]);
             }, [&](int r, Key k) { out.put(r, k); }, cands[sub], red);
         }
     }
@@ -400,8 +406,9 @@ __global__ void __launch_bounds__(256) logprob_join_kernel(const LogprobParams p
         const int n = prm.parts * prm.top;
         uint32_t lane_top = 0;
         for (int i = t; i < n; i += 256) lane_top = max(lane_top, static_cast<uint32_t>(keys[i] >> 32));
-        auto each = [&](auto f) {
-            for (int i = t; i < n; i += 256) f(keys[i]);
+        auto each = [&](float least, auto f) {
+            for (int i = t; i < n; i += 256)
+                if (keys[i] >= key_from(least)) f(keys[i]);
         };
         best<256, CTA_CANDS>(prm.top, lane_top, each, [&](int r, Key k) { out.put(r, k); }, cands, red);
     }
