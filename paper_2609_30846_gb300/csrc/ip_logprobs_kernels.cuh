@@ -35,7 +35,7 @@ using namespace ipr;
 // the load, the reductions and the join.
 
 constexpr int MAX_TOP = 32, MAX_CLUSTER = 16;
-constexpr int WARP_CANDS = 256, CTA_CANDS = 512;
+constexpr int WARP_CANDS = 512, CTA_CANDS = 512;
 
 typedef unsigned long long Key;
 
@@ -107,8 +107,33 @@ __device__ __forceinline__ Key warp_max_key(Key v) {
     return static_cast<Key>(hi) << 32 | lo;
 }
 
-// The `top` largest of a group's keys, in order, to put(rank, key).  each(least, f): f(key) for those of a
-// thread's keys whose logit is not below `least`; lane_top: the largest of their upper halves (0: none).
+// The lanes' value of rank `top` (from 1 on; equal ones share the rank of the last), in all lanes.  For few by
+// taking the largest away, for more by every lane's rank.
+__device__ __forceinline__ uint32_t lane_max_of_rank(uint32_t v, int top) {
+    if (top <= 8) {
+        uint32_t m = 0;
+        for (int left = top; left > 0;) {
+            m = __reduce_max_sync(0xffffffffu, v);
+            const unsigned lanes = __ballot_sync(0xffffffffu, v == m);
+            left -= __popc(lanes);
+            if (m == 0) break;
+            if (v == m) v = 0;
+        }
+        return m;
+    }
+    const int lane = threadIdx.x & 31;
+    int rank = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        const uint32_t o = __shfl_sync(0xffffffffu, v, i);
+        rank += o > v || (o == v && i < lane);
+    }
+    return __reduce_max_sync(0xffffffffu, rank == top - 1 ? v : 0u);
+}
+
+// The `top` largest of a group's keys, in order, to put(rank, key).  each(least, f): f(have, key), by all lanes
+// together, for those of the threads' keys whose logit is not below `least`; lane_top: the largest of
+// the upper halves of a thread's (0: none).
 template <int TPR, int CANDS, typename Each, typename Put>
 __device__ __forceinline__ void best(int top, uint32_t lane_top, Each each, Put put, Key *cand, uint32_t *red) {
     using G = Group<TPR>;
@@ -117,43 +142,56 @@ __device__ __forceinline__ void best(int top, uint32_t lane_top, Each each, Put 
     if (top == 1) {
         bound = G::max_u32(lane_top, red);
     } else {
-        int rank = 0;
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            const uint32_t o = __shfl_sync(0xffffffffu, lane_top, i);
-            rank += o > lane_top || (o == lane_top && i < lane);
-        }
         // `top` elements reach a warp's lane maximum of rank `top`, or every warp's of rank top / warps
-        bound = G::max_u32(rank == top - 1 ? lane_top : 0u, red);
-        if (G::WARPS > 1) {
-            const uint32_t own = __reduce_max_sync(0xffffffffu, rank == (top - 1) / G::WARPS ? lane_top : 0u);
-            bound = max(bound, ~G::max_u32(~own, red));
-        }
+        const uint32_t alone = lane_max_of_rank(lane_top, top);
+        bound = G::max_u32(alone, red);
+        if (G::WARPS > 1) bound = max(bound, ~G::max_u32(~lane_max_of_rank(lane_top, (top - 1) / G::WARPS + 1), red));
     }
     uint32_t *count = reinterpret_cast<uint32_t *>(cand);      // the keys from cand[1] on
     G::sync();
     if (t == 0) *count = 0;
     G::sync();
-    if (lane_top != 0 && lane_top >= bound)
-        each(value_of(max(bound, order_of(-INFINITY))), [&](Key k) {
-            const uint32_t p = atomicAdd(count, 1u);
-            if (p < CANDS) cand[1 + p] = k;
+    uint32_t found = 0;
+    if (__any_sync(0xffffffffu, lane_top != 0 && lane_top >= bound))
+        each(value_of(max(bound, order_of(-INFINITY))), [&](bool have, Key k) {
+            const unsigned lanes = __ballot_sync(0xffffffffu, have);
+            uint32_t p = found;
+            if (G::WARPS > 1) {
+                if (lane == 0) p = atomicAdd(count, static_cast<uint32_t>(__popc(lanes)));
+                p = __shfl_sync(0xffffffffu, p, 0);
+            }
+            found += __popc(lanes);
+            p += __popc(lanes & ((1u << lane) - 1));
+            if (have && p < CANDS) cand[1 + p] = k;
         });
     G::sync();
-    const uint32_t found = *count;
+    if (G::WARPS > 1) found = *count;
     if (found <= CANDS) {
-        for (uint32_t p = t; p < found; p += TPR) {
-            const Key k = cand[1 + p];
-            int r = 0;
-            for (uint32_t j = 0; j < found; ++j) r += cand[1 + j] > k;
-            if (r < top) put(r, k);
+        // up to four a thread at a time
+        for (uint32_t p = t; p < found; p += 4 * TPR) {
+            Key k[4];
+            int r[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) k[i] = p + i * TPR < found ? cand[1 + p + i * TPR] : ~Key(0);
+            if (found <= TPR) {
+                for (uint32_t j = 0; j < found; ++j) r[0] += cand[1 + j] > k[0];
+            } else {
+                for (uint32_t j = 0; j < found; ++j) {
+                    const Key o = cand[1 + j];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) r[i] += o > k[i];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (p + i * TPR < found && r[i] < top) put(r[i], k[i]);
         }
         for (int r = static_cast<int>(found) + t; r < top; r += TPR) put(r, Key(0));
     } else {
         Key last = ~Key(0);
         for (int r = 0; r < top; ++r) {
             Key k = 0;
-            each(-INFINITY, [&](Key o) { k = o < last && o > k ? o : k; });
+            each(-INFINITY, [&](bool have, Key o) { k = have && o < last && o > k ? o : k; });
             k = warp_max_key(k);
             if (G::WARPS > 1) {
                 __syncthreads();
@@ -329,16 +367,26 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? (U > 4 ? 4 
     sums.u = u0 + u1;
     sums.s = G::sum(sums.s, reinterpret_cast<float *>(red));
     sums.u = G::sum(sums.u, reinterpret_cast<float *>(red));
+    // the few elements that reach a bound are read again: an index into registers would have every one's code unrolled
     auto each = [&](float least, auto f) {
-        auto one = [&](float a, int k) {
-            if (a >= least && static_cast<uint32_t>(k) < static_cast<uint32_t>(n)) f(key_of(order_of(a), first + k));
-        };
 #pragma unroll
-        for (int i = 0; i < U; ++i)
+        for (int i = 0; i < U; ++i) {
+            uint32_t found = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) one(v[i].at(j), (i * TPR + t) * 8 - shift + j);
+            for (int j = 0; j < 8; ++j) found |= v[i].at(j) >= least ? 1u << j : 0u;
+            while (__any_sync(0xffffffffu, found != 0)) {
+                const int k = (i * TPR + t) * 8 - shift + __ffs(static_cast<int>(found)) - 1;
+                const bool have = found != 0 && static_cast<uint32_t>(k) < static_cast<uint32_t>(n);
+                found &= found - 1;
+                f(have, have ? key_of(order_of(to_f32(x[k])), first + k) : Key(0));
+            }
+        }
 #pragma unroll
-        for (int i = 0; i < S; ++i) one(tail[i], (U * 8 + i) * TPR + t - shift);
+        for (int i = 0; i < S; ++i) {
+            const int k = (U * 8 + i) * TPR + t - shift;
+            const bool have = tail[i] >= least && k < n;
+            if (__any_sync(0xffffffffu, have)) f(have, key_of(order_of(tail[i]), first + k));
+        }
     };
     // a thread without elements has nothing to offer (one whose elements are all -inf does)
     const uint32_t lane_top = t * 8 - shift < n ? order_of(most) : 0u;
@@ -378,8 +426,10 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? (U > 4 ? 4 
             uint32_t my_top = 0;
             for (int i = t; i < keys; i += TPR) my_top = max(my_top, static_cast<uint32_t>(part_keys[i] >> 32));
             best<TPR, CANDS>(prm.top, my_top, [&](float least, auto f) {
-                for (int i = t; i < keys; i += TPR)
-                    if (part_keys[i] >= key_from(least)) f(part_keys[i]);
+                for (int i = t; i - t < keys; i += TPR) {
+                    const Key k = i < keys ? part_keys[i] : Key(0);
+                    f(k >= key_from(least), k);
+                }
             }, [&](int r, Key k) { out.put(r, k); }, cands[sub], red);
         }
     }
@@ -407,8 +457,10 @@ __global__ void __launch_bounds__(256) logprob_join_kernel(const LogprobParams p
         uint32_t lane_top = 0;
         for (int i = t; i < n; i += 256) lane_top = max(lane_top, static_cast<uint32_t>(keys[i] >> 32));
         auto each = [&](float least, auto f) {
-            for (int i = t; i < n; i += 256)
-                if (keys[i] >= key_from(least)) f(keys[i]);
+            for (int i = t; i - t < n; i += 256) {
+                const Key k = i < n ? keys[i] : Key(0);
+                f(k >= key_from(least), k);
+            }
         };
         best<256, CTA_CANDS>(prm.top, lane_top, each, [&](int r, Key k) { out.put(r, k); }, cands, red);
     }
