@@ -59,7 +59,7 @@ struct Tile {
     static constexpr int SF_COLS = 16 + 16 * WT;      // of a stage
     static constexpr int COLS = 512;
     static constexpr int TMEM_PTR = 256, DEAD = 260;
-    static constexpr int FETCHED = 272;               // stages, of x and of w
+    static constexpr int FETCHED = 272;               // stages, of x, of w and of scales
     static constexpr int OTHER = 288;                 // of the other CTA of a pair: given up, -, stages fetched
     static constexpr int CONSTS = 512;                // sw and bias of a tile's columns
     // per output warp: a block of 32 rows x 64 bytes on its way out
@@ -356,12 +356,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                     if (++s == C::ST) s = 0, ph ^= 1;
                 }
             }
-            // after a wait that ran out the copies in flight land before the CTA ends: the scales here, the others below
-            if (warp != SCALES_WARP)
-                fetched[warp == W_WARP] = issued;
-            else if (!ok)
-                for (int i = issued > C::ST ? issued - C::ST : 0; i < issued; ++i)
-                    mbar_wait(scales(i % C::ST), static_cast<uint32_t>((i / C::ST) & 1), ips::LAND_CYCLES);
+            fetched[warp == X_WARP ? 0 : (warp == W_WARP ? 1 : 2)] = issued;
         }
     } else if (warp == MMA_WARP) {
         if (rank == 0 && worker < prm.tiles) {
@@ -529,8 +524,9 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         if (!ODD && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");      // no block is still on its way
     }
-    // A pair's copies report to the first CTA's barriers, so there is one place to wait for those in flight:
-    // a stage that not all of its fetching threads came to lacks their arrivals.
+    // After a wait that ran out the copies in flight land before a CTA ends.  The scales' report to their own CTA's
+    // barriers; a pair's others to the first CTA's, where a stage that not all of its fetching
+    // threads came to lacks their arrivals.
     volatile int *other = reinterpret_cast<volatile int *>(smem + C::OTHER);
     __syncthreads();
     if (PAIR) {
@@ -541,6 +537,9 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         cluster_sync();
     }
+    if (threadIdx.x == 0 && (*dead || (PAIR && other[0])))
+        for (int n = fetched[2], i = n > C::ST ? n - C::ST : 0; i < n; ++i)
+            mbar_wait(scales(i % C::ST), static_cast<uint32_t>((i / C::ST) & 1), ips::LAND_CYCLES);
     if (threadIdx.x == 0 && rank == 0 && (*dead || (PAIR && other[0]))) {
         const int n[4] = {fetched[0], fetched[1], PAIR ? other[2] : fetched[0], PAIR ? other[3] : fetched[1]};
         const int last = max(max(n[0], n[1]), max(n[2], n[3]));

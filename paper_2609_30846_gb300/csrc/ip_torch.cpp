@@ -433,6 +433,21 @@ bool type_of(PyObject *dtype, PyObject *out, at::ScalarType &type) {
     return code_of(type) >= 0;
 }
 
+// Stride of rows whose leading axes are walked with one, 0 for what the general form has to look at.
+int64_t rows_stride(const at::Tensor &t) {
+    if (t.stride(-1) != 1 && t.size(-1) != 1) return 0;
+    if (t.numel() <= t.size(-1)) return (t.size(-1) + 15) / 16 * 16;      // one row or none: any stride does
+    int64_t ld = 0, rows = 1;
+    for (int64_t i = t.dim() - 2; i >= 0; --i) {
+        if (t.size(i) != 1) {
+            if (ld == 0) ld = t.stride(i);
+            else if (t.stride(i) != ld * rows) return 0;
+        }
+        rows *= t.size(i);
+    }
+    return ld;
+}
+
 // Rows of bytes with a scale each, and for 4-bit rows (d elements, -1: two a byte) their blocks.
 struct ByteRows {
     const at::Tensor *q, *scale, *blocks;
@@ -447,7 +462,7 @@ struct ByteRows {
         if (n < 1 || n > INT_MAX / 2 || scale->sizes() != lead()) return false;
         d = oblocks ? (want < 0 ? 2 * n : want) : n;
         rows = q->numel() / n;
-        ld = row_stride(*q);
+        ld = rows_stride(*q);
         if (ld < n) return false;
         if (!oblocks) return true;
         return (d + 1) / 2 == n && contiguous(blocks, at::kByte, dev) && blocks->dim() == 3 &&
@@ -460,10 +475,12 @@ struct ByteRows {
 };
 
 PyObject *values(PyObject *oq, PyObject *oscale, PyObject *oblocks, int64_t d, PyObject *dtype, PyObject *o) {
-    const int dev = c10::cuda::current_device();
+    const at::Tensor *q = tensor(oq);
     ByteRows r;
     at::ScalarType type;
-    if (!type_of(dtype, o, type) || !r.take(oq, oscale, oblocks, d, dev)) Py_RETURN_NONE;
+    if (!q || !type_of(dtype, o, type)) Py_RETURN_NONE;
+    const int dev = q->get_device();
+    if (dev != c10::cuda::current_device() || !r.take(oq, oscale, oblocks, d, dev)) Py_RETURN_NONE;
     c10::SmallVector<int64_t, 6> shape(r.lead().begin(), r.lead().end());
     shape.push_back(r.d);
     at::Tensor out;
