@@ -366,7 +366,13 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, rows_ctas<T, TPR, UNITS
                 reduce<WARPS>(ss, unused, red, turn);
             }
             root = __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, static_cast<float>(d)), eps));
+            // of a large row half of the power on either side of the quotient, so that a large weight's stays in range
+            if (up < 1.0f) root *= 0x1p40f, up = 0x1p-40f;
         }
+        // v / (root / up); of a small row a small v is scaled first
+        auto over_root = [&](float v) {
+            return up > 1.0f && v < 1.0f ? __fdiv_rn(__fmul_rn(v, up), root) : __fmul_rn(__fdiv_rn(v, root), up);
+        };
         const bool zero = !finite || bits == 0;
         const int e = static_cast<int>(bits >> 23);
         uint8_t *q = prm.q + row * prm.ldq;
@@ -380,7 +386,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, rows_ctas<T, TPR, UNITS
         };
         if constexpr (OUT == OUT_I8) {
             if (t == 0)
-                prm.scale[row] = finite ? (bits == 0 ? 0.0f : __fdiv_rn(__fmul_rn(__fdiv_rn(amax, root), up), 127.0f)) : __uint_as_float(0x7fc00000u);
+                prm.scale[row] = finite ? (bits == 0 ? 0.0f : __fdiv_rn(over_root(amax), 127.0f)) : __uint_as_float(0x7fc00000u);
             // rows near the ends of the range are brought to the middle by a power of two
             const bool far = e < 32 || e > 222;
             const int fe = 254 - e < 1 ? 1 : (254 - e > 253 ? 253 : 254 - e);
@@ -414,7 +420,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, rows_ctas<T, TPR, UNITS
             ex = ex < -126 ? -126 : ex;
             const float f = __uint_as_float(static_cast<unsigned>(127 - ex) << 23);
             const float r = __uint_as_float(static_cast<unsigned>(127 + ex) << 23);
-            if (t == 0) prm.scale[row] = finite ? (bits == 0 ? 0.0f : NORM ? __fmul_rn(__fdiv_rn(r, root), up) : r) : __uint_as_float(0x7fc00000u);
+            if (t == 0) prm.scale[row] = finite ? (bits == 0 ? 0.0f : NORM ? over_root(r) : r) : __uint_as_float(0x7fc00000u);
             // a row near the ends of the range is scaled by f itself, others' elements stay as they are
             const bool far = ex < -100 || ex > 100;
             const Fp4Row fr{far ? 1.0f : f, far ? 1.0f : r};

@@ -99,6 +99,16 @@ def test_extreme_ranges(ip, dtype, scale, eps):
         check(ip, x, g, eps=eps)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale,weight", [(1e17, 1e20), (1e30, 1e7), (1e20, 1e-38), (1e-12, 1e-30), (1e-20, 1e-20), (1e-12, 1e30),
+                                          (1e-30, 1e20)])
+def test_extreme_weights(ip, dtype, scale, weight):
+    # the scale itself is well inside f32's range, its factors are not
+    for d in (300, 2000, 9000):
+        x, g, _ = draw(5, d, torch.float32, d, False)
+        check(ip, (x / x.abs().amax() * scale).to(DT[dtype]), (g / g.abs().amax() * weight).to(DT[dtype]), eps=0.0)
+
+
 @pytest.mark.parametrize("dtype", list(DT))
 @pytest.mark.parametrize("bad", ["nan", "inf", "-inf"])
 def test_not_finite(ip, dtype, bad):
