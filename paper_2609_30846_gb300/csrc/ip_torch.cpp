@@ -7,17 +7,20 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
-#include <ATen/ops/empty.h>
-#include <ATen/ops/empty_strided.h>
+#include <c10/core/Storage.h>
+#include <c10/core/TensorImpl.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <array>
 #include <climits>
 #include <initializer_list>
 #include <type_traits>
+#include <utility>
 
 #include "ip_mhsa.h"
 
@@ -71,8 +74,51 @@ bool fits(int64_t n) { return n <= INT_MAX; }
 ip_stream_t stream_of(int dev) {
     return reinterpret_cast<ip_stream_t>(c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(dev)).stream());
 }
-at::Tensor empty(at::IntArrayRef shape, const at::Tensor &like, at::ScalarType type) {
-    return at::empty(shape, like.options().dtype(type).requires_grad(false));
+
+// Memory of the current device and stream for a call's outputs, taken piece by piece.  Outputs of up to
+// TOGETHER bytes in all share one allocation, which is what they cost the host most of (a call with four of
+// them 4.8 us of a Grace core, 7.9 one by one); larger ones have their own, so that none keeps another's memory alive.
+class Memory {
+public:
+    static constexpr size_t TOGETHER = 1 << 20;
+    // what a piece of n bytes takes
+    static size_t piece(int64_t n) { return (static_cast<size_t>(n) + 127) & ~static_cast<size_t>(127); }
+
+    explicit Memory(size_t bytes) : shared_(bytes <= TOGETHER) {
+        if (shared_) storage_ = allocate(bytes);
+    }
+    // strides empty: contiguous; n: the bytes
+    at::Tensor take(at::IntArrayRef shape, at::IntArrayRef strides, at::ScalarType type, int64_t n) {
+        c10::Storage own = shared_ ? storage_ : allocate(static_cast<size_t>(n));
+        at::Tensor t = at::detail::make_tensor<at::TensorImpl>(std::move(own), c10::DispatchKeySet(c10::DispatchKey::CUDA),
+                                                               c10::scalarTypeToTypeMeta(type));
+        at::TensorImpl *impl = t.unsafeGetTensorImpl();
+        if (strides.empty()) impl->set_sizes_contiguous(shape);
+        else impl->set_sizes_and_strides(shape, strides);
+        if (shared_) {
+            impl->set_storage_offset(static_cast<int64_t>(used_ / c10::elementSize(type)));
+            used_ += piece(n);
+        }
+        return t;
+    }
+    at::Tensor take(at::IntArrayRef shape, at::ScalarType type) { return take(shape, {}, type, bytes_of(shape, type)); }
+    static int64_t bytes_of(at::IntArrayRef shape, at::ScalarType type) {
+        return c10::multiply_integers(shape) * static_cast<int64_t>(c10::elementSize(type));
+    }
+
+private:
+    static c10::Storage allocate(size_t n) {
+        c10::Allocator *a = c10::cuda::CUDACachingAllocator::get();
+        return c10::Storage(c10::Storage::use_byte_size_t(), n, a->allocate(n), a, true);
+    }
+    bool shared_;
+    c10::Storage storage_;
+    size_t used_ = 0;
+};
+
+// A new tensor on the current device, which is like's.
+at::Tensor empty(at::IntArrayRef shape, const at::Tensor &, at::ScalarType type) {
+    return Memory(Memory::TOGETHER + 1).take(shape, type);
 }
 // The caller's output o, or a new one for None; false for what the general form has to look at.
 bool output(PyObject *o, at::IntArrayRef shape, const at::Tensor &like, at::ScalarType type, at::Tensor &out) {
@@ -116,6 +162,21 @@ bool arity(Py_ssize_t n, Py_ssize_t want) {
     return false;
 }
 
+// Rows of n elements of one byte each, `lead` of them, on multiples of 16 bytes.
+struct ByteShape {
+    c10::SmallVector<int64_t, 6> shape, strides;
+    int64_t ld, bytes;
+
+    ByteShape(at::IntArrayRef lead, int64_t n) : shape(lead.begin(), lead.end()), ld((n + 15) / 16 * 16) {
+        shape.push_back(n);
+        bytes = c10::multiply_integers(lead) * ld;
+        if (ld == n) return;
+        strides.resize(shape.size(), 1);
+        int64_t step = ld;
+        for (size_t i = shape.size() - 1; i-- > 0; step *= shape[i] > 1 ? shape[i] : 1) strides[i] = step;
+    }
+};
+
 // (x, q, scale)
 PyObject *quantize_rows(PyObject *, PyObject *const *a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
@@ -132,10 +193,8 @@ PyObject *quantize_rows(PyObject *, PyObject *const *a, Py_ssize_t n) {
         if (!output(a[1], shape, *x, at::kChar, q)) Py_RETURN_NONE;
         ld = d;
     } else {
-        c10::SmallVector<int64_t, 6> strides(shape.size(), 1);
-        int64_t step = ld;
-        for (size_t i = shape.size() - 1; i-- > 0; step *= shape[i] > 1 ? shape[i] : 1) strides[i] = step;
-        q = at::empty_strided(shape, strides, x->options().dtype(at::kChar).requires_grad(false));
+        const ByteShape rows(x->sizes().slice(0, x->dim() - 1), d);
+        q = Memory(Memory::TOGETHER + 1).take(rows.shape, rows.strides, at::kChar, rows.bytes);
     }
     shape.pop_back();
     if (!output(a[2], shape, *x, at::kFloat, scale)) Py_RETURN_NONE;
@@ -327,18 +386,6 @@ PyObject *tuple(std::initializer_list<const at::Tensor *> list) {
     return r;
 }
 
-// New rows of n elements of one byte each, `lead` of them, on multiples of 16 bytes; ld: their stride.
-at::Tensor byte_rows(at::IntArrayRef lead, int64_t n, const at::Tensor &like, at::ScalarType type, int64_t &ld) {
-    c10::SmallVector<int64_t, 6> shape(lead.begin(), lead.end());
-    shape.push_back(n);
-    ld = (n + 15) / 16 * 16;
-    if (ld == n) return empty(shape, like, type);
-    c10::SmallVector<int64_t, 6> strides(shape.size(), 1);
-    int64_t step = ld;
-    for (size_t i = shape.size() - 1; i-- > 0; step *= shape[i] > 1 ? shape[i] : 1) strides[i] = step;
-    return at::empty_strided(shape, strides, like.options().dtype(type).requires_grad(false));
-}
-
 // Contiguous rows of real values on the current device.
 struct Rows {
     const at::Tensor *x;
@@ -356,10 +403,7 @@ struct Rows {
         return true;
     }
     at::IntArrayRef lead() const { return x->sizes().slice(0, x->dim() - 1); }
-    at::Tensor blocks() const {
-        const int64_t shape[3] = {(rows + 127) / 128, (d + 63) / 64, 512};
-        return empty(shape, *x, at::kByte);
-    }
+    std::array<int64_t, 3> blocks() const { return {(rows + 127) / 128, (d + 63) / 64, 512}; }
 };
 
 // (x, q, blocks, scale), the last three None
@@ -368,9 +412,11 @@ PyObject *quantize_fp4(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (!arity(n, 4)) return nullptr;
     Rows r;
     if (a[1] != Py_None || a[2] != Py_None || a[3] != Py_None || !r.take(a[0])) Py_RETURN_NONE;
-    int64_t ld;
-    const at::Tensor q = byte_rows(r.lead(), (r.d + 1) / 2, *r.x, at::kByte, ld), blocks = r.blocks(),
-                     scale = empty(r.lead(), *r.x, at::kFloat);
+    const ByteShape codes(r.lead(), (r.d + 1) / 2);
+    const int64_t block_bytes = Memory::bytes_of(r.blocks(), at::kByte), ld = codes.ld;
+    Memory mem(Memory::piece(codes.bytes) + Memory::piece(block_bytes) + Memory::piece(4 * r.rows));
+    const at::Tensor q = mem.take(codes.shape, codes.strides, at::kByte, codes.bytes), blocks = mem.take(r.blocks(), at::kByte),
+                     scale = mem.take(r.lead(), at::kFloat);
     const int rc = unlocked([&] {
         return g_entry.quantize_fp4(r.x->const_data_ptr(), r.code, r.rows, static_cast<int>(r.d), r.d,
                                     static_cast<uint8_t *>(q.data_ptr()), ld, static_cast<uint8_t *>(blocks.data_ptr()),
@@ -392,18 +438,24 @@ PyObject *norm(PyObject *const *a, Py_ssize_t n, bool fp4) {
     const at::Tensor *w = tensor(a[1]), *res = nullptr;
     if (!vector(w, type, r.d, r.dev)) Py_RETURN_NONE;
     at::Tensor sum;
+    const bool new_sum = a[2] != Py_None && a[4] == Py_None;
     if (a[2] != Py_None) {
         res = tensor(a[2]);
-        if (!contiguous(res, type, r.dev) || res->sizes() != r.x->sizes() || !output(a[4], r.x->sizes(), *r.x, type, sum))
+        if (!contiguous(res, type, r.dev) || res->sizes() != r.x->sizes() ||
+            (!new_sum && !output(a[4], r.x->sizes(), *r.x, type, sum)))
             Py_RETURN_NONE;
     } else if (a[4] != Py_None) {
         Py_RETURN_NONE;
     }
-    int64_t ld;
-    const at::Tensor q = byte_rows(r.lead(), fp4 ? (r.d + 1) / 2 : r.d, *r.x, fp4 ? at::kByte : at::kChar, ld);
-    const at::Tensor scale = empty(r.lead(), *r.x, at::kFloat);
+    const ByteShape codes(r.lead(), fp4 ? (r.d + 1) / 2 : r.d);
+    const int64_t block_bytes = fp4 ? Memory::bytes_of(r.blocks(), at::kByte) : 0, ld = codes.ld;
+    const int64_t sum_bytes = new_sum ? Memory::bytes_of(r.x->sizes(), type) : 0;
+    Memory mem(Memory::piece(codes.bytes) + Memory::piece(block_bytes) + Memory::piece(4 * r.rows) + Memory::piece(sum_bytes));
+    const at::Tensor q = mem.take(codes.shape, codes.strides, fp4 ? at::kByte : at::kChar, codes.bytes);
+    const at::Tensor scale = mem.take(r.lead(), at::kFloat);
     at::Tensor blocks;
-    if (fp4) blocks = r.blocks();
+    if (fp4) blocks = mem.take(r.blocks(), at::kByte);
+    if (new_sum) sum = mem.take(r.x->sizes(), type);
     const float eps = static_cast<float>(PyFloat_AS_DOUBLE(a[3]));
     const void *pr = res ? res->const_data_ptr() : nullptr;
     void *ps = res ? sum.data_ptr() : nullptr;
@@ -567,18 +619,20 @@ PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
         wide = tok->scalar_type() == at::kLong;
         if (!wide && tok->scalar_type() != at::kInt) Py_RETURN_NONE;
     }
-    at::Tensor lp, ent = empty(lead, *x, at::kFloat), tlp, ttok;
-    if (tok) lp = empty(lead, *x, at::kFloat);
+    const int64_t rows = x->numel() / V;
+    Memory mem(2 * Memory::piece(4 * rows) + 2 * Memory::piece(4 * rows * top));
+    at::Tensor lp, ent = mem.take(lead, at::kFloat), tlp, ttok;
+    if (tok) lp = mem.take(lead, at::kFloat);
     if (top > 0) {
         c10::SmallVector<int64_t, 6> shape(lead.begin(), lead.end());
         shape.push_back(top);
-        tlp = empty(shape, *x, at::kFloat);
-        ttok = empty(shape, *x, at::kInt);
+        tlp = mem.take(shape, at::kFloat);
+        ttok = mem.take(shape, at::kInt);
     }
     const float scale = static_cast<float>(PyFloat_AS_DOUBLE(a[3]));
     auto data = [](const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
     const int rc = unlocked([&] {
-        return g_entry.logprobs(x->const_data_ptr(), code, x->numel() / V, static_cast<int>(V), ld,
+        return g_entry.logprobs(x->const_data_ptr(), code, rows, static_cast<int>(V), ld,
                                 tok ? tok->const_data_ptr() : nullptr, wide ? 1 : 0, scale, static_cast<int>(top),
                                 static_cast<float *>(data(lp)), static_cast<float *>(data(ent)),
                                 static_cast<float *>(data(tlp)), static_cast<int32_t *>(data(ttok)), ws->data_ptr(),
