@@ -152,21 +152,56 @@ int run(const Operands &o, ip4::Params prm, int nsm, cudaStream_t st) {
 
 long long rounds(long long tiles, int workers) { return (tiles + workers - 1) / workers; }
 
-// The form that a launch is expected to take the least time in, ns: a start, and for each round of tiles over
-// the SMs the stages (all forms are held up by shared memory, which serves the MMAs, the copies in and the
+// The times, ns, that the forms of tiles are expected to take: a start, and for each round of tiles over the
+// SMs the stages (all forms are held up by shared memory, which serves the MMAs, the copies in and the
 // scales) with what does not overlap of the hand-over to the output warps, or their time where K is short.
-template <typename T>
-int run(const Operands &o, const ip4::Params &prm, int nsm, cudaStream_t st) {
-    const long long stages = (prm.steps + 3) / 4, tm = (prm.M + ip4::TILE_M - 1) / ip4::TILE_M;
+struct Times {
+    long long t64, t128, pair;
+    long long least() const { return t64 < t128 ? (t64 < pair ? t64 : pair) : (t128 < pair ? t128 : pair); }
+};
+Times tile_times(long long M, int N, int steps, int nsm) {
+    const long long stages = (steps + 3) / 4, tm = (M + ip4::TILE_M - 1) / ip4::TILE_M;
     auto time = [&](long long start, long long tiles, int workers, long long stage, long long over, long long out) {
         const long long tile = stage * stages + over;
         return start + rounds(tiles, workers) * (tile > out ? tile : out);
     };
-    const long long t64 = time(3300, tm * ((prm.N + 63) / 64), nsm, 340, 300, 930);
-    const long long t128 = time(3700, tm * ((prm.N + 127) / 128), nsm, 340, 360, 1200);
-    const long long pair = time(5100, (tm + 1) / 2 * ((prm.N + 255) / 256), nsm / 2, 385, 1200, 2050);
-    if (pair < t64 && pair < t128) return run<T, 256, true>(o, prm, nsm, st);
-    return t128 < t64 ? run<T, 128, false>(o, prm, nsm, st) : run<T, 64, false>(o, prm, nsm, st);
+    return {time(3300, tm * ((N + 63) / 64), nsm, 340, 300, 930), time(3700, tm * ((N + 127) / 128), nsm, 340, 360, 1200),
+            time(5100, (tm + 1) / 2 * ((N + 255) / 256), nsm / 2, 385, 1200, 2050)};
+}
+
+template <typename T>
+int run(const Operands &o, const ip4::Params &prm, const Times &t, int nsm, cudaStream_t st) {
+    if (t.pair < t.t64 && t.pair < t.t128) return run<T, 256, true>(o, prm, nsm, st);
+    return t.t128 < t.t64 ? run<T, 128, false>(o, prm, nsm, st) : run<T, 64, false>(o, prm, nsm, st);
+}
+
+// Up to this many rows ordinary lanes may take, with one reading of the weights (few_rows_kernel).
+constexpr int FEW_ROWS = 8;
+
+// Rows that the few-rows kernel is built for, 0 for more than it takes.
+int few_rows(long long M) { return M > FEW_ROWS ? 0 : (M <= 2 ? static_cast<int>(M) : (M <= 4 ? 4 : 8)); }
+
+template <typename T, int MR>
+int run_few(const ip4::FewParams &prm, cudaStream_t st) {
+    const unsigned sets = static_cast<unsigned>((prm.N + 127) / 128) * 32;
+    // a warp's lanes take 1024 elements at a time: longer rows are shared by a CTA's four
+    return launched(prm.bytes <= 512 ? iph::launch_pdl(ip4::few_rows_kernel<T, MR, 1>, dim3(sets / 4), dim3(128), 0, st, prm)
+                                     : iph::launch_pdl(ip4::few_rows_kernel<T, MR, 4>, dim3(sets), dim3(128), 0, st, prm));
+}
+template <typename T>
+int run_few(const ip4::FewParams &prm, cudaStream_t st) {
+    switch (few_rows(prm.M)) {
+    case 1: return run_few<T, 1>(prm, st);
+    case 2: return run_few<T, 2>(prm, st);
+    case 4: return run_few<T, 4>(prm, st);
+    default: return run_few<T, 8>(prm, st);
+    }
+}
+
+// Its time, ns: a start, and the elements of the weights with each row's products of them (1024 -> 4096 with 1, 2, 4 and 8
+// rows 2.7, 2.8, 3.4 and 5.2 us, by tiles 4.3; 4096 -> 1024 as long, by tiles 7.8; 1024 -> 65536 11, 16, 22, 32 and 12).
+long long few_time(int rows, int K, int N) {
+    return 1600 + 130 * rows + static_cast<long long>(K) * N * (100 + 48 * rows) / 1000000;
 }
 
 }  // namespace
@@ -191,6 +226,15 @@ int ip_linear_fp4(const uint8_t *x, long long ldx, const uint8_t *x_blocks, cons
     if (workspace_bytes < 256) return IP_ERR_WORKSPACE;
     const int nsm = sm_count();
     if (nsm <= 0) return IP_ERR_CUDA;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const Times times = tile_times(rows, N, (K + 63) / 64, nsm);
+    const int few_m = few_rows(rows);
+    if (few_m && few_time(few_m, K, N) <= times.least()) {
+        const ip4::FewParams few{x, x_blocks, w, w_blocks, sx, sw, bias, y, ldx, ldw, ldy, static_cast<int>(rows), N, act, bytes, (K + 63) / 64};
+        if (dtype == IP_F32) return run_few<float>(few, st);
+        if (dtype == IP_F16) return run_few<__half>(few, st);
+        return run_few<__nv_bfloat16>(few, st);
+    }
     ip4::Params prm;
     prm.sx = sx;
     prm.sw = sw;
@@ -207,10 +251,9 @@ int ip_linear_fp4(const uint8_t *x, long long ldx, const uint8_t *x_blocks, cons
     prm.timeout_cycles = iph::wait_limit();
     prm.stall = iph::stall_injection();
     const Operands o{x, w, x_blocks, w_blocks, ldx, ldw, bytes};
-    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    if (dtype == IP_F32) return run<float>(o, prm, nsm, st);
-    if (dtype == IP_F16) return run<__half>(o, prm, nsm, st);
-    return run<__nv_bfloat16>(o, prm, nsm, st);
+    if (dtype == IP_F32) return run<float>(o, prm, times, nsm, st);
+    if (dtype == IP_F16) return run<__half>(o, prm, times, nsm, st);
+    return run<__nv_bfloat16>(o, prm, times, nsm, st);
 }
 
 }  // extern "C"

@@ -555,4 +555,136 @@ __global__ void __launch_bounds__(THREADS, 1)
     if (threadIdx.x == 0 && *dead) atomicOr(prm.err, ips::ERR_TIMEOUT);
 }
 
+// ---- few rows ------------------------------------------------------------
+//
+// Up to eight rows, where that is sooner than tiles (few_time in ip_fp4.cu): ordinary lanes read the weights once, a warp has the four channels n, n + 32, n + 64, n + 96 of
+// 128, whose scales lie side by side, a lane 32 elements of them (16 bytes) at a time.  Products of codes are multiples
+// of 1/4 up to 36, so f16 holds the sums of eight exactly; a block's two sums and its scales' product go to f32.
+// PARTS warps of a CTA share a row's elements and add up in a fixed order.  What bounds it: latency (launch, loads,
+// join) with one or two rows, their products with more: 1 x 1024 -> 4096 2.7 us (2.4 MB), by tiles 4.3.
+
+struct FewParams {
+    const uint8_t *x, *xb, *w, *wb;
+    const float *sx, *sw, *bias;
+    void *y;
+    long long ldx, ldw, ldy;
+    int M, N, act, bytes, steps;
+};
+
+// The 16 bytes of a row's codes from c on, zeros behind its last.
+__device__ __forceinline__ uint4 codes16(const uint8_t *row, int c, int bytes) {
+    if (c + 16 <= bytes) return *reinterpret_cast<const uint4 *>(row + c);
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll 1
+    for (int i = 0; c + i < bytes; ++i) {
+        const uint32_t v = static_cast<uint32_t>(row[c + i]) << (8 * (i & 3));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] |= i >> 2 == k ? v : 0u;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Eight codes as f16 pairs.
+__device__ __forceinline__ void halves8(uint32_t w, __half2 *v) {
+    uint32_t h[4];
+    asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n"
+        " cvt.rn.f16x2.e2m1x2 %0, a;\n cvt.rn.f16x2.e2m1x2 %1, b;\n"
+        " cvt.rn.f16x2.e2m1x2 %2, c;\n cvt.rn.f16x2.e2m1x2 %3, d;\n}\n"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+        : "r"(w));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const __half2 *>(&h[i]);
+}
+__device__ __forceinline__ void halves32(uint4 c, __half2 (&v)[16]) {
+    halves8(c.x, v), halves8(c.y, v + 4), halves8(c.z, v + 8), halves8(c.w, v + 12);
+}
+// The two scales of one half of a word.
+__device__ __forceinline__ float2 scales2(uint32_t word, int half) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(half ? word >> 16 : word)));
+    return __half22float2(*reinterpret_cast<const __half2 *>(&h));
+}
+
+template <typename T, int MR, int PARTS>
+__global__ void __launch_bounds__(128) few_rows_kernel(const FewParams prm) {
+    constexpr int SETS = 4 / PARTS;            // of four channels, a CTA
+    __shared__ float sums[PARTS][SETS][4 * MR];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % PARTS, set = warp / PARTS;
+    const int at = static_cast<int>(blockIdx.x) * SETS + set, group = at >> 5, r = at & 31, n0 = group * 128 + r;
+    const int chunks = (prm.bytes + 15) / 16;
+    float acc[4][MR];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int m = 0; m < MR; ++m) acc[j][m] = 0.0f;
+    if (n0 < prm.N) {
+        for (int c = part * 32 + lane; c < chunks; c += 32 * PARTS) {
+            uint4 wc[4], xc[MR];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                wc[j] = n0 + 32 * j < prm.N ? codes16(prm.w + (n0 + 32 * j) * prm.ldw, 16 * c, prm.bytes) : make_uint4(0, 0, 0, 0);
+            const uint4 ws = *reinterpret_cast<const uint4 *>(prm.wb + (static_cast<long long>(group) * prm.steps + (c >> 1)) * 512 + 16 * r);
+            uint32_t xs[MR];
+#pragma unroll
+            for (int m = 0; m < MR; ++m) {
+                const bool in = m < prm.M;
+                xc[m] = in ? codes16(prm.x + m * prm.ldx, 16 * c, prm.bytes) : make_uint4(0, 0, 0, 0);
+                xs[m] = in ? *reinterpret_cast<const uint32_t *>(prm.xb + static_cast<long long>(c >> 1) * 512 + 16 * m) : 0;
+            }
+            const uint32_t wsj[4] = {ws.x, ws.y, ws.z, ws.w};
+            __half2 w[4][16];
+            float2 s[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                halves32(wc[j], w[j]);
+                s[j] = scales2(wsj[j], c & 1);
+            }
+#pragma unroll
+            for (int m = 0; m < MR; ++m) {
+                __half2 x[16];
+                halves32(xc[m], x);
+                const float2 sx = scales2(xs[m], c & 1);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    __half2 a = __hmul2(w[j][0], x[0]), b = __hmul2(w[j][8], x[8]);
+#pragma unroll
+                    for (int i = 1; i < 8; ++i) {
+                        a = __hfma2(w[j][i], x[i], a);
+                        b = __hfma2(w[j][8 + i], x[8 + i], b);
+                    }
+                    acc[j][m] = __fmaf_rn(__low2float(a) + __high2float(a), s[j].x * sx.x, acc[j][m]);
+                    acc[j][m] = __fmaf_rn(__low2float(b) + __high2float(b), s[j].y * sx.y, acc[j][m]);
+                }
+            }
+        }
+    }
+    // the lanes' sums: at each step a lane hands half of its values over and keeps the others, until value `lane` is left
+    constexpr int V = 4 * MR;
+    float a[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) a[i] = acc[i & 3][i >> 2];
+#pragma unroll
+    for (int h = V / 2; h; h >>= 1)
+#pragma unroll
+        for (int i = 0; i < h; ++i) {
+            const bool up = lane & h;
+            const float give = up ? a[i] : a[i + h];
+            a[i] = (up ? a[i + h] : a[i]) + __shfl_xor_sync(0xffffffffu, give, h);
+        }
+#pragma unroll
+    for (int o = V; o < 32; o <<= 1) a[0] += __shfl_xor_sync(0xffffffffu, a[0], o);
+    if (lane < V) sums[part][set][lane] = a[0];
+    if (PARTS > 1) __syncthreads();
+    else __syncwarp();
+    const int j = lane & 3, m = lane >> 2, n = n0 + 32 * j;
+    if (part != 0 || lane >= 4 * MR || m >= prm.M || n >= prm.N) return;
+    float v = sums[0][set][lane];
+#pragma unroll
+    for (int i = 1; i < PARTS; ++i) v += sums[i][set][lane];
+    float z = __fmaf_rn(v, __fmul_rn(prm.sw[n], prm.sx[m]), prm.bias ? prm.bias[n] : 0.0f), other = 0.0f;
+    if (prm.act) swish2<T>(z, other);
+    static_cast<T *>(prm.y)[m * prm.ldy + n] = from_f32<T>(z);
+}
+
 }  // namespace ip4
