@@ -7,6 +7,8 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
+#include <climits>
 #include <mutex>
 
 namespace {
@@ -97,13 +99,13 @@ struct Operands {
     int bytes;            // of a row's codes
 };
 
-template <typename T, int BN, bool PAIR, bool ODD>
+template <typename T, int BN, bool PAIR, bool ODD, int PARTS = 1>
 int launch(const CUtensorMap (&maps)[5], const ip4::Params &prm, int nsm, cudaStream_t st) {
     using C = ip4::Tile<BN, PAIR>;
     static bool set[64] = {false};
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return IP_ERR_CUDA;
-    auto *fn = ip4::fp4_kernel<T, BN, PAIR, ODD>;
+    auto *fn = ip4::fp4_kernel<T, BN, PAIR, ODD, PARTS>;
     {
         std::lock_guard<std::mutex> lock(g_mu);
         if (!set[dev]) {
@@ -115,9 +117,9 @@ int launch(const CUtensorMap (&maps)[5], const ip4::Params &prm, int nsm, cudaSt
             set[dev] = true;
         }
     }
-    const long long most = nsm / C::CTAS, workers = prm.tiles < most ? prm.tiles : most;
+    const long long most = PARTS > 1 ? prm.tiles : nsm / C::CTAS, workers = prm.tiles < most ? prm.tiles : most;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(workers * C::CTAS));
+    cfg.gridDim = dim3(static_cast<unsigned>(workers * C::CTAS * PARTS));
     cfg.blockDim = dim3(ip4::THREADS);
     cfg.dynamicSmemBytes = C::SMEM;
     cfg.stream = st;
@@ -125,15 +127,15 @@ int launch(const CUtensorMap (&maps)[5], const ip4::Params &prm, int nsm, cudaSt
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = C::CTAS;
+    attr[1].val.clusterDim.x = C::CTAS * PARTS;
     attr[1].val.clusterDim.y = 1;
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = PAIR ? 2 : 1;
+    cfg.numAttrs = PAIR || PARTS > 1 ? 2 : 1;
     return launched(cudaLaunchKernelEx(&cfg, fn, maps[0], maps[1], maps[2], maps[3], maps[4], prm));
 }
 
-template <typename T, int BN, bool PAIR>
+template <typename T, int BN, bool PAIR, int PARTS = 1>
 int run(const Operands &o, ip4::Params prm, int nsm, cudaStream_t st) {
     using C = ip4::Tile<BN, PAIR>;
     CUtensorMap maps[5];
@@ -142,6 +144,10 @@ int run(const Operands &o, ip4::Params prm, int nsm, cudaStream_t st) {
         return IP_ERR_CUDA;
     prm.tiles_n = (prm.N + BN - 1) / BN;
     prm.tiles = (prm.M + ip4::TILE_M * C::CTAS - 1) / (ip4::TILE_M * C::CTAS) * prm.tiles_n;
+    if constexpr (PARTS > 1) {
+        maps[4] = maps[0];      // not used
+        return launch<T, BN, PAIR, true, PARTS>(maps, prm, nsm, st);
+    }
     constexpr int es = static_cast<int>(sizeof(T));
     const bool odd = !aligned(prm.y, 16) || prm.ldy * es % 16 != 0 || prm.N * es % 16 != 0;
     constexpr CUtensorMapDataType type = es == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16;
@@ -155,9 +161,10 @@ long long rounds(long long tiles, int workers) { return (tiles + workers - 1) / 
 // The times, ns, that the forms of tiles are expected to take: a start, and for each round of tiles over the
 // SMs the stages (all forms are held up by shared memory, which serves the MMAs, the copies in and the
 // scales) with what does not overlap of the hand-over to the output warps, or their time where K is short.
+// t64s: tiles of 64 channels whose K four CTAs share (125 x 4096 -> 1024 6.2 us, by whole tiles 8.0; x 1024 -> 1024 5.1 and 4.1).
 struct Times {
-    long long t64, t128, pair;
-    long long least() const { return t64 < t128 ? (t64 < pair ? t64 : pair) : (t128 < pair ? t128 : pair); }
+    long long t64, t128, pair, t64s;
+    long long least() const { return std::min(std::min(t64, t128), std::min(pair, t64s)); }
 };
 Times tile_times(long long M, int N, int steps, int nsm) {
     const long long stages = (steps + 3) / 4, tm = (M + ip4::TILE_M - 1) / ip4::TILE_M;
@@ -165,12 +172,17 @@ Times tile_times(long long M, int N, int steps, int nsm) {
         const long long tile = stage * stages + over;
         return start + rounds(tiles, workers) * (tile > out ? tile : out);
     };
-    return {time(3300, tm * ((N + 63) / 64), nsm, 340, 300, 930), time(3700, tm * ((N + 127) / 128), nsm, 340, 360, 1200),
-            time(5100, (tm + 1) / 2 * ((N + 255) / 256), nsm / 2, 385, 1200, 2050)};
+    const long long t64 = tm * ((N + 63) / 64), share = (stages + 3) / 4;
+    // one tile a cluster, all clusters at once (of 152 SMs 32 find room, 38 take two rounds), and each part has stages
+    const bool shared = t64 * 4 <= nsm * 27 / 32 && 3 * share < stages;
+    return {time(3300, t64, nsm, 340, 300, 930), time(3700, tm * ((N + 127) / 128), nsm, 340, 360, 1200),
+            time(5100, (tm + 1) / 2 * ((N + 255) / 256), nsm / 2, 385, 1200, 2050),
+            shared ? 5500 + 340 * share : LLONG_MAX};
 }
 
 template <typename T>
 int run(const Operands &o, const ip4::Params &prm, const Times &t, int nsm, cudaStream_t st) {
+    if (t.t64s == t.least()) return run<T, 64, false, 4>(o, prm, nsm, st);
     if (t.pair < t.t64 && t.pair < t.t128) return run<T, 256, true>(o, prm, nsm, st);
     return t.t128 < t.t64 ? run<T, 128, false>(o, prm, nsm, st) : run<T, 64, false>(o, prm, nsm, st);
 }

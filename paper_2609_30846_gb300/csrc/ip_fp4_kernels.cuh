@@ -29,6 +29,7 @@ constexpr int TILE_M = 128;
 constexpr int BKB = 128;                 // bytes of a row in a stage
 constexpr int BK = 256;                  // elements
 constexpr int THREADS = 768;             // six warpgroups (registers are dealt by warpgroup)
+constexpr int SUMS_LD = 72;              // floats a row of a part's sums
 constexpr int REGS = 80;                 // registers a thread at launch
 constexpr int EPI_WARPS = 16, SCALE_WARP = 16, X_WARP = 20, MMA_WARP = 21, W_WARP = 22, SCALES_WARP = 23;
 
@@ -264,13 +265,14 @@ __device__ __forceinline__ void store_block(const CUtensorMap *map, uint32_t src
                  : "memory");
 }
 // ODD: output rows that are not on 16 bytes or whose N columns do not end there: written element by element, others
-// by TMA.
-template <typename T, int BN, bool PAIR, bool ODD>
+// by TMA.  PARTS: CTAs of a cluster that share a tile's K, one tile a cluster; each then adds up 128 / PARTS rows.
+template <typename T, int BN, bool PAIR, bool ODD, int PARTS = 1>
 __global__ void __launch_bounds__(THREADS, 1)
     fp4_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w,
                const __grid_constant__ CUtensorMap tm_xb, const __grid_constant__ CUtensorMap tm_wb,
                const __grid_constant__ CUtensorMap tm_y, const Params prm) {
     using C = Tile<BN, PAIR>;
+    static_assert(PARTS == 1 || (!PAIR && ODD), "forms");
     // 256 columns are 64 registers of an output thread: its warpgroups take over what the others can
     // spare, 4 x 96 + 2 x 48 = 6 x 80
     constexpr bool DEAL = BN == 256;
@@ -288,7 +290,8 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t drained = base + 8u * (4 * C::ST + 4), never = drained + 8u;
     volatile int *dead = reinterpret_cast<volatile int *>(smem + C::DEAD);
     const int rank = PAIR ? static_cast<int>(blockIdx.x & 1u) : 0;      // clusters are (2, 1, 1)
-    const long long worker = blockIdx.x / C::CTAS, workers = gridDim.x / C::CTAS;
+    const int part = PARTS > 1 ? static_cast<int>(blockIdx.x % PARTS) : 0;      // clusters are (PARTS, 1, 1)
+    const long long worker = blockIdx.x / (C::CTAS * PARTS), workers = gridDim.x / (C::CTAS * PARTS);
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::ST; ++s) {
@@ -320,7 +323,8 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t tmem = lds32(base + C::TMEM_PTR);
     pdl_wait();
 
-    const int stages = (prm.steps + 3) / 4;
+    const int stages = (prm.steps + 3) / 4, share = (stages + PARTS - 1) / PARTS;
+    const int from = part * share, to = PARTS > 1 ? min(stages, from + share) : stages;
     const long long limit = prm.timeout_cycles;
 
     if (DEAL && warp >= SCALE_WARP) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
@@ -334,7 +338,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             for (long long tile = worker; ok && tile < prm.tiles; tile += workers) {
                 const int mt = static_cast<int>(tile / prm.tiles_n) * C::CTAS + rank;
                 const int n0 = static_cast<int>(tile % prm.tiles_n) * BN;
-                for (int it = 0; it < stages; ++it) {
+                for (int it = from; it < to; ++it) {
                     ok = wait_or_dead(empty(s), ph ^ 1, dead, limit);
                     if (!ok) break;
                     const uint32_t st = base + C::STAGES_AT + s * C::STAGE;
@@ -370,7 +374,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 ok = warp_wait_or_dead(acc_empty(a), aph ^ 1, dead, limit);
                 if (!ok) break;
                 const int n0 = static_cast<int>(tile % prm.tiles_n) * BN;
-                for (int it = 0; it < stages; ++it) {
+                for (int it = from; it < to; ++it) {
                     ok = warp_wait_or_dead(ready(s), ph, dead, limit) && warp_wait_or_dead(full(s), ph, dead, limit);
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -380,7 +384,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                     const int nk = prm.steps - 4 * it < 4 ? prm.steps - 4 * it : 4;
                     if (elect_one()) {
                         for (int k = 0; k < nk; ++k)
-                            mma_fp4<PAIR>(tmem + a * BN, da + 2 * k, db + 2 * k, idesc, sa + 4 * k, sb + 4 * C::WT * k, it > 0 || k > 0);
+                            mma_fp4<PAIR>(tmem + a * BN, da + 2 * k, db + 2 * k, idesc, sa + 4 * k, sb + 4 * C::WT * k, it > from || k > 0);
                         mma_commit<PAIR>(empty(s));
                     }
                     __syncwarp();
@@ -405,7 +409,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         int s = 0, ph = 0;
         bool ok = true;
         for (long long tile = worker; ok && tile < prm.tiles; tile += workers)
-            for (int it = 0; it < stages; ++it) {
+            for (int it = from; it < to; ++it) {
                 ok = warp_wait_or_dead(scales(s), ph, dead, limit);
                 if (!ok) break;
                 const uint32_t src = base + C::STAGES_AT + s * C::STAGE + C::A + C::B + 16 * lane;
@@ -478,6 +482,17 @@ __global__ void __launch_bounds__(THREADS, 1)
             asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");      // the sums are in registers, the constants there
             if (quarter == 0 && lane == 0) arrive_first<PAIR>(acc_empty(a));
             if (++a == C::ACCS) a = 0, aph ^= 1;
+            if constexpr (PARTS > 1) {
+                // the MMAs are done with the stages: the sums go there
+#pragma unroll
+                for (int c = 0; c < CW / 8; ++c)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t *v = &r[c / 2][i / 2][4 * (c & 1) + 2 * (i & 1)];
+                        sts64(base + C::STAGES_AT + 4 * ((quarter * 32 + lane / 4 + 8 * i) * SUMS_LD + col0 + 8 * c + 2 * (lane & 3)),
+                              static_cast<int>(v[0]), static_cast<int>(v[1]));
+                    }
+            } else {
 #pragma unroll
             for (int c = 0; c < CW; c += BC) {
                 if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");      // the last block has been read
@@ -521,8 +536,40 @@ __global__ void __launch_bounds__(THREADS, 1)
                     }
                 }
             }
+            }
         }
         if (!ODD && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");      // no block is still on its way
+    }
+    if constexpr (PARTS > 1) {
+        __syncthreads();
+        cluster_sync();
+        constexpr int ROWS = TILE_M / PARTS;
+        for (int e = threadIdx.x; e < ROWS * BN / 2; e += THREADS) {
+            const int row = part * ROWS + e / (BN / 2), col = e % (BN / 2) * 2;
+            const long long m = worker / prm.tiles_n * TILE_M + row;
+            const int n = static_cast<int>(worker % prm.tiles_n) * BN + col;
+            if (m >= prm.M || n >= prm.N) continue;
+            const uint32_t at = base + C::STAGES_AT + 4 * (row * SUMS_LD + col);
+            float v0 = 0.0f, v1 = 0.0f;
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) {
+                uint32_t there;
+                float u0, u1;
+                asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(p));
+                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(u0), "=f"(u1) : "r"(there) : "memory");
+                v0 += u0, v1 += u1;
+            }
+            const bool both = n + 1 < prm.N;
+            const float sx = prm.sx[m];
+            float z0 = __fmaf_rn(v0, __fmul_rn(prm.sw[n], sx), prm.bias ? prm.bias[n] : 0.0f);
+            float z1 = both ? __fmaf_rn(v1, __fmul_rn(prm.sw[n + 1], sx), prm.bias ? prm.bias[n + 1] : 0.0f) : 0.0f;
+            if (prm.act) swish2<T>(z0, z1);
+            T *y = static_cast<T *>(prm.y) + m * prm.ldy + n;
+            y[0] = from_f32<T>(z0);
+            if (both) y[1] = from_f32<T>(z1);
+        }
+        __syncthreads();
+        cluster_sync();      // no CTA ends while another one reads its sums
     }
     // After a wait that ran out the copies in flight land before a CTA ends.  The scales' report to their own CTA's
     // barriers; a pair's others to the first CTA's, where a stage that not all of its fetching

@@ -18,7 +18,7 @@ int launched(cudaError_t rc) {
 constexpr int hold(int threads, int units, bool on16 = false) { return threads * units * 8 - (on16 ? 0 : 8); }
 
 // Parts of a row and their elements: one while a CTA holds the row; else a cluster's, as many as come to
-// four CTAs an SM, few rows by sixteen CTAs of few elements (1 x 65536 XX us by 16 CTAs, by 8 XX) and many by those
+// four CTAs an SM, few rows by sixteen CTAs of few elements (1 x 65536 with twenty 6.7 us by 16 CTAs, by 8 7.5) and many by those
 // whose registers the parts fill; parts that a second kernel joins for what sixteen CTAs do not hold.
 struct Plan {
     int parts, per, cluster;

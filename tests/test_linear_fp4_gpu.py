@@ -36,7 +36,7 @@ def rows(n, k, seed, scales=True):
 
 
 SIZES = [(1, 1, 1), (1, 16, 8), (1, 64, 64), (3, 40, 17), (128, 64, 64), (128, 256, 64), (7, 300, 100), (128, 512, 128), (130, 1000, 777),
-         (1, 1024, 4096), (2, 1025, 130), (4, 4000, 257), (5, 2080, 1000), (8, 4096, 1024), (8, 33, 129), (9, 1024, 512), (64, 4096, 1024), (125, 4096, 1024), (333, 1000, 777), (200, 2000, 9728), (2000, 100, 1024), (1500, 1024, 4096),
+         (1, 1024, 4096), (2, 1025, 130), (4, 4000, 257), (5, 2080, 1000), (8, 4096, 1024), (8, 33, 129), (9, 1024, 512), (64, 4096, 1024), (300, 1100, 200), (9, 32768, 70), (129, 5000, 65), (1000, 4000, 300), (125, 4096, 1024), (333, 1000, 777), (200, 2000, 9728), (2000, 100, 1024), (1500, 1024, 4096),
          (2049, 333, 4097), (40, 32768, 33), (5000, 576, 3000), (1000, 2048, 5001)]
 
 

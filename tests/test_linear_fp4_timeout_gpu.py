@@ -19,7 +19,7 @@ def ip():
 
 # tiles of 128 x 64, of 128 x 128 and of 256 x 256 by two CTAs; one stage and more than the buffers hold, one
 # tile an SM and several, output rows of any alignment
-SIZES = [(9, 100, 64), (13, 1024, 1000), (128, 8192, 512), (300, 256, 4096), (300, 3000, 4097), (1500, 1024, 4096), (4096, 1024, 4096),
+SIZES = [(9, 100, 64), (13, 1024, 1000), (40, 4096, 300), (200, 20000, 1000), (128, 8192, 512), (300, 256, 4096), (300, 3000, 4097), (1500, 1024, 4096), (4096, 1024, 4096),
          (3000, 8192, 4096), (2049, 200, 8193)]
 
 
