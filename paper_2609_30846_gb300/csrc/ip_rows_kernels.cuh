@@ -178,6 +178,15 @@ __device__ __forceinline__ float larger(float a, float b) {
     return r;
 }
 
+// The same of two pairs of 16-bit numbers.
+template <typename T>
+__device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    if (std::is_same<T, __half>::value) asm("max.NaN.xorsign.abs.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    else asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
 // Sixteen elements to int8 (ip_scaled_kernels.cuh has the argument; f, inv, top of the row).
 __device__ __forceinline__ uint2 to_i8(const float *z, float f, float inv, float top, bool far) {
     uint32_t k[8];
@@ -226,7 +235,11 @@ __device__ __forceinline__ uint32_t to_fp4(const float (&z)[16], float big, Fp4R
         i *= row.down;
         uint32_t h[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h[j]) : "f"(z[2 * j + 1] * i), "f"(z[2 * j] * i));
+        for (int j = 0; j < 8; ++j)      // both products by one instruction
+            asm("{\n .reg .b64 p, q;\n .reg .f32 a, b;\n mov.b64 p, {%1, %2};\n mov.b64 q, {%3, %3};\n mul.rn.f32x2 p, p, q;\n"
+                " mov.b64 {a, b}, p;\n cvt.rn.f16x2.f32 %0, b, a;\n}\n"
+                : "=r"(h[j])
+                : "f"(z[2 * j]), "f"(z[2 * j + 1]), "f"(i));
         code = make_uint2(e2m1_of8(h), e2m1_of8(h + 4));
         return sb;
     }
@@ -335,7 +348,13 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, rows_ctas<T, TPR, UNITS
 #pragma unroll
             for (int i = 0; i < UNITS; ++i) {
                 most[i] = 0;
-                raw[i].h[0].largest(most[i]), raw[i].h[1].largest(most[i]);
+                if constexpr (sizeof(T) == 4) {
+                    raw[i].h[0].largest(most[i]), raw[i].h[1].largest(most[i]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) most[i] = larger2<T>(most[i], raw[i].h[j >> 2].w[j & 3]);
+                    most[i] &= 0x7fff7fffu;
+                }
                 bits = sizeof(T) == 4 ? max(bits, most[i]) : __vmaxu2(bits, most[i]);
             }
             for (int c = KEPT + t * 16; c < d; c += TPR * 16) {
