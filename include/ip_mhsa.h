@@ -510,8 +510,9 @@ int ip_dequantize_fp4(const uint8_t *q, long long ldq, const uint8_t *blocks, co
 /* Product of 4-bit rows:
  *   y[m][n] = act(sx[m] sw[n] S + bias[n]),  S = sum over blocks b of s_x[m][b] s_w[n][b] sum of
  * the block's 16 products of codes, for m < rows, n < N: products and scales are exact, S is
- * summed in f32 (on the tensor cores), the rest is f32 (sx[m] sw[n] first), rounded once to y's
- * type.  act: IP_ACT_NONE or IP_ACT_SWISH.
+ * summed in f32 (on the tensor cores, few rows by ordinary lanes; in an order that goes by the
+ * sizes), the rest is f32 (sx[m] sw[n] first), rounded once to y's type.  Equal calls give equal
+ * bits.  act: IP_ACT_NONE or IP_ACT_SWISH.
  * x, x_blocks, sx: 4-bit rows [rows][K] as above, w, w_blocks, sw: [N][K], one per output channel; any
  * codes behind the first K of a row's last byte count as elements (0 as the calls above write them).
  * bias: device f32 [N] or NULL.  y: device, dtype IP_F32, IP_F16 or IP_BF16, rows of ldy >= N

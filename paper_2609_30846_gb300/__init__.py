@@ -731,7 +731,8 @@ _short = _Unbound
 
 
 def _bind_short(lib):
-    """The short forms, bound to the library; none without torch (the C entry points need none)."""
+    """The short forms, bound to the library; none without torch (the C entry points need none).  What they
+    return is what the general forms do; new outputs of up to 1 MB a call in all share one storage."""
     path = _build.torch_extension()
     if path is None:
         return _Unbound
@@ -1123,7 +1124,8 @@ def dequantize_fp4(q, blocks, scale, d=None, *, dtype=None, out=None, stream=Non
 
 def linear_fp4(x, x_blocks, sx, w, w_blocks, sw, bias=None, *, act: int = ACT_NONE, dtype=None, out=None,
                workspace=None, stream=None):
-    """Product of 4-bit rows (quantize_fp4, rmsnorm_fp4) on the block-scaled tensor cores:
+    """Product of 4-bit rows (quantize_fp4, rmsnorm_fp4) on the block-scaled tensor cores (a few rows go by
+    ordinary lanes):
     out[..., n] = act(sum of the products of the values of x's and w's rows + bias[n]), codes and
     scales exact, sums in float32.  x: uint8 [..., ceil(K / 2)] with its block scales and sx: float32
     [...]; w: uint8 [N, ceil(K / 2)], w_blocks, sw: float32 [N] (quantize_fp4 of the weights); bias: float32 [N]

@@ -79,6 +79,22 @@ def test_logprobs(ip, monkeypatch, shape):  # noqa: F811
             ip.token_logprobs(x, top=33, workspace=ws)
 
 
+@pytest.mark.parametrize("M", [1, 3, 600])
+def test_outputs_lie_apart(ip, M):  # noqa: F811
+    # small outputs of a call share an allocation: each starts on 16 bytes and is its own
+    x, g = torch.randn(M, 1000, device="cuda").half(), torch.ones(1000, device="cuda").half()
+    ws = torch.zeros(256, dtype=torch.uint8, device="cuda")
+    calls = (lambda: ip.quantize_fp4(x), lambda: ip.rmsnorm_i8(x, g, x), lambda: ip.rmsnorm_fp4(x, g, x),
+             lambda: ip.token_logprobs(x, torch.zeros(M, dtype=torch.int32, device="cuda"), top=3, workspace=ws))
+    for call in calls:
+        want, got = [t.clone() for t in call()], call()
+        ends = sorted((t.data_ptr(), t.data_ptr() + (1 + sum((n - 1) * k for n, k in zip(t.shape, t.stride()))) * t.element_size()) for t in got)
+        assert all(a[1] <= b[0] for a, b in zip(ends, ends[1:])) and all(a[0] % 16 == 0 for a in ends)
+        for i, t in enumerate(got):
+            t.zero_()
+            assert all(torch.equal(u, v) for u, v in list(zip(got, want))[i + 1:] if u.dim() != 3)
+
+
 class Step:
     """A decoder's feed-forward block and head on M tokens: norm with residual into 4-bit rows, two 4-bit
     products, norm into int8, the head's product, log probabilities with the best tokens."""
