@@ -66,6 +66,9 @@ __device__ __forceinline__ Key key_of(uint32_t order, int i) {
 __device__ __forceinline__ Key key_from(float least) { return static_cast<Key>(order_of(least)) << 32; }
 __device__ __forceinline__ int index_of(Key k) { return static_cast<int>(~static_cast<uint32_t>(k)); }
 
+// Where the warps of a CTA leave what they reduce.  Each reduction of a kernel has its own, so that one barrier does.
+typedef uint2 *Slot;
+
 // The group of threads that holds a row: a warp or a CTA of 256.
 template <int TPR>
 struct Group {
@@ -74,30 +77,34 @@ struct Group {
         if (WARPS == 1) __syncwarp();
         else __syncthreads();
     }
-    static __device__ __forceinline__ float sum(float v, float *red) {
+    // Two sums over the group.
+    static __device__ __forceinline__ void sum2(float &a, float &b, Slot red) {
 #pragma unroll
-        for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        for (int o = 16; o; o >>= 1) {
+            a += __shfl_xor_sync(0xffffffffu, a, o);
+            b += __shfl_xor_sync(0xffffffffu, b, o);
+        }
         if (WARPS > 1) {
+            if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = make_uint2(__float_as_uint(a), __float_as_uint(b));
             __syncthreads();
+            a = __uint_as_float(red[0].x), b = __uint_as_float(red[0].y);
+#pragma unroll
+            for (int i = 1; i < WARPS; ++i) a += __uint_as_float(red[i].x), b += __uint_as_float(red[i].y);
+        }
+    }
+    // The largest of the warps' values, which are a warp's lanes' own already.
+    static __device__ __forceinline__ uint2 max2_of_warps(uint2 v, Slot red) {
+        if (WARPS > 1) {
             if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
             __syncthreads();
             v = red[0];
 #pragma unroll
-            for (int i = 1; i < WARPS; ++i) v += red[i];
+            for (int i = 1; i < WARPS; ++i) v.x = max(v.x, red[i].x), v.y = max(v.y, red[i].y);
         }
         return v;
     }
-    static __device__ __forceinline__ uint32_t max_u32(uint32_t v, uint32_t *red) {
-        v = __reduce_max_sync(0xffffffffu, v);
-        if (WARPS > 1) {
-            __syncthreads();
-            if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-            __syncthreads();
-            v = red[0];
-#pragma unroll
-            for (int i = 1; i < WARPS; ++i) v = max(v, red[i]);
-        }
-        return v;
+    static __device__ __forceinline__ uint32_t max_u32(uint32_t v, Slot red) {
+        return max2_of_warps(make_uint2(__reduce_max_sync(0xffffffffu, v), 0u), red).x;
     }
 };
 
@@ -135,22 +142,16 @@ __device__ __forceinline__ uint32_t lane_max_of_rank(uint32_t v, int top) {
 // together, for those of the threads' keys whose logit is not below `least`; lane_top: the largest of
 // the upper halves of a thread's (0: none).
 template <int TPR, int CANDS, typename Each, typename Put>
-__device__ __forceinline__ void best(int top, uint32_t lane_top, Each each, Put put, Key *cand, uint32_t *red) {
+__device__ __forceinline__ void best(int top, uint32_t lane_top, Each each, Put put, Key *cand, Slot red) {
     using G = Group<TPR>;
     const int lane = threadIdx.x & 31, t = threadIdx.x % TPR;
-    uint32_t bound;
-    if (top == 1) {
-        bound = G::max_u32(lane_top, red);
-    } else {
-        // `top` elements reach a warp's lane maximum of rank `top`, or every warp's of rank top / warps
-        const uint32_t alone = lane_max_of_rank(lane_top, top);
-        bound = G::max_u32(alone, red);
-        if (G::WARPS > 1) bound = max(bound, ~G::max_u32(~lane_max_of_rank(lane_top, (top - 1) / G::WARPS + 1), red));
-    }
     uint32_t *count = reinterpret_cast<uint32_t *>(cand);      // the keys from cand[1] on
-    G::sync();
     if (t == 0) *count = 0;
-    G::sync();
+    // `top` elements reach a warp's lane maximum of rank `top`, or every warp's of rank top / warps
+    uint2 lim = make_uint2(top == 1 ? __reduce_max_sync(0xffffffffu, lane_top) : lane_max_of_rank(lane_top, top), 0u);
+    if (G::WARPS > 1 && top > 1) lim.y = ~lane_max_of_rank(lane_top, (top - 1) / G::WARPS + 1);
+    lim = G::max2_of_warps(lim, red);
+    const uint32_t bound = G::WARPS > 1 && top > 1 ? max(lim.x, ~lim.y) : lim.x;
     uint32_t found = 0;
     if (__any_sync(0xffffffffu, lane_top != 0 && lane_top >= bound))
         each(value_of(max(bound, order_of(-INFINITY))), [&](bool have, Key k) {
@@ -269,7 +270,7 @@ __device__ __forceinline__ void add_exp(float x0, float x1, Two minus_from, Two 
 
 // Joins parts' sums, the thread's being first, first + step, ...
 template <int TPR, typename At>
-__device__ __forceinline__ Sums join(int parts, int first, int step, float c, At at, uint32_t *red) {
+__device__ __forceinline__ Sums join(int parts, int first, int step, float c, At at, Slot red) {
     using G = Group<TPR>;
     float most = -INFINITY;
     for (int i = first; i < parts; i += step) most = fmaxf(most, at(i).m);
@@ -286,8 +287,7 @@ __device__ __forceinline__ Sums join(int parts, int first, int step, float c, At
         v.s = __fmaf_rn(p.s, e, v.s);
         v.u = __fmaf_rn(__fmaf_rn(p.s, fmaxf(d, -1e30f), p.u), e, v.u);
     }
-    v.s = G::sum(v.s, reinterpret_cast<float *>(red));
-    v.u = G::sum(v.u, reinterpret_cast<float *>(red));
+    G::sum2(v.s, v.u, red + 8);
     return v;
 }
 
@@ -302,7 +302,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? (U > 4 ? 4 
     constexpr bool PART = HOLDS != WHOLE;
     constexpr int RPC = TPR == 32 ? 4 : 1, CANDS = TPR == 32 ? WARP_CANDS : CTA_CANDS;
     __shared__ Key cands[RPC][CANDS + 1];
-    __shared__ uint32_t red[8];
+    __shared__ uint2 red[HOLDS == CLUSTER ? 48 : 24];      // slots of eight: maximum, sums, bound; those of the join
     __shared__ Sums part_sums[HOLDS == CLUSTER ? MAX_CLUSTER : 1];
     __shared__ Key part_keys[HOLDS == CLUSTER ? MAX_CLUSTER * MAX_TOP : 1];
     pdl_launch_dependents();
@@ -365,8 +365,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? (U > 4 ? 4 
     split(u2, u0, u1);
     sums.s = s0 + s1;
     sums.u = u0 + u1;
-    sums.s = G::sum(sums.s, reinterpret_cast<float *>(red));
-    sums.u = G::sum(sums.u, reinterpret_cast<float *>(red));
+    G::sum2(sums.s, sums.u, red + 8);
     // the few elements that reach a bound are read again: an index into registers would have every one's code unrolled
     auto each = [&](float least, auto f) {
 #pragma unroll
@@ -393,12 +392,12 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? (U > 4 ? 4 
     if constexpr (HOLDS == WHOLE) {
         const RowOut<T> out(prm, row, sums);
         if (t == 0) out.write(sums);
-        if (prm.top > 0) best<TPR, CANDS>(prm.top, lane_top, each, [&](int r, Key k) { out.put(r, k); }, cands[sub], red);
+        if (prm.top > 0) best<TPR, CANDS>(prm.top, lane_top, each, [&](int r, Key k) { out.put(r, k); }, cands[sub], red + 16);
     } else if constexpr (HOLDS == PARTS) {
         const long long at = row * prm.parts + blockIdx.y;
         if (t == 0) *reinterpret_cast<float4 *>(prm.sums + 4 * at) = make_float4(sums.m, sums.s, sums.u, 0.0f);
         if (prm.top > 0)
-            best<TPR, CANDS>(prm.top, lane_top, each, [&](int r, Key k) { prm.keys[at * prm.top + r] = k; }, cands[sub], red);
+            best<TPR, CANDS>(prm.top, lane_top, each, [&](int r, Key k) { prm.keys[at * prm.top + r] = k; }, cands[sub], red + 16);
     } else {
         // to the cluster's first CTA, which is not done before all have been there
         uint32_t to_sums, to_keys;
@@ -414,11 +413,11 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? (U > 4 ? 4 
         if (prm.top > 0)
             best<TPR, CANDS>(prm.top, lane_top, each, [&](int r, Key k) {
                 asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to_keys + 8 * r), "l"(k) : "memory");
-            }, cands[sub], red);
+            }, cands[sub], red + 16);
         __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
         if (blockIdx.y != 0) return;
-        const Sums all = join<TPR>(prm.parts, t, TPR, c, [&](int i) { return part_sums[i]; }, red);
+        const Sums all = join<TPR>(prm.parts, t, TPR, c, [&](int i) { return part_sums[i]; }, red + 24);
         const RowOut<T> out(prm, row, all);
         if (t == 0) out.write(all);
         if (prm.top > 0) {
@@ -430,7 +429,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? (U > 4 ? 4 
                     const Key k = i < keys ? part_keys[i] : Key(0);
                     f(k >= key_from(least), k);
                 }
-            }, [&](int r, Key k) { out.put(r, k); }, cands[sub], red);
+            }, [&](int r, Key k) { out.put(r, k); }, cands[sub], red + 40);
         }
     }
 }
@@ -439,7 +438,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? (U > 4 ? 4 
 template <typename T>
 __global__ void __launch_bounds__(256) logprob_join_kernel(const LogprobParams prm) {
     __shared__ Key cands[CTA_CANDS + 1];
-    __shared__ uint32_t red[8];
+    __shared__ uint2 red[24];
     pdl_launch_dependents();
     pdl_wait();
     const int t = threadIdx.x;
@@ -462,7 +461,7 @@ __global__ void __launch_bounds__(256) logprob_join_kernel(const LogprobParams p
                 f(k >= key_from(least), k);
             }
         };
-        best<256, CTA_CANDS>(prm.top, lane_top, each, [&](int r, Key k) { out.put(r, k); }, cands, red);
+        best<256, CTA_CANDS>(prm.top, lane_top, each, [&](int r, Key k) { out.put(r, k); }, cands, red + 16);
     }
 }
 
