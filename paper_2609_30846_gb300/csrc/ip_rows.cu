@@ -112,7 +112,7 @@ int ip_rmsnorm_i8(const void *x, long long ldx, const void *residual, long long 
     if (!q || !scale) return IP_ERR_NULL;
     if (!aligned(scale, 4)) return IP_ERR_ALIGN;
     const ipw::RowsParams prm{x, residual, weight, rows, ldx, ldres, ldsum, ldq, d, eps, sum,
-                              reinterpret_cast<uint8_t *>(q), nullptr, scale};
+                              reinterpret_cast<uint8_t *>(q), nullptr, scale, aligned(q, 16) && (rows == 1 || ldq % 16 == 0)};
     return run_rows<ipw::OUT_I8, true>(dtype, prm, stream);
 }
 
@@ -122,7 +122,7 @@ int ip_rmsnorm_fp4(const void *x, long long ldx, const void *residual, long long
     int rc = check_norm(x, ldx, residual, ldres, weight, eps, dtype, rows, d, sum, ldsum);
     if (rc == IP_OK) rc = check_fp4(rows, d, q, ldq, blocks, scale);
     if (rc != IP_OK || rows == 0) return rc;
-    const ipw::RowsParams prm{x, residual, weight, rows, ldx, ldres, ldsum, ldq, d, eps, sum, q, blocks, scale};
+    const ipw::RowsParams prm{x, residual, weight, rows, ldx, ldres, ldsum, ldq, d, eps, sum, q, blocks, scale, true};
     return run_rows<ipw::OUT_FP4, true>(dtype, prm, stream);
 }
 
@@ -138,7 +138,7 @@ int ip_quantize_fp4(const void *x, int dtype, long long rows, int d, long long l
     if (rc != IP_OK || rows == 0) return rc;
     if (!x) return IP_ERR_NULL;
     if (!aligned(x, elem_size(dtype))) return IP_ERR_ALIGN;
-    const ipw::RowsParams prm{x, nullptr, nullptr, rows, ldx, 0, 0, ldq, d, 0.0f, nullptr, q, blocks, scale};
+    const ipw::RowsParams prm{x, nullptr, nullptr, rows, ldx, 0, 0, ldq, d, 0.0f, nullptr, q, blocks, scale, true};
     return run_rows<ipw::OUT_FP4, false>(dtype, prm, stream);
 }
 

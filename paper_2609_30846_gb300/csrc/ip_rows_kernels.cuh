@@ -99,6 +99,7 @@ struct RowsParams {
     uint8_t *q;
     uint8_t *blocks;          // 4-bit rows: their e4m3 scales
     float *scale;
+    bool q16;                 // rows of q start on 16 bytes
 };
 
 enum { OUT_I8 = 0, OUT_FP4 = 1 };
@@ -128,8 +129,32 @@ template <typename T>
 struct Raw16 {
     Raw8<T> h[2];
 
+    // p: c elements into its row, of which n are left.  Rows that are not on 16 bytes: the aligned vectors that hold the
+    // elements, where all of them lie within the row, turned by the words and bytes that p is off.
     template <bool VEC>
-    __device__ __forceinline__ void load(const T *p, int n) {
+    __device__ __forceinline__ void load(const T *p, int n, int c) {
+        if constexpr (!VEC) {
+            constexpr int ES = sizeof(T), WORDS = Raw8<T>::WORDS;
+            const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & 15;
+            const int before = off / ES;
+            if (before <= c && 16 + (off ? 16 / ES - before : 0) <= n) {
+                const uint4 *from = reinterpret_cast<const uint4 *>(p - before);
+                uint32_t x[4 * ES + 4];
+#pragma unroll
+                for (int i = 0; i <= ES; ++i) {
+                    const uint4 u = i < ES || off ? from[i] : make_uint4(0, 0, 0, 0);
+                    x[4 * i] = u.x, x[4 * i + 1] = u.y, x[4 * i + 2] = u.z, x[4 * i + 3] = u.w;
+                }
+#pragma unroll
+                for (int i = 0; i < 4 * ES + 3; ++i) x[i] = off & 4 ? x[i + 1] : x[i];
+#pragma unroll
+                for (int i = 0; i < 4 * ES + 1; ++i) x[i] = off & 8 ? x[i + 2] : x[i];
+#pragma unroll
+                for (int i = 0; i < 4 * ES; ++i)
+                    h[i / WORDS].w[i % WORDS] = ES == 4 ? x[i] : __funnelshift_r(x[i], x[i + 1], 8 * (off & 2));
+                return;
+            }
+        }
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             if (8 * k < n) h[k].template load<VEC>(p + 8 * k, n - 8 * k);
@@ -306,15 +331,15 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, rows_ctas<T, TPR, UNITS
 #pragma unroll
             for (int i = 0; i < UNITS; ++i) {
                 const int c = (i * TPR + t) * 16;
-                h[i].template load<VEC>(x + c, d - c);
-                w[i].template load<VEC>(g + c, d - c);
+                h[i].template load<VEC>(x + c, d - c, c);
+                w[i].template load<VEC>(g + c, d - c, c);
             }
             if (with_res) {
                 Raw16<T> r[UNITS];
 #pragma unroll
                 for (int i = 0; i < UNITS; ++i) {
                     const int c = (i * TPR + t) * 16;
-                    r[i].template load<VEC>(res + c, d - c);
+                    r[i].template load<VEC>(res + c, d - c, c);
                 }
 #pragma unroll
                 for (int i = 0; i < UNITS; ++i) {
@@ -329,13 +354,13 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, rows_ctas<T, TPR, UNITS
             for (int c = KEPT + t * 16; c < d; c += TPR * 16) {
                 Raw16<T> v, u;
                 float unused[16];
-                v.template load<VEC>(x + c, d - c);
+                v.template load<VEC>(x + c, d - c, c);
                 if (with_res) {
-                    u.template load<VEC>(res + c, d - c);
+                    u.template load<VEC>(res + c, d - c, c);
                     v.add(u);
                     v.template store<VEC>(sum + c, d - c);
                 }
-                u.template load<VEC>(g + c, d - c);
+                u.template load<VEC>(g + c, d - c, c);
                 take(v, u, unused);
             }
             bits = __float_as_uint(top) & 0x7fffffffu;
@@ -343,7 +368,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, rows_ctas<T, TPR, UNITS
 #pragma unroll
             for (int i = 0; i < UNITS; ++i) {
                 const int c = (i * TPR + t) * 16;
-                raw[i].template load<VEC>(x + c, d - c);
+                raw[i].template load<VEC>(x + c, d - c, c);
             }
 #pragma unroll
             for (int i = 0; i < UNITS; ++i) {
@@ -359,7 +384,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, rows_ctas<T, TPR, UNITS
             }
             for (int c = KEPT + t * 16; c < d; c += TPR * 16) {
                 Raw16<T> v;
-                v.template load<VEC>(x + c, d - c);
+                v.template load<VEC>(x + c, d - c, c);
                 v.h[0].largest(bits), v.h[1].largest(bits);
             }
             bits = Raw8<T>::value(bits);
@@ -378,7 +403,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, rows_ctas<T, TPR, UNITS
                 uint32_t unused = 0;
                 for (int c = t * 16; c < d; c += TPR * 16) {
                     Raw16<T> v;
-                    v.template load<VEC>(again + c, d - c);
+                    v.template load<VEC>(again + c, d - c, c);
 #pragma unroll
                     for (int j = 0; j < 16; ++j) ss = __fmaf_rn(v.at(j) * up, v.at(j) * up, ss);
                 }
@@ -398,8 +423,8 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, rows_ctas<T, TPR, UNITS
         // the elements from c on: those that are kept, or read again
         auto again16 = [&](int c, float (&v)[16]) {
             Raw16<T> h, w;
-            h.template load<VEC>(again + c, d - c);
-            if (NORM) w.template load<VEC>(g + c, d - c);
+            h.template load<VEC>(again + c, d - c, c);
+            if (NORM) w.template load<VEC>(g + c, d - c, c);
 #pragma unroll
             for (int j = 0; j < 16; ++j) v[j] = NORM ? __fmul_rn(h.at(j), w.at(j)) : h.at(j);
         };
@@ -414,7 +439,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, rows_ctas<T, TPR, UNITS
             auto put = [&](int c, const float (&v)[16]) {
                 uint2 b[2] = {make_uint2(0u, 0u), make_uint2(0u, 0u)};
                 if (!zero) b[0] = to_i8(v, f, inv, ntop, far), b[1] = to_i8(v + 8, f, inv, ntop, far);
-                if (VEC) {
+                if (VEC || (prm.q16 && c + 16 <= d)) {
                     if (c + 16 <= d) *reinterpret_cast<uint4 *>(q + c) = make_uint4(b[0].x, b[0].y, b[1].x, b[1].y);
                     else *reinterpret_cast<uint2 *>(q + c) = b[0];
                 } else {
