@@ -197,7 +197,7 @@ struct Raw16 {
 };
 
 // Rows that are not on 16 bytes leave through shared memory, so that a warp's lanes write neighbours (a lane's own sixteen
-// one by one: values of 6000 x 1023 29.6 us, norm with residual 42).  Per warp, sixteen elements a lane.
+// one by one: values of 6000 x 1023 29.6 us for 8.9, norm with residual 42 for 19).  Per warp, sixteen elements a lane.
 template <typename T>
 struct Turn {
     static constexpr int LD = sizeof(T) == 4 ? 17 : 18;
@@ -554,6 +554,7 @@ struct ValuesParams {
     unsigned long long magic;      // of the units a row
     int units;
     int wide;                      // rows of y start on 32 bytes
+    bool qvec;                     // those of q on 16 (4-bit rows: 8)
 };
 
 // code x scale (a 4-bit row's: code x block scale, exact, x row scale), rounded once.  A thread
@@ -573,12 +574,12 @@ __global__ void __launch_bounds__(256) values_kernel(const ValuesParams prm) {
         const long long row = i < (1ll << 32) ? static_cast<long long>(udiv_magic(static_cast<uint32_t>(i), prm.magic)) : i / prm.units;
         const int c = static_cast<int>(i - row * prm.units) * 16, d = prm.d;
         const float scale = prm.scale[row];
-        const bool whole = VEC && (EVEN || c + 16 <= d);
+        const bool whole = VEC && (EVEN || c + 16 <= d), qwhole = VEC ? whole : prm.qvec && c + 16 <= d;
         float v[16];
         if (IN == OUT_I8) {
             const uint8_t *q = prm.q + row * prm.ldq + c;
             uint32_t w[4] = {0, 0, 0, 0};
-            if (whole) {
+            if (qwhole) {
                 const uint4 u = *reinterpret_cast<const uint4 *>(q);
                 w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
             } else {
@@ -589,7 +590,7 @@ __global__ void __launch_bounds__(256) values_kernel(const ValuesParams prm) {
         } else {
             const uint8_t *q = prm.q + row * prm.ldq + (c >> 1);
             uint32_t w[2] = {0, 0};
-            if (whole) {
+            if (qwhole) {
                 const uint2 u = *reinterpret_cast<const uint2 *>(q);
                 w[0] = u.x, w[1] = u.y;
             } else {
