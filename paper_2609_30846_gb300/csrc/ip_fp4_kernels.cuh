@@ -29,7 +29,6 @@ constexpr int TILE_M = 128;
 constexpr int BKB = 128;                 // bytes of a row in a stage
 constexpr int BK = 256;                  // elements
 constexpr int THREADS = 768;             // six warpgroups (registers are dealt by warpgroup)
-constexpr int SUMS_LD = 72;              // floats a row of a part's sums
 constexpr int REGS = 80;                 // registers a thread at launch
 constexpr int EPI_WARPS = 16, SCALE_WARP = 16, X_WARP = 20, MMA_WARP = 21, W_WARP = 22, SCALES_WARP = 23;
 
@@ -73,24 +72,14 @@ struct Tile {
     static_assert(STAGE % 1024 == 0 && B % 1024 == 0 , "alignment");
 };
 
-// The barriers guard what the asynchronous units read and write (tiles, scales, accumulators), never
-// generic accesses, so neither waits nor arrivals order any: a pair's arrivals on the first CTA's
-// barriers with the release of the cluster take 0.7 us each (12000 x 16384 -> 1024: 164 us, relaxed 87).
-__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n"
-        " selp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
+// Waits acquire, within the CTA: the scale warps read with ordinary loads what the copies left.  A pair's arrivals on the first CTA's
+// barriers release nothing: what they report are TMEM and tiles, which only asynchronous units touch and the
+// tcgen05 fences order, and with the release of the cluster they take 0.7 us each (12000 x 16384 -> 1024: 164 us, relaxed 87).
 // Bounded wait that also ends when another role of the CTA has given up.
 __device__ __forceinline__ bool wait_or_dead(uint32_t bar, uint32_t parity, volatile int *dead, long long limit) {
-    if (try_wait(bar, parity)) return true;
+    if (mbar_try_wait(bar, parity)) return true;
     const long long t0 = clock64();
-    while (!try_wait(bar, parity)) {
+    while (!mbar_try_wait(bar, parity)) {
         if (*dead) return false;
         if (clock64() - t0 > limit) {
             *dead = 1;
@@ -291,6 +280,12 @@ __device__ __forceinline__ void store_block(const CUtensorMap *map, uint32_t src
                  "r"(n), "r"(m), "r"(src)
                  : "memory");
 }
+// Byte offset of a part's sum: rows of BN, groups of eight columns moved by the row so that a warp's stores fall on different banks.
+template <int BN>
+__device__ __forceinline__ uint32_t sum_at(int row, int col) {
+    static_assert(BN >= 64, "groups of eight columns");
+    return 4u * static_cast<uint32_t>(row * BN + (col ^ (row & 7) << 3));
+}
 // ODD: output rows that are not on 16 bytes or whose N columns do not end there: written element by element, others
 // by TMA.  PARTS: CTAs of a cluster that share a tile's K, one tile a cluster; each then adds up 128 / PARTS rows.
 template <typename T, int BN, bool PAIR, bool ODD, int PARTS = 1>
@@ -457,6 +452,8 @@ __global__ void __launch_bounds__(THREADS, 1)
                 }
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                // these reads come before the copy that refills the stage (release_stage has the same fence)
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) arrive_first<PAIR>(ready(s));
                 if (++s == C::ST) s = 0, ph ^= 1;
@@ -510,13 +507,14 @@ __global__ void __launch_bounds__(THREADS, 1)
             if (quarter == 0 && lane == 0) arrive_first<PAIR>(acc_empty(a));
             if (++a == C::ACCS) a = 0, aph ^= 1;
             if constexpr (PARTS > 1) {
-                // the MMAs are done with the stages: the sums go there
+                // where blocks on their way out would be, none of which this form has
+                static_assert(4 * TILE_M * BN <= EPI_WARPS * C::OUT, "room for a part's sums");
 #pragma unroll
                 for (int c = 0; c < CW / 8; ++c)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const uint32_t *v = &r[c / 2][i / 2][4 * (c & 1) + 2 * (i & 1)];
-                        sts64(base + C::STAGES_AT + 4 * ((quarter * 32 + lane / 4 + 8 * i) * SUMS_LD + col0 + 8 * c + 2 * (lane & 3)),
+                        sts64(base + C::OUT_AT + sum_at<BN>(quarter * 32 + lane / 4 + 8 * i, col0 + 8 * c + 2 * (lane & 3)),
                               static_cast<int>(v[0]), static_cast<int>(v[1]));
                     }
             } else {
@@ -586,7 +584,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             const long long m = worker / prm.tiles_n * TILE_M + row;
             const int n = static_cast<int>(worker % prm.tiles_n) * BN + col;
             if (m >= prm.M || n >= prm.N) continue;
-            const uint32_t at = base + C::STAGES_AT + 4 * (row * SUMS_LD + col);
+            const uint32_t at = base + C::OUT_AT + sum_at<BN>(row, col);
             float v0 = 0.0f, v1 = 0.0f;
 #pragma unroll
             for (int p = 0; p < PARTS; ++p) {
