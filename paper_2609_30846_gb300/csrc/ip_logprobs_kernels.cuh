@@ -17,7 +17,9 @@ using namespace ipr;
 
 // With a_i = scale x_i, m their maximum, s = sum exp(a_i - m), u = sum (a_i - m) exp(a_i - m):
 //   log p_t = (a_t - m) - log s,   entropy = log s - u / s,
-// both terms of the entropy >= 0, so that nothing cancels.  An a of -inf has no weight.
+// both terms of the entropy >= 0, so that nothing cancels.  An a of -inf has no weight.  Differences are taken of halves,
+// x / 2 - m / 2 by one fma, and scaled twice as much: those of logits of opposite signs can pass f32's range,
+// where `scale` brings them back.
 //
 // A row (or one of its parts) is held in registers: one pass over memory, the maximum before the
 // exponentials, so one of them an element.  A short row is a warp's, a longer one a CTA's, a longer one
@@ -223,7 +225,7 @@ struct RowOut {
         : prm(p), row(r), m(v.m), ls(logf(v.s)),
           none(!(v.m > -INFINITY && v.m < INFINITY) || v.s != v.s) {}
     __device__ __forceinline__ float nan() const { return __uint_as_float(0x7fc00000u); }
-    __device__ __forceinline__ float logp(float x) const { return none ? nan() : __fmaf_rn(x - m, prm.scale, -ls); }
+    __device__ __forceinline__ float logp(float x) const { return none ? nan() : __fmaf_rn(__fmaf_rn(x, 0.5f, -0.5f * m), 2.0f * prm.scale, -ls); }
     __device__ __forceinline__ void write(const Sums &v) const {
         prm.entropy[row] = none ? nan() : ls - 0.693147181f * (v.u / v.s);
         if (!prm.tokens) return;
@@ -253,11 +255,11 @@ __device__ __forceinline__ Two two(float a, float b) {
 }
 __device__ __forceinline__ void split(Two v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
 
-// Adds the exponentials of two elements, 2^p for p = (x - from) c, and p 2^p; p = -inf: 0.  The difference
+// Adds the exponentials of two elements, 2^p for p = (x / 2 + minus_half) c, and p 2^p; p = -inf: 0.  The difference
 // first, so that an error of p is relative to p and the largest element's is 0.
-__device__ __forceinline__ void add_exp(float x0, float x1, Two minus_from, Two c, Two &s, Two &u) {
+__device__ __forceinline__ void add_exp(float x0, float x1, Two minus_half, Two c, Two &s, Two &u) {
     Two p = two(x0, x1);
-    asm("add.rn.f32x2 %0, %0, %1;" : "+l"(p) : "l"(minus_from));
+    asm("fma.rn.f32x2 %0, %0, %1, %2;" : "+l"(p) : "l"(two(0.5f, 0.5f)), "l"(minus_half));
     asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(p) : "l"(c));
     float p0, p1, e0, e1;
     split(p, p0, p1);
@@ -268,7 +270,10 @@ __device__ __forceinline__ void add_exp(float x0, float x1, Two minus_from, Two 
     asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(u) : "l"(e), "l"(q));
 }
 
-// Joins parts' sums, the thread's being first, first + step, ...
+// log2(e) x 2 scale: what half a difference of logits is multiplied by.
+__device__ __forceinline__ float factor(float scale) { return scale * (2.0f * 1.44269504f); }
+
+// Joins parts' sums, the thread's being first, first + step, ...; c: factor(scale).
 template <int TPR, typename At>
 __device__ __forceinline__ Sums join(int parts, int first, int step, float c, At at, Slot red) {
     using G = Group<TPR>;
@@ -281,7 +286,7 @@ __device__ __forceinline__ Sums join(int parts, int first, int step, float c, At
             v.s += p.s;      // 0, or NaN
             continue;
         }
-        const float d = (p.m - v.m) * c;
+        const float d = __fmaf_rn(p.m, 0.5f, -0.5f * v.m) * c;
         float e;
         asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(d));
         v.s = __fmaf_rn(p.s, e, v.s);
@@ -351,15 +356,15 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? (U > 4 ? 4 
     for (int i = 0; i < S; ++i) most = fmaxf(most, tail[i]);
     Sums sums{value_of(G::max_u32(order_of(most), red)), 0.0f, 0.0f, 0.0f};
     // nothing but -inf (and NaN): weights of 0, or NaN
-    const float from = sums.m == -INFINITY ? 0.0f : sums.m, c = prm.scale * 1.44269504f;
-    const Two from2 = two(-from, -from), c2 = two(c, c);
+    const float from = sums.m == -INFINITY ? 0.0f : sums.m, c = factor(prm.scale);
+    const Two minus_half = two(-0.5f * from, -0.5f * from), c2 = two(c, c);
     Two s2 = two(0.0f, 0.0f), u2 = s2;
 #pragma unroll
     for (int i = 0; i < U; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; j += 2) add_exp(v[i].at(j), v[i].at(j + 1), from2, c2, s2, u2);
+        for (int j = 0; j < 8; j += 2) add_exp(v[i].at(j), v[i].at(j + 1), minus_half, c2, s2, u2);
 #pragma unroll
-    for (int i = 0; i < S; ++i) add_exp(tail[i], -INFINITY, from2, c2, s2, u2);
+    for (int i = 0; i < S; ++i) add_exp(tail[i], -INFINITY, minus_half, c2, s2, u2);
     float s0, s1, u0, u1;
     split(s2, s0, s1);
     split(u2, u0, u1);
@@ -444,7 +449,7 @@ __global__ void __launch_bounds__(256) logprob_join_kernel(const LogprobParams p
     const int t = threadIdx.x;
     const long long row = blockIdx.x;
     const float4 *parts = reinterpret_cast<const float4 *>(prm.sums) + row * prm.parts;
-    const Sums all = join<256>(prm.parts, t, 256, prm.scale * 1.44269504f, [&](int i) {
+    const Sums all = join<256>(prm.parts, t, 256, factor(prm.scale), [&](int i) {
         const float4 p = parts[i];
         return Sums{p.x, p.y, p.z, p.w};
     }, red);
