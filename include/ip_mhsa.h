@@ -467,7 +467,8 @@ int ip_linear_scaled_i8(const int8_t *x, long long ldx, const float *sx, const i
  * order [ceil(rows / 128)][ceil(d / 64)]; in them the scale of row m and block b (element / 16) is byte
  * 16 (m mod 32) + 4 ((m mod 128) / 32) + (b mod 4).  Blocks behind column d have the scale 0;
  * scales of rows behind the last are neither written nor used.  scale: f32 [rows].
- * Any r is fine in what the calls read, and any s but NaN. */
+ * In what the calls read any r is fine, and any s from 0 on but NaN (bytes 0 to 0x7e).  ip_dequantize_fp4
+ * takes negative scales too, by the bytes' sign bit; the tensor cores' scales have none, so ip_linear_fp4's must not. */
 
 /* Bytes of the block scales, 0 for an invalid shape (and for no rows). */
 size_t ip_fp4_block_bytes(long long rows, int d);

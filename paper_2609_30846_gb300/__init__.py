@@ -1127,8 +1127,9 @@ def linear_fp4(x, x_blocks, sx, w, w_blocks, sw, bias=None, *, act: int = ACT_NO
     """Product of 4-bit rows (quantize_fp4, rmsnorm_fp4) on the block-scaled tensor cores (a few rows go by
     ordinary lanes):
     out[..., n] = act(sum of the products of the values of x's and w's rows + bias[n]), codes and
-    scales exact, sums in float32.  x: uint8 [..., ceil(K / 2)] with its block scales and sx: float32
-    [...]; w: uint8 [N, ceil(K / 2)], w_blocks, sw: float32 [N] (quantize_fp4 of the weights); bias: float32 [N]
+    scales exact, sums in float32.  Block scales are from 0 on (bytes 0 to 0x7e: the tensor cores'
+    have no sign), as the writing calls give them.  x: uint8 [..., ceil(K / 2)] with its block scales and sx:
+    float32 [...]; w: uint8 [N, ceil(K / 2)], w_blocks, sw: float32 [N] (quantize_fp4 of the weights); bias: float32 [N]
     or None; act: ACT_NONE or ACT_SWISH; all CUDA tensors.  K and N may be any size; the rows of x
     and w start on multiples of 16 bytes.  Returns out: [..., N] of `dtype` (bfloat16 unless out
     gives it).  Asynchronous on `stream` (default: torch's current stream)."""

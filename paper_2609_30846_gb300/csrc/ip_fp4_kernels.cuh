@@ -424,7 +424,8 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
         }
     } else if (warp >= SCALE_WARP) {
-        // Scales to TMEM: lane l of every quarter holds those of the rows l, l + 32, l + 64, l + 96, four columns
+        // Scales to TMEM, byte by byte as they are (a sign bit, which the contract excludes, would have to be cleared
+        // here: 1 to 3 % of the large products' time): lane l of every quarter holds those of the rows l, l + 32, l + 64, l + 96, four columns
         // for each 64 elements.  A stage's slot there is free when its shared memory is: its scales
         // are fetched after the MMAs that read the ones before.
         const uint32_t at = tmem + C::SF + (static_cast<uint32_t>((warp & 3) * 32) << 16);
