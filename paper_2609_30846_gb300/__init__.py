@@ -966,8 +966,9 @@ def quantize_fp4(x, *, q=None, blocks=None, scale=None, stream=None):
     NaN or an infinity the scale NaN and codes 0.  Returns (q, blocks, scale): uint8
     [..., ceil(d / 2)] (the first code in the low nibble; a new q has rows of a multiple of 16
     bytes, as linear_fp4 reads them, so it may be a view of them), uint8
-    fp4_block_shape(rows, d) and float32 of x.shape[:-1].  Asynchronous on `stream`
-    (default: torch's current stream)."""
+    fp4_block_shape(rows, d) and float32 of x.shape[:-1].  New outputs of up to 1 MB in all may share one
+    storage: clone one that is to be kept, saved or resized by itself.
+    Asynchronous on `stream` (default: torch's current stream)."""
     if stream is None:
         r = _short.quantize_fp4(x, q, blocks, scale)
         if r is not None:
@@ -1005,8 +1006,9 @@ def rmsnorm_i8(x, weight, residual=None, *, eps: float = 1e-5, out=None, q=None,
     as quantize_rows_i8 rounds rows (the row's factor leaves the codes as they are: they are
     exactly those of h weight).  x, residual: float32, float16 or bfloat16 [..., d] CUDA
     tensors; weight: x's type [d].  Returns (q, scale, h): int8 of x's shape (a new q has rows of
-    a multiple of 16 bytes), float32 of x.shape[:-1], and h of x's type, None without a residual.  out:
-    where h goes, which may be x or residual itself.  Asynchronous on `stream`."""
+    a multiple of 16 bytes), float32 of x.shape[:-1], and h of x's type, None without a residual; new ones may share one
+    storage (quantize_fp4).  out: where h goes, which may be x or residual itself.
+    Asynchronous on `stream`."""
     if stream is None:
         r = _short.rmsnorm_i8(x, weight, residual, eps, out, q, scale)
         if r is not None:
@@ -1336,7 +1338,7 @@ def token_logprobs(logits, tokens=None, *, top: int = 0, scale: float = 1.0, out
     lowest index first of equal ones.  scale: 1 / temperature.  Returns (logprob, entropy,
     top_logprob, top_token): float32 [...] (None without tokens), float32 [...], float32 and int32
     [..., top] (None for top = 0).  A row with a NaN or +inf, or of nothing but -inf, gives NaN and
-    tokens -1.  out: such a tuple, contiguous.  workspace: a uint8 tensor of
+    tokens -1.  New outputs may share one storage (quantize_fp4).  out: such a tuple, contiguous.  workspace: a uint8 tensor of
     token_logprobs_workspace_bytes(rows, V, top).  Asynchronous on `stream` (default: torch's
     current stream)."""
     if stream is None and out is None:

@@ -121,7 +121,8 @@ at::Tensor empty(at::IntArrayRef shape, const at::Tensor &like, at::ScalarType t
 
 // A call's new outputs, taken piece by piece; like: an input, whose device is the current one.  Outputs of up to
 // TOGETHER bytes in all share one allocation, which is what they cost the host most of (a call with four of
-// them 4.8 us of a Grace core, 7.9 one by one); larger ones have their own, so that none keeps another's memory alive.
+// them 4.0 us of a Grace core, 5.1 one by one); larger ones have their own, so that none keeps more than this of
+// the others' memory alive.
 class Memory {
 public:
     static constexpr size_t TOGETHER = 1 << 20;
