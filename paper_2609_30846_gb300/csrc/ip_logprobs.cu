@@ -17,6 +17,9 @@ int launched(cudaError_t rc) {
 // Elements that U units a thread hold: all, where rows start on 16 bytes, or eight less (up to seven before a row).
 constexpr int hold(int threads, int units, bool on16 = false) { return threads * units * 8 - (on16 ? 0 : 8); }
 
+// SMs of a GB300.  A constant, so that the workspace's size needs no device.
+constexpr int SMS = 152;
+
 // Parts of a row and their elements: one while a CTA holds the row; else a cluster's, as many as come to
 // four CTAs an SM, few rows by sixteen CTAs of few elements (1 x 65536 with twenty 6.7 us by 16 CTAs, by 8 7.5) and many by those
 // whose registers the parts fill; parts that a second kernel joins for what sixteen CTAs do not hold.
@@ -30,7 +33,7 @@ Plan plan(long long rows, int V, bool on16 = false) {
     int parts = 2;
     while (parts < ipl::MAX_CLUSTER && per_of(parts) > most) parts *= 2;
     if (per_of(parts) > most) return {(V + hold(256, 4) - 1) / hold(256, 4), hold(256, 4), 0};
-    while (parts < ipl::MAX_CLUSTER && rows * parts * 2 <= 608) parts *= 2;
+    while (parts < ipl::MAX_CLUSTER && rows * parts * 2 <= 4 * SMS) parts *= 2;
     return {parts, per_of(parts), 1};
 }
 
@@ -78,9 +81,14 @@ int run(const ipl::LogprobParams &prm, bool cluster, bool on16, cudaStream_t st)
         if (rc != IP_OK) return rc;
         return launched(iph::launch_pdl(ipl::logprob_join_kernel<T>, dim3(static_cast<unsigned>(prm.rows)), dim3(256), 0, st, prm));
     }
-    // a warp's lanes hold a row of up to 1048 in four units and one element more
+    // A warp's lanes: units by powers of two, and one element more a lane where that spares twice the units (12000 bf16
+    // rows of 280 4.5 us for 4.9, 536 5.2 for 6.8, 1048 7.4 and 1049, with eight units, 12.1).  Not behind eight: the CTA's form that
+    // follows is sooner with few rows (1 x 2056 1.65 us, by a warp 1.93).
     if (prm.V <= hold(32, 1)) return launch<T, 32, 1, 0, ipl::WHOLE>(prm, st);
+    if (prm.V <= hold(32, 1) + 32) return launch<T, 32, 1, 1, ipl::WHOLE>(prm, st);
     if (prm.V <= hold(32, 2)) return launch<T, 32, 2, 0, ipl::WHOLE>(prm, st);
+    if (prm.V <= hold(32, 2) + 32) return launch<T, 32, 2, 1, ipl::WHOLE>(prm, st);
+    if (prm.V <= hold(32, 4)) return launch<T, 32, 4, 0, ipl::WHOLE>(prm, st);
     if (prm.V <= hold(32, 4) + 32) return launch<T, 32, 4, 1, ipl::WHOLE>(prm, st);
     if (prm.V <= hold(32, 8)) return launch<T, 32, 8, 0, ipl::WHOLE>(prm, st);
     if (prm.V <= hold(256, 2, on16)) return launch<T, 256, 2, 0, ipl::WHOLE>(prm, st);

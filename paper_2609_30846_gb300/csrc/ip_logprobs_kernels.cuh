@@ -300,7 +300,7 @@ enum { WHOLE = 0, CLUSTER = 1, PARTS = 2 };      // what a group holds: a row, a
 
 // TPR threads (32: four rows a CTA, or 256) hold a row or a part of one in U units of eight
 // elements a thread, the first of them `shift` elements before the row, on 16 bytes, and S more elements a thread behind
-// them (a row of 1025 would take a fifth unit for its last elements).
+// them (a row of a few more than U units hold would take twice as many for its last elements).
 template <typename T, int TPR, int U, int S, int HOLDS>
 __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? (U > 4 ? 4 : (U == 4 ? 6 : 8)) : (U > 2 ? 4 : 5)) logprob_kernel(const LogprobParams prm) {
     using G = Group<TPR>;
