@@ -53,7 +53,7 @@ struct Tile {
     static constexpr int WT = BN <= 128 ? 1 : BN / 128;      // tiles of scales of w
     static constexpr int A = TILE_M * BKB, B = BR * BKB, SA = 2048, SB = 2048 * WT;
     static constexpr int STAGE = A + B + SA + SB;
-    static constexpr int ST = BN == 64 || (BN == 128 && PAIR_) ? 6 : 5;
+    static constexpr int ST = BN == 64 ? 6 : 5;
     static constexpr int ACCS = BN == 256 ? 1 : 2;    // accumulators
     static constexpr int SF = ACCS * BN;              // first column of the scales
     static constexpr int SF_COLS = 16 + 16 * WT;      // of a stage

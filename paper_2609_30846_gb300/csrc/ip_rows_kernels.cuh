@@ -161,22 +161,15 @@ struct Raw16 {
             else h[k].zero();
         }
     }
-    template <bool VEC>
+    // p on 16 bytes, n a multiple of eight
     __device__ __forceinline__ void store(T *p, int n) const {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            if (VEC) {
-                if (8 * k < n)
+        for (int k = 0; k < 2; ++k)
+            if (8 * k < n)
 #pragma unroll
-                    for (int i = 0; i < Raw8<T>::WORDS; i += 4)
-                        *reinterpret_cast<uint4 *>(reinterpret_cast<uint32_t *>(p + 8 * k) + i) =
-                            make_uint4(h[k].w[i], h[k].w[i + 1], h[k].w[i + 2], h[k].w[i + 3]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (8 * k + j < n) p[8 * k + j] = from_f32<T>(h[k].at(j));
-            }
-        }
+                for (int i = 0; i < Raw8<T>::WORDS; i += 4)
+                    *reinterpret_cast<uint4 *>(reinterpret_cast<uint32_t *>(p + 8 * k) + i) =
+                        make_uint4(h[k].w[i], h[k].w[i + 1], h[k].w[i + 2], h[k].w[i + 3]);
     }
     __device__ __forceinline__ float at(int j) const { return h[j >> 3].at(j & 7); }
     // + r, rounded to T once (the sum of two 16-bit numbers by an instruction that rounds the exact one)
@@ -315,8 +308,8 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, rows_ctas<T, TPR, UNITS
     const T *g = static_cast<const T *>(prm.weight);
     // the sum's elements from c on, by all lanes of a warp together
     auto store_sum = [&](const Raw16<T> &h, T *sum, int c) {
-        if constexpr (VEC || !NORM) {
-            h.template store<VEC>(sum + c, d - c);
+        if constexpr (VEC) {
+            h.store(sum + c, d - c);
         } else {
             Turn<T> &own = turns[threadIdx.x >> 5];
             __syncwarp();
