@@ -296,7 +296,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     using C = Tile<BN, PAIR>;
     static_assert(PARTS == 1 || (!PAIR && ODD), "forms");
     // 256 columns are 64 registers of an output thread: its warpgroups take over what the others can
-    // spare, 4 x 96 + 2 x 48 = 6 x 80
+    // spare, 4 x 96 + 2 x 48 = 6 x 80 (ptxas, which allows for the 80, spills 44 bytes a thread)
     constexpr bool DEAL = BN == 256;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>(

@@ -83,8 +83,10 @@ __device__ __forceinline__ long long scale_at(long long row, int kc, int kcs) {
 // codes as they are, so they are z's, exactly as the definitions of the rows say, and only the
 // row's scale carries it.
 //
-// What bounds it: DRAM, and close behind it the instructions: 12000 x 1024 bf16 with residual 13.2 us, 6.5 TB/s
-// (17.5 while each element's operations were done twice).  A row stays in registers between the passes up to 16 UNITS elements a thread (a longer one is read again, from L2).
+// What bounds it: DRAM, and close behind it the instructions: 12000 x 1024 bf16 with residual 13.4-13.8 us, 6.3 TB/s, to 4 bits
+// 13.0 (17.5 while each element's operations were done twice).  f32 rows hold twice the bytes in registers: 6000 x 1024 with residual 16.1
+// us, 5.0 TB/s.  Not so where rows are short, a warp each whatever their length (12000 x 40 6.2 us, 96000 x 128 42), or not on
+// 16 bytes (6000 x 1023 bf16 16.8, x 1024 7.7; f32 25 and 16).  A row stays in registers between the passes up to 16 UNITS elements a thread (a longer one is read again, from L2).
 //
 // The squares are summed in f32.  Sums that leave the middle of its range (bf16 and f32 rows
 // beyond 2^55 or below 2^-35) are formed again from elements scaled by 2^-80 or 2^96, and the
@@ -283,7 +285,8 @@ __device__ __forceinline__ uint32_t to_fp4(const float (&z)[16], float big, Fp4R
 
 // CTAs that an SM is to hold, which bounds the registers: a row's bytes in flight are what hides DRAM's latency
 // (rows to 4 bits, us, at 6 / 8 / 10 CTAs: 12000 x 4096 f16 29.3 / 24.8 / 24.5, x 2048 21.9 / 17.4 / 15.7; norm of 12000 x
-// 1024 bf16 17.8 / 20.3 / 25.9, its registers spill).
+// 1024 bf16 17.8 / 20.3 / 25.9, its registers spill).  What is left of spills at these bounds, bytes stored a thread: none in 16-bit
+// norms up to 4096, up to 140 beyond; 16 to 112 in f32 norms of more than 2048 on 16 bytes, 28 to 712 off 16 bytes.
 template <typename T, int TPR, int UNITS, bool NORM>
 constexpr int rows_ctas() {
     constexpr bool WIDE = sizeof(T) == 4;
