@@ -72,7 +72,8 @@ struct Tile {
     static_assert(STAGE % 1024 == 0 && B % 1024 == 0 , "alignment");
 };
 
-// Waits acquire, within the CTA: the scale warps read with ordinary loads what the copies left.  A pair's arrivals on the first CTA's
+// Waits acquire, within the CTA: the scale warps read with ordinary loads what the copies left (volatile, as the waits are, so
+// that the compiler keeps their order).  A pair's arrivals on the first CTA's
 // barriers release nothing: what they report are TMEM and tiles, which only asynchronous units touch and the
 // tcgen05 fences order, and with the release of the cluster they take 0.7 us each (12000 x 16384 -> 1024: 164 us, relaxed 87).
 // Bounded wait that also ends when another role of the CTA has given up.

@@ -113,7 +113,10 @@ int64_t bytes_of(at::IntArrayRef shape, at::ScalarType type) {
 at::Tensor empty(at::IntArrayRef shape, at::IntArrayRef strides, const at::Tensor &like, at::ScalarType type, int64_t n) {
     if (!watched()) return over(allocate(static_cast<size_t>(n)), 0, shape, strides, type);
     const at::TensorOptions options = like.options().dtype(type).requires_grad(false);
-    return strides.empty() ? at::empty(shape, options) : at::empty_strided(shape, strides, options);
+    at::Tensor t = strides.empty() ? at::empty(shape, options) : at::empty_strided(shape, strides, options);
+    // memory of the device: under some dispatch modes a tensor has none, or another's
+    TORCH_CHECK(n == 0 || (t.is_cuda() && t.data_ptr() != nullptr), "no memory of the device for an output");
+    return t;
 }
 at::Tensor empty(at::IntArrayRef shape, const at::Tensor &like, at::ScalarType type) {
     return empty(shape, {}, like, type, bytes_of(shape, type));
@@ -135,10 +138,7 @@ public:
             memory_ = allocate(bytes);
             return;
         }
-        const at::Tensor buffer = at::empty({static_cast<int64_t>(bytes)}, like.options().dtype(at::kByte).requires_grad(false));
-        // memory that is there: under some dispatch modes a tensor has none
-        TORCH_CHECK(bytes == 0 || (buffer.is_cuda() && buffer.data_ptr() != nullptr), "no memory for the outputs");
-        memory_ = buffer.storage();
+        memory_ = empty({static_cast<int64_t>(bytes)}, like, at::kByte).storage();
     }
     // strides empty: contiguous; n: the bytes
     at::Tensor take(at::IntArrayRef shape, at::IntArrayRef strides, at::ScalarType type, int64_t n) {
